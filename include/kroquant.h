@@ -48,7 +48,8 @@ typedef enum {
     KQ_ERR_CUDA = 6          /* a CUDA call or launch failed (no device, bad pointer kind, ...) */
 } kq_status_t;
 
-typedef enum { KQ_OUT_F32 = 0, KQ_OUT_BF16 = 1 } kq_dtype_t;
+/* KQ_OUT_FP16 is served by the kroquant_linear_* and kroquant_norm_* calls; the others take the first two. */
+typedef enum { KQ_OUT_F32 = 0, KQ_OUT_BF16 = 1, KQ_OUT_FP16 = 2 } kq_dtype_t;
 
 /* Element type of the activations X.  The entry points without `_ex` take bf16. */
 typedef enum { KQ_X_BF16 = 0, KQ_X_FP16 = 1 } kq_xdtype_t;
@@ -336,6 +337,97 @@ kq_status_t kroquant_linear_w4a4(const void *X, kq_xdtype_t x_dtype, int64_t tok
                                  const kroquant_factors_t *f, const uint8_t *w_codes,
                                  const uint8_t *w_scales, int o, uint8_t *q_work, uint8_t *s_work,
                                  const void *add_bf16, void *out, kq_dtype_t out_dtype, void *stream);
+
+/* ---- The transformer block around the W4A4 product ---------------------------------------------
+ *
+ * kroquant_linear_mxfp4: the W4A4 product with the layer's epilogue,
+ *     acc[m][r] = sum_k a[m][k] 2^(sa[m][k/32] - 127) * b[r][k] 2^(sb[r][k/32] - 127)      (fp32)
+ *     v[m][n]   = act(acc[m][n] + bias[n])                                                  glu == 0
+ *               = act(acc[m][g(n)] + bias[g(n)]) * (acc[m][g(n)+32] + bias[g(n)+32])        glu == 1, g(n) = n/32*64 + n%32
+ *     out[m][n] = residual_scale residual[m][n] + row_scale[m] gate[m / rows_per_gate][n] v[m][n]
+ * every optional term left out where its pointer is NULL.  With glu the stored weight interleaves its rows, 32 gate rows
+ * then the 32 value rows of the same features, the last block filled up with zero rows: b has 64 ceil(N/32) rows, else N.
+ * a_codes [M][K/2], a_scales (tiled, M rows), b_codes, b_scales (tiled): as for kroquant_gemm_mxfp4, 16-byte aligned;
+ * K % 32 == 0, M <= 2^24, any N >= 1.  out: [M] rows of ld_out elements (ld_out >= N) of out_dtype (any of the three), any
+ * alignment of its element type; out may be the residual itself (same type and pitch).  Everything is held in fp32 and rounded once. */
+typedef enum { KQ_ACT_NONE = 0, KQ_ACT_RELU = 1, KQ_ACT_SILU = 2, KQ_ACT_GELU = 3 /* erf */, KQ_ACT_GELU_TANH = 4 } kq_act_t;
+
+typedef struct kq_epilogue {
+    int activation;            /* kq_act_t */
+    int glu;                   /* 0 or 1 */
+    const void *bias;          /* DEVICE [rows of b] ([experts][rows of b] in the grouped call) of bias_dtype, or NULL */
+    int bias_dtype;            /* kq_dtype_t */
+    const void *gate;          /* DEVICE, row i (N elements) at gate + i * gate_stride, of gate_dtype, or NULL */
+    int gate_dtype;
+    int64_t gate_stride;       /* elements; 0: one row for all */
+    int64_t rows_per_gate;     /* >= 1 (with a gate): row m uses gate row m / rows_per_gate */
+    const float *row_scale;    /* DEVICE [M], or NULL */
+    const void *residual;      /* DEVICE [M] rows of ld_residual elements of residual_dtype, or NULL */
+    int residual_dtype;
+    int64_t ld_residual;       /* >= N (with a residual) */
+    float residual_scale;
+} kq_epilogue_t;
+
+/* Writes the defaults: no activation, no vectors, residual_scale 1, rows_per_gate 1.  NULL is ignored. */
+void kroquant_epilogue_default(kq_epilogue_t *e);
+
+/* epilogue NULL: the defaults.  Errors: KQ_ERR_NULL, KQ_ERR_SHAPE, KQ_ERR_ALIGN, KQ_ERR_UNSUPPORTED (an unknown activation,
+ * glu or type), KQ_ERR_CUDA.  M == 0 launches nothing. */
+kq_status_t kroquant_linear_mxfp4(const uint8_t *a_codes, const uint8_t *a_scales, const uint8_t *b_codes,
+                                  const uint8_t *b_scales, int64_t M, int N, int K, const kq_epilogue_t *epilogue,
+                                  void *out, kq_dtype_t out_dtype, int64_t ld_out, void *stream);
+
+/* The same with one weight per expert (mixture of experts): rows offsets[e] .. offsets[e+1] - 1 of A, quantized once over
+ * all M rows, meet weight e.  offsets: DEVICE int32 [experts + 1], non-decreasing; groups may be empty, and rows outside
+ * [offsets[0], offsets[experts]) are not written.  Offsets are read on the device (no host synchronization) and clamped to
+ * [0, M], so that no value leads outside the buffers.  b_codes [experts][rows of b][K/2], b_scales [experts][tiled size];
+ * 1 <= experts <= 1024.  Groups need no padding and no alignment. */
+kq_status_t kroquant_linear_mxfp4_grouped(const uint8_t *a_codes, const uint8_t *a_scales, const uint8_t *b_codes,
+                                          const uint8_t *b_scales, const int32_t *offsets, int experts, int64_t M, int N,
+                                          int K, const kq_epilogue_t *epilogue, void *out, kq_dtype_t out_dtype,
+                                          int64_t ld_out, void *stream);
+
+/* Norms before and after a block, fused with its gate and residual scale.  Row t, channel c, batch b = t / rows_per_batch:
+ *     r = post(y) post_weight,   h = residual_scale x + gate_b r,   n = norm(h) weight (1 + scale_b) + shift_b
+ * post, norm: none, rms (v / sqrt(mean v^2 + eps)) or layer (v less its mean first).  x and h have stream_dtype, y and n
+ * branch_dtype: equal, or a float stream with a 16-bit branch (KQ_ERR_UNSUPPORTED otherwise).  The vectors have vec_dtype
+ * and may be NULL (factors 1, scale and shift 0).  Rows are ld_* elements apart.  y == NULL: h = residual_scale x; h == NULL: not
+ * written; post_weight needs a post norm and weight, scale and shift a norm (KQ_ERR_UNSUPPORTED); n may be NULL with norm none only.  h may be x and n may be y (same pitch).  1 <= d <= 16384, any d, any
+ * alignment of the element types (16-byte aligned rows run fastest).  fp32 inside, h enters the norm unrounded. */
+typedef enum { KQ_NORM_NONE = 0, KQ_NORM_RMS = 1, KQ_NORM_LAYER = 2 } kq_norm_t;
+
+typedef struct kq_norm_args {
+    int64_t rows;
+    int d;
+    int norm, post_norm;                 /* kq_norm_t */
+    int stream_dtype, branch_dtype, vec_dtype;   /* kq_dtype_t */
+    float residual_scale, eps;
+    int64_t rows_per_batch;              /* >= 1; batches = ceil(rows / rows_per_batch) */
+    const void *gate, *post_weight, *weight, *scale, *shift;     /* DEVICE [d], or rows at the strides below per batch */
+    int64_t gate_stride, scale_stride, shift_stride;             /* elements between batches; 0: one vector for all */
+    const void *x, *y;                   /* forward only */
+    void *h, *n;                         /* forward: out; backward: h in (as the forward wrote it), n unused */
+    int64_t ld_x, ld_y, ld_h, ld_n;
+    /* backward only */
+    const void *dn, *dh;                 /* gradients at n (branch_dtype; unused with norm none) and at h (stream_dtype, may be NULL) */
+    void *dx, *dy;                       /* stream_dtype, branch_dtype; dy unused without y.  dx may be dh, dy may be dn or y */
+    int64_t ld_dn, ld_dh, ld_dx, ld_dy;
+    /* float gradients of the vectors, NULL where not wanted.  Per batch ([batches][d]) where the vector's stride is not
+     * 0, else [d], summed over all rows. */
+    float *dgate, *dpost_weight, *dweight, *dscale, *dshift;
+} kq_norm_args_t;
+
+/* Writes the defaults: zeros, residual_scale 1, eps 1e-6, rows_per_batch 1.  NULL is ignored. */
+void kroquant_norm_args_default(kq_norm_args_t *a);
+
+kq_status_t kroquant_norm_residual(const kq_norm_args_t *args, void *stream);
+
+/* Backward pass: dx, dy and the vectors' gradients from dn, dh, h and y (statistics are recomputed).  scratch: DEVICE,
+ * 16-byte aligned, at least kroquant_norm_residual_grad_scratch_bytes(args) bytes (0 when no vector gradient is
+ * wanted: then it may be NULL).  Deterministic: sums over rows are added in a fixed order.  rows == 0 writes zeros to the
+ * vector gradients of [d]. */
+int64_t kroquant_norm_residual_grad_scratch_bytes(const kq_norm_args_t *args);
+kq_status_t kroquant_norm_residual_grad(const kq_norm_args_t *args, void *scratch, int64_t scratch_bytes, void *stream);
 
 /* ---- Layer-wise calibration of the transform (Section 3.3; set-up of Appendix D) ----
  *

@@ -30,6 +30,8 @@ EXPORTS = [
     "kroquant_tuning_default", "kroquant_quantize_tuned", "kroquant_quantize_dual_tuned", "kroquant_transform_f32_tuned",
     "kroquant_scale_quantize_tuned", "kroquant_mxfp4_quantize_tuned", "kroquant_fwht_quantize_tuned", "kroquant_debug_set_timeline", "kroquant_debug_withhold_arrival", "kroquant_debug_boundary_probe", "kroquant_launch_count", "kroquant_last_device_error",
     "kroquant_status_string",
+    "kroquant_epilogue_default", "kroquant_linear_mxfp4", "kroquant_linear_mxfp4_grouped", "kroquant_norm_args_default",
+    "kroquant_norm_residual", "kroquant_norm_residual_grad", "kroquant_norm_residual_grad_scratch_bytes",
     "kroquant_calib_create", "kroquant_calib_destroy", "kroquant_calib_set_theta", "kroquant_calib_get_theta",
     "kroquant_calib_set_lambdas", "kroquant_calib_get_lambdas", "kroquant_calib_get_factors",
     "kroquant_calib_loss_grad", "kroquant_calib_run",
@@ -114,6 +116,16 @@ def load_library() -> C.CDLL:
     L.kroquant_gemm_mxfp4.argtypes = [vp, vp, vp, vp, i64, i32, i32, vp, vp, i32, vp]
     L.kroquant_gemm_bf16.argtypes = [vp, vp, i64, i32, i32, vp, vp, i32, vp]
     L.kroquant_linear_w4a4.argtypes = [vp, i32, i64, i32, vp, vp, vp, i32, vp, vp, vp, vp, i32, vp]
+    L.kroquant_epilogue_default.argtypes = [vp]
+    L.kroquant_epilogue_default.restype = None
+    L.kroquant_linear_mxfp4.argtypes = [vp, vp, vp, vp, i64, i32, i32, vp, vp, i32, i64, vp]
+    L.kroquant_linear_mxfp4_grouped.argtypes = [vp, vp, vp, vp, vp, i32, i64, i32, i32, vp, vp, i32, i64, vp]
+    L.kroquant_norm_args_default.argtypes = [vp]
+    L.kroquant_norm_args_default.restype = None
+    L.kroquant_norm_residual.argtypes = [vp, vp]
+    L.kroquant_norm_residual_grad_scratch_bytes.argtypes = [vp]
+    L.kroquant_norm_residual_grad_scratch_bytes.restype = i64
+    L.kroquant_norm_residual_grad.argtypes = [vp, vp, i64, vp]
     _lib = L
     return L
 
@@ -523,6 +535,303 @@ class LinearW4A4:
             _ptr(q), _ptr(s), _ptr(add), _ptr(out), 1 if out.dtype == torch.bfloat16 else 0, _stream(stream)),
             "kroquant_linear_w4a4")
         return out
+
+
+# ---- the transformer block around the W4A4 product -----------------------------------------------------------------
+ACTIVATIONS = {"none": 0, "relu": 1, "silu": 2, "gelu": 3, "gelu_tanh": 4}
+NORMS = {"none": 0, "rms": 1, "layer": 2}
+_DTYPES = {torch.float32: 0, torch.bfloat16: 1, torch.float16: 2}
+
+
+class _Epilogue(C.Structure):
+    """kq_epilogue_t (include/kroquant.h)."""
+    _fields_ = [("activation", C.c_int), ("glu", C.c_int), ("bias", C.c_void_p), ("bias_dtype", C.c_int), ("gate", C.c_void_p),
+                ("gate_dtype", C.c_int), ("gate_stride", C.c_int64), ("rows_per_gate", C.c_int64), ("row_scale", C.c_void_p),
+                ("residual", C.c_void_p), ("residual_dtype", C.c_int), ("ld_residual", C.c_int64), ("residual_scale", C.c_float)]
+
+
+class _NormArgs(C.Structure):
+    """kq_norm_args_t (include/kroquant.h)."""
+    _fields_ = ([("rows", C.c_int64)] + [(n, C.c_int) for n in ("d", "norm", "post_norm", "stream_dtype", "branch_dtype", "vec_dtype")] +
+                [("residual_scale", C.c_float), ("eps", C.c_float), ("rows_per_batch", C.c_int64)] +
+                [(n, C.c_void_p) for n in ("gate", "post_weight", "weight", "scale", "shift")] +
+                [(n, C.c_int64) for n in ("gate_stride", "scale_stride", "shift_stride")] +
+                [(n, C.c_void_p) for n in ("x", "y", "h", "n")] + [(n, C.c_int64) for n in ("ld_x", "ld_y", "ld_h", "ld_n")] +
+                [(n, C.c_void_p) for n in ("dn", "dh", "dx", "dy")] + [(n, C.c_int64) for n in ("ld_dn", "ld_dh", "ld_dx", "ld_dy")] +
+                [(n, C.c_void_p) for n in ("dgate", "dpost_weight", "dweight", "dscale", "dshift")])
+
+
+def interleave_glu(W_gate: torch.Tensor, W_value: torch.Tensor) -> torch.Tensor:
+    """[F, K] gate and value weights (or [F] biases) -> the rows a gated layer stores: 32 gate rows, their 32 value rows, ...,
+    the last block filled up with zeros; [64 * ceil(F / 32), K].  Quantize the result as the layer's weight."""
+    if W_gate.shape != W_value.shape or W_gate.dtype != W_value.dtype:
+        raise ValueError("W_gate and W_value must have the same shape and dtype")
+    F, blocks = W_gate.shape[0], (W_gate.shape[0] + 31) // 32
+    out = W_gate.new_zeros((2, blocks * 32) + tuple(W_gate.shape[1:]))
+    out[0, :F], out[1, :F] = W_gate, W_value
+    return out.view(2, blocks, 32, -1).transpose(0, 1).reshape((blocks * 64,) + tuple(W_gate.shape[1:]))
+
+
+def _rows2d(t: torch.Tensor, rows: int, cols: int, what: str) -> int:
+    """Pitch of a [rows, cols] CUDA tensor with contiguous rows."""
+    if t.dim() != 2 or t.shape[0] != rows or t.shape[1] != cols or t.dtype not in _DTYPES or not t.is_cuda or \
+            (cols > 1 and t.stride(1) != 1) or (rows > 1 and t.stride(0) < cols):
+        raise ValueError(f"{what} must be a CUDA float32, bfloat16 or float16 tensor [{rows}, {cols}] with contiguous rows that do not overlap")
+    return t.stride(0) if rows > 1 else max(t.stride(0), cols)
+
+
+def _operand(codes: torch.Tensor, scales: torch.Tensor, what: str) -> None:
+    if codes.dtype != torch.uint8 or scales.dtype != torch.uint8 or not codes.is_cuda or not scales.is_cuda or \
+            not codes.is_contiguous() or not scales.is_contiguous():
+        raise ValueError(f"codes and scales of {what} must be contiguous CUDA uint8 tensors")
+
+
+def _linear(a_codes, a_scales, b_codes, b_scales, offsets, features, bias, activation, glu, gate, rows_per_gate, row_scale,
+            residual, residual_scale, out, out_dtype, stream, where):
+    grouped = offsets is not None
+    _operand(a_codes, a_scales, "A")
+    _operand(b_codes, b_scales, "B")
+    if a_codes.dim() != 2 or b_codes.dim() != (3 if grouped else 2) or b_codes.shape[-1] != a_codes.shape[1]:
+        raise ValueError("A is [M, K/2] codes, B [rows, K/2] ([experts, rows, K/2] in the grouped call) with the same K")
+    M, half = a_codes.shape
+    K, R = 2 * half, b_codes.shape[-2]
+    experts = b_codes.shape[0] if grouped else 1
+    if a_scales.numel() != tiled_scale_bytes(M, K) or b_scales.numel() != experts * tiled_scale_bytes(R, K):
+        raise ValueError("scales must be in the tiled layout (tiled_scale_bytes(rows, K) bytes, per expert for B)")
+    N = (R // 2 if glu else R) if features is None else int(features)
+    if (glu and R != 64 * ((N + 31) // 32)) or (not glu and R != N):
+        raise ValueError("B must have `features` rows, or 64 * ceil(features / 32) interleaved rows with glu")
+    if activation not in ACTIVATIONS:
+        raise ValueError(f"activation must be one of {sorted(ACTIVATIONS)}")
+    device = a_codes.device
+    e = _Epilogue()
+    e.activation, e.glu, e.rows_per_gate, e.residual_scale = ACTIVATIONS[activation], 1 if glu else 0, 1, residual_scale
+    if bias is not None:
+        if tuple(bias.shape) != ((experts, R) if grouped else (R,)) or bias.dtype not in _DTYPES or not bias.is_cuda or not bias.is_contiguous():
+            raise ValueError("bias must be a contiguous CUDA floating tensor with one entry per row of B")
+        e.bias, e.bias_dtype = bias.data_ptr(), _DTYPES[bias.dtype]
+    if gate is not None:
+        rows = 1 if gate.dim() == 1 else gate.shape[0]
+        if gate.dim() not in (1, 2) or gate.shape[-1] != N or gate.dtype not in _DTYPES or not gate.is_cuda or \
+                (N > 1 and gate.stride(-1) != 1) or (rows > 1 and gate.stride(0) < N):
+            raise ValueError("gate must be a CUDA floating tensor [N] or [batches, N] with contiguous rows")
+        if rows_per_gate is None:
+            if rows < 1 or M % rows:
+                raise ValueError("M is not a multiple of the gate's rows: pass rows_per_gate")
+            rows_per_gate = max(M // rows, 1)
+        if rows_per_gate < 1 or rows * rows_per_gate < M:
+            raise ValueError("gate has too few rows for rows_per_gate")
+        e.gate, e.gate_dtype, e.gate_stride, e.rows_per_gate = gate.data_ptr(), _DTYPES[gate.dtype], gate.stride(0) if rows > 1 else 0, rows_per_gate
+    if row_scale is not None:
+        if tuple(row_scale.shape) != (M,) or row_scale.dtype != torch.float32 or not row_scale.is_cuda or not row_scale.is_contiguous():
+            raise ValueError("row_scale must be a contiguous CUDA float32 tensor [M]")
+        e.row_scale = row_scale.data_ptr()
+    if residual is not None:
+        e.ld_residual = _rows2d(residual, M, N, "residual")
+        e.residual, e.residual_dtype = residual.data_ptr(), _DTYPES[residual.dtype]
+    if out is None:
+        out = torch.empty((M, N), dtype=out_dtype, device=device)
+        ld_out = N
+    else:
+        ld_out = _rows2d(out, M, N, "out")
+    if out.dtype not in _DTYPES:
+        raise ValueError("out_dtype must be float32, bfloat16 or float16")
+    if grouped:
+        if offsets.dtype != torch.int32 or tuple(offsets.shape) != (experts + 1,) or not offsets.is_cuda or not offsets.is_contiguous():
+            raise ValueError("offsets must be a contiguous CUDA int32 tensor [experts + 1]")
+        rc = load_library().kroquant_linear_mxfp4_grouped(
+            a_codes.data_ptr(), a_scales.data_ptr(), b_codes.data_ptr(), b_scales.data_ptr(), offsets.data_ptr(), experts, M, N, K,
+            C.addressof(e), out.data_ptr(), _DTYPES[out.dtype], ld_out, _stream(stream))
+    else:
+        rc = load_library().kroquant_linear_mxfp4(
+            a_codes.data_ptr(), a_scales.data_ptr(), b_codes.data_ptr(), b_scales.data_ptr(), M, N, K, C.addressof(e), out.data_ptr(),
+            _DTYPES[out.dtype], ld_out, _stream(stream))
+    _check(rc, where)
+    return out
+
+
+def kroquant_linear_mxfp4(a_codes: torch.Tensor, a_scales: torch.Tensor, b_codes: torch.Tensor, b_scales: torch.Tensor, *,
+                          features: Optional[int] = None, bias: Optional[torch.Tensor] = None, activation: str = "none",
+                          glu: bool = False, gate: Optional[torch.Tensor] = None, rows_per_gate: Optional[int] = None,
+                          row_scale: Optional[torch.Tensor] = None, residual: Optional[torch.Tensor] = None,
+                          residual_scale: float = 1.0, out: Optional[torch.Tensor] = None, out_dtype=torch.bfloat16,
+                          stream=None) -> torch.Tensor:
+    """The W4A4 product with the layer's epilogue:
+
+        out = residual_scale * residual + row_scale[:, None] * gate * act(A B^T + bias)
+
+    A, B: codes and tiled scales as the quantizer writes them (``scale_layout="tiled"``).  With ``glu`` B's rows (and
+    bias's entries) are interleaved by :func:`interleave_glu` and v = act(A B_g^T + bias_g) * (A B_v^T + bias_v);
+    ``features`` then gives the number of output columns (default: half of B's rows).  activation: none, relu, silu,
+    gelu (erf) or gelu_tanh; gate [N] or [batches, N] (row m uses row m // rows_per_gate; default: M / batches); row_scale
+    float32 [M].  bias, gate, residual and out may each be float32, bfloat16 or float16; residual and out may have a row
+    pitch, and out may be the residual.  fp32 inside, rounded once."""
+    return _linear(a_codes, a_scales, b_codes, b_scales, None, features, bias, activation, glu, gate, rows_per_gate, row_scale,
+                   residual, residual_scale, out, out_dtype, stream, "kroquant_linear_mxfp4")
+
+
+def kroquant_linear_mxfp4_grouped(a_codes: torch.Tensor, a_scales: torch.Tensor, b_codes: torch.Tensor, b_scales: torch.Tensor,
+                                  offsets: torch.Tensor, *, features: Optional[int] = None, bias: Optional[torch.Tensor] = None,
+                                  activation: str = "none", glu: bool = False, row_scale: Optional[torch.Tensor] = None,
+                                  residual: Optional[torch.Tensor] = None, residual_scale: float = 1.0,
+                                  out: Optional[torch.Tensor] = None, out_dtype=torch.bfloat16, stream=None) -> torch.Tensor:
+    """:func:`kroquant_linear_mxfp4` with one weight per expert: rows offsets[e] .. offsets[e + 1] - 1 of A (sorted by expert,
+    quantized once, not padded) meet b_codes[e] ([experts, rows, K/2]; b_scales: the experts' tiled buffers one after
+    another).  offsets: CUDA int32 [experts + 1], read on the device; groups may be empty.  Rows outside
+    [offsets[0], offsets[-1]) are not written.  bias: [experts, rows of B]; row_scale: the router's weight of each row."""
+    if offsets is None:
+        raise ValueError("offsets must be a contiguous CUDA int32 tensor [experts + 1]")
+    return _linear(a_codes, a_scales, b_codes, b_scales, offsets, features, bias, activation, glu, None, None, row_scale, residual,
+                   residual_scale, out, out_dtype, stream, "kroquant_linear_mxfp4_grouped")
+
+
+def _norm_vectors(a: "_NormArgs", rows: int, d: int, rows_per_batch, vectors) -> int:
+    """Checks the parameter vectors, fills their pointers and strides; -> batches."""
+    batches, dtype = 1, None
+    for name, v, batched in vectors:
+        if v is None:
+            continue
+        if v.dim() not in ((1, 2) if batched else (1,)) or v.shape[-1] != d or v.dtype not in _DTYPES or not v.is_cuda or \
+                (d > 1 and v.stride(-1) != 1) or (v.dim() == 2 and v.shape[0] > 1 and v.stride(0) < d):
+            raise ValueError(f"{name} must be a CUDA floating tensor [d]" + (" or [batches, d] with contiguous rows" if batched else ""))
+        if dtype is None:
+            dtype = v.dtype
+        elif v.dtype != dtype:
+            raise ValueError("gate, post_weight, weight, scale and shift must share a dtype")
+        setattr(a, name, v.data_ptr())
+        if v.dim() == 2:
+            if batches not in (1, v.shape[0]) and v.shape[0] != 1:
+                raise ValueError("batched vectors must agree on the number of batches")
+            batches = max(batches, v.shape[0])
+            # a gradient keeps the shape of its vector, so one row of [1, d] counts as one vector for all rows
+            setattr(a, name + "_stride", v.stride(0) if v.shape[0] > 1 else 0)
+    a.vec_dtype = _DTYPES[dtype] if dtype is not None else 0
+    if batches == 1:
+        rows_per_batch = max(rows, 1)
+    elif rows_per_batch is None:
+        if rows % batches:
+            raise ValueError("rows is not a multiple of the batches: pass rows_per_batch")
+        rows_per_batch = max(rows // batches, 1)
+    if rows_per_batch < 1 or (rows + rows_per_batch - 1) // rows_per_batch > batches:
+        raise ValueError("the batched vectors have too few rows for rows_per_batch")
+    a.rows_per_batch = rows_per_batch
+    return batches
+
+
+def _norm_kinds(a: "_NormArgs", norm: str, post_norm: str) -> None:
+    if norm not in NORMS or post_norm not in NORMS:
+        raise ValueError(f"norm and post_norm must be one of {sorted(NORMS)}")
+    a.norm, a.post_norm = NORMS[norm], NORMS[post_norm]
+
+
+def kroquant_norm_residual(x: torch.Tensor, y: Optional[torch.Tensor] = None, *, gate: Optional[torch.Tensor] = None,
+                           post_weight: Optional[torch.Tensor] = None, residual_scale: float = 1.0,
+                           weight: Optional[torch.Tensor] = None, scale: Optional[torch.Tensor] = None,
+                           shift: Optional[torch.Tensor] = None, norm: str = "rms", post_norm: str = "none", eps: float = 1e-6,
+                           rows_per_batch: Optional[int] = None, h_out: Optional[torch.Tensor] = None,
+                           n_out: Optional[torch.Tensor] = None, branch_dtype: Optional[torch.dtype] = None, stream=None):
+    """The step between two sub-blocks, one pass: -> (h, n) with
+
+        h = residual_scale * x + gate * post_norm(y) * post_weight
+        n = norm(h) * weight * (1 + scale) + shift
+
+    x [rows, d] is the residual stream, y [rows, d] the branch (None: h = residual_scale * x, which is x itself for 1.0
+    and is then not written unless h_out is given).  norm / post_norm: "none", "rms" or "layer".  gate, scale, shift:
+    [d] or [batches, d] (row t uses row t // rows_per_batch); weight, post_weight: [d]; one dtype for all five.  x and h
+    share a dtype, y and n share one (``branch_dtype`` without y): equal, or a float32 stream with a 16-bit branch.
+    norm "none": n is None.  h_out may be x and n_out may be y."""
+    if x.dim() != 2:
+        raise ValueError("x must be [rows, d]")
+    rows, d = x.shape
+    a = _NormArgs()
+    _norm_kinds(a, norm, post_norm)
+    a.rows, a.d, a.residual_scale, a.eps = rows, d, residual_scale, eps
+    a.x, a.ld_x, a.stream_dtype = x.data_ptr(), _rows2d(x, rows, d, "x"), _DTYPES[x.dtype]
+    if y is not None:
+        a.y, a.ld_y = y.data_ptr(), _rows2d(y, rows, d, "y")
+        branch_dtype = y.dtype
+    elif branch_dtype is None:
+        branch_dtype = x.dtype
+    if branch_dtype not in _DTYPES:
+        raise ValueError("branch_dtype must be float32, bfloat16 or float16")
+    a.branch_dtype = _DTYPES[branch_dtype]
+    _norm_vectors(a, rows, d, rows_per_batch, (("gate", gate, True), ("post_weight", post_weight, False), ("weight", weight, False),
+                                               ("scale", scale, True), ("shift", shift, True)))
+    h, n = h_out, n_out
+    if h is None and (y is not None or residual_scale != 1.0 or norm == "none"):
+        h = torch.empty((rows, d), dtype=x.dtype, device=x.device)
+    if h is not None:
+        a.ld_h = _rows2d(h, rows, d, "h_out")
+        if h.dtype != x.dtype:
+            raise ValueError("h_out must have x's dtype")
+        a.h = h.data_ptr()
+    if norm == "none":
+        n = None
+    else:
+        if n is None:
+            n = torch.empty((rows, d), dtype=branch_dtype, device=x.device)
+        a.ld_n = _rows2d(n, rows, d, "n_out")
+        if n.dtype != branch_dtype:
+            raise ValueError("n_out must have the branch's dtype")
+        a.n = n.data_ptr()
+    _check(load_library().kroquant_norm_residual(C.addressof(a), _stream(stream)), "kroquant_norm_residual")
+    return (x if h is None else h), n
+
+
+def kroquant_norm_residual_grad(dn: Optional[torch.Tensor], h: torch.Tensor, *, dh: Optional[torch.Tensor] = None,
+                                y: Optional[torch.Tensor] = None, gate: Optional[torch.Tensor] = None,
+                                post_weight: Optional[torch.Tensor] = None, residual_scale: float = 1.0,
+                                weight: Optional[torch.Tensor] = None, scale: Optional[torch.Tensor] = None,
+                                shift: Optional[torch.Tensor] = None, norm: str = "rms", post_norm: str = "none",
+                                eps: float = 1e-6, rows_per_batch: Optional[int] = None, stream=None) -> dict:
+    """Backward pass of :func:`kroquant_norm_residual` (same vectors and settings): dn, dh = gradients at n and h (dh None:
+    zero; dn None with norm "none"), h as the forward wrote it, y the branch.  -> dict with dx, with dy if y is given, and
+    a float32 gradient ("dgate", "dpost_weight", "dweight", "dscale", "dshift") in the shape of every vector given."""
+    if h.dim() != 2:
+        raise ValueError("h must be [rows, d]")
+    rows, d = h.shape
+    a = _NormArgs()
+    _norm_kinds(a, norm, post_norm)
+    a.rows, a.d, a.residual_scale, a.eps = rows, d, residual_scale, eps
+    a.h, a.ld_h, a.stream_dtype = h.data_ptr(), _rows2d(h, rows, d, "h"), _DTYPES[h.dtype]
+    if (dn is None) != (norm == "none"):
+        raise ValueError("dn goes with a norm")
+    branch_dtype = dn.dtype if dn is not None else y.dtype if y is not None else h.dtype
+    if dn is not None:
+        a.dn, a.ld_dn = dn.data_ptr(), _rows2d(dn, rows, d, "dn")
+    if dh is not None:
+        a.dh, a.ld_dh = dh.data_ptr(), _rows2d(dh, rows, d, "dh")
+        if dh.dtype != h.dtype:
+            raise ValueError("dh must have h's dtype")
+    if y is not None:
+        a.y, a.ld_y = y.data_ptr(), _rows2d(y, rows, d, "y")
+        if y.dtype != branch_dtype:
+            raise ValueError("y and dn must share a dtype")
+    elif gate is not None or (post_weight is not None and post_norm != "none"):
+        raise ValueError("gate and post_weight act on the branch: y is needed")
+    if branch_dtype not in _DTYPES:
+        raise ValueError("dn and y must be float32, bfloat16 or float16")
+    a.branch_dtype = _DTYPES[branch_dtype]
+    vectors = (("gate", gate, True), ("post_weight", post_weight, False), ("weight", weight, False), ("scale", scale, True),
+               ("shift", shift, True))
+    _norm_vectors(a, rows, d, rows_per_batch, vectors)
+    out = {"dx": torch.empty((rows, d), dtype=h.dtype, device=h.device)}
+    a.dx, a.ld_dx = out["dx"].data_ptr(), d
+    if y is not None:
+        out["dy"] = torch.empty((rows, d), dtype=branch_dtype, device=h.device)
+        a.dy, a.ld_dy = out["dy"].data_ptr(), d
+    covered = (rows + a.rows_per_batch - 1) // a.rows_per_batch          # batches that have rows: the kernel writes those
+    for name, v, _ in vectors:
+        if v is not None:
+            short = v.dim() == 2 and v.shape[0] > covered
+            out["d" + name] = g = (torch.zeros if short else torch.empty)(v.shape, dtype=torch.float32, device=h.device)
+            setattr(a, "d" + name, g.data_ptr())
+    L = load_library()
+    nbytes = int(L.kroquant_norm_residual_grad_scratch_bytes(C.addressof(a)))
+    scratch = torch.empty(nbytes, dtype=torch.uint8, device=h.device) if nbytes else None
+    _check(L.kroquant_norm_residual_grad(C.addressof(a), scratch.data_ptr() if nbytes else None, nbytes, _stream(stream)),
+           "kroquant_norm_residual_grad")
+    return out
 
 
 _GEMM_PAIR = True

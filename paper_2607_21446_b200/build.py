@@ -14,7 +14,7 @@ CSRC = os.path.join(PKG, "csrc")
 LIB = os.path.join(PKG, "libkroquant.so")
 SOURCES = [os.path.join(CSRC, "kroquant_api.cu")]
 HEADERS = [os.path.join(CSRC, n) for n in ("kq_common.cuh", "kq_stream.cuh", "kq_umma.cuh", "kq_gemm.cuh", "kq_gemm2.cuh", "kq_gemm_fp4.cuh", "kq_gemm_fp4_pair.cuh", "kq_calib.cuh",
-                                               "kroquant_calib_api.cuh")] + [
+                                               "kq_norm.cuh", "kq_linear.cuh", "kroquant_calib_api.cuh", "kroquant_block_api.cuh")] + [
     os.path.join(os.path.dirname(PKG), "include", "kroquant.h")]
 
 NVCC_FLAGS = [

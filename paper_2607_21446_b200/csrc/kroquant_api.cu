@@ -8,6 +8,7 @@
 #include <cstring>
 #include <mutex>
 #include <new>
+#include <utility>
 #include <vector>
 
 #include <cuda.h>
@@ -1163,6 +1164,7 @@ const char* kroquant_status_string(kq_status_t s) {
 }  // extern "C"
 
 #include "kroquant_calib_api.cuh"
+#include "kroquant_block_api.cuh"
 
 // ---- block gradient without any allocation -------------------------------------------------
 // Same kernels as kroquant_block_grad; the partial sums go to a buffer that is part of the
