@@ -102,9 +102,6 @@ __device__ __forceinline__ void store_typed(void* p, int type, int64_t at, float
     else if (type == kTypeF16) static_cast<__half*>(p)[at] = __float2half_rn(v);
     else static_cast<__nv_bfloat16*>(p)[at] = __float2bfloat16_rn(v);
 }
-__device__ __forceinline__ float vec_entry(const NormVec& p, int64_t which, int at, float none) {
-    return p.ptr ? load_typed(p.ptr, p.type, which * p.stride + at) : none;
-}
 
 // One output element from its accumulator(s): feature n, weight row r (the gate row; its value row is r + 32).
 template <bool GLU>
@@ -213,11 +210,11 @@ __device__ __forceinline__ void epilogue_row(const LinearEpilogue& p, float (&v)
 #pragma unroll
         for (int q = 0; q < 4; ++q) {
             float b[8];
-            load_param(p.bias, expert, r + 8 * q, 8, true, 0.f, b);
+            load_param(p.bias, expert, r + 8 * q, 8, true, 1, 0.f, b);
 #pragma unroll
             for (int i = 0; i < 8; ++i) v[8 * q + i] += b[i];
             if (GLU) {
-                load_param(p.bias, expert, r + 32 + 8 * q, 8, true, 0.f, b);
+                load_param(p.bias, expert, r + 32 + 8 * q, 8, true, 1, 0.f, b);
 #pragma unroll
                 for (int i = 0; i < 8; ++i) u[8 * q + i] += b[i];
             }
@@ -233,7 +230,7 @@ __device__ __forceinline__ void epilogue_row(const LinearEpilogue& p, float (&v)
 #pragma unroll
         for (int q = 0; q < 4; ++q) {
             float b[8];
-            load_param(p.gate, which, col + 8 * q, 8, true, 1.f, b);
+            load_param(p.gate, which, col + 8 * q, 8, true, 1, 1.f, b);
 #pragma unroll
             for (int i = 0; i < 8; ++i) v[8 * q + i] *= b[i];
         }

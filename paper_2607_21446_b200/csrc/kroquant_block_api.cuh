@@ -192,24 +192,20 @@ kq_status_t run_linear(const uint8_t* a_codes, const uint8_t* a_scales, const ui
 
 struct NormShape {
     int threads, rows;          // block: threads of a row, rows of a CTA
-    int vpt;                    // 8-channel groups per thread: 1, 2 or 4
+    int vpt;                    // 8-channel groups per thread
 };
-// One warp per row while a lane's share is at most max_warp groups, else one CTA per row with two groups per thread (four
-// where more than 1024 threads, backward 512, would be needed).
-NormShape norm_shape(int d, int max_warp, int max_threads) {
+// Forward: one warp per row while a lane's share is at most four groups (d <= 1024), else one CTA per row with two.
+NormShape forward_shape(int d) {
     const int groups = (d + 7) / 8;
-    NormShape s;
-    if (groups <= 32 * max_warp) {
-        const int per = (groups + 31) / 32;
-        s.threads = 32;
-        s.rows = 8;
-        s.vpt = per <= 1 ? 1 : (per <= 2 ? 2 : 4);
-        return s;
-    }
-    s.rows = 1;
-    s.vpt = (groups + 1) / 2 <= max_threads ? 2 : 4;
-    s.threads = ((groups + s.vpt - 1) / s.vpt + 31) / 32 * 32;
-    return s;
+    if (groups <= 128) return {32, 8, groups <= 32 ? 1 : (groups <= 64 ? 2 : 4)};
+    return {((groups + 1) / 2 + 31) / 32 * 32, 1, 2};
+}
+// Backward: one warp per row for d <= 512, else one CTA per row: two groups per thread up to d = 9216 (576 threads), four above.
+NormShape backward_shape(int d) {
+    const int groups = (d + 7) / 8;
+    if (groups <= 64) return {32, 8, groups <= 32 ? 1 : 2};
+    const int vpt = groups <= 2 * 576 ? 2 : 4;
+    return {((groups + vpt - 1) / vpt + 31) / 32 * 32, 1, vpt};
 }
 bool vec_row(const void* p, int64_t ld, int type) { return rows_aligned(p, ld, type, 16); }
 
@@ -245,7 +241,7 @@ bool norm_vectors_vec(const kq_norm_args_t& a) {
 
 template <typename S, typename Y>
 kq_status_t launch_norm_forward(const kq::NormForward& p, cudaStream_t st) {
-    const NormShape s = norm_shape(p.d, 4, 1024);
+    const NormShape s = forward_shape(p.d);
     cudaLaunchConfig_t cfg;
     cudaLaunchAttribute attr[2];
     launch_config(&cfg, attr, dim3((unsigned)((p.rows + s.rows - 1) / s.rows)), dim3((unsigned)s.threads, (unsigned)s.rows), 0, 1, st);
@@ -256,17 +252,45 @@ kq_status_t launch_norm_forward(const kq::NormForward& p, cudaStream_t st) {
     }
 }
 
-// Workers of the backward pass: as many as run at once, and no more than there are rows.
+// Workers of the backward pass: as many as run at once, and no more than there are rows; the staged kernel's use of
+// shared memory.
 struct NormWorkers {
     NormShape shape;
     int64_t workers, rows_per_worker, batches;
+    int smem;                   // dynamic shared memory (staged kernel)
 };
-NormWorkers norm_workers(const kq_norm_args_t& a, int sms) {
-    NormWorkers w;
-    w.shape = norm_shape(a.d, 2, 512);
-    const int per_sm = w.shape.threads >= 512 ? 1 : 512 / (w.shape.threads * w.shape.rows);
-    int64_t most = (int64_t)sms * (per_sm < 1 ? 1 : per_sm) * w.shape.rows;
-    if (most < 1) most = 1;
+constexpr int kSmemPerSm = 228 * 1024, kSmemPerCta = 227 * 1024;
+
+NormWorkers norm_workers(const kq_norm_args_t& a, int sms, kq::NormBackward* p) {
+    NormWorkers w = {};
+    w.shape = backward_shape(a.d);
+    int per_sm = 8;             // 8 CTAs of 256 threads: two warps per scheduler and more hide the loads of a warp's row
+    if (w.shape.rows == 1) {
+        // registers let 576 (two groups per thread) or 512 threads run on an SM
+        per_sm = (w.shape.vpt == 2 ? 576 : 512) / w.shape.threads;
+        if (per_sm > 8) per_sm = 8;
+        const int ss = type_size(a.stream_dtype), sb = type_size(a.branch_dtype), padded = (a.d + 7) / 8 * 8;
+        const bool post = a.y && a.post_norm != KQ_NORM_NONE, dn = a.norm != KQ_NORM_NONE;
+        // the second phase's values take the place of h and dh: both rows must exist
+        // (a 32-bit stream has the room in h's row alone); four 32-bit rows above d = 14000 do not fit, then dh, which is
+        // read once, is not staged
+        const int room = (per_sm == 1 ? kSmemPerCta : kSmemPerSm / per_sm - 1024) - kq::kNormHeadBytes;
+        const bool fits = padded * (2 * ss + (dn ? sb : 0) + (a.y ? sb : 0)) <= room;
+        const int stage_dh = a.dh && fits ? 1 : 0, rows_s = stage_dh || (post && ss == 2) ? 2 : 1;
+        const int off_dh = padded * ss, off_dn = off_dh * rows_s;
+        const int off_y = off_dn + (dn ? padded * sb : 0), stage = off_y + (a.y ? padded * sb : 0);
+        int cache_m = dn && (a.weight || a.scale) ? 1 : 0, cache_gate = a.y && a.gate ? 1 : 0, cache_post = post && a.post_weight ? 1 : 0;
+        int params = 4 * padded * (cache_m + cache_gate + cache_post);
+        if (params + 2 * stage > room) params = cache_m = cache_gate = cache_post = 0;    // rows in flight come first
+        int stages = (room - params) / stage;
+        stages = stages < 1 ? 1 : (stages > kq::kNormStageMax ? kq::kNormStageMax : stages);
+        w.smem = kq::kNormHeadBytes + params + stages * stage;
+        if (p) {
+            p->stages = stages; p->stage_bytes = stage; p->stage_dh = stage_dh; p->off_dh = off_dh; p->off_dn = off_dn; p->off_y = off_y;
+            p->cache_m = cache_m; p->cache_gate = cache_gate; p->cache_post = cache_post;
+        }
+    }
+    const int64_t most = (int64_t)(sms > 0 ? sms : 1) * per_sm * w.shape.rows;
     w.rows_per_worker = (a.rows + most - 1) / most;
     if (w.rows_per_worker < 1) w.rows_per_worker = 1;
     w.workers = (a.rows + w.rows_per_worker - 1) / w.rows_per_worker;
@@ -275,17 +299,29 @@ NormWorkers norm_workers(const kq_norm_args_t& a, int sms) {
 }
 bool wants_vector_gradients(const kq_norm_args_t& a) { return a.dgate || a.dpost_weight || a.dweight || a.dscale || a.dshift; }
 
+template <typename S, typename Y, int VPT>
+kq_status_t launch_norm_staged(const kq::NormBackward& p, const NormWorkers& w, cudaStream_t st) {
+    static DeviceOnce attr_done;
+    if (attr_done.needed()) {
+        if (cudaFuncSetAttribute(kq::norm_residual_backward<S, Y, VPT>, cudaFuncAttributeMaxDynamicSharedMemorySize, kSmemPerCta) != cudaSuccess) {
+            (void)cudaGetLastError();
+            return KQ_ERR_CUDA;
+        }
+        attr_done.done();
+    }
+    cudaLaunchConfig_t cfg;
+    cudaLaunchAttribute attr[2];
+    launch_config(&cfg, attr, dim3((unsigned)w.workers), dim3((unsigned)w.shape.threads), (size_t)w.smem, 1, st);
+    return launch(cfg, kq::norm_residual_backward<S, Y, VPT>, p);
+}
 template <typename S, typename Y>
 kq_status_t launch_norm_backward(const kq::NormBackward& p, const NormWorkers& w, cudaStream_t st) {
+    if (w.shape.rows == 1) return w.shape.vpt == 2 ? launch_norm_staged<S, Y, 2>(p, w, st) : launch_norm_staged<S, Y, 4>(p, w, st);
     cudaLaunchConfig_t cfg;
     cudaLaunchAttribute attr[2];
     launch_config(&cfg, attr, dim3((unsigned)((w.workers + w.shape.rows - 1) / w.shape.rows)),
                   dim3((unsigned)w.shape.threads, (unsigned)w.shape.rows), 0, 1, st);
-    switch (w.shape.vpt) {
-        case 1: return launch(cfg, kq::norm_residual_backward<S, Y, 1>, p);
-        case 2: return launch(cfg, kq::norm_residual_backward<S, Y, 2>, p);
-        default: return launch(cfg, kq::norm_residual_backward<S, Y, 4>, p);
-    }
+    return w.shape.vpt == 1 ? launch(cfg, kq::norm_residual_backward_warp<S, Y, 1>, p) : launch(cfg, kq::norm_residual_backward_warp<S, Y, 2>, p);
 }
 
 }  // namespace
@@ -350,7 +386,7 @@ kq_status_t kroquant_norm_residual(const kq_norm_args_t* args, void* stream) {
 
 int64_t kroquant_norm_residual_grad_scratch_bytes(const kq_norm_args_t* args) {
     if (!args || check_norm(*args, true) != KQ_OK || args->rows == 0 || !wants_vector_gradients(*args)) return 0;
-    const NormWorkers w = norm_workers(*args, sm_count());
+    const NormWorkers w = norm_workers(*args, sm_count(), nullptr);
     return (w.workers + w.batches - 1) * 3 * args->d * (int64_t)sizeof(float);
 }
 
@@ -374,13 +410,13 @@ kq_status_t kroquant_norm_residual_grad(const kq_norm_args_t* args, void* scratc
     if (!a.h || !a.dx || (a.norm != KQ_NORM_NONE && !a.dn) || (a.y && !a.dy)) return KQ_ERR_NULL;
     const int sms = sm_count();
     if (sms <= 0) return KQ_ERR_CUDA;
-    const NormWorkers w = norm_workers(a, sms);
+    kq::NormBackward p = {};
+    const NormWorkers w = norm_workers(a, sms, &p);
     if (vectors) {
         if (!scratch) return KQ_ERR_NULL;
         if (!aligned16(scratch)) return KQ_ERR_ALIGN;
         if (scratch_bytes < kroquant_norm_residual_grad_scratch_bytes(args)) return KQ_ERR_SHAPE;
     }
-    kq::NormBackward p = {};
     p.rows = a.rows; p.d = a.d; p.rows_per_batch = a.rows_per_batch; p.rows_per_worker = w.rows_per_worker;
     p.dn = a.norm == KQ_NORM_NONE ? nullptr : a.dn; p.ld_dn = a.ld_dn; p.dh = a.dh; p.ld_dh = a.ld_dh;
     p.h = a.h; p.ld_h = a.ld_h; p.y = a.y; p.ld_y = a.ld_y; p.dx = a.dx; p.ld_dx = a.ld_dx; p.dy = a.dy; p.ld_dy = a.ld_dy;
@@ -410,7 +446,7 @@ kq_status_t kroquant_norm_residual_grad(const kq_norm_args_t* args, void* scratc
     g.dshift_stride = a.shift_stride ? a.d : 0;
     cudaLaunchConfig_t cfg;
     cudaLaunchAttribute attr[2];
-    launch_config(&cfg, attr, dim3((unsigned)((a.d + 31) / 32)), dim3(32, 32), 0, 1, st);
+    launch_config(&cfg, attr, dim3((unsigned)((a.d + 31) / 32)), dim3(32, kq::kSlotLanes), 0, 1, st);
     return launch(cfg, kq::norm_vector_gradients, g);
 }
 
