@@ -126,6 +126,13 @@ __device__ __forceinline__ void store8(T* p, int count, bool vec, int step, cons
             if (i < count) p[i * step] = Elem<T>::from_f32(v[i]);
     }
 }
+__device__ __forceinline__ float vec_entry(const NormVec& p, int64_t which, int at, float none) {
+    if (!p.ptr) return none;
+    const int64_t i = which * p.stride + at;
+    if (p.type == kTypeF32) return static_cast<const float*>(p.ptr)[i];
+    if (p.type == kTypeF16) return __half2float(static_cast<const __half*>(p.ptr)[i]);
+    return __bfloat162float(static_cast<const __nv_bfloat16*>(p.ptr)[i]);
+}
 // how many of the elements c, c + step, ..., c + 7 step of a row of d exist
 __device__ __forceinline__ int owned(int d, int c, int step) {
     const int left = c < d ? (d - c + step - 1) / step : 0;
@@ -206,6 +213,21 @@ __device__ __forceinline__ void warp_sum4(float (&v)[4], int lane) {
     for (int i = 0; i < 4; ++i) v[i] = __shfl_sync(0xFFFFFFFFu, k, 8 * i);
 }
 
+__device__ __forceinline__ uint32_t cluster_rank() {
+    uint32_t r;
+    asm volatile("mov.u32 %0, %%cluster_ctarank;" : "=r"(r));
+    return r;
+}
+__device__ __forceinline__ void cluster_barrier() {
+    asm volatile("barrier.cluster.arrive.release.aligned;\n\tbarrier.cluster.wait.acquire.aligned;" ::: "memory");
+}
+// four floats to the same place in the shared memory of CTA `rank` of the cluster
+__device__ __forceinline__ void st_cluster_v4(uint32_t addr, uint32_t rank, const float4& v) {
+    asm volatile("{\n\t.reg .u32 a;\n\tmapa.shared::cluster.u32 a, %0, %1;\n\t"
+                 "st.shared::cluster.v4.f32 [a], {%2, %3, %4, %5};\n\t}"
+                 ::"r"(addr), "r"(rank), "f"(v.x), "f"(v.y), "f"(v.z), "f"(v.w) : "memory");
+}
+
 struct NormForward {
     int64_t rows;
     int d;
@@ -223,7 +245,7 @@ struct NormForward {
 // blockDim = (threads of a row, rows of a CTA): one warp per row and several rows for narrow d, else one row per CTA.
 // Thread i owns the 8-channel groups i, i + blockDim.x, ...: VPT of them.
 template <typename S, typename Y, int VPT>
-__global__ void norm_residual_forward(const NormForward p) {
+__global__ void __launch_bounds__(VPT == 2 ? 1024 : 256) norm_residual_forward(const __grid_constant__ NormForward p) {
     __shared__ float red[2 * 128];
     const int64_t row = (int64_t)blockIdx.x * blockDim.y + threadIdx.y;
     pdl_wait_prior_grid();
@@ -350,8 +372,9 @@ struct NormBackward {
     int norm, post;
     int vec;
     float* partial;                   // [slots][3][d]: P, S, Q of a worker's rows of one batch; null: no vector gradient wanted
-    // staged kernel: stages, bytes of a stage, whether dh is staged, offsets of the rows, which parameter vectors are kept in shared memory
-    int stages, stage_bytes, stage_dh, off_dh, off_dn, off_y, cache_m, cache_gate, cache_post;
+    // staged kernel: CTAs of a worker and columns of each, stages, bytes of a stage, offsets of its rows, which parameter
+    // vectors are kept in shared memory
+    int cluster, columns, stages, stage_bytes, off_dh, off_dn, off_y, cache_m, cache_gate, cache_post;
 };
 
 // ---- backward, narrow rows: one warp per row --------------------------------------------------------
@@ -507,359 +530,484 @@ __global__ void __launch_bounds__(256) norm_residual_backward_warp(const NormBac
     if (p.partial) flush(worker + batch);
 }
 
-// ---- backward, wide rows: one CTA per row, rows staged in shared memory ---------------------------------
-// A CTA is a worker.  The four rows of an iteration arrive in shared memory by bulk copies issued `stages` rows ahead, so
-// that nothing waits for a load latency and a row needs no registers; a thread owns the 8-channel groups t, t + T, ... and
-// reads them again in every phase.  What a thread writes to shared memory (parameters, see below) only it reads.
-// One barrier for all statistics of a row: each warp takes its means, then its squares about ITS means, and every warp
-// combines the warps' (mean, sum of squares) pairs by Chan's update, exact in the sense that nothing cancels:
-//     M2 = sum_w M2_w + n_w (mean_w - mean)^2,    sum g (h - mean) = sum_w [G1_w + (mean_w - mean) G0_w].
-// Parameter vectors (weight (1 + scale), gate, post_weight) are kept in shared memory as floats where they fit, refreshed
-// at the start of a batch; else they are read through the caches.
+// ---- backward, wide rows: a CTA, or a cluster of two or four, per row; rows staged in shared memory ----------------
+// A worker is one CTA up to d = 4608 and a cluster of two or four above, each CTA with its part of the columns: one group of 8
+// channels per thread, so that the column sums (24 registers) and two rows with their parameters (shared memory) always
+// fit.  The four rows of an iteration arrive in shared memory by bulk copies issued `stages` rows ahead: nothing waits for a
+// load, and a row needs no registers.  A thread reads its group twice (statistics, gradients) or, with a post norm, y and
+// one more value a third time.  What a thread writes to shared memory (parameters, the value between the phases) only it reads.
+// The statistics take one pass and one barrier: sums about a pivot p, s1 = sum (v - p), s2 = sum (v - p)^2, so that
+//     M2 = sum (v - mean)^2 = s2 - s1^2 / d,    sum g (h - mean) = sum g (h - p) - (mean - p) sum g.
+// The pivot is the mean of 32 values spread over the row.  The mean of any n of d values lies within sqrt(d / n - 1)
+// deviations of the mean, so in the worst case (all 32 of them the row's outliers) a factor d / 32 of the 2^-24 is lost,
+// ordinarily nothing, however large the mean is.
+// With 18 warps on an SM the instructions bound the kernel next to memory, so the arithmetic is done on pairs (f32x2).
+// Parameter vectors (weight (1 + scale), gate, post_weight) are kept in shared memory as floats, refreshed at the start of a batch.
 // Rows that bulk copies cannot take (16-byte alignment) are copied into the same place by the threads, element by element.
 constexpr int kNormStageMax = 4;
+constexpr int kNormThreads = 576;
+constexpr int kNormColumns = 8 * kNormThreads;                      // of a CTA
+constexpr int kNormMaxCluster = 4;
 constexpr int kNormRedOff = 128;                                    // barriers and the abort word in front
-constexpr int kNormHeadBytes = kNormRedOff + 2 * 32 * 8 * 4;
+constexpr int kNormRedFloats = kNormMaxCluster * (kNormThreads / 32) * 8;
+constexpr int kNormHeadBytes = kNormRedOff + 3 * kNormRedFloats * 4;   // two sets of statistics used in turn, one of the second phase
 
-template <typename T>
-__device__ __forceinline__ void lds_widen(const uint8_t* row, int group, float (&v)[8]) {
-    Pack8<T> q;
-    const uint4* at = reinterpret_cast<const uint4*>(row) + group * (sizeof(T) / 2);
-    const uint4 a = at[0];
-    q.w[0] = a.x; q.w[1] = a.y; q.w[2] = a.z; q.w[3] = a.w;
-    if constexpr (sizeof(T) == 4) {
-        const uint4 b = at[1];
-        q.w[4] = b.x; q.w[5] = b.y; q.w[6] = b.z; q.w[7] = b.w;
-    }
-    pack_widen(q, v);
+typedef unsigned long long f32x2;
+__device__ __forceinline__ f32x2 pack2(float a, float b) {
+    f32x2 d;
+    asm("mov.b64 %0, {%1, %2};" : "=l"(d) : "f"(a), "f"(b));
+    return d;
 }
-__device__ __forceinline__ void lds_floats(const float* at, float (&v)[8]) {
-    const float4 a = reinterpret_cast<const float4*>(at)[0], b = reinterpret_cast<const float4*>(at)[1];
-    v[0] = a.x; v[1] = a.y; v[2] = a.z; v[3] = a.w; v[4] = b.x; v[5] = b.y; v[6] = b.z; v[7] = b.w;
+__device__ __forceinline__ float2 unpack2(f32x2 v) {
+    float2 d;
+    asm("mov.b64 {%0, %1}, %2;" : "=f"(d.x), "=f"(d.y) : "l"(v));
+    return d;
+}
+__device__ __forceinline__ f32x2 fma2(f32x2 a, f32x2 b, f32x2 c) {
+    f32x2 d;
+    asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(d) : "l"(a), "l"(b), "l"(c));
+    return d;
+}
+__device__ __forceinline__ f32x2 add2(f32x2 a, f32x2 b) {
+    f32x2 d;
+    asm("add.rn.f32x2 %0, %1, %2;" : "=l"(d) : "l"(a), "l"(b));
+    return d;
+}
+__device__ __forceinline__ f32x2 mul2(f32x2 a, f32x2 b) {
+    f32x2 d;
+    asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(d) : "l"(a), "l"(b));
+    return d;
+}
+__device__ __forceinline__ float sum2(f32x2 v) { const float2 f = unpack2(v); return f.x + f.y; }
+
+// two 16-bit elements -> a pair
+template <typename T>
+__device__ __forceinline__ f32x2 widen2(uint32_t w) {
+    if constexpr (__is_same(T, __half)) {
+        const float2 f = __half22float2(*reinterpret_cast<const __half2*>(&w));
+        return pack2(f.x, f.y);
+    } else {
+        return pack2(bf16lo_to_f32(w), bf16hi_to_f32(w));
+    }
+}
+// elements 4 quad .. 4 quad + 3 of a row in shared memory
+template <typename T>
+__device__ __forceinline__ void lds4(const uint8_t* row, int quad, f32x2 (&v)[2]) {
+    if constexpr (sizeof(T) == 4) {
+        const ulonglong2 a = reinterpret_cast<const ulonglong2*>(row)[quad];
+        v[0] = a.x;
+        v[1] = a.y;
+    } else {
+        const uint2 a = reinterpret_cast<const uint2*>(row)[quad];
+        v[0] = widen2<T>(a.x);
+        v[1] = widen2<T>(a.y);
+    }
+}
+template <typename T>
+__device__ __forceinline__ void lds8(const uint8_t* row, int group, f32x2 (&v)[4]) {
+    if constexpr (sizeof(T) == 4) {
+        const ulonglong2 a = reinterpret_cast<const ulonglong2*>(row)[2 * group], b = reinterpret_cast<const ulonglong2*>(row)[2 * group + 1];
+        v[0] = a.x; v[1] = a.y; v[2] = b.x; v[3] = b.y;
+    } else {
+        const uint4 a = reinterpret_cast<const uint4*>(row)[group];
+        v[0] = widen2<T>(a.x); v[1] = widen2<T>(a.y); v[2] = widen2<T>(a.z); v[3] = widen2<T>(a.w);
+    }
 }
 __device__ __forceinline__ void sts_floats(float* at, const float (&v)[8]) {
     reinterpret_cast<float4*>(at)[0] = make_float4(v[0], v[1], v[2], v[3]);
     reinterpret_cast<float4*>(at)[1] = make_float4(v[4], v[5], v[6], v[7]);
 }
-// a row that is not 16-byte aligned, into shared memory; the tail of the last group becomes 0
 template <typename T>
-__device__ __forceinline__ void copy_row(uint8_t* dst, const T* src, int d) {
-    T* out = reinterpret_cast<T*>(dst);
-    for (int c = (int)threadIdx.x; c < (d + 7) / 8 * 8; c += (int)blockDim.x) out[c] = c < d ? src[c] : Elem<T>::from_f32(0.f);
+__device__ __forceinline__ void store4(T* p, int count, bool vec, const f32x2 (&w)[2]) {
+    const float2 a = unpack2(w[0]), b = unpack2(w[1]);
+    if (vec) {
+        if constexpr (sizeof(T) == 4) {
+            *reinterpret_cast<float4*>(p) = make_float4(a.x, a.y, b.x, b.y);
+        } else if constexpr (__is_same(T, __half)) {
+            const __half2 x = __floats2half2_rn(a.x, a.y), y = __floats2half2_rn(b.x, b.y);
+            *reinterpret_cast<uint2*>(p) = make_uint2(*reinterpret_cast<const uint32_t*>(&x), *reinterpret_cast<const uint32_t*>(&y));
+        } else {
+            const __nv_bfloat162 x = __floats2bfloat162_rn(a.x, a.y), y = __floats2bfloat162_rn(b.x, b.y);
+            *reinterpret_cast<uint2*>(p) = make_uint2(*reinterpret_cast<const uint32_t*>(&x), *reinterpret_cast<const uint32_t*>(&y));
+        }
+    } else {
+        const float v[4] = {a.x, a.y, b.x, b.y};
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+            if (i < count) p[i] = Elem<T>::from_f32(v[i]);
+    }
+}
+// `d` columns of the four rows of an iteration that are not 16-byte aligned, into shared memory: sixteen loads in flight per
+// thread; the tail of the last group is 0
+template <typename S, typename Y>
+__device__ __noinline__ void copy_rows(uint8_t* stage, const NormBackward& p, int64_t row, int c0, int d) {
+    const S* src_s[2] = {static_cast<const S*>(p.h) + row * p.ld_h + c0, static_cast<const S*>(p.dh) + row * p.ld_dh + c0};
+    const Y* src_y[2] = {static_cast<const Y*>(p.dn) + row * p.ld_dn + c0, static_cast<const Y*>(p.y) + row * p.ld_y + c0};
+    S* dst_s[2] = {reinterpret_cast<S*>(stage), reinterpret_cast<S*>(stage + p.off_dh)};
+    Y* dst_y[2] = {reinterpret_cast<Y*>(stage + p.off_dn), reinterpret_cast<Y*>(stage + p.off_y)};
+    const bool have_s[2] = {true, p.dh != nullptr}, have_y[2] = {p.dn != nullptr, p.y != nullptr};
+    const int T = (int)blockDim.x, padded = (d + 7) / 8 * 8;
+    for (int c = (int)threadIdx.x; c < padded; c += 4 * T) {
+        S a[2][4];
+        Y b[2][4];
+#pragma unroll
+        for (int q = 0; q < 2; ++q)
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                const bool in = c + i * T < d;
+                a[q][i] = have_s[q] && in ? src_s[q][c + i * T] : Elem<S>::from_f32(0.f);
+                b[q][i] = have_y[q] && in ? src_y[q][c + i * T] : Elem<Y>::from_f32(0.f);
+            }
+#pragma unroll
+        for (int q = 0; q < 2; ++q)
+#pragma unroll
+            for (int i = 0; i < 4; ++i)
+                if (c + i * T < padded) {
+                    if (have_s[q]) dst_s[q][c + i * T] = a[q][i];
+                    if (have_y[q]) dst_y[q][c + i * T] = b[q][i];
+                }
+    }
 }
 
-template <typename S, typename Y, int VPT>
-__global__ void __launch_bounds__(VPT == 2 ? 576 : 512, 1) norm_residual_backward(const NormBackward p) {
+template <typename S, typename Y, bool POST>
+__global__ void __launch_bounds__(kNormThreads, 1) norm_residual_backward(const __grid_constant__ NormBackward p) {
     extern __shared__ __align__(128) uint8_t smem[];
     const uint32_t base = smem_u32(smem);
     volatile int* abort_flag = reinterpret_cast<volatile int*>(smem + 64);
     float* red = reinterpret_cast<float*>(smem + kNormRedOff);
-    const int T = (int)blockDim.x, t = (int)threadIdx.x, warp = t >> 5, lane = t & 31, warps = T >> 5;
-    const int padded = (p.d + 7) / 8 * 8;
+    const int t = (int)threadIdx.x, warp = t >> 5, lane = t & 31, warps = (int)blockDim.x >> 5;
+    const int rank = p.cluster > 1 ? (int)cluster_rank() : 0;
+    const int64_t worker = blockIdx.x / (unsigned)p.cluster;
+    const int c0 = rank * p.columns;                                  // this CTA's columns: c0 .. c0 + d - 1
+    const int d = p.d - c0 < p.columns ? p.d - c0 : p.columns;
     float* par_m = reinterpret_cast<float*>(smem + kNormHeadBytes);
-    float* par_gate = par_m + (p.cache_m ? padded : 0);
-    float* par_post = par_gate + (p.cache_gate ? padded : 0);
-    const int stage0 = kNormHeadBytes + 4 * padded * (p.cache_m + p.cache_gate + p.cache_post);
-    const int64_t worker = blockIdx.x, first = worker * p.rows_per_worker;
-    const int64_t last = first + p.rows_per_worker < p.rows ? first + p.rows_per_worker : p.rows;
+    float* par_gate = par_m + (p.cache_m ? p.columns : 0);
+    float* par_post = par_gate + (p.cache_gate ? p.columns : 0);
+    const int stage0 = kNormHeadBytes + 4 * p.columns * (p.cache_m + p.cache_gate + p.cache_post);
+    const int64_t first = worker * p.rows_per_worker;
+    const int rows = (int)(first + p.rows_per_worker < p.rows ? p.rows_per_worker : p.rows - first);
     const bool vec = p.vec != 0;
     const float inv_d = 1.0f / (float)p.d;
-    const bool layer_h = p.norm == kNormLayer, layer_y = p.post == kNormLayer, post = p.y && p.post != kNormNone;
+    const bool layer_h = p.norm == kNormLayer, layer_y = POST && p.post == kNormLayer, norm = p.norm != kNormNone;
+    // all threads of the worker; the values that the warps exchange go to every CTA's shared memory
+    auto barrier = [&]() { if (p.cluster > 1) cluster_barrier(); else __syncthreads(); };
+    auto exchange = [&](float* at, const float4& a) {
+        *reinterpret_cast<float4*>(at) = a;
+        for (int q = 1; q < p.cluster; ++q) st_cluster_v4(smem_u32(at), (uint32_t)((rank + q) % p.cluster), a);
+    };
+    const int all_warps = warps * p.cluster, my_warp = warp + rank * warps;
     if (t == 0) {
         for (int s = 0; s < p.stages; ++s) mbar_init(base + 8u * s, 1);
         *abort_flag = 0;
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
         asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
     }
-    __syncthreads();
+    barrier();
     pdl_wait_prior_grid();
-    auto issue = [&](int64_t row) {                                  // thread 0
-        const int s = (int)((row - first) % p.stages);
+    auto issue = [&](int r, int s) {                                  // thread 0: row `r` of this worker into stage s
+        const int64_t row = first + r;
         const uint32_t bar = base + 8u * s, dst = base + (uint32_t)(stage0 + s * p.stage_bytes);
-        const uint32_t bytes_s = (uint32_t)p.d * sizeof(S), bytes_y = (uint32_t)p.d * sizeof(Y);
-        mbar_expect_tx(bar, bytes_s * (p.stage_dh ? 2 : 1) + bytes_y * ((p.dn ? 1 : 0) + (p.y ? 1 : 0)));
-        bulk_load(dst, static_cast<const S*>(p.h) + row * p.ld_h, bytes_s, bar);
-        if (p.stage_dh) bulk_load(dst + p.off_dh, static_cast<const S*>(p.dh) + row * p.ld_dh, bytes_s, bar);
-        if (p.dn) bulk_load(dst + p.off_dn, static_cast<const Y*>(p.dn) + row * p.ld_dn, bytes_y, bar);
-        if (p.y) bulk_load(dst + p.off_y, static_cast<const Y*>(p.y) + row * p.ld_y, bytes_y, bar);
+        const uint32_t bytes_s = (uint32_t)d * sizeof(S), bytes_y = (uint32_t)d * sizeof(Y);
+        mbar_expect_tx(bar, bytes_s * (p.dh ? 2 : 1) + bytes_y * ((p.dn ? 1 : 0) + (p.y ? 1 : 0)));
+        bulk_load(dst, static_cast<const S*>(p.h) + row * p.ld_h + c0, bytes_s, bar);
+        if (p.dh) bulk_load(dst + p.off_dh, static_cast<const S*>(p.dh) + row * p.ld_dh + c0, bytes_s, bar);
+        if (p.dn) bulk_load(dst + p.off_dn, static_cast<const Y*>(p.dn) + row * p.ld_dn + c0, bytes_y, bar);
+        if (p.y) bulk_load(dst + p.off_y, static_cast<const Y*>(p.y) + row * p.ld_y + c0, bytes_y, bar);
     };
     if (vec && t == 0)
-        for (int64_t r = first; r < first + p.stages && r < last; ++r) issue(r);
-    int count[VPT];
-    int mine = 0;
-#pragma unroll
-    for (int k = 0; k < VPT; ++k) {
-        count[k] = owned(p.d, (t + k * T) * 8, 1);
-        mine += count[k];
-    }
-#pragma unroll
-    for (int o = 16; o > 0; o >>= 1) mine += __shfl_xor_sync(0xFFFFFFFFu, mine, o);
-    const float n_w = (float)mine, inv_n = 1.f / (mine ? (float)mine : 1.f);
-    float sum[3][VPT][8];
+        for (int r = 0; r < p.stages && r < rows; ++r) issue(r, r);
+    const int c = t * 8, count = owned(d, c, 1);                       // this thread's channels in the CTA's columns
+    f32x2 sum[3][4];
     auto clear = [&]() {
 #pragma unroll
         for (int q = 0; q < 3; ++q)
 #pragma unroll
-            for (int k = 0; k < VPT; ++k)
-#pragma unroll
-                for (int i = 0; i < 8; ++i) sum[q][k][i] = 0.f;
+            for (int i = 0; i < 4; ++i) sum[q][i] = 0ull;
     };
     auto flush = [&](int64_t slot) {
-        float* out = p.partial + slot * 3 * p.d;
+        float* out = p.partial + slot * 3 * p.d + c0 + c;
 #pragma unroll
         for (int q = 0; q < 3; ++q)
 #pragma unroll
-            for (int k = 0; k < VPT; ++k)
-                if (count[k] > 0) store8(out + (int64_t)q * p.d + (t + k * T) * 8, count[k], vec, 1, sum[q][k]);
+            for (int half = 0; half < 2; ++half)
+                if (count > 4 * half) {
+                    const f32x2 v[2] = {sum[q][2 * half], sum[q][2 * half + 1]};
+                    store4(out + (int64_t)q * p.d + 4 * half, count - 4 * half, vec, v);
+                }
         clear();
     };
     clear();
     int64_t batch = first / p.rows_per_batch;
-    auto multiplier = [&](int k, float (&m)[8]) {
-        if (p.cache_m) {
-            lds_floats(par_m + (t + k * T) * 8, m);
-        } else {
-            float a[8];
-            load_param(p.weight, 0, (t + k * T) * 8, count[k], vec, 1, 1.f, m);
-            load_param(p.scale, batch, (t + k * T) * 8, count[k], vec, 1, 0.f, a);
+    // rows of this worker before the next batch begins
+    auto rows_left = [&](int64_t row) { const int64_t n = (batch + 1) * p.rows_per_batch - row; return (int)(n < rows ? n : rows); };
+    int batch_end = rows_left(first);
+    auto refresh = [&]() {
+        if (count > 0) {
+            float m[8], a[8];
+            if (p.cache_m) {
+                load_param(p.weight, 0, c0 + c, count, vec, 1, 1.f, m);
+                load_param(p.scale, batch, c0 + c, count, vec, 1, 0.f, a);
 #pragma unroll
-            for (int i = 0; i < 8; ++i) m[i] = fmaf(m[i], a[i], m[i]);
+                for (int i = 0; i < 8; ++i) m[i] = fmaf(m[i], a[i], m[i]);
+                sts_floats(par_m + c, m);
+            }
+            if (p.cache_gate) {
+                load_param(p.gate, batch, c0 + c, count, vec, 1, 1.f, m);
+                sts_floats(par_gate + c, m);
+            }
+            if (p.cache_post) {
+                load_param(p.post_weight, 0, c0 + c, count, vec, 1, 1.f, m);
+                sts_floats(par_post + c, m);
+            }
         }
     };
-    auto refresh = [&]() {
-#pragma unroll
-        for (int k = 0; k < VPT; ++k)
-            if (count[k] > 0) {
-                const int c = (t + k * T) * 8;
-                float m[8], a[8];
-                if (p.cache_m) {
-                    load_param(p.weight, 0, c, count[k], vec, 1, 1.f, m);
-                    load_param(p.scale, batch, c, count[k], vec, 1, 0.f, a);
-#pragma unroll
-                    for (int i = 0; i < 8; ++i) m[i] = fmaf(m[i], a[i], m[i]);
-                    sts_floats(par_m + c, m);
-                }
-                if (p.cache_gate) {
-                    load_param(p.gate, batch, c, count[k], vec, 1, 1.f, m);
-                    sts_floats(par_gate + c, m);
-                }
-                if (p.cache_post) {
-                    load_param(p.post_weight, 0, c, count[k], vec, 1, 1.f, m);
-                    sts_floats(par_post + c, m);
-                }
-            }
-    };
     refresh();
-    for (int64_t row = first; row < last; ++row) {
-        const int64_t i_row = row - first;
-        const int s = (int)(i_row % p.stages);
+    const f32x2 one2 = pack2(1.f, 1.f), alpha2 = pack2(p.alpha, p.alpha);
+    auto parameters = [&](int have, const float* at, f32x2 (&m)[2]) {
+        const ulonglong2 w = have ? *reinterpret_cast<const ulonglong2*>(at) : make_ulonglong2(one2, one2);
+        m[0] = w.x;
+        m[1] = w.y;
+    };
+    // the mean of 32 values spread over this CTA's columns of a row, the same in every warp (the CTAs of a cluster use their own)
+    auto pivot_of = [&](float v) {
+#pragma unroll
+        for (int o = 16; o > 0; o >>= 1) v += __shfl_xor_sync(0xFFFFFFFFu, v, o);
+        return v * 0.03125f;
+    };
+    const int sample = (int)((int64_t)lane * d / 32);
+    S* dx = static_cast<S*>(p.dx) + first * p.ld_dx + c0 + c;
+    Y* dy = static_cast<Y*>(p.dy) + first * p.ld_dy + c0 + c;
+    int s = 0;
+    uint32_t parity = 0;
+    for (int r = 0; r < rows; ++r) {
         uint8_t* stage = smem + stage0 + s * p.stage_bytes;
-        if (row >= (batch + 1) * p.rows_per_batch) {
+        if (r == batch_end) {
             if (p.partial) flush(worker + batch);
-            batch = row / p.rows_per_batch;
+            ++batch;
+            batch_end = r + rows_left(first + r);
             refresh();
         }
         if (vec) {
-            if (p.stages == 1 && i_row > 0) {                        // no second slot: the next row starts when this one is done
-                __syncthreads();
-                if (t == 0) issue(row);
-            }
             // a wait that gives up records it and goes on (the barriers below stay matched)
-            if (!mbar_wait(base + 8u * s, (uint32_t)(i_row / p.stages) & 1u, abort_flag) && !*abort_flag) {
+            if (!mbar_wait(base + 8u * s, parity, abort_flag) && !*abort_flag) {
                 atomicExch(&g_kq_device_error, KQ_DEV_TIMEOUT_NORM);
                 *abort_flag = 1;
             }
         } else {
             __syncthreads();
-            copy_row(stage, static_cast<const S*>(p.h) + row * p.ld_h, p.d);
-            if (p.stage_dh) copy_row(stage + p.off_dh, static_cast<const S*>(p.dh) + row * p.ld_dh, p.d);
-            if (p.dn) copy_row(stage + p.off_dn, static_cast<const Y*>(p.dn) + row * p.ld_dn, p.d);
-            if (p.y) copy_row(stage + p.off_y, static_cast<const Y*>(p.y) + row * p.ld_y, p.d);
+            copy_rows<S, Y>(stage, p, first + r, c0, d);
             __syncthreads();
         }
-        // this warp's means of h and y and its sum of g (layer)
-        float mu[4] = {0.f, 0.f, 0.f, 0.f};
-        if (layer_h || layer_y) {
+        // ---- statistics ----
+        float pivot_h = 0.f, pivot_y = 0.f;
+        if (layer_h) pivot_h = pivot_of(Elem<S>::to_f32(reinterpret_cast<const S*>(stage)[sample]));
+        if (layer_y) pivot_y = pivot_of(Elem<Y>::to_f32(reinterpret_cast<const Y*>(stage + p.off_y)[sample]));
+        float st[4] = {0.f, 0.f, 0.f, 0.f}, sty[4] = {0.f, 0.f, 0.f, 0.f};       // s1, s2, sum g, sum g (h - p) of h; s1, s2 of y
+        if (count == 8) {
+            if (norm) {
+                const f32x2 minus = pack2(-pivot_h, -pivot_h);
+                f32x2 v[4], g[4], m[2], s1 = 0ull, s2 = 0ull, g0 = 0ull, g1 = 0ull;
+                lds8<S>(stage, t, v);
+                lds8<Y>(stage + p.off_dn, t, g);
 #pragma unroll
-            for (int k = 0; k < VPT; ++k)
-                if (count[k] > 0) {
-                    float v[8], m[8];
-                    if (layer_h) {
-                        lds_widen<S>(stage, t + k * T, v);
+                for (int half = 0; half < 2; ++half) {
+                    parameters(p.cache_m, par_m + c + 4 * half, m);
 #pragma unroll
-                        for (int i = 0; i < 8; ++i) mu[0] += v[i];
-                        lds_widen<Y>(stage + p.off_dn, t + k * T, v);
-                        multiplier(k, m);
-#pragma unroll
-                        for (int i = 0; i < 8; ++i) mu[1] = fmaf(v[i], m[i], mu[1]);
-                    }
-                    if (layer_y) {
-                        lds_widen<Y>(stage + p.off_y, t + k * T, v);
-#pragma unroll
-                        for (int i = 0; i < 8; ++i) mu[2] += v[i];
-                    }
-                }
-            warp_sum4(mu, lane);
-            mu[0] *= inv_n;
-            mu[2] *= inv_n;
-        }
-        // squares about them
-        float sq[4] = {0.f, 0.f, 0.f, 0.f};
-        if (p.norm != kNormNone || post) {
-#pragma unroll
-            for (int k = 0; k < VPT; ++k)
-                if (count[k] > 0) {
-                    float v[8], m[8], g[8];
-                    if (p.norm != kNormNone) {
-                        lds_widen<S>(stage, t + k * T, v);
-                        lds_widen<Y>(stage + p.off_dn, t + k * T, g);
-                        multiplier(k, m);
-#pragma unroll
-                        for (int i = 0; i < 8; ++i) {
-                            const float u = i < count[k] ? v[i] - mu[0] : 0.f;
-                            sq[0] = fmaf(u, u, sq[0]);
-                            sq[1] = fmaf(g[i] * m[i], u, sq[1]);
-                        }
-                    }
-                    if (post) {
-                        lds_widen<Y>(stage + p.off_y, t + k * T, v);
-#pragma unroll
-                        for (int i = 0; i < 8; ++i) {
-                            const float u = i < count[k] ? v[i] - mu[2] : 0.f;
-                            sq[2] = fmaf(u, u, sq[2]);
-                        }
+                    for (int i = 0; i < 2; ++i) {
+                        const f32x2 u = add2(v[2 * half + i], minus), w = mul2(g[2 * half + i], m[i]);
+                        s1 = add2(s1, u);
+                        s2 = fma2(u, u, s2);
+                        g0 = add2(g0, w);
+                        g1 = fma2(w, u, g1);
                     }
                 }
-            warp_sum4(sq, lane);
+                st[0] = sum2(s1); st[1] = sum2(s2); st[2] = sum2(g0); st[3] = sum2(g1);
+            }
+            if (POST) {
+                const f32x2 minus = pack2(-pivot_y, -pivot_y);
+                f32x2 v[4], s1 = 0ull, s2 = 0ull;
+                lds8<Y>(stage + p.off_y, t, v);
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    const f32x2 u = add2(v[i], minus);
+                    s1 = add2(s1, u);
+                    s2 = fma2(u, u, s2);
+                }
+                sty[0] = sum2(s1); sty[1] = sum2(s2);
+            }
+        } else {                                                     // the ragged end of a row: one thread, one by one
+#pragma unroll 1
+            for (int i = 0; i < count; ++i) {
+                if (norm) {
+                    const float u = Elem<S>::to_f32(reinterpret_cast<const S*>(stage)[c + i]) - pivot_h;
+                    const float w = Elem<Y>::to_f32(reinterpret_cast<const Y*>(stage + p.off_dn)[c + i]) * (p.cache_m ? par_m[c + i] : 1.f);
+                    st[0] += u; st[1] = fmaf(u, u, st[1]); st[2] += w; st[3] = fmaf(w, u, st[3]);
+                }
+                if (POST) {
+                    const float u = Elem<Y>::to_f32(reinterpret_cast<const Y*>(stage + p.off_y)[c + i]) - pivot_y;
+                    sty[0] += u; sty[1] = fmaf(u, u, sty[1]);
+                }
+            }
         }
+        warp_sum4(st, lane);
+        if (POST) warp_sum4(sty, lane);
+        float* exchanged = red + (r & 1) * kNormRedFloats;           // the row before may still be read
         if (lane == 0) {
-            float4* at = reinterpret_cast<float4*>(red + warp * 8);
-            at[0] = make_float4(n_w, mu[0], mu[1], mu[2]);
-            at[1] = make_float4(sq[0], sq[1], sq[2], 0.f);
+            exchange(exchanged + my_warp * 8, make_float4(st[0], st[1], st[2], st[3]));
+            if (POST || p.cluster > 1) exchange(exchanged + my_warp * 8 + 4, make_float4(sty[0], sty[1], pivot_h, pivot_y));
         }
-        __syncthreads();
+        barrier();
         // every thread is done with the row before: its slot takes the row `stages` further on
-        if (vec && t == 0 && p.stages > 1 && i_row > 0 && row - 1 + p.stages < last) issue(row - 1 + p.stages);
-        float mean_h = 0.f, mean_g = 0.f, mean_y = 0.f;
-        {
-            float4 a = make_float4(0.f, 0.f, 0.f, 0.f), b = a;
+        if (vec && t == 0 && r > 0 && r - 1 + p.stages < rows) issue(r - 1 + p.stages, s == 0 ? p.stages - 1 : s - 1);
+        st[0] = st[1] = st[2] = st[3] = sty[0] = sty[1] = sty[2] = sty[3] = 0.f;
+        if (p.cluster == 1) {
             if (lane < warps) {
-                a = reinterpret_cast<const float4*>(red + lane * 8)[0];
-                b = reinterpret_cast<const float4*>(red + lane * 8)[1];
+                const float4 a = reinterpret_cast<const float4*>(exchanged + lane * 8)[0];
+                st[0] = a.x; st[1] = a.y; st[2] = a.z; st[3] = a.w;
+                if (POST) {
+                    const float2 b = reinterpret_cast<const float2*>(exchanged + lane * 8)[2];
+                    sty[0] = b.x; sty[1] = b.y;
+                }
             }
-            if (layer_h || layer_y) {
-                float tot[4] = {a.x * a.y, a.z, a.x * a.w, 0.f};
-                warp_sum4(tot, lane);
-                mean_h = tot[0] * inv_d;
-                mean_g = tot[1] * inv_d;
-                mean_y = tot[2] * inv_d;
+        } else {
+            // every CTA summed about its own pivot: moved to that of rank 0, s1 + n e, s2 + 2 e s1 + n e^2, g1 + e g0
+            const float ph = exchanged[6], py = exchanged[7];
+            for (int w = lane; w < all_warps; w += 32) {
+                const float4 a = reinterpret_cast<const float4*>(exchanged + w * 8)[0], b = reinterpret_cast<const float4*>(exchanged + w * 8)[1];
+                const int q = w / warps, left = (p.d - q * p.columns < p.columns ? p.d - q * p.columns : p.columns) - (w - q * warps) * 256;
+                const float n = (float)(left < 0 ? 0 : (left > 256 ? 256 : left));
+                const float eh = b.z - ph, ey = b.w - py;
+                st[0] += fmaf(n, eh, a.x);
+                st[1] += fmaf(eh, fmaf(n, eh, 2.f * a.x), a.y);
+                st[2] += a.z;
+                st[3] += fmaf(eh, a.z, a.w);
+                sty[0] += fmaf(n, ey, b.x);
+                sty[1] += fmaf(ey, fmaf(n, ey, 2.f * b.x), b.y);
             }
-            const float dh_ = a.y - mean_h, dy_ = a.w - mean_y;
-            sq[0] = fmaf(a.x * dh_, dh_, b.x);
-            sq[1] = fmaf(dh_, a.z, b.y);
-            sq[2] = fmaf(a.x * dy_, dy_, b.z);
-            sq[3] = 0.f;
-            warp_sum4(sq, lane);
+            pivot_h = ph;
+            pivot_y = py;
         }
-        const float inv_h = 1.0f / sqrtf(sq[0] * inv_d + p.eps);
-        const float along_h = sq[1] * inv_d * inv_h;
-        const float inv_y = post ? 1.0f / sqrtf(sq[2] * inv_d + p.eps) : 1.f;
-        float back[2] = {0.f, 0.f};
+        warp_sum4(st, lane);
+        if (POST) warp_sum4(sty, lane);
+        // layer: mean = pivot + s1 / d, the squares and products moved to the mean; rms: mean 0, which the pivot was
+        const float shift_h = layer_h ? st[0] * inv_d : 0.f, shift_y = layer_y ? sty[0] * inv_d : 0.f;
+        const float mean_h = pivot_h + shift_h, mean_y = pivot_y + shift_y, mean_g = layer_h ? st[2] * inv_d : 0.f;
+        // ---- gradients: H = dh + inv_h (g m - mean_g - xhat along_h) ----
+        const float inv_h = norm ? 1.0f / sqrtf(fmaf(st[1], inv_d, -shift_h * shift_h) + p.eps) : 0.f;
+        const float along_h = fmaf(-shift_h, st[2], st[3]) * inv_d * inv_h;
+        const float inv_y = POST ? 1.0f / sqrtf(fmaf(sty[1], inv_d, -shift_y * shift_y) + p.eps) : 1.f;
+        const f32x2 inv_h2 = pack2(inv_h, inv_h), off_h2 = pack2(-mean_h, -mean_h), along2 = pack2(-along_h, -along_h), mean_g2 = pack2(-mean_g, -mean_g);
+        const f32x2 inv_y2 = pack2(inv_y, inv_y), off_y2 = pack2(-mean_y, -mean_y);
+        f32x2 back0 = 0ull, back1 = 0ull;
+        if (count > 0) {
 #pragma unroll
-        for (int k = 0; k < VPT; ++k)
-            if (count[k] > 0) {
-                asm volatile("" ::: "memory");                     // one group at a time: the registers hold the column sums
-                const int gi = t + k * T, c = gi * 8;
-                float Hk[8], v[8], m[8];
-                if (p.stage_dh) {
-                    lds_widen<S>(stage + p.off_dh, gi, Hk);
-                } else if (p.dh) {
-                    Pack8<S> q;
-                    load_pack(static_cast<const S*>(p.dh) + row * p.ld_dh + c, count[k], vec, 1, q);
-                    pack_widen(q, Hk);
-                } else {
+            for (int half = 0; half < 2; ++half) {
+                const int quad = 2 * t + half, left = count - 4 * half;
+                f32x2 H[2] = {0ull, 0ull}, v[2], m[2];
+                if (p.dh) lds4<S>(stage + p.off_dh, quad, H);
+                if (norm) {
+                    f32x2 g[2];
+                    lds4<S>(stage, quad, v);
+                    lds4<Y>(stage + p.off_dn, quad, g);
+                    parameters(p.cache_m, par_m + c + 4 * half, m);
 #pragma unroll
-                    for (int i = 0; i < 8; ++i) Hk[i] = 0.f;
-                }
-                if (p.norm != kNormNone) {
-                    float g[8];
-                    lds_widen<S>(stage, gi, v);
-                    lds_widen<Y>(stage + p.off_dn, gi, g);
-                    multiplier(k, m);
-#pragma unroll
-                    for (int i = 0; i < 8; ++i) {
-                        const float xhat = (v[i] - mean_h) * inv_h;
-                        sum[0][k][i] = fmaf(g[i], xhat, sum[0][k][i]);
-                        sum[1][k][i] += g[i];
-                        Hk[i] = fmaf(inv_h, fmaf(g[i], m[i], -mean_g) - xhat * along_h, Hk[i]);
+                    for (int i = 0; i < 2; ++i) {
+                        const f32x2 xhat = mul2(add2(v[i], off_h2), inv_h2);
+                        sum[0][2 * half + i] = fma2(g[i], xhat, sum[0][2 * half + i]);
+                        sum[1][2 * half + i] = add2(sum[1][2 * half + i], g[i]);
+                        H[i] = fma2(inv_h2, fma2(xhat, along2, fma2(g[i], m[i], mean_g2)), H[i]);
                     }
                 }
-#pragma unroll
-                for (int i = 0; i < 8; ++i) v[i] = p.alpha * Hk[i];
-                store8(static_cast<S*>(p.dx) + row * p.ld_dx + c, count[k], vec, 1, v);
+                v[0] = mul2(alpha2, H[0]);
+                v[1] = mul2(alpha2, H[1]);
+                store4(dx + 4 * half, left, vec, v);
                 if (p.y) {
-                    float a[8];
-                    lds_widen<Y>(stage + p.off_y, gi, v);
-                    if (p.cache_gate) lds_floats(par_gate + c, m); else load_param(p.gate, batch, c, count[k], vec, 1, 1.f, m);
-                    if (post) {
-                        if (p.cache_post) lds_floats(par_post + c, a); else load_param(p.post_weight, 0, c, count[k], vec, 1, 1.f, a);
-                    }
+                    lds4<Y>(stage + p.off_y, quad, v);
+                    parameters(p.cache_gate, par_gate + c + 4 * half, m);
+                    if (!POST) {
 #pragma unroll
-                    for (int i = 0; i < 8; ++i) {
-                        const float yhat = (v[i] - mean_y) * inv_y;
-                        sum[2][k][i] = fmaf(Hk[i], yhat, sum[2][k][i]);
-                        Hk[i] *= m[i];                          // from here on the gradient at the branch
-                        if (post) {
-                            Hk[i] = i < count[k] ? Hk[i] * a[i] : 0.f;
-                            back[0] += Hk[i];
-                            back[1] = fmaf(Hk[i], yhat, back[1]);
+                        for (int i = 0; i < 2; ++i) {
+                            sum[2][2 * half + i] = fma2(H[i], v[i], sum[2][2 * half + i]);
+                            H[i] = mul2(H[i], m[i]);
+                        }
+                        store4(dy + 4 * half, left, vec, H);
+                    } else {
+                        f32x2 w[2];
+                        parameters(p.cache_post, par_post + c + 4 * half, w);
+                        if (left < 4) {                                            // nothing beyond the row in the sums below
+                            H[0] = pack2(left > 0 ? unpack2(H[0]).x : 0.f, left > 1 ? unpack2(H[0]).y : 0.f);
+                            H[1] = pack2(left > 2 ? unpack2(H[1]).x : 0.f, 0.f);
+                        }
+#pragma unroll
+                        for (int i = 0; i < 2; ++i) {
+                            const f32x2 yhat = mul2(add2(v[i], off_y2), inv_y2);
+                            sum[2][2 * half + i] = fma2(H[i], yhat, sum[2][2 * half + i]);
+                            H[i] = mul2(mul2(H[i], m[i]), w[i]);                   // the gradient at yhat
+                            back0 = add2(back0, H[i]);
+                            back1 = fma2(H[i], yhat, back1);
+                        }
+                        // kept for the second phase in the place of these channels' h (32 bits) or h and dh (16), which have been read
+                        if constexpr (sizeof(S) == 4) {
+                            reinterpret_cast<ulonglong2*>(stage)[quad] = make_ulonglong2(H[0], H[1]);
+                        } else {
+                            reinterpret_cast<f32x2*>(stage)[quad] = H[0];
+                            reinterpret_cast<f32x2*>(stage + p.off_dh)[quad] = H[1];
                         }
                     }
-                    if (!post) store8(static_cast<Y*>(p.dy) + row * p.ld_dy + c, count[k], vec, 1, Hk);
-                    else {
-                        // kept for the second phase in the place of this group's h and dh, which have been read
-                        uint4* lo = reinterpret_cast<uint4*>(stage) + gi * (sizeof(S) / 2);
-                        uint4* hi = sizeof(S) == 4 ? lo + 1 : reinterpret_cast<uint4*>(stage + p.off_dh) + gi;
-                        *reinterpret_cast<float4*>(lo) = make_float4(Hk[0], Hk[1], Hk[2], Hk[3]);
-                        *reinterpret_cast<float4*>(hi) = make_float4(Hk[4], Hk[5], Hk[6], Hk[7]);
-                    }
                 }
             }
-        if (post) {
-#pragma unroll
-            for (int o = 16; o > 0; o >>= 1) {
-                back[0] += __shfl_xor_sync(0xFFFFFFFFu, back[0], o);
-                back[1] += __shfl_xor_sync(0xFFFFFFFFu, back[1], o);
-            }
-            float* at = red + 32 * 8;
-            if (lane == 0) { at[warp * 2] = back[0]; at[warp * 2 + 1] = back[1]; }
-            asm volatile("fence.proxy.async.shared::cta;" ::: "memory");   // H lies where the next copy lands
-            __syncthreads();
-            back[0] = lane < warps ? at[lane * 2] : 0.f;
-            back[1] = lane < warps ? at[lane * 2 + 1] : 0.f;
-#pragma unroll
-            for (int o = 16; o > 0; o >>= 1) {
-                back[0] += __shfl_xor_sync(0xFFFFFFFFu, back[0], o);
-                back[1] += __shfl_xor_sync(0xFFFFFFFFu, back[1], o);
-            }
-            const float mean_a = layer_y ? back[0] * inv_d : 0.f, along_y = back[1] * inv_d;
-#pragma unroll
-            for (int k = 0; k < VPT; ++k)
-                if (count[k] > 0) {
-                    const int gi = t + k * T;
-                    float v[8], a[8];
-                    lds_widen<Y>(stage + p.off_y, gi, v);
-                    const uint4* lo = reinterpret_cast<const uint4*>(stage) + gi * (sizeof(S) / 2);
-                    const uint4* hi = sizeof(S) == 4 ? lo + 1 : reinterpret_cast<const uint4*>(stage + p.off_dh) + gi;
-                    const float4 x = *reinterpret_cast<const float4*>(lo), z = *reinterpret_cast<const float4*>(hi);
-                    a[0] = x.x; a[1] = x.y; a[2] = x.z; a[3] = x.w; a[4] = z.x; a[5] = z.y; a[6] = z.z; a[7] = z.w;
-#pragma unroll
-                    for (int i = 0; i < 8; ++i) v[i] = (a[i] - mean_a - (v[i] - mean_y) * inv_y * along_y) * inv_y;
-                    store8(static_cast<Y*>(p.dy) + row * p.ld_dy + gi * 8, count[k], vec, 1, v);
-                }
         }
+        if (POST) {
+            float b0 = sum2(back0), b1 = sum2(back1);
+#pragma unroll
+            for (int o = 16; o > 0; o >>= 1) {
+                b0 += __shfl_xor_sync(0xFFFFFFFFu, b0, o);
+                b1 += __shfl_xor_sync(0xFFFFFFFFu, b1, o);
+            }
+            float* at = red + 2 * kNormRedFloats;
+            if (lane == 0) exchange(at + my_warp * 4, make_float4(b0, b1, 0.f, 0.f));
+            asm volatile("fence.proxy.async.shared::cta;" ::: "memory");     // the kept values lie where the next copy lands
+            barrier();
+            b0 = b1 = 0.f;
+            for (int w = lane; w < all_warps; w += 32) {
+                b0 += at[w * 4];
+                b1 += at[w * 4 + 1];
+            }
+#pragma unroll
+            for (int o = 16; o > 0; o >>= 1) {
+                b0 += __shfl_xor_sync(0xFFFFFFFFu, b0, o);
+                b1 += __shfl_xor_sync(0xFFFFFFFFu, b1, o);
+            }
+            // dy = (a - mean_a - yhat along_y) inv_y
+            const float mean_a = layer_y ? b0 * inv_d : 0.f, along_y = b1 * inv_d;
+            const f32x2 mean_a2 = pack2(-mean_a, -mean_a), along_y2 = pack2(-along_y, -along_y);
+            if (count > 0) {
+#pragma unroll
+                for (int half = 0; half < 2; ++half) {
+                    const int quad = 2 * t + half;
+                    f32x2 v[2], H[2];
+                    lds4<Y>(stage + p.off_y, quad, v);
+                    if constexpr (sizeof(S) == 4) {
+                        const ulonglong2 a = reinterpret_cast<const ulonglong2*>(stage)[quad];
+                        H[0] = a.x;
+                        H[1] = a.y;
+                    } else {
+                        H[0] = reinterpret_cast<const f32x2*>(stage)[quad];
+                        H[1] = reinterpret_cast<const f32x2*>(stage + p.off_dh)[quad];
+                    }
+#pragma unroll
+                    for (int i = 0; i < 2; ++i)
+                        v[i] = mul2(fma2(mul2(add2(v[i], off_y2), inv_y2), along_y2, add2(H[i], mean_a2)), inv_y2);
+                    store4(dy + 4 * half, count - 4 * half, vec, v);
+                }
+            }
+        }
+        dx += p.ld_dx;
+        dy += p.ld_dy;
+        if (++s == p.stages) { s = 0; parity ^= 1u; }
     }
-    if (p.partial && first < last) flush(worker + batch);
+    if (p.partial) flush(worker + batch);
+    if (p.cluster > 1) cluster_barrier();                             // nobody's shared memory goes away while a peer writes to it
 }
 
 struct NormVecGrads {
@@ -873,13 +1021,6 @@ struct NormVecGrads {
     int64_t dgate_stride, dscale_stride, dshift_stride;
 };
 
-__device__ __forceinline__ float vec_entry(const NormVec& p, int64_t which, int at, float none) {
-    if (!p.ptr) return none;
-    const int64_t i = which * p.stride + at;
-    if (p.type == kTypeF32) return static_cast<const float*>(p.ptr)[i];
-    if (p.type == kTypeF16) return __half2float(static_cast<const __half*>(p.ptr)[i]);
-    return __bfloat162float(static_cast<const __nv_bfloat16*>(p.ptr)[i]);
-}
 // blockDim = (32 columns, kSlotLanes): lane l of a column adds slots l, l + kSlotLanes, ...; lane 0 adds the lanes' sums in order.
 constexpr int kSlotLanes = 16;
 __global__ void __launch_bounds__(32 * kSlotLanes) norm_vector_gradients(const __grid_constant__ NormVecGrads p) {

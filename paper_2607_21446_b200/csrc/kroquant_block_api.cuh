@@ -200,12 +200,13 @@ NormShape forward_shape(int d) {
     if (groups <= 128) return {32, 8, groups <= 32 ? 1 : (groups <= 64 ? 2 : 4)};
     return {((groups + 1) / 2 + 31) / 32 * 32, 1, 2};
 }
-// Backward: one warp per row for d <= 512, else one CTA per row: two groups per thread up to d = 9216 (576 threads), four above.
-NormShape backward_shape(int d) {
+// Backward: one warp per row for d <= 512, else one group per thread in one CTA per row, above d = 4608 in a cluster of two or four.
+NormShape backward_shape(int d, int* cluster) {
     const int groups = (d + 7) / 8;
+    *cluster = 1;
     if (groups <= 64) return {32, 8, groups <= 32 ? 1 : 2};
-    const int vpt = groups <= 2 * 576 ? 2 : 4;
-    return {((groups + vpt - 1) / vpt + 31) / 32 * 32, 1, vpt};
+    while (groups > *cluster * kq::kNormThreads) *cluster *= 2;
+    return {((groups + *cluster - 1) / *cluster + 31) / 32 * 32, 1, 1};
 }
 bool vec_row(const void* p, int64_t ld, int type) { return rows_aligned(p, ld, type, 16); }
 
@@ -257,40 +258,39 @@ kq_status_t launch_norm_forward(const kq::NormForward& p, cudaStream_t st) {
 struct NormWorkers {
     NormShape shape;
     int64_t workers, rows_per_worker, batches;
-    int smem;                   // dynamic shared memory (staged kernel)
+    int cluster, smem;          // CTAs of a worker and dynamic shared memory (staged kernel)
 };
 constexpr int kSmemPerSm = 228 * 1024, kSmemPerCta = 227 * 1024;
 
 NormWorkers norm_workers(const kq_norm_args_t& a, int sms, kq::NormBackward* p) {
     NormWorkers w = {};
-    w.shape = backward_shape(a.d);
+    w.shape = backward_shape(a.d, &w.cluster);
     int per_sm = 8;             // 8 CTAs of 256 threads: two warps per scheduler and more hide the loads of a warp's row
     if (w.shape.rows == 1) {
-        // registers let 576 (two groups per thread) or 512 threads run on an SM
-        per_sm = (w.shape.vpt == 2 ? 576 : 512) / w.shape.threads;
+        per_sm = kq::kNormThreads / w.shape.threads;                 // what the registers let run on an SM
         if (per_sm > 8) per_sm = 8;
-        const int ss = type_size(a.stream_dtype), sb = type_size(a.branch_dtype), padded = (a.d + 7) / 8 * 8;
+        const int columns = ((a.d + 7) / 8 + w.cluster - 1) / w.cluster * 8;      // of a CTA; the last one's may be fewer
+        const int ss = type_size(a.stream_dtype), sb = type_size(a.branch_dtype);
         const bool post = a.y && a.post_norm != KQ_NORM_NONE, dn = a.norm != KQ_NORM_NONE;
-        // the second phase's values take the place of h and dh: both rows must exist
-        // (a 32-bit stream has the room in h's row alone); four 32-bit rows above d = 14000 do not fit, then dh, which is
-        // read once, is not staged
-        const int room = (per_sm == 1 ? kSmemPerCta : kSmemPerSm / per_sm - 1024) - kq::kNormHeadBytes;
-        const bool fits = padded * (2 * ss + (dn ? sb : 0) + (a.y ? sb : 0)) <= room;
-        const int stage_dh = a.dh && fits ? 1 : 0, rows_s = stage_dh || (post && ss == 2) ? 2 : 1;
-        const int off_dh = padded * ss, off_dn = off_dh * rows_s;
-        const int off_y = off_dn + (dn ? padded * sb : 0), stage = off_y + (a.y ? padded * sb : 0);
-        int cache_m = dn && (a.weight || a.scale) ? 1 : 0, cache_gate = a.y && a.gate ? 1 : 0, cache_post = post && a.post_weight ? 1 : 0;
-        int params = 4 * padded * (cache_m + cache_gate + cache_post);
-        if (params + 2 * stage > room) params = cache_m = cache_gate = cache_post = 0;    // rows in flight come first
-        int stages = (room - params) / stage;
-        stages = stages < 1 ? 1 : (stages > kq::kNormStageMax ? kq::kNormStageMax : stages);
+        // the second phase's values take the place of h and dh: both rows must exist (a 32-bit stream has the room in h's)
+        const int rows_s = a.dh || (post && ss == 2) ? 2 : 1;
+        const int off_dh = columns * ss, off_dn = off_dh * rows_s;
+        const int off_y = off_dn + (dn ? columns * sb : 0), stage = off_y + (a.y ? columns * sb : 0);
+        const int cache_m = dn && (a.weight || a.scale) ? 1 : 0, cache_gate = a.y && a.gate ? 1 : 0, cache_post = post && a.post_weight ? 1 : 0;
+        const int params = 4 * columns * (cache_m + cache_gate + cache_post);
+        auto room = [&]() { return (per_sm == 1 ? kSmemPerCta : kSmemPerSm / per_sm - 1024) - kq::kNormHeadBytes; };
+        // two stages at least: 4608 columns of four 32-bit rows, twice, and three vectors are 198 KB
+        while (per_sm > 1 && params + 2 * stage > room()) --per_sm;
+        int stages = (room() - params) / stage;
+        stages = stages > kq::kNormStageMax ? kq::kNormStageMax : stages;
         w.smem = kq::kNormHeadBytes + params + stages * stage;
         if (p) {
-            p->stages = stages; p->stage_bytes = stage; p->stage_dh = stage_dh; p->off_dh = off_dh; p->off_dn = off_dn; p->off_y = off_y;
+            p->cluster = w.cluster; p->columns = columns; p->stages = stages; p->stage_bytes = stage;
+            p->off_dh = off_dh; p->off_dn = off_dn; p->off_y = off_y;
             p->cache_m = cache_m; p->cache_gate = cache_gate; p->cache_post = cache_post;
         }
     }
-    const int64_t most = (int64_t)(sms > 0 ? sms : 1) * per_sm * w.shape.rows;
+    const int64_t most = (int64_t)(sms > 1 ? sms : 2) * per_sm * w.shape.rows / w.cluster;
     w.rows_per_worker = (a.rows + most - 1) / most;
     if (w.rows_per_worker < 1) w.rows_per_worker = 1;
     w.workers = (a.rows + w.rows_per_worker - 1) / w.rows_per_worker;
@@ -299,11 +299,11 @@ NormWorkers norm_workers(const kq_norm_args_t& a, int sms, kq::NormBackward* p) 
 }
 bool wants_vector_gradients(const kq_norm_args_t& a) { return a.dgate || a.dpost_weight || a.dweight || a.dscale || a.dshift; }
 
-template <typename S, typename Y, int VPT>
+template <typename S, typename Y, bool POST>
 kq_status_t launch_norm_staged(const kq::NormBackward& p, const NormWorkers& w, cudaStream_t st) {
     static DeviceOnce attr_done;
     if (attr_done.needed()) {
-        if (cudaFuncSetAttribute(kq::norm_residual_backward<S, Y, VPT>, cudaFuncAttributeMaxDynamicSharedMemorySize, kSmemPerCta) != cudaSuccess) {
+        if (cudaFuncSetAttribute(kq::norm_residual_backward<S, Y, POST>, cudaFuncAttributeMaxDynamicSharedMemorySize, kSmemPerCta) != cudaSuccess) {
             (void)cudaGetLastError();
             return KQ_ERR_CUDA;
         }
@@ -311,12 +311,12 @@ kq_status_t launch_norm_staged(const kq::NormBackward& p, const NormWorkers& w, 
     }
     cudaLaunchConfig_t cfg;
     cudaLaunchAttribute attr[2];
-    launch_config(&cfg, attr, dim3((unsigned)w.workers), dim3((unsigned)w.shape.threads), (size_t)w.smem, 1, st);
-    return launch(cfg, kq::norm_residual_backward<S, Y, VPT>, p);
+    launch_config(&cfg, attr, dim3((unsigned)(w.workers * w.cluster)), dim3((unsigned)w.shape.threads), (size_t)w.smem, w.cluster, st);
+    return launch(cfg, kq::norm_residual_backward<S, Y, POST>, p);
 }
 template <typename S, typename Y>
 kq_status_t launch_norm_backward(const kq::NormBackward& p, const NormWorkers& w, cudaStream_t st) {
-    if (w.shape.rows == 1) return w.shape.vpt == 2 ? launch_norm_staged<S, Y, 2>(p, w, st) : launch_norm_staged<S, Y, 4>(p, w, st);
+    if (w.shape.rows == 1) return p.y && p.post != KQ_NORM_NONE ? launch_norm_staged<S, Y, true>(p, w, st) : launch_norm_staged<S, Y, false>(p, w, st);
     cudaLaunchConfig_t cfg;
     cudaLaunchAttribute attr[2];
     launch_config(&cfg, attr, dim3((unsigned)((w.workers + w.shape.rows - 1) / w.shape.rows)),
