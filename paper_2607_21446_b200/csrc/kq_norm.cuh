@@ -295,7 +295,7 @@ __global__ void __launch_bounds__(VPT == 2 ? 1024 : 256) norm_residual_forward(c
                     if (i < count[k]) s[0] = fmaf(v[i] - mean_y, v[i] - mean_y, s[0]);
             }
         row_sum<1>(s, red, phase);
-        inv_y = 1.0f / sqrtf(s[0] * inv_d + p.eps);
+        inv_y = rsqrtf(s[0] * inv_d + p.eps);
     }
 #pragma unroll
     for (int k = 0; k < VPT; ++k) {
@@ -340,7 +340,7 @@ __global__ void __launch_bounds__(VPT == 2 ? 1024 : 256) norm_residual_forward(c
         for (int i = 0; i < 8; ++i)
             if (i < count[k]) s[0] = fmaf(h[k][i] - mean, h[k][i] - mean, s[0]);
     row_sum<1>(s, red, phase);
-    const float inv = 1.0f / sqrtf(s[0] * inv_d + p.eps);
+    const float inv = rsqrtf(s[0] * inv_d + p.eps);
 #pragma unroll
     for (int k = 0; k < VPT; ++k)
         if (count[k] > 0) {
@@ -480,9 +480,9 @@ __global__ void __launch_bounds__(256) norm_residual_backward_warp(const NormBac
                     }
             }
         warp_sum4(sq, lane);
-        const float inv_h = 1.0f / sqrtf(sq[0] * inv_d + p.eps);
+        const float inv_h = rsqrtf(sq[0] * inv_d + p.eps);
         const float along_h = sq[1] * inv_d * inv_h;
-        const float inv_y = post ? 1.0f / sqrtf(sq[2] * inv_d + p.eps) : 1.f;
+        const float inv_y = post ? rsqrtf(sq[2] * inv_d + p.eps) : 1.f;
         float back[4] = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
         for (int k = 0; k < VPT; ++k)
@@ -544,13 +544,13 @@ __global__ void __launch_bounds__(256) norm_residual_backward_warp(const NormBac
 // With 18 warps on an SM the instructions bound the kernel next to memory, so the arithmetic is done on pairs (f32x2).
 // Parameter vectors (weight (1 + scale), gate, post_weight) are kept in shared memory as floats, refreshed at the start of a batch.
 // Rows that bulk copies cannot take (16-byte alignment) are copied into the same place by the threads, element by element.
-constexpr int kNormStageMax = 4;
+constexpr int kNormStageMax = 6;
 constexpr int kNormThreads = 576;
 constexpr int kNormColumns = 8 * kNormThreads;                      // of a CTA
 constexpr int kNormMaxCluster = 4;
 constexpr int kNormRedOff = 128;                                    // barriers and the abort word in front
 constexpr int kNormRedFloats = kNormMaxCluster * (kNormThreads / 32) * 8;
-constexpr int kNormHeadBytes = kNormRedOff + 3 * kNormRedFloats * 4;   // two sets of statistics used in turn, one of the second phase
+constexpr int kNormHeadBytes = kNormRedOff + 4 * kNormRedFloats * 4;   // two sets of statistics used in turn, two of the second phase
 
 typedef unsigned long long f32x2;
 __device__ __forceinline__ f32x2 pack2(float a, float b) {
@@ -590,19 +590,7 @@ __device__ __forceinline__ f32x2 widen2(uint32_t w) {
         return pack2(bf16lo_to_f32(w), bf16hi_to_f32(w));
     }
 }
-// elements 4 quad .. 4 quad + 3 of a row in shared memory
-template <typename T>
-__device__ __forceinline__ void lds4(const uint8_t* row, int quad, f32x2 (&v)[2]) {
-    if constexpr (sizeof(T) == 4) {
-        const ulonglong2 a = reinterpret_cast<const ulonglong2*>(row)[quad];
-        v[0] = a.x;
-        v[1] = a.y;
-    } else {
-        const uint2 a = reinterpret_cast<const uint2*>(row)[quad];
-        v[0] = widen2<T>(a.x);
-        v[1] = widen2<T>(a.y);
-    }
-}
+// the eight elements of a group of a row in shared memory
 template <typename T>
 __device__ __forceinline__ void lds8(const uint8_t* row, int group, f32x2 (&v)[4]) {
     if constexpr (sizeof(T) == 4) {
@@ -613,29 +601,16 @@ __device__ __forceinline__ void lds8(const uint8_t* row, int group, f32x2 (&v)[4
         v[0] = widen2<T>(a.x); v[1] = widen2<T>(a.y); v[2] = widen2<T>(a.z); v[3] = widen2<T>(a.w);
     }
 }
-__device__ __forceinline__ void sts_floats(float* at, const float (&v)[8]) {
-    reinterpret_cast<float4*>(at)[0] = make_float4(v[0], v[1], v[2], v[3]);
-    reinterpret_cast<float4*>(at)[1] = make_float4(v[4], v[5], v[6], v[7]);
-}
 template <typename T>
-__device__ __forceinline__ void store4(T* p, int count, bool vec, const f32x2 (&w)[2]) {
-    const float2 a = unpack2(w[0]), b = unpack2(w[1]);
-    if (vec) {
-        if constexpr (sizeof(T) == 4) {
-            *reinterpret_cast<float4*>(p) = make_float4(a.x, a.y, b.x, b.y);
-        } else if constexpr (__is_same(T, __half)) {
-            const __half2 x = __floats2half2_rn(a.x, a.y), y = __floats2half2_rn(b.x, b.y);
-            *reinterpret_cast<uint2*>(p) = make_uint2(*reinterpret_cast<const uint32_t*>(&x), *reinterpret_cast<const uint32_t*>(&y));
-        } else {
-            const __nv_bfloat162 x = __floats2bfloat162_rn(a.x, a.y), y = __floats2bfloat162_rn(b.x, b.y);
-            *reinterpret_cast<uint2*>(p) = make_uint2(*reinterpret_cast<const uint32_t*>(&x), *reinterpret_cast<const uint32_t*>(&y));
-        }
-    } else {
-        const float v[4] = {a.x, a.y, b.x, b.y};
+__device__ __forceinline__ void store_pairs(T* p, int count, bool vec, const f32x2 (&w)[4]) {
+    float v[8];
 #pragma unroll
-        for (int i = 0; i < 4; ++i)
-            if (i < count) p[i] = Elem<T>::from_f32(v[i]);
+    for (int i = 0; i < 4; ++i) {
+        const float2 f = unpack2(w[i]);
+        v[2 * i] = f.x;
+        v[2 * i + 1] = f.y;
     }
+    store8(p, count, vec, 1, v);
 }
 // `d` columns of the four rows of an iteration that are not 16-byte aligned, into shared memory: sixteen loads in flight per
 // thread; the tail of the last group is 0
@@ -728,12 +703,7 @@ __global__ void __launch_bounds__(kNormThreads, 1) norm_residual_backward(const 
         float* out = p.partial + slot * 3 * p.d + c0 + c;
 #pragma unroll
         for (int q = 0; q < 3; ++q)
-#pragma unroll
-            for (int half = 0; half < 2; ++half)
-                if (count > 4 * half) {
-                    const f32x2 v[2] = {sum[q][2 * half], sum[q][2 * half + 1]};
-                    store4(out + (int64_t)q * p.d + 4 * half, count - 4 * half, vec, v);
-                }
+            if (count > 0) store_pairs(out + (int64_t)q * p.d, count, vec, sum[q]);
         clear();
     };
     clear();
@@ -741,6 +711,10 @@ __global__ void __launch_bounds__(kNormThreads, 1) norm_residual_backward(const 
     // rows of this worker before the next batch begins
     auto rows_left = [&](int64_t row) { const int64_t n = (batch + 1) * p.rows_per_batch - row; return (int)(n < rows ? n : rows); };
     int batch_end = rows_left(first);
+    auto keep = [&](float* vector, const float (&v)[8]) {
+        reinterpret_cast<float4*>(vector)[t] = make_float4(v[0], v[1], v[2], v[3]);
+        reinterpret_cast<float4*>(vector + (p.columns >> 1))[t] = make_float4(v[4], v[5], v[6], v[7]);
+    };
     auto refresh = [&]() {
         if (count > 0) {
             float m[8], a[8];
@@ -749,24 +723,30 @@ __global__ void __launch_bounds__(kNormThreads, 1) norm_residual_backward(const 
                 load_param(p.scale, batch, c0 + c, count, vec, 1, 0.f, a);
 #pragma unroll
                 for (int i = 0; i < 8; ++i) m[i] = fmaf(m[i], a[i], m[i]);
-                sts_floats(par_m + c, m);
+                keep(par_m, m);
             }
             if (p.cache_gate) {
                 load_param(p.gate, batch, c0 + c, count, vec, 1, 1.f, m);
-                sts_floats(par_gate + c, m);
+                keep(par_gate, m);
             }
             if (p.cache_post) {
                 load_param(p.post_weight, 0, c0 + c, count, vec, 1, 1.f, m);
-                sts_floats(par_post + c, m);
+                keep(par_post, m);
             }
         }
     };
     refresh();
+    __syncthreads();
     const f32x2 one2 = pack2(1.f, 1.f), alpha2 = pack2(p.alpha, p.alpha);
-    auto parameters = [&](int have, const float* at, f32x2 (&m)[2]) {
-        const ulonglong2 w = have ? *reinterpret_cast<const ulonglong2*>(at) : make_ulonglong2(one2, one2);
-        m[0] = w.x;
-        m[1] = w.y;
+    // a vector lies in two planes, the first and the last four entries of every group (no bank conflicts either way)
+    const int plane = p.columns >> 1;
+    auto parameters = [&](int have, const float* vector, int group, f32x2 (&m)[4]) {
+        ulonglong2 a = make_ulonglong2(one2, one2), b = a;
+        if (have) {
+            a = reinterpret_cast<const ulonglong2*>(vector)[group];
+            b = reinterpret_cast<const ulonglong2*>(vector + plane)[group];
+        }
+        m[0] = a.x; m[1] = a.y; m[2] = b.x; m[3] = b.y;
     };
     // the mean of 32 values spread over this CTA's columns of a row, the same in every warp (the CTAs of a cluster use their own)
     auto pivot_of = [&](float v) {
@@ -777,106 +757,130 @@ __global__ void __launch_bounds__(kNormThreads, 1) norm_residual_backward(const 
     const int sample = (int)((int64_t)lane * d / 32);
     S* dx = static_cast<S*>(p.dx) + first * p.ld_dx + c0 + c;
     Y* dy = static_cast<Y*>(p.dy) + first * p.ld_dy + c0 + c;
-    int s = 0;
-    uint32_t parity = 0;
-    for (int r = 0; r < rows; ++r) {
-        uint8_t* stage = smem + stage0 + s * p.stage_bytes;
+    int s = 0, next = p.stages < rows ? p.stages : rows;              // stage of row r; next row to be fetched (thread 0)
+    uint32_t parity = 0, turn = 0;
+    for (int r = 0, nr; r < rows; r += nr) {
         if (r == batch_end) {
+            __syncthreads();                                          // other threads read this thread's parameters too
             if (p.partial) flush(worker + batch);
             ++batch;
             batch_end = r + rows_left(first + r);
             refresh();
+            __syncthreads();
         }
+        // two rows of one batch at a time where the stages leave two more in flight
+        nr = p.stages >= 4 && r + 1 < rows && r + 1 < batch_end ? 2 : 1;
+        uint8_t* stages[2];
+        stages[0] = smem + stage0 + s * p.stage_bytes;
+        stages[1] = smem + stage0 + (s + 1 < p.stages ? s + 1 : 0) * p.stage_bytes;
         if (vec) {
             // a wait that gives up records it and goes on (the barriers below stay matched)
-            if (!mbar_wait(base + 8u * s, parity, abort_flag) && !*abort_flag) {
+            bool ok = mbar_wait(base + 8u * s, parity, abort_flag);
+            if (nr == 2) ok = ok && mbar_wait(base + 8u * (s + 1 < p.stages ? s + 1 : 0), s + 1 < p.stages ? parity : parity ^ 1u, abort_flag);
+            if (!ok && !*abort_flag) {
                 atomicExch(&g_kq_device_error, KQ_DEV_TIMEOUT_NORM);
                 *abort_flag = 1;
             }
         } else {
             __syncthreads();
-            copy_rows<S, Y>(stage, p, first + r, c0, d);
+            for (int j = 0; j < nr; ++j) copy_rows<S, Y>(stages[j], p, first + r + j, c0, d);
             __syncthreads();
         }
-        // ---- statistics ----
-        float pivot_h = 0.f, pivot_y = 0.f;
-        if (layer_h) pivot_h = pivot_of(Elem<S>::to_f32(reinterpret_cast<const S*>(stage)[sample]));
-        if (layer_y) pivot_y = pivot_of(Elem<Y>::to_f32(reinterpret_cast<const Y*>(stage + p.off_y)[sample]));
-        float st[4] = {0.f, 0.f, 0.f, 0.f}, sty[4] = {0.f, 0.f, 0.f, 0.f};       // s1, s2, sum g, sum g (h - p) of h; s1, s2 of y
-        if (count == 8) {
-            if (norm) {
-                const f32x2 minus = pack2(-pivot_h, -pivot_h);
-                f32x2 v[4], g[4], m[2], s1 = 0ull, s2 = 0ull, g0 = 0ull, g1 = 0ull;
-                lds8<S>(stage, t, v);
-                lds8<Y>(stage + p.off_dn, t, g);
+        // ---- statistics: with two rows, half of the warps take one row each and a warp 512 columns, else 256 ----
+        const int per_row = nr == 2 ? warps >> 1 : warps;
+        const int my_row = nr == 2 && warp >= per_row ? 1 : 0, part = warp - my_row * per_row;
+        {
+            const uint8_t* stage = my_row ? stages[1] : stages[0];
+            float pivot_h = 0.f, pivot_y = 0.f;
+            if (layer_h) pivot_h = pivot_of(Elem<S>::to_f32(reinterpret_cast<const S*>(stage)[sample]));
+            if (layer_y) pivot_y = pivot_of(Elem<Y>::to_f32(reinterpret_cast<const Y*>(stage + p.off_y)[sample]));
+            const f32x2 minus_h = pack2(-pivot_h, -pivot_h), minus_y = pack2(-pivot_y, -pivot_y);
+            f32x2 s1 = 0ull, s2 = 0ull, g0 = 0ull, g1 = 0ull, y1 = 0ull, y2 = 0ull;
+#pragma unroll 2
+            for (int k = 0; k < nr; ++k) {
+                const int gi = (part * nr + k) * 32 + lane, have = owned(d, gi * 8, 1);
+                if (have == 8) {
+                    if (norm) {
+                        f32x2 v[4], g[4], m[4];
+                        lds8<S>(stage, gi, v);
+                        lds8<Y>(stage + p.off_dn, gi, g);
+                        parameters(p.cache_m, par_m, gi, m);
 #pragma unroll
-                for (int half = 0; half < 2; ++half) {
-                    parameters(p.cache_m, par_m + c + 4 * half, m);
+                        for (int i = 0; i < 4; ++i) {
+                            const f32x2 u = add2(v[i], minus_h), w = mul2(g[i], m[i]);
+                            s1 = add2(s1, u);
+                            s2 = fma2(u, u, s2);
+                            g0 = add2(g0, w);
+                            g1 = fma2(w, u, g1);
+                        }
+                    }
+                    if (POST) {
+                        f32x2 v[4];
+                        lds8<Y>(stage + p.off_y, gi, v);
 #pragma unroll
-                    for (int i = 0; i < 2; ++i) {
-                        const f32x2 u = add2(v[2 * half + i], minus), w = mul2(g[2 * half + i], m[i]);
-                        s1 = add2(s1, u);
-                        s2 = fma2(u, u, s2);
-                        g0 = add2(g0, w);
-                        g1 = fma2(w, u, g1);
+                        for (int i = 0; i < 4; ++i) {
+                            const f32x2 u = add2(v[i], minus_y);
+                            y1 = add2(y1, u);
+                            y2 = fma2(u, u, y2);
+                        }
+                    }
+                } else {                                             // the ragged end of a row: one thread, one by one
+#pragma unroll 1
+                    for (int i = gi * 8; i < gi * 8 + have; ++i) {
+                        if (norm) {
+                            const float u = Elem<S>::to_f32(reinterpret_cast<const S*>(stage)[i]) - pivot_h;
+                            const float w = Elem<Y>::to_f32(reinterpret_cast<const Y*>(stage + p.off_dn)[i]) * (p.cache_m ? par_m[(i & 4 ? plane : 0) + (i >> 3) * 4 + (i & 3)] : 1.f);
+                            s1 = add2(s1, pack2(u, 0.f));
+                            s2 = add2(s2, pack2(u * u, 0.f));
+                            g0 = add2(g0, pack2(w, 0.f));
+                            g1 = add2(g1, pack2(w * u, 0.f));
+                        }
+                        if (POST) {
+                            const float u = Elem<Y>::to_f32(reinterpret_cast<const Y*>(stage + p.off_y)[i]) - pivot_y;
+                            y1 = add2(y1, pack2(u, 0.f));
+                            y2 = add2(y2, pack2(u * u, 0.f));
+                        }
                     }
                 }
-                st[0] = sum2(s1); st[1] = sum2(s2); st[2] = sum2(g0); st[3] = sum2(g1);
             }
-            if (POST) {
-                const f32x2 minus = pack2(-pivot_y, -pivot_y);
-                f32x2 v[4], s1 = 0ull, s2 = 0ull;
-                lds8<Y>(stage + p.off_y, t, v);
-#pragma unroll
-                for (int i = 0; i < 4; ++i) {
-                    const f32x2 u = add2(v[i], minus);
-                    s1 = add2(s1, u);
-                    s2 = fma2(u, u, s2);
-                }
-                sty[0] = sum2(s1); sty[1] = sum2(s2);
+            float st[4] = {sum2(s1), sum2(s2), sum2(g0), sum2(g1)}, sty[4] = {sum2(y1), sum2(y2), 0.f, 0.f};
+            warp_sum4(st, lane);
+            if (POST) warp_sum4(sty, lane);
+            if (lane == 0) {
+                float* at = red + turn * kNormRedFloats + (my_row * p.cluster * per_row + rank * per_row + part) * 8;
+                exchange(at, make_float4(st[0], st[1], st[2], st[3]));
+                exchange(at + 4, make_float4(sty[0], sty[1], pivot_h, pivot_y));
             }
-        } else {                                                     // the ragged end of a row: one thread, one by one
-#pragma unroll 1
-            for (int i = 0; i < count; ++i) {
-                if (norm) {
-                    const float u = Elem<S>::to_f32(reinterpret_cast<const S*>(stage)[c + i]) - pivot_h;
-                    const float w = Elem<Y>::to_f32(reinterpret_cast<const Y*>(stage + p.off_dn)[c + i]) * (p.cache_m ? par_m[c + i] : 1.f);
-                    st[0] += u; st[1] = fmaf(u, u, st[1]); st[2] += w; st[3] = fmaf(w, u, st[3]);
-                }
-                if (POST) {
-                    const float u = Elem<Y>::to_f32(reinterpret_cast<const Y*>(stage + p.off_y)[c + i]) - pivot_y;
-                    sty[0] += u; sty[1] = fmaf(u, u, sty[1]);
-                }
-            }
-        }
-        warp_sum4(st, lane);
-        if (POST) warp_sum4(sty, lane);
-        float* exchanged = red + (r & 1) * kNormRedFloats;           // the row before may still be read
-        if (lane == 0) {
-            exchange(exchanged + my_warp * 8, make_float4(st[0], st[1], st[2], st[3]));
-            if (POST || p.cluster > 1) exchange(exchanged + my_warp * 8 + 4, make_float4(sty[0], sty[1], pivot_h, pivot_y));
         }
         barrier();
-        // every thread is done with the row before: its slot takes the row `stages` further on
-        if (vec && t == 0 && r > 0 && r - 1 + p.stages < rows) issue(r - 1 + p.stages, s == 0 ? p.stages - 1 : s - 1);
-        st[0] = st[1] = st[2] = st[3] = sty[0] = sty[1] = sty[2] = sty[3] = 0.f;
+        // every thread is done with the rows before r: their stages take the rows that follow
+        if (vec && t == 0)
+            for (; next < rows && next < r + p.stages; ++next) issue(next, next % p.stages);
+        const float* exchanged = red + turn * kNormRedFloats;        // (the other set may be written before all have read this one)
+        turn ^= 1u;
+#pragma unroll 1
+        for (int j = 0; j < nr; ++j) {
+        uint8_t* stage = j ? stages[1] : stages[0];
+        const float* of_row = exchanged + j * p.cluster * per_row * 8;
+        const float pivot_h = of_row[6], pivot_y = of_row[7];
+        float st[4] = {0.f, 0.f, 0.f, 0.f}, sty[4] = {0.f, 0.f, 0.f, 0.f};
         if (p.cluster == 1) {
-            if (lane < warps) {
-                const float4 a = reinterpret_cast<const float4*>(exchanged + lane * 8)[0];
+            if (lane < per_row) {
+                const float4 a = reinterpret_cast<const float4*>(of_row + lane * 8)[0];
                 st[0] = a.x; st[1] = a.y; st[2] = a.z; st[3] = a.w;
                 if (POST) {
-                    const float2 b = reinterpret_cast<const float2*>(exchanged + lane * 8)[2];
+                    const float2 b = reinterpret_cast<const float2*>(of_row + lane * 8)[2];
                     sty[0] = b.x; sty[1] = b.y;
                 }
             }
         } else {
             // every CTA summed about its own pivot: moved to that of rank 0, s1 + n e, s2 + 2 e s1 + n e^2, g1 + e g0
-            const float ph = exchanged[6], py = exchanged[7];
-            for (int w = lane; w < all_warps; w += 32) {
-                const float4 a = reinterpret_cast<const float4*>(exchanged + w * 8)[0], b = reinterpret_cast<const float4*>(exchanged + w * 8)[1];
-                const int q = w / warps, left = (p.d - q * p.columns < p.columns ? p.d - q * p.columns : p.columns) - (w - q * warps) * 256;
-                const float n = (float)(left < 0 ? 0 : (left > 256 ? 256 : left));
-                const float eh = b.z - ph, ey = b.w - py;
+            for (int w = lane; w < p.cluster * per_row; w += 32) {
+                const float4 a = reinterpret_cast<const float4*>(of_row + w * 8)[0], b = reinterpret_cast<const float4*>(of_row + w * 8)[1];
+                const int q = w / per_row, all = p.d - q * p.columns < p.columns ? p.d - q * p.columns : p.columns;
+                const int left = all - (w - q * per_row) * 256 * nr;
+                const float n = (float)(left < 0 ? 0 : (left > 256 * nr ? 256 * nr : left));
+                const float eh = b.z - pivot_h, ey = b.w - pivot_y;
                 st[0] += fmaf(n, eh, a.x);
                 st[1] += fmaf(eh, fmaf(n, eh, 2.f * a.x), a.y);
                 st[2] += a.z;
@@ -884,8 +888,6 @@ __global__ void __launch_bounds__(kNormThreads, 1) norm_residual_backward(const 
                 sty[0] += fmaf(n, ey, b.x);
                 sty[1] += fmaf(ey, fmaf(n, ey, 2.f * b.x), b.y);
             }
-            pivot_h = ph;
-            pivot_y = py;
         }
         warp_sum4(st, lane);
         if (POST) warp_sum4(sty, lane);
@@ -893,67 +895,59 @@ __global__ void __launch_bounds__(kNormThreads, 1) norm_residual_backward(const 
         const float shift_h = layer_h ? st[0] * inv_d : 0.f, shift_y = layer_y ? sty[0] * inv_d : 0.f;
         const float mean_h = pivot_h + shift_h, mean_y = pivot_y + shift_y, mean_g = layer_h ? st[2] * inv_d : 0.f;
         // ---- gradients: H = dh + inv_h (g m - mean_g - xhat along_h) ----
-        const float inv_h = norm ? 1.0f / sqrtf(fmaf(st[1], inv_d, -shift_h * shift_h) + p.eps) : 0.f;
+        const float inv_h = norm ? rsqrtf(fmaf(st[1], inv_d, -shift_h * shift_h) + p.eps) : 0.f;
         const float along_h = fmaf(-shift_h, st[2], st[3]) * inv_d * inv_h;
-        const float inv_y = POST ? 1.0f / sqrtf(fmaf(sty[1], inv_d, -shift_y * shift_y) + p.eps) : 1.f;
+        const float inv_y = POST ? rsqrtf(fmaf(sty[1], inv_d, -shift_y * shift_y) + p.eps) : 1.f;
         const f32x2 inv_h2 = pack2(inv_h, inv_h), off_h2 = pack2(-mean_h, -mean_h), along2 = pack2(-along_h, -along_h), mean_g2 = pack2(-mean_g, -mean_g);
         const f32x2 inv_y2 = pack2(inv_y, inv_y), off_y2 = pack2(-mean_y, -mean_y);
         f32x2 back0 = 0ull, back1 = 0ull;
         if (count > 0) {
+            f32x2 H[4] = {0ull, 0ull, 0ull, 0ull}, v[4], m[4];
+            if (p.dh) lds8<S>(stage + p.off_dh, t, H);
+            if (norm) {
+                f32x2 g[4];
+                lds8<S>(stage, t, v);
+                lds8<Y>(stage + p.off_dn, t, g);
+                parameters(p.cache_m, par_m, t, m);
 #pragma unroll
-            for (int half = 0; half < 2; ++half) {
-                const int quad = 2 * t + half, left = count - 4 * half;
-                f32x2 H[2] = {0ull, 0ull}, v[2], m[2];
-                if (p.dh) lds4<S>(stage + p.off_dh, quad, H);
-                if (norm) {
-                    f32x2 g[2];
-                    lds4<S>(stage, quad, v);
-                    lds4<Y>(stage + p.off_dn, quad, g);
-                    parameters(p.cache_m, par_m + c + 4 * half, m);
-#pragma unroll
-                    for (int i = 0; i < 2; ++i) {
-                        const f32x2 xhat = mul2(add2(v[i], off_h2), inv_h2);
-                        sum[0][2 * half + i] = fma2(g[i], xhat, sum[0][2 * half + i]);
-                        sum[1][2 * half + i] = add2(sum[1][2 * half + i], g[i]);
-                        H[i] = fma2(inv_h2, fma2(xhat, along2, fma2(g[i], m[i], mean_g2)), H[i]);
-                    }
+                for (int i = 0; i < 4; ++i) {
+                    const f32x2 xhat = mul2(add2(v[i], off_h2), inv_h2);
+                    sum[0][i] = fma2(g[i], xhat, sum[0][i]);
+                    sum[1][i] = add2(sum[1][i], g[i]);
+                    H[i] = fma2(inv_h2, fma2(xhat, along2, fma2(g[i], m[i], mean_g2)), H[i]);
                 }
-                v[0] = mul2(alpha2, H[0]);
-                v[1] = mul2(alpha2, H[1]);
-                store4(dx + 4 * half, left, vec, v);
-                if (p.y) {
-                    lds4<Y>(stage + p.off_y, quad, v);
-                    parameters(p.cache_gate, par_gate + c + 4 * half, m);
-                    if (!POST) {
+            }
 #pragma unroll
-                        for (int i = 0; i < 2; ++i) {
-                            sum[2][2 * half + i] = fma2(H[i], v[i], sum[2][2 * half + i]);
-                            H[i] = mul2(H[i], m[i]);
-                        }
-                        store4(dy + 4 * half, left, vec, H);
-                    } else {
-                        f32x2 w[2];
-                        parameters(p.cache_post, par_post + c + 4 * half, w);
-                        if (left < 4) {                                            // nothing beyond the row in the sums below
-                            H[0] = pack2(left > 0 ? unpack2(H[0]).x : 0.f, left > 1 ? unpack2(H[0]).y : 0.f);
-                            H[1] = pack2(left > 2 ? unpack2(H[1]).x : 0.f, 0.f);
-                        }
+            for (int i = 0; i < 4; ++i) v[i] = mul2(alpha2, H[i]);
+            store_pairs(dx, count, vec, v);
+            if (p.y) {
+                lds8<Y>(stage + p.off_y, t, v);
+                parameters(p.cache_gate, par_gate, t, m);
+                if (!POST) {
 #pragma unroll
-                        for (int i = 0; i < 2; ++i) {
-                            const f32x2 yhat = mul2(add2(v[i], off_y2), inv_y2);
-                            sum[2][2 * half + i] = fma2(H[i], yhat, sum[2][2 * half + i]);
-                            H[i] = mul2(mul2(H[i], m[i]), w[i]);                   // the gradient at yhat
-                            back0 = add2(back0, H[i]);
-                            back1 = fma2(H[i], yhat, back1);
-                        }
-                        // kept for the second phase in the place of these channels' h (32 bits) or h and dh (16), which have been read
-                        if constexpr (sizeof(S) == 4) {
-                            reinterpret_cast<ulonglong2*>(stage)[quad] = make_ulonglong2(H[0], H[1]);
-                        } else {
-                            reinterpret_cast<f32x2*>(stage)[quad] = H[0];
-                            reinterpret_cast<f32x2*>(stage + p.off_dh)[quad] = H[1];
-                        }
+                    for (int i = 0; i < 4; ++i) {
+                        sum[2][i] = fma2(H[i], v[i], sum[2][i]);
+                        H[i] = mul2(H[i], m[i]);
                     }
+                    store_pairs(dy, count, vec, H);
+                } else {
+                    f32x2 w[4];
+                    parameters(p.cache_post, par_post, t, w);
+                    if (count < 8) {                                               // nothing beyond the row in the sums below
+#pragma unroll
+                        for (int i = 0; i < 4; ++i) H[i] = pack2(2 * i < count ? unpack2(H[i]).x : 0.f, 2 * i + 1 < count ? unpack2(H[i]).y : 0.f);
+                    }
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) {
+                        const f32x2 yhat = mul2(add2(v[i], off_y2), inv_y2);
+                        sum[2][i] = fma2(H[i], yhat, sum[2][i]);
+                        H[i] = mul2(mul2(H[i], m[i]), w[i]);                       // the gradient at yhat
+                        back0 = add2(back0, H[i]);
+                        back1 = fma2(H[i], yhat, back1);
+                    }
+                    // kept for the second phase in the place of these channels' h (32 bits) or h and dh (16), which have been read
+                    reinterpret_cast<ulonglong2*>(stage)[sizeof(S) == 4 ? 2 * t : t] = make_ulonglong2(H[0], H[1]);
+                    (sizeof(S) == 4 ? reinterpret_cast<ulonglong2*>(stage) + 2 * t + 1 : reinterpret_cast<ulonglong2*>(stage + p.off_dh) + t)[0] = make_ulonglong2(H[2], H[3]);
                 }
             }
         }
@@ -964,7 +958,7 @@ __global__ void __launch_bounds__(kNormThreads, 1) norm_residual_backward(const 
                 b0 += __shfl_xor_sync(0xFFFFFFFFu, b0, o);
                 b1 += __shfl_xor_sync(0xFFFFFFFFu, b1, o);
             }
-            float* at = red + 2 * kNormRedFloats;
+            float* at = red + (2 + j) * kNormRedFloats;
             if (lane == 0) exchange(at + my_warp * 4, make_float4(b0, b1, 0.f, 0.f));
             asm volatile("fence.proxy.async.shared::cta;" ::: "memory");     // the kept values lie where the next copy lands
             barrier();
@@ -982,29 +976,21 @@ __global__ void __launch_bounds__(kNormThreads, 1) norm_residual_backward(const 
             const float mean_a = layer_y ? b0 * inv_d : 0.f, along_y = b1 * inv_d;
             const f32x2 mean_a2 = pack2(-mean_a, -mean_a), along_y2 = pack2(-along_y, -along_y);
             if (count > 0) {
+                f32x2 v[4];
+                lds8<Y>(stage + p.off_y, t, v);
+                const ulonglong2 lo = reinterpret_cast<const ulonglong2*>(stage)[sizeof(S) == 4 ? 2 * t : t];
+                const ulonglong2 hi = (sizeof(S) == 4 ? reinterpret_cast<const ulonglong2*>(stage) + 2 * t + 1 : reinterpret_cast<const ulonglong2*>(stage + p.off_dh) + t)[0];
+                const f32x2 H[4] = {lo.x, lo.y, hi.x, hi.y};
 #pragma unroll
-                for (int half = 0; half < 2; ++half) {
-                    const int quad = 2 * t + half;
-                    f32x2 v[2], H[2];
-                    lds4<Y>(stage + p.off_y, quad, v);
-                    if constexpr (sizeof(S) == 4) {
-                        const ulonglong2 a = reinterpret_cast<const ulonglong2*>(stage)[quad];
-                        H[0] = a.x;
-                        H[1] = a.y;
-                    } else {
-                        H[0] = reinterpret_cast<const f32x2*>(stage)[quad];
-                        H[1] = reinterpret_cast<const f32x2*>(stage + p.off_dh)[quad];
-                    }
-#pragma unroll
-                    for (int i = 0; i < 2; ++i)
-                        v[i] = mul2(fma2(mul2(add2(v[i], off_y2), inv_y2), along_y2, add2(H[i], mean_a2)), inv_y2);
-                    store4(dy + 4 * half, count - 4 * half, vec, v);
-                }
+                for (int i = 0; i < 4; ++i)
+                    v[i] = mul2(fma2(mul2(add2(v[i], off_y2), inv_y2), along_y2, add2(H[i], mean_a2)), inv_y2);
+                store_pairs(dy, count, vec, v);
             }
         }
         dx += p.ld_dx;
         dy += p.ld_dy;
         if (++s == p.stages) { s = 0; parity ^= 1u; }
+        }
     }
     if (p.partial) flush(worker + batch);
     if (p.cluster > 1) cluster_barrier();                             // nobody's shared memory goes away while a peer writes to it

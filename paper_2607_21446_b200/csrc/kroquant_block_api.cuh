@@ -206,7 +206,7 @@ NormShape backward_shape(int d, int* cluster) {
     *cluster = 1;
     if (groups <= 64) return {32, 8, groups <= 32 ? 1 : 2};
     while (groups > *cluster * kq::kNormThreads) *cluster *= 2;
-    return {((groups + *cluster - 1) / *cluster + 31) / 32 * 32, 1, 1};
+    return {((groups + *cluster - 1) / *cluster + 63) / 64 * 64, 1, 1};        // an even number of warps
 }
 bool vec_row(const void* p, int64_t ld, int type) { return rows_aligned(p, ld, type, 16); }
 
