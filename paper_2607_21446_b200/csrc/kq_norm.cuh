@@ -221,11 +221,13 @@ __device__ __forceinline__ uint32_t cluster_rank() {
 __device__ __forceinline__ void cluster_barrier() {
     asm volatile("barrier.cluster.arrive.release.aligned;\n\tbarrier.cluster.wait.acquire.aligned;" ::: "memory");
 }
-// four floats to the same place in the shared memory of CTA `rank` of the cluster
-__device__ __forceinline__ void st_cluster_v4(uint32_t addr, uint32_t rank, const float4& v) {
-    asm volatile("{\n\t.reg .u32 a;\n\tmapa.shared::cluster.u32 a, %0, %1;\n\t"
-                 "st.shared::cluster.v4.f32 [a], {%2, %3, %4, %5};\n\t}"
-                 ::"r"(addr), "r"(rank), "f"(v.x), "f"(v.y), "f"(v.z), "f"(v.w) : "memory");
+// Four floats to the same place in the shared memory of CTA `rank` of the cluster, counted as 16 bytes on the mbarrier at the
+// same place there.  (A cluster barrier would order the exchange too, but its release waits for the global stores in
+// flight: 1.7 us per row.)
+__device__ __forceinline__ void st_async_v4(uint32_t addr, uint32_t bar, uint32_t rank, const float4& v) {
+    asm volatile("{\n\t.reg .u32 a, b;\n\tmapa.shared::cluster.u32 a, %0, %2;\n\tmapa.shared::cluster.u32 b, %1, %2;\n\t"
+                 "st.async.shared::cluster.mbarrier::complete_tx::bytes.v4.f32 [a], {%3, %4, %5, %6}, [b];\n\t}"
+                 ::"r"(addr), "r"(bar), "r"(rank), "f"(v.x), "f"(v.y), "f"(v.z), "f"(v.w) : "memory");
 }
 
 struct NormForward {
@@ -378,14 +380,17 @@ struct NormBackward {
 };
 
 // ---- backward, narrow rows: one warp per row --------------------------------------------------------
-// Worker w = blockIdx.x * blockDim.y + threadIdx.y takes rows [w rows_per_worker, ...); d <= 256 VPT, rows in registers.
+// A CTA of eight warps is a worker and takes the rows [blockIdx.x rows_per_worker, ...), its warps every eighth of them; d <= 256
+// VPT, rows in registers.  At the end of a batch the warps' column sums meet in shared memory and are added in warp order.
+constexpr int kNormWarps = 8;
+
 template <typename S, typename Y, int VPT>
-__global__ void __launch_bounds__(256) norm_residual_backward_warp(const NormBackward p) {
-    const int64_t worker = (int64_t)blockIdx.x * blockDim.y + threadIdx.y;
-    const int64_t first = worker * p.rows_per_worker;
+__global__ void __launch_bounds__(32 * kNormWarps) norm_residual_backward_warp(const __grid_constant__ NormBackward p) {
+    extern __shared__ float warp_sums[];                              // [warps][3][d]
+    const int64_t first = (int64_t)blockIdx.x * p.rows_per_worker;
     const int64_t last = first + p.rows_per_worker < p.rows ? first + p.rows_per_worker : p.rows;
     pdl_wait_prior_grid();
-    if (first >= last) return;
+    const int warp = (int)threadIdx.y;
     const int lane = (int)threadIdx.x;
     const bool vec = p.vec != 0;
     const float inv_d = 1.0f / (float)p.d;
@@ -396,29 +401,37 @@ __global__ void __launch_bounds__(256) norm_residual_backward_warp(const NormBac
 #pragma unroll
     for (int k = 0; k < VPT; ++k) count[k] = owned(p.d, column(k), step);
     float sum[3][VPT][8];
-    auto flush = [&](int64_t slot) {
-        float* out = p.partial + slot * 3 * p.d;
+    auto clear = [&]() {
 #pragma unroll
         for (int q = 0; q < 3; ++q)
 #pragma unroll
-            for (int k = 0; k < VPT; ++k) {
-                if (count[k] > 0) store8(out + (int64_t)q * p.d + column(k), count[k], vec, step, sum[q][k]);
+            for (int k = 0; k < VPT; ++k)
 #pragma unroll
                 for (int i = 0; i < 8; ++i) sum[q][k][i] = 0.f;
-            }
     };
+    auto flush = [&](int64_t slot) {
 #pragma unroll
-    for (int q = 0; q < 3; ++q)
+        for (int q = 0; q < 3; ++q)
 #pragma unroll
-        for (int k = 0; k < VPT; ++k)
+            for (int k = 0; k < VPT; ++k)
 #pragma unroll
-            for (int i = 0; i < 8; ++i) sum[q][k][i] = 0.f;
-    int64_t batch = first / p.rows_per_batch;
-    for (int64_t row = first; row < last; ++row) {
-        if (row >= (batch + 1) * p.rows_per_batch) {
-            if (p.partial) flush(worker + batch);
-            batch = row / p.rows_per_batch;
+                for (int i = 0; i < 8; ++i)
+                    if (i < count[k]) warp_sums[(warp * 3 + q) * p.d + column(k) + i * step] = sum[q][k][i];
+        __syncthreads();
+        for (int x = (int)(threadIdx.y * 32 + threadIdx.x); x < 3 * p.d; x += 32 * kNormWarps) {
+            float a = 0.f;
+#pragma unroll
+            for (int w = 0; w < kNormWarps; ++w) a += warp_sums[w * 3 * p.d + x];
+            p.partial[slot * 3 * p.d + x] = a;
         }
+        __syncthreads();
+        clear();
+    };
+    clear();
+    for (int64_t begin = first; begin < last;) {
+    const int64_t batch = begin / p.rows_per_batch;
+    const int64_t end = (batch + 1) * p.rows_per_batch < last ? (batch + 1) * p.rows_per_batch : last;
+    for (int64_t row = begin + warp; row < end; row += kNormWarps) {
         float h[VPT][8], g[VPT][8], H[VPT][8], y[VPT][8];
 #pragma unroll
         for (int k = 0; k < VPT; ++k) {
@@ -527,7 +540,9 @@ __global__ void __launch_bounds__(256) norm_residual_backward_warp(const NormBac
                 }
         }
     }
-    if (p.partial) flush(worker + batch);
+    if (p.partial) flush(blockIdx.x + batch);
+    begin = end;
+    }
 }
 
 // ---- backward, wide rows: a CTA, or a cluster of two or four, per row; rows staged in shared memory ----------------
@@ -648,7 +663,7 @@ template <typename S, typename Y, bool POST>
 __global__ void __launch_bounds__(kNormThreads, 1) norm_residual_backward(const __grid_constant__ NormBackward p) {
     extern __shared__ __align__(128) uint8_t smem[];
     const uint32_t base = smem_u32(smem);
-    volatile int* abort_flag = reinterpret_cast<volatile int*>(smem + 64);
+    volatile int* abort_flag = reinterpret_cast<volatile int*>(smem + 120);
     float* red = reinterpret_cast<float*>(smem + kNormRedOff);
     const int t = (int)threadIdx.x, warp = t >> 5, lane = t & 31, warps = (int)blockDim.x >> 5;
     const int rank = p.cluster > 1 ? (int)cluster_rank() : 0;
@@ -664,20 +679,36 @@ __global__ void __launch_bounds__(kNormThreads, 1) norm_residual_backward(const 
     const bool vec = p.vec != 0;
     const float inv_d = 1.0f / (float)p.d;
     const bool layer_h = p.norm == kNormLayer, layer_y = POST && p.post == kNormLayer, norm = p.norm != kNormNone;
-    // all threads of the worker; the values that the warps exchange go to every CTA's shared memory
-    auto barrier = [&]() { if (p.cluster > 1) cluster_barrier(); else __syncthreads(); };
-    auto exchange = [&](float* at, const float4& a) {
-        *reinterpret_cast<float4*>(at) = a;
-        for (int q = 1; q < p.cluster; ++q) st_cluster_v4(smem_u32(at), (uint32_t)((rank + q) % p.cluster), a);
+    // What the warps of a worker exchange: in one CTA by a barrier; in a cluster every warp sends its values to all CTAs and
+    // an mbarrier counts their bytes.  Four sets of values, each with its barrier: statistics (two, used in turn, so that a
+    // set is not written before all have read what it held), second phase (of the first and the second row of an iteration).
+    auto exchange = [&](int set, float* at, const float4& a) {
+        if (p.cluster == 1) *reinterpret_cast<float4*>(at) = a;
+        else
+            for (int q = 0; q < p.cluster; ++q) st_async_v4(smem_u32(at), base + 8u * (kNormStageMax + set), (uint32_t)q, a);
+    };
+    uint32_t set_parity = 0;                                          // bit = parity of a set's next phase
+    auto exchanged_all = [&](int set, int bytes) {
+        if (p.cluster == 1) {
+            __syncthreads();
+            return;
+        }
+        const uint32_t bar = base + 8u * (kNormStageMax + set);
+        if (t == 0) mbar_expect_tx(bar, (uint32_t)bytes);
+        if (!mbar_wait(bar, (set_parity >> set) & 1u, abort_flag) && !*abort_flag) {
+            atomicExch(&g_kq_device_error, KQ_DEV_TIMEOUT_NORM);
+            *abort_flag = 1;
+        }
+        set_parity ^= 1u << set;
     };
     const int all_warps = warps * p.cluster, my_warp = warp + rank * warps;
     if (t == 0) {
-        for (int s = 0; s < p.stages; ++s) mbar_init(base + 8u * s, 1);
+        for (int s = 0; s < kNormStageMax + 4; ++s) mbar_init(base + 8u * s, 1);
         *abort_flag = 0;
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
         asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
     }
-    barrier();
+    if (p.cluster > 1) cluster_barrier(); else __syncthreads();
     pdl_wait_prior_grid();
     auto issue = [&](int r, int s) {                                  // thread 0: row `r` of this worker into stage s
         const int64_t row = first + r;
@@ -758,7 +789,8 @@ __global__ void __launch_bounds__(kNormThreads, 1) norm_residual_backward(const 
     S* dx = static_cast<S*>(p.dx) + first * p.ld_dx + c0 + c;
     Y* dy = static_cast<Y*>(p.dy) + first * p.ld_dy + c0 + c;
     int s = 0, next = p.stages < rows ? p.stages : rows;              // stage of row r; next row to be fetched (thread 0)
-    uint32_t parity = 0, turn = 0;
+    uint32_t parity = 0;
+    int turn = 0;
     for (int r = 0, nr; r < rows; r += nr) {
         if (r == batch_end) {
             __syncthreads();                                          // other threads read this thread's parameters too
@@ -848,16 +880,16 @@ __global__ void __launch_bounds__(kNormThreads, 1) norm_residual_backward(const 
             if (POST) warp_sum4(sty, lane);
             if (lane == 0) {
                 float* at = red + turn * kNormRedFloats + (my_row * p.cluster * per_row + rank * per_row + part) * 8;
-                exchange(at, make_float4(st[0], st[1], st[2], st[3]));
-                exchange(at + 4, make_float4(sty[0], sty[1], pivot_h, pivot_y));
+                exchange(turn, at, make_float4(st[0], st[1], st[2], st[3]));
+                exchange(turn, at + 4, make_float4(sty[0], sty[1], pivot_h, pivot_y));
             }
         }
-        barrier();
+        exchanged_all(turn, all_warps * 32);
         // every thread is done with the rows before r: their stages take the rows that follow
         if (vec && t == 0)
             for (; next < rows && next < r + p.stages; ++next) issue(next, next % p.stages);
         const float* exchanged = red + turn * kNormRedFloats;        // (the other set may be written before all have read this one)
-        turn ^= 1u;
+        turn ^= 1;
 #pragma unroll 1
         for (int j = 0; j < nr; ++j) {
         uint8_t* stage = j ? stages[1] : stages[0];
@@ -959,9 +991,9 @@ __global__ void __launch_bounds__(kNormThreads, 1) norm_residual_backward(const 
                 b1 += __shfl_xor_sync(0xFFFFFFFFu, b1, o);
             }
             float* at = red + (2 + j) * kNormRedFloats;
-            if (lane == 0) exchange(at + my_warp * 4, make_float4(b0, b1, 0.f, 0.f));
+            if (lane == 0) exchange(2 + j, at + my_warp * 4, make_float4(b0, b1, 0.f, 0.f));
             asm volatile("fence.proxy.async.shared::cta;" ::: "memory");     // the kept values lie where the next copy lands
-            barrier();
+            exchanged_all(2 + j, all_warps * 16);
             b0 = b1 = 0.f;
             for (int w = lane; w < all_warps; w += 32) {
                 b0 += at[w * 4];

@@ -204,7 +204,7 @@ NormShape forward_shape(int d) {
 NormShape backward_shape(int d, int* cluster) {
     const int groups = (d + 7) / 8;
     *cluster = 1;
-    if (groups <= 64) return {32, 8, groups <= 32 ? 1 : 2};
+    if (groups <= 64) return {32, kq::kNormWarps, groups <= 32 ? 1 : 2};
     while (groups > *cluster * kq::kNormThreads) *cluster *= 2;
     return {((groups + *cluster - 1) / *cluster + 63) / 64 * 64, 1, 1};        // an even number of warps
 }
@@ -265,10 +265,10 @@ constexpr int kSmemPerSm = 228 * 1024, kSmemPerCta = 227 * 1024;
 NormWorkers norm_workers(const kq_norm_args_t& a, int sms, kq::NormBackward* p) {
     NormWorkers w = {};
     w.shape = backward_shape(a.d, &w.cluster);
-    int per_sm = 8;             // 8 CTAs of 256 threads: two warps per scheduler and more hide the loads of a warp's row
+    int per_sm = w.shape.vpt == 1 ? 2 : 1;                           // narrow rows: 110 to 183 registers
+    w.smem = kq::kNormWarps * 3 * a.d * (int)sizeof(float);          // at most 48 KB
     if (w.shape.rows == 1) {
-        per_sm = kq::kNormThreads / w.shape.threads;                 // what the registers let run on an SM
-        if (per_sm > 8) per_sm = 8;
+        per_sm = 20 * 32 / w.shape.threads;                          // 96 registers: five warps per scheduler
         const int columns = ((a.d + 7) / 8 + w.cluster - 1) / w.cluster * 8;      // of a CTA; the last one's may be fewer
         const int ss = type_size(a.stream_dtype), sb = type_size(a.branch_dtype);
         const bool post = a.y && a.post_norm != KQ_NORM_NONE, dn = a.norm != KQ_NORM_NONE;
@@ -290,7 +290,9 @@ NormWorkers norm_workers(const kq_norm_args_t& a, int sms, kq::NormBackward* p) 
             p->cache_m = cache_m; p->cache_gate = cache_gate; p->cache_post = cache_post;
         }
     }
-    const int64_t most = (int64_t)(sms > 1 ? sms : 2) * per_sm * w.shape.rows / w.cluster;
+    // a cluster of four needs four SMs of one GPC: 32 of them fit (8 GPCs of 16 to 20 SMs), not 37
+    int64_t most = (int64_t)(sms > 3 ? sms : 4) * per_sm / w.cluster;
+    if (w.cluster > 2) most = most * 7 / 8;
     w.rows_per_worker = (a.rows + most - 1) / most;
     if (w.rows_per_worker < 1) w.rows_per_worker = 1;
     w.workers = (a.rows + w.rows_per_worker - 1) / w.rows_per_worker;
@@ -319,8 +321,7 @@ kq_status_t launch_norm_backward(const kq::NormBackward& p, const NormWorkers& w
     if (w.shape.rows == 1) return p.y && p.post != KQ_NORM_NONE ? launch_norm_staged<S, Y, true>(p, w, st) : launch_norm_staged<S, Y, false>(p, w, st);
     cudaLaunchConfig_t cfg;
     cudaLaunchAttribute attr[2];
-    launch_config(&cfg, attr, dim3((unsigned)((w.workers + w.shape.rows - 1) / w.shape.rows)),
-                  dim3((unsigned)w.shape.threads, (unsigned)w.shape.rows), 0, 1, st);
+    launch_config(&cfg, attr, dim3((unsigned)w.workers), dim3((unsigned)w.shape.threads, (unsigned)w.shape.rows), (size_t)w.smem, 1, st);
     return w.shape.vpt == 1 ? launch(cfg, kq::norm_residual_backward_warp<S, Y, 1>, p) : launch(cfg, kq::norm_residual_backward_warp<S, Y, 2>, p);
 }
 
