@@ -13,7 +13,7 @@
 // weight tile than padding would give, no copy of A, and the group sizes are never needed on the host.
 //
 // Two kernels.
-//   linear_mxfp4_pair    CTA pairs on 256 rows x 256 weight rows (tcgen05.mma.cta_group::2): many rows per weight.
+//   linear_mxfp4_pair    CTA pairs on 256 rows x 192 weight rows (tcgen05.mma.cta_group::2): many rows per weight.
 //   linear_mxfp4_narrow  the weight as the 128-row operand and up to 128 rows of A as the narrow one: few rows per
 //                        weight, bound by reading the weights; K split over a cluster when there are few weight tiles.
 // The tensor-core path is that of kq_gemm_fp4_pair.cuh: codes by TMA, scale tiles copied to tensor memory.
@@ -35,8 +35,7 @@ struct LinearEpilogue {
     const float* row_scale;              // [M] or null
     const void* residual; int residual_type; int64_t ld_residual; float residual_scale;
     void* out; int out_type; int64_t ld_out;
-    int vec;                             // bias, gate, residual, out: full 32-column chunks allow 16-byte accesses
-    int wide;                            // out: and 32-byte stores
+    int vec, wide;                       // residual and out allow 16-byte accesses; out 32-byte ones
 };
 
 struct LinearProblem {
@@ -91,6 +90,17 @@ __device__ __forceinline__ void act_apply(int act, float (&v)[COUNT]) {
     }
 }
 
+// eight words to one row: one 32-byte store where the address allows it, else two of 16
+template <int N>
+__device__ __forceinline__ void store_words(void* p, const uint32_t (&w)[N], int wide) {
+    if (wide) {
+        st_global_32(p, w);
+    } else {
+        reinterpret_cast<uint4*>(p)[0] = make_uint4(w[0], w[1], w[2], w[3]);
+        reinterpret_cast<uint4*>(p)[1] = make_uint4(w[4], w[5], w[6], w[7]);
+    }
+}
+
 // ---- scalar access by runtime type ------------------------------------------------------------------
 __device__ __forceinline__ float load_typed(const void* p, int type, int64_t at) {
     if (type == kTypeF32) return static_cast<const float*>(p)[at];
@@ -113,6 +123,19 @@ __device__ __forceinline__ float linear_element(const LinearEpilogue& p, int exp
     if (p.gate.ptr) v[0] *= vec_entry(p.gate, row / p.rows_per_gate, n, 1.f);
     if (p.row_scale) v[0] *= __ldg(p.row_scale + row);
     return v[0];
+}
+
+// Arrival on another CTA's barrier that hands over tensor memory only.  Its release has CTA scope: at cluster scope it would
+// wait for the global stores of the item before, 2 to 3 us behind the operand loads.
+__device__ __forceinline__ void mbar_arrive_remote(uint32_t cluster_addr) {
+    asm volatile("mbarrier.arrive.shared::cluster.b64 _, [%0];" ::"r"(cluster_addr) : "memory");
+}
+// sixteen columns of this warp's 32 TMEM lanes, without the completion wait
+__device__ __forceinline__ void tc_ld_32x16_nowait(uint32_t taddr, uint32_t* r) {
+    asm volatile("tcgen05.ld.sync.aligned.32x32b.x16.b32 {%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15}, [%16];"
+                 : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]),
+                   "=r"(r[8]), "=r"(r[9]), "=r"(r[10]), "=r"(r[11]), "=r"(r[12]), "=r"(r[13]), "=r"(r[14]), "=r"(r[15])
+                 : "r"(taddr) : "memory");
 }
 
 // ---- items of work --------------------------------------------------------------------------------
@@ -180,175 +203,236 @@ __device__ __forceinline__ LinearItem linear_item(const LinearProblem& p, const 
 }
 
 // ---- pair kernel ------------------------------------------------------------------------------------
-// Stage layout, barriers and roles are those of gemm_mxfp4_umma_pair; what is new: items instead of tiles, the 3-D map of
-// the weights (experts), and the epilogue.
-constexpr int kLinPStages = kF4PStages;
-constexpr int kLinPBarOff = kLinPStages * kF4PStageBytes;
-constexpr int kLinPNumBars = 3 * kLinPStages + 2;
-constexpr int kLinPSlotOff = kLinPBarOff + 8 * kLinPNumBars;
-constexpr int kLinPAbortOff = kLinPSlotOff + 4;
-constexpr int kLinPCumOff = kLinPAbortOff + 4;
-constexpr int kLinPDynBytes = kLinPCumOff + 4 * (kMaxExperts + 1) + 1024;
+// Clusters of two CTAs on 256 rows x 192 weight rows (tcgen05.mma.cta_group::2): CTA r holds rows 128 r .. of the A tile with
+// their scale tile, weight rows 96 r .. of the tile, and the scale tiles of all 192.  192 columns and not 256 because two
+// accumulators (384 columns) and the scales of five stages (24 columns each) fit tensor memory: an item's epilogue has
+// the main loop of the next one to run in, and the next main loop starts without waiting for it.  (One accumulator of 256
+// columns costs 2 us between two items, 12 x 0.46 us of main loop at K = 3072.)  A weight tile of 192 rows starts in the middle
+// of a 128-row scale tile every other time; the instruction then finds its scales two columns (64 rows) further on.
+// The stages in flight are also a queue in front of every load of the epilogue (some 3000 cycles), so nothing is loaded
+// when it is needed: before a warp waits for its accumulator it fetches its 64 columns' bias and gate and its part of the
+// residual (a bulk copy per row) into shared memory.
+// Barriers as in gemm_mxfp4_umma_pair; 12 epilogue warps per CTA, one for each 32 rows x 64 columns.
+constexpr int kLinN = 192;
+constexpr int kLinStages = 5;
+constexpr int kLinABytes = 128 * 128;
+constexpr int kLinBBytes = kLinN / 2 * 128;
+constexpr int kLinSfaOff = kLinABytes + kLinBBytes;                  // 1 KB: [k tile]
+constexpr int kLinSfbOff = kLinSfaOff + 1024;                        // 2 KB: [row tile][k tile]
+constexpr int kLinStageBytes = kLinSfbOff + 2048;
+constexpr int kLinSfCol0 = 2 * kLinN;
+constexpr int kLinEpiWarps = 12;
+constexpr int kLinCols = 64;                                         // accumulator columns of a warp
+constexpr int kLinThreads = 32 * (3 + kLinEpiWarps);
+constexpr int kLinRowBytes = 128;                                    // of the residual, per row and copy
+constexpr int kLinRowStride = kLinRowBytes + 16;                     // rows of a warp's copy: no bank conflicts, a lane per row
+constexpr int kLinTileStride = 36;                                   // floats between the rows when the same place turns rows into columns
+constexpr int kLinVecOff = 32 * kLinRowStride;                       // floats [2][64]: bias by accumulator column, gate by column of out
+constexpr int kLinWarpBytes = kLinVecOff + 2 * kLinCols * 4;
+constexpr int kLinWarpOff = kLinStages * kLinStageBytes;
+constexpr int kLinBarOff = kLinWarpOff + kLinEpiWarps * kLinWarpBytes;
+constexpr int kLinNumBars = 3 * kLinStages + 4 + kLinEpiWarps;       // full, empty, sfready, tfull[2], tempty[2], residual of each warp
+constexpr int kLinSlotOff = kLinBarOff + 8 * kLinNumBars;
+constexpr int kLinAbortOff = kLinSlotOff + 4;
+constexpr int kLinCumOff = kLinAbortOff + 4;
+constexpr int kLinDynBytes = kLinCumOff + 4 * (kMaxExperts + 1) + 1024;
+static_assert(kLinSfCol0 + 24 * kLinStages <= 512, "tensor memory");
+static_assert(kLinStageBytes % 1024 == 0 && kLinWarpBytes % 16 == 0 && 32 * kLinTileStride * 4 <= kLinVecOff && kLinDynBytes <= 227 * 1024, "shared memory");
 
-// lane l, register i  <->  lane i, register l
-__device__ __forceinline__ void warp_transpose(float (&v)[32], int lane) {
-#pragma unroll
-    for (int s = 16; s >= 1; s >>= 1)
-#pragma unroll
-        for (int i = 0; i < 32; ++i)
-            if (!(i & s)) {
-                const bool up = lane & s;
-                const float got = __shfl_xor_sync(0xFFFFFFFFu, up ? v[i] : v[i | s], s);
-                if (up) v[i] = got; else v[i | s] = got;
-            }
+__device__ __forceinline__ uint32_t idesc_mxf4_192(uint32_t sf_id) {
+    return (sf_id << 4) | (1u << 7) | (1u << 10) | ((uint32_t)(kLinN >> 3) << 17) | (1u << 23) | ((256u >> 4) << 24) | (sf_id << 29);
 }
 
-// 32 columns of one row held by one thread; every access of the chunk is a vector (epi.vec, all 32 columns exist).
-template <bool GLU>
-__device__ __forceinline__ void epilogue_row(const LinearEpilogue& p, float (&v)[32], float (&u)[32], int expert, int row, int col, int r) {
-    if (p.bias.ptr) {
+// ---- epilogue of 32 rows x 32 accumulator columns, a lane per row ----
+// Bias, activation, gate and row scale act on the lane's own registers: 32 independent elements, vectors read from shared
+// memory by all lanes at once.  out: whole vectors of the lane's row where the alignment allows it (a chunk is 64 bytes of 16-bit
+// elements, full sectors); at other pitches, and at the ragged end of a row, the chunk goes through a tile of shared memory and
+// a lane takes a column, so that a warp's accesses stay neighbours in memory.  Gated: 16 features, gate half first.
+struct EpiChunk {
+    int row0, lo, hi;                    // first row of the warp, rows of the group
+    int col, at;                         // first column of out; first accumulator column within the warp's 64
+    int out_at;                          // first column of out within the warp's
+    int which;                           // gate row of this lane's row; uniform: the whole warp's, in shared memory
+    bool uniform;
+    float scale;                         // row scale of this lane's row
+    int res_at;                          // byte of the residual within the warp's copied rows
+};
+template <int C, bool MUL>
+__device__ __forceinline__ void apply_shared(const float* vector, float (&v)[C]) {
 #pragma unroll
-        for (int q = 0; q < 4; ++q) {
-            float b[8];
-            load_param(p.bias, expert, r + 8 * q, 8, true, 1, 0.f, b);
-#pragma unroll
-            for (int i = 0; i < 8; ++i) v[8 * q + i] += b[i];
-            if (GLU) {
-                load_param(p.bias, expert, r + 32 + 8 * q, 8, true, 1, 0.f, b);
-#pragma unroll
-                for (int i = 0; i < 8; ++i) u[8 * q + i] += b[i];
-            }
-        }
+    for (int q = 0; q < C / 4; ++q) {
+        const float4 b = reinterpret_cast<const float4*>(vector)[q];
+        v[4 * q] = MUL ? v[4 * q] * b.x : v[4 * q] + b.x;
+        v[4 * q + 1] = MUL ? v[4 * q + 1] * b.y : v[4 * q + 1] + b.y;
+        v[4 * q + 2] = MUL ? v[4 * q + 2] * b.z : v[4 * q + 2] + b.z;
+        v[4 * q + 3] = MUL ? v[4 * q + 3] * b.w : v[4 * q + 3] + b.w;
     }
-    act_apply<32>(p.act, v);
-    if (GLU) {
+}
+
+template <bool GLU>
+__device__ __forceinline__ void epilogue_chunk(const LinearEpilogue& p, const uint32_t (&r)[32], uint8_t* mem, const EpiChunk& c, int lane) {
+    constexpr int C = GLU ? 16 : 32;                                 // columns of out
+    const int row = c.row0 + lane, have = p.N - c.col;
+    const bool mine = row >= c.lo && row < c.hi;
+    const float* vec = reinterpret_cast<const float*>(mem + kLinVecOff);
+    float v[C];
 #pragma unroll
-        for (int i = 0; i < 32; ++i) v[i] *= u[i];
+    for (int i = 0; i < C; ++i) v[i] = __uint_as_float(r[i]);
+    if (p.bias.ptr) apply_shared<C, false>(vec + c.at, v);
+    act_apply<C>(p.act, v);
+    if (GLU) {
+        float u[C];
+#pragma unroll
+        for (int i = 0; i < C; ++i) u[i] = __uint_as_float(r[(C + i) & 31]);
+        if (p.bias.ptr) apply_shared<C, false>(vec + c.at + 32, u);
+#pragma unroll
+        for (int i = 0; i < C; ++i) v[i] *= u[i];
     }
     if (p.gate.ptr) {
-        const int which = row / p.rows_per_gate;
+        if (c.uniform) {
+            apply_shared<C, true>(vec + kLinCols + c.out_at, v);
+        } else {                                                     // rows of several gate rows in one warp
 #pragma unroll
-        for (int q = 0; q < 4; ++q) {
-            float b[8];
-            load_param(p.gate, which, col + 8 * q, 8, true, 1, 1.f, b);
-#pragma unroll
-            for (int i = 0; i < 8; ++i) v[8 * q + i] *= b[i];
+            for (int i = 0; i < C; ++i) v[i] *= i < have ? vec_entry(p.gate, c.which, c.col + i, 1.f) : 1.f;
         }
     }
     if (p.row_scale) {
-        const float s = __ldg(p.row_scale + row);
 #pragma unroll
-        for (int i = 0; i < 32; ++i) v[i] *= s;
+        for (int i = 0; i < C; ++i) v[i] *= c.scale;
     }
-    if (p.residual) {
-        const int64_t at = (int64_t)row * p.ld_residual + col;
-        if (p.residual_type == kTypeF32) {
-            const float4* q = reinterpret_cast<const float4*>(static_cast<const float*>(p.residual) + at);
+    if (p.vec && have >= C) {
+        if (p.residual) {
+            const uint8_t* res = mem + lane * kLinRowStride + c.res_at;
+            if (p.residual_type == kTypeF32) {
 #pragma unroll
-            for (int i = 0; i < 8; ++i) {
-                const float4 t = q[i];
-                v[4 * i] = fmaf(p.residual_scale, t.x, v[4 * i]);
-                v[4 * i + 1] = fmaf(p.residual_scale, t.y, v[4 * i + 1]);
-                v[4 * i + 2] = fmaf(p.residual_scale, t.z, v[4 * i + 2]);
-                v[4 * i + 3] = fmaf(p.residual_scale, t.w, v[4 * i + 3]);
-            }
-        } else {
-            const uint4* q = reinterpret_cast<const uint4*>(static_cast<const uint16_t*>(p.residual) + at);
+                for (int i = 0; i < C / 4; ++i) {
+                    const float4 t = reinterpret_cast<const float4*>(res)[i];
+                    v[4 * i] = fmaf(p.residual_scale, t.x, v[4 * i]);
+                    v[4 * i + 1] = fmaf(p.residual_scale, t.y, v[4 * i + 1]);
+                    v[4 * i + 2] = fmaf(p.residual_scale, t.z, v[4 * i + 2]);
+                    v[4 * i + 3] = fmaf(p.residual_scale, t.w, v[4 * i + 3]);
+                }
+            } else {
 #pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                float t[8];
-                if (p.residual_type == kTypeF16) widen8_f16(q[i], t); else widen8(q[i], t);
+                for (int i = 0; i < C / 8; ++i) {
+                    float t[8];
+                    const uint4 q = reinterpret_cast<const uint4*>(res)[i];
+                    if (p.residual_type == kTypeF16) widen8_f16(q, t); else widen8(q, t);
 #pragma unroll
-                for (int e = 0; e < 8; ++e) v[8 * i + e] = fmaf(p.residual_scale, t[e], v[8 * i + e]);
+                    for (int e = 0; e < 8; ++e) v[8 * i + e] = fmaf(p.residual_scale, t[e], v[8 * i + e]);
+                }
             }
         }
-    }
-    const int64_t at = (int64_t)row * p.ld_out + col;
-    if (p.out_type == kTypeF32) {
-        float* o = static_cast<float*>(p.out) + at;
+        if (!mine) return;
+        const int64_t at = (int64_t)row * p.ld_out + c.col;
+        if (p.out_type == kTypeF32) {
+            float* o = static_cast<float*>(p.out) + at;
 #pragma unroll
-        for (int q = 0; q < 4; ++q) {
-            if (p.wide) {
+            for (int q = 0; q < C / 8; ++q) {
                 uint32_t w[8];
 #pragma unroll
                 for (int i = 0; i < 8; ++i) w[i] = __float_as_uint(v[8 * q + i]);
-                st_global_32(o + 8 * q, w);
-            } else {
-                reinterpret_cast<float4*>(o)[2 * q] = make_float4(v[8 * q], v[8 * q + 1], v[8 * q + 2], v[8 * q + 3]);
-                reinterpret_cast<float4*>(o)[2 * q + 1] = make_float4(v[8 * q + 4], v[8 * q + 5], v[8 * q + 6], v[8 * q + 7]);
+                store_words<8>(o + 8 * q, w, p.wide);
             }
-        }
-    } else {
-        uint16_t* o = static_cast<uint16_t*>(p.out) + at;
-        uint32_t w[16];
-#pragma unroll
-        for (int i = 0; i < 16; ++i) {
-            if (p.out_type == kTypeF16) {
-                const __half2 h = __floats2half2_rn(v[2 * i], v[2 * i + 1]);
-                w[i] = *reinterpret_cast<const uint32_t*>(&h);
-            } else {
-                const __nv_bfloat162 h = __floats2bfloat162_rn(v[2 * i], v[2 * i + 1]);
-                w[i] = *reinterpret_cast<const uint32_t*>(&h);
-            }
-        }
-        if (p.wide) {
-            const uint32_t lo[8] = {w[0], w[1], w[2], w[3], w[4], w[5], w[6], w[7]};
-            const uint32_t hi[8] = {w[8], w[9], w[10], w[11], w[12], w[13], w[14], w[15]};
-            st_global_32(o, lo);
-            st_global_32(o + 16, hi);
         } else {
+            uint16_t* o = static_cast<uint16_t*>(p.out) + at;
 #pragma unroll
-            for (int q = 0; q < 4; ++q) reinterpret_cast<uint4*>(o)[q] = make_uint4(w[4 * q], w[4 * q + 1], w[4 * q + 2], w[4 * q + 3]);
+            for (int q = 0; q < C / 16; ++q) {
+                uint32_t w[8];
+#pragma unroll
+                for (int i = 0; i < 8; ++i) {
+                    const float lo = v[16 * q + 2 * i], hi = v[16 * q + 2 * i + 1];
+                    if (p.out_type == kTypeF16) {
+                        const __half2 h = __floats2half2_rn(lo, hi);
+                        w[i] = *reinterpret_cast<const uint32_t*>(&h);
+                    } else {
+                        const __nv_bfloat162 h = __floats2bfloat162_rn(lo, hi);
+                        w[i] = *reinterpret_cast<const uint32_t*>(&h);
+                    }
+                }
+                store_words<8>(o + 16 * q, w, p.wide);
+            }
+        }
+        return;
+    }
+    // (an unaligned residual has not been copied: it is read in the column layout)
+    float* tile = reinterpret_cast<float*>(mem);
+    __syncwarp();                                                    // the chunk before has been read
+    float4* at4 = reinterpret_cast<float4*>(tile + lane * kLinTileStride);
+#pragma unroll
+    for (int i = 0; i < C / 4; ++i) at4[i] = make_float4(v[4 * i], v[4 * i + 1], v[4 * i + 2], v[4 * i + 3]);
+    __syncwarp();
+    constexpr int kRows = 32 / C;                                    // rows of an access
+    const int x = lane % C, first = lane / C;
+    if (x < have) {
+        // rows of the warp's 32 that are in the group
+        const int begin = c.lo - c.row0 > 0 ? c.lo - c.row0 : 0, end = c.hi - c.row0 < 32 ? c.hi - c.row0 : 32;
+        const int64_t pitch = p.ld_out * kRows, pitch_r = p.ld_residual * kRows;
+        int64_t at = (int64_t)(c.row0 + first) * p.ld_out + c.col + x, at_r = (int64_t)(c.row0 + first) * p.ld_residual + c.col + x;
+#pragma unroll 1
+        for (int in = first; in < 32; in += 8 * kRows) {             // eight rows of a column at a time
+            float t[8];
+            bool ok[8];
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+                t[i] = tile[(in + i * kRows) * kLinTileStride + x];
+                ok[i] = in + i * kRows >= begin && in + i * kRows < end;
+            }
+            if (p.residual) {
+                float q[8];
+#pragma unroll
+                for (int i = 0; i < 8; ++i) q[i] = ok[i] ? load_typed(p.residual, p.residual_type, at_r + i * pitch_r) : 0.f;
+#pragma unroll
+                for (int i = 0; i < 8; ++i) t[i] = fmaf(p.residual_scale, q[i], t[i]);
+            }
+            if (p.out_type == kTypeF32) {
+#pragma unroll
+                for (int i = 0; i < 8; ++i)
+                    if (ok[i]) static_cast<float*>(p.out)[at + i * pitch] = t[i];
+            } else if (p.out_type == kTypeF16) {
+#pragma unroll
+                for (int i = 0; i < 8; ++i)
+                    if (ok[i]) static_cast<__half*>(p.out)[at + i * pitch] = __float2half_rn(t[i]);
+            } else {
+#pragma unroll
+                for (int i = 0; i < 8; ++i)
+                    if (ok[i]) static_cast<__nv_bfloat16*>(p.out)[at + i * pitch] = __float2bfloat16_rn(t[i]);
+            }
+            at += 8 * pitch;
+            at_r += 8 * pitch_r;
         }
     }
 }
 
-// 32 rows x 32 columns of a warp, lane = column after the transpose: any alignment, any pitch, a ragged last chunk.
+// Before the accumulator is there: the warp's bias (64 accumulator columns from weight row wrow on) and gate (columns of out
+// from col on), zero where they end, into shared memory.
 template <bool GLU>
-__device__ __forceinline__ void epilogue_column(const LinearEpilogue& p, float (&v)[32], float (&u)[32], int expert, int row0, int lo, int hi,
-                                                int col0, int r0, int lane) {
-    warp_transpose(v, lane);
-    if (GLU) warp_transpose(u, lane);
-    const int n = col0 + lane, r = r0 + lane;
-    if (n >= p.N) return;
-    const float bias = vec_entry(p.bias, expert, r, 0.f), bias_u = GLU ? vec_entry(p.bias, expert, r + 32, 0.f) : 0.f;
+__device__ __forceinline__ void fetch_vectors(const LinearEpilogue& p, float* vec, int expert, int wrow, int rows, int col, int which, bool gate, int lane) {
 #pragma unroll
-    for (int i = 0; i < 32; ++i) v[i] += bias;
-    act_apply<32>(p.act, v);
-    if (GLU) {
-#pragma unroll
-        for (int i = 0; i < 32; ++i) v[i] *= u[i] + bias_u;
+    for (int i = 0; i < 2; ++i) {
+        const int x = lane + 32 * i;
+        if (p.bias.ptr) vec[x] = wrow + x < rows ? vec_entry(p.bias, expert, wrow + x, 0.f) : 0.f;
+        if (gate && (!GLU || i == 0)) vec[kLinCols + x] = col + x < p.N ? vec_entry(p.gate, which, col + x, 0.f) : 0.f;
     }
-    if (p.gate.ptr) {
-        // one load per change of the gate row
-        int which = -1;
-        float g = 1.f;
-#pragma unroll
-        for (int i = 0; i < 32; ++i) {
-            const int w = (row0 + i < hi ? row0 + i : hi - 1) / p.rows_per_gate;
-            if (w != which) { which = w; g = vec_entry(p.gate, w, n, 1.f); }
-            v[i] *= g;
-        }
-    }
-    if (p.row_scale) {
-#pragma unroll
-        for (int i = 0; i < 32; ++i)
-            if (row0 + i < hi) v[i] *= __ldg(p.row_scale + row0 + i);
-    }
-    if (p.residual) {
-#pragma unroll
-        for (int i = 0; i < 32; ++i)
-            if (row0 + i >= lo && row0 + i < hi)
-                v[i] = fmaf(p.residual_scale, load_typed(p.residual, p.residual_type, (int64_t)(row0 + i) * p.ld_residual + n), v[i]);
-    }
-#pragma unroll
-    for (int i = 0; i < 32; ++i)
-        if (row0 + i >= lo && row0 + i < hi) store_typed(p.out, p.out_type, (int64_t)(row0 + i) * p.ld_out + n, v[i]);
+}
+// This lane's row of the residual from column `col` on, up to kLinRowBytes of it, and the warp's barrier armed with all of them.
+// (Only whole 16-byte pieces: what a ragged last chunk needs is read in the column layout.)
+__device__ __forceinline__ void fetch_residual(const LinearEpilogue& p, uint8_t* mem, uint32_t bar, int row, int lo, int hi, int col, int lane) {
+    const int size = p.residual_type == kTypeF32 ? 4 : 2;
+    const int bytes = (p.N - col) * size < kLinRowBytes ? (p.N - col) * size & ~15 : kLinRowBytes;
+    const bool mine = row >= lo && row < hi && bytes > 0;
+    const int rows = __popc(__ballot_sync(0xFFFFFFFFu, mine));
+    asm volatile("fence.proxy.async.shared::cta;" ::: "memory");     // the place may have held a tile of columns
+    __syncwarp();
+    if (lane == 0) mbar_expect_tx(bar, (uint32_t)(bytes > 0 ? rows * bytes : 0));
+    __syncwarp();
+    if (mine)
+        bulk_load(smem_u32(mem) + lane * kLinRowStride, static_cast<const char*>(p.residual) + ((int64_t)row * p.ld_residual + col) * size, (uint32_t)bytes, bar);
 }
 
 // tmap_a: codes [M][K/2]; tmap_b: codes [experts][R][K/2]; tmap_sfa / tmap_sfb: scale tiles [row tiles][k tiles][128 x u32].
 template <bool GLU>
-__global__ void __launch_bounds__(kF4PThreads, 1)
+__global__ void __launch_bounds__(kLinThreads, 1)
 linear_mxfp4_pair(const __grid_constant__ CUtensorMap tmap_a, const __grid_constant__ CUtensorMap tmap_b,
                   const __grid_constant__ CUtensorMap tmap_sfa, const __grid_constant__ CUtensorMap tmap_sfb,
                   const __grid_constant__ LinearProblem p) {
@@ -356,15 +440,15 @@ linear_mxfp4_pair(const __grid_constant__ CUtensorMap tmap_a, const __grid_const
     const uint32_t raw = smem_u32(smem_raw);
     const uint32_t base = (raw + 1023u) & ~1023u;
     uint8_t* base_ptr = smem_raw + (base - raw);
-    const uint32_t bar0 = base + kLinPBarOff;
+    const uint32_t bar0 = base + kLinBarOff;
     auto bar_full = [&](int s) { return bar0 + 8u * s; };
-    auto bar_empty = [&](int s) { return bar0 + 8u * (kLinPStages + s); };
-    auto bar_sfready = [&](int s) { return bar0 + 8u * (2 * kLinPStages + s); };
-    const uint32_t bar_tfull = bar0 + 8u * (3 * kLinPStages);
-    const uint32_t bar_tempty = bar0 + 8u * (3 * kLinPStages + 1);
-    volatile uint32_t* tmem_slot = reinterpret_cast<volatile uint32_t*>(base_ptr + kLinPSlotOff);
-    volatile int* abort_flag = reinterpret_cast<volatile int*>(base_ptr + kLinPAbortOff);
-    int* cum = reinterpret_cast<int*>(base_ptr + kLinPCumOff);
+    auto bar_empty = [&](int s) { return bar0 + 8u * (kLinStages + s); };
+    auto bar_sfready = [&](int s) { return bar0 + 8u * (2 * kLinStages + s); };
+    auto bar_tfull = [&](int a) { return bar0 + 8u * (3 * kLinStages + a); };
+    auto bar_tempty = [&](int a) { return bar0 + 8u * (3 * kLinStages + 2 + a); };
+    volatile uint32_t* tmem_slot = reinterpret_cast<volatile uint32_t*>(base_ptr + kLinSlotOff);
+    volatile int* abort_flag = reinterpret_cast<volatile int*>(base_ptr + kLinAbortOff);
+    int* cum = reinterpret_cast<int*>(base_ptr + kLinCumOff);
 
     const int warp = threadIdx.x >> 5;
     const int lane = threadIdx.x & 31;
@@ -372,9 +456,9 @@ linear_mxfp4_pair(const __grid_constant__ CUtensorMap tmap_a, const __grid_const
     const int pair = (int)(blockIdx.x >> 1), n_pairs = (int)(gridDim.x >> 1);
 
     if (threadIdx.x == 0) {
-        for (int s = 0; s < kLinPStages; ++s) { mbar_init(bar_full(s), 1); mbar_init(bar_empty(s), 1); mbar_init(bar_sfready(s), 1); }
-        mbar_init(bar_tfull, 1);
-        mbar_init(bar_tempty, 16);
+        for (int s = 0; s < kLinStages; ++s) { mbar_init(bar_full(s), 1); mbar_init(bar_empty(s), 1); mbar_init(bar_sfready(s), 1); }
+        for (int a = 0; a < 2; ++a) { mbar_init(bar_tfull(a), 1); mbar_init(bar_tempty(a), 2 * kLinEpiWarps); }
+        for (int e = 0; e < kLinEpiWarps; ++e) mbar_init(bar0 + 8u * (3 * kLinStages + 4 + e), 1);
         *abort_flag = 0;
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
         asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
@@ -386,7 +470,7 @@ linear_mxfp4_pair(const __grid_constant__ CUtensorMap tmap_a, const __grid_const
     if (warp == 1) {
         __syncwarp();
         asm volatile("tcgen05.alloc.cta_group::2.sync.aligned.shared::cta.b32 [%0], %1;"
-                     ::"r"(base + (uint32_t)kLinPSlotOff), "r"(512u) : "memory");
+                     ::"r"(base + (uint32_t)kLinSlotOff), "r"(512u) : "memory");
         asm volatile("tcgen05.relinquish_alloc_permit.cta_group::2.sync.aligned;" ::: "memory");
     }
     if (warp == 2 && p.experts) {
@@ -409,19 +493,20 @@ linear_mxfp4_pair(const __grid_constant__ CUtensorMap tmap_a, const __grid_const
             int it = 0;
             for (int i = 0; i < my_items && !*abort_flag; ++i) {
                 const LinearItem w = linear_item<256>(p, cum, pair + i * n_pairs, kGemmGroupM);
+                const int sf_tile = w.expert * p.sf_row_tiles + w.tile_n * kLinN / 128;
                 for (int kb = 0; kb < p.k_blocks; ++kb, ++it) {
-                    const int s = it % kLinPStages;
-                    if (it >= kLinPStages && !mbar_wait(bar_empty(s), ((it / kLinPStages) - 1) & 1, abort_flag)) {
+                    const int s = it % kLinStages;
+                    if (it >= kLinStages && !mbar_wait(bar_empty(s), ((it / kLinStages) - 1) & 1, abort_flag)) {
                         if (!*abort_flag) { atomicExch(&g_kq_device_error, KQ_DEV_TIMEOUT_GEMM_PRODUCER); *abort_flag = 1; }
                         break;
                     }
-                    const uint32_t dst = base + s * kF4PStageBytes;
+                    const uint32_t dst = base + s * kLinStageBytes;
                     const uint32_t leader_full = mapa_shared(bar_full(s), 0);
-                    if (rank == 0) mbar_expect_tx(bar_full(s), 2 * kF4PLoadBytes);
-                    tma_load_2d_pair(dst, &tmap_a, kb * kF4PKBytes, w.tile_m * 256 + (int)rank * 128, leader_full);
-                    tma_load_3d_pair(dst + kF4PABytes, &tmap_b, kb * kF4PKBytes, w.tile_n * 256 + (int)rank * 128, w.expert, leader_full);
-                    tma_load_3d_pair(dst + kF4PSfaOff, &tmap_sfa, 0, 2 * kb, w.tile_m * 2 + (int)rank, leader_full);
-                    tma_load_3d_pair(dst + kF4PSfbOff, &tmap_sfb, 0, 2 * kb, w.expert * p.sf_row_tiles + w.tile_n * 2, leader_full);
+                    if (rank == 0) mbar_expect_tx(bar_full(s), 2 * kLinStageBytes);
+                    tma_load_2d_pair(dst, &tmap_a, kb * 128, w.tile_m * 256 + (int)rank * 128, leader_full);
+                    tma_load_3d_pair(dst + kLinABytes, &tmap_b, kb * 128, w.tile_n * kLinN + (int)rank * (kLinN / 2), w.expert, leader_full);
+                    tma_load_3d_pair(dst + kLinSfaOff, &tmap_sfa, 0, 2 * kb, w.tile_m * 2 + (int)rank, leader_full);
+                    tma_load_3d_pair(dst + kLinSfbOff, &tmap_sfb, 0, 2 * kb, sf_tile, leader_full);
                     issued = it + 1;
                 }
             }
@@ -430,51 +515,53 @@ linear_mxfp4_pair(const __grid_constant__ CUtensorMap tmap_a, const __grid_const
         // ---------------- MMA issuer (leader CTA only) ----------------
         if (lane == 0 && rank == 0) {
             const uint64_t a_desc0 = smem_desc_sw128(base);
-            const uint64_t b_desc0 = smem_desc_sw128(base + kF4PABytes);
+            const uint64_t b_desc0 = smem_desc_sw128(base + kLinABytes);
             int it = 0;
             bool ok = true;
             for (int i = 0; ok && i < my_items; ++i) {
-                if (i >= 1 && !mbar_wait(bar_tempty, (i - 1) & 1, abort_flag)) {
+                const int acc = i & 1;
+                if (i >= 2 && !mbar_wait(bar_tempty(acc), ((i >> 1) - 1) & 1, abort_flag)) {
                     if (!*abort_flag) { atomicExch(&g_kq_device_error, KQ_DEV_TIMEOUT_GEMM_MMA); *abort_flag = 1; }
                     break;
                 }
                 tc_fence_after();
+                const LinearItem w = linear_item<256>(p, cum, pair + i * n_pairs, kGemmGroupM);
+                const uint32_t d_addr = tmem_base + (uint32_t)(acc * kLinN), shift = (w.tile_n & 1) ? 2u : 0u;
                 for (int kb = 0; kb < p.k_blocks; ++kb, ++it) {
-                    const int s = it % kLinPStages;
-                    if (!mbar_wait(bar_sfready(s), (it / kLinPStages) & 1, abort_flag)) {
+                    const int s = it % kLinStages;
+                    if (!mbar_wait(bar_sfready(s), (it / kLinStages) & 1, abort_flag)) {
                         if (!*abort_flag) { atomicExch(&g_kq_device_error, KQ_DEV_TIMEOUT_GEMM_MMA); *abort_flag = 1; }
                         ok = false;
                         break;
                     }
                     tc_fence_after();
-                    const uint64_t off = (uint64_t)((s * kF4PStageBytes) >> 4);
-                    const uint32_t t_sfa = tmem_base + (uint32_t)(kF4PSfCol0 + 24 * s);
-                    const uint32_t t_sfb = t_sfa + 8;
+                    const uint64_t off = (uint64_t)((s * kLinStageBytes) >> 4);
+                    const uint32_t t_sfa = tmem_base + (uint32_t)(kLinSfCol0 + 24 * s);
+                    const uint32_t t_sfb = t_sfa + 8 + shift;
 #pragma unroll
                     for (int k = 0; k < 4; ++k)
-                        tc_mma_mxf4_pair(tmem_base, a_desc0 + off + (uint64_t)(2 * k), b_desc0 + off + (uint64_t)(2 * k),
-                                         idesc_mxf4_pair(2u * (k & 1), 2u * (k & 1)), t_sfa + 4 * (k >> 1), t_sfb + 8 * (k >> 1),
-                                         (uint32_t)((kb | k) != 0));
+                        tc_mma_mxf4_pair(d_addr, a_desc0 + off + (uint64_t)(2 * k), b_desc0 + off + (uint64_t)(2 * k),
+                                         idesc_mxf4_192(2u * (k & 1)), t_sfa + 4 * (k >> 1), t_sfb + 8 * (k >> 1), (uint32_t)((kb | k) != 0));
                     tc_commit_pair(bar_empty(s));
                 }
-                if (ok) tc_commit_pair(bar_tfull);
+                if (ok) tc_commit_pair(bar_tfull(acc));
             }
         }
-    } else if (warp == 10) {
+    } else if (warp == 2) {
         // ---------------- scale tiles: shared memory -> TMEM of both CTAs (leader CTA only) ----------------
         if (lane == 0 && rank == 0) {
-            const uint64_t sfa_desc0 = smem_desc_sf(base + kF4PSfaOff);
-            const uint64_t sfb_desc0 = smem_desc_sf(base + kF4PSfbOff);
+            const uint64_t sfa_desc0 = smem_desc_sf(base + kLinSfaOff);
+            const uint64_t sfb_desc0 = smem_desc_sf(base + kLinSfbOff);
             const int total = my_items * p.k_blocks;
             for (int it = 0; it < total; ++it) {
-                const int s = it % kLinPStages;
-                if (!mbar_wait(bar_full(s), (it / kLinPStages) & 1, abort_flag)) {
+                const int s = it % kLinStages;
+                if (!mbar_wait(bar_full(s), (it / kLinStages) & 1, abort_flag)) {
                     if (!*abort_flag) { atomicExch(&g_kq_device_error, KQ_DEV_TIMEOUT_GEMM_MMA); *abort_flag = 1; }
                     break;
                 }
                 tc_fence_after();
-                const uint64_t off = (uint64_t)((s * kF4PStageBytes) >> 4);
-                const uint32_t t_sfa = tmem_base + (uint32_t)(kF4PSfCol0 + 24 * s);
+                const uint64_t off = (uint64_t)((s * kLinStageBytes) >> 4);
+                const uint32_t t_sfa = tmem_base + (uint32_t)(kLinSfCol0 + 24 * s);
                 const uint32_t t_sfb = t_sfa + 8;
 #pragma unroll
                 for (int y = 0; y < 2; ++y) {
@@ -487,50 +574,79 @@ linear_mxfp4_pair(const __grid_constant__ CUtensorMap tmap_a, const __grid_const
             }
         }
     } else {
-        // ---------------- epilogue: warps 2..9 of both CTAs; warp = lane quarter x column half ----------------
-        const int quarter = warp & 3;
-        const int chalf = (warp - 2) >> 2;
+        // ---------------- epilogue: warp = lane quarter x third of the columns ----------------
+        const int quarter = warp & 3;            // the lanes of TMEM that this warp may read
+        const int third = (warp - 3) >> 2;
+        uint8_t* mem = base_ptr + kLinWarpOff + (warp - 3) * kLinWarpBytes;
+        const uint32_t bar_res = bar0 + 8u * (3 * kLinStages + 4 + (warp - 3));
+        const bool copied = p.epi.residual && p.epi.vec;
+        uint32_t res_parity = 0;
         pdl_wait_prior_grid();
         for (int i = 0; i < my_items; ++i) {
             const LinearItem w = linear_item<256>(p, cum, pair + i * n_pairs, kGemmGroupM);
-            if (!mbar_wait(bar_tfull, i & 1, abort_flag)) {
+            EpiChunk c;
+            c.row0 = w.tile_m * 256 + (int)rank * 128 + quarter * 32;
+            c.lo = w.lo;
+            c.hi = w.hi;
+            const int wrow = w.tile_n * kLinN + third * kLinCols, col = GLU ? wrow / 2 : wrow;
+            const bool live = c.row0 < c.hi && c.row0 + 32 > c.lo && wrow < p.R;    // warp-uniform
+            if (live) {
+                const int row = c.row0 + lane < c.hi ? (c.row0 + lane > c.lo ? c.row0 + lane : c.lo) : c.hi - 1;
+                c.which = p.epi.gate.ptr ? row / p.epi.rows_per_gate : 0;
+                c.uniform = __all_sync(0xFFFFFFFFu, c.which == __shfl_sync(0xFFFFFFFFu, c.which, 0));
+                c.scale = p.epi.row_scale ? __ldg(p.epi.row_scale + row) : 1.f;
+                __syncwarp();                                                       // the vectors of the item before have been read
+                if (copied) fetch_residual(p.epi, mem, bar_res, c.row0 + lane, c.lo, c.hi, col, lane);
+                fetch_vectors<GLU>(p.epi, reinterpret_cast<float*>(mem + kLinVecOff), w.expert, wrow, p.R, col, c.which, p.epi.gate.ptr && c.uniform, lane);
+                __syncwarp();
+            }
+            const int acc = i & 1;
+            const bool ok = mbar_wait(bar_tfull(acc), (i >> 1) & 1, abort_flag);
+            if (live && copied) {                                                   // (also when giving up: no copy may outlive the CTA)
+                int never = 0;
+                if (!mbar_wait(bar_res, res_parity, &never) && !*abort_flag) { atomicExch(&g_kq_device_error, KQ_DEV_TIMEOUT_GEMM_EPILOGUE); *abort_flag = 1; }
+                res_parity ^= 1u;
+            }
+            if (!ok) {
                 if (!*abort_flag) { atomicExch(&g_kq_device_error, KQ_DEV_TIMEOUT_GEMM_EPILOGUE); *abort_flag = 1; }
                 break;
             }
             tc_fence_after();
-            // 32 lanes x 128 columns to registers in one sweep; the accumulator goes back to the issuer at once
-            uint32_t r[4][32];
+            // 32 lanes x 64 columns to registers in one sweep, as two chunks: 32 columns each or, gated, 16 gate columns and
+            // their 16 value columns; then the accumulator goes back to the issuer
+            uint32_t r[2][32];
+            if (live) {
+                const uint32_t taddr = tmem_base + ((uint32_t)(quarter * 32) << 16) + (uint32_t)(acc * kLinN + third * kLinCols);
 #pragma unroll
-            for (int cc = 0; cc < 4; ++cc)
-                tc_ld_32x32_nowait(tmem_base + ((uint32_t)(quarter * 32) << 16) + (uint32_t)((chalf * 4 + cc) * 32), r[cc]);
-            tc_wait_ld();
+                for (int q = 0; q < 2; ++q) {
+                    const uint32_t lo = taddr + (uint32_t)(GLU ? 16 * q : 32 * q);
+                    tc_ld_32x16_nowait(lo, r[q]);
+                    tc_ld_32x16_nowait(lo + (GLU ? 32 : 16), r[q] + 16);
+                }
+                tc_wait_ld();
 #pragma unroll
-            for (int cc = 0; cc < 4; ++cc) pin_after_wait(r[cc]);
+                for (int q = 0; q < 2; ++q) pin_after_wait(r[q]);
+            }
             tc_fence_before();
             __syncwarp();
-            if (lane == 0) mbar_arrive_cluster(mapa_shared(bar_tempty, 0));
-            const int row0 = w.tile_m * 256 + (int)rank * 128 + quarter * 32;
-            const int row = row0 + lane;
-            const int wrow = w.tile_n * 256 + chalf * 128;           // weight row of r[0][0]
-            if (row0 >= w.hi || row0 + 32 <= w.lo) continue;         // warp-uniform: no row of this warp is in the group
-#pragma unroll
-            for (int cc = 0; cc < 4; cc += GLU ? 2 : 1) {
-                const int col = GLU ? (wrow + cc * 32) / 2 : wrow + cc * 32;
-                if (col < p.epi.N) {
-                    float v[32], u[32];
-#pragma unroll
-                    for (int q = 0; q < 32; ++q) {
-                        v[q] = __uint_as_float(r[cc][q]);
-                        if (GLU) u[q] = __uint_as_float(r[cc + (GLU ? 1 : 0)][q]);
-                    }
-                    if (p.epi.vec && col + 32 <= p.epi.N) {
-                        if (row >= w.lo && row < w.hi) epilogue_row<GLU>(p.epi, v, u, w.expert, row, col, wrow + cc * 32);
-                        __syncwarp();
-                    } else {
-                        epilogue_column<GLU>(p.epi, v, u, w.expert, row0, w.lo, w.hi, col, wrow + cc * 32, lane);
-                        __syncwarp();
-                    }
+            if (lane == 0) mbar_arrive_remote(mapa_shared(bar_tempty(acc), 0));
+            if (!live) continue;
+            // one copy of the epilogue's code for both chunks (a gigantic one does not fit the instruction cache): the registers of
+            // the next chunk move up
+#pragma unroll 1
+            for (int q = 0; q < 2; ++q) {
+                c.at = GLU ? 16 * q : 32 * q;
+                c.out_at = GLU ? 16 * q : 32 * q;
+                c.col = col + c.out_at;
+                c.res_at = c.out_at * (p.epi.residual_type == kTypeF32 ? 4 : 2) % kLinRowBytes;
+                if (copied && c.res_at == 0 && q > 0 && c.col < p.epi.N) {          // 32-bit residual: the other half of the columns
+                    fetch_residual(p.epi, mem, bar_res, c.row0 + lane, c.lo, c.hi, c.col, lane);
+                    if (!mbar_wait(bar_res, res_parity, abort_flag) && !*abort_flag) { atomicExch(&g_kq_device_error, KQ_DEV_TIMEOUT_GEMM_EPILOGUE); *abort_flag = 1; }
+                    res_parity ^= 1u;
                 }
+                if (c.col < p.epi.N) epilogue_chunk<GLU>(p.epi, r[0], mem, c, lane);
+#pragma unroll
+                for (int x = 0; x < 32; ++x) r[0][x] = r[1][x];
             }
         }
     }
@@ -540,8 +656,8 @@ linear_mxfp4_pair(const __grid_constant__ CUtensorMap tmap_a, const __grid_const
     __syncthreads();
     if (*abort_flag && threadIdx.x == 0 && rank == 0) {
         int never = 0;
-        for (int m = (issued > kLinPStages ? issued - kLinPStages : 0); m < issued; ++m)
-            if (!mbar_wait(bar_full(m % kLinPStages), (m / kLinPStages) & 1, &never))
+        for (int m = (issued > kLinStages ? issued - kLinStages : 0); m < issued; ++m)
+            if (!mbar_wait(bar_full(m % kLinStages), (m / kLinStages) & 1, &never))
                 atomicExch(&g_kq_device_error, KQ_DEV_TIMEOUT_GEMM_DRAIN);
     }
     __syncthreads();

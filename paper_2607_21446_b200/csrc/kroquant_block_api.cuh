@@ -77,7 +77,7 @@ template <bool GLU>
 kq_status_t launch_pair(LinearLaunch& l, EncodeTiledFn enc, int sms, cudaStream_t st) {
     static DeviceOnce attr_done;
     if (attr_done.needed()) {
-        if (cudaFuncSetAttribute(kq::linear_mxfp4_pair<GLU>, cudaFuncAttributeMaxDynamicSharedMemorySize, kq::kLinPDynBytes) != cudaSuccess) {
+        if (cudaFuncSetAttribute(kq::linear_mxfp4_pair<GLU>, cudaFuncAttributeMaxDynamicSharedMemorySize, kq::kLinDynBytes) != cudaSuccess) {
             (void)cudaGetLastError();
             return KQ_ERR_CUDA;
         }
@@ -86,17 +86,17 @@ kq_status_t launch_pair(LinearLaunch& l, EncodeTiledFn enc, int sms, cudaStream_
     kq::LinearProblem& p = l.p;
     CUtensorMap ta, tb, tsa, tsb;
     const int64_t a_tiles = ((int64_t)p.M + 127) / 128;
-    if (!code_map(enc, &ta, l.a_codes, l.K, p.M, 0, 128) || !code_map(enc, &tb, l.b_codes, l.K, p.R, l.count, 128) ||
+    if (!code_map(enc, &ta, l.a_codes, l.K, p.M, 0, 128) || !code_map(enc, &tb, l.b_codes, l.K, p.R, l.count, kq::kLinN / 2) ||
         !scale_map(enc, &tsa, l.a_scales, l.K, a_tiles, 1) || !scale_map(enc, &tsb, l.b_scales, l.K, (int64_t)p.sf_row_tiles * l.count, 2))
         return KQ_ERR_CUDA;
     p.tiles_m = (p.M + 255) / 256;
-    p.tiles_n = (p.R + 255) / 256;
+    p.tiles_n = (p.R + kq::kLinN - 1) / kq::kLinN;
     // an upper bound of the items: every boundary between two groups can add one row tile
     const int64_t items = ((int64_t)p.tiles_m + (p.experts ? l.count - 1 : 0)) * p.tiles_n;
     const int pairs = (int)(items < sms / 2 ? items : sms / 2);
     cudaLaunchConfig_t cfg;
     cudaLaunchAttribute attr[2];
-    launch_config(&cfg, attr, dim3((unsigned)(2 * pairs)), dim3(kq::kF4PThreads), kq::kLinPDynBytes, 2, st);
+    launch_config(&cfg, attr, dim3((unsigned)(2 * pairs)), dim3(kq::kLinThreads), kq::kLinDynBytes, 2, st);
     return launch(cfg, kq::linear_mxfp4_pair<GLU>, ta, tb, tsa, tsb, p);
 }
 
@@ -176,8 +176,7 @@ kq_status_t run_linear(const uint8_t* a_codes, const uint8_t* a_scales, const ui
     ep.row_scale = e.row_scale;
     ep.residual = e.residual; ep.residual_type = e.residual_dtype; ep.ld_residual = e.ld_residual; ep.residual_scale = e.residual_scale;
     ep.out = out; ep.out_type = out_dtype; ep.ld_out = ld_out;
-    ep.vec = rows_aligned(out, ld_out, out_dtype, 16) && rows_aligned(e.bias, ep.bias.stride, e.bias_dtype, 16) &&
-             rows_aligned(e.gate, e.gate_stride, e.gate_dtype, 16) && rows_aligned(e.residual, e.ld_residual, e.residual_dtype, 16);
+    ep.vec = rows_aligned(out, ld_out, out_dtype, 16) && rows_aligned(e.residual, e.ld_residual, e.residual_dtype, 16);
     ep.wide = rows_aligned(out, ld_out, out_dtype, 32);
     cudaStream_t st = reinterpret_cast<cudaStream_t>(stream);
     // few rows per weight: the weight is the wide operand and is what is read
