@@ -139,8 +139,14 @@ def _check(status: int, where: str) -> None:
         raise KroQuantError(status, where)
 
 
+# the handle itself where torch offers it: building a Stream object around it takes 4 us of a call
+_raw_stream, _device = getattr(torch._C, "_cuda_getCurrentRawStream", None), getattr(torch._C, "_cuda_getDevice", None)
+
+
 def _stream(stream) -> int:
     if stream is None:
+        if _raw_stream is not None and _device is not None:
+            return _raw_stream(_device())
         stream = torch.cuda.current_stream()
     return int(stream.cuda_stream) if hasattr(stream, "cuda_stream") else int(stream)
 
@@ -572,42 +578,38 @@ def interleave_glu(W_gate: torch.Tensor, W_value: torch.Tensor) -> torch.Tensor:
     return out.view(2, blocks, 32, -1).transpose(0, 1).reshape((blocks * 64,) + tuple(W_gate.shape[1:]))
 
 
-def _rows2d(t: torch.Tensor, rows: int, cols: int, what: str) -> int:
-    """Pitch of a [rows, cols] CUDA tensor with contiguous rows."""
-    if t.dim() != 2 or t.shape[0] != rows or t.shape[1] != cols or t.dtype not in _DTYPES or not t.is_cuda or \
-            (cols > 1 and t.stride(1) != 1) or (rows > 1 and t.stride(0) < cols):
-        raise ValueError(f"{what} must be a CUDA float32, bfloat16 or float16 tensor [{rows}, {cols}] with contiguous rows that do not overlap")
-    return t.stride(0) if rows > 1 else max(t.stride(0), cols)
-
-
-def _operand(codes: torch.Tensor, scales: torch.Tensor, what: str) -> None:
-    if codes.dtype != torch.uint8 or scales.dtype != torch.uint8 or not codes.is_cuda or not scales.is_cuda or \
-            not codes.is_contiguous() or not scales.is_contiguous():
-        raise ValueError(f"codes and scales of {what} must be contiguous CUDA uint8 tensors")
+def _rows2d(t: torch.Tensor, shape, what: str) -> int:
+    """Pitch of a CUDA tensor of this 2-D shape with contiguous rows."""
+    if t.shape == shape and t.dtype in _DTYPES and t.is_cuda:
+        if t.is_contiguous():
+            return shape[1]
+        rows, cols = shape
+        if (cols <= 1 or t.stride(1) == 1) and (rows <= 1 or t.stride(0) >= cols):
+            return t.stride(0) if rows > 1 else cols
+    raise ValueError(f"{what} must be a CUDA float32, bfloat16 or float16 tensor {list(shape)} with contiguous rows that do not overlap")
 
 
 def _linear(a_codes, a_scales, b_codes, b_scales, offsets, features, bias, activation, glu, gate, rows_per_gate, row_scale,
-            residual, residual_scale, out, out_dtype, stream, where):
-    grouped = offsets is not None
-    _operand(a_codes, a_scales, "A")
-    _operand(b_codes, b_scales, "B")
-    if a_codes.dim() != 2 or b_codes.dim() != (3 if grouped else 2) or b_codes.shape[-1] != a_codes.shape[1]:
+            residual, residual_scale, out, out_dtype, stream):
+    for t in (a_codes, a_scales, b_codes, b_scales):
+        if t.dtype is not torch.uint8 or not t.is_cuda or not t.is_contiguous():
+            raise ValueError("codes and scales must be contiguous CUDA uint8 tensors")
+    a_shape, b_shape, grouped = a_codes.shape, b_codes.shape, offsets is not None
+    if len(a_shape) != 2 or len(b_shape) != (3 if grouped else 2) or b_shape[-1] != a_shape[1]:
         raise ValueError("A is [M, K/2] codes, B [rows, K/2] ([experts, rows, K/2] in the grouped call) with the same K")
-    M, half = a_codes.shape
-    K, R = 2 * half, b_codes.shape[-2]
-    experts = b_codes.shape[0] if grouped else 1
+    M, K, R, experts = a_shape[0], 2 * a_shape[1], b_shape[-2], b_shape[0] if grouped else 1
     if a_scales.numel() != tiled_scale_bytes(M, K) or b_scales.numel() != experts * tiled_scale_bytes(R, K):
         raise ValueError("scales must be in the tiled layout (tiled_scale_bytes(rows, K) bytes, per expert for B)")
-    N = (R // 2 if glu else R) if features is None else int(features)
-    if (glu and R != 64 * ((N + 31) // 32)) or (not glu and R != N):
+    N = (R // 2 if glu else R) if features is None else features
+    if R != (64 * ((N + 31) // 32) if glu else N):
         raise ValueError("B must have `features` rows, or 64 * ceil(features / 32) interleaved rows with glu")
-    if activation not in ACTIVATIONS:
+    act = ACTIVATIONS.get(activation)
+    if act is None:
         raise ValueError(f"activation must be one of {sorted(ACTIVATIONS)}")
-    device = a_codes.device
     e = _Epilogue()
-    e.activation, e.glu, e.rows_per_gate, e.residual_scale = ACTIVATIONS[activation], 1 if glu else 0, 1, residual_scale
+    e.activation, e.glu, e.rows_per_gate, e.residual_scale = act, 1 if glu else 0, 1, residual_scale
     if bias is not None:
-        if tuple(bias.shape) != ((experts, R) if grouped else (R,)) or bias.dtype not in _DTYPES or not bias.is_cuda or not bias.is_contiguous():
+        if bias.shape != ((experts, R) if grouped else (R,)) or bias.dtype not in _DTYPES or not bias.is_cuda or not bias.is_contiguous():
             raise ValueError("bias must be a contiguous CUDA floating tensor with one entry per row of B")
         e.bias, e.bias_dtype = bias.data_ptr(), _DTYPES[bias.dtype]
     if gate is not None:
@@ -623,21 +625,20 @@ def _linear(a_codes, a_scales, b_codes, b_scales, offsets, features, bias, activ
             raise ValueError("gate has too few rows for rows_per_gate")
         e.gate, e.gate_dtype, e.gate_stride, e.rows_per_gate = gate.data_ptr(), _DTYPES[gate.dtype], gate.stride(0) if rows > 1 else 0, rows_per_gate
     if row_scale is not None:
-        if tuple(row_scale.shape) != (M,) or row_scale.dtype != torch.float32 or not row_scale.is_cuda or not row_scale.is_contiguous():
+        if row_scale.shape != (M,) or row_scale.dtype is not torch.float32 or not row_scale.is_cuda or not row_scale.is_contiguous():
             raise ValueError("row_scale must be a contiguous CUDA float32 tensor [M]")
         e.row_scale = row_scale.data_ptr()
     if residual is not None:
-        e.ld_residual = _rows2d(residual, M, N, "residual")
+        e.ld_residual = _rows2d(residual, (M, N), "residual")
         e.residual, e.residual_dtype = residual.data_ptr(), _DTYPES[residual.dtype]
     if out is None:
-        out = torch.empty((M, N), dtype=out_dtype, device=device)
-        ld_out = N
+        if out_dtype not in _DTYPES:
+            raise ValueError("out_dtype must be float32, bfloat16 or float16")
+        out, ld_out = a_codes.new_empty((M, N), dtype=out_dtype), N
     else:
-        ld_out = _rows2d(out, M, N, "out")
-    if out.dtype not in _DTYPES:
-        raise ValueError("out_dtype must be float32, bfloat16 or float16")
+        ld_out = _rows2d(out, (M, N), "out")
     if grouped:
-        if offsets.dtype != torch.int32 or tuple(offsets.shape) != (experts + 1,) or not offsets.is_cuda or not offsets.is_contiguous():
+        if offsets.dtype is not torch.int32 or offsets.shape != (experts + 1,) or not offsets.is_cuda or not offsets.is_contiguous():
             raise ValueError("offsets must be a contiguous CUDA int32 tensor [experts + 1]")
         rc = load_library().kroquant_linear_mxfp4_grouped(
             a_codes.data_ptr(), a_scales.data_ptr(), b_codes.data_ptr(), b_scales.data_ptr(), offsets.data_ptr(), experts, M, N, K,
@@ -646,7 +647,8 @@ def _linear(a_codes, a_scales, b_codes, b_scales, offsets, features, bias, activ
         rc = load_library().kroquant_linear_mxfp4(
             a_codes.data_ptr(), a_scales.data_ptr(), b_codes.data_ptr(), b_scales.data_ptr(), M, N, K, C.addressof(e), out.data_ptr(),
             _DTYPES[out.dtype], ld_out, _stream(stream))
-    _check(rc, where)
+    if rc:
+        raise KroQuantError(rc, "kroquant_linear_mxfp4_grouped" if grouped else "kroquant_linear_mxfp4")
     return out
 
 
@@ -667,7 +669,7 @@ def kroquant_linear_mxfp4(a_codes: torch.Tensor, a_scales: torch.Tensor, b_codes
     float32 [M].  bias, gate, residual and out may each be float32, bfloat16 or float16; residual and out may have a row
     pitch, and out may be the residual.  fp32 inside, rounded once."""
     return _linear(a_codes, a_scales, b_codes, b_scales, None, features, bias, activation, glu, gate, rows_per_gate, row_scale,
-                   residual, residual_scale, out, out_dtype, stream, "kroquant_linear_mxfp4")
+                   residual, residual_scale, out, out_dtype, stream)
 
 
 def kroquant_linear_mxfp4_grouped(a_codes: torch.Tensor, a_scales: torch.Tensor, b_codes: torch.Tensor, b_scales: torch.Tensor,
@@ -682,46 +684,50 @@ def kroquant_linear_mxfp4_grouped(a_codes: torch.Tensor, a_scales: torch.Tensor,
     if offsets is None:
         raise ValueError("offsets must be a contiguous CUDA int32 tensor [experts + 1]")
     return _linear(a_codes, a_scales, b_codes, b_scales, offsets, features, bias, activation, glu, None, None, row_scale, residual,
-                   residual_scale, out, out_dtype, stream, "kroquant_linear_mxfp4_grouped")
+                   residual_scale, out, out_dtype, stream)
 
 
-def _norm_vectors(a: "_NormArgs", rows: int, d: int, rows_per_batch, vectors) -> int:
-    """Checks the parameter vectors, fills their pointers and strides; -> batches."""
+def _norm_args(rows: int, d: int, norm: str, post_norm: str, residual_scale: float, eps: float, rows_per_batch, gate, post_weight,
+               weight, scale, shift) -> "_NormArgs":
+    """The arguments that forward and backward share: settings, parameter vectors and their strides."""
+    a = _NormArgs()
+    try:
+        a.norm, a.post_norm = NORMS[norm], NORMS[post_norm]
+    except KeyError:
+        raise ValueError(f"norm and post_norm must be one of {sorted(NORMS)}") from None
+    a.rows, a.d, a.residual_scale, a.eps = rows, d, residual_scale, eps
     batches, dtype = 1, None
-    for name, v, batched in vectors:
+    for name, v in (("gate", gate), ("post_weight", post_weight), ("weight", weight), ("scale", scale), ("shift", shift)):
         if v is None:
             continue
-        if v.dim() not in ((1, 2) if batched else (1,)) or v.shape[-1] != d or v.dtype not in _DTYPES or not v.is_cuda or \
-                (d > 1 and v.stride(-1) != 1) or (v.dim() == 2 and v.shape[0] > 1 and v.stride(0) < d):
-            raise ValueError(f"{name} must be a CUDA floating tensor [d]" + (" or [batches, d] with contiguous rows" if batched else ""))
+        shape = v.shape
         if dtype is None:
             dtype = v.dtype
-        elif v.dtype != dtype:
+        batched = len(shape) == 2 and name != "weight" and name != "post_weight"
+        if shape[-1:] != (d,) or (len(shape) != 1 and not batched) or v.dtype not in _DTYPES or not v.is_cuda or \
+                not (v.is_contiguous() or ((d <= 1 or v.stride(-1) == 1) and (not batched or shape[0] <= 1 or v.stride(0) >= d))):
+            raise ValueError(f"{name} must be a CUDA floating tensor [d]" + ("" if "weight" in name else " or [batches, d] with contiguous rows"))
+        if v.dtype is not dtype:
             raise ValueError("gate, post_weight, weight, scale and shift must share a dtype")
         setattr(a, name, v.data_ptr())
-        if v.dim() == 2:
-            if batches not in (1, v.shape[0]) and v.shape[0] != 1:
+        if batched and shape[0] != 1:
+            if batches != 1 and batches != shape[0]:
                 raise ValueError("batched vectors must agree on the number of batches")
-            batches = max(batches, v.shape[0])
-            # a gradient keeps the shape of its vector, so one row of [1, d] counts as one vector for all rows
-            setattr(a, name + "_stride", v.stride(0) if v.shape[0] > 1 else 0)
-    a.vec_dtype = _DTYPES[dtype] if dtype is not None else 0
+            batches = shape[0]
+            # (a gradient keeps the shape of its vector, so one row of [1, d] counts as one vector for all rows)
+            setattr(a, name + "_stride", v.stride(0))
+    if dtype is not None:
+        a.vec_dtype = _DTYPES[dtype]
     if batches == 1:
-        rows_per_batch = max(rows, 1)
+        rows_per_batch = rows or 1
     elif rows_per_batch is None:
-        if rows % batches:
+        if batches < 1 or rows % batches:
             raise ValueError("rows is not a multiple of the batches: pass rows_per_batch")
-        rows_per_batch = max(rows // batches, 1)
-    if rows_per_batch < 1 or (rows + rows_per_batch - 1) // rows_per_batch > batches:
+        rows_per_batch = rows // batches or 1
+    if rows_per_batch < 1 or rows > batches * rows_per_batch:
         raise ValueError("the batched vectors have too few rows for rows_per_batch")
     a.rows_per_batch = rows_per_batch
-    return batches
-
-
-def _norm_kinds(a: "_NormArgs", norm: str, post_norm: str) -> None:
-    if norm not in NORMS or post_norm not in NORMS:
-        raise ValueError(f"norm and post_norm must be one of {sorted(NORMS)}")
-    a.norm, a.post_norm = NORMS[norm], NORMS[post_norm]
+    return a
 
 
 def kroquant_norm_residual(x: torch.Tensor, y: Optional[torch.Tensor] = None, *, gate: Optional[torch.Tensor] = None,
@@ -742,39 +748,40 @@ def kroquant_norm_residual(x: torch.Tensor, y: Optional[torch.Tensor] = None, *,
     norm "none": n is None.  h_out may be x and n_out may be y."""
     if x.dim() != 2:
         raise ValueError("x must be [rows, d]")
-    rows, d = x.shape
-    a = _NormArgs()
-    _norm_kinds(a, norm, post_norm)
-    a.rows, a.d, a.residual_scale, a.eps = rows, d, residual_scale, eps
-    a.x, a.ld_x, a.stream_dtype = x.data_ptr(), _rows2d(x, rows, d, "x"), _DTYPES[x.dtype]
+    shape = x.shape
+    a = _norm_args(shape[0], shape[1], norm, post_norm, residual_scale, eps, rows_per_batch, gate, post_weight, weight, scale, shift)
+    a.ld_x = _rows2d(x, shape, "x")
+    a.x, a.stream_dtype = x.data_ptr(), _DTYPES[x.dtype]
     if y is not None:
-        a.y, a.ld_y = y.data_ptr(), _rows2d(y, rows, d, "y")
-        branch_dtype = y.dtype
+        a.ld_y = _rows2d(y, shape, "y")
+        a.y, branch_dtype = y.data_ptr(), y.dtype
     elif branch_dtype is None:
         branch_dtype = x.dtype
     if branch_dtype not in _DTYPES:
         raise ValueError("branch_dtype must be float32, bfloat16 or float16")
     a.branch_dtype = _DTYPES[branch_dtype]
-    _norm_vectors(a, rows, d, rows_per_batch, (("gate", gate, True), ("post_weight", post_weight, False), ("weight", weight, False),
-                                               ("scale", scale, True), ("shift", shift, True)))
     h, n = h_out, n_out
-    if h is None and (y is not None or residual_scale != 1.0 or norm == "none"):
-        h = torch.empty((rows, d), dtype=x.dtype, device=x.device)
     if h is not None:
-        a.ld_h = _rows2d(h, rows, d, "h_out")
-        if h.dtype != x.dtype:
+        a.ld_h = _rows2d(h, shape, "h_out")
+        if h.dtype is not x.dtype:
             raise ValueError("h_out must have x's dtype")
         a.h = h.data_ptr()
+    elif y is not None or residual_scale != 1.0 or norm == "none":
+        h = x.new_empty(shape)
+        a.h, a.ld_h = h.data_ptr(), shape[1]
     if norm == "none":
         n = None
-    else:
-        if n is None:
-            n = torch.empty((rows, d), dtype=branch_dtype, device=x.device)
-        a.ld_n = _rows2d(n, rows, d, "n_out")
-        if n.dtype != branch_dtype:
+    elif n is not None:
+        a.ld_n = _rows2d(n, shape, "n_out")
+        if n.dtype is not branch_dtype:
             raise ValueError("n_out must have the branch's dtype")
         a.n = n.data_ptr()
-    _check(load_library().kroquant_norm_residual(C.addressof(a), _stream(stream)), "kroquant_norm_residual")
+    else:
+        n = x.new_empty(shape, dtype=branch_dtype)
+        a.n, a.ld_n = n.data_ptr(), shape[1]
+    rc = load_library().kroquant_norm_residual(C.addressof(a), _stream(stream))
+    if rc:
+        raise KroQuantError(rc, "kroquant_norm_residual")
     return (x if h is None else h), n
 
 
@@ -789,48 +796,58 @@ def kroquant_norm_residual_grad(dn: Optional[torch.Tensor], h: torch.Tensor, *, 
     a float32 gradient ("dgate", "dpost_weight", "dweight", "dscale", "dshift") in the shape of every vector given."""
     if h.dim() != 2:
         raise ValueError("h must be [rows, d]")
-    rows, d = h.shape
-    a = _NormArgs()
-    _norm_kinds(a, norm, post_norm)
-    a.rows, a.d, a.residual_scale, a.eps = rows, d, residual_scale, eps
-    a.h, a.ld_h, a.stream_dtype = h.data_ptr(), _rows2d(h, rows, d, "h"), _DTYPES[h.dtype]
+    shape = h.shape
+    rows, d = shape
+    a = _norm_args(rows, d, norm, post_norm, residual_scale, eps, rows_per_batch, gate, post_weight, weight, scale, shift)
+    a.ld_h = _rows2d(h, shape, "h")
+    a.h, a.stream_dtype = h.data_ptr(), _DTYPES[h.dtype]
     if (dn is None) != (norm == "none"):
         raise ValueError("dn goes with a norm")
     branch_dtype = dn.dtype if dn is not None else y.dtype if y is not None else h.dtype
     if dn is not None:
-        a.dn, a.ld_dn = dn.data_ptr(), _rows2d(dn, rows, d, "dn")
+        a.ld_dn = _rows2d(dn, shape, "dn")
+        a.dn = dn.data_ptr()
     if dh is not None:
-        a.dh, a.ld_dh = dh.data_ptr(), _rows2d(dh, rows, d, "dh")
-        if dh.dtype != h.dtype:
+        a.ld_dh = _rows2d(dh, shape, "dh")
+        if dh.dtype is not h.dtype:
             raise ValueError("dh must have h's dtype")
+        a.dh = dh.data_ptr()
     if y is not None:
-        a.y, a.ld_y = y.data_ptr(), _rows2d(y, rows, d, "y")
-        if y.dtype != branch_dtype:
+        a.ld_y = _rows2d(y, shape, "y")
+        if y.dtype is not branch_dtype:
             raise ValueError("y and dn must share a dtype")
-    elif gate is not None or (post_weight is not None and post_norm != "none"):
+        a.y = y.data_ptr()
+    elif gate is not None or post_weight is not None:
         raise ValueError("gate and post_weight act on the branch: y is needed")
-    if branch_dtype not in _DTYPES:
-        raise ValueError("dn and y must be float32, bfloat16 or float16")
     a.branch_dtype = _DTYPES[branch_dtype]
-    vectors = (("gate", gate, True), ("post_weight", post_weight, False), ("weight", weight, False), ("scale", scale, True),
-               ("shift", shift, True))
-    _norm_vectors(a, rows, d, rows_per_batch, vectors)
-    out = {"dx": torch.empty((rows, d), dtype=h.dtype, device=h.device)}
-    a.dx, a.ld_dx = out["dx"].data_ptr(), d
+    dx = h.new_empty(shape)
+    out = {"dx": dx}
+    a.dx, a.ld_dx = dx.data_ptr(), d
     if y is not None:
-        out["dy"] = torch.empty((rows, d), dtype=branch_dtype, device=h.device)
-        a.dy, a.ld_dy = out["dy"].data_ptr(), d
-    covered = (rows + a.rows_per_batch - 1) // a.rows_per_batch          # batches that have rows: the kernel writes those
-    for name, v, _ in vectors:
-        if v is not None:
-            short = v.dim() == 2 and v.shape[0] > covered
-            out["d" + name] = g = (torch.zeros if short else torch.empty)(v.shape, dtype=torch.float32, device=h.device)
-            setattr(a, "d" + name, g.data_ptr())
-    L = load_library()
-    nbytes = int(L.kroquant_norm_residual_grad_scratch_bytes(C.addressof(a)))
-    scratch = torch.empty(nbytes, dtype=torch.uint8, device=h.device) if nbytes else None
-    _check(L.kroquant_norm_residual_grad(C.addressof(a), scratch.data_ptr() if nbytes else None, nbytes, _stream(stream)),
-           "kroquant_norm_residual_grad")
+        out["dy"] = dy = h.new_empty(shape, dtype=branch_dtype)
+        a.dy, a.ld_dy = dy.data_ptr(), d
+    vectors = [(n, v.shape) for n, v in (("dgate", gate), ("dpost_weight", post_weight), ("dweight", weight), ("dscale", scale),
+                                         ("dshift", shift)) if v is not None]
+    if vectors:
+        # the gradients are one allocation; the kernel's scratch space is another, so that it is free again after the call
+        sizes = [s.numel() for _, s in vectors]
+        a.dweight = 16                                                # any pointer: whether vector gradients are wanted at all
+        nbytes = load_library().kroquant_norm_residual_grad_scratch_bytes(C.addressof(a))
+        a.dweight = None
+        store, scratch = h.new_empty(sum(sizes), dtype=torch.float32), h.new_empty(nbytes, dtype=torch.uint8)
+        covered = (rows + a.rows_per_batch - 1) // a.rows_per_batch      # batches that have rows: the kernel writes those
+        base, pos = store.data_ptr(), 0
+        for (name, s), size in zip(vectors, sizes):
+            out[name] = g = store.as_strided(s, (d, 1) if len(s) == 2 else (1,), pos)
+            setattr(a, name, base + 4 * pos)
+            if len(s) == 2 and s[0] > covered:
+                g.zero_()
+            pos += size
+        rc = load_library().kroquant_norm_residual_grad(C.addressof(a), scratch.data_ptr() if nbytes else None, nbytes, _stream(stream))
+    else:
+        rc = load_library().kroquant_norm_residual_grad(C.addressof(a), None, 0, _stream(stream))
+    if rc:
+        raise KroQuantError(rc, "kroquant_norm_residual_grad")
     return out
 
 

@@ -22,7 +22,6 @@ NVCC_FLAGS = [
     "-gencode", "arch=compute_100a,code=sm_100a",
     "-shared", "-Xcompiler", "-fPIC",
     "-Xptxas", "-v",
-    "--split-compile=0",          # the back end on all cores
 ]
 
 

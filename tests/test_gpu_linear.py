@@ -102,6 +102,37 @@ def test_plain_product_of_every_size(M, N, K):
     _check_device()
 
 
+@pytest.mark.parametrize("M,N,K", [(4099, 2001, 256), (6000, 1504, 1152)])
+@pytest.mark.parametrize("residual", [False, True])
+def test_several_tiles_per_cta(M, N, K, residual):
+    """More tiles than the GPU runs at once: stages, scale slots and both accumulators go round."""
+    qa, sa, a = _quantized(M, K, 41)
+    qw, sw, w = _quantized(N, K, 42)
+    bias = torch.randn(N, device="cuda", generator=_gen(43))
+    for dt in (torch.float32, torch.bfloat16):
+        res = torch.randn(M, N, device="cuda", generator=_gen(44)).to(dt) if residual else None
+        for _ in range(3):
+            out = kb.kroquant_linear_mxfp4(qa, sa, qw, sw, bias=bias, activation="silu", residual=res, out_dtype=dt)
+        _check(out, *_reference(a, w, N, "silu", False, bias, residual=res))
+    _check_device()
+
+
+@pytest.mark.parametrize("glu", [False, True])
+def test_several_tiles_per_cta_in_groups(glu):
+    sizes, N, K = [2000, 0, 1500, 3000], 1504, 544
+    R = 2 * N if glu else N
+    qa, sa, a = _quantized(sum(sizes), K, 45)
+    w = [_quantized(R, K, 46 + e) for e in range(4)]
+    out = kb.kroquant_linear_mxfp4_grouped(qa, sa, torch.stack([x[0] for x in w]), torch.stack([x[1] for x in w]), _groups(sizes),
+                                           activation="silu", glu=glu)
+    lo = 0
+    for e, n in enumerate(sizes):
+        if n:
+            _check(out[lo:lo + n], *_reference(a[lo:lo + n], w[e][2], N, "silu", glu))
+        lo += n
+    _check_device()
+
+
 @pytest.mark.parametrize("M", [1, 40, 100, 700])
 @pytest.mark.parametrize("act", ["none", "relu", "silu", "gelu", "gelu_tanh"])
 @pytest.mark.parametrize("glu", [False, True])
