@@ -242,6 +242,9 @@ struct NormForward {
     float alpha, eps;
     int norm, post;
     int vec;                          // every pointer, pitch and d allow 16-byte accesses
+    // staged kernel: rows of a worker, stages, bytes of a stage, offset of y, which parameter vectors are kept in shared memory
+    int64_t rows_per_worker;
+    int stages, stage_bytes, off_y, cache;
 };
 
 // blockDim = (threads of a row, rows of a CTA): one warp per row and several rows for narrow d, else one row per CTA.
@@ -1026,6 +1029,241 @@ __global__ void __launch_bounds__(kNormThreads, 1) norm_residual_backward(const 
     }
     if (p.partial) flush(worker + batch);
     if (p.cluster > 1) cluster_barrier();                             // nobody's shared memory goes away while a peer writes to it
+}
+
+// ---- forward, many wide rows: persistent CTAs, rows staged in shared memory --------------------------------
+// The kernel above starts a CTA per row, whose load latency, two reductions and parameter reads follow one another; with many
+// rows that is what it costs (8192 x 2240, layer norm, gate and modulation: 44 us).  Here a CTA keeps its threads, its parameter
+// vectors (shared memory) and two rows at a time, which share every barrier and every sum over a warp, while the next rows
+// arrive by bulk copies.  Statistics in one pass about a sampled pivot, as in the backward kernel; h stays in registers.
+constexpr int kNormFwdRedOff = 128;
+constexpr int kNormFwdHead = kNormFwdRedOff + 4 * 32 * 16;            // two sets of sums for each of the two norms, used in turn
+enum { kCacheGate = 1, kCachePost = 2, kCacheMul = 4, kCacheShift = 8 };
+
+template <typename S, typename Y, int VPT, bool POST>
+__global__ void __launch_bounds__(1024, 1) norm_residual_forward_rows(const __grid_constant__ NormForward p) {
+    extern __shared__ __align__(128) uint8_t smem[];
+    const uint32_t base = smem_u32(smem);
+    volatile int* abort_flag = reinterpret_cast<volatile int*>(smem + 120);
+    float4* red = reinterpret_cast<float4*>(smem + kNormFwdRedOff);
+    const int T = (int)blockDim.x, t = (int)threadIdx.x, warp = t >> 5, lane = t & 31, warps = T >> 5;
+    const int plane = p.d >> 1;                                       // a vector: the first, then the last four entries of every group
+    float* at_vec = reinterpret_cast<float*>(smem + kNormFwdHead);
+    float* par_gate = at_vec;
+    float* par_post = par_gate + (p.cache & kCacheGate ? p.d : 0);
+    float* par_mul = par_post + (p.cache & kCachePost ? p.d : 0);
+    float* par_shift = par_mul + (p.cache & kCacheMul ? p.d : 0);
+    const int stage0 = kNormFwdHead + 4 * p.d * __popc((unsigned)p.cache);
+    const int64_t first = (int64_t)blockIdx.x * p.rows_per_worker;
+    const int rows = (int)(first + p.rows_per_worker < p.rows ? p.rows_per_worker : p.rows - first);
+    const float inv_d = 1.0f / (float)p.d;
+    const bool layer_h = p.norm == kNormLayer, layer_y = POST && p.post == kNormLayer, norm = p.norm != kNormNone;
+    if (t == 0) {
+        for (int s = 0; s < p.stages; ++s) mbar_init(base + 8u * s, 1);
+        *abort_flag = 0;
+        asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+        asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+    }
+    __syncthreads();
+    pdl_wait_prior_grid();
+    auto issue = [&](int r, int s) {                                  // thread 0: row `r` of this worker into stage s
+        const uint32_t bar = base + 8u * s, dst = base + (uint32_t)(stage0 + s * p.stage_bytes);
+        mbar_expect_tx(bar, (uint32_t)p.d * (uint32_t)(sizeof(S) + (p.y ? sizeof(Y) : 0)));
+        bulk_load(dst, static_cast<const S*>(p.x) + (first + r) * p.ld_x, (uint32_t)p.d * sizeof(S), bar);
+        if (p.y) bulk_load(dst + p.off_y, static_cast<const Y*>(p.y) + (first + r) * p.ld_y, (uint32_t)p.d * sizeof(Y), bar);
+    };
+    int next = p.stages < rows ? p.stages : rows;
+    if (t == 0)
+        for (int r = 0; r < next; ++r) issue(r, r);
+    int64_t batch = first / p.rows_per_batch;
+    auto rows_left = [&](int64_t row) { const int64_t n = (batch + 1) * p.rows_per_batch - row; return (int)(n < rows ? n : rows); };
+    int batch_end = rows_left(first);
+    bool have[VPT];
+#pragma unroll
+    for (int k = 0; k < VPT; ++k) have[k] = (t + k * T) * 8 < p.d;
+    const int sample = (int)((int64_t)lane * p.d / 32);
+    float gate_s = 1.f, post_s = 1.f;                                 // gate and post_weight at this lane's sampled channel
+    auto refresh = [&]() {                                            // every thread its own groups
+#pragma unroll
+        for (int k = 0; k < VPT; ++k)
+            if (have[k]) {
+                const int gi = t + k * T, c = gi * 8;
+                float m[8], a[8];
+                auto keep = [&](float* vector) {
+                    reinterpret_cast<float4*>(vector)[gi] = make_float4(m[0], m[1], m[2], m[3]);
+                    reinterpret_cast<float4*>(vector + plane)[gi] = make_float4(m[4], m[5], m[6], m[7]);
+                };
+                if (p.cache & kCacheGate) { load_param(p.gate, batch, c, 8, true, 1, 1.f, m); keep(par_gate); }
+                if (p.cache & kCachePost) { load_param(p.post_weight, 0, c, 8, true, 1, 1.f, m); keep(par_post); }
+                if (p.cache & kCacheShift) { load_param(p.shift, batch, c, 8, true, 1, 0.f, m); keep(par_shift); }
+                if (p.cache & kCacheMul) {
+                    load_param(p.weight, 0, c, 8, true, 1, 1.f, m);
+                    load_param(p.scale, batch, c, 8, true, 1, 0.f, a);
+#pragma unroll
+                    for (int i = 0; i < 8; ++i) m[i] = fmaf(m[i], a[i], m[i]);
+                    keep(par_mul);
+                }
+            }
+        if (layer_h && p.y) {
+            gate_s = vec_entry(p.gate, batch, sample, 1.f);
+            post_s = vec_entry(p.post_weight, 0, sample, 1.f);
+        }
+    };
+    refresh();
+    // eight entries of a vector: kept, read through the caches, or absent
+    auto entries = [&](int bit, const float* vector, const NormVec& v, int64_t which, int gi, float none, f32x2 (&m)[4]) {
+        if (p.cache & bit) {
+            const ulonglong2 a = reinterpret_cast<const ulonglong2*>(vector)[gi], b = reinterpret_cast<const ulonglong2*>(vector + plane)[gi];
+            m[0] = a.x; m[1] = a.y; m[2] = b.x; m[3] = b.y;
+        } else {
+            float f[8];
+            load_param(v, which, gi * 8, 8, true, 1, none, f);
+#pragma unroll
+            for (int i = 0; i < 4; ++i) m[i] = pack2(f[2 * i], f[2 * i + 1]);
+        }
+    };
+    auto sum32 = [&](float v) {
+#pragma unroll
+        for (int o = 16; o > 0; o >>= 1) v += __shfl_xor_sync(0xFFFFFFFFu, v, o);
+        return v;
+    };
+    // {s1, s2} of both rows over the CTA
+    auto row_sums = [&](float (&v)[4], int set) {
+        warp_sum4(v, lane);
+        if (lane == 0) red[set * 32 + warp] = make_float4(v[0], v[1], v[2], v[3]);
+        __syncthreads();
+        const float4 a = lane < warps ? red[set * 32 + lane] : make_float4(0.f, 0.f, 0.f, 0.f);
+        v[0] = a.x; v[1] = a.y; v[2] = a.z; v[3] = a.w;
+        warp_sum4(v, lane);
+    };
+    const f32x2 alpha2 = pack2(p.alpha, p.alpha);
+    int s = 0, turn = 0;
+    uint32_t parity = 0;
+    for (int r = 0, nr; r < rows; r += nr) {
+        if (r == batch_end) {
+            ++batch;
+            batch_end = r + rows_left(first + r);
+            refresh();
+        }
+        nr = r + 1 < rows && r + 1 < batch_end ? 2 : 1;
+        const uint8_t* stage[2];
+#pragma unroll
+        for (int j = 0; j < 2; ++j) {
+            stage[j] = smem + stage0 + s * p.stage_bytes;
+            if (j < nr) {
+                // a wait that gives up records it and goes on (the barriers below stay matched)
+                if (!mbar_wait(base + 8u * s, parity, abort_flag) && !*abort_flag) {
+                    atomicExch(&g_kq_device_error, KQ_DEV_TIMEOUT_NORM);
+                    *abort_flag = 1;
+                }
+                if (++s == p.stages) { s = 0; parity ^= 1u; }
+            }
+        }
+        if (nr == 1) stage[1] = stage[0];                            // (computed twice, stored once)
+        float mean_y[2] = {0.f, 0.f}, inv_y[2] = {1.f, 1.f};
+        if (POST) {
+            float v[4] = {0.f, 0.f, 0.f, 0.f}, pivot[2] = {0.f, 0.f};
+#pragma unroll
+            for (int j = 0; j < 2; ++j) {
+                if (layer_y) pivot[j] = sum32(Elem<Y>::to_f32(reinterpret_cast<const Y*>(stage[j] + p.off_y)[sample])) * 0.03125f;
+                const f32x2 minus = pack2(-pivot[j], -pivot[j]);
+                f32x2 s1 = 0ull, s2 = 0ull;
+#pragma unroll
+                for (int k = 0; k < VPT; ++k)
+                    if (have[k]) {
+                        f32x2 y[4];
+                        lds8<Y>(stage[j] + p.off_y, t + k * T, y);
+#pragma unroll
+                        for (int i = 0; i < 4; ++i) {
+                            const f32x2 u = add2(y[i], minus);
+                            s1 = add2(s1, u);
+                            s2 = fma2(u, u, s2);
+                        }
+                    }
+                v[2 * j] = sum2(s1);
+                v[2 * j + 1] = sum2(s2);
+            }
+            row_sums(v, turn);
+#pragma unroll
+            for (int j = 0; j < 2; ++j) {
+                const float shift = layer_y ? v[2 * j] * inv_d : 0.f;
+                mean_y[j] = pivot[j] + shift;
+                inv_y[j] = rsqrtf(fmaf(v[2 * j + 1], inv_d, -shift * shift) + p.eps);
+            }
+        }
+        f32x2 h[2][VPT][4];
+        float v[4] = {0.f, 0.f, 0.f, 0.f}, pivot[2] = {0.f, 0.f};
+#pragma unroll
+        for (int j = 0; j < 2; ++j) {
+            if (layer_h) {
+                float q = p.alpha * Elem<S>::to_f32(reinterpret_cast<const S*>(stage[j])[sample]);
+                if (p.y) q = fmaf(gate_s, (Elem<Y>::to_f32(reinterpret_cast<const Y*>(stage[j] + p.off_y)[sample]) - mean_y[j]) * inv_y[j] * post_s, q);
+                pivot[j] = sum32(q) * 0.03125f;
+            }
+            const f32x2 minus = pack2(-pivot[j], -pivot[j]), off_y = pack2(-mean_y[j], -mean_y[j]), inv_y2 = pack2(inv_y[j], inv_y[j]);
+            f32x2 s1 = 0ull, s2 = 0ull;
+#pragma unroll
+            for (int k = 0; k < VPT; ++k)
+                if (have[k]) {
+                    const int gi = t + k * T;
+                    f32x2 x[4], m[4];
+                    lds8<S>(stage[j], gi, x);
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) h[j][k][i] = mul2(alpha2, x[i]);
+                    if (p.y) {
+                        lds8<Y>(stage[j] + p.off_y, gi, x);
+                        if (POST) {
+                            entries(kCachePost, par_post, p.post_weight, 0, gi, 1.f, m);
+#pragma unroll
+                            for (int i = 0; i < 4; ++i) x[i] = mul2(mul2(add2(x[i], off_y), inv_y2), m[i]);
+                        }
+                        entries(kCacheGate, par_gate, p.gate, batch, gi, 1.f, m);
+#pragma unroll
+                        for (int i = 0; i < 4; ++i) h[j][k][i] = fma2(m[i], x[i], h[j][k][i]);
+                    }
+                    if (p.h && j < nr) store_pairs(static_cast<S*>(p.h) + (first + r + j) * p.ld_h + gi * 8, 8, true, h[j][k]);
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) {
+                        const f32x2 u = add2(h[j][k][i], minus);
+                        s1 = add2(s1, u);
+                        s2 = fma2(u, u, s2);
+                    }
+                }
+            v[2 * j] = sum2(s1);
+            v[2 * j + 1] = sum2(s2);
+        }
+        row_sums(v, 2 + turn);
+        turn ^= 1;
+        // every thread has read its part of these rows: their stages take the rows that follow
+        if (t == 0)
+            for (; next < rows && next < r + nr + p.stages; ++next) issue(next, next % p.stages);
+        if (!norm) continue;
+#pragma unroll
+        for (int j = 0; j < 2; ++j)
+            if (j < nr) {
+                const float shift = layer_h ? v[2 * j] * inv_d : 0.f, mean = pivot[j] + shift;
+                const float inv = rsqrtf(fmaf(v[2 * j + 1], inv_d, -shift * shift) + p.eps);
+                const f32x2 off = pack2(-mean, -mean), inv2 = pack2(inv, inv);
+#pragma unroll
+                for (int k = 0; k < VPT; ++k)
+                    if (have[k]) {
+                        const int gi = t + k * T;
+                        f32x2 m[4], a[4];
+                        if (p.cache & kCacheMul) {
+                            entries(kCacheMul, par_mul, p.weight, 0, gi, 1.f, m);
+                        } else {
+                            entries(0, par_mul, p.weight, 0, gi, 1.f, m);
+                            entries(0, par_mul, p.scale, batch, gi, 0.f, a);
+#pragma unroll
+                            for (int i = 0; i < 4; ++i) m[i] = fma2(m[i], a[i], m[i]);
+                        }
+                        entries(kCacheShift, par_shift, p.shift, batch, gi, 0.f, a);
+#pragma unroll
+                        for (int i = 0; i < 4; ++i) a[i] = fma2(mul2(add2(h[j][k][i], off), inv2), m[i], a[i]);
+                        store_pairs(static_cast<Y*>(p.n) + (first + r + j) * p.ld_n + gi * 8, 8, true, a);
+                    }
+            }
+    }
 }
 
 struct NormVecGrads {

@@ -239,8 +239,55 @@ bool norm_vectors_vec(const kq_norm_args_t& a) {
            rows_aligned(a.weight, 0, v, 16) && rows_aligned(a.scale, a.scale_stride, v, 16) && rows_aligned(a.shift, a.shift_stride, v, 16);
 }
 
+constexpr int kSmemPerSm = 228 * 1024, kSmemPerCta = 227 * 1024;
+
+template <typename S, typename Y, int VPT, bool POST>
+kq_status_t launch_norm_rows(kq::NormForward& p, int threads, int sms, cudaStream_t st) {
+    static DeviceOnce attr_done;
+    if (attr_done.needed()) {
+        if (cudaFuncSetAttribute(kq::norm_residual_forward_rows<S, Y, VPT, POST>, cudaFuncAttributeMaxDynamicSharedMemorySize, kSmemPerCta) != cudaSuccess) {
+            (void)cudaGetLastError();
+            return KQ_ERR_CUDA;
+        }
+        attr_done.done();
+    }
+    int per_sm = 1024 / threads;                                     // 64 registers a thread
+    if (per_sm > 4) per_sm = 4;
+    p.off_y = p.d * (int)sizeof(S);
+    p.stage_bytes = p.off_y + (p.y ? p.d * (int)sizeof(Y) : 0);
+    auto room = [&]() { return (per_sm == 1 ? kSmemPerCta : kSmemPerSm / per_sm - 1024) - kq::kNormFwdHead; };
+    auto params = [&]() { return 4 * p.d * __builtin_popcount((unsigned)p.cache); };
+    p.cache = (p.y && p.gate.ptr ? kq::kCacheGate : 0) | (POST && p.post_weight.ptr ? kq::kCachePost : 0) |
+              (p.norm != KQ_NORM_NONE && (p.weight.ptr || p.scale.ptr) ? kq::kCacheMul : 0) | (p.norm != KQ_NORM_NONE && p.shift.ptr ? kq::kCacheShift : 0);
+    // four rows in flight come before the vectors, those before a second CTA
+    while (per_sm > 1 && params() + 4 * p.stage_bytes > room()) --per_sm;
+    if (params() + 4 * p.stage_bytes > room()) p.cache = 0;
+    int stages = (room() - params()) / p.stage_bytes;
+    p.stages = stages > 8 ? 8 : stages;
+    const int64_t most = (int64_t)sms * per_sm;
+    p.rows_per_worker = (p.rows + most - 1) / most;
+    cudaLaunchConfig_t cfg;
+    cudaLaunchAttribute attr[2];
+    launch_config(&cfg, attr, dim3((unsigned)((p.rows + p.rows_per_worker - 1) / p.rows_per_worker)), dim3((unsigned)threads),
+                  (size_t)(kq::kNormFwdHead + params() + p.stages * p.stage_bytes), 1, st);
+    return launch(cfg, kq::norm_residual_forward_rows<S, Y, VPT, POST>, p);
+}
+
 template <typename S, typename Y>
-kq_status_t launch_norm_forward(const kq::NormForward& p, cudaStream_t st) {
+kq_status_t launch_norm_forward(kq::NormForward& p, cudaStream_t st) {
+    const int sms = sm_count(), groups = p.d / 8;
+    if (sms <= 0) return KQ_ERR_CUDA;
+    // Many rows of more than 1024 channels: persistent CTAs.  Few rows: a CTA each, which has the shorter way (one token: 3.5 us).
+    // Two stages need two rows in 225 KB.
+    if (p.vec && p.d > 1024 && p.rows >= 4 * (int64_t)sms && 2 * p.d * (int)(sizeof(S) + (p.y ? sizeof(Y) : 0)) <= kSmemPerCta - kq::kNormFwdHead) {
+        const bool post = p.y && p.post != KQ_NORM_NONE;
+        if (groups <= 1024) {
+            const int threads = (groups + 31) / 32 * 32;
+            return post ? launch_norm_rows<S, Y, 1, true>(p, threads, sms, st) : launch_norm_rows<S, Y, 1, false>(p, threads, sms, st);
+        }
+        const int threads = ((groups + 1) / 2 + 31) / 32 * 32;
+        return post ? launch_norm_rows<S, Y, 2, true>(p, threads, sms, st) : launch_norm_rows<S, Y, 2, false>(p, threads, sms, st);
+    }
     const NormShape s = forward_shape(p.d);
     cudaLaunchConfig_t cfg;
     cudaLaunchAttribute attr[2];
@@ -259,8 +306,6 @@ struct NormWorkers {
     int64_t workers, rows_per_worker, batches;
     int cluster, smem;          // CTAs of a worker and dynamic shared memory (staged kernel)
 };
-constexpr int kSmemPerSm = 228 * 1024, kSmemPerCta = 227 * 1024;
-
 NormWorkers norm_workers(const kq_norm_args_t& a, int sms, kq::NormBackward* p) {
     NormWorkers w = {};
     w.shape = backward_shape(a.d, &w.cluster);

@@ -115,6 +115,34 @@ def test_batches_and_vector_types(vec, d):
         _check(n, ref_n, tol_n)
 
 
+@pytest.mark.parametrize("d", [1032, 2240, 4096, 4104, 5600, 12288, 16384])
+@pytest.mark.parametrize("norm,post", [("rms", "none"), ("layer", "rms"), ("rms", "layer"), ("layer", "none"), ("none", "rms")])
+def test_many_rows(d, norm, post):
+    """Enough rows for persistent CTAs: several rows each, odd counts, batches that end inside a CTA's rows."""
+    for (stream, branch), rows, batches, per in zip(TYPES, (1001, 701, 997, 650, 600), (1, 7, 997, 2, 3), (None, 101, 1, 333, 250)):
+        x, y, s = _case(rows, d, stream, branch, d + rows, batches, norm=norm, post=post)
+        h, n = kb.kroquant_norm_residual(x, y, rows_per_batch=per, **s)
+        ref_h, tol_h, ref_n, tol_n = _forward(x, y, s, per or rows)
+        _check(h, ref_h, tol_h)
+        if n is not None:
+            _check(n, ref_n, tol_n)
+    assert kb.kroquant_last_device_error() == 0
+
+
+def test_many_rows_in_place_without_branch_and_vectors():
+    x, y, s = _case(900, 2240, torch.bfloat16, torch.bfloat16, 3, post="rms")
+    ref = _forward(x, y, s, 900)
+    h, n = kb.kroquant_norm_residual(x, y, h_out=x, n_out=y, **s)
+    assert h is x and n is y
+    _check(h, *ref[:2])
+    _check(n, *ref[2:])
+    x = _rand(_gen(4), torch.float32, 800, 2240, mean=1000.0)
+    _, n = kb.kroquant_norm_residual(x, norm="layer")
+    c = x.double() - x.double().mean(1, keepdim=True)
+    want = c / (c.square().mean(1, keepdim=True) + EPS).sqrt()
+    assert float((n.double() - want).abs().max()) <= 64 * U * 1000 * 1.1
+
+
 def test_without_branch_the_stream_is_handed_on():
     x, _, s = _case(12, 640, torch.bfloat16, torch.bfloat16, 5, gated=False)
     s["residual_scale"] = 1.0
