@@ -662,7 +662,8 @@ __device__ __noinline__ void copy_rows(uint8_t* stage, const NormBackward& p, in
     }
 }
 
-template <typename S, typename Y, bool POST>
+// VEC: every row on 16-byte boundaries (bulk copies, whole groups); else any alignment and any d.
+template <typename S, typename Y, bool POST, bool VEC>
 __global__ void __launch_bounds__(kNormThreads, 1) norm_residual_backward(const __grid_constant__ NormBackward p) {
     extern __shared__ __align__(128) uint8_t smem[];
     const uint32_t base = smem_u32(smem);
@@ -679,7 +680,7 @@ __global__ void __launch_bounds__(kNormThreads, 1) norm_residual_backward(const 
     const int stage0 = kNormHeadBytes + 4 * p.columns * (p.cache_m + p.cache_gate + p.cache_post);
     const int64_t first = worker * p.rows_per_worker;
     const int rows = (int)(first + p.rows_per_worker < p.rows ? p.rows_per_worker : p.rows - first);
-    const bool vec = p.vec != 0;
+    constexpr bool vec = VEC;
     const float inv_d = 1.0f / (float)p.d;
     const bool layer_h = p.norm == kNormLayer, layer_y = POST && p.post == kNormLayer, norm = p.norm != kNormNone;
     // What the warps of a worker exchange: in one CTA by a barrier; in a cluster every warp sends its values to all CTAs and
@@ -725,7 +726,7 @@ __global__ void __launch_bounds__(kNormThreads, 1) norm_residual_backward(const 
     };
     if (vec && t == 0)
         for (int r = 0; r < p.stages && r < rows; ++r) issue(r, r);
-    const int c = t * 8, count = owned(d, c, 1);                       // this thread's channels in the CTA's columns
+    const int c = t * 8, count = VEC ? (c < d ? 8 : 0) : owned(d, c, 1);                       // this thread's channels in the CTA's columns
     f32x2 sum[3][4];
     auto clear = [&]() {
 #pragma unroll
@@ -831,9 +832,9 @@ __global__ void __launch_bounds__(kNormThreads, 1) norm_residual_backward(const 
             if (layer_y) pivot_y = pivot_of(Elem<Y>::to_f32(reinterpret_cast<const Y*>(stage + p.off_y)[sample]));
             const f32x2 minus_h = pack2(-pivot_h, -pivot_h), minus_y = pack2(-pivot_y, -pivot_y);
             f32x2 s1 = 0ull, s2 = 0ull, g0 = 0ull, g1 = 0ull, y1 = 0ull, y2 = 0ull;
-#pragma unroll 2
+#pragma unroll 1
             for (int k = 0; k < nr; ++k) {
-                const int gi = (part * nr + k) * 32 + lane, have = owned(d, gi * 8, 1);
+                const int gi = (part * nr + k) * 32 + lane, have = VEC ? (gi * 8 < d ? 8 : 0) : owned(d, gi * 8, 1);
                 if (have == 8) {
                     if (norm) {
                         f32x2 v[4], g[4], m[4];
@@ -859,7 +860,7 @@ __global__ void __launch_bounds__(kNormThreads, 1) norm_residual_backward(const 
                             y2 = fma2(u, u, y2);
                         }
                     }
-                } else {                                             // the ragged end of a row: one thread, one by one
+                } else if (!VEC) {                                   // the ragged end of a row: one thread, one by one
 #pragma unroll 1
                     for (int i = gi * 8; i < gi * 8 + have; ++i) {
                         if (norm) {
@@ -968,7 +969,7 @@ __global__ void __launch_bounds__(kNormThreads, 1) norm_residual_backward(const 
                 } else {
                     f32x2 w[4];
                     parameters(p.cache_post, par_post, t, w);
-                    if (count < 8) {                                               // nothing beyond the row in the sums below
+                    if (!VEC && count < 8) {                                               // nothing beyond the row in the sums below
 #pragma unroll
                         for (int i = 0; i < 4; ++i) H[i] = pack2(2 * i < count ? unpack2(H[i]).x : 0.f, 2 * i + 1 < count ? unpack2(H[i]).y : 0.f);
                     }
@@ -1200,7 +1201,7 @@ __global__ void __launch_bounds__(1024, 1) norm_residual_forward_rows(const __gr
                 if (p.y) q = fmaf(gate_s, (Elem<Y>::to_f32(reinterpret_cast<const Y*>(stage[j] + p.off_y)[sample]) - mean_y[j]) * inv_y[j] * post_s, q);
                 pivot[j] = sum32(q) * 0.03125f;
             }
-            const f32x2 minus = pack2(-pivot[j], -pivot[j]), off_y = pack2(-mean_y[j], -mean_y[j]), inv_y2 = pack2(inv_y[j], inv_y[j]);
+            const f32x2 minus = pack2(-pivot[j], -pivot[j]), off_y = pack2(-mean_y[j] * inv_y[j], -mean_y[j] * inv_y[j]), inv_y2 = pack2(inv_y[j], inv_y[j]);
             f32x2 s1 = 0ull, s2 = 0ull;
 #pragma unroll
             for (int k = 0; k < VPT; ++k)
@@ -1209,13 +1210,17 @@ __global__ void __launch_bounds__(1024, 1) norm_residual_forward_rows(const __gr
                     f32x2 x[4], m[4];
                     lds8<S>(stage[j], gi, x);
 #pragma unroll
-                    for (int i = 0; i < 4; ++i) h[j][k][i] = mul2(alpha2, x[i]);
+                    for (int i = 0; i < 4; ++i) h[j][k][i] = x[i];
+                    if (p.alpha != 1.f) {
+#pragma unroll
+                        for (int i = 0; i < 4; ++i) h[j][k][i] = mul2(alpha2, x[i]);
+                    }
                     if (p.y) {
                         lds8<Y>(stage[j] + p.off_y, gi, x);
                         if (POST) {
                             entries(kCachePost, par_post, p.post_weight, 0, gi, 1.f, m);
 #pragma unroll
-                            for (int i = 0; i < 4; ++i) x[i] = mul2(mul2(add2(x[i], off_y), inv_y2), m[i]);
+                            for (int i = 0; i < 4; ++i) x[i] = mul2(fma2(x[i], inv_y2, off_y), m[i]);
                         }
                         entries(kCacheGate, par_gate, p.gate, batch, gi, 1.f, m);
 #pragma unroll
@@ -1224,8 +1229,8 @@ __global__ void __launch_bounds__(1024, 1) norm_residual_forward_rows(const __gr
                     if (p.h && j < nr) store_pairs(static_cast<S*>(p.h) + (first + r + j) * p.ld_h + gi * 8, 8, true, h[j][k]);
 #pragma unroll
                     for (int i = 0; i < 4; ++i) {
-                        const f32x2 u = add2(h[j][k][i], minus);
-                        s1 = add2(s1, u);
+                        const f32x2 u = layer_h ? add2(h[j][k][i], minus) : h[j][k][i];
+                        if (layer_h) s1 = add2(s1, u);
                         s2 = fma2(u, u, s2);
                     }
                 }

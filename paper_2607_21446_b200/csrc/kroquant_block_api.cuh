@@ -345,11 +345,11 @@ NormWorkers norm_workers(const kq_norm_args_t& a, int sms, kq::NormBackward* p) 
 }
 bool wants_vector_gradients(const kq_norm_args_t& a) { return a.dgate || a.dpost_weight || a.dweight || a.dscale || a.dshift; }
 
-template <typename S, typename Y, bool POST>
+template <typename S, typename Y, bool POST, bool VEC>
 kq_status_t launch_norm_staged(const kq::NormBackward& p, const NormWorkers& w, cudaStream_t st) {
     static DeviceOnce attr_done;
     if (attr_done.needed()) {
-        if (cudaFuncSetAttribute(kq::norm_residual_backward<S, Y, POST>, cudaFuncAttributeMaxDynamicSharedMemorySize, kSmemPerCta) != cudaSuccess) {
+        if (cudaFuncSetAttribute(kq::norm_residual_backward<S, Y, POST, VEC>, cudaFuncAttributeMaxDynamicSharedMemorySize, kSmemPerCta) != cudaSuccess) {
             (void)cudaGetLastError();
             return KQ_ERR_CUDA;
         }
@@ -358,11 +358,14 @@ kq_status_t launch_norm_staged(const kq::NormBackward& p, const NormWorkers& w, 
     cudaLaunchConfig_t cfg;
     cudaLaunchAttribute attr[2];
     launch_config(&cfg, attr, dim3((unsigned)(w.workers * w.cluster)), dim3((unsigned)w.shape.threads), (size_t)w.smem, w.cluster, st);
-    return launch(cfg, kq::norm_residual_backward<S, Y, POST>, p);
+    return launch(cfg, kq::norm_residual_backward<S, Y, POST, VEC>, p);
 }
 template <typename S, typename Y>
 kq_status_t launch_norm_backward(const kq::NormBackward& p, const NormWorkers& w, cudaStream_t st) {
-    if (w.shape.rows == 1) return p.y && p.post != KQ_NORM_NONE ? launch_norm_staged<S, Y, true>(p, w, st) : launch_norm_staged<S, Y, false>(p, w, st);
+    if (w.shape.rows == 1) {
+        if (p.y && p.post != KQ_NORM_NONE) return p.vec ? launch_norm_staged<S, Y, true, true>(p, w, st) : launch_norm_staged<S, Y, true, false>(p, w, st);
+        return p.vec ? launch_norm_staged<S, Y, false, true>(p, w, st) : launch_norm_staged<S, Y, false, false>(p, w, st);
+    }
     cudaLaunchConfig_t cfg;
     cudaLaunchAttribute attr[2];
     launch_config(&cfg, attr, dim3((unsigned)w.workers), dim3((unsigned)w.shape.threads, (unsigned)w.shape.rows), (size_t)w.smem, 1, st);
