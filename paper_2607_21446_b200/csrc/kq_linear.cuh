@@ -113,18 +113,6 @@ __device__ __forceinline__ void store_typed(void* p, int type, int64_t at, float
     else static_cast<__nv_bfloat16*>(p)[at] = __float2bfloat16_rn(v);
 }
 
-// One output element from its accumulator(s): feature n, weight row r (the gate row; its value row is r + 32).
-template <bool GLU>
-__device__ __forceinline__ float linear_element(const LinearEpilogue& p, int expert, int row, int n, int r, float acc, float acc_u,
-                                                float bias, float bias_u) {
-    float v[1] = {acc + bias};
-    act_apply<1>(p.act, v);
-    if (GLU) v[0] *= acc_u + bias_u;
-    if (p.gate.ptr) v[0] *= vec_entry(p.gate, row / p.rows_per_gate, n, 1.f);
-    if (p.row_scale) v[0] *= __ldg(p.row_scale + row);
-    return v[0];
-}
-
 // Arrival on another CTA's barrier that hands over tensor memory only.  Its release has CTA scope: at cluster scope it would
 // wait for the global stores of the item before, 2 to 3 us behind the operand loads.
 __device__ __forceinline__ void mbar_arrive_remote(uint32_t cluster_addr) {
@@ -673,28 +661,34 @@ linear_mxfp4_pair(const __grid_constant__ CUtensorMap tmap_a, const __grid_const
 // D[128 weight rows][TB rows of A]: the weight is the M operand, so its tiles are read once, by as many CTAs as there are
 // tiles (times the K split), and a few rows of A cost a narrow instruction instead of a mostly empty one.  TB = 32, 64
 // (all of A in one tile of that many rows) or 128.  Stages of 256 K-elements: 16 KB of weight codes, 1 KB of their scales,
-// TB x 128 bytes of A, 1 KB of A's scales.  Cluster of `splits` CTAs: CTA r takes the K-stages [r, r + 1) * k_blocks /
-// splits of one item; partial accumulators meet in shared memory and every CTA adds its share of the elements in rank
-// order (the same bits every time).  With splits > 1 a cluster has exactly one item, so the partials use the pipeline's
-// memory after its last read; with one CTA per item the kernel is persistent and they have their own.
+// TB x 128 bytes of A (of a tile of 128 only the boxes of 32 rows that the group touches), 1 KB of A's scales.  Bound by
+// reading the weights: what counts is the bytes in flight, so nearly all shared memory is stages and the epilogue turns 32
+// rows of A at a time through 16 KB.
+// Cluster of `splits` CTAs: CTA r takes the K-stages [r, r + 1) * k_blocks / splits of one item; partial accumulators meet in
+// shared memory and every CTA adds its share of the elements in rank order (the same bits every time).  With splits > 1 a
+// cluster has exactly one item, so the partials use the pipeline's memory after its last read; with one CTA per item the
+// kernel is persistent.
+constexpr int kNarrowThreads = 352;                                      // producer, MMA issuer, 8 epilogue warps, scale copies
 template <int TB>
 struct NarrowSmem {
-    static constexpr int kStages = TB == 32 ? 8 : (TB == 64 ? 6 : 4);
+    static constexpr int kStages = TB == 32 ? 9 : (TB == 64 ? 7 : 6);
     static constexpr int kWBytes = 128 * 128;
     static constexpr int kABytes = TB * 128;
     static constexpr int kSfwOff = kWBytes + kABytes;
     static constexpr int kSfaOff = kSfwOff + 1024;
-    static constexpr int kLoadBytes = kSfaOff + 1024;
-    static constexpr int kStageBytes = (kLoadBytes + 1023) / 1024 * 1024;
-    static constexpr int kAccOff = kStages * kStageBytes;                 // [TB][128] float
-    static constexpr int kBarOff = kAccOff + TB * 512;
-    static constexpr int kNumBars = 2 * kStages + 4;                      // full, empty, tfull[2], tempty[2]
+    static constexpr int kStageBytes = kSfaOff + 1024;
+    static constexpr int kAccOff = kStages * kStageBytes;                 // [32][128] float
+    static constexpr int kScalesOff = kAccOff + 32 * 512;                 // [128] float: row scales of the tile
+    static constexpr int kBarOff = kScalesOff + 512;
+    static constexpr int kNumBars = 3 * kStages + 4;                      // full, empty, sfready, tfull[2], tempty[2]
     static constexpr int kSlotOff = kBarOff + 8 * kNumBars;
     static constexpr int kAbortOff = kSlotOff + 4;
     static constexpr int kEpiFailOff = kAbortOff + 4;
     static constexpr int kCumOff = kEpiFailOff + 4;
     static constexpr int kDynBytes = kCumOff + 4 * (kMaxExperts + 1) + 1024;
     static constexpr int kSfCol0 = 256;                                   // two accumulators of up to 128 columns in front
+    static_assert(kStageBytes % 1024 == 0 && TB * 512 <= kStages * kStageBytes && kDynBytes <= 227 * 1024, "shared memory");
+    static_assert(kSfCol0 + 16 * kStages <= 512, "tensor memory");
 };
 
 __device__ __forceinline__ void tma_load_3d(uint32_t dst, const CUtensorMap* tmap, int x, int y, int z, uint32_t bar) {
@@ -704,7 +698,7 @@ __device__ __forceinline__ void tma_load_3d(uint32_t dst, const CUtensorMap* tma
 }
 __device__ __forceinline__ float ld_cluster_f32(uint32_t cluster_addr) {
     float v;
-    asm volatile("ld.shared::cluster.f32 %0, [%1];" : "=f"(v) : "r"(cluster_addr) : "memory");
+    asm volatile("ld.shared::cluster.f32 %0, [%1];" : "=f"(v) : "r"(cluster_addr));      // (no memory clobber: several in flight)
     return v;
 }
 // M = 128, N = TB, scales of 32-element blocks `id` and `id + 1` of the 128-element scale tile
@@ -713,13 +707,70 @@ __device__ __forceinline__ uint32_t idesc_mxf4_narrow(uint32_t sf_id) {
     return (sf_id << 4) | (1u << 7) | (1u << 10) | ((uint32_t)(TB >> 3) << 17) | (1u << 23) | ((128u >> 4) << 24) | (sf_id << 29);
 }
 
+// A thread's column of out in an item of the narrow kernel and the rows it takes: first, first + kStep, ...
+template <bool GLU>
+struct NarrowColumn {
+    static constexpr int kCols = GLU ? 64 : 128, kStep = 256 / kCols;
+    int first, r, n;                     // first row, accumulator lane (gate half), column of out
+    float bias, bias_u;
+    bool live;
+    __device__ __forceinline__ void open(const LinearProblem& p, const LinearItem& w, int thread) {
+        const int f = thread % kCols;
+        first = thread / kCols;
+        r = GLU ? f / 32 * 64 + f % 32 : f;
+        n = w.tile_n * kCols + f;
+        live = n < p.epi.N;
+        bias = live ? vec_entry(p.epi.bias, w.expert, w.tile_n * 128 + r, 0.f) : 0.f;
+        bias_u = GLU && live ? vec_entry(p.epi.bias, w.expert, w.tile_n * 128 + r + 32, 0.f) : 0.f;
+    }
+    // J rows of the column: row0, row0 + stride, ..., `count` of them; all loads go out before the first is used.  row_scale:
+    // entries of the rows in shared memory from the first on (null: read here).
+    template <int J>
+    __device__ __forceinline__ void write(const LinearEpilogue& p, int row0, int stride, int count, const float* row_scale, float (&v)[J], float (&u)[J]) const {
+        if (!live) return;
+        float res[J], scale[J], gate[J];
+#pragma unroll
+        for (int j = 0; j < J; ++j) {
+            const int row = row0 + j * stride;
+            const bool ok = j < count;
+            res[j] = p.residual && ok ? load_typed(p.residual, p.residual_type, (int64_t)row * p.ld_residual + n) : 0.f;
+            gate[j] = p.gate.ptr && ok ? vec_entry(p.gate, row / p.rows_per_gate, n, 1.f) : 1.f;
+            scale[j] = !p.row_scale || !ok ? 1.f : (row_scale ? row_scale[j * stride] : __ldg(p.row_scale + row));
+        }
+#pragma unroll
+        for (int j = 0; j < J; ++j) v[j] += bias;
+        act_apply<J>(p.act, v);
+#pragma unroll
+        for (int j = 0; j < J; ++j) {
+            if (GLU) v[j] *= u[j] + bias_u;
+            if (p.gate.ptr) v[j] *= gate[j];
+            if (p.row_scale) v[j] *= scale[j];
+            if (p.residual) v[j] = fmaf(p.residual_scale, res[j], v[j]);
+        }
+        const int64_t at = (int64_t)row0 * p.ld_out + n, step = (int64_t)stride * p.ld_out;
+        if (p.out_type == kTypeF32) {
+#pragma unroll
+            for (int j = 0; j < J; ++j)
+                if (j < count) static_cast<float*>(p.out)[at + j * step] = v[j];
+        } else if (p.out_type == kTypeF16) {
+#pragma unroll
+            for (int j = 0; j < J; ++j)
+                if (j < count) static_cast<__half*>(p.out)[at + j * step] = __float2half_rn(v[j]);
+        } else {
+#pragma unroll
+            for (int j = 0; j < J; ++j)
+                if (j < count) static_cast<__nv_bfloat16*>(p.out)[at + j * step] = __float2bfloat16_rn(v[j]);
+        }
+    }
+};
+
 template <bool GLU, int TB>
-__global__ void __launch_bounds__(kGemmThreads, 1)
+__global__ void __launch_bounds__(kNarrowThreads, 1)
 linear_mxfp4_narrow(const __grid_constant__ CUtensorMap tmap_w, const __grid_constant__ CUtensorMap tmap_a,
                     const __grid_constant__ CUtensorMap tmap_sfw, const __grid_constant__ CUtensorMap tmap_sfa,
                     const __grid_constant__ LinearProblem p, const int splits) {
     using L = NarrowSmem<TB>;
-    constexpr int NS = L::kStages;
+    constexpr int NS = L::kStages, kBox = TB == 128 ? 32 : TB;          // rows of a TMA box of A
     extern __shared__ uint8_t smem_raw[];
     const uint32_t raw = smem_u32(smem_raw);
     const uint32_t base = (raw + 1023u) & ~1023u;
@@ -727,8 +778,9 @@ linear_mxfp4_narrow(const __grid_constant__ CUtensorMap tmap_w, const __grid_con
     const uint32_t bar0 = base + L::kBarOff;
     auto bar_full = [&](int s) { return bar0 + 8u * s; };
     auto bar_empty = [&](int s) { return bar0 + 8u * (NS + s); };
-    auto bar_tfull = [&](int a) { return bar0 + 8u * (2 * NS + a); };
-    auto bar_tempty = [&](int a) { return bar0 + 8u * (2 * NS + 2 + a); };
+    auto bar_sfready = [&](int s) { return bar0 + 8u * (2 * NS + s); };
+    auto bar_tfull = [&](int a) { return bar0 + 8u * (3 * NS + a); };
+    auto bar_tempty = [&](int a) { return bar0 + 8u * (3 * NS + 2 + a); };
     volatile uint32_t* tmem_slot = reinterpret_cast<volatile uint32_t*>(base_ptr + L::kSlotOff);
     volatile int* abort_flag = reinterpret_cast<volatile int*>(base_ptr + L::kAbortOff);
     volatile int* epi_fail = reinterpret_cast<volatile int*>(base_ptr + L::kEpiFailOff);
@@ -741,7 +793,7 @@ linear_mxfp4_narrow(const __grid_constant__ CUtensorMap tmap_w, const __grid_con
     const int kb0 = (int)((int64_t)p.k_blocks * rank / splits), kb1 = (int)((int64_t)p.k_blocks * (rank + 1) / splits);
 
     if (threadIdx.x == 0) {
-        for (int s = 0; s < NS; ++s) { mbar_init(bar_full(s), 1); mbar_init(bar_empty(s), 1); }
+        for (int s = 0; s < NS; ++s) { mbar_init(bar_full(s), 1); mbar_init(bar_empty(s), 1); mbar_init(bar_sfready(s), 1); }
         for (int a = 0; a < 2; ++a) { mbar_init(bar_tfull(a), 1); mbar_init(bar_tempty(a), 8); }
         *abort_flag = 0;
         *epi_fail = 0;
@@ -777,6 +829,12 @@ linear_mxfp4_narrow(const __grid_constant__ CUtensorMap tmap_w, const __grid_con
             int it = 0;
             for (int i = 0; i < my_items && !*abort_flag; ++i) {
                 const LinearItem w = linear_item<128>(p, cum, first + i * step, 4);
+                int box0 = 0, box1 = 1;
+                if (TB == 128) {
+                    const int lo = w.lo - w.tile_m * 128, hi = w.hi - w.tile_m * 128;
+                    box0 = lo > 0 ? lo / kBox : 0;
+                    box1 = hi < 128 ? (hi + kBox - 1) / kBox : 4;
+                }
                 for (int kb = kb0; kb < kb1; ++kb, ++it) {
                     const int s = it % NS;
                     if (it >= NS && !mbar_wait(bar_empty(s), ((it / NS) - 1) & 1, abort_flag)) {
@@ -784,9 +842,10 @@ linear_mxfp4_narrow(const __grid_constant__ CUtensorMap tmap_w, const __grid_con
                         break;
                     }
                     const uint32_t dst = base + s * L::kStageBytes;
-                    mbar_expect_tx(bar_full(s), L::kLoadBytes);
+                    mbar_expect_tx(bar_full(s), (uint32_t)(L::kWBytes + 2048 + (box1 - box0) * kBox * 128));
                     tma_load_3d(dst, &tmap_w, kb * 128, w.tile_n * 128, w.expert, bar_full(s));
-                    tma_load_2d(dst + L::kWBytes, &tmap_a, kb * 128, w.tile_m * 128, bar_full(s));
+                    for (int b = box0; b < box1; ++b)
+                        tma_load_2d(dst + L::kWBytes + b * kBox * 128, &tmap_a, kb * 128, w.tile_m * 128 + b * kBox, bar_full(s));
                     tma_load_3d(dst + L::kSfwOff, &tmap_sfw, 0, 2 * kb, w.expert * p.sf_row_tiles + w.tile_n, bar_full(s));
                     tma_load_3d(dst + L::kSfaOff, &tmap_sfa, 0, 2 * kb, w.tile_m, bar_full(s));
                     issued = it + 1;
@@ -794,12 +853,10 @@ linear_mxfp4_narrow(const __grid_constant__ CUtensorMap tmap_w, const __grid_con
             }
         }
     } else if (warp == 1) {
-        // ---------------- scale copies and MMA ----------------
+        // ---------------- MMA issuer ----------------
         if (lane == 0) {
             const uint64_t w_desc0 = smem_desc_sw128(base);
             const uint64_t a_desc0 = smem_desc_sw128(base + L::kWBytes);
-            const uint64_t sfw_desc0 = smem_desc_sf(base + L::kSfwOff);
-            const uint64_t sfa_desc0 = smem_desc_sf(base + L::kSfaOff);
             int it = 0;
             bool ok = true;
             for (int i = 0; ok && i < my_items; ++i) {
@@ -811,7 +868,8 @@ linear_mxfp4_narrow(const __grid_constant__ CUtensorMap tmap_w, const __grid_con
                 tc_fence_after();
                 for (int kb = kb0; kb < kb1; ++kb, ++it) {
                     const int s = it % NS;
-                    if (!mbar_wait(bar_full(s), (it / NS) & 1, abort_flag)) {
+                    // sfready[s]: the stage's codes have landed and its scales are in TMEM
+                    if (!mbar_wait(bar_sfready(s), (it / NS) & 1, abort_flag)) {
                         if (!*abort_flag) { atomicExch(&g_kq_device_error, KQ_DEV_TIMEOUT_GEMM_MMA); *abort_flag = 1; }
                         ok = false;
                         break;
@@ -820,11 +878,6 @@ linear_mxfp4_narrow(const __grid_constant__ CUtensorMap tmap_w, const __grid_con
                     const uint64_t off = (uint64_t)((s * L::kStageBytes) >> 4);
                     const uint32_t t_sfw = tmem_base + (uint32_t)(L::kSfCol0 + 16 * s);
                     const uint32_t t_sfa = t_sfw + 8;
-#pragma unroll
-                    for (int y = 0; y < 2; ++y) {
-                        tc_cp_sf(t_sfw + 4 * y, sfw_desc0 + off + (uint64_t)((512 * y) >> 4));
-                        tc_cp_sf(t_sfa + 4 * y, sfa_desc0 + off + (uint64_t)((512 * y) >> 4));
-                    }
 #pragma unroll
                     for (int k = 0; k < 4; ++k)
                         tc_mma_mxf4(tmem_base + (uint32_t)(acc * 128), w_desc0 + off + (uint64_t)(2 * k), a_desc0 + off + (uint64_t)(2 * k),
@@ -835,15 +888,44 @@ linear_mxfp4_narrow(const __grid_constant__ CUtensorMap tmap_w, const __grid_con
                 if (ok) tc_commit(bar_tfull(acc));
             }
         }
+    } else if (warp == 10) {
+        // ---------------- scale tiles: shared memory -> TMEM (from a thread of their own they overlap the products) ----------------
+        if (lane == 0) {
+            const uint64_t sfw_desc0 = smem_desc_sf(base + L::kSfwOff);
+            const uint64_t sfa_desc0 = smem_desc_sf(base + L::kSfaOff);
+            const int total = my_items * (kb1 - kb0);
+            for (int it = 0; it < total; ++it) {
+                const int s = it % NS;
+                if (!mbar_wait(bar_full(s), (it / NS) & 1, abort_flag)) {
+                    if (!*abort_flag) { atomicExch(&g_kq_device_error, KQ_DEV_TIMEOUT_GEMM_MMA); *abort_flag = 1; }
+                    break;
+                }
+                tc_fence_after();
+                const uint64_t off = (uint64_t)((s * L::kStageBytes) >> 4);
+                const uint32_t t_sfw = tmem_base + (uint32_t)(L::kSfCol0 + 16 * s);
+#pragma unroll
+                for (int y = 0; y < 2; ++y) {
+                    tc_cp_sf(t_sfw + 4 * y, sfw_desc0 + off + (uint64_t)((512 * y) >> 4));
+                    tc_cp_sf(t_sfw + 8 + 4 * y, sfa_desc0 + off + (uint64_t)((512 * y) >> 4));
+                }
+                tc_commit(bar_sfready(s));
+            }
+        }
     } else {
         // ---------------- epilogue: warps 2..9 ----------------
         const int quarter = warp & 3;
         const int chalf = (warp - 2) >> 2;
         float* part = reinterpret_cast<float*>(base_ptr + (splits > 1 ? 0 : L::kAccOff));
+        float* scales = reinterpret_cast<float*>(base_ptr + L::kScalesOff);
         pdl_wait_prior_grid();
         for (int i = 0; i < my_items; ++i) {
             const LinearItem w = linear_item<128>(p, cum, first + i * step, 4);
             const int acc = i & 1;
+            // loads wait behind the operand stages in flight (2 us): the row scales come while the item is multiplied
+            if (p.epi.row_scale && threadIdx.x < 64 + 128) {
+                const int row = w.tile_m * 128 + (int)threadIdx.x - 64;
+                scales[threadIdx.x - 64] = row < p.M ? __ldg(p.epi.row_scale + row) : 0.f;
+            }
             // A wait that gives up must not keep this warp from the barriers below: the decision to stop is taken by all
             // epilogue warps together, from a word that is only written before the first of them.
             const bool ok = mbar_wait(bar_tfull(acc), (i >> 1) & 1, abort_flag);
@@ -854,35 +936,44 @@ linear_mxfp4_narrow(const __grid_constant__ CUtensorMap tmap_w, const __grid_con
             tc_fence_after();
             const int c0 = w.lo > w.tile_m * 128 ? w.lo - w.tile_m * 128 : 0;                // columns = rows of A in the group
             const int c1 = w.hi < w.tile_m * 128 + 128 ? w.hi - w.tile_m * 128 : 128;
-            for (int c = (c0 / 8 + chalf) * 8; ok && c < c1; c += 16) {
-                uint32_t r[8];
-                tc_ld_32x8_nowait(tmem_base + ((uint32_t)(quarter * 32) << 16) + (uint32_t)(acc * 128 + c), r);
-                tc_wait_ld();
+            NarrowColumn<GLU> col;
+            if (splits == 1) col.open(p, w, (int)threadIdx.x - 64);                          // (its loads overlap the accumulator's)
+            bool stop = false;
+            for (int base_c = c0 & ~31; base_c < c1 && !stop; base_c += 32) {
+                if (ok && base_c + 16 * chalf < c1) {
+                    uint32_t r[16];
+                    tc_ld_32x16_nowait(tmem_base + ((uint32_t)(quarter * 32) << 16) + (uint32_t)(acc * 128 + base_c + 16 * chalf), r);
+                    tc_wait_ld();
 #pragma unroll
-                for (int q = 0; q < 8; ++q) asm volatile("" : "+r"(r[q]));
+                    for (int q = 0; q < 16; ++q) asm volatile("" : "+r"(r[q]));
+                    float* at = part + ((splits > 1 ? base_c : 0) + 16 * chalf) * 128 + quarter * 32 + lane;
 #pragma unroll
-                for (int q = 0; q < 8; ++q) part[(c + q) * 128 + quarter * 32 + lane] = __uint_as_float(r[q]);
-            }
-            tc_fence_before();
-            __syncwarp();
-            if (lane == 0) mbar_arrive(bar_tempty(acc));
-            if (splits > 1) break;                                                           // the rest follows the cluster barrier
-            named_barrier_sync(1, 256);
-            if (*epi_fail) break;
-            constexpr int kCols = GLU ? 64 : 128;
-            for (int x = (int)threadIdx.x - 64; x < (c1 - c0) * kCols; x += 256) {
-                const int c = c0 + x / kCols, f = x % kCols;
-                const int r = GLU ? f / 32 * 64 + f % 32 : f;
-                const int n = GLU ? w.tile_n * 64 + f : w.tile_n * 128 + f, wrow = w.tile_n * 128 + r, row = w.tile_m * 128 + c;
-                if (n < p.epi.N) {
-                    float v = linear_element<GLU>(p.epi, w.expert, row, n, wrow, part[c * 128 + r], GLU ? part[c * 128 + r + 32] : 0.f,
-                                                  vec_entry(p.epi.bias, w.expert, wrow, 0.f), GLU ? vec_entry(p.epi.bias, w.expert, wrow + 32, 0.f) : 0.f);
-                    if (p.epi.residual)
-                        v = fmaf(p.epi.residual_scale, load_typed(p.epi.residual, p.epi.residual_type, (int64_t)row * p.epi.ld_residual + n), v);
-                    store_typed(p.epi.out, p.epi.out_type, (int64_t)row * p.epi.ld_out + n, v);
+                    for (int q = 0; q < 16; ++q) at[q * 128] = __uint_as_float(r[q]);
                 }
+                if (base_c + 32 >= c1) {
+                    tc_fence_before();
+                    __syncwarp();
+                    if (lane == 0) mbar_arrive(bar_tempty(acc));
+                }
+                if (splits > 1) continue;                                                    // the rest follows the cluster barrier
+                named_barrier_sync(1, 256);
+                stop = *epi_fail != 0;
+                const int from = c0 > base_c ? c0 : base_c, to = c1 < base_c + 32 ? c1 : base_c + 32;
+                constexpr int kStep = NarrowColumn<GLU>::kStep;
+                if (!stop)
+                    for (int c = from + col.first; c < to; c += 4 * kStep) {
+                        float v[4], u[4];
+#pragma unroll
+                        for (int j = 0; j < 4; ++j) {
+                            const float* at = part + ((c + j * kStep - base_c) & 31) * 128 + col.r;
+                            v[j] = at[0];
+                            u[j] = GLU ? at[32] : 0.f;
+                        }
+                        col.template write<4>(p.epi, w.tile_m * 128 + c, kStep, (to - c + kStep - 1) / kStep, scales + c, v, u);
+                    }
+                named_barrier_sync(1, 256);                                                  // before the next rows' partials
             }
-            named_barrier_sync(1, 256);                                                      // before the next item's partials
+            if (stop || splits > 1) break;
         }
     }
 
@@ -890,28 +981,38 @@ linear_mxfp4_narrow(const __grid_constant__ CUtensorMap tmap_w, const __grid_con
     __syncthreads();
     if (splits > 1) {
         cluster_sync_all();
-        if (my_items && warp >= 2 && !*abort_flag) {
+        if (my_items && warp >= 2 && warp < 10 && !*abort_flag) {
             const LinearItem w = linear_item<128>(p, cum, first, 4);
             const int c0 = w.lo > w.tile_m * 128 ? w.lo - w.tile_m * 128 : 0;
             const int c1 = w.hi < w.tile_m * 128 + 128 ? w.hi - w.tile_m * 128 : 128;
-            constexpr int kCols = GLU ? 64 : 128;
-            for (int x = rank * 256 + (int)threadIdx.x - 64; x < (c1 - c0) * kCols; x += 256 * splits) {
-                const int c = c0 + x / kCols, f = x % kCols;
-                const int r = GLU ? f / 32 * 64 + f % 32 : f;
-                const int n = GLU ? w.tile_n * 64 + f : w.tile_n * 128 + f, wrow = w.tile_n * 128 + r, row = w.tile_m * 128 + c;
-                if (n < p.epi.N) {
-                    float acc = 0.f, acc_u = 0.f;
-                    for (int q = 0; q < splits; ++q) {
-                        const uint32_t at = mapa_shared(base + (uint32_t)(c * 128 + r) * 4u, (uint32_t)q);
-                        acc += ld_cluster_f32(at);
-                        if (GLU) acc_u += ld_cluster_f32(at + 128u);
-                    }
-                    float v = linear_element<GLU>(p.epi, w.expert, row, n, wrow, acc, acc_u, vec_entry(p.epi.bias, w.expert, wrow, 0.f),
-                                                  GLU ? vec_entry(p.epi.bias, w.expert, wrow + 32, 0.f) : 0.f);
-                    if (p.epi.residual)
-                        v = fmaf(p.epi.residual_scale, load_typed(p.epi.residual, p.epi.residual_type, (int64_t)row * p.epi.ld_residual + n), v);
-                    store_typed(p.epi.out, p.epi.out_type, (int64_t)row * p.epi.ld_out + n, v);
+            NarrowColumn<GLU> col;
+            col.open(p, w, (int)threadIdx.x - 64);
+            // four rows and four CTAs' partials in flight; the sum goes in rank order
+            const int stride = NarrowColumn<GLU>::kStep * splits;
+            for (int c = c0 + col.first + rank * NarrowColumn<GLU>::kStep; c < c1; c += 4 * stride) {
+                float sum[4] = {0.f, 0.f, 0.f, 0.f}, sum_u[4] = {0.f, 0.f, 0.f, 0.f};
+                for (int q0 = 0; q0 < splits; q0 += 4) {
+                    float x[4][4], y[4][4];
+#pragma unroll
+                    for (int q = 0; q < 4; ++q)
+#pragma unroll
+                        for (int j = 0; j < 4; ++j) {
+                            x[q][j] = y[q][j] = 0.f;
+                            if (q0 + q < splits && c + j * stride < c1) {
+                                const uint32_t at = mapa_shared(base + (uint32_t)((c + j * stride) * 128 + col.r) * 4u, (uint32_t)(q0 + q));
+                                x[q][j] = ld_cluster_f32(at);
+                                if (GLU) y[q][j] = ld_cluster_f32(at + 128u);
+                            }
+                        }
+#pragma unroll
+                    for (int q = 0; q < 4; ++q)
+#pragma unroll
+                        for (int j = 0; j < 4; ++j) {
+                            sum[j] += x[q][j];
+                            if (GLU) sum_u[j] += y[q][j];
+                        }
                 }
+                col.template write<4>(p.epi, w.tile_m * 128 + c, stride, (c1 - c + stride - 1) / stride, nullptr, sum, sum_u);
             }
         }
     }

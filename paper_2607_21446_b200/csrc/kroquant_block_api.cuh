@@ -114,21 +114,22 @@ kq_status_t launch_narrow(LinearLaunch& l, EncodeTiledFn enc, int sms, cudaStrea
     kq::LinearProblem& p = l.p;
     CUtensorMap tw, ta, tsw, tsa;
     const int64_t a_tiles = ((int64_t)p.M + 127) / 128;
-    if (!code_map(enc, &tw, l.b_codes, l.K, p.R, l.count, 128) || !code_map(enc, &ta, l.a_codes, l.K, p.M, 0, TB) ||
+    if (!code_map(enc, &tw, l.b_codes, l.K, p.R, l.count, 128) || !code_map(enc, &ta, l.a_codes, l.K, p.M, 0, TB == 128 ? 32 : TB) ||
         !scale_map(enc, &tsw, l.b_scales, l.K, (int64_t)p.sf_row_tiles * l.count, 1) || !scale_map(enc, &tsa, l.a_scales, l.K, a_tiles, 1))
         return KQ_ERR_CUDA;
     p.tiles_m = (int)a_tiles;
     p.tiles_n = (p.R + 127) / 128;
     const int64_t live = p.experts ? (l.count < p.M ? l.count : p.M) : 1;         // experts that can have rows
     const int64_t items = (a_tiles + live - 1) * p.tiles_n;
-    // K split: as many CTAs as there are SMs, at least two stages each
+    // K split: as many CTAs as there are SMs, at least two stages each; a cluster of four or eight needs as many SMs of one GPC
+    // (16 to 20), so that fewer of them run at once than there are SMs for (18 clusters of eight: 14.4 us instead of 11)
     int splits = 1;
-    while (splits < 8 && items * splits * 2 <= sms && p.k_blocks >= 4 * splits) splits *= 2;
+    while (splits < 8 && items * splits * 2 <= (splits == 1 ? sms : sms * 7 / 8 - 16 * (splits / 4)) && p.k_blocks >= 4 * splits) splits *= 2;
     const int64_t ctas = items * splits;
     const int grid = (int)(ctas < sms ? ctas : sms);
     cudaLaunchConfig_t cfg;
     cudaLaunchAttribute attr[2];
-    launch_config(&cfg, attr, dim3((unsigned)grid), dim3(kq::kGemmThreads), L::kDynBytes, splits, st);
+    launch_config(&cfg, attr, dim3((unsigned)grid), dim3(kq::kNarrowThreads), L::kDynBytes, splits, st);
     return launch(cfg, kq::linear_mxfp4_narrow<GLU, TB>, tw, ta, tsw, tsa, p, splits);
 }
 
@@ -179,8 +180,11 @@ kq_status_t run_linear(const uint8_t* a_codes, const uint8_t* a_scales, const ui
     ep.vec = rows_aligned(out, ld_out, out_dtype, 16) && rows_aligned(e.residual, e.ld_residual, e.residual_dtype, 16);
     ep.wide = rows_aligned(out, ld_out, out_dtype, 32);
     cudaStream_t st = reinterpret_cast<cudaStream_t>(stream);
-    // few rows per weight: the weight is the wide operand and is what is read
-    const bool narrow = M <= 128 * (int64_t)count;
+    // Few rows per weight: the weight is the wide operand and is what is read.  Narrow against pair kernel, us: dense N x K = 4096 x
+    // 4096 8.3 / 11.6 (1 row), 9.0 / 11.4 (32), 11.0 / 11.7 (64), 15.5 / 12.7 (128); 12288 x 2240 7.3 / 11.9, 11.7 / 10.7 (32), 16.8 / 11.1;
+    // 8 gated experts of 4096 x 4096 29 / 44 (4 rows each), 33 / 41 (32), 40 / 46 (64), 58 / 52 (128); 32 of 1024 x 2048 16 / 22,
+    // 26 / 25 (32), 35 / 30 (64).
+    const bool narrow = M <= (experts ? 40 : 32) * (int64_t)count;
     if (!narrow) return e.glu ? launch_pair<true>(l, enc, sms, st) : launch_pair<false>(l, enc, sms, st);
     if (M <= 32) return e.glu ? launch_narrow<true, 32>(l, enc, sms, st) : launch_narrow<false, 32>(l, enc, sms, st);
     if (M <= 64) return e.glu ? launch_narrow<true, 64>(l, enc, sms, st) : launch_narrow<false, 64>(l, enc, sms, st);
