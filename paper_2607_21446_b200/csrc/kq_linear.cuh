@@ -52,17 +52,29 @@ struct LinearProblem {
 // silu and the tanh form of gelu as v / (1 + e^-z): gelu_tanh(v) = v sigmoid(2 sqrt(2/pi) (v + 0.044715 v^3)).
 // gelu with erf by Abramowitz and Stegun 7.1.26, |error of erf| <= 1.5e-7 (absolute): the result's error stays below
 // 1e-7 |v|, one 24-bit rounding.  e^x by the hardware exponential.
+// (ex2 and rcp directly, denormals as zero: the ordinary functions spend three instructions on results below 2^-126, which
+// change nothing next to the 1 of 1 + e^x.)
+__device__ __forceinline__ float ex2_approx(float x) {
+    float y;
+    asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+    return y;
+}
+__device__ __forceinline__ float rcp_approx(float x) {
+    float y;
+    asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+    return y;
+}
 template <int ACT>
 __device__ __forceinline__ float act_fn(float v) {
+    constexpr float kLog2e = 1.4426950408889634f;
     if constexpr (ACT == kActRelu) return v > 0.f ? v : 0.f;
-    if constexpr (ACT == kActSilu) return __fdividef(v, 1.f + __expf(-v));
-    if constexpr (ACT == kActGeluTanh)
-        return __fdividef(v, 1.f + __expf(-1.5957691216057308f * fmaf(0.044715f * v * v, v, v)));
+    if constexpr (ACT == kActSilu) return v * rcp_approx(1.f + ex2_approx(-kLog2e * v));
+    if constexpr (ACT == kActGeluTanh) return v * rcp_approx(1.f + ex2_approx(-kLog2e * 1.5957691216057308f * fmaf(0.044715f * v * v, v, v)));
     if constexpr (ACT == kActGelu) {
         const float x = fabsf(v) * 0.70710678118654752f;
-        const float t = __fdividef(1.f, fmaf(0.3275911f, x, 1.f));
+        const float t = rcp_approx(fmaf(0.3275911f, x, 1.f));
         const float poly = t * fmaf(t, fmaf(t, fmaf(t, fmaf(t, 1.061405429f, -1.453152027f), 1.421413741f), -0.284496736f), 0.254829592f);
-        const float q = 0.5f * poly * __expf(-x * x);               // half of erfc(|v| / sqrt 2)
+        const float q = 0.5f * poly * ex2_approx(-kLog2e * x * x);  // half of erfc(|v| / sqrt 2)
         return v * (v >= 0.f ? 1.f - q : q);
     }
     return v;
@@ -300,12 +312,19 @@ __device__ __forceinline__ void epilogue_chunk(const LinearEpilogue& p, const ui
                     v[4 * i + 2] = fmaf(p.residual_scale, t.z, v[4 * i + 2]);
                     v[4 * i + 3] = fmaf(p.residual_scale, t.w, v[4 * i + 3]);
                 }
+            } else if (p.residual_type == kTypeF16) {
+#pragma unroll
+                for (int i = 0; i < C / 8; ++i) {
+                    float t[8];
+                    widen8_f16(reinterpret_cast<const uint4*>(res)[i], t);
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) v[8 * i + e] = fmaf(p.residual_scale, t[e], v[8 * i + e]);
+                }
             } else {
 #pragma unroll
                 for (int i = 0; i < C / 8; ++i) {
                     float t[8];
-                    const uint4 q = reinterpret_cast<const uint4*>(res)[i];
-                    if (p.residual_type == kTypeF16) widen8_f16(q, t); else widen8(q, t);
+                    widen8(reinterpret_cast<const uint4*>(res)[i], t);
 #pragma unroll
                     for (int e = 0; e < 8; ++e) v[8 * i + e] = fmaf(p.residual_scale, t[e], v[8 * i + e]);
                 }
@@ -322,23 +341,27 @@ __device__ __forceinline__ void epilogue_chunk(const LinearEpilogue& p, const ui
                 for (int i = 0; i < 8; ++i) w[i] = __float_as_uint(v[8 * q + i]);
                 store_words<8>(o + 8 * q, w, p.wide);
             }
-        } else {
-            uint16_t* o = static_cast<uint16_t*>(p.out) + at;
+        } else if (p.out_type == kTypeF16) {
 #pragma unroll
             for (int q = 0; q < C / 16; ++q) {
                 uint32_t w[8];
 #pragma unroll
                 for (int i = 0; i < 8; ++i) {
-                    const float lo = v[16 * q + 2 * i], hi = v[16 * q + 2 * i + 1];
-                    if (p.out_type == kTypeF16) {
-                        const __half2 h = __floats2half2_rn(lo, hi);
-                        w[i] = *reinterpret_cast<const uint32_t*>(&h);
-                    } else {
-                        const __nv_bfloat162 h = __floats2bfloat162_rn(lo, hi);
-                        w[i] = *reinterpret_cast<const uint32_t*>(&h);
-                    }
+                    const __half2 h = __floats2half2_rn(v[16 * q + 2 * i], v[16 * q + 2 * i + 1]);
+                    w[i] = *reinterpret_cast<const uint32_t*>(&h);
                 }
-                store_words<8>(o + 16 * q, w, p.wide);
+                store_words<8>(static_cast<uint16_t*>(p.out) + at + 16 * q, w, p.wide);
+            }
+        } else {
+#pragma unroll
+            for (int q = 0; q < C / 16; ++q) {
+                uint32_t w[8];
+#pragma unroll
+                for (int i = 0; i < 8; ++i) {
+                    const __nv_bfloat162 h = __floats2bfloat162_rn(v[16 * q + 2 * i], v[16 * q + 2 * i + 1]);
+                    w[i] = *reinterpret_cast<const uint32_t*>(&h);
+                }
+                store_words<8>(static_cast<uint16_t*>(p.out) + at + 16 * q, w, p.wide);
             }
         }
         return;
@@ -393,14 +416,22 @@ __device__ __forceinline__ void epilogue_chunk(const LinearEpilogue& p, const ui
 }
 
 // Before the accumulator is there: the warp's bias (64 accumulator columns from weight row wrow on) and gate (columns of out
-// from col on), zero where they end, into shared memory.
+// from col on), zero where they end, into shared memory.  Floats go there by asynchronous copies, which nothing waits for here.
+__device__ __forceinline__ void fetch_entry(const NormVec& p, int64_t which, int at, bool exists, float* dst) {
+    if (p.type == kTypeF32) {
+        const float* src = static_cast<const float*>(p.ptr) + (exists ? which * p.stride + at : 0);
+        asm volatile("cp.async.ca.shared.global [%0], [%1], 4, %2;" ::"r"(smem_u32(dst)), "l"(src), "r"(exists ? 4 : 0) : "memory");
+    } else {
+        *dst = exists ? vec_entry(p, which, at, 0.f) : 0.f;
+    }
+}
 template <bool GLU>
 __device__ __forceinline__ void fetch_vectors(const LinearEpilogue& p, float* vec, int expert, int wrow, int rows, int col, int which, bool gate, int lane) {
 #pragma unroll
     for (int i = 0; i < 2; ++i) {
         const int x = lane + 32 * i;
-        if (p.bias.ptr) vec[x] = wrow + x < rows ? vec_entry(p.bias, expert, wrow + x, 0.f) : 0.f;
-        if (gate && (!GLU || i == 0)) vec[kLinCols + x] = col + x < p.N ? vec_entry(p.gate, which, col + x, 0.f) : 0.f;
+        if (p.bias.ptr) fetch_entry(p.bias, expert, wrow + x, wrow + x < rows, vec + x);
+        if (gate && (!GLU || i == 0)) fetch_entry(p.gate, which, col + x, col + x < p.N, vec + kLinCols + x);
     }
 }
 // This lane's row of the residual from column `col` on, up to kLinRowBytes of it, and the warp's barrier armed with all of them.
@@ -586,7 +617,6 @@ linear_mxfp4_pair(const __grid_constant__ CUtensorMap tmap_a, const __grid_const
                 __syncwarp();                                                       // the vectors of the item before have been read
                 if (copied) fetch_residual(p.epi, mem, bar_res, c.row0 + lane, c.lo, c.hi, col, lane);
                 fetch_vectors<GLU>(p.epi, reinterpret_cast<float*>(mem + kLinVecOff), w.expert, wrow, p.R, col, c.which, p.epi.gate.ptr && c.uniform, lane);
-                __syncwarp();
             }
             const int acc = i & 1;
             const bool ok = mbar_wait(bar_tfull(acc), (i >> 1) & 1, abort_flag);
@@ -619,6 +649,8 @@ linear_mxfp4_pair(const __grid_constant__ CUtensorMap tmap_a, const __grid_const
             __syncwarp();
             if (lane == 0) mbar_arrive_remote(mapa_shared(bar_tempty(acc), 0));
             if (!live) continue;
+            asm volatile("cp.async.wait_all;" ::: "memory");
+            __syncwarp();                                                           // every lane's entries are there
             // one copy of the epilogue's code for both chunks (a gigantic one does not fit the instruction cache): the registers of
             // the next chunk move up
 #pragma unroll 1
