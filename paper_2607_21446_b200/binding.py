@@ -140,12 +140,13 @@ def _check(status: int, where: str) -> None:
 
 
 # the handle itself where torch offers it: building a Stream object around it takes 4 us of a call
-_raw_stream, _device = getattr(torch._C, "_cuda_getCurrentRawStream", None), getattr(torch._C, "_cuda_getDevice", None)
+_raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None)
+_device = getattr(torch._C, "_cuda_getDevice", torch.cuda.current_device)
 
 
 def _stream(stream) -> int:
     if stream is None:
-        if _raw_stream is not None and _device is not None:
+        if _raw_stream is not None:
             return _raw_stream(_device())
         stream = torch.cuda.current_stream()
     return int(stream.cuda_stream) if hasattr(stream, "cuda_stream") else int(stream)
@@ -525,15 +526,19 @@ class LinearW4A4:
         fw.destroy()
         return cls(Factors.create(G_act), q, s)
 
+    def _quantized(self, tokens: int, device):
+        """Work buffers for Q(X T) of this many tokens."""
+        if tokens not in self._work:
+            self._work[tokens] = (torch.empty((tokens, self.d // 2), dtype=torch.uint8, device=device),
+                                  torch.zeros(tiled_scale_bytes(tokens, self.d), dtype=torch.uint8, device=device))
+        return self._work[tokens]
+
     def __call__(self, X: torch.Tensor, add: Optional[torch.Tensor] = None, out: Optional[torch.Tensor] = None,
                  out_dtype=torch.bfloat16, stream=None) -> torch.Tensor:
         tokens, d = _x_shape(X)
         if d != self.d:
             raise ValueError("X [tokens, d] does not match the weights")
-        if tokens not in self._work:
-            self._work[tokens] = (torch.empty((tokens, d // 2), dtype=torch.uint8, device=X.device),
-                                  torch.zeros(tiled_scale_bytes(tokens, d), dtype=torch.uint8, device=X.device))
-        q, s = self._work[tokens]
+        q, s = self._quantized(tokens, X.device)
         if out is None:
             out = torch.empty((tokens, self.o), dtype=out_dtype, device=X.device)
         _check(load_library().kroquant_linear_w4a4(
@@ -541,6 +546,16 @@ class LinearW4A4:
             _ptr(q), _ptr(s), _ptr(add), _ptr(out), 1 if out.dtype == torch.bfloat16 else 0, _stream(stream)),
             "kroquant_linear_w4a4")
         return out
+
+    def fused(self, X: torch.Tensor, *, stream=None, **epilogue) -> torch.Tensor:
+        """The layer with its epilogue: quantizer, then :func:`kroquant_linear_mxfp4` with the keyword arguments given here
+        (bias, activation, glu, gate, row_scale, residual, out, ...).  Two launches."""
+        tokens, d = _x_shape(X)
+        if d != self.d:
+            raise ValueError("X [tokens, d] does not match the weights")
+        q, s = self._quantized(tokens, X.device)
+        kroquant_quantize(X, self.factors, q, s, stream=stream, scale_layout="tiled")
+        return kroquant_linear_mxfp4(q, s, self.w_codes, self.w_scales, stream=stream, **epilogue)
 
 
 # ---- the transformer block around the W4A4 product -----------------------------------------------------------------
@@ -579,21 +594,23 @@ def interleave_glu(W_gate: torch.Tensor, W_value: torch.Tensor) -> torch.Tensor:
 
 
 def _rows2d(t: torch.Tensor, shape, what: str) -> int:
-    """Pitch of a CUDA tensor of this 2-D shape with contiguous rows."""
-    if t.shape == shape and t.dtype in _DTYPES and t.is_cuda:
+    """Pitch of a tensor of this 2-D shape with contiguous rows on the current device."""
+    if t.shape == shape and t.dtype in _DTYPES and t.get_device() == _device():
         if t.is_contiguous():
             return shape[1]
         rows, cols = shape
         if (cols <= 1 or t.stride(1) == 1) and (rows <= 1 or t.stride(0) >= cols):
             return t.stride(0) if rows > 1 else cols
-    raise ValueError(f"{what} must be a CUDA float32, bfloat16 or float16 tensor {list(shape)} with contiguous rows that do not overlap")
+    raise ValueError(f"{what} must be a float32, bfloat16 or float16 tensor {list(shape)} on the current CUDA device with "
+                     "contiguous rows that do not overlap")
 
 
 def _linear(a_codes, a_scales, b_codes, b_scales, offsets, features, bias, activation, glu, gate, rows_per_gate, row_scale,
             residual, residual_scale, out, out_dtype, stream):
+    dev = _device()
     for t in (a_codes, a_scales, b_codes, b_scales):
-        if t.dtype is not torch.uint8 or not t.is_cuda or not t.is_contiguous():
-            raise ValueError("codes and scales must be contiguous CUDA uint8 tensors")
+        if t.dtype is not torch.uint8 or t.get_device() != dev or not t.is_contiguous():
+            raise ValueError("codes and scales must be contiguous uint8 tensors on the current CUDA device")
     a_shape, b_shape, grouped = a_codes.shape, b_codes.shape, offsets is not None
     if len(a_shape) != 2 or len(b_shape) != (3 if grouped else 2) or b_shape[-1] != a_shape[1]:
         raise ValueError("A is [M, K/2] codes, B [rows, K/2] ([experts, rows, K/2] in the grouped call) with the same K")
@@ -609,12 +626,12 @@ def _linear(a_codes, a_scales, b_codes, b_scales, offsets, features, bias, activ
     e = _Epilogue()
     e.activation, e.glu, e.rows_per_gate, e.residual_scale = act, 1 if glu else 0, 1, residual_scale
     if bias is not None:
-        if bias.shape != ((experts, R) if grouped else (R,)) or bias.dtype not in _DTYPES or not bias.is_cuda or not bias.is_contiguous():
+        if bias.shape != ((experts, R) if grouped else (R,)) or bias.dtype not in _DTYPES or bias.get_device() != dev or not bias.is_contiguous():
             raise ValueError("bias must be a contiguous CUDA floating tensor with one entry per row of B")
         e.bias, e.bias_dtype = bias.data_ptr(), _DTYPES[bias.dtype]
     if gate is not None:
         rows = 1 if gate.dim() == 1 else gate.shape[0]
-        if gate.dim() not in (1, 2) or gate.shape[-1] != N or gate.dtype not in _DTYPES or not gate.is_cuda or \
+        if gate.dim() not in (1, 2) or gate.shape[-1] != N or gate.dtype not in _DTYPES or gate.get_device() != dev or \
                 (N > 1 and gate.stride(-1) != 1) or (rows > 1 and gate.stride(0) < N):
             raise ValueError("gate must be a CUDA floating tensor [N] or [batches, N] with contiguous rows")
         if rows_per_gate is None:
@@ -625,7 +642,7 @@ def _linear(a_codes, a_scales, b_codes, b_scales, offsets, features, bias, activ
             raise ValueError("gate has too few rows for rows_per_gate")
         e.gate, e.gate_dtype, e.gate_stride, e.rows_per_gate = gate.data_ptr(), _DTYPES[gate.dtype], gate.stride(0) if rows > 1 else 0, rows_per_gate
     if row_scale is not None:
-        if row_scale.shape != (M,) or row_scale.dtype is not torch.float32 or not row_scale.is_cuda or not row_scale.is_contiguous():
+        if row_scale.shape != (M,) or row_scale.dtype is not torch.float32 or row_scale.get_device() != dev or not row_scale.is_contiguous():
             raise ValueError("row_scale must be a contiguous CUDA float32 tensor [M]")
         e.row_scale = row_scale.data_ptr()
     if residual is not None:
@@ -638,7 +655,7 @@ def _linear(a_codes, a_scales, b_codes, b_scales, offsets, features, bias, activ
     else:
         ld_out = _rows2d(out, (M, N), "out")
     if grouped:
-        if offsets.dtype is not torch.int32 or offsets.shape != (experts + 1,) or not offsets.is_cuda or not offsets.is_contiguous():
+        if offsets.dtype is not torch.int32 or offsets.shape != (experts + 1,) or offsets.get_device() != dev or not offsets.is_contiguous():
             raise ValueError("offsets must be a contiguous CUDA int32 tensor [experts + 1]")
         rc = load_library().kroquant_linear_mxfp4_grouped(
             a_codes.data_ptr(), a_scales.data_ptr(), b_codes.data_ptr(), b_scales.data_ptr(), offsets.data_ptr(), experts, M, N, K,
@@ -696,7 +713,7 @@ def _norm_args(rows: int, d: int, norm: str, post_norm: str, residual_scale: flo
     except KeyError:
         raise ValueError(f"norm and post_norm must be one of {sorted(NORMS)}") from None
     a.rows, a.d, a.residual_scale, a.eps = rows, d, residual_scale, eps
-    batches, dtype = 1, None
+    batches, dtype, dev = 1, None, _device()
     for name, v in (("gate", gate), ("post_weight", post_weight), ("weight", weight), ("scale", scale), ("shift", shift)):
         if v is None:
             continue
@@ -704,7 +721,7 @@ def _norm_args(rows: int, d: int, norm: str, post_norm: str, residual_scale: flo
         if dtype is None:
             dtype = v.dtype
         batched = len(shape) == 2 and name != "weight" and name != "post_weight"
-        if shape[-1:] != (d,) or (len(shape) != 1 and not batched) or v.dtype not in _DTYPES or not v.is_cuda or \
+        if shape[-1:] != (d,) or (len(shape) != 1 and not batched) or v.dtype not in _DTYPES or v.get_device() != dev or \
                 not (v.is_contiguous() or ((d <= 1 or v.stride(-1) == 1) and (not batched or shape[0] <= 1 or v.stride(0) >= d))):
             raise ValueError(f"{name} must be a CUDA floating tensor [d]" + ("" if "weight" in name else " or [batches, d] with contiguous rows"))
         if v.dtype is not dtype:
