@@ -23,12 +23,14 @@ def randn(g, *shape, gain=1.0, dtype=torch.bfloat16):
     return (gain * torch.randn(*shape, device="cuda", generator=g)).to(dtype)
 
 
-def dense_layer(W, seed):
-    """W4A4 layer with Kronecker factors on the activations and their inverse transpose on the weights."""
+def dense_layer(W):
+    """W4A4 layer with the Hadamard initialisation of the Kronecker factors (what calibration starts from) on the activations and
+    its inverse transpose on the weights."""
     import numpy as np
-    G = wl.gen_factors(seed)
-    H = np.stack([[np.linalg.inv(G[0, k].astype(np.float64)).T for k in range(5)]]).astype(np.float32)
-    return kb.LinearW4A4.from_weights(W, G, H)
+    a, b, c = (wl.hadamard_lu_params()[0, :, i].astype(np.float64) for i in range(3))
+    G = np.stack([[[[a[k], b[k]], [a[k] * c[k], b[k] * c[k] - 1 / a[k]]] for k in range(5)]])
+    H = np.stack([[np.linalg.inv(G[0, k]).T for k in range(5)]])
+    return kb.LinearW4A4.from_weights(W, G.astype(np.float32), H.astype(np.float32))
 
 
 def run(tokens=4096, width=2240, hidden=5600, experts=8, batches=2, seed=0):
@@ -41,7 +43,7 @@ def run(tokens=4096, width=2240, hidden=5600, experts=8, batches=2, seed=0):
 
     # ---- the block ----
     h, n = kb.kroquant_norm_residual(x, branch, gate=gate, scale=scale, shift=shift, norm="layer")
-    first, second = dense_layer(kb.interleave_glu(Wg, Wv), 1), dense_layer(Wo, 2)
+    first, second = dense_layer(kb.interleave_glu(Wg, Wv)), dense_layer(Wo)
     u = first.fused(n, features=hidden, activation="silu", glu=True)
     y = second.fused(u, gate=gate_out, residual=h)
 

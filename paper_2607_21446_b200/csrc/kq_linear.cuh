@@ -141,10 +141,8 @@ __device__ __forceinline__ void tc_ld_32x16_nowait(uint32_t taddr, uint32_t* r) 
 // ---- items of work --------------------------------------------------------------------------------
 struct LinearItem { int expert, tile_m, tile_n, lo, hi; };
 
-// Rows of group e, clamped so that no offsets, whatever they hold, lead outside A.
-__device__ __forceinline__ void group_rows(const LinearProblem& p, int e, int& lo, int& hi) {
-    lo = __ldg(p.offsets + e);
-    hi = __ldg(p.offsets + e + 1);
+// A group's rows, clamped so that no offsets, whatever they hold, lead outside A.
+__device__ __forceinline__ void clamp_rows(const LinearProblem& p, int& lo, int& hi) {
     lo = lo < 0 ? 0 : (lo > p.M ? p.M : lo);
     hi = hi < lo ? lo : (hi > p.M ? p.M : hi);
 }
@@ -156,8 +154,8 @@ __device__ __forceinline__ void build_item_table(const LinearProblem& p, int* cu
         const int e = e0 + lane;
         int items = 0;
         if (e < p.experts) {
-            int lo, hi;
-            group_rows(p, e, lo, hi);
+            int lo = __ldg(p.offsets + e), hi = __ldg(p.offsets + e + 1);
+            clamp_rows(p, lo, hi);
             if (hi > lo) items = ((hi - 1) / ROWS - lo / ROWS + 1) * p.tiles_n;
         }
         int scan = items;
@@ -179,25 +177,36 @@ __device__ __forceinline__ void raster(int t, int rows, int cols, int group, int
     r = first + in % count;
     c = in / count;
 }
+// Item t in two steps: its expert (shared memory) and the loads of the group's bounds, then the rest.  A load waits some 2 us
+// behind the operand stages in flight, so a role takes the first step for its next item when it begins one.
+struct ItemAhead { int t, expert, lo, hi; };
+__device__ __forceinline__ ItemAhead item_ahead(const LinearProblem& p, const int* cum, int t, int n_items) {
+    ItemAhead a = {t, 0, 0, p.M};
+    if (p.experts && t < n_items) {
+        int lo = 0, hi = p.experts;               // cum[lo] <= t < cum[hi]
+        while (hi - lo > 1) {
+            const int mid = (lo + hi) >> 1;
+            if (cum[mid] <= t) lo = mid; else hi = mid;
+        }
+        a.expert = lo;
+        a.lo = __ldg(p.offsets + lo);
+        a.hi = __ldg(p.offsets + lo + 1);
+    }
+    return a;
+}
 template <int ROWS>
-__device__ __forceinline__ LinearItem linear_item(const LinearProblem& p, const int* cum, int t, int group) {
+__device__ __forceinline__ LinearItem linear_item(const LinearProblem& p, const int* cum, const ItemAhead& a, int group) {
     LinearItem it;
+    it.expert = a.expert;
+    it.lo = a.lo;
+    it.hi = a.hi;
     if (!p.experts) {
-        it.expert = 0;
-        raster(t, p.tiles_m, p.tiles_n, group, it.tile_m, it.tile_n);
-        it.lo = 0;
-        it.hi = p.M;
+        raster(a.t, p.tiles_m, p.tiles_n, group, it.tile_m, it.tile_n);
         return it;
     }
-    int a = 0, b = p.experts;                     // cum[a] <= t < cum[b]
-    while (b - a > 1) {
-        const int mid = (a + b) >> 1;
-        if (cum[mid] <= t) a = mid; else b = mid;
-    }
-    it.expert = a;
-    group_rows(p, a, it.lo, it.hi);
+    clamp_rows(p, it.lo, it.hi);
     const int first = it.lo / ROWS, rows = (it.hi - 1) / ROWS - first + 1;
-    raster(t - cum[a], rows, p.tiles_n, group, it.tile_m, it.tile_n);
+    raster(a.t - cum[a.expert], rows, p.tiles_n, group, it.tile_m, it.tile_n);
     it.tile_m += first;
     return it;
 }
@@ -510,8 +519,10 @@ linear_mxfp4_pair(const __grid_constant__ CUtensorMap tmap_a, const __grid_const
         if (lane == 0) {
             pdl_wait_prior_grid();
             int it = 0;
+            ItemAhead ahead = item_ahead(p, cum, pair, n_items);
             for (int i = 0; i < my_items && !*abort_flag; ++i) {
-                const LinearItem w = linear_item<256>(p, cum, pair + i * n_pairs, kGemmGroupM);
+                const LinearItem w = linear_item<256>(p, cum, ahead, kGemmGroupM);
+                ahead = item_ahead(p, cum, pair + (i + 1) * n_pairs, n_items);
                 const int sf_tile = w.expert * p.sf_row_tiles + w.tile_n * kLinN / 128;
                 for (int kb = 0; kb < p.k_blocks; ++kb, ++it) {
                     const int s = it % kLinStages;
@@ -537,6 +548,7 @@ linear_mxfp4_pair(const __grid_constant__ CUtensorMap tmap_a, const __grid_const
             const uint64_t b_desc0 = smem_desc_sw128(base + kLinABytes);
             int it = 0;
             bool ok = true;
+            ItemAhead ahead = item_ahead(p, cum, pair, n_items);
             for (int i = 0; ok && i < my_items; ++i) {
                 const int acc = i & 1;
                 if (i >= 2 && !mbar_wait(bar_tempty(acc), ((i >> 1) - 1) & 1, abort_flag)) {
@@ -544,7 +556,8 @@ linear_mxfp4_pair(const __grid_constant__ CUtensorMap tmap_a, const __grid_const
                     break;
                 }
                 tc_fence_after();
-                const LinearItem w = linear_item<256>(p, cum, pair + i * n_pairs, kGemmGroupM);
+                const LinearItem w = linear_item<256>(p, cum, ahead, kGemmGroupM);
+                ahead = item_ahead(p, cum, pair + (i + 1) * n_pairs, n_items);
                 const uint32_t d_addr = tmem_base + (uint32_t)(acc * kLinN), shift = (w.tile_n & 1) ? 2u : 0u;
                 for (int kb = 0; kb < p.k_blocks; ++kb, ++it) {
                     const int s = it % kLinStages;
@@ -602,7 +615,7 @@ linear_mxfp4_pair(const __grid_constant__ CUtensorMap tmap_a, const __grid_const
         uint32_t res_parity = 0;
         pdl_wait_prior_grid();
         for (int i = 0; i < my_items; ++i) {
-            const LinearItem w = linear_item<256>(p, cum, pair + i * n_pairs, kGemmGroupM);
+            const LinearItem w = linear_item<256>(p, cum, item_ahead(p, cum, pair + i * n_pairs, n_items), kGemmGroupM);
             EpiChunk c;
             c.row0 = w.tile_m * 256 + (int)rank * 128 + quarter * 32;
             c.lo = w.lo;
@@ -859,8 +872,10 @@ linear_mxfp4_narrow(const __grid_constant__ CUtensorMap tmap_w, const __grid_con
         if (lane == 0) {
             pdl_wait_prior_grid();
             int it = 0;
+            ItemAhead ahead = item_ahead(p, cum, first, n_items);
             for (int i = 0; i < my_items && !*abort_flag; ++i) {
-                const LinearItem w = linear_item<128>(p, cum, first + i * step, 4);
+                const LinearItem w = linear_item<128>(p, cum, ahead, 4);
+                ahead = item_ahead(p, cum, first + (i + 1) * step, n_items);
                 int box0 = 0, box1 = 1;
                 if (TB == 128) {
                     const int lo = w.lo - w.tile_m * 128, hi = w.hi - w.tile_m * 128;
@@ -950,8 +965,10 @@ linear_mxfp4_narrow(const __grid_constant__ CUtensorMap tmap_w, const __grid_con
         float* part = reinterpret_cast<float*>(base_ptr + (splits > 1 ? 0 : L::kAccOff));
         float* scales = reinterpret_cast<float*>(base_ptr + L::kScalesOff);
         pdl_wait_prior_grid();
+        ItemAhead ahead = item_ahead(p, cum, first, n_items);
         for (int i = 0; i < my_items; ++i) {
-            const LinearItem w = linear_item<128>(p, cum, first + i * step, 4);
+            const LinearItem w = linear_item<128>(p, cum, ahead, 4);
+            ahead = item_ahead(p, cum, first + (i + 1) * step, n_items);
             const int acc = i & 1;
             // loads wait behind the operand stages in flight (2 us): the row scales come while the item is multiplied
             if (p.epi.row_scale && threadIdx.x < 64 + 128) {
@@ -1014,7 +1031,7 @@ linear_mxfp4_narrow(const __grid_constant__ CUtensorMap tmap_w, const __grid_con
     if (splits > 1) {
         cluster_sync_all();
         if (my_items && warp >= 2 && warp < 10 && !*abort_flag) {
-            const LinearItem w = linear_item<128>(p, cum, first, 4);
+            const LinearItem w = linear_item<128>(p, cum, item_ahead(p, cum, first, n_items), 4);
             const int c0 = w.lo > w.tile_m * 128 ? w.lo - w.tile_m * 128 : 0;
             const int c1 = w.hi < w.tile_m * 128 + 128 ? w.hi - w.tile_m * 128 : 128;
             NarrowColumn<GLU> col;

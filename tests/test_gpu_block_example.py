@@ -22,7 +22,7 @@ def test_fused_layer_equals_its_two_calls():
     g = torch.Generator(device="cuda")
     g.manual_seed(1)
     X, W, bias = randn(g, 300, 1152), randn(g, 640, 1152, gain=0.03), randn(g, 640, dtype=torch.float32)
-    layer = dense_layer(W, 3)
+    layer = dense_layer(W)
     q, s = kb.kroquant_quantize(X, layer.factors, scale_layout="tiled")
     want = kb.kroquant_linear_mxfp4(q, s, layer.w_codes, layer.w_scales, bias=bias, activation="gelu")
     assert torch.equal(layer.fused(X, bias=bias, activation="gelu"), want)
