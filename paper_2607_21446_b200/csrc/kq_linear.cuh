@@ -27,8 +27,7 @@ enum { kActNone = 0, kActRelu = 1, kActSilu = 2, kActGelu = 3, kActGeluTanh = 4 
 constexpr int kMaxExperts = 1024;
 
 struct LinearEpilogue {
-    int M, N;                            // rows of A; columns of out
-    int act;
+    int N, act;                          // columns of out
     NormVec bias;                        // [weight rows], stride: between experts
     NormVec gate;                        // [N], stride: between gate rows
     int rows_per_gate;
@@ -67,7 +66,7 @@ __device__ __forceinline__ float rcp_approx(float x) {
 template <int ACT>
 __device__ __forceinline__ float act_fn(float v) {
     constexpr float kLog2e = 1.4426950408889634f;
-    if constexpr (ACT == kActRelu) return v > 0.f ? v : 0.f;
+    if constexpr (ACT == kActRelu) return v < 0.f ? 0.f : v;         // (NaN stays)
     if constexpr (ACT == kActSilu) return v * rcp_approx(1.f + ex2_approx(-kLog2e * v));
     if constexpr (ACT == kActGeluTanh) return v * rcp_approx(1.f + ex2_approx(-kLog2e * 1.5957691216057308f * fmaf(0.044715f * v * v, v, v)));
     if constexpr (ACT == kActGelu) {
@@ -664,8 +663,8 @@ linear_mxfp4_pair(const __grid_constant__ CUtensorMap tmap_a, const __grid_const
             if (!live) continue;
             asm volatile("cp.async.wait_all;" ::: "memory");
             __syncwarp();                                                           // every lane's entries are there
-            // one copy of the epilogue's code for both chunks (a gigantic one does not fit the instruction cache): the registers of
-            // the next chunk move up
+            // one copy of the epilogue's code for both chunks (two copies of all its variants do not fit the instruction cache): the
+            // registers of the next chunk move up
 #pragma unroll 1
             for (int q = 0; q < 2; ++q) {
                 c.at = GLU ? 16 * q : 32 * q;

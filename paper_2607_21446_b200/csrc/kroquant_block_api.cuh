@@ -121,10 +121,12 @@ kq_status_t launch_narrow(LinearLaunch& l, EncodeTiledFn enc, int sms, cudaStrea
     p.tiles_n = (p.R + 127) / 128;
     const int64_t live = p.experts ? (l.count < p.M ? l.count : p.M) : 1;         // experts that can have rows
     const int64_t items = (a_tiles + live - 1) * p.tiles_n;
-    // K split: as many CTAs as there are SMs, at least two stages each; a cluster of four or eight needs as many SMs of one GPC
-    // (16 to 20), so that fewer of them run at once than there are SMs for (18 clusters of eight: 14.4 us instead of 11)
+    // K split: doubled while the CTAs fit the SMs and keep two stages each.  A cluster of four or eight needs as many free SMs of one
+    // GPC (16 to 20 of them), so fewer SMs can be filled with those: 7/8, and 16 less (18 clusters of eight ran in two waves: 14.4 us
+    // instead of the 11 of 18 clusters of four).
+    const int room[3] = {sms, sms * 7 / 8, sms * 7 / 8 - 16};                     // SMs for clusters of 2, 4, 8
     int splits = 1;
-    while (splits < 8 && items * splits * 2 <= (splits == 1 ? sms : sms * 7 / 8 - 16 * (splits / 4)) && p.k_blocks >= 4 * splits) splits *= 2;
+    for (int i = 0; i < 3 && items * splits * 2 <= room[i] && p.k_blocks >= 4 * splits; ++i) splits *= 2;
     const int64_t ctas = items * splits;
     const int grid = (int)(ctas < sms ? ctas : sms);
     cudaLaunchConfig_t cfg;
@@ -168,7 +170,6 @@ kq_status_t run_linear(const uint8_t* a_codes, const uint8_t* a_scales, const ui
     p.experts = experts;
     p.offsets = offsets;
     kq::LinearEpilogue& ep = p.epi;
-    ep.M = (int)M;
     ep.N = N;
     ep.act = e.activation;
     ep.bias = {e.bias, experts ? R : 0, e.bias_dtype};

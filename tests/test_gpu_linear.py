@@ -148,6 +148,25 @@ def test_activations_and_bias(M, act, glu):
     _check_device()
 
 
+@pytest.mark.parametrize("M", [2, 200])
+@pytest.mark.parametrize("act", ["none", "relu", "silu", "gelu", "gelu_tanh"])
+def test_what_is_not_finite_stays_so(M, act):
+    """NaN and infinity in a column: NaN stays NaN, +inf stays +inf, relu takes -inf to 0; other columns are untouched."""
+    N, K = 96, 128
+    qa, sa, a = _quantized(M, K, 51)
+    qw, sw, w = _quantized(N, K, 52)
+    bias = torch.zeros(N, device="cuda")
+    bias[3], bias[40], bias[70] = float("nan"), float("inf"), float("-inf")
+    out = kb.kroquant_linear_mxfp4(qa, sa, qw, sw, bias=bias, activation=act, out_dtype=torch.float32)
+    assert bool(torch.isnan(out[:, 3]).all()) and bool((out[:, 40] == float("inf")).all())
+    if act == "relu":
+        assert bool((out[:, 70] == 0).all())
+    rest = [c for c in range(N) if c not in (3, 40, 70)]
+    ref, tol = _reference(a, w, N, act)
+    _check(out[:, rest], ref[:, rest], tol[:, rest])
+    _check_device()
+
+
 @pytest.mark.parametrize("M,N", [(5, 64), (48, 320), (96, 101), (512, 512), (774, 577)])
 @pytest.mark.parametrize("dt", [torch.float32, torch.bfloat16, torch.float16])
 def test_gate_row_scale_and_residual(M, N, dt):
