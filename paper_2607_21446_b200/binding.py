@@ -7,6 +7,7 @@ non-zero status, a :class:`KroQuantError` is raised.
 """
 from __future__ import annotations
 
+import contextlib
 import ctypes as C
 import os
 from typing import Optional
@@ -150,6 +151,17 @@ def _stream(stream) -> int:
             return _raw_stream(_device())
         stream = torch.cuda.current_stream()
     return int(stream.cuda_stream) if hasattr(stream, "cuda_stream") else int(stream)
+
+
+_CURRENT = contextlib.nullcontext()
+
+
+def _allocating(stream):
+    """Context in which outputs and scratch space are allocated for a call on `stream`: that stream's, so that the memory is
+    neither still in use by another stream nor handed on before the call has run."""
+    if stream is None:
+        return _CURRENT
+    return torch.cuda.stream(stream if hasattr(stream, "cuda_stream") else torch.cuda.ExternalStream(int(stream)))
 
 
 def _ptr(t: Optional[torch.Tensor]):
@@ -553,7 +565,8 @@ class LinearW4A4:
         tokens, d = _x_shape(X)
         if d != self.d:
             raise ValueError("X [tokens, d] does not match the weights")
-        q, s = self._quantized(tokens, X.device)
+        with _allocating(stream):
+            q, s = self._quantized(tokens, X.device)
         kroquant_quantize(X, self.factors, q, s, stream=stream, scale_layout="tiled")
         return kroquant_linear_mxfp4(q, s, self.w_codes, self.w_scales, stream=stream, **epilogue)
 
@@ -651,7 +664,9 @@ def _linear(a_codes, a_scales, b_codes, b_scales, offsets, features, bias, activ
     if out is None:
         if out_dtype not in _DTYPES:
             raise ValueError("out_dtype must be float32, bfloat16 or float16")
-        out, ld_out = a_codes.new_empty((M, N), dtype=out_dtype), N
+        with _allocating(stream):
+            out = a_codes.new_empty((M, N), dtype=out_dtype)
+        ld_out = N
     else:
         ld_out = _rows2d(out, (M, N), "out")
     if grouped:
@@ -784,7 +799,8 @@ def kroquant_norm_residual(x: torch.Tensor, y: Optional[torch.Tensor] = None, *,
             raise ValueError("h_out must have x's dtype")
         a.h = h.data_ptr()
     elif y is not None or residual_scale != 1.0 or norm == "none":
-        h = x.new_empty(shape)
+        with _allocating(stream):
+            h = x.new_empty(shape)
         a.h, a.ld_h = h.data_ptr(), shape[1]
     if norm == "none":
         n = None
@@ -794,7 +810,8 @@ def kroquant_norm_residual(x: torch.Tensor, y: Optional[torch.Tensor] = None, *,
             raise ValueError("n_out must have the branch's dtype")
         a.n = n.data_ptr()
     else:
-        n = x.new_empty(shape, dtype=branch_dtype)
+        with _allocating(stream):
+            n = x.new_empty(shape, dtype=branch_dtype)
         a.n, a.ld_n = n.data_ptr(), shape[1]
     rc = load_library().kroquant_norm_residual(C.addressof(a), _stream(stream))
     if rc:
@@ -837,32 +854,33 @@ def kroquant_norm_residual_grad(dn: Optional[torch.Tensor], h: torch.Tensor, *, 
     elif gate is not None or post_weight is not None:
         raise ValueError("gate and post_weight act on the branch: y is needed")
     a.branch_dtype = _DTYPES[branch_dtype]
-    dx = h.new_empty(shape)
-    out = {"dx": dx}
-    a.dx, a.ld_dx = dx.data_ptr(), d
-    if y is not None:
-        out["dy"] = dy = h.new_empty(shape, dtype=branch_dtype)
-        a.dy, a.ld_dy = dy.data_ptr(), d
-    vectors = [(n, v.shape) for n, v in (("dgate", gate), ("dpost_weight", post_weight), ("dweight", weight), ("dscale", scale),
-                                         ("dshift", shift)) if v is not None]
-    if vectors:
-        # the gradients are one allocation; the kernel's scratch space is another, so that it is free again after the call
-        sizes = [s.numel() for _, s in vectors]
-        a.dweight = 16                                                # any pointer: whether vector gradients are wanted at all
-        nbytes = load_library().kroquant_norm_residual_grad_scratch_bytes(C.addressof(a))
-        a.dweight = None
-        store, scratch = h.new_empty(sum(sizes), dtype=torch.float32), h.new_empty(nbytes, dtype=torch.uint8)
-        covered = (rows + a.rows_per_batch - 1) // a.rows_per_batch      # batches that have rows: the kernel writes those
-        base, pos = store.data_ptr(), 0
-        for (name, s), size in zip(vectors, sizes):
-            out[name] = g = store.as_strided(s, (d, 1) if len(s) == 2 else (1,), pos)
-            setattr(a, name, base + 4 * pos)
-            if len(s) == 2 and s[0] > covered:
-                g.zero_()
-            pos += size
-        rc = load_library().kroquant_norm_residual_grad(C.addressof(a), scratch.data_ptr() if nbytes else None, nbytes, _stream(stream))
-    else:
-        rc = load_library().kroquant_norm_residual_grad(C.addressof(a), None, 0, _stream(stream))
+    with _allocating(stream):
+        dx = h.new_empty(shape)
+        out = {"dx": dx}
+        a.dx, a.ld_dx = dx.data_ptr(), d
+        if y is not None:
+            out["dy"] = dy = h.new_empty(shape, dtype=branch_dtype)
+            a.dy, a.ld_dy = dy.data_ptr(), d
+        vectors = [(n, v.shape) for n, v in (("dgate", gate), ("dpost_weight", post_weight), ("dweight", weight), ("dscale", scale),
+                                             ("dshift", shift)) if v is not None]
+        if vectors:
+            # the gradients are one allocation; the kernel's scratch space is another, so that it is free again after the call
+            sizes = [s.numel() for _, s in vectors]
+            a.dweight = 16                                                # any pointer: whether vector gradients are wanted at all
+            nbytes = load_library().kroquant_norm_residual_grad_scratch_bytes(C.addressof(a))
+            a.dweight = None
+            store, scratch = h.new_empty(sum(sizes), dtype=torch.float32), h.new_empty(nbytes, dtype=torch.uint8)
+            covered = (rows + a.rows_per_batch - 1) // a.rows_per_batch      # batches that have rows: the kernel writes those
+            base, pos = store.data_ptr(), 0
+            for (name, s), size in zip(vectors, sizes):
+                out[name] = g = store.as_strided(s, (d, 1) if len(s) == 2 else (1,), pos)
+                setattr(a, name, base + 4 * pos)
+                if len(s) == 2 and s[0] > covered:
+                    g.zero_()
+                pos += size
+            rc = load_library().kroquant_norm_residual_grad(C.addressof(a), scratch.data_ptr() if nbytes else None, nbytes, _stream(stream))
+        else:
+            rc = load_library().kroquant_norm_residual_grad(C.addressof(a), None, 0, _stream(stream))
     if rc:
         raise KroQuantError(rc, "kroquant_norm_residual_grad")
     return out

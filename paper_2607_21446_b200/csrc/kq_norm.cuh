@@ -249,6 +249,7 @@ struct NormForward {
 
 // blockDim = (threads of a row, rows of a CTA): one warp per row and several rows for narrow d, else one row per CTA.
 // Thread i owns the 8-channel groups i, i + blockDim.x, ...: VPT of them.
+// Measured: one row of 4096 3.2 us (a launch); 16384 x 256 30 to 34 us; 16384 x 2241 (no vector accesses) 129 us.
 template <typename S, typename Y, int VPT>
 __global__ void __launch_bounds__(VPT == 2 ? 1024 : 256) norm_residual_forward(const __grid_constant__ NormForward p) {
     __shared__ float red[2 * 128];
@@ -561,6 +562,8 @@ __global__ void __launch_bounds__(32 * kNormWarps) norm_residual_backward_warp(c
 // ordinarily nothing, however large the mean is.
 // With 18 warps on an SM the instructions bound the kernel next to memory, so the arithmetic is done on pairs (f32x2).
 // Parameter vectors (weight (1 + scale), gate, post_weight) are kept in shared memory as floats, refreshed at the start of a batch.
+// Measured (layer, gate and modulation, 16-bit): 16384 x 4608 210 us, 4.3 TB/s; rms around rms, 6000 x 12288 in clusters of four 519 us,
+// 1.7 TB/s (every row waits for an exchange between CTAs); 16384 x 2241 (element copies) 374 us.
 // Rows that bulk copies cannot take (16-byte alignment) are copied into the same place by the threads, element by element.
 constexpr int kNormStageMax = 6;
 constexpr int kNormThreads = 576;
@@ -1037,6 +1040,8 @@ __global__ void __launch_bounds__(kNormThreads, 1) norm_residual_backward(const 
 // rows that is what it costs (8192 x 2240, layer norm, gate and modulation: 44 us).  Here a CTA keeps its threads, its parameter
 // vectors (shared memory) and two rows at a time, which share every barrier and every sum over a warp, while the next rows
 // arrive by bulk copies.  Statistics in one pass about a sampled pivot, as in the backward kernel; h stays in registers.
+// Measured: the same 34 us (4.3 TB/s, bound by instruction issue: conversions and pairs of sums); 16385 x 5600, rms around rms with a
+// 32-bit stream, 217 to 228 us (4.8 to 5.1 TB/s, bound by memory).  Taken from four rows per SM on: below, a CTA has no next row to load.
 constexpr int kNormFwdRedOff = 128;
 constexpr int kNormFwdHead = kNormFwdRedOff + 4 * 32 * 16;            // two sets of sums for each of the two norms, used in turn
 enum { kCacheGate = 1, kCachePost = 2, kCacheMul = 4, kCacheShift = 8 };

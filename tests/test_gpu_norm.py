@@ -321,6 +321,29 @@ def test_backward_is_deterministic_and_runs_on_another_stream():
         assert all(torch.equal(first[k], r[k]) for k in first)
 
 
+@pytest.mark.parametrize("handle", [False, True])
+def test_outputs_and_scratch_of_a_call_with_a_stream_belong_to_it(handle):
+    """Memory freed on the current stream while its work is pending must not become the output or scratch of another stream's
+    call, and what that call frees must not be taken by the current stream before the call has run."""
+    rows, d = 2048, 1152
+    x, y, s = _case(rows, d, torch.bfloat16, torch.bfloat16, 12, 2, post="rms")
+    dn = _rand(_gen(7), torch.bfloat16, rows, d)
+    want_h, want_n = kb.kroquant_norm_residual(x, y, **s)
+    want = kb.kroquant_norm_residual_grad(dn, x, y=y, **s)
+    torch.cuda.synchronize()
+    side = torch.cuda.Stream()
+    stream = side.cuda_stream if handle else side
+    results = []
+    for _ in range(4):
+        results.append((kb.kroquant_norm_residual(x, y, stream=stream, **s), kb.kroquant_norm_residual_grad(dn, x, y=y, stream=stream, **s)))
+        for _ in range(8):                                   # the current stream allocates and writes at once
+            torch.full((rows, d), float("nan"), device="cuda", dtype=torch.bfloat16)
+    torch.cuda.synchronize()
+    for (h, n), g in results:
+        assert torch.equal(h, want_h) and torch.equal(n, want_n)
+        assert all(torch.equal(g[k], want[k]) for k in want)
+
+
 def test_masked_rows_and_non_finite_values_stay_in_their_rows():
     rows, d = 6, 512
     x, y, s = _case(rows, d, torch.float32, torch.float32, 11, post="rms")
