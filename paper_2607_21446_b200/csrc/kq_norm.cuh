@@ -1040,8 +1040,8 @@ __global__ void __launch_bounds__(kNormThreads, 1) norm_residual_backward(const 
 // rows that is what it costs (8192 x 2240, layer norm, gate and modulation: 44 us).  Here a CTA keeps its threads, its parameter
 // vectors (shared memory) and two rows at a time, which share every barrier and every sum over a warp, while the next rows
 // arrive by bulk copies.  Statistics in one pass about a sampled pivot, as in the backward kernel; h stays in registers.
-// Measured: the same 34 us (4.3 TB/s; 2.0 of 4 instructions per cycle with 27 warps per SM, neither memory nor issue alone); 16385 x 5600, rms around rms with a
-// 32-bit stream, 217 to 228 us (4.8 to 5.1 TB/s, bound by memory).  Taken from four rows per SM on: below, a CTA has no next row to load.
+// Measured: the same 34 us (4.3 TB/s; 2.0 of 4 instructions per cycle with 27 warps per SM, neither memory nor issue alone);
+// 16385 x 5600, rms around rms with a 32-bit stream, 217 to 228 us (4.8 to 5.1 TB/s, bound by memory).
 constexpr int kNormFwdRedOff = 128;
 constexpr int kNormFwdHead = kNormFwdRedOff + 4 * 32 * 16;            // two sets of sums for each of the two norms, used in turn
 enum { kCacheGate = 1, kCachePost = 2, kCacheMul = 4, kCacheShift = 8 };

@@ -282,9 +282,11 @@ template <typename S, typename Y>
 kq_status_t launch_norm_forward(kq::NormForward& p, cudaStream_t st) {
     const int sms = sm_count(), groups = p.d / 8;
     if (sms <= 0) return KQ_ERR_CUDA;
-    // Many rows of more than 1024 channels: persistent CTAs.  Few rows: a CTA each, which has the shorter way (one token: 3.5 us).
+    // Rows of more than 1024 channels, two or more per SM: persistent CTAs.  Few rows: a CTA each, which has the shorter way (one token:
+    // 3.2 us).  CTA per row against persistent, us, with 148, 296, 1184, 2368 rows: d = 1152 4.3 / 3.9, 4.5 / 4.2, 5.3 / 4.9, 10.3 / 7.3;
+    // 2240 4.5 / 4.2, 4.6 / 4.5, 10.7 / 8.0, 15.9 / 14.1; 5600 with a 32-bit stream and two norms 5.1 / 5.6, 7.0 / 6.2, 24.0 / 21.2, 43.1 / 36.4.
     // Two stages need two rows in 225 KB.
-    if (p.vec && p.d > 1024 && p.rows >= 4 * (int64_t)sms && 2 * p.d * (int)(sizeof(S) + (p.y ? sizeof(Y) : 0)) <= kSmemPerCta - kq::kNormFwdHead) {
+    if (p.vec && p.d > 1024 && p.rows >= 2 * (int64_t)sms && 2 * p.d * (int)(sizeof(S) + (p.y ? sizeof(Y) : 0)) <= kSmemPerCta - kq::kNormFwdHead) {
         const bool post = p.y && p.post != KQ_NORM_NONE;
         if (groups <= 1024) {
             const int threads = (groups + 31) / 32 * 32;

@@ -129,6 +129,20 @@ def test_many_rows(d, norm, post):
     assert kb.kroquant_last_device_error() == 0
 
 
+@pytest.mark.parametrize("rows", [147, 295, 296, 297, 445, 593])
+@pytest.mark.parametrize("d,norm,post", [(1032, "layer", "rms"), (2240, "rms", "none"), (5600, "rms", "rms"), (16384, "layer", "layer")])
+def test_about_as_many_rows_as_persistent_workers(rows, d, norm, post):
+    """One row per worker, some with two, the last one with fewer than the others."""
+    for stream, branch in TYPES[:2]:
+        x, y, s = _case(rows, d, stream, branch, d + rows, 3, norm=norm, post=post)
+        per = (rows + 2) // 3
+        h, n = kb.kroquant_norm_residual(x, y, rows_per_batch=per, **s)
+        ref_h, tol_h, ref_n, tol_n = _forward(x, y, s, per)
+        _check(h, ref_h, tol_h)
+        _check(n, ref_n, tol_n)
+    assert kb.kroquant_last_device_error() == 0
+
+
 def test_many_rows_in_place_without_branch_and_vectors():
     x, y, s = _case(900, 2240, torch.bfloat16, torch.bfloat16, 3, post="rms")
     ref = _forward(x, y, s, 900)
