@@ -164,6 +164,14 @@ def _allocating(stream):
     return torch.cuda.stream(stream if hasattr(stream, "cuda_stream") else torch.cuda.ExternalStream(int(stream)))
 
 
+def _empty_rows(like: torch.Tensor, dtype, stream) -> torch.Tensor:
+    """A tensor of like's shape with rows one after the other (empty_like costs 1 us of a call, new_empty with a shape 2)."""
+    if stream is None:
+        return torch.empty_like(like, dtype=dtype, memory_format=torch.contiguous_format)
+    with _allocating(stream):
+        return torch.empty_like(like, dtype=dtype, memory_format=torch.contiguous_format)
+
+
 def _ptr(t: Optional[torch.Tensor]):
     return None if t is None else C.c_void_p(t.data_ptr())
 
@@ -664,8 +672,11 @@ def _linear(a_codes, a_scales, b_codes, b_scales, offsets, features, bias, activ
     if out is None:
         if out_dtype not in _DTYPES:
             raise ValueError("out_dtype must be float32, bfloat16 or float16")
-        with _allocating(stream):
-            out = a_codes.new_empty((M, N), dtype=out_dtype)
+        if stream is None:
+            out = torch.empty_strided((M, N), (N, 1), dtype=out_dtype, device=a_codes.device)
+        else:
+            with _allocating(stream):
+                out = torch.empty_strided((M, N), (N, 1), dtype=out_dtype, device=a_codes.device)
         ld_out = N
     else:
         ld_out = _rows2d(out, (M, N), "out")
@@ -799,8 +810,7 @@ def kroquant_norm_residual(x: torch.Tensor, y: Optional[torch.Tensor] = None, *,
             raise ValueError("h_out must have x's dtype")
         a.h = h.data_ptr()
     elif y is not None or residual_scale != 1.0 or norm == "none":
-        with _allocating(stream):
-            h = x.new_empty(shape)
+        h = _empty_rows(x, x.dtype, stream)
         a.h, a.ld_h = h.data_ptr(), shape[1]
     if norm == "none":
         n = None
@@ -810,8 +820,7 @@ def kroquant_norm_residual(x: torch.Tensor, y: Optional[torch.Tensor] = None, *,
             raise ValueError("n_out must have the branch's dtype")
         a.n = n.data_ptr()
     else:
-        with _allocating(stream):
-            n = x.new_empty(shape, dtype=branch_dtype)
+        n = _empty_rows(x, branch_dtype, stream)
         a.n, a.ld_n = n.data_ptr(), shape[1]
     rc = load_library().kroquant_norm_residual(C.addressof(a), _stream(stream))
     if rc:
@@ -855,11 +864,11 @@ def kroquant_norm_residual_grad(dn: Optional[torch.Tensor], h: torch.Tensor, *, 
         raise ValueError("gate and post_weight act on the branch: y is needed")
     a.branch_dtype = _DTYPES[branch_dtype]
     with _allocating(stream):
-        dx = h.new_empty(shape)
+        dx = _empty_rows(h, h.dtype, None)
         out = {"dx": dx}
         a.dx, a.ld_dx = dx.data_ptr(), d
         if y is not None:
-            out["dy"] = dy = h.new_empty(shape, dtype=branch_dtype)
+            out["dy"] = dy = _empty_rows(h, branch_dtype, None)
             a.dy, a.ld_dy = dy.data_ptr(), d
         vectors = [(n, v.shape) for n, v in (("dgate", gate), ("dpost_weight", post_weight), ("dweight", weight), ("dscale", scale),
                                              ("dshift", shift)) if v is not None]
