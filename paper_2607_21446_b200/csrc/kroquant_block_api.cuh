@@ -238,6 +238,8 @@ kq_status_t check_norm(const kq_norm_args_t& a, bool backward) {
     }
     return KQ_OK;
 }
+// rows of a batch, never more than there are rows (the caller may say "all of them" with any large number; rows >= 1)
+int64_t batch_rows(const kq_norm_args_t& a) { return a.rows_per_batch < a.rows ? a.rows_per_batch : a.rows; }
 bool norm_vectors_vec(const kq_norm_args_t& a) {
     const int v = a.vec_dtype;
     return a.d % 8 == 0 && rows_aligned(a.gate, a.gate_stride, v, 16) && rows_aligned(a.post_weight, 0, v, 16) &&
@@ -347,7 +349,7 @@ NormWorkers norm_workers(const kq_norm_args_t& a, int sms, kq::NormBackward* p) 
     w.rows_per_worker = (a.rows + most - 1) / most;
     if (w.rows_per_worker < 1) w.rows_per_worker = 1;
     w.workers = (a.rows + w.rows_per_worker - 1) / w.rows_per_worker;
-    w.batches = (a.rows + a.rows_per_batch - 1) / a.rows_per_batch;
+    w.batches = (a.rows + batch_rows(a) - 1) / batch_rows(a);
     return w;
 }
 bool wants_vector_gradients(const kq_norm_args_t& a) { return a.dgate || a.dpost_weight || a.dweight || a.dscale || a.dshift; }
@@ -421,7 +423,7 @@ kq_status_t kroquant_norm_residual(const kq_norm_args_t* args, void* stream) {
     if (a.rows == 0) return KQ_OK;
     if (!a.x || (a.norm != KQ_NORM_NONE && !a.n) || (a.norm == KQ_NORM_NONE && !a.h)) return KQ_ERR_NULL;
     kq::NormForward p = {};
-    p.rows = a.rows; p.d = a.d; p.rows_per_batch = a.rows_per_batch;
+    p.rows = a.rows; p.d = a.d; p.rows_per_batch = batch_rows(a);
     p.x = a.x; p.ld_x = a.ld_x; p.y = a.y; p.ld_y = a.ld_y; p.h = a.h; p.ld_h = a.ld_h; p.n = a.n; p.ld_n = a.ld_n;
     p.gate = {a.gate, a.gate_stride, a.vec_dtype};
     p.post_weight = {a.post_weight, 0, a.vec_dtype};
@@ -472,7 +474,7 @@ kq_status_t kroquant_norm_residual_grad(const kq_norm_args_t* args, void* scratc
         if (!aligned16(scratch)) return KQ_ERR_ALIGN;
         if (scratch_bytes < kroquant_norm_residual_grad_scratch_bytes(args)) return KQ_ERR_SHAPE;
     }
-    p.rows = a.rows; p.d = a.d; p.rows_per_batch = a.rows_per_batch; p.rows_per_worker = w.rows_per_worker;
+    p.rows = a.rows; p.d = a.d; p.rows_per_batch = batch_rows(a); p.rows_per_worker = w.rows_per_worker;
     p.dn = a.norm == KQ_NORM_NONE ? nullptr : a.dn; p.ld_dn = a.ld_dn; p.dh = a.dh; p.ld_dh = a.ld_dh;
     p.h = a.h; p.ld_h = a.ld_h; p.y = a.y; p.ld_y = a.ld_y; p.dx = a.dx; p.ld_dx = a.ld_dx; p.dy = a.dy; p.ld_dy = a.ld_dy;
     p.gate = {a.gate, a.gate_stride, a.vec_dtype};
@@ -491,7 +493,7 @@ kq_status_t kroquant_norm_residual_grad(const kq_norm_args_t* args, void* scratc
     else rc = launch_norm_backward<float, float>(p, w, st);
     if (rc != KQ_OK || !vectors) return rc;
     kq::NormVecGrads g = {};
-    g.rows = a.rows; g.d = a.d; g.rows_per_batch = a.rows_per_batch; g.rows_per_worker = w.rows_per_worker; g.batches = w.batches;
+    g.rows = a.rows; g.d = a.d; g.rows_per_batch = p.rows_per_batch; g.rows_per_worker = w.rows_per_worker; g.batches = w.batches;
     g.partial = p.partial;
     g.gate = p.gate; g.post_weight = p.post_weight; g.weight = p.weight; g.scale = p.scale;
     g.dgate = a.dgate; g.dscale = a.dscale; g.dshift = a.dshift; g.dweight = a.dweight; g.dpost_weight = a.dpost_weight;
