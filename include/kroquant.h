@@ -402,7 +402,7 @@ typedef struct kq_norm_args {
     int norm, post_norm;                 /* kq_norm_t */
     int stream_dtype, branch_dtype, vec_dtype;   /* kq_dtype_t */
     float residual_scale, eps;
-    int64_t rows_per_batch;              /* >= 1; batches = ceil(rows / rows_per_batch) */
+    int64_t rows_per_batch;              /* >= 1; batches = ceil(rows / rows_per_batch), one where all three strides are 0 */
     const void *gate, *post_weight, *weight, *scale, *shift;     /* DEVICE [d], or rows at the strides below per batch */
     int64_t gate_stride, scale_stride, shift_stride;             /* elements between batches; 0: one vector for all */
     const void *x, *y;                   /* forward only */

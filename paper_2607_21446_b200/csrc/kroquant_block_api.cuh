@@ -238,8 +238,13 @@ kq_status_t check_norm(const kq_norm_args_t& a, bool backward) {
     }
     return KQ_OK;
 }
-// rows of a batch, never more than there are rows (the caller may say "all of them" with any large number; rows >= 1)
-int64_t batch_rows(const kq_norm_args_t& a) { return a.rows_per_batch < a.rows ? a.rows_per_batch : a.rows; }
+// Rows of a batch, never more than there are rows (the caller may say "all of them" with any large number; rows >= 1).  Vectors that
+// are all shared make one batch: the boundaries of others would only cost (a flush, a slot of the scratch space and a step of the
+// gradients' sum each).
+int64_t batch_rows(const kq_norm_args_t& a) {
+    if (!a.gate_stride && !a.scale_stride && !a.shift_stride) return a.rows;
+    return a.rows_per_batch < a.rows ? a.rows_per_batch : a.rows;
+}
 bool norm_vectors_vec(const kq_norm_args_t& a) {
     const int v = a.vec_dtype;
     return a.d % 8 == 0 && rows_aligned(a.gate, a.gate_stride, v, 16) && rows_aligned(a.post_weight, 0, v, 16) &&

@@ -28,3 +28,10 @@ def test_batches_are_counted():
     one = scratch(rows=100, rows_per_batch=100, scale_stride=640)
     for per, batches in ((99, 2), (50, 2), (33, 4), (7, 15), (1, 100)):
         assert scratch(rows=100, rows_per_batch=per, scale_stride=640) == one + (batches - 1) * 3 * 640 * 4
+
+
+@pytest.mark.parametrize("rows", [1, 100, 16384])
+def test_shared_vectors_are_one_batch_whatever_rows_per_batch_says(rows):
+    """(The default of rows_per_batch is 1.)"""
+    assert scratch(rows=rows) == scratch(rows=rows, rows_per_batch=rows)
+    assert scratch(rows=rows, rows_per_batch=7) == scratch(rows=rows, rows_per_batch=rows)

@@ -69,3 +69,20 @@ def test_one_batch_of_any_number_of_rows(rows, d, per):
     for k in want:
         assert torch.equal(got[k], want[k]), k
     assert kb.kroquant_last_device_error() == 0
+
+
+@pytest.mark.parametrize("rows,d", [(700, 640), (700, 256), (700, 2240), (37, 5600)])
+@pytest.mark.parametrize("per", [None, 3])
+def test_shared_vectors_with_any_rows_per_batch(rows, d, per):
+    """The default is 1 row per batch; without a stride the vectors are one for all rows, and so are the work and its bits."""
+    p = NormProblem(rows, d, rows + d)
+    want_h, want_n = kb.kroquant_norm_residual(p.x, p.y, norm="layer", residual_scale=0.5, **p.vectors)
+    want = kb.kroquant_norm_residual_grad(p.dn, want_h, dh=p.dh, y=p.y, norm="layer", residual_scale=0.5, **p.vectors)
+    kw = {} if per is None else {"rows_per_batch": per}
+    h, n = p.forward(**kw)
+    assert torch.equal(h, want_h) and torch.equal(n, want_n)
+    got, nbytes = p.backward(h, **kw)
+    assert nbytes == p.backward(h, rows_per_batch=rows)[1]
+    for k in want:
+        assert torch.equal(got[k], want[k]), k
+    assert kb.kroquant_last_device_error() == 0
