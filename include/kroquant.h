@@ -360,7 +360,7 @@ typedef struct kq_epilogue {
     const void *gate;          /* DEVICE, row i (N elements) at gate + i * gate_stride, of gate_dtype, or NULL */
     int gate_dtype;
     int64_t gate_stride;       /* elements; 0: one row for all */
-    int64_t rows_per_gate;     /* >= 1 (with a gate): row m uses gate row m / rows_per_gate */
+    int64_t rows_per_gate;     /* >= 1 (with a gate): row m uses gate row m / rows_per_gate (with stride 0 the one row) */
     const float *row_scale;    /* DEVICE [M], or NULL */
     const void *residual;      /* DEVICE [M] rows of ld_residual elements of residual_dtype, or NULL */
     int residual_dtype;

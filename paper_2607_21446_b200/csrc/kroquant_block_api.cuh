@@ -174,7 +174,8 @@ kq_status_t run_linear(const uint8_t* a_codes, const uint8_t* a_scales, const ui
     ep.act = e.activation;
     ep.bias = {e.bias, experts ? R : 0, e.bias_dtype};
     ep.gate = {e.gate, e.gate_stride, e.gate_dtype};
-    ep.rows_per_gate = !e.gate || e.rows_per_gate > M ? (int)M : (int)e.rows_per_gate;
+    // (one gate row for all is one gate row, whatever rows_per_gate says: a warp then reads it once instead of a lane each for its row)
+    ep.rows_per_gate = !e.gate || !e.gate_stride || e.rows_per_gate > M ? (int)M : (int)e.rows_per_gate;
     ep.row_scale = e.row_scale;
     ep.residual = e.residual; ep.residual_type = e.residual_dtype; ep.ld_residual = e.ld_residual; ep.residual_scale = e.residual_scale;
     ep.out = out; ep.out_type = out_dtype; ep.ld_out = ld_out;

@@ -86,3 +86,25 @@ def test_shared_vectors_with_any_rows_per_batch(rows, d, per):
     for k in want:
         assert torch.equal(got[k], want[k]), k
     assert kb.kroquant_last_device_error() == 0
+
+
+@pytest.mark.parametrize("M", [5, 100, 700])
+@pytest.mark.parametrize("per", [None, 1, 3, 2 ** 63 - 1])
+def test_linear_with_one_gate_row_and_any_rows_per_gate(M, per):
+    """gate_stride 0: one row for all, whatever rows_per_gate says (its default is 1)."""
+    N, K = 200, 288
+    g = _gen(M)
+    qa, sa = kb.kroquant_mxfp4_quantize(torch.randn(M, K, device="cuda", generator=g).to(torch.bfloat16), scale_layout="tiled")
+    qw, sw = kb.kroquant_mxfp4_quantize(torch.randn(N, K, device="cuda", generator=g).to(torch.bfloat16), scale_layout="tiled")
+    gate = torch.randn(N, device="cuda", generator=g)
+    want = kb.kroquant_linear_mxfp4(qa, sa, qw, sw, gate=gate)
+    e = kb._Epilogue()
+    kb.load_library().kroquant_epilogue_default(C.addressof(e))
+    e.gate, e.gate_dtype = gate.data_ptr(), 0
+    if per is not None:
+        e.rows_per_gate = per
+    out = torch.empty_like(want)
+    assert kb.load_library().kroquant_linear_mxfp4(qa.data_ptr(), sa.data_ptr(), qw.data_ptr(), sw.data_ptr(), M, N, K, C.addressof(e),
+                                                   out.data_ptr(), 1, N, torch.cuda.current_stream().cuda_stream) == 0
+    assert torch.equal(out, want)
+    assert kb.kroquant_last_device_error() == 0
