@@ -10,6 +10,7 @@ from __future__ import annotations
 import contextlib
 import ctypes as C
 import os
+import threading
 from typing import Optional
 
 import numpy as np
@@ -143,6 +144,7 @@ def _check(status: int, where: str) -> None:
 # the handle itself where torch offers it: building a Stream object around it takes 4 us of a call
 _raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None)
 _device = getattr(torch._C, "_cuda_getDevice", torch.cuda.current_device)
+_capturing = getattr(torch._C, "_cuda_isCurrentStreamCapturing", torch.cuda.is_current_stream_capturing)
 
 
 def _stream(stream) -> int:
@@ -530,7 +532,8 @@ def kroquant_gemm_bf16(A: torch.Tensor, Bm: torch.Tensor, add: Optional[torch.Te
 class LinearW4A4:
     """The quantized linear layer of Section 3.4: holds the activation factors, the offline-quantized
     weights (codes + tiled scales) and the work buffers for Q(X T); ``__call__`` runs quantizer + FP4 GEMM
-    (two launches, nothing allocated after the first call for a given number of tokens)."""
+    (two launches, nothing allocated after the first call on a stream for the largest number of tokens).  Calls
+    on different streams and from different threads have work buffers of their own."""
 
     def __init__(self, factors: "Factors", w_codes: torch.Tensor, w_scales: torch.Tensor):
         self.factors, self.w_codes, self.w_scales = factors, w_codes, w_scales
@@ -546,24 +549,35 @@ class LinearW4A4:
         fw.destroy()
         return cls(Factors.create(G_act), q, s)
 
-    def _quantized(self, tokens: int, device):
-        """Work buffers for Q(X T) of this many tokens."""
-        if tokens not in self._work:
-            self._work[tokens] = (torch.empty((tokens, self.d // 2), dtype=torch.uint8, device=device),
-                                  torch.zeros(tiled_scale_bytes(tokens, self.d), dtype=torch.uint8, device=device))
-        return self._work[tokens]
+    def _buffers(self, tokens: int, device, stream, handle: int):
+        """Work buffers for Q(X T) of this many tokens: one pair for each stream and calling thread, as large as the largest call
+        needed, since calls that may overlap must not share them.  A graph under capture gets its own, since it may run next to
+        later calls.  Scale bytes that the quantizer leaves out must not be 0xFF: kept buffers start from zeros, a graph's where
+        there are such bytes."""
+        capturing = _capturing()
+        key = (handle, threading.get_ident())
+        work = None if capturing else self._work.get(key)
+        if work is None or work[0].shape[0] < tokens:
+            with _allocating(stream):
+                make = torch.empty if capturing and tokens % 128 == 0 and self.d % 128 == 0 else torch.zeros
+                work = (torch.empty((tokens, self.d // 2), dtype=torch.uint8, device=device),
+                        make(tiled_scale_bytes(tokens, self.d), dtype=torch.uint8, device=device))
+            if not capturing:
+                self._work[key] = work
+        return work
 
     def __call__(self, X: torch.Tensor, add: Optional[torch.Tensor] = None, out: Optional[torch.Tensor] = None,
                  out_dtype=torch.bfloat16, stream=None) -> torch.Tensor:
         tokens, d = _x_shape(X)
         if d != self.d:
             raise ValueError("X [tokens, d] does not match the weights")
-        q, s = self._quantized(tokens, X.device)
+        handle = _stream(stream)
+        q, s = self._buffers(tokens, X.device, stream, handle)
         if out is None:
             out = torch.empty((tokens, self.o), dtype=out_dtype, device=X.device)
         _check(load_library().kroquant_linear_w4a4(
             _ptr(X), X_DTYPES[X.dtype], tokens, d, self.factors._h, _ptr(self.w_codes), _ptr(self.w_scales), self.o,
-            _ptr(q), _ptr(s), _ptr(add), _ptr(out), 1 if out.dtype == torch.bfloat16 else 0, _stream(stream)),
+            _ptr(q), _ptr(s), _ptr(add), _ptr(out), 1 if out.dtype == torch.bfloat16 else 0, handle),
             "kroquant_linear_w4a4")
         return out
 
@@ -573,9 +587,11 @@ class LinearW4A4:
         tokens, d = _x_shape(X)
         if d != self.d:
             raise ValueError("X [tokens, d] does not match the weights")
-        with _allocating(stream):
-            q, s = self._quantized(tokens, X.device)
-        kroquant_quantize(X, self.factors, q, s, stream=stream, scale_layout="tiled")
+        handle = _stream(stream)
+        q, s = self._buffers(tokens, X.device, stream, handle)
+        if q.shape[0] != tokens:
+            q, s = q[:tokens], s[:tiled_scale_bytes(tokens, d)]
+        kroquant_quantize(X, self.factors, q, s, stream=handle, scale_layout="tiled")
         return kroquant_linear_mxfp4(q, s, self.w_codes, self.w_scales, stream=stream, **epilogue)
 
 
