@@ -380,7 +380,7 @@ kq_status_t kroquant_linear_mxfp4(const uint8_t *a_codes, const uint8_t *a_scale
 /* The same with one weight per expert (mixture of experts): rows offsets[e] .. offsets[e+1] - 1 of A, quantized once over
  * all M rows, meet weight e.  offsets: DEVICE int32 [experts + 1], non-decreasing; groups may be empty, and rows outside
  * [offsets[0], offsets[experts]) are not written.  Offsets are read on the device (no host synchronization) and clamped to
- * [0, M], so that no value leads outside the buffers.  b_codes [experts][rows of b][K/2], b_scales [experts][tiled size];
+ * [0, M], and where they decrease a group begins no earlier than the groups before it end, so that no value leads outside the buffers.  b_codes [experts][rows of b][K/2], b_scales [experts][tiled size];
  * 1 <= experts <= 1024.  Groups need no padding and no alignment. */
 kq_status_t kroquant_linear_mxfp4_grouped(const uint8_t *a_codes, const uint8_t *a_scales, const uint8_t *b_codes,
                                           const uint8_t *b_scales, const int32_t *offsets, int experts, int64_t M, int N,

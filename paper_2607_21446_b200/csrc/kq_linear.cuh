@@ -141,22 +141,37 @@ __device__ __forceinline__ void tc_ld_32x16_nowait(uint32_t taddr, uint32_t* r) 
 struct LinearItem { int expert, tile_m, tile_n, lo, hi; };
 
 // A group's rows, clamped so that no offsets, whatever they hold, lead outside A.
-__device__ __forceinline__ void clamp_rows(const LinearProblem& p, int& lo, int& hi) {
-    lo = lo < 0 ? 0 : (lo > p.M ? p.M : lo);
-    hi = hi < lo ? lo : (hi > p.M ? p.M : hi);
+__device__ __forceinline__ void clamp_rows(int M, int& lo, int& hi) {
+    lo = lo < 0 ? 0 : (lo > M ? M : lo);
+    hi = hi < lo ? lo : (hi > M ? M : hi);
 }
-// cum[e] = items of the experts before e; one warp.  ROWS: rows of a row tile.
+// Groups of offsets that decrease somewhere could overlap and make more items than the host allows for (a K split has memory for
+// one item per cluster), so a group then begins no earlier than the groups before it end: the end of those before `expert`.
+// (Not a function of its own: around a call the loads of the next item's bounds lost their lead, 48 -> 54 us with 32 small groups.)
+__device__ __forceinline__ int rows_taken(const int32_t* offsets, int M, int expert) {
+    int end = 0;
+#pragma unroll 1
+    for (int e = 0; e < expert; ++e) {
+        int lo = __ldg(offsets + e), hi = __ldg(offsets + e + 1);
+        clamp_rows(M, lo, hi);
+        if (hi > lo && hi > end) end = hi;
+    }
+    return end;
+}
+// cum[e] = items of the experts before e, cum[experts + 1] = whether the offsets decrease somewhere; one warp.  ROWS: rows of a row tile.
 template <int ROWS>
 __device__ __forceinline__ void build_item_table(const LinearProblem& p, int* cum, int lane) {
-    int base = 0;
+    int base = 0, wild = 0;
     for (int e0 = 0; e0 < p.experts; e0 += 32) {
         const int e = e0 + lane;
-        int items = 0;
+        int items = 0, decreases = 0;
         if (e < p.experts) {
             int lo = __ldg(p.offsets + e), hi = __ldg(p.offsets + e + 1);
-            clamp_rows(p, lo, hi);
+            decreases = hi < lo;
+            clamp_rows(p.M, lo, hi);
             if (hi > lo) items = ((hi - 1) / ROWS - lo / ROWS + 1) * p.tiles_n;
         }
+        wild |= __any_sync(0xFFFFFFFFu, decreases);
         int scan = items;
 #pragma unroll
         for (int o = 1; o < 32; o <<= 1) {
@@ -166,7 +181,24 @@ __device__ __forceinline__ void build_item_table(const LinearProblem& p, int* cu
         if (e < p.experts) cum[e] = base + scan - items;
         base += __shfl_sync(0xFFFFFFFFu, scan, 31);
     }
-    if (lane == 0) cum[p.experts] = base;
+    __syncwarp();
+    if (lane == 0) {
+        if (wild) {
+            int end = 0;
+            base = 0;
+            for (int e = 0; e < p.experts; ++e) {
+                int lo = __ldg(p.offsets + e), hi = __ldg(p.offsets + e + 1);
+                clamp_rows(p.M, lo, hi);
+                cum[e] = base;
+                if (hi <= lo || hi <= end) continue;
+                if (lo < end) lo = end;
+                end = hi;
+                base += ((hi - 1) / ROWS - lo / ROWS + 1) * p.tiles_n;
+            }
+        }
+        cum[p.experts] = base;
+        cum[p.experts + 1] = wild;
+    }
 }
 // Row tiles in groups of `group` sweep all weight tiles, so that the CTAs running at one time share a few panels in L2.
 __device__ __forceinline__ void raster(int t, int rows, int cols, int group, int& r, int& c) {
@@ -203,7 +235,11 @@ __device__ __forceinline__ LinearItem linear_item(const LinearProblem& p, const 
         raster(a.t, p.tiles_m, p.tiles_n, group, it.tile_m, it.tile_n);
         return it;
     }
-    clamp_rows(p, it.lo, it.hi);
+    clamp_rows(p.M, it.lo, it.hi);
+    if (cum[p.experts + 1]) {                     // (here, where the bounds are used: in the step before it would wait for their loads)
+        const int taken = rows_taken(p.offsets, p.M, a.expert);
+        if (it.lo < taken) it.lo = taken;
+    }
     const int first = it.lo / ROWS, rows = (it.hi - 1) / ROWS - first + 1;
     raster(a.t - cum[a.expert], rows, p.tiles_n, group, it.tile_m, it.tile_n);
     it.tile_m += first;
@@ -246,7 +282,7 @@ constexpr int kLinNumBars = 3 * kLinStages + 4 + kLinEpiWarps;       // full, em
 constexpr int kLinSlotOff = kLinBarOff + 8 * kLinNumBars;
 constexpr int kLinAbortOff = kLinSlotOff + 4;
 constexpr int kLinCumOff = kLinAbortOff + 4;
-constexpr int kLinDynBytes = kLinCumOff + 4 * (kMaxExperts + 1) + 1024;
+constexpr int kLinDynBytes = kLinCumOff + 4 * (kMaxExperts + 2) + 1024;
 static_assert(kLinSfCol0 + 24 * kLinStages <= 512, "tensor memory");
 static_assert(kLinStageBytes % 1024 == 0 && kLinWarpBytes % 16 == 0 && 32 * kLinTileStride * 4 <= kLinVecOff && kLinDynBytes <= 227 * 1024, "shared memory");
 
@@ -734,7 +770,7 @@ struct NarrowSmem {
     static constexpr int kAbortOff = kSlotOff + 4;
     static constexpr int kEpiFailOff = kAbortOff + 4;
     static constexpr int kCumOff = kEpiFailOff + 4;
-    static constexpr int kDynBytes = kCumOff + 4 * (kMaxExperts + 1) + 1024;
+    static constexpr int kDynBytes = kCumOff + 4 * (kMaxExperts + 2) + 1024;
     static constexpr int kSfCol0 = 256;                                   // two accumulators of up to 128 columns in front
     static_assert(kStageBytes % 1024 == 0 && TB * 512 <= kStages * kStageBytes && kDynBytes <= 227 * 1024, "shared memory");
     static_assert(kSfCol0 + 16 * kStages <= 512, "tensor memory");
