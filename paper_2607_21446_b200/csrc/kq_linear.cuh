@@ -49,10 +49,14 @@ struct LinearProblem {
 
 // ---- activations ---------------------------------------------------------------------------------
 // silu and the tanh form of gelu as v / (1 + e^-z): gelu_tanh(v) = v sigmoid(2 sqrt(2/pi) (v + 0.044715 v^3)).
-// gelu with erf by Abramowitz and Stegun 7.1.26, |error of erf| <= 1.5e-7 (absolute): the result's error stays below
-// 1e-7 |v|, one 24-bit rounding.  e^x by the hardware exponential.
+// gelu with erf: v Phi(v), with q = Phi(-|v|) as 2^R(|v|).  R(a) = log2 Phi(-a) is smooth and runs from -1 at 0 to -50.5 at 8: a
+// polynomial of degree 12 with R(0) = -1, fitted to Phi itself with the weight that its error has in v (1 - q) and v q.  Nothing
+// cancels where q is large: the result is off by at most 1.5 * 2^-23 |v|, its own rounding and the hardware exponential's 1.2 * 2^-23 q
+// included (measured over [-8, 8]: 1.0; 0.5 v (1 + erf) in 32 bits: 0.9), and the negative tail keeps a relative accuracy, 2^-19 down
+// to -4, 2^-17 to -6, 2^-14 to -8; below that the result, above -5e-15, is taken as 0.  On pairs (f32x2): 8192 x 1152 -> 4608 takes
+// 59.6 us, element by element 76.
 // (ex2 and rcp directly, denormals as zero: the ordinary functions spend three instructions on results below 2^-126, which
-// change nothing next to the 1 of 1 + e^x.)
+// change nothing next to the 1 of 1 + e^x, and make silu below -87.3 zero instead of 1e-36.)
 __device__ __forceinline__ float ex2_approx(float x) {
     float y;
     asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
@@ -69,14 +73,28 @@ __device__ __forceinline__ float act_fn(float v) {
     if constexpr (ACT == kActRelu) return v < 0.f ? 0.f : v;         // (NaN stays)
     if constexpr (ACT == kActSilu) return v * rcp_approx(1.f + ex2_approx(-kLog2e * v));
     if constexpr (ACT == kActGeluTanh) return v * rcp_approx(1.f + ex2_approx(-kLog2e * 1.5957691216057308f * fmaf(0.044715f * v * v, v, v)));
-    if constexpr (ACT == kActGelu) {
-        const float x = fabsf(v) * 0.70710678118654752f;
-        const float t = rcp_approx(fmaf(0.3275911f, x, 1.f));
-        const float poly = t * fmaf(t, fmaf(t, fmaf(t, fmaf(t, 1.061405429f, -1.453152027f), 1.421413741f), -0.284496736f), 0.254829592f);
-        const float q = 0.5f * poly * ex2_approx(-kLog2e * x * x);  // half of erfc(|v| / sqrt 2)
-        return v * (v >= 0.f ? 1.f - q : q);
-    }
     return v;
+}
+// a pair of values at a time
+__device__ __forceinline__ void gelu2(float& v0, float& v1) {
+    const f32x2 a = pack2(fabsf(v0), fabsf(v1));
+    auto both = [](float c) { return pack2(c, c); };
+    f32x2 r = fma2(both(-1.1298189467323638e-10f), a, both(5.902352384623555e-09f));
+    r = fma2(r, a, both(-1.371750073531075e-07f));
+    r = fma2(r, a, both(1.8654657196748303e-06f));
+    r = fma2(r, a, both(-1.6329351637978107e-05f));
+    r = fma2(r, a, both(9.349935135105625e-05f));
+    r = fma2(r, a, both(-0.0003115577856078744f));
+    r = fma2(r, a, both(3.248723805882037e-05f));
+    r = fma2(r, a, both(0.0069331880658864975f));
+    r = fma2(r, a, both(-0.05244309455156326f));
+    r = fma2(r, a, both(-0.4592180848121643f));
+    r = fma2(r, a, both(-1.1511045694351196f));
+    r = fma2(r, a, both(-1.f));
+    const float2 e = unpack2(r);
+    const float q0 = fabsf(v0) < 8.f ? ex2_approx(e.x) : 0.f, q1 = fabsf(v1) < 8.f ? ex2_approx(e.y) : 0.f;
+    v0 *= v0 >= 0.f ? 1.f - q0 : q0;
+    v1 *= v1 >= 0.f ? 1.f - q1 : q1;
 }
 template <int COUNT>
 __device__ __forceinline__ void act_apply(int act, float (&v)[COUNT]) {
@@ -90,8 +108,9 @@ __device__ __forceinline__ void act_apply(int act, float (&v)[COUNT]) {
             for (int i = 0; i < COUNT; ++i) v[i] = act_fn<kActSilu>(v[i]);
             break;
         case kActGelu:
+            static_assert(COUNT % 2 == 0, "pairs");
 #pragma unroll
-            for (int i = 0; i < COUNT; ++i) v[i] = act_fn<kActGelu>(v[i]);
+            for (int i = 0; i < COUNT; i += 2) gelu2(v[i], v[i + 1]);
             break;
         case kActGeluTanh:
 #pragma unroll
