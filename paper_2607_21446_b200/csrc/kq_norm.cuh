@@ -4,9 +4,10 @@
 //     r = post(y) post_weight          post, norm in {none, rms, layer}:  v -> (v - mean) / sqrt(mean((v - mean)^2) + eps)
 //     h = alpha x + gate_b r                                              (rms: mean taken as 0)
 //     n = norm(h) weight (1 + scale_b) + shift_b
-// The row stays in registers between its one read and its one write; h enters the norm unrounded (32 bits), so n does
-// not carry the rounding of h to the stream's type.  All statistics are 32-bit sums, the variance is taken about the mean
-// (two reductions) because E[v^2] - E[v]^2 loses what a large mean leaves.
+// One read and one write of a row; h enters the norm unrounded (32 bits), so n does not carry the rounding of h to the stream's
+// type.  All statistics are 32-bit sums, and squares are taken about a mean, because E[v^2] - E[v]^2 loses what a large mean, or a few
+// large channels, leave: the small kernels take two passes over the row, the staged ones (many rows; wide rows in the backward pass)
+// let every warp take squares about the mean of its own channels and join them by Chan's update.
 //
 // Backward, with m = weight (1 + scale_b), xhat = norm(h), yhat = post(y), g = dn m:
 //     H  = dh + (g - [mean g] - xhat mean(g xhat)) / dev(h)          [..]: layer only
@@ -19,7 +20,8 @@
 // the end of a batch it writes them to slot (worker + batch), unique because both only grow along the rows, and a second
 // kernel adds the slots in a fixed order: no atomics, the same bits every time.
 //
-// All kernels are bound by memory: 2 reads and 2 writes (forward), 4 reads and 2 writes (backward) per element.
+// 2 reads and 2 writes (forward), 4 reads and 2 writes (backward) per element.  Memory bounds the wide rows with a 32-bit stream; the
+// others wait for instructions and their latency next to it (figures at the kernels).
 #pragma once
 #include "kq_common.cuh"
 #include "kq_umma.cuh"
@@ -211,6 +213,17 @@ __device__ __forceinline__ void warp_sum4(float (&v)[4], int lane) {
     k += __shfl_xor_sync(0xFFFFFFFFu, k, 1);
 #pragma unroll
     for (int i = 0; i < 4; ++i) v[i] = __shfl_sync(0xFFFFFFFFu, k, 8 * i);
+}
+
+// the same with two values: seven shuffles instead of ten
+__device__ __forceinline__ void warp_sum2(float (&v)[2], int lane) {
+    const bool b4 = lane & 16;
+    float k = b4 ? v[1] : v[0];
+    k += __shfl_xor_sync(0xFFFFFFFFu, b4 ? v[0] : v[1], 16);
+#pragma unroll
+    for (int o = 8; o > 0; o >>= 1) k += __shfl_xor_sync(0xFFFFFFFFu, k, o);
+    v[0] = __shfl_sync(0xFFFFFFFFu, k, 0);
+    v[1] = __shfl_sync(0xFFFFFFFFu, k, 16);
 }
 
 __device__ __forceinline__ uint32_t cluster_rank() {
@@ -555,11 +568,11 @@ __global__ void __launch_bounds__(32 * kNormWarps) norm_residual_backward_warp(c
 // fit.  The four rows of an iteration arrive in shared memory by bulk copies issued `stages` rows ahead: nothing waits for a
 // load, and a row needs no registers.  A thread reads its group twice (statistics, gradients) or, with a post norm, y and
 // one more value a third time.  What a thread writes to shared memory (parameters, the value between the phases) only it reads.
-// The statistics take one pass and one barrier: sums about a pivot p, s1 = sum (v - p), s2 = sum (v - p)^2, so that
-//     M2 = sum (v - mean)^2 = s2 - s1^2 / d,    sum g (h - mean) = sum g (h - p) - (mean - p) sum g.
-// The pivot is the mean of 32 values spread over the row.  The mean of any n of d values lies within sqrt(d / n - 1)
-// deviations of the mean, so in the worst case (all 32 of them the row's outliers) a factor d / 32 of the 2^-24 is lost,
-// ordinarily nothing, however large the mean is.
+// The statistics take one pass and one barrier.  A warp sums about a pivot p, s1 = sum (v - p), s2 = sum (v - p)^2, g1 = sum g (h - p),
+// and moves them to its mean, M2 = s2 - s1^2 / n; Chan's update then joins the warps.  The pivot is the mean of the warp's first 256
+// channels of at most 512: the mean of n1 of n values lies within sqrt(n / n1 - 1) deviations of theirs, here one, so that at
+// most half of s2 cancels, wherever the outliers of a row are.  (A pivot from 32 sampled channels of the row, joined in one step,
+// was off by a factor d / 32 for rows with their outliers in those; it was faster only on narrow rows, 16384 x 1024 75 us against 80.)
 // With 18 warps on an SM the instructions bound the kernel next to memory, so the arithmetic is done on pairs (f32x2).
 // Parameter vectors (weight (1 + scale), gate, post_weight) are kept in shared memory as floats, refreshed at the start of a batch.
 // Measured (layer, gate and modulation, 16-bit): 16384 x 4608 210 us, 4.3 TB/s; rms around rms, 6000 x 12288 in clusters of four 519 us,
@@ -786,13 +799,6 @@ __global__ void __launch_bounds__(kNormThreads, 1) norm_residual_backward(const 
         }
         m[0] = a.x; m[1] = a.y; m[2] = b.x; m[3] = b.y;
     };
-    // the mean of 32 values spread over this CTA's columns of a row, the same in every warp (the CTAs of a cluster use their own)
-    auto pivot_of = [&](float v) {
-#pragma unroll
-        for (int o = 16; o > 0; o >>= 1) v += __shfl_xor_sync(0xFFFFFFFFu, v, o);
-        return v * 0.03125f;
-    };
-    const int sample = (int)((int64_t)lane * d / 32);
     S* dx = static_cast<S*>(p.dx) + first * p.ld_dx + c0 + c;
     Y* dy = static_cast<Y*>(p.dy) + first * p.ld_dy + c0 + c;
     int s = 0, next = p.stages < rows ? p.stages : rows;              // stage of row r; next row to be fetched (thread 0)
@@ -830,40 +836,65 @@ __global__ void __launch_bounds__(kNormThreads, 1) norm_residual_backward(const 
         const int my_row = nr == 2 && warp >= per_row ? 1 : 0, part = warp - my_row * per_row;
         {
             const uint8_t* stage = my_row ? stages[1] : stages[0];
-            float pivot_h = 0.f, pivot_y = 0.f;
-            if (layer_h) pivot_h = pivot_of(Elem<S>::to_f32(reinterpret_cast<const S*>(stage)[sample]));
-            if (layer_y) pivot_y = pivot_of(Elem<Y>::to_f32(reinterpret_cast<const Y*>(stage + p.off_y)[sample]));
-            const f32x2 minus_h = pack2(-pivot_h, -pivot_h), minus_y = pack2(-pivot_y, -pivot_y);
+            float pivot_h = 0.f, pivot_y = 0.f;                       // means of the first (up to) 256 of this warp's columns
+            const int exist = d - part * nr * 256;
+            const float share = exist >= 256 ? 0.00390625f : 1.f / (float)(exist > 0 ? exist : 1);
+            if (layer_h || layer_y) {
+                const int gi = part * nr * 32 + lane;
+                float q[2] = {0.f, 0.f};
+                if (gi * 8 < d) {                                    // (a ragged end of a row is filled up with zeros)
+                    f32x2 v[4];
+                    if (layer_h) {
+                        lds8<S>(stage, gi, v);
+                        q[0] = sum2(add2(add2(v[0], v[1]), add2(v[2], v[3])));
+                    }
+                    if (layer_y) {
+                        lds8<Y>(stage + p.off_y, gi, v);
+                        q[1] = sum2(add2(add2(v[0], v[1]), add2(v[2], v[3])));
+                    }
+                }
+                if (POST) {
+                    warp_sum2(q, lane);
+                } else {
+#pragma unroll
+                    for (int o = 16; o > 0; o >>= 1) q[0] += __shfl_xor_sync(0xFFFFFFFFu, q[0], o);
+                }
+                pivot_h = q[0] * share;
+                pivot_y = q[1] * share;
+            }
             f32x2 s1 = 0ull, s2 = 0ull, g0 = 0ull, g1 = 0ull, y1 = 0ull, y2 = 0ull;
 #pragma unroll 1
             for (int k = 0; k < nr; ++k) {
                 const int gi = (part * nr + k) * 32 + lane, have = VEC ? (gi * 8 < d ? 8 : 0) : owned(d, gi * 8, 1);
                 if (have == 8) {
+                    if (POST) {
+                        const f32x2 minus = pack2(-pivot_y, -pivot_y);
+                        f32x2 v[4];
+                        lds8<Y>(stage + p.off_y, gi, v);
+#pragma unroll
+                        for (int i = 0; i < 4; ++i) {
+                            const f32x2 u = add2(v[i], minus);
+                            y1 = add2(y1, u);
+                            y2 = fma2(u, u, y2);
+                        }
+                    }
                     if (norm) {
+                        const f32x2 minus = pack2(-pivot_h, -pivot_h);
                         f32x2 v[4], g[4], m[4];
                         lds8<S>(stage, gi, v);
                         lds8<Y>(stage + p.off_dn, gi, g);
                         parameters(p.cache_m, par_m, gi, m);
 #pragma unroll
                         for (int i = 0; i < 4; ++i) {
-                            const f32x2 u = add2(v[i], minus_h), w = mul2(g[i], m[i]);
+                            const f32x2 u = add2(v[i], minus), w = mul2(g[i], m[i]);
                             s1 = add2(s1, u);
                             s2 = fma2(u, u, s2);
                             g0 = add2(g0, w);
                             g1 = fma2(w, u, g1);
                         }
                     }
-                    if (POST) {
-                        f32x2 v[4];
-                        lds8<Y>(stage + p.off_y, gi, v);
-#pragma unroll
-                        for (int i = 0; i < 4; ++i) {
-                            const f32x2 u = add2(v[i], minus_y);
-                            y1 = add2(y1, u);
-                            y2 = fma2(u, u, y2);
-                        }
-                    }
-                } else if (!VEC) {                                   // the ragged end of a row: one thread, one by one
+                }
+                if (!VEC && have < 8) {                              // the ragged end of a row: one thread, one by one
 #pragma unroll 1
                     for (int i = gi * 8; i < gi * 8 + have; ++i) {
                         if (norm) {
@@ -886,9 +917,26 @@ __global__ void __launch_bounds__(kNormThreads, 1) norm_residual_backward(const 
             warp_sum4(st, lane);
             if (POST) warp_sum4(sty, lane);
             if (lane == 0) {
+                // mean and squares about it of this warp's columns, sum g, sum g (h - mean)
+                float n = 0.f;
+                if (layer_h || layer_y) {
+                    const int left = d - part * nr * 256;
+                    n = left >= 256 * nr ? 256.f * nr : (float)(left > 0 ? left : 0);
+                    const float one_nth = left >= 256 * nr ? (nr == 2 ? 0.001953125f : 0.00390625f) : (left > 0 ? 1.f / n : 0.f);
+                    const float dh = st[0] * one_nth, dy = sty[0] * one_nth;
+                    if (layer_h) {
+                        st[1] = fmaf(-dh, st[0], st[1]);
+                        st[3] = fmaf(-dh, st[2], st[3]);
+                        pivot_h += dh;
+                    }
+                    if (layer_y) {
+                        sty[1] = fmaf(-dy, sty[0], sty[1]);
+                        pivot_y += dy;
+                    }
+                }
                 float* at = red + turn * kNormRedFloats + (my_row * p.cluster * per_row + rank * per_row + part) * 8;
-                exchange(turn, at, make_float4(st[0], st[1], st[2], st[3]));
-                exchange(turn, at + 4, make_float4(sty[0], sty[1], pivot_h, pivot_y));
+                exchange(turn, at, make_float4(pivot_h, st[1], st[2], st[3]));
+                exchange(turn, at + 4, make_float4(pivot_y, sty[1], n, 0.f));
             }
         }
         exchanged_all(turn, all_warps * 32);
@@ -897,46 +945,62 @@ __global__ void __launch_bounds__(kNormThreads, 1) norm_residual_backward(const 
             for (; next < rows && next < r + p.stages; ++next) issue(next, next % p.stages);
         const float* exchanged = red + turn * kNormRedFloats;        // (the other set may be written before all have read this one)
         turn ^= 1;
+        // Chan's update over the warps: first the means, as offsets from the first warp's, then the sums moved to them,
+        // sum (v - mean)^2 = M2 + n e^2 and sum g (h - mean) = g1 + e g0 with e = the warp's mean - mean.  Half a warp for each row.
+        float half_mean_h = 0.f, half_mean_g = 0.f, half_mean_y = 0.f, half_inv_h, half_along_h, half_inv_y = 1.f;
+        {
+            const int parts = p.cluster * per_row;
+            const float4* of_row = reinterpret_cast<const float4*>(exchanged + (nr == 2 && lane >= 16 ? parts * 8 : 0));
+            auto each = [&](auto&& f) {                               // the warps of this lane
+                int w = lane & 15;
+                const float4 none = make_float4(0.f, 0.f, 0.f, 0.f);
+                f(w < parts ? of_row[2 * w] : none, w < parts ? of_row[2 * w + 1] : none);
+                if (parts > 16)
+                    for (w += 16; w < parts; w += 16) f(of_row[2 * w], of_row[2 * w + 1]);
+            };
+            auto half_sum = [](float v) {
+#pragma unroll
+                for (int o = 8; o > 0; o >>= 1) v += __shfl_xor_sync(0xFFFFFFFFu, v, o);
+                return v;
+            };
+            if (layer_h || layer_y) {
+                const float base_h = of_row[0].x, base_y = of_row[1].x;
+                float mu = 0.f, mu_g = 0.f, mu_y = 0.f;
+                each([&](const float4& a, const float4& b) {
+                    mu = fmaf(b.z, a.x - base_h, mu);
+                    mu_g += a.z;
+                    if (POST) mu_y = fmaf(b.z, b.x - base_y, mu_y);
+                });
+                mu = half_sum(mu);
+                mu_g = half_sum(mu_g);
+                if (POST) mu_y = half_sum(mu_y);
+                if (layer_h) {
+                    half_mean_h = fmaf(mu, inv_d, base_h);
+                    half_mean_g = mu_g * inv_d;
+                }
+                if (layer_y) half_mean_y = fmaf(mu_y, inv_d, base_y);
+            }
+            float sq = 0.f, sq_g = 0.f, sq_y = 0.f;
+            each([&](const float4& a, const float4& b) {
+                const float eh = a.x - half_mean_h, ey = b.x - half_mean_y;
+                sq += fmaf(b.z * eh, eh, a.y);
+                sq_g += fmaf(eh, a.z, a.w);
+                if (POST) sq_y += fmaf(b.z * ey, ey, b.y);
+            });
+            sq = half_sum(sq);
+            sq_g = half_sum(sq_g);
+            if (POST) sq_y = half_sum(sq_y);
+            half_inv_h = norm ? rsqrtf(fmaf(sq, inv_d, p.eps)) : 0.f;
+            half_along_h = sq_g * inv_d * half_inv_h;
+            if (POST) half_inv_y = rsqrtf(fmaf(sq_y, inv_d, p.eps));
+        }
+        // ---- gradients: H = dh + inv_h (g m - mean_g - xhat along_h) ----
 #pragma unroll 1
         for (int j = 0; j < nr; ++j) {
         uint8_t* stage = j ? stages[1] : stages[0];
-        const float* of_row = exchanged + j * p.cluster * per_row * 8;
-        const float pivot_h = of_row[6], pivot_y = of_row[7];
-        float st[4] = {0.f, 0.f, 0.f, 0.f}, sty[4] = {0.f, 0.f, 0.f, 0.f};
-        if (p.cluster == 1) {
-            if (lane < per_row) {
-                const float4 a = reinterpret_cast<const float4*>(of_row + lane * 8)[0];
-                st[0] = a.x; st[1] = a.y; st[2] = a.z; st[3] = a.w;
-                if (POST) {
-                    const float2 b = reinterpret_cast<const float2*>(of_row + lane * 8)[2];
-                    sty[0] = b.x; sty[1] = b.y;
-                }
-            }
-        } else {
-            // every CTA summed about its own pivot: moved to that of rank 0, s1 + n e, s2 + 2 e s1 + n e^2, g1 + e g0
-            for (int w = lane; w < p.cluster * per_row; w += 32) {
-                const float4 a = reinterpret_cast<const float4*>(of_row + w * 8)[0], b = reinterpret_cast<const float4*>(of_row + w * 8)[1];
-                const int q = w / per_row, all = p.d - q * p.columns < p.columns ? p.d - q * p.columns : p.columns;
-                const int left = all - (w - q * per_row) * 256 * nr;
-                const float n = (float)(left < 0 ? 0 : (left > 256 * nr ? 256 * nr : left));
-                const float eh = b.z - pivot_h, ey = b.w - pivot_y;
-                st[0] += fmaf(n, eh, a.x);
-                st[1] += fmaf(eh, fmaf(n, eh, 2.f * a.x), a.y);
-                st[2] += a.z;
-                st[3] += fmaf(eh, a.z, a.w);
-                sty[0] += fmaf(n, ey, b.x);
-                sty[1] += fmaf(ey, fmaf(n, ey, 2.f * b.x), b.y);
-            }
-        }
-        warp_sum4(st, lane);
-        if (POST) warp_sum4(sty, lane);
-        // layer: mean = pivot + s1 / d, the squares and products moved to the mean; rms: mean 0, which the pivot was
-        const float shift_h = layer_h ? st[0] * inv_d : 0.f, shift_y = layer_y ? sty[0] * inv_d : 0.f;
-        const float mean_h = pivot_h + shift_h, mean_y = pivot_y + shift_y, mean_g = layer_h ? st[2] * inv_d : 0.f;
-        // ---- gradients: H = dh + inv_h (g m - mean_g - xhat along_h) ----
-        const float inv_h = norm ? rsqrtf(fmaf(st[1], inv_d, -shift_h * shift_h) + p.eps) : 0.f;
-        const float along_h = fmaf(-shift_h, st[2], st[3]) * inv_d * inv_h;
-        const float inv_y = POST ? rsqrtf(fmaf(sty[1], inv_d, -shift_y * shift_y) + p.eps) : 1.f;
+        auto of_this = [&](float v) { return __shfl_sync(0xFFFFFFFFu, v, 16 * j); };
+        const float mean_h = of_this(half_mean_h), mean_g = of_this(half_mean_g), inv_h = of_this(half_inv_h), along_h = of_this(half_along_h);
+        const float mean_y = POST ? of_this(half_mean_y) : 0.f, inv_y = POST ? of_this(half_inv_y) : 1.f;
         const f32x2 inv_h2 = pack2(inv_h, inv_h), off_h2 = pack2(-mean_h, -mean_h), along2 = pack2(-along_h, -along_h), mean_g2 = pack2(-mean_g, -mean_g);
         const f32x2 inv_y2 = pack2(inv_y, inv_y), off_y2 = pack2(-mean_y, -mean_y);
         f32x2 back0 = 0ull, back1 = 0ull;
@@ -1039,7 +1103,8 @@ __global__ void __launch_bounds__(kNormThreads, 1) norm_residual_backward(const 
 // The kernel above starts a CTA per row, whose load latency, two reductions and parameter reads follow one another; with many
 // rows that is what it costs (8192 x 2240, layer norm, gate and modulation: 44 us).  Here a CTA keeps its threads, its parameter
 // vectors (shared memory) and two rows at a time, which share every barrier and every sum over a warp, while the next rows
-// arrive by bulk copies.  Statistics in one pass about a sampled pivot, as in the backward kernel; h stays in registers.
+// arrive by bulk copies.  Every warp takes the mean of its own values, then their squares about it (h in registers, y read again
+// from shared memory), and Chan's update joins the warps behind one barrier.
 // Measured: the same 34 us (4.3 TB/s; 2.0 of 4 instructions per cycle with 27 warps per SM, neither memory nor issue alone);
 // 16385 x 5600, rms around rms with a 32-bit stream, 217 to 228 us (4.8 to 5.1 TB/s, bound by memory).
 constexpr int kNormFwdRedOff = 128;
@@ -1087,8 +1152,17 @@ __global__ void __launch_bounds__(1024, 1) norm_residual_forward_rows(const __gr
     bool have[VPT];
 #pragma unroll
     for (int k = 0; k < VPT; ++k) have[k] = (t + k * T) * 8 < p.d;
-    const int sample = (int)((int64_t)lane * p.d / 32);
-    float gate_s = 1.f, post_s = 1.f;                                 // gate and post_weight at this lane's sampled channel
+    // channels of a warp: its own as a reciprocal; those of warp `lane`
+    auto channels = [&](int w) {
+        int n = 0;
+#pragma unroll
+        for (int k = 0; k < VPT; ++k) {
+            const int left = (p.d >> 3) - k * T - 32 * w;
+            n += left < 0 ? 0 : (left > 32 ? 32 : left);
+        }
+        return 8 * n;
+    };
+    const float own_share = 1.f / (float)channels(warp), n_lane = lane < warps ? (float)channels(lane) : 0.f;
     auto refresh = [&]() {                                            // every thread its own groups
 #pragma unroll
         for (int k = 0; k < VPT; ++k)
@@ -1110,10 +1184,6 @@ __global__ void __launch_bounds__(1024, 1) norm_residual_forward_rows(const __gr
                     keep(par_mul);
                 }
             }
-        if (layer_h && p.y) {
-            gate_s = vec_entry(p.gate, batch, sample, 1.f);
-            post_s = vec_entry(p.post_weight, 0, sample, 1.f);
-        }
     };
     refresh();
     // eight entries of a vector: kept, read through the caches, or absent
@@ -1128,19 +1198,63 @@ __global__ void __launch_bounds__(1024, 1) norm_residual_forward_rows(const __gr
             for (int i = 0; i < 4; ++i) m[i] = pack2(f[2 * i], f[2 * i + 1]);
         }
     };
-    auto sum32 = [&](float v) {
+    // mean (layer, else 0) and sum of squares about it of both rows, over the CTA: every warp about the mean of its own values, joined by
+    // Chan's update
+    auto statistics = [&](auto&& values, bool layer, int set, float (&mean)[2], float (&m2)[2]) {      // values(j, k, v): group k of row j
+        float own[2] = {0.f, 0.f};
+        if (layer) {
 #pragma unroll
-        for (int o = 16; o > 0; o >>= 1) v += __shfl_xor_sync(0xFFFFFFFFu, v, o);
-        return v;
-    };
-    // {s1, s2} of both rows over the CTA
-    auto row_sums = [&](float (&v)[4], int set) {
-        warp_sum4(v, lane);
-        if (lane == 0) red[set * 32 + warp] = make_float4(v[0], v[1], v[2], v[3]);
+            for (int j = 0; j < 2; ++j) {
+                f32x2 a = 0ull;
+#pragma unroll
+                for (int k = 0; k < VPT; ++k)
+                    if (have[k]) {
+                        f32x2 v[4];
+                        values(j, k, v);
+                        a = add2(a, add2(add2(v[0], v[1]), add2(v[2], v[3])));
+                    }
+                own[j] = sum2(a);
+            }
+            warp_sum2(own, lane);
+            own[0] *= own_share;
+            own[1] *= own_share;
+        }
+#pragma unroll
+        for (int j = 0; j < 2; ++j) {
+            const f32x2 minus = pack2(-own[j], -own[j]);
+            f32x2 a = 0ull;
+#pragma unroll
+            for (int k = 0; k < VPT; ++k)
+                if (have[k]) {
+                    f32x2 v[4];
+                    values(j, k, v);
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) {
+                        const f32x2 u = layer ? add2(v[i], minus) : v[i];
+                        a = fma2(u, u, a);
+                    }
+                }
+            m2[j] = sum2(a);
+        }
+        warp_sum2(m2, lane);
+        float4* at = red + set * 32;
+        if (lane == 0) at[warp] = make_float4(own[0], own[1], m2[0], m2[1]);
         __syncthreads();
-        const float4 a = lane < warps ? red[set * 32 + lane] : make_float4(0.f, 0.f, 0.f, 0.f);
-        v[0] = a.x; v[1] = a.y; v[2] = a.z; v[3] = a.w;
-        warp_sum4(v, lane);
+        const float4 a = lane < warps ? at[lane] : make_float4(0.f, 0.f, 0.f, 0.f);
+        m2[0] = a.z;
+        m2[1] = a.w;
+        mean[0] = mean[1] = 0.f;
+        if (layer) {
+            const float base0 = at[0].x, base1 = at[0].y;            // (means as offsets from the first warp's)
+            mean[0] = n_lane * (a.x - base0);
+            mean[1] = n_lane * (a.y - base1);
+            warp_sum2(mean, lane);
+            mean[0] = fmaf(mean[0], inv_d, base0);
+            mean[1] = fmaf(mean[1], inv_d, base1);
+            m2[0] = fmaf(n_lane * (a.x - mean[0]), a.x - mean[0], m2[0]);
+            m2[1] = fmaf(n_lane * (a.y - mean[1]), a.y - mean[1], m2[1]);
+        }
+        warp_sum2(m2, lane);
     };
     const f32x2 alpha2 = pack2(p.alpha, p.alpha);
     int s = 0, turn = 0;
@@ -1168,46 +1282,19 @@ __global__ void __launch_bounds__(1024, 1) norm_residual_forward_rows(const __gr
         if (nr == 1) stage[1] = stage[0];                            // (computed twice, stored once)
         float mean_y[2] = {0.f, 0.f}, inv_y[2] = {1.f, 1.f};
         if (POST) {
-            float v[4] = {0.f, 0.f, 0.f, 0.f}, pivot[2] = {0.f, 0.f};
+            float m2[2];
+            // (read again for every pass: kept, they would spill)
+            statistics([&](int j, int k, f32x2 (&v)[4]) {
+                asm volatile("" ::: "memory");
+                lds8<Y>(stage[j] + p.off_y, t + k * T, v);
+            }, layer_y, turn, mean_y, m2);
 #pragma unroll
-            for (int j = 0; j < 2; ++j) {
-                if (layer_y) pivot[j] = sum32(Elem<Y>::to_f32(reinterpret_cast<const Y*>(stage[j] + p.off_y)[sample])) * 0.03125f;
-                const f32x2 minus = pack2(-pivot[j], -pivot[j]);
-                f32x2 s1 = 0ull, s2 = 0ull;
-#pragma unroll
-                for (int k = 0; k < VPT; ++k)
-                    if (have[k]) {
-                        f32x2 y[4];
-                        lds8<Y>(stage[j] + p.off_y, t + k * T, y);
-#pragma unroll
-                        for (int i = 0; i < 4; ++i) {
-                            const f32x2 u = add2(y[i], minus);
-                            s1 = add2(s1, u);
-                            s2 = fma2(u, u, s2);
-                        }
-                    }
-                v[2 * j] = sum2(s1);
-                v[2 * j + 1] = sum2(s2);
-            }
-            row_sums(v, turn);
-#pragma unroll
-            for (int j = 0; j < 2; ++j) {
-                const float shift = layer_y ? v[2 * j] * inv_d : 0.f;
-                mean_y[j] = pivot[j] + shift;
-                inv_y[j] = rsqrtf(fmaf(v[2 * j + 1], inv_d, -shift * shift) + p.eps);
-            }
+            for (int j = 0; j < 2; ++j) inv_y[j] = rsqrtf(fmaf(m2[j], inv_d, p.eps));
         }
         f32x2 h[2][VPT][4];
-        float v[4] = {0.f, 0.f, 0.f, 0.f}, pivot[2] = {0.f, 0.f};
 #pragma unroll
         for (int j = 0; j < 2; ++j) {
-            if (layer_h) {
-                float q = p.alpha * Elem<S>::to_f32(reinterpret_cast<const S*>(stage[j])[sample]);
-                if (p.y) q = fmaf(gate_s, (Elem<Y>::to_f32(reinterpret_cast<const Y*>(stage[j] + p.off_y)[sample]) - mean_y[j]) * inv_y[j] * post_s, q);
-                pivot[j] = sum32(q) * 0.03125f;
-            }
-            const f32x2 minus = pack2(-pivot[j], -pivot[j]), off_y = pack2(-mean_y[j] * inv_y[j], -mean_y[j] * inv_y[j]), inv_y2 = pack2(inv_y[j], inv_y[j]);
-            f32x2 s1 = 0ull, s2 = 0ull;
+            const f32x2 off_y = pack2(-mean_y[j] * inv_y[j], -mean_y[j] * inv_y[j]), inv_y2 = pack2(inv_y[j], inv_y[j]);
 #pragma unroll
             for (int k = 0; k < VPT; ++k)
                 if (have[k]) {
@@ -1232,17 +1319,13 @@ __global__ void __launch_bounds__(1024, 1) norm_residual_forward_rows(const __gr
                         for (int i = 0; i < 4; ++i) h[j][k][i] = fma2(m[i], x[i], h[j][k][i]);
                     }
                     if (p.h && j < nr) store_pairs(static_cast<S*>(p.h) + (first + r + j) * p.ld_h + gi * 8, 8, true, h[j][k]);
-#pragma unroll
-                    for (int i = 0; i < 4; ++i) {
-                        const f32x2 u = layer_h ? add2(h[j][k][i], minus) : h[j][k][i];
-                        if (layer_h) s1 = add2(s1, u);
-                        s2 = fma2(u, u, s2);
-                    }
                 }
-            v[2 * j] = sum2(s1);
-            v[2 * j + 1] = sum2(s2);
         }
-        row_sums(v, 2 + turn);
+        float mean[2], m2[2];
+        statistics([&](int j, int k, f32x2 (&v)[4]) {
+#pragma unroll
+            for (int i = 0; i < 4; ++i) v[i] = h[j][k][i];
+        }, layer_h, 2 + turn, mean, m2);
         turn ^= 1;
         // every thread has read its part of these rows: their stages take the rows that follow
         if (t == 0)
@@ -1251,9 +1334,8 @@ __global__ void __launch_bounds__(1024, 1) norm_residual_forward_rows(const __gr
 #pragma unroll
         for (int j = 0; j < 2; ++j)
             if (j < nr) {
-                const float shift = layer_h ? v[2 * j] * inv_d : 0.f, mean = pivot[j] + shift;
-                const float inv = rsqrtf(fmaf(v[2 * j + 1], inv_d, -shift * shift) + p.eps);
-                const f32x2 off = pack2(-mean, -mean), inv2 = pack2(inv, inv);
+                const float inv = rsqrtf(fmaf(m2[j], inv_d, p.eps));
+                const f32x2 off = pack2(-mean[j], -mean[j]), inv2 = pack2(inv, inv);
 #pragma unroll
                 for (int k = 0; k < VPT; ++k)
                     if (have[k]) {
