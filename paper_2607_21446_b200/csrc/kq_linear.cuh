@@ -143,10 +143,32 @@ __device__ __forceinline__ void store_typed(void* p, int type, int64_t at, float
     else static_cast<__nv_bfloat16*>(p)[at] = __float2bfloat16_rn(v);
 }
 
-// Arrival on another CTA's barrier that hands over tensor memory only.  Its release has CTA scope: at cluster scope it would
-// wait for the global stores of the item before, 2 to 3 us behind the operand loads.
-__device__ __forceinline__ void mbar_arrive_remote(uint32_t cluster_addr) {
-    asm volatile("mbarrier.arrive.shared::cluster.b64 _, [%0];" ::"r"(cluster_addr) : "memory");
+// Arrival on the barrier of a CTA of the cluster, and the wait for it, that hand over tensor memory only: what orders the loads before
+// and the products behind them are the tcgen05 fences at both ends and the completed loads, so both are relaxed, at cluster scope.  (A
+// release there would wait for the global stores of the item before, 2 to 3 us behind the operand loads.)
+__device__ __forceinline__ void mbar_arrive_relaxed(uint32_t cluster_addr) {
+    asm volatile("mbarrier.arrive.relaxed.cluster.shared::cluster.b64 _, [%0];" ::"r"(cluster_addr) : "memory");
+}
+__device__ __forceinline__ bool mbar_try_wait_relaxed(uint32_t bar, uint32_t parity) {
+    uint32_t ok;
+    asm volatile("{\n\t.reg .pred p;\n\t"
+                 "mbarrier.try_wait.parity.relaxed.cluster.shared::cta.b64 p, [%1], %2;\n\t"
+                 "selp.u32 %0, 1, 0, p;\n\t}"
+                 : "=r"(ok) : "r"(bar), "r"(parity) : "memory");
+    return ok != 0;
+}
+__device__ __forceinline__ bool mbar_wait_relaxed(uint32_t bar, uint32_t parity, volatile int* abort_flag) {      // bounded as mbar_wait
+    uint64_t t0 = 0;
+    for (uint32_t i = 1; i < (1u << 30); ++i) {
+        if (mbar_try_wait_relaxed(bar, parity)) return true;
+        if ((i & 4095u) == 0u) {
+            if (*abort_flag) return false;
+            const uint64_t now = global_timer_ns();
+            if (t0 == 0) t0 = now;
+            else if (now - t0 > kWaitLimitNs) return false;
+        }
+    }
+    return false;
 }
 // sixteen columns of this warp's 32 TMEM lanes, without the completion wait
 __device__ __forceinline__ void tc_ld_32x16_nowait(uint32_t taddr, uint32_t* r) {
@@ -608,7 +630,7 @@ linear_mxfp4_pair(const __grid_constant__ CUtensorMap tmap_a, const __grid_const
             ItemAhead ahead = item_ahead(p, cum, pair, n_items);
             for (int i = 0; ok && i < my_items; ++i) {
                 const int acc = i & 1;
-                if (i >= 2 && !mbar_wait(bar_tempty(acc), ((i >> 1) - 1) & 1, abort_flag)) {
+                if (i >= 2 && !mbar_wait_relaxed(bar_tempty(acc), ((i >> 1) - 1) & 1, abort_flag)) {
                     if (!*abort_flag) { atomicExch(&g_kq_device_error, KQ_DEV_TIMEOUT_GEMM_MMA); *abort_flag = 1; }
                     break;
                 }
@@ -717,7 +739,7 @@ linear_mxfp4_pair(const __grid_constant__ CUtensorMap tmap_a, const __grid_const
             }
             tc_fence_before();
             __syncwarp();
-            if (lane == 0) mbar_arrive_remote(mapa_shared(bar_tempty(acc), 0));
+            if (lane == 0) mbar_arrive_relaxed(mapa_shared(bar_tempty(acc), 0));
             if (!live) continue;
             asm volatile("cp.async.wait_all;" ::: "memory");
             __syncwarp();                                                           // every lane's entries are there
