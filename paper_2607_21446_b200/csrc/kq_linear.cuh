@@ -137,11 +137,6 @@ __device__ __forceinline__ float load_typed(const void* p, int type, int64_t at)
     if (type == kTypeF16) return __half2float(static_cast<const __half*>(p)[at]);
     return __bfloat162float(static_cast<const __nv_bfloat16*>(p)[at]);
 }
-__device__ __forceinline__ void store_typed(void* p, int type, int64_t at, float v) {
-    if (type == kTypeF32) static_cast<float*>(p)[at] = v;
-    else if (type == kTypeF16) static_cast<__half*>(p)[at] = __float2half_rn(v);
-    else static_cast<__nv_bfloat16*>(p)[at] = __float2bfloat16_rn(v);
-}
 
 // Arrival on the barrier of a CTA of the cluster, and the wait for it, that hand over tensor memory only: what orders the loads before
 // and the products behind them are the tcgen05 fences at both ends and the completed loads, so both are relaxed, at cluster scope.  (A
@@ -338,8 +333,7 @@ __device__ __forceinline__ uint32_t idesc_mxf4_192(uint32_t sf_id) {
 // a lane takes a column, so that a warp's accesses stay neighbours in memory.  Gated: 16 features, gate half first.
 struct EpiChunk {
     int row0, lo, hi;                    // first row of the warp, rows of the group
-    int col, at;                         // first column of out; first accumulator column within the warp's 64
-    int out_at;                          // first column of out within the warp's
+    int col, at;                         // first column of out; the chunk's first entry in the warp's bias and gate
     int which;                           // gate row of this lane's row; uniform: the whole warp's, in shared memory
     bool uniform;
     float scale;                         // row scale of this lane's row
@@ -378,7 +372,7 @@ __device__ __forceinline__ void epilogue_chunk(const LinearEpilogue& p, const ui
     }
     if (p.gate.ptr) {
         if (c.uniform) {
-            apply_shared<C, true>(vec + kLinCols + c.out_at, v);
+            apply_shared<C, true>(vec + kLinCols + c.at, v);
         } else {                                                     // rows of several gate rows in one warp
 #pragma unroll
             for (int i = 0; i < C; ++i) v[i] *= i < have ? vec_entry(p.gate, c.which, c.col + i, 1.f) : 1.f;
@@ -748,9 +742,8 @@ linear_mxfp4_pair(const __grid_constant__ CUtensorMap tmap_a, const __grid_const
 #pragma unroll 1
             for (int q = 0; q < 2; ++q) {
                 c.at = GLU ? 16 * q : 32 * q;
-                c.out_at = GLU ? 16 * q : 32 * q;
-                c.col = col + c.out_at;
-                c.res_at = c.out_at * (p.epi.residual_type == kTypeF32 ? 4 : 2) % kLinRowBytes;
+                c.col = col + c.at;
+                c.res_at = c.at * (p.epi.residual_type == kTypeF32 ? 4 : 2) % kLinRowBytes;
                 if (copied && c.res_at == 0 && q > 0 && c.col < p.epi.N) {          // 32-bit residual: the other half of the columns
                     fetch_residual(p.epi, mem, bar_res, c.row0 + lane, c.lo, c.hi, c.col, lane);
                     if (!mbar_wait(bar_res, res_parity, abort_flag) && !*abort_flag) { atomicExch(&g_kq_device_error, KQ_DEV_TIMEOUT_GEMM_EPILOGUE); *abort_flag = 1; }

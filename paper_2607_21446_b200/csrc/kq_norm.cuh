@@ -580,7 +580,6 @@ __global__ void __launch_bounds__(32 * kNormWarps) norm_residual_backward_warp(c
 // Rows that bulk copies cannot take (16-byte alignment) are copied into the same place by the threads, element by element.
 constexpr int kNormStageMax = 6;
 constexpr int kNormThreads = 576;
-constexpr int kNormColumns = 8 * kNormThreads;                      // of a CTA
 constexpr int kNormMaxCluster = 4;
 constexpr int kNormRedOff = 128;                                    // barriers and the abort word in front
 constexpr int kNormRedFloats = kNormMaxCluster * (kNormThreads / 32) * 8;
