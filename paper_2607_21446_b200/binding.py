@@ -583,7 +583,8 @@ class LinearW4A4:
 
     def fused(self, X: torch.Tensor, *, stream=None, **epilogue) -> torch.Tensor:
         """The layer with its epilogue: quantizer, then :func:`kroquant_linear_mxfp4` with the keyword arguments given here
-        (bias, activation, glu, gate, row_scale, residual, out, ...).  Two launches."""
+        (bias, activation, glu, gate, row_scale, residual, out, ...).  Two launches.  (Without an epilogue ``__call__`` is the
+        faster one for many rows: 4608 x 3072 -> 12288 in 85 against 105 us.)"""
         tokens, d = _x_shape(X)
         if d != self.d:
             raise ValueError("X [tokens, d] does not match the weights")

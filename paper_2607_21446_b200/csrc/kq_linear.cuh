@@ -294,8 +294,9 @@ __device__ __forceinline__ LinearItem linear_item(const LinearProblem& p, const 
 // residual (a bulk copy per row) into shared memory.
 // Barriers as in gemm_mxfp4_umma_pair; 12 epilogue warps per CTA, one for each 32 rows x 64 columns.
 // Bound by the operands' way from L2 to the SMs (11 to 13 TB/s over all SMs) and, on long runs, by the power limit.  Measured: 16384 x
-// 4608 -> 12288 with bias, gate and residual 440 to 530 us (3.5 to 4.2 PFLOP/s), 8192 x 8192 -> 8192 plain 225 to 235 us (4.8), 8
-// gated experts of 4096 -> 5632 on 16384 rows 363 to 435 us, 4099 x 2240 -> 5601 with gelu and an odd pitch 58 us.
+// 4608 -> 12288 with bias, gate and residual 455 to 530 us (3.5 to 4.1 PFLOP/s; the upper end in sustained runs), 8192 x 8192 -> 8192
+// plain 225 to 235 us (4.8), where the 256 x 256 tiles of gemm_mxfp4_umma_pair, which move a seventh less per operation, take 191;
+// 8 gated experts of 4096 -> 5632 on 16384 rows 363 to 435 us, 4099 x 2240 -> 5601 with gelu_tanh and an odd pitch 58 us.
 constexpr int kLinN = 192;
 constexpr int kLinStages = 5;
 constexpr int kLinABytes = 128 * 128;
@@ -517,7 +518,8 @@ __device__ __forceinline__ void fetch_vectors(const LinearEpilogue& p, float* ve
     }
 }
 // This lane's row of the residual from column `col` on, up to kLinRowBytes of it, and the warp's barrier armed with all of them.
-// (Only whole 16-byte pieces: what a ragged last chunk needs is read in the column layout.)
+// (Only whole 16-byte pieces: what a ragged last chunk needs is read in the column layout.  A gated product takes half of what is
+// copied of a 16-bit residual: 32 columns a warp.)
 __device__ __forceinline__ void fetch_residual(const LinearEpilogue& p, uint8_t* mem, uint32_t bar, int row, int lo, int hi, int col, int lane) {
     const int size = p.residual_type == kTypeF32 ? 4 : 2;
     const int bytes = (p.N - col) * size < kLinRowBytes ? (p.N - col) * size & ~15 : kLinRowBytes;
@@ -785,8 +787,8 @@ linear_mxfp4_pair(const __grid_constant__ CUtensorMap tmap_a, const __grid_const
 // shared memory and every CTA adds its share of the elements in rank order (the same bits every time).  With splits > 1 a
 // cluster has exactly one item, so the partials use the pipeline's memory after its last read; with one CTA per item the
 // kernel is persistent.
-// Measured: 8 gated experts of 4096 -> 5632 with 16 rows 29 us (5.1 TB/s, 0.78 of what a copy reaches), 32 experts of 5600 -> 2240
-// with 1030 rows 48 us, 24 rows x 4096 -> 4096 8.6 us, one row x 1152 -> 6912 7.3 us (start of a kernel, not bytes).
+// Measured: 8 gated experts of 4096 -> 5632 with 16 rows 30 us (4.9 TB/s, 0.76 of what a copy reaches), 32 experts of 5600 -> 2240
+// with 1030 rows 48 to 49 us, 24 rows x 4096 -> 4096 8.7 us, one row x 1152 -> 6912 7.4 us (start of a kernel, not bytes).
 constexpr int kNarrowThreads = 352;                                      // producer, MMA issuer, 8 epilogue warps, scale copies
 template <int TB>
 struct NarrowSmem {

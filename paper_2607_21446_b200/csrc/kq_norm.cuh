@@ -262,7 +262,8 @@ struct NormForward {
 
 // blockDim = (threads of a row, rows of a CTA): one warp per row and several rows for narrow d, else one row per CTA.
 // Thread i owns the 8-channel groups i, i + blockDim.x, ...: VPT of them.
-// Measured: one row of 4096 3.2 us (a launch); 16384 x 256 30 to 34 us; 16384 x 2241 (no vector accesses) 129 us.
+// Measured: one row of 4096 3.2 us (a launch); layer, gate and modulation 16384 x 256 11 us, 16384 x 1024 41 us (a warp reloads its
+// vectors for every row); rms 16384 x 2241 (no vector accesses) 129 us.
 template <typename S, typename Y, int VPT>
 __global__ void __launch_bounds__(VPT == 2 ? 1024 : 256) norm_residual_forward(const __grid_constant__ NormForward p) {
     __shared__ float red[2 * 128];
@@ -575,8 +576,8 @@ __global__ void __launch_bounds__(32 * kNormWarps) norm_residual_backward_warp(c
 // was off by a factor d / 32 for rows with their outliers in those; it was faster only on narrow rows, 16384 x 1024 75 us against 80.)
 // With 18 warps on an SM the instructions bound the kernel next to memory, so the arithmetic is done on pairs (f32x2).
 // Parameter vectors (weight (1 + scale), gate, post_weight) are kept in shared memory as floats, refreshed at the start of a batch.
-// Measured (layer, gate and modulation, 16-bit): 16384 x 4608 210 us, 4.3 TB/s; rms around rms, 6000 x 12288 in clusters of four 519 us,
-// 1.7 TB/s (every row waits for an exchange between CTAs); 16384 x 2241 (element copies) 374 us.
+// Measured (layer, gate and modulation, 16-bit): 16384 x 4608 205 us, 4.4 TB/s; 16384 x 1024 81 us; rms around rms, 6000 x 12288 in
+// clusters of four 480 us, 1.8 TB/s (every row waits for an exchange between CTAs); 16384 x 2241 (element copies) 344 us.
 // Rows that bulk copies cannot take (16-byte alignment) are copied into the same place by the threads, element by element.
 constexpr int kNormStageMax = 6;
 constexpr int kNormThreads = 576;
@@ -1104,8 +1105,8 @@ __global__ void __launch_bounds__(kNormThreads, 1) norm_residual_backward(const 
 // vectors (shared memory) and two rows at a time, which share every barrier and every sum over a warp, while the next rows
 // arrive by bulk copies.  Every warp takes the mean of its own values, then their squares about it (h in registers, y read again
 // from shared memory), and Chan's update joins the warps behind one barrier.
-// Measured: the same 34 us (4.3 TB/s; 2.0 of 4 instructions per cycle with 27 warps per SM, neither memory nor issue alone);
-// 16385 x 5600, rms around rms with a 32-bit stream, 217 to 228 us (4.8 to 5.1 TB/s, bound by memory).
+// Measured: the same 33 us (4.5 TB/s; instructions and their latency with 27 warps per SM, neither memory nor issue alone);
+// 16385 x 5600, rms around rms with a 32-bit stream, 206 to 215 us (5.1 to 5.3 TB/s, bound by memory).
 constexpr int kNormFwdRedOff = 128;
 constexpr int kNormFwdHead = kNormFwdRedOff + 4 * 32 * 16;            // two sets of sums for each of the two norms, used in turn
 enum { kCacheGate = 1, kCachePost = 2, kCacheMul = 4, kCacheShift = 8 };
@@ -1369,6 +1370,7 @@ struct NormVecGrads {
 };
 
 // blockDim = (32 columns, kSlotLanes): lane l of a column adds slots l, l + kSlotLanes, ...; lane 0 adds the lanes' sums in order.
+// Batches follow one another, which a few of them hide; with a vector row for each of 16384 rows of 2240 the gradients take 36 ms.
 constexpr int kSlotLanes = 16;
 __global__ void __launch_bounds__(32 * kSlotLanes) norm_vector_gradients(const __grid_constant__ NormVecGrads p) {
     __shared__ float part[3][kSlotLanes][32];

@@ -185,7 +185,9 @@ kq_status_t run_linear(const uint8_t* a_codes, const uint8_t* a_scales, const ui
     // Few rows per weight: the weight is the wide operand and is what is read.  Narrow against pair kernel, us: dense N x K = 4096 x
     // 4096 8.3 / 11.6 (1 row), 9.0 / 11.4 (32), 11.0 / 11.7 (64), 15.5 / 12.7 (128); 12288 x 2240 7.3 / 11.9, 11.7 / 10.7 (32), 16.8 / 11.1;
     // 8 gated experts of 4096 x 4096 29 / 44 (4 rows each), 33 / 41 (32), 40 / 46 (64), 58 / 52 (128); 32 of 1024 x 2048 16 / 22,
-    // 26 / 25 (32), 35 / 30 (64).
+    // 26 / 25 (32), 35 / 30 (64).  The rule goes by rows per weight alone, between these: it gives away 1 us at 12288 x 2240 with 32
+    // rows and 6 us with 64 rows for each of the 8 experts.  It takes the mean over the experts (the sizes are on the device): all 2560
+    // rows on one of 64 experts of 1024 x 2048 take 29 us, spread evenly 34.
     const bool narrow = M <= (experts ? 40 : 32) * (int64_t)count;
     if (!narrow) return e.glu ? launch_pair<true>(l, enc, sms, st) : launch_pair<false>(l, enc, sms, st);
     if (M <= 32) return e.glu ? launch_narrow<true, 32>(l, enc, sms, st) : launch_narrow<false, 32>(l, enc, sms, st);
