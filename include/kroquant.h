@@ -429,6 +429,121 @@ kq_status_t kroquant_norm_residual(const kq_norm_args_t *args, void *stream);
 int64_t kroquant_norm_residual_grad_scratch_bytes(const kq_norm_args_t *args);
 kq_status_t kroquant_norm_residual_grad(const kq_norm_args_t *args, void *scratch, int64_t scratch_bytes, void *stream);
 
+/* ---- One step of a block over new tokens -------------------------------------------------------
+ *
+ * Positions, the cache of keys and values, the attention that reads it, and products whose rows stay in 16 bits: what a block
+ * with MXFP4 weights runs between its products when it takes a few new tokens at a time.
+ *
+ * kroquant_rotary: rotary positions with one to four axes (time, height, width, ...).  A head's first 2 P channels are P pairs; axis i
+ * owns the next axis_channels[i] / 2 of them (each even, 2 P = their sum <= head_dim), and pair p of axis i of token t turns by
+ *     angle = positions[t][i] * frequencies[p]:     (a, b) -> (a cos - b sin, a sin + b cos),    the channels behind 2 P are copied.
+ * The angle is formed and reduced in 64 bits, so that it keeps its digits far from 0; sine and cosine are 32-bit values.  inverse = 1
+ * turns by -angle: the backward pass (gradients in, gradients out).  Pairs are the channels (2p, 2p + 1) (INTERLEAVED) or (p, p + P)
+ * (HALF).  One or two tensors (queries and keys, x[1] may be NULL) of one type, any strides in elements with contiguous channels;
+ * out[i] may be x[i] (same strides) and overlaps no other tensor.  head_dim <= 512, batches * tokens < 2^31. */
+typedef enum { KQ_ROTARY_INTERLEAVED = 0, KQ_ROTARY_HALF = 1 } kq_rotary_layout_t;
+
+typedef struct kq_rotary_args {
+    int dtype;                           /* kq_dtype_t of x and out */
+    int64_t batches, tokens;
+    int head_dim, layout, inverse;
+    int axes, axis_channels[4];
+    const double *frequencies;           /* DEVICE [P] */
+    const void *positions;               /* DEVICE int32, or float with positions_f32: token t of batch b, axis i at b * batch stride + t * token stride + i */
+    int positions_f32;
+    int64_t position_batch_stride, position_token_stride;
+    const void *x[2];                    /* DEVICE */
+    void *out[2];
+    int heads[2];
+    int64_t x_batch_stride[2], x_token_stride[2], x_head_stride[2];
+    int64_t out_batch_stride[2], out_token_stride[2], out_head_stride[2];
+} kq_rotary_args_t;
+
+/* Writes the defaults: zeros, one batch, one axis.  NULL is ignored. */
+void kroquant_rotary_args_default(kq_rotary_args_t *a);
+kq_status_t kroquant_rotary(const kq_rotary_args_t *args, void *stream);
+
+/* The paged cache of keys and values: `pages` pages of `page_size` positions for `heads` heads, keys and values apart:
+ *     k, v               [pages][heads][page_size][row]            16-byte aligned
+ *     k_scales, v_scales [pages][heads][page_size][scale row]      8-byte aligned, not used by 16BIT
+ * A row holds a head's channels at one position, filled up with zeros to C = 32 ceil(head_dim / 32) channels: 16-bit values of
+ * `dtype` (16BIT), C E4M3 codes (MXFP8) or C/2 bytes of packed E2M1 codes (MXFP4, even channel in the low half); a scale row
+ * one E8M0 byte per 32 channels, filled up with zeros to 4 ceil(C / 128) bytes.  The encoder is the quantizer's: S = clamp(floor(log2 amax) -
+ * e + 127, 0, 254) with e = 2 (E2M1) or 8 (E4M3), codes of y 2^(127 - S) rounded to nearest even, saturating.  1 <= head_dim <= 256,
+ * pages * heads * page_size < 2^32. */
+typedef enum { KQ_CACHE_16BIT = 0, KQ_CACHE_MXFP8 = 1, KQ_CACHE_MXFP4 = 2 } kq_cache_format_t;
+
+typedef struct kq_cache {
+    int format, dtype;                   /* kq_cache_format_t; KQ_OUT_BF16 or KQ_OUT_FP16 (16BIT only) */
+    int64_t pages;
+    int page_size, heads, head_dim;
+    void *k, *v;
+    uint8_t *k_scales, *v_scales;
+} kq_cache_t;
+
+/* Rows of keys and values and the places in the cache that belong to them.  Sequence s has the pages table[s][0], table[s][1], ...
+ * (DEVICE int32, rows table_stride apart); its position t lies in page table[s][t / page_size].  Row i belongs to sequence s with
+ * offsets[s] <= i < offsets[s + 1] and has position starts[s] + i - offsets[s].  offsets: DEVICE int32 [sequences + 1], non-decreasing, or
+ * NULL: row i belongs to sequence i (rows == sequences).  starts: DEVICE int32 [sequences], or NULL: 0.  A position that is negative or
+ * beyond the table, and a table entry outside [0, pages), is no place: write leaves such a row out, read gives zeros.  Rows outside
+ * [offsets[0], offsets[sequences]) are neither written nor read.  No value of offsets, starts or table leads outside the buffers;
+ * pages that two sequences share may be read, but must not be written by both.
+ * k, v: DEVICE, row i of head h at i * row stride + h * head stride (elements), contiguous channels, any alignment of the type.
+ * write takes bf16 or fp16 (16BIT: the cache's dtype) and finite values; read gives any of the three types. */
+typedef struct kq_cache_rows {
+    int64_t rows;
+    int sequences;
+    const int32_t *table;
+    int64_t table_stride;
+    int table_width;
+    const int32_t *offsets, *starts;
+    int dtype;
+    void *k, *v;
+    int64_t k_row_stride, k_head_stride, v_row_stride, v_head_stride;
+} kq_cache_rows_t;
+
+/* One launch each.  Errors: KQ_ERR_NULL, KQ_ERR_SHAPE, KQ_ERR_ALIGN, KQ_ERR_UNSUPPORTED (format, type), KQ_ERR_CUDA. */
+kq_status_t kroquant_cache_write(const kq_cache_t *cache, const kq_cache_rows_t *rows, void *stream);
+kq_status_t kroquant_cache_read(const kq_cache_t *cache, const kq_cache_rows_t *rows, void *stream);
+
+/* Attention of one new token of every sequence over its part of the cache:
+ *     out[s][h] = sum_t w_t v_t,   w = softmax over t of  scale * q[s][h] . k_t,     k, v of head h / (q_heads / heads)
+ * over the positions max(0, lengths[s] - window) <= t < lengths[s] (window 0: all) that have a place in the cache.  A row without
+ * any gives zeros (and lse -inf).  lse (optional): float [sequences][q_heads], the natural logarithm of the sum of exponentials.
+ * q and out: strides in elements, contiguous channels, any alignment; q bf16 or fp16 (16BIT: the cache's dtype), out any type.
+ * q_heads a multiple of the cache's heads; lengths: DEVICE int32, read on the device, clamped to [0, table_width * page_size], which is
+ * at most 2^30.
+ * Products are formed on the tensor cores from the cache's own values (q as it is; the weights w to 11 bits or more), sums and
+ * softmax statistics are 32-bit.  The work is split over the length and joined in a fixed order: same bits every time.
+ * scratch: DEVICE, 16-byte aligned, kroquant_cache_attention_scratch_bytes(...) bytes (0: may be NULL), contents irrelevant; two
+ * calls that may overlap need one each. */
+typedef struct kq_attention_args {
+    int sequences, q_heads;
+    int q_dtype, out_dtype;              /* kq_dtype_t */
+    const void *q;
+    void *out;
+    int64_t q_row_stride, q_head_stride, out_row_stride, out_head_stride;
+    const int32_t *table;
+    int64_t table_stride;
+    int table_width;
+    const int32_t *lengths;              /* DEVICE [sequences] */
+    int window;
+    float scale;
+    float *lse;
+} kq_attention_args_t;
+
+int64_t kroquant_cache_attention_scratch_bytes(const kq_cache_t *cache, const kq_attention_args_t *args);
+kq_status_t kroquant_cache_attention(const kq_cache_t *cache, const kq_attention_args_t *args, void *scratch, int64_t scratch_bytes,
+                                     void *stream);
+
+/* kroquant_linear_mxfp4 with the rows of A left in 16 bits (x: DEVICE [M] rows of ld_x elements, bf16 or fp16, any alignment) instead of
+ * quantized: the weight is the same (codes and tiled scales, 16-byte aligned), and so are the epilogue and out.  For few rows, where
+ * reading the weight is the cost and 4-bit activations would save nothing: 1 <= M <= 64.  Products of the weight's values with x
+ * (x to 11 significant bits within 128 channels, which holds both types), fp32 sums, one rounding.  One launch. */
+kq_status_t kroquant_linear_w4a16(const void *x, kq_xdtype_t x_dtype, int64_t ld_x, const uint8_t *b_codes, const uint8_t *b_scales,
+                                  int64_t M, int N, int K, const kq_epilogue_t *epilogue, void *out, kq_dtype_t out_dtype,
+                                  int64_t ld_out, void *stream);
+
 /* ---- Layer-wise calibration of the transform (Section 3.3; set-up of Appendix D) ----
  *
  * Minimises, over the parameters theta = (a_k, b_k, c_k), k = 1..5, of every factor set,

@@ -40,6 +40,8 @@ EXPORTS = [
     "kroquant_block_grad_scratch_bytes", "kroquant_block_grad", "kroquant_block_grad_static",
     "kroquant_calib_set_gemm_variant", "kroquant_gemm_mxfp4_variant", "kroquant_gemm_bf16_variant", "kroquant_calib_get_weight_factors", "kroquant_gemm_mxfp4",
     "kroquant_linear_w4a4", "kroquant_gemm_bf16",
+    "kroquant_rotary_args_default", "kroquant_rotary", "kroquant_cache_write", "kroquant_cache_read",
+    "kroquant_cache_attention_scratch_bytes", "kroquant_cache_attention", "kroquant_linear_w4a16",
 ]
 
 
@@ -128,6 +130,15 @@ def load_library() -> C.CDLL:
     L.kroquant_norm_residual_grad_scratch_bytes.argtypes = [vp]
     L.kroquant_norm_residual_grad_scratch_bytes.restype = i64
     L.kroquant_norm_residual_grad.argtypes = [vp, vp, i64, vp]
+    L.kroquant_rotary_args_default.argtypes = [vp]
+    L.kroquant_rotary_args_default.restype = None
+    L.kroquant_rotary.argtypes = [vp, vp]
+    L.kroquant_cache_write.argtypes = [vp, vp, vp]
+    L.kroquant_cache_read.argtypes = [vp, vp, vp]
+    L.kroquant_cache_attention_scratch_bytes.argtypes = [vp, vp]
+    L.kroquant_cache_attention_scratch_bytes.restype = i64
+    L.kroquant_cache_attention.argtypes = [vp, vp, vp, i64, vp]
+    L.kroquant_linear_w4a16.argtypes = [vp, i32, i64, vp, vp, i64, i32, i32, vp, vp, i32, i64, vp]
     _lib = L
     return L
 
@@ -595,6 +606,22 @@ class LinearW4A4:
         kroquant_quantize(X, self.factors, q, s, stream=handle, scale_layout="tiled")
         return kroquant_linear_mxfp4(q, s, self.w_codes, self.w_scales, stream=stream, **epilogue)
 
+    def few(self, X: torch.Tensor, *, stream=None, **epilogue) -> torch.Tensor:
+        """The layer for a few rows (at most 64) whose activations are transformed but not quantized: X T in X's own type
+        (:func:`kroquant_quantize_dual`), then :func:`kroquant_linear_w4a16` with the keyword arguments given here.  Two launches."""
+        tokens, d = _x_shape(X)
+        if d != self.d:
+            raise ValueError("X [tokens, d] does not match the weights")
+        if tokens > 64:
+            raise ValueError("X has more than 64 rows: use fused")
+        handle = _stream(stream)
+        q, s = self._buffers(tokens, X.device, stream, handle)
+        q, s = q[:tokens], s[:tiled_scale_bytes(tokens, d)]
+        with _allocating(stream):
+            turned = torch.empty_like(X)
+        kroquant_quantize_dual(X, self.factors, q, s, turned, stream=handle, scale_layout="tiled")
+        return kroquant_linear_w4a16(turned, self.w_codes, self.w_scales, stream=stream, **epilogue)
+
 
 # ---- the transformer block around the W4A4 product -----------------------------------------------------------------
 ACTIVATIONS = {"none": 0, "relu": 1, "silu": 2, "gelu": 3, "gelu_tanh": 4}
@@ -644,16 +671,20 @@ def _rows2d(t: torch.Tensor, shape, what: str) -> int:
 
 
 def _linear(a_codes, a_scales, b_codes, b_scales, offsets, features, bias, activation, glu, gate, rows_per_gate, row_scale,
-            residual, residual_scale, out, out_dtype, stream):
+            residual, residual_scale, out, out_dtype, stream, ld_x=None):
     dev = _device()
-    for t in (a_codes, a_scales, b_codes, b_scales):
+    b_shape, grouped, quantized = b_codes.shape, offsets is not None, ld_x is None
+    for t in (a_codes, a_scales, b_codes, b_scales) if quantized else (b_codes, b_scales):
         if t.dtype is not torch.uint8 or t.get_device() != dev or not t.is_contiguous():
             raise ValueError("codes and scales must be contiguous uint8 tensors on the current CUDA device")
-    a_shape, b_shape, grouped = a_codes.shape, b_codes.shape, offsets is not None
-    if len(a_shape) != 2 or len(b_shape) != (3 if grouped else 2) or b_shape[-1] != a_shape[1]:
-        raise ValueError("A is [M, K/2] codes, B [rows, K/2] ([experts, rows, K/2] in the grouped call) with the same K")
-    M, K, R, experts = a_shape[0], 2 * a_shape[1], b_shape[-2], b_shape[0] if grouped else 1
-    if a_scales.numel() != tiled_scale_bytes(M, K) or b_scales.numel() != experts * tiled_scale_bytes(R, K):
+    M, K = a_codes.shape if a_codes.dim() == 2 else (0, -1)
+    if quantized:
+        K *= 2
+    if K < 0 or len(b_shape) != (3 if grouped else 2) or 2 * b_shape[-1] != K:
+        raise ValueError("A is [M, K/2] codes, B [rows, K/2] ([experts, rows, K/2] in the grouped call) with the same K" if quantized else
+                         "x is [M, K], B [rows, K/2] codes with the same K")
+    R, experts = b_shape[-2], b_shape[0] if grouped else 1
+    if (quantized and a_scales.numel() != tiled_scale_bytes(M, K)) or b_scales.numel() != experts * tiled_scale_bytes(R, K):
         raise ValueError("scales must be in the tiled layout (tiled_scale_bytes(rows, K) bytes, per expert for B)")
     N = (R // 2 if glu else R) if features is None else features
     if R != (64 * ((N + 31) // 32) if glu else N):
@@ -703,12 +734,16 @@ def _linear(a_codes, a_scales, b_codes, b_scales, offsets, features, bias, activ
         rc = load_library().kroquant_linear_mxfp4_grouped(
             a_codes.data_ptr(), a_scales.data_ptr(), b_codes.data_ptr(), b_scales.data_ptr(), offsets.data_ptr(), experts, M, N, K,
             C.addressof(e), out.data_ptr(), _DTYPES[out.dtype], ld_out, _stream(stream))
-    else:
+    elif quantized:
         rc = load_library().kroquant_linear_mxfp4(
             a_codes.data_ptr(), a_scales.data_ptr(), b_codes.data_ptr(), b_scales.data_ptr(), M, N, K, C.addressof(e), out.data_ptr(),
             _DTYPES[out.dtype], ld_out, _stream(stream))
+    else:
+        rc = load_library().kroquant_linear_w4a16(
+            a_codes.data_ptr(), X_DTYPES[a_codes.dtype], ld_x, b_codes.data_ptr(), b_scales.data_ptr(), M, N, K, C.addressof(e), out.data_ptr(),
+            _DTYPES[out.dtype], ld_out, _stream(stream))
     if rc:
-        raise KroQuantError(rc, "kroquant_linear_mxfp4_grouped" if grouped else "kroquant_linear_mxfp4")
+        raise KroQuantError(rc, "kroquant_linear_mxfp4_grouped" if grouped else "kroquant_linear_mxfp4" if quantized else "kroquant_linear_w4a16")
     return out
 
 
@@ -745,6 +780,25 @@ def kroquant_linear_mxfp4_grouped(a_codes: torch.Tensor, a_scales: torch.Tensor,
         raise ValueError("offsets must be a contiguous CUDA int32 tensor [experts + 1]")
     return _linear(a_codes, a_scales, b_codes, b_scales, offsets, features, bias, activation, glu, None, None, row_scale, residual,
                    residual_scale, out, out_dtype, stream)
+
+
+def kroquant_linear_w4a16(x: torch.Tensor, b_codes: torch.Tensor, b_scales: torch.Tensor, *, features: Optional[int] = None,
+                          bias: Optional[torch.Tensor] = None, activation: str = "none", glu: bool = False,
+                          gate: Optional[torch.Tensor] = None, rows_per_gate: Optional[int] = None,
+                          row_scale: Optional[torch.Tensor] = None, residual: Optional[torch.Tensor] = None,
+                          residual_scale: float = 1.0, out: Optional[torch.Tensor] = None, out_dtype=torch.bfloat16,
+                          stream=None) -> torch.Tensor:
+    """:func:`kroquant_linear_mxfp4` with rows that stay in 16 bits: x [M, K] bfloat16 or float16 (a row pitch is allowed),
+    1 <= M <= 64, the weight and the keyword arguments as there.  For a few rows (a decode step, a conditioning vector)
+    it reads what the quantized form reads and keeps the activations' digits."""
+    if x.dtype not in X_DTYPES:
+        raise ValueError("x must be bfloat16 or float16")
+    if x.dim() != 2:
+        raise ValueError("x must be [M, K]")
+    if x.shape[0] > 64:
+        raise ValueError("x has more than 64 rows: quantize it and use kroquant_linear_mxfp4")
+    return _linear(x, None, b_codes, b_scales, None, features, bias, activation, glu, gate, rows_per_gate, row_scale, residual,
+                   residual_scale, out, out_dtype, stream, _rows2d(x, x.shape, "x"))
 
 
 def _norm_args(rows: int, d: int, norm: str, post_norm: str, residual_scale: float, eps: float, rows_per_batch, gate, post_weight,
@@ -910,6 +964,312 @@ def kroquant_norm_residual_grad(dn: Optional[torch.Tensor], h: torch.Tensor, *, 
     if rc:
         raise KroQuantError(rc, "kroquant_norm_residual_grad")
     return out
+
+
+# ---- one step over new tokens: positions, the cache of keys and values, attention --------------------------------------
+ROTARY_LAYOUTS = {"interleaved": 0, "half": 1}
+CACHE_FORMATS = {"16bit": 0, "mxfp8": 1, "mxfp4": 2}
+
+
+class _RotaryArgs(C.Structure):
+    """kq_rotary_args_t (include/kroquant.h); arrays of two are two fields."""
+    _fields_ = ([("dtype", C.c_int), ("batches", C.c_int64), ("tokens", C.c_int64)] +
+                [(n, C.c_int) for n in ("head_dim", "layout", "inverse", "axes", "axis0", "axis1", "axis2", "axis3")] +
+                [("frequencies", C.c_void_p), ("positions", C.c_void_p), ("positions_f32", C.c_int),
+                 ("position_batch_stride", C.c_int64), ("position_token_stride", C.c_int64)] +
+                [(n, C.c_void_p) for n in ("x0", "x1", "out0", "out1")] + [("heads0", C.c_int), ("heads1", C.c_int)] +
+                [(n + i, C.c_int64) for n in ("x_batch_stride", "x_token_stride", "x_head_stride", "out_batch_stride", "out_token_stride",
+                                              "out_head_stride") for i in "01"])
+
+
+class _Cache(C.Structure):
+    """kq_cache_t (include/kroquant.h)."""
+    _fields_ = ([("format", C.c_int), ("dtype", C.c_int), ("pages", C.c_int64)] + [(n, C.c_int) for n in ("page_size", "heads", "head_dim")] +
+                [(n, C.c_void_p) for n in ("k", "v", "k_scales", "v_scales")])
+
+
+class _CacheRows(C.Structure):
+    """kq_cache_rows_t (include/kroquant.h)."""
+    _fields_ = [("rows", C.c_int64), ("sequences", C.c_int), ("table", C.c_void_p), ("table_stride", C.c_int64), ("table_width", C.c_int),
+                ("offsets", C.c_void_p), ("starts", C.c_void_p), ("dtype", C.c_int), ("k", C.c_void_p), ("v", C.c_void_p),
+                ("k_row_stride", C.c_int64), ("k_head_stride", C.c_int64), ("v_row_stride", C.c_int64), ("v_head_stride", C.c_int64)]
+
+
+class _AttentionArgs(C.Structure):
+    """kq_attention_args_t (include/kroquant.h)."""
+    _fields_ = ([(n, C.c_int) for n in ("sequences", "q_heads", "q_dtype", "out_dtype")] + [("q", C.c_void_p), ("out", C.c_void_p)] +
+                [(n, C.c_int64) for n in ("q_row_stride", "q_head_stride", "out_row_stride", "out_head_stride")] +
+                [("table", C.c_void_p), ("table_stride", C.c_int64), ("table_width", C.c_int), ("lengths", C.c_void_p), ("window", C.c_int),
+                 ("scale", C.c_float), ("lse", C.c_void_p)])
+
+
+def rotary_frequencies(axes, theta: float = 10000.0, device="cuda") -> torch.Tensor:
+    """float64 [sum(axes) / 2]: theta ** (-2 i / a) for the a / 2 pairs of every axis of a channels."""
+    return torch.cat([theta ** (-torch.arange(0, a, 2, dtype=torch.float64) / a) for a in axes]).to(device)
+
+
+def _apart(t: torch.Tensor) -> bool:
+    """Whether the elements of t lie at different addresses."""
+    if t.is_contiguous():
+        return True
+    reach = 1
+    for size, stride in sorted(((n, s) for n, s in zip(t.shape, t.stride()) if n > 1), key=lambda p: p[1]):
+        if stride < reach:
+            return False
+        reach = stride * (size - 1) + reach
+    return True
+
+
+def _span(t: torch.Tensor):
+    """First byte of t and the one behind its last."""
+    base = t.data_ptr()
+    return base, base + t.element_size() * (1 + sum((n - 1) * s for n, s in zip(t.shape, t.stride()))) if t.numel() else base
+
+
+def _heads_last(t: torch.Tensor, what: str, dims: int, dtypes=_DTYPES) -> None:
+    if t.dim() != dims or t.dtype not in dtypes or t.get_device() != _device() or (t.shape[-1] > 1 and t.stride(-1) != 1):
+        raise ValueError(f"{what} must be a {dims}-D CUDA tensor of {', '.join(str(d)[6:] for d in dtypes)} on the current device with contiguous channels")
+
+
+def kroquant_rotary(q: torch.Tensor, k: Optional[torch.Tensor], positions: torch.Tensor, frequencies: torch.Tensor, *, axes=None,
+                    layout: str = "interleaved", inverse: bool = False, out=None, stream=None):
+    """Rotary positions: -> q turned, or (q, k) turned where k is given.
+
+    q, k: [tokens, heads, d] or [batch, tokens, heads, d] of one dtype, each with its own number of heads, any strides with
+    contiguous channels.  positions: int32 or float32 [tokens, axes] ([tokens] for one axis; [batch, tokens, axes] per sample).
+    axes: channels of each axis (time, height, width, ...; up to four, each even), by default one axis of all the frequencies'
+    pairs; frequencies: float64 [sum(axes) / 2] (:func:`rotary_frequencies`).  Pair p of axis i turns by
+    positions[t, i] * frequencies[p], formed in 64 bits; channels behind the axes are copied.  layout: "interleaved" pairs
+    (2p, 2p + 1) or "half" (p, p + pairs).  inverse turns back: the backward pass, with the gradients in place of q and k.
+    out: tensor, or pair of tensors with k, to write to; each may be its input."""
+    dims = q.dim()
+    if dims not in (3, 4):
+        raise ValueError("q must be [tokens, heads, d] or [batch, tokens, heads, d]")
+    _heads_last(q, "q", dims)
+    shape, dtype, dev = q.shape, q.dtype, q.get_device()
+    d, tokens, batches = shape[-1], shape[-3], shape[0] if dims == 4 else 1
+    if k is not None:
+        _heads_last(k, "k", dims)
+        if k.dtype is not dtype or k.shape[-1] != d or k.shape[:-2] != shape[:-2]:
+            raise ValueError("k must have q's dtype and shape but for the number of heads")
+    if frequencies.dtype is not torch.float64 or frequencies.dim() != 1 or frequencies.get_device() != dev or not frequencies.is_contiguous():
+        raise ValueError("frequencies must be a contiguous CUDA float64 tensor [pairs]")
+    pairs = frequencies.shape[0]
+    axes = (2 * pairs,) if axes is None else tuple(axes)
+    n = len(axes)
+    if not 1 <= n <= 4 or any(a < 0 or a % 2 for a in axes) or sum(axes) != 2 * pairs or not 0 < 2 * pairs <= d:
+        raise ValueError("axes: one to four even numbers of channels, together twice the frequencies and at most d")
+    way = ROTARY_LAYOUTS.get(layout)
+    if way is None:
+        raise ValueError(f"layout must be one of {sorted(ROTARY_LAYOUTS)}")
+    if positions.dtype not in (torch.int32, torch.float32) or positions.get_device() != dev:
+        raise ValueError("positions must be a CUDA int32 or float32 tensor")
+    if n == 1 and positions.dim() == 1:
+        positions = positions.unsqueeze(1)
+    if positions.shape != (tokens, n) and (dims != 4 or positions.shape != (batches, tokens, n)) or (n > 1 and positions.stride(-1) != 1):
+        raise ValueError("positions must be [tokens, axes], or [batch, tokens, axes], with contiguous axes")
+    outs = (None, None) if out is None else (out, None) if k is None else tuple(out)
+    made = []
+    for x, o in ((q, outs[0]), (k, outs[1])):
+        if x is None:
+            continue
+        if o is None:
+            o = _empty_rows(x, dtype, stream)
+        else:
+            _heads_last(o, "out", dims)
+            if o.shape != x.shape or o.dtype is not dtype or not _apart(o):
+                raise ValueError("out must have its input's shape and dtype, and elements of their own")
+            (a0, a1), (b0, b1) = _span(o), _span(x)
+            if a0 < b1 and b0 < a1 and (a0 != b0 or o.stride() != x.stride()):
+                raise ValueError("out may be its input, but must not overlap it in another way")
+        made.append(o)
+
+    def strides(t):
+        s = t.stride()
+        return (0, s[0], s[1]) if dims == 3 else s[:3]
+
+    xs, os = strides(q), strides(made[0])
+    if k is None:
+        second, ks, ko = (None, None, 0), (0, 0, 0), (0, 0, 0)
+    else:
+        second, ks, ko = (k.data_ptr(), made[1].data_ptr(), k.shape[-2]), strides(k), strides(made[1])
+    ps = positions.stride()
+    a = _RotaryArgs(_DTYPES[dtype], batches, tokens, d, way, 1 if inverse else 0, n, *axes, *(0,) * (4 - n), frequencies.data_ptr(),
+                    positions.data_ptr(), 1 if positions.dtype is torch.float32 else 0, ps[0] if len(ps) == 3 else 0, ps[-2],
+                    q.data_ptr(), second[0], made[0].data_ptr(), second[1], shape[-2], second[2], xs[0], ks[0], xs[1], ks[1], xs[2], ks[2],
+                    os[0], ko[0], os[1], ko[1], os[2], ko[2])
+    rc = load_library().kroquant_rotary(C.addressof(a), _stream(stream))
+    if rc:
+        raise KroQuantError(rc, "kroquant_rotary")
+    return made[0] if k is None else (made[0], made[1])
+
+
+class KVCache:
+    """A paged cache of keys and values (kq_cache_t): `pages` pages of `page_size` positions for `heads` heads of head_dim channels,
+    as they are ("16bit") or in MXFP8 or MXFP4.  The buffers are torch tensors: k, v [pages, heads, page_size, row] (16-bit values of
+    `dtype`, or uint8 codes) and for the codes k_scales, v_scales uint8 [pages, heads, page_size, scale row]; a row has
+    32 * ceil(head_dim / 32) channels, those behind head_dim zero.  dtype is what :func:`kroquant_cache_read` gives unless asked
+    for another.  Which pages belong to which sequence is the caller's table."""
+
+    def __init__(self, k: torch.Tensor, v: torch.Tensor, k_scales: Optional[torch.Tensor] = None, v_scales: Optional[torch.Tensor] = None, *,
+                 head_dim: int, format: str = "mxfp4", dtype=None):
+        code = CACHE_FORMATS.get(format)
+        if code is None:
+            raise ValueError(f"format must be one of {sorted(CACHE_FORMATS)}")
+        if not 1 <= head_dim <= 256:
+            raise ValueError("head_dim must be in 1 .. 256")
+        channels = 32 * ((head_dim + 31) // 32)
+        row = channels if code < 2 else channels // 2
+        if k.dim() != 4 or k.shape[-1] != row or v.shape != k.shape or v.dtype is not k.dtype or min(k.shape) < 1:
+            raise ValueError(f"k and v must be [pages, heads, page_size, {row}]")
+        if k.dtype is not torch.uint8 if code else k.dtype not in X_DTYPES:
+            raise ValueError("k and v must be uint8 codes" if code else "k and v must be bfloat16 or float16")
+        if code == 0:
+            if dtype not in (None, k.dtype) or k_scales is not None or v_scales is not None:
+                raise ValueError("a 16bit cache has its buffers' dtype and no scales")
+            dtype = k.dtype
+        else:
+            dtype = torch.bfloat16 if dtype is None else dtype
+            if dtype not in X_DTYPES:
+                raise ValueError("dtype must be bfloat16 or float16")
+            scales = tuple(k.shape[:3]) + (4 * ((channels + 127) // 128),)
+            for t in (k_scales, v_scales):
+                if t is None or t.dtype is not torch.uint8 or tuple(t.shape) != scales:
+                    raise ValueError(f"k_scales and v_scales must be uint8 {list(scales)}")
+        for t in (k, v) if code == 0 else (k, v, k_scales, v_scales):
+            if not t.is_contiguous() or t.get_device() != k.get_device():
+                raise ValueError("the cache's buffers must be contiguous tensors on one device")
+        self.k, self.v, self.k_scales, self.v_scales = k, v, k_scales, v_scales
+        self.format, self.dtype, self.head_dim, self.device = format, dtype, head_dim, k.device
+        self.pages, self.heads, self.page_size = k.shape[0], k.shape[1], k.shape[2]
+        self._device, self._c = k.get_device(), _Cache(code, _DTYPES[dtype], k.shape[0], k.shape[2], k.shape[1], head_dim, k.data_ptr(), v.data_ptr(),
+                                                       None if code == 0 else k_scales.data_ptr(), None if code == 0 else v_scales.data_ptr())
+        self._at = C.addressof(self._c)
+
+    @classmethod
+    def empty(cls, pages: int, page_size: int, heads: int, head_dim: int, format: str = "mxfp4", dtype=torch.bfloat16, device="cuda") -> "KVCache":
+        """A cache of zeros."""
+        if format not in CACHE_FORMATS:
+            raise ValueError(f"format must be one of {sorted(CACHE_FORMATS)}")
+        channels, make = 32 * ((head_dim + 31) // 32), lambda row, dt: torch.zeros((pages, heads, page_size, row), dtype=dt, device=device)
+        if format == "16bit":
+            return cls(make(channels, dtype), make(channels, dtype), head_dim=head_dim, format=format)
+        row, scales = channels if format == "mxfp8" else channels // 2, 4 * ((channels + 127) // 128)
+        return cls(make(row, torch.uint8), make(row, torch.uint8), make(scales, torch.uint8), make(scales, torch.uint8), head_dim=head_dim,
+                   format=format, dtype=dtype)
+
+
+def _int_vector(t: torch.Tensor, size: int, dev: int, what: str) -> int:
+    if t.dtype is not torch.int32 or t.shape != (size,) or t.get_device() != dev or not t.is_contiguous():
+        raise ValueError(f"{what} must be a contiguous int32 tensor [{size}] on the cache's device")
+    return t.data_ptr()
+
+
+def _table(cache: KVCache, table: torch.Tensor):
+    """(sequences, pointer, stride, width) of a table of pages, on the cache's device, which must be the current one."""
+    if cache._device != _device():
+        raise ValueError("the cache is not on the current CUDA device")
+    if table.dtype is not torch.int32 or table.dim() != 2 or table.get_device() != cache._device or \
+            (table.shape[1] > 1 and table.stride(1) != 1) or (table.shape[0] > 1 and table.stride(0) < 0):
+        raise ValueError("table must be an int32 tensor [sequences, pages of a sequence] on the cache's device with contiguous rows")
+    return table.shape[0], table.data_ptr(), table.stride(0), table.shape[1]
+
+
+def _cache_rows(call: str, cache: KVCache, k, v, rows, where, offsets, starts, stream) -> None:
+    n, table, stride, width = where
+    a = _CacheRows(rows, n, table, stride, width, None if offsets is None else _int_vector(offsets, n + 1, cache._device, "offsets"),
+                   None if starts is None else _int_vector(starts, n, cache._device, "starts"), _DTYPES[k.dtype], k.data_ptr(), v.data_ptr(),
+                   k.stride(0), k.stride(1), v.stride(0), v.stride(1))
+    rc = getattr(load_library(), call)(cache._at, C.addressof(a), _stream(stream))
+    if rc:
+        raise KroQuantError(rc, call)
+
+
+def kroquant_cache_write(cache: KVCache, k: torch.Tensor, v: torch.Tensor, table: torch.Tensor, *, offsets: Optional[torch.Tensor] = None,
+                         starts: Optional[torch.Tensor] = None, stream=None) -> None:
+    """Keys and values of new tokens into the cache, encoded as it holds them.  k, v [rows, heads, head_dim] bfloat16 or float16 (a 16bit
+    cache: its dtype), any strides with contiguous channels.  table int32 [sequences, n]: the pages of each sequence in order.
+    offsets int32 [sequences + 1]: rows offsets[s] .. offsets[s + 1] - 1 belong to sequence s (None: one row per sequence); starts
+    int32 [sequences]: the position of each sequence's first row (None: 0).  All three are read on the device; a row whose
+    position lies before 0 or beyond the table, or whose table entry is no page (-1, say), is left out."""
+    where = _table(cache, table)
+    _heads_last(k, "k", 3, X_DTYPES)
+    _heads_last(v, "v", 3, X_DTYPES)
+    shape = (k.shape[0], cache.heads, cache.head_dim)
+    if k.shape != shape or v.shape != shape or v.dtype is not k.dtype or (cache.format == "16bit" and k.dtype is not cache.dtype):
+        raise ValueError("k and v must be [rows, heads, head_dim] of the cache, of one dtype (a 16bit cache: its own)")
+    if offsets is None and shape[0] != where[0]:
+        raise ValueError("without offsets there is one row per sequence")
+    _cache_rows("kroquant_cache_write", cache, k, v, shape[0], where, offsets, starts, stream)
+
+
+def kroquant_cache_read(cache: KVCache, table: torch.Tensor, rows: int, *, offsets: Optional[torch.Tensor] = None,
+                        starts: Optional[torch.Tensor] = None, dtype=None, out=None, stream=None):
+    """The inverse of :func:`kroquant_cache_write`: -> (k, v) [rows, heads, head_dim] in `dtype` (default: the cache's; float32 is allowed), the
+    values that the cache holds at the places of the rows.  Rows without a place are zeros; rows outside the sequences
+    (before offsets[0], from offsets[-1] on) are left as they are.  out: a pair of tensors to write to."""
+    where = _table(cache, table)
+    shape = (rows, cache.heads, cache.head_dim)
+    if out is None:
+        dtype = cache.dtype if dtype is None else dtype
+        if dtype not in _DTYPES:
+            raise ValueError("dtype must be float32, bfloat16 or float16")
+        with _allocating(stream):
+            k, v = torch.empty(shape, dtype=dtype, device=cache.device), torch.empty(shape, dtype=dtype, device=cache.device)
+    else:
+        k, v = out
+        for t in (k, v):
+            _heads_last(t, "out", 3)
+            if t.shape != shape or t.dtype is not k.dtype or dtype not in (None, t.dtype) or not _apart(t):
+                raise ValueError("out must be two tensors [rows, heads, head_dim] of one dtype with elements of their own")
+    if offsets is None and rows != where[0]:
+        raise ValueError("without offsets there is one row per sequence")
+    _cache_rows("kroquant_cache_read", cache, k, v, rows, where, offsets, starts, stream)
+    return k, v
+
+
+def kroquant_cache_attention(q: torch.Tensor, cache: KVCache, table: torch.Tensor, lengths: torch.Tensor, *, scale: Optional[float] = None,
+                             window: int = 0, out: Optional[torch.Tensor] = None, out_dtype=None, lse: bool = False, stream=None):
+    """Attention of one new token of every sequence over its pages: -> out [sequences, q_heads, head_dim], softmax(scale q K^T) V
+    over positions max(0, lengths - window) .. lengths - 1 (window 0: from 0); with lse also the float32 [sequences, q_heads]
+    logarithms of the sums of exponentials.  q [sequences, q_heads, head_dim] bfloat16 or float16 (a 16bit cache: its dtype),
+    q_heads a multiple of the cache's heads: query head h reads cache head h // (q_heads / heads).  scale: default
+    head_dim ** -0.5.  lengths int32 [sequences] counts the new token, written before; it is read on the device.  A sequence
+    without positions (length 0, no pages) gives zeros and -inf.  out_dtype: default q's."""
+    where = _table(cache, table)
+    _heads_last(q, "q", 3, X_DTYPES)
+    n, heads, d = q.shape
+    if n != where[0] or d != cache.head_dim or heads < 1 or heads % cache.heads or (cache.format == "16bit" and q.dtype is not cache.dtype):
+        raise ValueError("q must be [sequences, q_heads, head_dim], q_heads a multiple of the cache's heads (a 16bit cache: its dtype)")
+    if window < 0:
+        raise ValueError("window must not be negative")
+    if out is None:
+        out_dtype = q.dtype if out_dtype is None else out_dtype
+        if out_dtype not in _DTYPES:
+            raise ValueError("out_dtype must be float32, bfloat16 or float16")
+        out = _empty_rows(q, out_dtype, stream)
+    else:
+        _heads_last(out, "out", 3)
+        if out.shape != q.shape or out_dtype not in (None, out.dtype) or not _apart(out):
+            raise ValueError("out must have q's shape and elements of its own")
+    lib = load_library()
+    a = _AttentionArgs(n, heads, _DTYPES[q.dtype], _DTYPES[out.dtype], q.data_ptr(), out.data_ptr(), q.stride(0), q.stride(1), out.stride(0),
+                       out.stride(1), where[1], where[2], where[3], _int_vector(lengths, n, cache._device, "lengths"), min(window, 0x7FFFFFFF),
+                       d ** -0.5 if scale is None else scale, None)
+    at = C.addressof(a)
+    nbytes = lib.kroquant_cache_attention_scratch_bytes(cache._at, at)
+    logs = scratch = None
+    if lse or nbytes:
+        with _allocating(stream):
+            if lse:
+                logs = torch.empty((n, heads), dtype=torch.float32, device=q.device)
+                a.lse = logs.data_ptr()
+            if nbytes:
+                scratch = torch.empty(nbytes, dtype=torch.uint8, device=q.device)
+    rc = lib.kroquant_cache_attention(cache._at, at, None if scratch is None else scratch.data_ptr(), nbytes, _stream(stream))
+    if rc:
+        raise KroQuantError(rc, "kroquant_cache_attention")
+    return (out, logs) if lse else out
 
 
 _GEMM_PAIR = True

@@ -12,8 +12,8 @@ import sys
 PKG = os.path.dirname(os.path.abspath(__file__))
 CSRC = os.path.join(PKG, "csrc")
 LIB = os.path.join(PKG, "libkroquant.so")
-SOURCES = [os.path.join(CSRC, "kroquant_api.cu")]
-HEADERS = [os.path.join(CSRC, n) for n in ("kq_common.cuh", "kq_stream.cuh", "kq_umma.cuh", "kq_gemm.cuh", "kq_gemm2.cuh", "kq_gemm_fp4.cuh", "kq_gemm_fp4_pair.cuh", "kq_calib.cuh",
+SOURCES = [os.path.join(CSRC, n) for n in ("kroquant_api.cu", "kroquant_decode.cu")]
+HEADERS = [os.path.join(CSRC, n) for n in ("kq_common.cuh", "kq_host.cuh", "kq_mma16.cuh", "kq_rotary.cuh", "kq_cache.cuh", "kq_cache_attention.cuh", "kq_linear_w4a16.cuh", "kq_stream.cuh", "kq_umma.cuh", "kq_gemm.cuh", "kq_gemm2.cuh", "kq_gemm_fp4.cuh", "kq_gemm_fp4_pair.cuh", "kq_calib.cuh",
                                                "kq_norm.cuh", "kq_linear.cuh", "kroquant_calib_api.cuh", "kroquant_block_api.cuh")] + [
     os.path.join(os.path.dirname(PKG), "include", "kroquant.h")]
 
@@ -22,6 +22,7 @@ NVCC_FLAGS = [
     "-gencode", "arch=compute_100a,code=sm_100a",
     "-shared", "-Xcompiler", "-fPIC",
     "-Xptxas", "-v",
+    "-t", "2",                               # the two sources side by side
 ]
 
 

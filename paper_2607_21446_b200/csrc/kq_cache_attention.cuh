@@ -1,0 +1,767 @@
+// Attention of one new token per sequence over the paged cache, sm_100a:
+//     out[s][h] = sum_t w_t v_t / sum_t w_t,    w_t = exp(scale q[s][h] . k_t - m),   m the largest score so far
+// One pass over the positions with a running maximum and sum: when m grows, the sum and the accumulated values are scaled down.
+//
+// The cache is read once, by 4 warps of a CTA that each take every fourth step of 16 (16-bit) or 32 positions, with rings of their own
+// in shared memory (cp.async; no barrier between the warps until the end of a segment).  A warp multiplies with mma.sync, positions
+// as the 16 rows of the product and the query heads of one cache head as its 8 (or twice 8) columns:
+//     S^T [position][query] = K Q^T,     O^T [channel][query] += V^T P^T.
+// So nothing is padded to 128 rows, and codes go from shared memory through the converter into the operand registers, never back: an
+// operand for tcgen05 would have to be written to shared memory again.  What limits is memory (16 bit, MXFP8) and the converter's issue (MXFP4).
+//
+// Operand order.  Any order of channels serves K Q^T, and any order of positions P^T as long as both products use the same, so that a
+// lane takes what lies together: of K, with j = lane % 4, whole 16-byte chunks of the rows of positions lane / 4 and lane / 4 + 8; of V,
+// with g = lane / 4, D/8 consecutive channels of four positions.  P^T is S^T with rows and columns of 8 x 8 blocks exchanged (movmatrix).
+// Chunks are stored permuted within a row so that both kinds of access take all banks.
+//
+// Scales.  A code times 2^(S - 127) would leave fp16, so K is taken relative to the largest scale byte of its position (a factor of the
+// score, fp32) and V relative to the largest of its position, which goes into P: p 2^(S_t - R + 14), R the largest S_t so far (a
+// running maximum that rescales the accumulator as m does).  Code times 2^(S - S_t) has at most 4 significant bits, exact in fp16 down to
+// 2^-24: what falls below is 2^-25 of a code's unit.  Queries are fp16 times a power of two per row, exact for both 16-bit types up to
+// values 2^-29 of the row's largest.  P is rounded to fp16 (11 bits; a weight below 2^-28 of the largest keeps fewer, which is 2^-39 of the
+// largest value at most), with bf16 values to two bf16 terms (16 bits).
+//
+// Work.  Tiles (4 steps) of all (sequence, head) items are laid end to end and every CTA takes an equal run of them: ragged batches
+// balance, one long sequence fills the GPU.  An item that ends within its CTA is written; the parts of others go to the scratch
+// space (at most two per CTA) and a second kernel joins them in order.  Lengths are read on the device.
+#pragma once
+#include "kq_cache.cuh"
+#include "kq_mma16.cuh"
+
+namespace kq {
+
+enum { kAttnBf16 = 0, kAttnF16 = 1, kAttnFp8 = 2, kAttnFp4 = 3 };
+constexpr int kAttnWarps = 4;
+constexpr int kAttnThreads = 32 * kAttnWarps;
+
+struct AttentionProblem {
+    CacheRef c;
+    int sequences, q_heads, group, chunks;       // group: query heads of a cache head, taken in `chunks` runs
+    const void* q;
+    int q_f16;
+    int64_t q_row, q_head;
+    void* out;
+    int out_type;
+    int64_t out_row, out_head;
+    const int32_t* table;
+    int64_t table_stride;
+    int table_width;
+    const int32_t* lengths;
+    int window;
+    float scale_log2e;
+    float* lse;
+    float* partial;                      // [2 per CTA][NQ][D], then [2 per CTA][2][NQ]: maximum, sum.  null: items are taken whole
+    int ctas;                            // of the attention kernel
+    int min_tiles;                       // smallest run of a CTA
+};
+
+// Positions of a sequence that its token sees, and their tiles (at least one, so that an empty row is written).
+struct VisibleRange { int begin, end; };
+__device__ __forceinline__ VisibleRange visible_range(const AttentionProblem& p, int s) {
+    const int64_t room = (int64_t)p.table_width * p.c.page_size;
+    int n = __ldg(p.lengths + s);
+    n = n < 0 ? 0 : (n > room ? (int)room : n);
+    return {p.window > 0 && n > p.window ? n - p.window : 0, n};
+}
+template <int TN>
+__device__ __forceinline__ int tiles_of(const VisibleRange& v) {
+    const int n = v.end - v.begin;
+    return n <= TN ? 1 : (n - 1) / TN + 1;
+}
+// Tiles of an item of sequences 0 .. upto - 1, by one warp; upto < 0: of all.
+template <int TN>
+__device__ __forceinline__ int64_t tiles_before(const AttentionProblem& p, int upto, int lane) {
+    int64_t sum = 0;
+    for (int s = lane; s < upto; s += 32) sum += tiles_of<TN>(visible_range(p, s));
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1) sum += __shfl_xor_sync(0xFFFFFFFFu, sum, o);
+    return sum;
+}
+__device__ __forceinline__ int64_t run_length(const AttentionProblem& p, int64_t total) {
+    const int64_t even = (total + p.ctas - 1) / p.ctas;
+    return even < p.min_tiles ? p.min_tiles : even;
+}
+
+__device__ __forceinline__ float exp2_fast(float x) {
+    float y;
+    asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+    return y;
+}
+__device__ __forceinline__ uint32_t shared_u32(const void* p) { return (uint32_t)__cvta_generic_to_shared(p); }
+// N bytes (4, 8 or 16), zeros where `exists` does not hold
+template <int N>
+__device__ __forceinline__ void copy_async(uint32_t dst, const void* src, bool exists) {
+    if constexpr (N == 16)
+        asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst), "l"(src), "r"(exists ? 16 : 0) : "memory");
+    else
+        asm volatile("cp.async.ca.shared.global [%0], [%1], %3, %2;" ::"r"(dst), "l"(src), "r"(exists ? N : 0), "n"(N) : "memory");
+}
+
+template <int FMT, int D, int NQ>
+struct AttnShape {
+    static constexpr bool kCodes = FMT >= kAttnFp8;
+    static constexpr int kBits = FMT == kAttnFp4 ? 4 : (FMT == kAttnFp8 ? 8 : 16);
+    static constexpr int kStep = kCodes ? 32 : 16;               // positions of a step
+    static constexpr int kTile = kStep * kAttnWarps;
+    static constexpr int kRow = D * kBits / 8;                   // bytes of a row in shared memory
+    static constexpr int kChunks = kRow / 16;
+    static constexpr int kScaleRow = kCodes ? (D > 128 ? 8 : 4) : 0;
+    static constexpr int kScaleOff = 2 * kStep * kRow;
+    static constexpr int kMaskOff = kScaleOff + 2 * kStep * kScaleRow;
+    static constexpr int kStageBytes = kMaskOff + 16;
+    static constexpr int kStages = D > 128 && !kCodes ? 2 : 3;
+    static constexpr int kMulBytes = kCodes ? 2 * (D / 32) * kStep * 2 : 0;      // fp16 multipliers [K, V][block][position]
+    static constexpr int kRing = kStages * kStageBytes;
+    static constexpr int kWarpBytes = kRing + kMulBytes;
+    static constexpr int kJoinStride = D + 4;                    // floats
+    static constexpr int kJoinBytes = kAttnWarps * NQ * kJoinStride * 4;
+    static constexpr int kStatsOff = kAttnWarps * kWarpBytes > kJoinBytes ? kAttnWarps * kWarpBytes : kJoinBytes;
+    static constexpr int kBytes = kStatsOff + kAttnWarps * NQ * 2 * 4;
+    // CTAs of an SM: what registers (operands and accumulators of a lane, some 60 besides) and shared memory allow
+    static constexpr int kRegs = D * NQ / 32 + D * NQ / 64;
+    static constexpr int kByRegs = kRegs <= 48 ? 4 : (kRegs <= 96 ? 3 : 2);
+    static constexpr int kBySmem = 227 * 1024 / (kBytes + 1024);
+    static constexpr int kPerSm = kByRegs < kBySmem ? kByRegs : kBySmem;
+    static_assert(kPerSm >= 1 && kStageBytes % 16 == 0 && kWarpBytes % 16 == 0, "shared memory");
+
+    // where chunk c of a step's row r lies
+    static __device__ __forceinline__ int chunk_at(int r, int c) {
+        if constexpr (!kCodes) return c ^ (r & 7);
+        else if constexpr (kChunks >= 8) return c ^ (2 * (r & 3));
+        else if constexpr (kChunks == 4) return c ^ (r & 2);
+        else return c;
+    }
+    // row of a step that is position k of the products
+    static __device__ __forceinline__ int row_of(int k) {
+        if constexpr (!kCodes) return k;
+        const int j = (k & 7) >> 1;
+        return (k & ~7) | ((k & 1) ? 4 + (j ^ (kChunks >= 8 ? 2 : 1)) : j);
+    }
+    // first of the four channels that lane quarter j holds for product m of K Q^T
+    static __device__ __forceinline__ int k_channel(int m, int j) {
+        if constexpr (!kCodes) {
+            const int l = m >> 1;
+            return 8 * (2 * j + (l & 1) + 8 * (l >> 1)) + 4 * (m & 1);
+        } else if constexpr (FMT == kAttnFp8) {
+            return 16 * (j + 4 * (m >> 2)) + 4 * (m & 3);
+        } else if constexpr (kChunks >= 4) {
+            return 32 * (j + 4 * (m >> 3)) + 4 * (m & 7);
+        } else {
+            return 16 * j + 4 * m;
+        }
+    }
+};
+
+template <int FMT, int D, int NQ>
+__global__ void __launch_bounds__(kAttnThreads, (AttnShape<FMT, D, NQ>::kPerSm)) cache_attention_kernel(const __grid_constant__ AttentionProblem p) {
+    using L = AttnShape<FMT, D, NQ>;
+    constexpr int NT = NQ / 8, kM = D / 16;                              // column tiles; products of K Q^T = row tiles of O^T
+    constexpr int kMt = L::kStep / 16;                                   // row tiles of S^T
+    constexpr float kMinus = -INFINITY;
+    extern __shared__ __align__(16) uint8_t attn_smem[];
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, g = lane >> 2, j = lane & 3;
+    uint8_t* ring = attn_smem + warp * L::kWarpBytes;
+    __half* mul = reinterpret_cast<__half*>(ring + L::kRing);
+    float* join = reinterpret_cast<float*>(attn_smem);
+    float* stats = reinterpret_cast<float*>(attn_smem + L::kStatsOff);
+    const int real_chunks = p.c.row_bytes() / 16, blocks = p.c.blocks;
+    const bool padded = real_chunks < L::kChunks;
+    const uint32_t byte_mask0 = blocks >= 4 ? 0xFFFFFFFFu : (1u << (8 * blocks)) - 1u;
+    const uint32_t byte_mask1 = blocks >= 8 ? 0xFFFFFFFFu : (blocks <= 4 ? 0u : (1u << (8 * (blocks - 4))) - 1u);
+    pdl_launch_dependents();
+    pdl_wait_prior_grid();
+
+    // ---- this CTA's run of tiles ----
+    const int per_seq = p.c.heads * p.chunks;
+    int64_t at = 0, stop = 0, quota = 0;
+    int seq = 0, item = 0, tile = 0;
+    if (p.partial) {
+        const int64_t total = tiles_before<L::kTile>(p, p.sequences, lane) * per_seq;
+        quota = run_length(p, total);
+        at = blockIdx.x * quota;
+        stop = at + quota < total ? at + quota : total;
+        if (at >= stop) return;
+        int64_t before = 0;                                              // tiles per head of the sequences before
+        for (int s0 = 0;; s0 += 32) {
+            const int n = s0 + lane < p.sequences ? tiles_of<L::kTile>(visible_range(p, s0 + lane)) : 0;
+            int64_t upto = n;
+#pragma unroll
+            for (int o = 1; o < 32; o <<= 1) {
+                const int64_t v = __shfl_up_sync(0xFFFFFFFFu, upto, o);
+                if (lane >= o) upto += v;
+            }
+            const uint32_t past = __ballot_sync(0xFFFFFFFFu, (before + upto) * per_seq > at);
+            if (past) {
+                const int first = __ffs(past) - 1;
+                seq = s0 + first;
+                const int tiles = __shfl_sync(0xFFFFFFFFu, n, first);
+                const int64_t rest = at - (before + __shfl_sync(0xFFFFFFFFu, upto, first) - tiles) * per_seq;
+                item = (int)(rest / tiles);
+                tile = (int)(rest - (int64_t)item * tiles);
+                break;
+            }
+            before += __shfl_sync(0xFFFFFFFFu, upto, 31);
+        }
+    } else {
+        at = blockIdx.x;
+        stop = (int64_t)p.sequences * per_seq;
+    }
+
+    bool first_segment = true;
+    while (at < stop) {
+        if (!p.partial) {
+            seq = (int)(at / per_seq);
+            item = (int)(at - (int64_t)seq * per_seq);
+        }
+        const VisibleRange range = visible_range(p, seq);
+        const int tiles = tiles_of<L::kTile>(range);
+        int count = tiles - tile;
+        if (p.partial && count > stop - at) count = (int)(stop - at);
+        const bool whole = tile == 0 && count == tiles;
+        const int slot = 2 * (int)blockIdx.x + (tile == 0 ? 1 : 0);
+        const int head = item / p.chunks, chunk = item - head * p.chunks;
+        const int token0 = range.begin + tile * L::kTile;
+        const int64_t token_end = (int64_t)token0 + (int64_t)count * L::kTile;
+        const int end = token_end < range.end ? (int)token_end : range.end;
+        const int steps = end > token0 ? (end - token0 + L::kStep - 1) / L::kStep : 0;
+        const int my_steps = steps > warp ? (steps - warp + kAttnWarps - 1) / kAttnWarps : 0;
+        const int32_t* table = p.table + (int64_t)seq * p.table_stride;
+
+        if (padded || first_segment) {                                   // columns behind the rows' channels stay zero
+            if (padded)
+                for (int i = lane; i < L::kRing / 16; i += 32) reinterpret_cast<uint4*>(ring)[i] = make_uint4(0, 0, 0, 0);
+            first_segment = false;
+            __syncwarp();
+        }
+
+        // ---- queries: operand registers and the power of two of each row ----
+        uint32_t qf[kM][NT][2];
+        float q_scale[NT][2];
+#pragma unroll
+        for (int nt = 0; nt < NT; ++nt) {
+            const int row = chunk * NQ + nt * 8 + g;                     // query head within the group
+            const bool exists = row < p.group;
+            const uint16_t* q = static_cast<const uint16_t*>(p.q) + (int64_t)seq * p.q_row + (int64_t)(head * p.group + (exists ? row : 0)) * p.q_head;
+            uint32_t amax = 0;                                           // of the magnitude bits
+#pragma unroll
+            for (int m = 0; m < kM; ++m) {
+                const int ch = L::k_channel(m, j);
+                uint32_t v[4];
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    v[i] = exists && ch + i < p.c.head_dim ? q[ch + i] : 0u;
+                    amax = max(amax, v[i] & 0x7FFFu);
+                }
+                qf[m][nt][0] = v[0] | (v[1] << 16);
+                qf[m][nt][1] = v[2] | (v[3] << 16);
+            }
+            q_scale[nt][0] = q_scale[nt][1] = p.scale_log2e;
+            if constexpr (L::kCodes) {
+                amax = max(amax, __shfl_xor_sync(0xFFFFFFFFu, amax, 1));
+                amax = max(amax, __shfl_xor_sync(0xFFFFFFFFu, amax, 2));
+                const float top = p.q_f16 ? __half2float(__ushort_as_half((unsigned short)amax)) : __uint_as_float(amax << 16);
+                int e = (int)(__float_as_uint(top) >> 23) - 127;         // (0 and subnormal rows: -127)
+                e = e < -112 ? -112 : e;
+                const float up = exp2_int(14 - e);
+#pragma unroll
+                for (int m = 0; m < kM; ++m)
+#pragma unroll
+                    for (int i = 0; i < 2; ++i) {
+                        const uint32_t w = qf[m][nt][i];
+                        float lo, hi;
+                        if (p.q_f16) {
+                            lo = __half2float(__ushort_as_half((unsigned short)(w & 0xFFFFu)));
+                            hi = __half2float(__ushort_as_half((unsigned short)(w >> 16)));
+                        } else {
+                            lo = bf16lo_to_f32(w);
+                            hi = bf16hi_to_f32(w);
+                        }
+                        qf[m][nt][i] = pack_f16(lo * up, hi * up);
+                    }
+                const float down = exp2_int(e - 14);
+#pragma unroll
+                for (int i = 0; i < 2; ++i) q_scale[nt][i] *= __shfl_sync(0xFFFFFFFFu, down, 4 * (2 * j + i));
+            }
+        }
+
+        float o[kM][NT][4];
+        float m_run[NT][2], l_run[NT][2];
+        int v_run = 0;                                                   // R of the comment above
+#pragma unroll
+        for (int nt = 0; nt < NT; ++nt) {
+#pragma unroll
+            for (int m = 0; m < kM; ++m)
+#pragma unroll
+                for (int i = 0; i < 4; ++i) o[m][nt][i] = 0.f;
+            m_run[nt][0] = m_run[nt][1] = kMinus;
+            l_run[nt][0] = l_run[nt][1] = 0.f;
+        }
+
+        // ---- copies of a step ----
+        // cell of position `lane` of step i of this warp; false: none
+        auto locate = [&](int i, uint32_t& cell) -> bool {
+            const int t = token0 + (warp + i * kAttnWarps) * L::kStep + lane;
+            if (i >= my_steps || lane >= L::kStep || t >= end) return false;
+            const uint32_t entry = p.c.by_page.div((uint32_t)t);
+            const int page = __ldg(table + entry);
+            if (page < 0 || page >= p.c.pages) return false;
+            cell = (uint32_t)(((uint32_t)page * (uint32_t)p.c.heads + (uint32_t)head) * (uint32_t)p.c.page_size + ((uint32_t)t - entry * (uint32_t)p.c.page_size));
+            return true;
+        };
+        uint32_t cell_next = 0;
+        bool live_next = locate(0, cell_next);
+        auto issue = [&](int i) {
+            if (i < my_steps) {
+                const uint32_t cell = cell_next;
+                const uint32_t mask = __ballot_sync(0xFFFFFFFFu, live_next);
+                const bool live = live_next;
+                cell_next = 0;
+                live_next = locate(i + 1, cell_next);
+                uint8_t* stage = ring + (i % L::kStages) * L::kStageBytes;
+                const uint32_t base = shared_u32(stage);
+                const int64_t row_bytes = p.c.row_bytes();
+#pragma unroll
+                for (int c0 = 0; c0 < L::kStep * L::kChunks; c0 += 32) {
+                    const int r = (c0 + lane) / L::kChunks, c = (c0 + lane) % L::kChunks;
+                    const uint32_t from = __shfl_sync(0xFFFFFFFFu, cell, r);
+                    const int64_t off = (int64_t)from * row_bytes + 16 * c;
+                    const bool exists = (mask >> r) & 1u;
+                    if (c < real_chunks) {
+                        const uint32_t dst = base + r * L::kRow + 16 * L::chunk_at(r, c);
+                        copy_async<16>(dst, exists ? p.c.k + off : p.c.k, exists);
+                        copy_async<16>(dst + L::kStep * L::kRow, exists ? p.c.v + off : p.c.v, exists);
+                    }
+                }
+                if constexpr (L::kCodes) {
+                    const int64_t off = live ? (int64_t)cell * L::kScaleRow : 0;
+                    copy_async<L::kScaleRow>(base + L::kScaleOff + lane * L::kScaleRow, p.c.k_scales + off, live);
+                    copy_async<L::kScaleRow>(base + L::kScaleOff + (L::kStep + lane) * L::kScaleRow, p.c.v_scales + off, live);
+                }
+                if (lane == 0) *reinterpret_cast<uint32_t*>(stage + L::kMaskOff) = mask;
+            }
+            asm volatile("cp.async.commit_group;" ::: "memory");
+        };
+
+#pragma unroll
+        for (int i = 0; i < L::kStages - 1; ++i) issue(i);
+        for (int it = 0; it < my_steps; ++it) {
+            asm volatile("cp.async.wait_group %0;" ::"n"(L::kStages - 2) : "memory");
+            __syncwarp();
+            issue(it + L::kStages - 1);                                  // (into the stage of the step before, which all lanes have left)
+            const uint8_t* stage = ring + (it % L::kStages) * L::kStageBytes;
+            const uint8_t* kst = stage;
+            const uint8_t* vst = stage + L::kStep * L::kRow;
+            const uint32_t mask = *reinterpret_cast<const uint32_t*>(stage + L::kMaskOff);
+
+            // ---- scales: lane = position of the products ----
+            float k_factor = 1.f, v_factor = 1.f;
+            int v_new = v_run;
+            if constexpr (L::kCodes) {
+                const int r = L::row_of(lane);
+                const bool live = (mask >> r) & 1u;
+                int top[2];
+#pragma unroll
+                for (int kv = 0; kv < 2; ++kv) {
+                    const uint8_t* s = stage + L::kScaleOff + (kv * L::kStep + r) * L::kScaleRow;
+                    uint32_t w[L::kScaleRow / 4];
+                    w[0] = *reinterpret_cast<const uint32_t*>(s) & byte_mask0;
+                    if constexpr (L::kScaleRow == 8) w[1] = *reinterpret_cast<const uint32_t*>(s + 4) & byte_mask1;
+                    int S[D / 32], most = 0;
+#pragma unroll
+                    for (int b = 0; b < D / 32; ++b) {
+                        S[b] = (int)((w[b / 4] >> (8 * (b & 3))) & 0xFFu);
+                        most = max(most, S[b]);
+                    }
+                    top[kv] = most;
+#pragma unroll
+                    for (int b = 0; b < D / 32; ++b) mul[(kv * (D / 32) + b) * L::kStep + lane] = __float2half_rn(exp2_int(S[b] - most));
+                }
+                k_factor = exp2_int(top[0] - 127);
+                v_new = max(v_run, (int)__reduce_max_sync(0xFFFFFFFFu, live ? top[1] : 0));
+                v_factor = exp2_int(top[1] - v_new + 14);
+                __syncwarp();
+            }
+
+            // ---- S^T = K Q^T ----
+            float s[kMt][NT][4];
+#pragma unroll
+            for (int mt = 0; mt < kMt; ++mt) {
+#pragma unroll
+                for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) s[mt][nt][i] = 0.f;
+                const int r0 = L::row_of(16 * mt + g), r1 = r0 + 8;
+                const uint8_t* a = kst + r0 * L::kRow;
+                const uint8_t* b = kst + r1 * L::kRow;
+                if constexpr (FMT == kAttnFp4 && L::kChunks == 2) {
+                    const uint2 x = *reinterpret_cast<const uint2*>(a + 8 * j), y = *reinterpret_cast<const uint2*>(b + 8 * j);
+                    const __half2 ma = __half2half2(mul[(j >> 1) * L::kStep + 16 * mt + g]), mb = __half2half2(mul[(j >> 1) * L::kStep + 16 * mt + g + 8]);
+                    const uint32_t xs = *reinterpret_cast<const uint32_t*>(&ma), ys = *reinterpret_cast<const uint32_t*>(&mb);
+#pragma unroll
+                    for (int w = 0; w < 2; ++w) {
+                        uint32_t hx[4], hy[4];
+                        e2m1x8_to_f16(w ? x.y : x.x, hx);
+                        e2m1x8_to_f16(w ? y.y : y.x, hy);
+#pragma unroll
+                        for (int i = 0; i < 4; ++i) { hx[i] = mul_f16x2(hx[i], xs); hy[i] = mul_f16x2(hy[i], ys); }
+#pragma unroll
+                        for (int h = 0; h < 2; ++h)
+#pragma unroll
+                            for (int nt = 0; nt < NT; ++nt)
+                                mma_16816_f16(s[mt][nt], hx[2 * h], hy[2 * h], hx[2 * h + 1], hy[2 * h + 1], qf[2 * w + h][nt][0], qf[2 * w + h][nt][1]);
+                    }
+                } else {
+#pragma unroll
+                    for (int l = 0; l < L::kChunks / 4; ++l) {
+                        const int c = L::kCodes ? j + 4 * l : 2 * j + (l & 1) + 8 * (l >> 1);
+                        const uint4 x = *reinterpret_cast<const uint4*>(a + 16 * L::chunk_at(r0, c));
+                        const uint4 y = *reinterpret_cast<const uint4*>(b + 16 * L::chunk_at(r1, c));
+                        const uint32_t xw[4] = {x.x, x.y, x.z, x.w}, yw[4] = {y.x, y.y, y.z, y.w};
+                        if constexpr (!L::kCodes) {
+#pragma unroll
+                            for (int h = 0; h < 2; ++h)
+#pragma unroll
+                                for (int nt = 0; nt < NT; ++nt) {
+                                    if constexpr (FMT == kAttnBf16)
+                                        mma_16816_bf16(s[mt][nt], xw[2 * h], yw[2 * h], xw[2 * h + 1], yw[2 * h + 1], qf[2 * l + h][nt][0], qf[2 * l + h][nt][1]);
+                                    else
+                                        mma_16816_f16(s[mt][nt], xw[2 * h], yw[2 * h], xw[2 * h + 1], yw[2 * h + 1], qf[2 * l + h][nt][0], qf[2 * l + h][nt][1]);
+                                }
+                        } else {
+                            const int block = FMT == kAttnFp8 ? c >> 1 : c;
+                            const __half2 ma = __half2half2(mul[block * L::kStep + 16 * mt + g]), mb = __half2half2(mul[block * L::kStep + 16 * mt + g + 8]);
+                            const uint32_t xs = *reinterpret_cast<const uint32_t*>(&ma), ys = *reinterpret_cast<const uint32_t*>(&mb);
+#pragma unroll
+                            for (int w = 0; w < 4; ++w) {
+                                if constexpr (FMT == kAttnFp8) {
+                                    uint32_t x0, x1, y0, y1;
+                                    e4m3x4_to_f16(xw[w], x0, x1);
+                                    e4m3x4_to_f16(yw[w], y0, y1);
+                                    x0 = mul_f16x2(x0, xs); x1 = mul_f16x2(x1, xs);
+                                    y0 = mul_f16x2(y0, ys); y1 = mul_f16x2(y1, ys);
+#pragma unroll
+                                    for (int nt = 0; nt < NT; ++nt)
+                                        mma_16816_f16(s[mt][nt], x0, y0, x1, y1, qf[4 * l + w][nt][0], qf[4 * l + w][nt][1]);
+                                } else {
+                                    uint32_t hx[4], hy[4];
+                                    e2m1x8_to_f16(xw[w], hx);
+                                    e2m1x8_to_f16(yw[w], hy);
+#pragma unroll
+                                    for (int i = 0; i < 4; ++i) { hx[i] = mul_f16x2(hx[i], xs); hy[i] = mul_f16x2(hy[i], ys); }
+#pragma unroll
+                                    for (int h = 0; h < 2; ++h)
+#pragma unroll
+                                        for (int nt = 0; nt < NT; ++nt)
+                                            mma_16816_f16(s[mt][nt], hx[2 * h], hy[2 * h], hx[2 * h + 1], hy[2 * h + 1], qf[8 * l + 2 * w + h][nt][0], qf[8 * l + 2 * w + h][nt][1]);
+                                }
+                            }
+                        }
+                    }
+                }
+            }
+
+            // ---- scores, running maximum and sum ----
+            float vf[kMt][2];
+#pragma unroll
+            for (int mt = 0; mt < kMt; ++mt)
+#pragma unroll
+                for (int h = 0; h < 2; ++h) {
+                    const int k = 16 * mt + 8 * h + g;
+                    float kf = 1.f;
+                    vf[mt][h] = FMT == kAttnF16 ? 16384.f : 1.f;
+                    if constexpr (L::kCodes) {
+                        kf = __shfl_sync(0xFFFFFFFFu, k_factor, k);
+                        vf[mt][h] = __shfl_sync(0xFFFFFFFFu, v_factor, k);
+                    }
+                    const bool live = (mask >> L::row_of(k)) & 1u;
+#pragma unroll
+                    for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+                        for (int i = 0; i < 2; ++i) s[mt][nt][2 * h + i] = live ? s[mt][nt][2 * h + i] * q_scale[nt][i] * kf : kMinus;
+                }
+            bool grown = v_new != v_run;
+            float m_new[NT][2];
+#pragma unroll
+            for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+                for (int i = 0; i < 2; ++i) {
+                    float m = m_run[nt][i];
+#pragma unroll
+                    for (int mt = 0; mt < kMt; ++mt) m = fmaxf(m, fmaxf(s[mt][nt][i], s[mt][nt][2 + i]));
+                    m = fmaxf(m, __shfl_xor_sync(0xFFFFFFFFu, m, 4));
+                    m = fmaxf(m, __shfl_xor_sync(0xFFFFFFFFu, m, 8));
+                    m = fmaxf(m, __shfl_xor_sync(0xFFFFFFFFu, m, 16));
+                    m_new[nt][i] = m;
+                    grown |= m != m_run[nt][i];
+                }
+            if (__any_sync(0xFFFFFFFFu, grown)) {
+                const float v_down = exp2_int(v_run - v_new);
+#pragma unroll
+                for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+                    for (int i = 0; i < 2; ++i) {
+                        const float down = m_run[nt][i] == kMinus ? 0.f : exp2_fast(m_run[nt][i] - m_new[nt][i]);
+                        m_run[nt][i] = m_new[nt][i];
+                        l_run[nt][i] *= down;
+                        const float both = down * v_down;
+#pragma unroll
+                        for (int m = 0; m < kM; ++m) {
+                            o[m][nt][i] *= both;
+                            o[m][nt][2 + i] *= both;
+                        }
+                    }
+                v_run = v_new;
+            }
+            // weights, as operand B of O^T += V^T P^T
+            uint32_t pb[kMt][NT][2], pl[FMT == kAttnBf16 ? kMt : 1][NT][2];
+#pragma unroll
+            for (int nt = 0; nt < NT; ++nt) {
+                const float m0 = m_run[nt][0] == kMinus ? 0.f : m_run[nt][0], m1 = m_run[nt][1] == kMinus ? 0.f : m_run[nt][1];
+#pragma unroll
+                for (int mt = 0; mt < kMt; ++mt)
+#pragma unroll
+                    for (int h = 0; h < 2; ++h) {
+                        const float p0 = exp2_fast(s[mt][nt][2 * h] - m0), p1 = exp2_fast(s[mt][nt][2 * h + 1] - m1);
+                        l_run[nt][0] += p0;
+                        l_run[nt][1] += p1;
+                        if constexpr (FMT == kAttnBf16) {
+                            const uint32_t hi = pack_bf16(p0, p1);
+                            pb[mt][nt][h] = transpose_8x8(hi);
+                            pl[mt][nt][h] = transpose_8x8(pack_bf16(p0 - bf16lo_to_f32(hi), p1 - bf16hi_to_f32(hi)));
+                        } else {
+                            pb[mt][nt][h] = transpose_8x8(pack_f16(p0 * vf[mt][h], p1 * vf[mt][h]));
+                        }
+                    }
+            }
+
+            // ---- O^T += V^T P^T ----
+            if constexpr (!L::kCodes) {
+                const int r = (lane & 7) + ((lane >> 4) & 1) * 8;
+                const uint32_t row = shared_u32(vst) + r * L::kRow;
+#pragma unroll
+                for (int m = 0; m < kM; ++m) {
+                    uint32_t a0, a1, a2, a3;
+                    asm volatile("ldmatrix.sync.aligned.m8n8.x4.trans.shared.b16 {%0,%1,%2,%3}, [%4];"
+                                 : "=r"(a0), "=r"(a1), "=r"(a2), "=r"(a3) : "r"(row + 16 * L::chunk_at(r, 2 * m + ((lane >> 3) & 1))) : "memory");
+#pragma unroll
+                    for (int nt = 0; nt < NT; ++nt) {
+                        if constexpr (FMT == kAttnBf16) {
+                            mma_16816_bf16(o[m][nt], a0, a1, a2, a3, pb[0][nt][0], pb[0][nt][1]);
+                            mma_16816_bf16(o[m][nt], a0, a1, a2, a3, pl[0][nt][0], pl[0][nt][1]);
+                        } else {
+                            mma_16816_f16(o[m][nt], a0, a1, a2, a3, pb[0][nt][0], pb[0][nt][1]);
+                        }
+                    }
+                }
+            } else {
+                constexpr int kBytesV = L::kRow / 8, kWords = kBytesV / 4;   // of a lane's channels at one position
+                const int block = g * (D / 8) / 32;
+#pragma unroll
+                for (int mt = 0; mt < kMt; ++mt) {
+                    uint32_t w[4][kWords];
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) {                        // positions 2j, 2j + 1, 2j + 8, 2j + 9
+                        const int r = L::row_of(16 * mt + 2 * j + (i & 1) + 8 * (i >> 1));
+                        const uint8_t* row = vst + r * L::kRow;
+                        if constexpr (kBytesV == 4) {
+                            w[i][0] = *reinterpret_cast<const uint32_t*>(row + 16 * L::chunk_at(r, g >> 2) + 4 * (g & 3));
+                        } else if constexpr (kBytesV == 8) {
+                            const uint2 x = *reinterpret_cast<const uint2*>(row + 16 * L::chunk_at(r, g >> 1) + 8 * (g & 1));
+                            w[i][0] = x.x; w[i][1] = x.y;
+                        } else {
+#pragma unroll
+                            for (int c = 0; c < kBytesV / 16; ++c) {
+                                const uint4 x = *reinterpret_cast<const uint4*>(row + 16 * L::chunk_at(r, g * (kBytesV / 16) + c));
+                                w[i][4 * c] = x.x; w[i][4 * c + 1] = x.y; w[i][4 * c + 2] = x.z; w[i][4 * c + 3] = x.w;
+                            }
+                        }
+                    }
+                    const __half* mv = mul + (D / 32 + block) * L::kStep + 16 * mt + 2 * j;
+                    const uint32_t m01 = *reinterpret_cast<const uint32_t*>(mv), m23 = *reinterpret_cast<const uint32_t*>(mv + 8);
+#pragma unroll
+                    for (int x = 0; x < kWords; ++x) {
+                        if constexpr (FMT == kAttnFp8) {                 // four channels: the same channel of two positions side by side
+#pragma unroll
+                            for (int h = 0; h < 2; ++h) {
+                                uint32_t a0, a1, a2, a3;
+                                e4m3x4_to_f16(__byte_perm(w[0][x], w[1][x], h ? 0x7362 : 0x5140), a0, a1);
+                                e4m3x4_to_f16(__byte_perm(w[2][x], w[3][x], h ? 0x7362 : 0x5140), a2, a3);
+                                a0 = mul_f16x2(a0, m01); a1 = mul_f16x2(a1, m01);
+                                a2 = mul_f16x2(a2, m23); a3 = mul_f16x2(a3, m23);
+#pragma unroll
+                                for (int nt = 0; nt < NT; ++nt) mma_16816_f16(o[2 * x + h][nt], a0, a1, a2, a3, pb[mt][nt][0], pb[mt][nt][1]);
+                            }
+                        } else {                                         // eight channels
+                            constexpr uint32_t kLow = 0x0F0F0F0Fu;
+                            uint32_t e01[4], o01[4], e23[4], o23[4];     // even and odd channels of the pairs of positions
+                            e2m1x8_to_f16((w[0][x] & kLow) | ((w[1][x] << 4) & ~kLow), e01);
+                            e2m1x8_to_f16(((w[0][x] >> 4) & kLow) | (w[1][x] & ~kLow), o01);
+                            e2m1x8_to_f16((w[2][x] & kLow) | ((w[3][x] << 4) & ~kLow), e23);
+                            e2m1x8_to_f16(((w[2][x] >> 4) & kLow) | (w[3][x] & ~kLow), o23);
+#pragma unroll
+                            for (int i = 0; i < 4; ++i) {
+                                const uint32_t a0 = mul_f16x2(e01[i], m01), a1 = mul_f16x2(o01[i], m01);
+                                const uint32_t a2 = mul_f16x2(e23[i], m23), a3 = mul_f16x2(o23[i], m23);
+#pragma unroll
+                                for (int nt = 0; nt < NT; ++nt) mma_16816_f16(o[4 * x + i][nt], a0, a1, a2, a3, pb[mt][nt][0], pb[mt][nt][1]);
+                            }
+                        }
+                    }
+                }
+            }
+            __syncwarp();                                                // the multipliers' place is free again
+        }
+        asm volatile("cp.async.wait_group 0;" ::: "memory");
+
+        // ---- the warps' parts together ----
+#pragma unroll
+        for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+            for (int i = 0; i < 2; ++i) {
+                float l = l_run[nt][i];
+                l += __shfl_xor_sync(0xFFFFFFFFu, l, 4);
+                l += __shfl_xor_sync(0xFFFFFFFFu, l, 8);
+                l += __shfl_xor_sync(0xFFFFFFFFu, l, 16);
+                if (g == 0) {
+                    stats[warp * NQ + nt * 8 + 2 * j + i] = m_run[nt][i];
+                    stats[(kAttnWarps + warp) * NQ + nt * 8 + 2 * j + i] = l;
+                }
+            }
+        __syncthreads();                                                 // all warps have left their rings
+        const float unit = L::kCodes ? exp2_int(v_run - 127 - 14) : (FMT == kAttnF16 ? 1.f / 16384.f : 1.f);
+#pragma unroll
+        for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+            for (int i = 0; i < 2; ++i) {
+                const int col = nt * 8 + 2 * j + i;
+                float top = kMinus;
+#pragma unroll
+                for (int w = 0; w < kAttnWarps; ++w) top = fmaxf(top, stats[w * NQ + col]);
+                const float f = m_run[nt][i] == kMinus ? 0.f : exp2_fast(m_run[nt][i] - top) * unit;
+                float* to = join + (warp * NQ + col) * L::kJoinStride;
+#pragma unroll
+                for (int m = 0; m < kM; ++m) {
+                    if constexpr (L::kCodes) {
+                        *reinterpret_cast<float2*>(to + g * (D / 8) + 2 * m) = make_float2(o[m][nt][i] * f, o[m][nt][2 + i] * f);
+                    } else {
+                        to[16 * m + g] = o[m][nt][i] * f;
+                        to[16 * m + 8 + g] = o[m][nt][2 + i] * f;
+                    }
+                }
+            }
+        __syncthreads();
+        const int live_q = p.group - chunk * NQ < NQ ? p.group - chunk * NQ : NQ;
+        for (int i = threadIdx.x; i < live_q * D; i += kAttnThreads) {
+            const int col = i / D, ch = i - col * D;
+            float top = kMinus, sum = 0.f, l = 0.f;
+#pragma unroll
+            for (int w = 0; w < kAttnWarps; ++w) top = fmaxf(top, stats[w * NQ + col]);
+            const float ref = top == kMinus ? 0.f : top;
+#pragma unroll
+            for (int w = 0; w < kAttnWarps; ++w) {
+                sum += join[(w * NQ + col) * L::kJoinStride + ch];
+                l += stats[(kAttnWarps + w) * NQ + col] * exp2_fast(stats[w * NQ + col] - ref);
+            }
+            if (whole) {
+                const int q_head = head * p.group + chunk * NQ + col;
+                const float v = l == 0.f ? 0.f : sum / l;
+                if (ch < p.c.head_dim) {
+                    const int64_t to = (int64_t)seq * p.out_row + (int64_t)q_head * p.out_head + ch;
+                    if (p.out_type == 0) static_cast<float*>(p.out)[to] = v;
+                    else if (p.out_type == 2) static_cast<__half*>(p.out)[to] = __float2half_rn(v);
+                    else static_cast<__nv_bfloat16*>(p.out)[to] = __float2bfloat16_rn(v);
+                }
+                if (p.lse && ch == 0) p.lse[(int64_t)seq * p.q_heads + q_head] = l == 0.f ? kMinus : (top + log2f(l)) * 0.6931471805599453f;
+            } else {
+                p.partial[((int64_t)slot * NQ + col) * D + ch] = sum;
+                if (ch == 0) {
+                    float* st = p.partial + (int64_t)2 * p.ctas * NQ * D + (int64_t)slot * 2 * NQ;
+                    st[col] = top;
+                    st[NQ + col] = l;
+                }
+            }
+        }
+        __syncthreads();                                                 // the rings are free again
+
+        if (p.partial) {
+            at += count;
+            tile = 0;
+            if (++item == per_seq) {
+                item = 0;
+                ++seq;
+            }
+        } else {
+            at += gridDim.x;
+        }
+    }
+}
+
+constexpr int kJoinThreads = 256;
+
+// Joins the parts of an item that several CTAs took: blockIdx.x = item, blockIdx.y = query of the chunk.  The threads are D/4 groups of
+// four channels times lanes that take every so many parts; the lanes' sums are added in order.
+template <int TN, int D, int NQ>
+__global__ void __launch_bounds__(kJoinThreads) cache_attention_join(const __grid_constant__ AttentionProblem p) {
+    constexpr int kCols = D / 4, kLanes = kJoinThreads / kCols;
+    __shared__ float4 sums[kJoinThreads];
+    __shared__ float weights[kLanes];
+    pdl_launch_dependents();
+    pdl_wait_prior_grid();
+    const int per_seq = p.c.heads * p.chunks, lane = threadIdx.x & 31;
+    const int seq = (int)blockIdx.x / per_seq, item = (int)blockIdx.x - seq * per_seq;
+    const int head = item / p.chunks, col = blockIdx.y, row = (item - head * p.chunks) * NQ + col;
+    if (row >= p.group) return;
+    const int64_t before = tiles_before<TN>(p, seq, lane);
+    const int tiles = tiles_of<TN>(visible_range(p, seq));
+    int64_t rest = 0;
+    for (int s = seq + lane; s < p.sequences; s += 32) rest += tiles_of<TN>(visible_range(p, s));
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1) rest += __shfl_xor_sync(0xFFFFFFFFu, rest, o);
+    const int64_t quota = run_length(p, (before + rest) * per_seq);
+    const int64_t a = before * per_seq + (int64_t)item * tiles;
+    const int c0 = (int)(a / quota), c1 = (int)((a + tiles - 1) / quota);
+    if (c0 == c1) return;                                                // written by its CTA
+    const float* st = p.partial + (int64_t)2 * p.ctas * NQ * D;
+    auto slot = [&](int c) { return 2 * c + (c == c0 ? 1 : 0); };
+    float top = -INFINITY;
+    for (int c = c0 + lane; c <= c1; c += 32) top = fmaxf(top, st[(int64_t)slot(c) * 2 * NQ + col]);
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1) top = fmaxf(top, __shfl_xor_sync(0xFFFFFFFFu, top, o));
+    const float ref = top == -INFINITY ? 0.f : top;
+    const int x = threadIdx.x % kCols, y = threadIdx.x / kCols;
+    float4 sum = make_float4(0.f, 0.f, 0.f, 0.f);
+    float l = 0.f;
+#pragma unroll 4
+    for (int c = c0 + y; c <= c1; c += kLanes) {
+        const float4 v = *reinterpret_cast<const float4*>(p.partial + ((int64_t)slot(c) * NQ + col) * D + 4 * x);
+        const float* s = st + (int64_t)slot(c) * 2 * NQ + col;
+        const float f = exp2_fast(s[0] - ref);
+        l += f * s[NQ];
+        sum.x += f * v.x; sum.y += f * v.y; sum.z += f * v.z; sum.w += f * v.w;
+    }
+    sums[threadIdx.x] = sum;
+    if (x == 0) weights[y] = l;
+    __syncthreads();
+    if (y != 0) return;
+    l = weights[0];
+    for (int k = 1; k < kLanes; ++k) {
+        const float4 v = sums[k * kCols + x];
+        sum.x += v.x; sum.y += v.y; sum.z += v.z; sum.w += v.w;
+        l += weights[k];
+    }
+    const int q_head = head * p.group + row;
+    const float inv[4] = {sum.x, sum.y, sum.z, sum.w};
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        const int ch = 4 * x + i;
+        if (ch >= p.c.head_dim) continue;
+        const float v = l == 0.f ? 0.f : inv[i] / l;
+        const int64_t to = (int64_t)seq * p.out_row + (int64_t)q_head * p.out_head + ch;
+        if (p.out_type == 0) static_cast<float*>(p.out)[to] = v;
+        else if (p.out_type == 2) static_cast<__half*>(p.out)[to] = __float2half_rn(v);
+        else static_cast<__nv_bfloat16*>(p.out)[to] = __float2bfloat16_rn(v);
+    }
+    if (p.lse && x == 0) p.lse[(int64_t)seq * p.q_heads + q_head] = l == 0.f ? -INFINITY : (top + log2f(l)) * 0.6931471805599453f;
+}
+
+}  // namespace kq

@@ -246,11 +246,6 @@ __device__ __forceinline__ void named_barrier_sync(uint32_t id, uint32_t threads
     asm volatile("bar.sync %0, %1;" ::"r"(id), "r"(threads) : "memory");
 }
 
-// Programmatic dependent launch: let the next kernel in the stream start its prologue
-// early, and wait for the previous kernel's memory before touching global data.
-__device__ __forceinline__ void pdl_launch_dependents() { asm volatile("griddepcontrol.launch_dependents;" ::: "memory"); }
-__device__ __forceinline__ void pdl_wait_prior_grid() { asm volatile("griddepcontrol.wait;" ::: "memory"); }
-
 // ---- shared memory plan ----------------------------------------------------------
 // PB = false: one factor image for the whole launch at offset 0, stages of 8 KB (A only).
 // PB = true : every stage carries its own factor image: 8 KB of A + 6 KB of B.

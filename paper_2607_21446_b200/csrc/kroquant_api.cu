@@ -14,8 +14,11 @@
 #include <cuda.h>
 #include <cuda_runtime.h>
 
+#include "kq_host.cuh"
 #include "kq_stream.cuh"
 #include "kq_umma.cuh"
+
+std::atomic<int64_t> g_launches{0};
 
 struct kroquant_factors {
     int n_sets = 0;
@@ -32,8 +35,6 @@ struct kroquant_factors {
 };
 
 namespace {
-
-std::atomic<int64_t> g_launches{0};
 
 // ---- tensor-core kernel configuration ----------------------------------------
 // Defaults (measured on the 28-call FLUX step): the shared-factor bf16 kernel runs as (8 slots, 2 MMA warps,
@@ -73,34 +74,6 @@ EncodeTiledFn get_encode_tiled() {
     });
     return fn;
 }
-
-int sm_count() {
-    static int cached[64] = {0};
-    int dev = 0;
-    if (cudaGetDevice(&dev) != cudaSuccess || dev < 0 || dev >= 64) return 0;
-    if (cached[dev] == 0) {
-        int n = 0;
-        if (cudaDeviceGetAttribute(&n, cudaDevAttrMultiProcessorCount, dev) != cudaSuccess) return 0;
-        cached[dev] = n;
-    }
-    return cached[dev];
-}
-
-// Per-device "do once" for set-up that belongs to a device (function attributes).  needed() is true until
-// done() has been called with the same device current; a race between two first calls only repeats the set-up.
-struct DeviceOnce {
-    std::atomic<int> flag[64];
-    DeviceOnce() { for (auto& f : flag) f.store(0); }
-    static int dev() {
-        int d = -1;
-        if (cudaGetDevice(&d) != cudaSuccess || d < 0 || d >= 64) return -1;
-        return d;
-    }
-    bool needed() const { const int d = dev(); return d < 0 || !flag[d].load(std::memory_order_acquire); }
-    void done() { const int d = dev(); if (d >= 0) flag[d].store(1, std::memory_order_release); }
-};
-
-bool aligned16(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15u) == 0; }
 
 kq_status_t check_shape(int64_t tokens, int d) {
     if (d <= 0 || d % 32 != 0 || tokens < 0) return KQ_ERR_SHAPE;

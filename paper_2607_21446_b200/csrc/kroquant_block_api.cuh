@@ -3,46 +3,10 @@
 // translation unit, one device error word.
 #pragma once
 #include "kq_linear.cuh"
+#include "kq_linear_w4a16.cuh"
 #include "kq_norm.cuh"
 
 namespace {
-
-int type_size(int t) { return t == KQ_OUT_F32 ? 4 : 2; }
-bool known_type(int t) { return t == KQ_OUT_F32 || t == KQ_OUT_BF16 || t == KQ_OUT_FP16; }
-bool element_aligned(const void* p, int type) { return reinterpret_cast<uintptr_t>(p) % type_size(type) == 0; }
-// pointer and pitch (in elements) both keep rows on `bytes`-byte boundaries
-bool rows_aligned(const void* p, int64_t pitch, int type, int bytes) {
-    return !p || (reinterpret_cast<uintptr_t>(p) % bytes == 0 && pitch * type_size(type) % bytes == 0);
-}
-
-// a launch that may set up while the kernel before it drains (every kernel here waits for it before it touches memory)
-void launch_config(cudaLaunchConfig_t* cfg, cudaLaunchAttribute* attr, dim3 grid, dim3 block, size_t smem, int cluster, cudaStream_t st) {
-    *cfg = {};
-    cfg->gridDim = grid;
-    cfg->blockDim = block;
-    cfg->dynamicSmemBytes = smem;
-    cfg->stream = st;
-    attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
-    attr[0].val.programmaticStreamSerializationAllowed = 1;
-    cfg->attrs = attr;
-    cfg->numAttrs = 1;
-    if (cluster > 1) {
-        attr[1].id = cudaLaunchAttributeClusterDimension;
-        attr[1].val.clusterDim.x = (unsigned)cluster;
-        attr[1].val.clusterDim.y = 1;
-        attr[1].val.clusterDim.z = 1;
-        cfg->numAttrs = 2;
-    }
-}
-template <typename... Params, typename... Args>
-kq_status_t launch(const cudaLaunchConfig_t& cfg, void (*kernel)(Params...), Args&&... args) {
-    if (cudaLaunchKernelEx(&cfg, kernel, std::forward<Args>(args)...) != cudaSuccess) {
-        (void)cudaGetLastError();
-        return KQ_ERR_CUDA;
-    }
-    g_launches.fetch_add(1, std::memory_order_relaxed);
-    return KQ_OK;
-}
 
 bool encode_map(EncodeTiledFn enc, CUtensorMap* tm, CUtensorMapDataType type, int rank, const void* ptr, const cuuint64_t* dims,
                 const cuuint64_t* strides, const cuuint32_t* box, CUtensorMapSwizzle swizzle, CUtensorMapL2promotion promote) {
@@ -135,21 +99,42 @@ kq_status_t launch_narrow(LinearLaunch& l, EncodeTiledFn enc, int sms, cudaStrea
     return launch(cfg, kq::linear_mxfp4_narrow<GLU, TB>, tw, ta, tsw, tsa, p, splits);
 }
 
+// What every linear call asks of its epilogue and out.
+kq_status_t check_epilogue(const kq_epilogue_t& e, int N, int K, const void* out, kq_dtype_t out_dtype, int64_t ld_out) {
+    if (N <= 0 || N > (1 << 26) || K <= 0 || K % 32 || ld_out < N) return KQ_ERR_SHAPE;
+    if (e.activation < KQ_ACT_NONE || e.activation > KQ_ACT_GELU_TANH || (e.glu | 1) != 1 || !known_type(out_dtype) ||
+        (e.bias && !known_type(e.bias_dtype)) || (e.gate && !known_type(e.gate_dtype)) || (e.residual && !known_type(e.residual_dtype)))
+        return KQ_ERR_UNSUPPORTED;
+    if ((e.gate && (e.rows_per_gate < 1 || (e.gate_stride != 0 && e.gate_stride < N))) || (e.residual && e.ld_residual < N)) return KQ_ERR_SHAPE;
+    if (!element_aligned(out, out_dtype) || (e.bias && !element_aligned(e.bias, e.bias_dtype)) || (e.gate && !element_aligned(e.gate, e.gate_dtype)) ||
+        (e.residual && !element_aligned(e.residual, e.residual_dtype)) || reinterpret_cast<uintptr_t>(e.row_scale) % 4)
+        return KQ_ERR_ALIGN;
+    return KQ_OK;
+}
+void fill_epilogue(kq::LinearEpilogue& ep, const kq_epilogue_t& e, int64_t M, int N, int64_t bias_stride, void* out, kq_dtype_t out_dtype, int64_t ld_out) {
+    ep.N = N;
+    ep.act = e.activation;
+    ep.bias = {e.bias, bias_stride, e.bias_dtype};
+    ep.gate = {e.gate, e.gate_stride, e.gate_dtype};
+    // (one gate row for all is one gate row, whatever rows_per_gate says: a warp then reads it once instead of a lane each for its row)
+    ep.rows_per_gate = !e.gate || !e.gate_stride || e.rows_per_gate > M ? (int)M : (int)e.rows_per_gate;
+    ep.row_scale = e.row_scale;
+    ep.residual = e.residual; ep.residual_type = e.residual_dtype; ep.ld_residual = e.ld_residual; ep.residual_scale = e.residual_scale;
+    ep.out = out; ep.out_type = out_dtype; ep.ld_out = ld_out;
+    ep.vec = rows_aligned(out, ld_out, out_dtype, 16) && rows_aligned(e.residual, e.ld_residual, e.residual_dtype, 16);
+    ep.wide = rows_aligned(out, ld_out, out_dtype, 32);
+}
+
 kq_status_t run_linear(const uint8_t* a_codes, const uint8_t* a_scales, const uint8_t* b_codes, const uint8_t* b_scales,
                        const int32_t* offsets, int experts, int64_t M, int N, int K, const kq_epilogue_t* epilogue, void* out,
                        kq_dtype_t out_dtype, int64_t ld_out, void* stream) {
     kq_epilogue_t e;
     if (epilogue) e = *epilogue; else kroquant_epilogue_default(&e);
     if (!b_codes || !b_scales || (M > 0 && (!a_codes || !a_scales || !out))) return KQ_ERR_NULL;
-    if (M < 0 || M > (1 << 24) || N <= 0 || N > (1 << 26) || K <= 0 || K % 32 || ld_out < N) return KQ_ERR_SHAPE;
-    if (e.activation < KQ_ACT_NONE || e.activation > KQ_ACT_GELU_TANH || (e.glu | 1) != 1 || !known_type(out_dtype) ||
-        (e.bias && !known_type(e.bias_dtype)) || (e.gate && !known_type(e.gate_dtype)) || (e.residual && !known_type(e.residual_dtype)))
-        return KQ_ERR_UNSUPPORTED;
-    if ((e.gate && (e.rows_per_gate < 1 || (e.gate_stride != 0 && e.gate_stride < N))) || (e.residual && e.ld_residual < N)) return KQ_ERR_SHAPE;
-    if (!aligned16(a_codes) || !aligned16(a_scales) || !aligned16(b_codes) || !aligned16(b_scales) || !element_aligned(out, out_dtype) ||
-        (e.bias && !element_aligned(e.bias, e.bias_dtype)) || (e.gate && !element_aligned(e.gate, e.gate_dtype)) ||
-        (e.residual && !element_aligned(e.residual, e.residual_dtype)) || reinterpret_cast<uintptr_t>(e.row_scale) % 4)
-        return KQ_ERR_ALIGN;
+    if (M < 0 || M > (1 << 24)) return KQ_ERR_SHAPE;
+    const kq_status_t rc = check_epilogue(e, N, K, out, out_dtype, ld_out);
+    if (rc != KQ_OK) return rc;
+    if (!aligned16(a_codes) || !aligned16(a_scales) || !aligned16(b_codes) || !aligned16(b_scales)) return KQ_ERR_ALIGN;
     const int64_t R = e.glu ? (int64_t)64 * ((N + 31) / 32) : N;
     const int count = experts ? experts : 1;
     if ((M / 128 + 1 + count) * ((R + 127) / 128) >= ((int64_t)1 << 31) || ((R + 127) / 128) * count >= ((int64_t)1 << 31)) return KQ_ERR_SHAPE;
@@ -169,18 +154,7 @@ kq_status_t run_linear(const uint8_t* a_codes, const uint8_t* a_scales, const ui
     p.sf_row_tiles = (int)((R + 127) / 128);
     p.experts = experts;
     p.offsets = offsets;
-    kq::LinearEpilogue& ep = p.epi;
-    ep.N = N;
-    ep.act = e.activation;
-    ep.bias = {e.bias, experts ? R : 0, e.bias_dtype};
-    ep.gate = {e.gate, e.gate_stride, e.gate_dtype};
-    // (one gate row for all is one gate row, whatever rows_per_gate says: a warp then reads it once instead of a lane each for its row)
-    ep.rows_per_gate = !e.gate || !e.gate_stride || e.rows_per_gate > M ? (int)M : (int)e.rows_per_gate;
-    ep.row_scale = e.row_scale;
-    ep.residual = e.residual; ep.residual_type = e.residual_dtype; ep.ld_residual = e.ld_residual; ep.residual_scale = e.residual_scale;
-    ep.out = out; ep.out_type = out_dtype; ep.ld_out = ld_out;
-    ep.vec = rows_aligned(out, ld_out, out_dtype, 16) && rows_aligned(e.residual, e.ld_residual, e.residual_dtype, 16);
-    ep.wide = rows_aligned(out, ld_out, out_dtype, 32);
+    fill_epilogue(p.epi, e, M, N, experts ? R : 0, out, out_dtype, ld_out);
     cudaStream_t st = reinterpret_cast<cudaStream_t>(stream);
     // Few rows per weight: the weight is the wide operand and is what is read.  Narrow against pair kernel, us: dense N x K = 4096 x
     // 4096 8.3 / 11.6 (1 row), 9.0 / 11.4 (32), 11.0 / 11.7 (64), 15.5 / 12.7 (128); 12288 x 2240 7.3 / 11.9, 11.7 / 10.7 (32), 16.8 / 11.1;
@@ -194,6 +168,26 @@ kq_status_t run_linear(const uint8_t* a_codes, const uint8_t* a_scales, const ui
     if (M <= 64) return e.glu ? launch_narrow<true, 64>(l, enc, sms, st) : launch_narrow<false, 64>(l, enc, sms, st);
     return e.glu ? launch_narrow<true, 128>(l, enc, sms, st) : launch_narrow<false, 128>(l, enc, sms, st);
 }
+
+// ---- rows in 16 bits ----------------------------------------------------------------------------------
+
+template <bool GLU, int NT, bool XF16>
+kq_status_t launch_w4a16(const kq::W4A16Problem& p, int tiles, int splits, cudaStream_t st) {
+    constexpr int kBytes = kq::W4Smem<NT>::kBytes;
+    static DeviceOnce attr_done;
+    if (attr_done.needed()) {
+        if (cudaFuncSetAttribute(kq::linear_w4a16_kernel<GLU, NT, XF16>, cudaFuncAttributeMaxDynamicSharedMemorySize, kBytes) != cudaSuccess) {
+            (void)cudaGetLastError();
+            return KQ_ERR_CUDA;
+        }
+        attr_done.done();
+    }
+    cudaLaunchConfig_t cfg;
+    cudaLaunchAttribute attr[2];
+    launch_config(&cfg, attr, dim3((unsigned)(tiles * splits), (unsigned)((p.lin.M + 8 * NT - 1) / (8 * NT))), dim3(kq::kW4Threads), kBytes, splits, st);
+    return launch(cfg, kq::linear_w4a16_kernel<GLU, NT, XF16>, p, splits);
+}
+constexpr int kW4MaxRows = 64;
 
 // ---- norms ------------------------------------------------------------------------------------------
 
@@ -413,6 +407,48 @@ kq_status_t kroquant_linear_mxfp4_grouped(const uint8_t* a_codes, const uint8_t*
     if (experts < 1 || experts > kq::kMaxExperts) return KQ_ERR_SHAPE;
     if (reinterpret_cast<uintptr_t>(offsets) % 4) return KQ_ERR_ALIGN;
     return run_linear(a_codes, a_scales, b_codes, b_scales, offsets, experts, M, N, K, epilogue, out, out_dtype, ld_out, stream);
+}
+
+kq_status_t kroquant_linear_w4a16(const void* x, kq_xdtype_t x_dtype, int64_t ld_x, const uint8_t* b_codes, const uint8_t* b_scales, int64_t M,
+                                  int N, int K, const kq_epilogue_t* epilogue, void* out, kq_dtype_t out_dtype, int64_t ld_out, void* stream) {
+    kq_epilogue_t e;
+    if (epilogue) e = *epilogue; else kroquant_epilogue_default(&e);
+    if (!b_codes || !b_scales || (M > 0 && (!x || !out))) return KQ_ERR_NULL;
+    if (x_dtype != KQ_X_BF16 && x_dtype != KQ_X_FP16) return KQ_ERR_UNSUPPORTED;
+    if (M < 0 || M > kW4MaxRows || ld_x < K) return KQ_ERR_SHAPE;
+    const kq_status_t rc = check_epilogue(e, N, K, out, out_dtype, ld_out);
+    if (rc != KQ_OK) return rc;
+    if (reinterpret_cast<uintptr_t>(x) % 2 || !aligned16(b_codes) || !aligned16(b_scales)) return KQ_ERR_ALIGN;
+    if (M == 0) return KQ_OK;
+    const int sms = sm_count();
+    if (sms <= 0) return KQ_ERR_CUDA;
+    const int64_t R = e.glu ? (int64_t)64 * ((N + 31) / 32) : N;
+    kq::W4A16Problem p = {};
+    p.lin.M = (int)M;
+    p.lin.R = (int)R;
+    fill_epilogue(p.lin.epi, e, M, N, 0, out, out_dtype, ld_out);
+    p.x = x;
+    p.ld_x = ld_x;
+    p.x_vec = reinterpret_cast<uintptr_t>(x) % 16 == 0 && (M == 1 || ld_x % 8 == 0);
+    p.K = K;
+    p.units = (K + 127) / 128;
+    p.codes = b_codes;
+    p.scales = b_scales;
+    const int tiles = (int)((R + 127) / 128);
+    // as many CTAs of a cluster along K as two CTAs per SM have room for, two units each at least
+    const int runs = M <= 8 ? 1 : (int)((M + 15) / 16);
+    int splits = 1;
+    while (splits < 8 && (int64_t)tiles * runs * (splits + 1) <= 2 * sms && p.units >= 2 * (splits + 1)) ++splits;
+    cudaStream_t st = reinterpret_cast<cudaStream_t>(stream);
+    auto go = [&](auto glu, auto nt) {
+        constexpr bool GLU = decltype(glu)::value;
+        constexpr int NT = decltype(nt)::value;
+        return x_dtype == KQ_X_FP16 ? launch_w4a16<GLU, NT, true>(p, tiles, splits, st) : launch_w4a16<GLU, NT, false>(p, tiles, splits, st);
+    };
+    using One = std::integral_constant<int, 1>;
+    using Two = std::integral_constant<int, 2>;
+    if (M <= 8) return e.glu ? go(std::true_type{}, One{}) : go(std::false_type{}, One{});
+    return e.glu ? go(std::true_type{}, Two{}) : go(std::false_type{}, Two{});
 }
 
 void kroquant_norm_args_default(kq_norm_args_t* a) {
