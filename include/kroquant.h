@@ -440,7 +440,8 @@ kq_status_t kroquant_norm_residual_grad(const kq_norm_args_t *args, void *scratc
  * The angle is formed and reduced in 64 bits, so that it keeps its digits far from 0; sine and cosine are 32-bit values.  inverse = 1
  * turns by -angle: the backward pass (gradients in, gradients out).  Pairs are the channels (2p, 2p + 1) (INTERLEAVED) or (p, p + P)
  * (HALF).  One or two tensors (queries and keys, x[1] may be NULL) of one type, any strides in elements with contiguous channels;
- * out[i] may be x[i] (same strides) and overlaps no other tensor.  head_dim <= 512, batches * tokens < 2^31. */
+ * out[i] may be x[i] (same strides) and overlaps no other tensor.  head_dim <= 512, batches * tokens < 2^31, token and head strides
+ * below 2^31. */
 typedef enum { KQ_ROTARY_INTERLEAVED = 0, KQ_ROTARY_HALF = 1 } kq_rotary_layout_t;
 
 typedef struct kq_rotary_args {

@@ -10,6 +10,7 @@ from __future__ import annotations
 import contextlib
 import ctypes as C
 import os
+import struct
 import threading
 from typing import Optional
 
@@ -179,6 +180,8 @@ def _allocating(stream):
 
 def _empty_rows(like: torch.Tensor, dtype, stream) -> torch.Tensor:
     """A tensor of like's shape with rows one after the other (empty_like costs 1 us of a call, new_empty with a shape 2)."""
+    if stream is None and like.dtype is dtype and like.is_contiguous():
+        return torch.empty_like(like)
     if stream is None:
         return torch.empty_like(like, dtype=dtype, memory_format=torch.contiguous_format)
     with _allocating(stream):
@@ -968,6 +971,7 @@ def kroquant_norm_residual_grad(dn: Optional[torch.Tensor], h: torch.Tensor, *, 
 
 # ---- one step over new tokens: positions, the cache of keys and values, attention --------------------------------------
 ROTARY_LAYOUTS = {"interleaved": 0, "half": 1}
+_NO_AXES = (0, 0, 0, 0)
 CACHE_FORMATS = {"16bit": 0, "mxfp8": 1, "mxfp4": 2}
 
 
@@ -1003,6 +1007,12 @@ class _AttentionArgs(C.Structure):
                  ("scale", C.c_float), ("lse", C.c_void_p)])
 
 
+# The same structs as bytes: packing one takes 1 us of a call, filling a ctypes structure 4.
+_PACK_ROTARY = struct.Struct("@iqq8iPPiqq4P2i12q").pack
+_PACK_ROWS = struct.Struct("@qiPqiPPiPPqqqq").pack
+_PACK_ATTENTION = struct.Struct("@4iPPqqqqPqiPifP").pack
+
+
 def rotary_frequencies(axes, theta: float = 10000.0, device="cuda") -> torch.Tensor:
     """float64 [sum(axes) / 2]: theta ** (-2 i / a) for the a / 2 pairs of every axis of a channels."""
     return torch.cat([theta ** (-torch.arange(0, a, 2, dtype=torch.float64) / a) for a in axes]).to(device)
@@ -1027,7 +1037,7 @@ def _span(t: torch.Tensor):
 
 
 def _heads_last(t: torch.Tensor, what: str, dims: int, dtypes=_DTYPES) -> None:
-    if t.dim() != dims or t.dtype not in dtypes or t.get_device() != _device() or (t.shape[-1] > 1 and t.stride(-1) != 1):
+    if t.dim() != dims or t.dtype not in dtypes or t.get_device() != _device() or (t.stride(-1) != 1 and t.shape[-1] > 1):
         raise ValueError(f"{what} must be a {dims}-D CUDA tensor of {', '.join(str(d)[6:] for d in dtypes)} on the current device with contiguous channels")
 
 
@@ -1064,9 +1074,10 @@ def kroquant_rotary(q: torch.Tensor, k: Optional[torch.Tensor], positions: torch
         raise ValueError(f"layout must be one of {sorted(ROTARY_LAYOUTS)}")
     if positions.dtype not in (torch.int32, torch.float32) or positions.get_device() != dev:
         raise ValueError("positions must be a CUDA int32 or float32 tensor")
-    if n == 1 and positions.dim() == 1:
-        positions = positions.unsqueeze(1)
-    if positions.shape != (tokens, n) and (dims != 4 or positions.shape != (batches, tokens, n)) or (n > 1 and positions.stride(-1) != 1):
+    place, ps = positions.shape, positions.stride()
+    if n == 1 and len(place) == 1:
+        place, ps = (place[0], 1), (ps[0], 1)
+    if place != (tokens, n) and (dims != 4 or place != (batches, tokens, n)) or (n > 1 and ps[-1] != 1):
         raise ValueError("positions must be [tokens, axes], or [batch, tokens, axes], with contiguous axes")
     outs = (None, None) if out is None else (out, None) if k is None else tuple(out)
     made = []
@@ -1084,21 +1095,23 @@ def kroquant_rotary(q: torch.Tensor, k: Optional[torch.Tensor], positions: torch
                 raise ValueError("out may be its input, but must not overlap it in another way")
         made.append(o)
 
-    def strides(t):
-        s = t.stride()
-        return (0, s[0], s[1]) if dims == 3 else s[:3]
-
-    xs, os = strides(q), strides(made[0])
-    if k is None:
-        second, ks, ko = (None, None, 0), (0, 0, 0), (0, 0, 0)
+    if dims == 3:
+        (xt, xh, _), (ot, oh, _) = q.stride(), made[0].stride()
+        xb = ob = 0
     else:
-        second, ks, ko = (k.data_ptr(), made[1].data_ptr(), k.shape[-2]), strides(k), strides(made[1])
-    ps = positions.stride()
-    a = _RotaryArgs(_DTYPES[dtype], batches, tokens, d, way, 1 if inverse else 0, n, *axes, *(0,) * (4 - n), frequencies.data_ptr(),
-                    positions.data_ptr(), 1 if positions.dtype is torch.float32 else 0, ps[0] if len(ps) == 3 else 0, ps[-2],
-                    q.data_ptr(), second[0], made[0].data_ptr(), second[1], shape[-2], second[2], xs[0], ks[0], xs[1], ks[1], xs[2], ks[2],
-                    os[0], ko[0], os[1], ko[1], os[2], ko[2])
-    rc = load_library().kroquant_rotary(C.addressof(a), _stream(stream))
+        (xb, xt, xh, _), (ob, ot, oh, _) = q.stride(), made[0].stride()
+    if k is None:
+        k_at = ko_at = kv = kb = kt = kh = pb = pt = ph = 0
+    else:
+        k_at, ko_at, kv, kb, pb = k.data_ptr(), made[1].data_ptr(), k.shape[-2], 0, 0
+        if dims == 3:
+            (kt, kh, _), (pt, ph, _) = k.stride(), made[1].stride()
+        else:
+            (kb, kt, kh, _), (pb, pt, ph, _) = k.stride(), made[1].stride()
+    a = _PACK_ROTARY(_DTYPES[dtype], batches, tokens, d, way, 1 if inverse else 0, n, *axes, *_NO_AXES[n:], frequencies.data_ptr(),
+                     positions.data_ptr(), 1 if positions.dtype is torch.float32 else 0, ps[0] if len(ps) == 3 else 0, ps[-2],
+                     q.data_ptr(), k_at, made[0].data_ptr(), ko_at, shape[-2], kv, xb, kb, xt, kt, xh, kh, ob, pb, ot, pt, oh, ph)
+    rc = load_library().kroquant_rotary(a, _stream(stream))
     if rc:
         raise KroQuantError(rc, "kroquant_rotary")
     return made[0] if k is None else (made[0], made[1])
@@ -1177,10 +1190,11 @@ def _table(cache: KVCache, table: torch.Tensor):
 
 def _cache_rows(call: str, cache: KVCache, k, v, rows, where, offsets, starts, stream) -> None:
     n, table, stride, width = where
-    a = _CacheRows(rows, n, table, stride, width, None if offsets is None else _int_vector(offsets, n + 1, cache._device, "offsets"),
-                   None if starts is None else _int_vector(starts, n, cache._device, "starts"), _DTYPES[k.dtype], k.data_ptr(), v.data_ptr(),
-                   k.stride(0), k.stride(1), v.stride(0), v.stride(1))
-    rc = getattr(load_library(), call)(cache._at, C.addressof(a), _stream(stream))
+    (k_row, k_head, _), (v_row, v_head, _) = k.stride(), v.stride()
+    a = _PACK_ROWS(rows, n, table, stride, width, 0 if offsets is None else _int_vector(offsets, n + 1, cache._device, "offsets"),
+                   0 if starts is None else _int_vector(starts, n, cache._device, "starts"), _DTYPES[k.dtype], k.data_ptr(), v.data_ptr(),
+                   k_row, k_head, v_row, v_head)
+    rc = getattr(load_library(), call)(cache._at, a, _stream(stream))
     if rc:
         raise KroQuantError(rc, call)
 
@@ -1252,21 +1266,22 @@ def kroquant_cache_attention(q: torch.Tensor, cache: KVCache, table: torch.Tenso
         _heads_last(out, "out", 3)
         if out.shape != q.shape or out_dtype not in (None, out.dtype) or not _apart(out):
             raise ValueError("out must have q's shape and elements of its own")
-    lib = load_library()
-    a = _AttentionArgs(n, heads, _DTYPES[q.dtype], _DTYPES[out.dtype], q.data_ptr(), out.data_ptr(), q.stride(0), q.stride(1), out.stride(0),
-                       out.stride(1), where[1], where[2], where[3], _int_vector(lengths, n, cache._device, "lengths"), min(window, 0x7FFFFFFF),
-                       d ** -0.5 if scale is None else scale, None)
-    at = C.addressof(a)
-    nbytes = lib.kroquant_cache_attention_scratch_bytes(cache._at, at)
-    logs = scratch = None
-    if lse or nbytes:
+    lib, logs, scratch = load_library(), None, None
+    if lse:
         with _allocating(stream):
-            if lse:
-                logs = torch.empty((n, heads), dtype=torch.float32, device=q.device)
-                a.lse = logs.data_ptr()
-            if nbytes:
+            logs = torch.empty((n, heads), dtype=torch.float32, device=q.device)
+    (q_row, q_head, _), (o_row, o_head, _) = q.stride(), out.stride()
+    a = _PACK_ATTENTION(n, heads, _DTYPES[q.dtype], _DTYPES[out.dtype], q.data_ptr(), out.data_ptr(), q_row, q_head, o_row, o_head,
+                        where[1], where[2], where[3], _int_vector(lengths, n, cache._device, "lengths"), min(window, 0x7FFFFFFF),
+                        d ** -0.5 if scale is None else scale, 0 if logs is None else logs.data_ptr())
+    nbytes = lib.kroquant_cache_attention_scratch_bytes(cache._at, a)
+    if nbytes:
+        if stream is None:
+            scratch = torch.empty(nbytes, dtype=torch.uint8, device=q.device)
+        else:
+            with _allocating(stream):
                 scratch = torch.empty(nbytes, dtype=torch.uint8, device=q.device)
-    rc = lib.kroquant_cache_attention(cache._at, at, None if scratch is None else scratch.data_ptr(), nbytes, _stream(stream))
+    rc = lib.kroquant_cache_attention(cache._at, a, None if scratch is None else scratch.data_ptr(), nbytes, _stream(stream))
     if rc:
         raise KroQuantError(rc, "kroquant_cache_attention")
     return (out, logs) if lse else out

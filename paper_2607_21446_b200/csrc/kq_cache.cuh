@@ -7,10 +7,11 @@
 // lines.  Encoder per 32 channels, as in the quantizer:  S = max(floor(log2 amax) - e + 127, 0),  code = rn(y 2^(127 - S)), saturating.
 //
 // Both directions are bound by memory (2 bytes of 16-bit values and 0.53, 1.03 or 2 bytes of cache per element) or, for a few rows,
-// by latency.  A thread takes 8 channels of a row at a time, 16 bytes of it; the four threads of a block of 32 channels exchange
-// its largest magnitude by two shuffles.  The place of a row (a search of offsets by one warp, 32 entries at a time, and one table
-// entry) is found once per CTA and row.
+// by latency.  A thread keeps a place within a row, 16 channels of one head, and walks the rows of its CTA, so that what it computes
+// per 16 channels is two addresses and the code; the two threads of a block of 32 channels exchange its largest magnitude by one
+// shuffle.  The cell of a row (a search of offsets by one warp, 32 entries at a time, and one table entry) is found once per CTA and row.
 #pragma once
+#include "kq_mma16.cuh"
 #include "kq_rotary.cuh"
 
 namespace kq {
@@ -28,13 +29,13 @@ struct CacheRef {
     __host__ __device__ int row_bytes() const { return format == kCache16 ? 64 * blocks : format == kCacheFp8 ? 32 * blocks : 16 * blocks; }
 };
 
-struct CachePlace { int page, slot; };   // page -1: no place, -2: a row of no sequence
-__device__ __forceinline__ CachePlace cache_place(const CacheRef& c, const int32_t* table_row, int table_width, int64_t position) {
-    if (position < 0 || position >= (int64_t)table_width * c.page_size) return {-1, 0};
+// Cell of head 0 at a position (the heads' cells are page_size apart), -1 without a place.
+__device__ __forceinline__ int64_t cache_cell(const CacheRef& c, const int32_t* table_row, int table_width, int64_t position) {
+    if (position < 0 || position >= (int64_t)table_width * c.page_size) return -1;
     const uint32_t entry = position < 0x7FFFFFFF ? c.by_page.div((uint32_t)position) : (uint32_t)(position / c.page_size);
     const int page = __ldg(table_row + entry);
-    if (page < 0 || page >= c.pages) return {-1, 0};
-    return {page, (int)(position - (int64_t)entry * c.page_size)};
+    if (page < 0 || page >= c.pages) return -1;
+    return (int64_t)page * c.heads * c.page_size + (position - (int64_t)entry * c.page_size);
 }
 
 struct CacheRows {
@@ -47,8 +48,8 @@ struct CacheRows {
     void *k, *v;
     int64_t k_row, k_head, v_row, v_head;
     int rows_per_cta;
-    int units;                           // of a row: heads * groups
-    FastDiv by_units, by_groups;         // units of a row, groups of 8 channels of a head
+    int units;                           // of a row: heads * groups of 16 channels
+    FastDiv by_groups;
 };
 
 // The last sequence whose offset is <= row, by one warp: 32 entries at a time.
@@ -65,22 +66,23 @@ __device__ __forceinline__ int find_sequence(const int32_t* offsets, int sequenc
     }
     return lo;
 }
-// places[i]: of row row0 + i.  All warps of the CTA.
-__device__ __forceinline__ void find_places(const CacheRef& c, const CacheRows& p, int64_t row0, int rows, CachePlace* places) {
-    const int lane = threadIdx.x & 31;
-    for (int i = threadIdx.x >> 5; i < rows; i += blockDim.x >> 5) {
-        const int64_t row = row0 + i;
-        int s = (int)row;
-        int64_t first = row;
-        bool exists = true;
-        if (p.offsets) {
-            s = find_sequence(p.offsets, p.sequences, row, lane);
-            first = __ldg(p.offsets + s);
-            exists = row >= first && row < __ldg(p.offsets + s + 1);
+// cells[i]: of row row0 + i for head 0; -1: no place, -2: a row of no sequence.  All threads of the CTA.
+__device__ __forceinline__ void find_cells(const CacheRef& c, const CacheRows& p, int64_t row0, int rows, int64_t* cells, int thread, int threads) {
+    const int lane = thread & 31, whole = threads >> 5;                   // (a last warp that is not whole leaves the search to the others)
+    if (!p.offsets) {
+        for (int i = thread; i < rows; i += threads) {
+            const int64_t s = row0 + i;
+            cells[i] = cache_cell(c, p.table + s * p.table_stride, p.table_width, p.starts ? (int64_t)__ldg(p.starts + s) : 0);
         }
-        if (lane == 0) {
-            const int64_t position = (p.starts ? (int64_t)__ldg(p.starts + s) : 0) + (row - first);
-            places[i] = exists ? cache_place(c, p.table + (int64_t)s * p.table_stride, p.table_width, position) : CachePlace{-2, 0};
+    } else if (thread >> 5 < whole) {
+        for (int i = thread >> 5; i < rows; i += whole) {
+            const int64_t row = row0 + i;
+            const int s = find_sequence(p.offsets, p.sequences, row, lane);
+            if (lane == 0) {
+                const int64_t first = __ldg(p.offsets + s), position = (p.starts ? (int64_t)__ldg(p.starts + s) : 0) + (row - first);
+                const bool exists = row >= first && row < __ldg(p.offsets + s + 1);
+                cells[i] = exists ? cache_cell(c, p.table + (int64_t)s * p.table_stride, p.table_width, position) : -2;
+            }
         }
     }
     __syncthreads();
@@ -98,174 +100,201 @@ __device__ __forceinline__ uint2 e4m3x8(const float (&v)[8]) {
     }
     return make_uint2(h[0] | (h[1] << 16), h[2] | (h[3] << 16));
 }
-__device__ __forceinline__ float2 e4m3x2_to_float2(uint32_t two) {
-    uint32_t h2;
-    asm("cvt.rn.f16x2.e4m3x2 %0, %1;" : "=r"(h2) : "h"((uint16_t)two));
-    return __half22float2(*reinterpret_cast<const __half2*>(&h2));
+__device__ __forceinline__ void store_32_bytes(void* p, uint32_t a, uint32_t b, uint32_t c, uint32_t d, uint32_t e, uint32_t f, uint32_t g, uint32_t h) {
+    asm volatile("st.global.v8.b32 [%0], {%1,%2,%3,%4,%5,%6,%7,%8};"
+                 ::"l"(p), "r"(a), "r"(b), "r"(c), "r"(d), "r"(e), "r"(f), "r"(g), "r"(h) : "memory");
 }
 
-constexpr int kCacheThreads = 256;
+constexpr int kCacheThreads = 256;       // at most, and at least 32
 constexpr int kCacheRowsMax = 64;        // rows of a CTA
 
-// blockIdx.y: keys, values.  T: type of the rows.  VEC: rows allow 16-byte accesses and head_dim is a multiple of 8.
+// blockDim: x = units of a row (or 256 of them), y = rows at a time.  blockIdx.y: keys, values.  T: type of the rows.  VEC: rows allow
+// 16-byte accesses and head_dim is a multiple of 8.
 template <typename T, int FORMAT, bool VEC>
 __global__ void __launch_bounds__(kCacheThreads) cache_write_kernel(const __grid_constant__ CacheRef c, const __grid_constant__ CacheRows p) {
-    __shared__ CachePlace places[kCacheRowsMax];
+    __shared__ int64_t cells[kCacheRowsMax];
     pdl_launch_dependents();
     pdl_wait_prior_grid();
     const int64_t row0 = (int64_t)blockIdx.x * p.rows_per_cta;
     const int rows = (int)(p.rows - row0 < p.rows_per_cta ? p.rows - row0 : p.rows_per_cta);
-    find_places(c, p, row0, rows, places);
+    const int thread = threadIdx.y * blockDim.x + threadIdx.x;
+    find_cells(c, p, row0, rows, cells, thread, blockDim.x * blockDim.y);
     const bool values = blockIdx.y != 0;
-    const T* src = static_cast<const T*>(values ? p.v : p.k);
     const int64_t row_stride = values ? p.v_row : p.k_row, head_stride = values ? p.v_head : p.k_head;
-    uint8_t* codes = values ? c.v : c.k;
-    uint8_t* scales = values ? c.v_scales : c.k_scales;
-    const int groups = 4 * c.blocks, total = rows * p.units, row_bytes = c.row_bytes();
-    // (units of a block of 32 channels are four neighbours: whole quads of lanes pass or fail every test below but the channel's)
-    for (int u = threadIdx.x; u < total; u += kCacheThreads) {
-        const int r = (int)p.by_units.div((uint32_t)u), rest = u - r * p.units;
-        const int head = (int)p.by_groups.div((uint32_t)rest), g = rest - head * groups;
-        const CachePlace place = places[r];
-        if (place.page < 0) continue;
-        const int64_t cell = ((int64_t)place.page * c.heads + head) * c.page_size + place.slot;
-        const T* at = src + (row0 + r) * row_stride + head * head_stride + 8 * g;
-        const int left = c.head_dim - 8 * g;
-        uint32_t w[4] = {0, 0, 0, 0};                                    // eight 16-bit values
-        if (VEC) {
-            if (left > 0) {
-                const uint4 q = ld_stream_16(at);
-                w[0] = q.x; w[1] = q.y; w[2] = q.z; w[3] = q.w;
+    const T* src = static_cast<const T*>(values ? p.v : p.k) + row0 * row_stride;
+    const int groups = 2 * c.blocks;
+    const uint32_t row_bytes = (uint32_t)c.row_bytes();
+    // (the units of a block of 32 channels are two neighbouring lanes, which pass or fail every test but the channel's together)
+    const uint32_t pair = 3u << (thread & 30);
+    for (int u = threadIdx.x; u < p.units; u += blockDim.x) {
+        const int head = (int)p.by_groups.div((uint32_t)u), g = u - head * groups, left = c.head_dim - 16 * g;
+        const T* from = src + head * head_stride + 16 * g;
+        const uint64_t head_cells = (uint64_t)head * c.page_size;
+        uint8_t* codes = (values ? c.v : c.k) + head_cells * row_bytes + g * (FORMAT == kCache16 ? 32 : FORMAT == kCacheFp8 ? 16 : 8);
+        uint8_t* scales = (values ? c.v_scales : c.k_scales) + head_cells * c.scale_row + (g >> 1);
+#pragma unroll 2
+        for (int r = threadIdx.y; r < rows; r += blockDim.y) {
+            const int64_t cell = cells[r];
+            if (cell < 0) continue;
+            const T* at = from + r * row_stride;
+            uint32_t w[8];                                               // sixteen 16-bit values
+            if (VEC) {
+                const uint4 zero = make_uint4(0, 0, 0, 0);
+                const uint4 a = left > 0 ? ld_stream_16(at) : zero, b = left > 8 ? ld_stream_16(at + 8) : zero;
+                w[0] = a.x; w[1] = a.y; w[2] = a.z; w[3] = a.w; w[4] = b.x; w[5] = b.y; w[6] = b.z; w[7] = b.w;
+            } else {
+                const uint16_t* q = reinterpret_cast<const uint16_t*>(at);
+#pragma unroll
+                for (int i = 0; i < 8; ++i)
+                    w[i] = (2 * i < left ? (uint32_t)q[2 * i] : 0u) | (2 * i + 1 < left ? (uint32_t)q[2 * i + 1] << 16 : 0u);
             }
-        } else {
-            const uint16_t* q = reinterpret_cast<const uint16_t*>(at);
+            uint8_t* to = codes + (uint64_t)(uint32_t)cell * row_bytes;
+            if constexpr (FORMAT == kCache16) {
+                reinterpret_cast<uint4*>(to)[0] = make_uint4(w[0], w[1], w[2], w[3]);
+                reinterpret_cast<uint4*>(to)[1] = make_uint4(w[4], w[5], w[6], w[7]);
+            } else {
+                float v[8], x[8];
+                widen8_any<__is_same(T, __half)>(make_uint4(w[0], w[1], w[2], w[3]), v);
+                widen8_any<__is_same(T, __half)>(make_uint4(w[4], w[5], w[6], w[7]), x);
+                float amax = fmaxf(absmax8(v), absmax8(x));
+                amax = fmaxf(amax, __shfl_xor_sync(pair, amax, 1));
+                const int e = (int)((__float_as_uint(amax) >> 23) & 0xFFu) - (FORMAT == kCacheFp8 ? 8 : 2);
+                const uint32_t S = (uint32_t)(e < 0 ? 0 : e);
+                const float inv = inv_scale_from_e8m0(S);
 #pragma unroll
-            for (int i = 0; i < 8; ++i)
-                if (i < left) w[i / 2] |= (uint32_t)q[i] << (16 * (i & 1));
-        }
-        if constexpr (FORMAT == kCache16) {
-            *reinterpret_cast<uint4*>(codes + cell * row_bytes + 16 * g) = make_uint4(w[0], w[1], w[2], w[3]);
-        } else {
-            float v[8];
-            widen8_any<__is_same(T, __half)>(make_uint4(w[0], w[1], w[2], w[3]), v);
-            float amax = absmax8(v);
-            const uint32_t quad = 0xFu << (threadIdx.x & 28);
-            amax = fmaxf(amax, __shfl_xor_sync(quad, amax, 1));
-            amax = fmaxf(amax, __shfl_xor_sync(quad, amax, 2));
-            const int e = (int)((__float_as_uint(amax) >> 23) & 0xFFu) - (FORMAT == kCacheFp8 ? 8 : 2);
-            const uint32_t S = (uint32_t)(e < 0 ? 0 : e);
-            const float inv = inv_scale_from_e8m0(S);
-#pragma unroll
-            for (int i = 0; i < 8; ++i) v[i] *= inv;
-            if constexpr (FORMAT == kCacheFp8)
-                *reinterpret_cast<uint2*>(codes + cell * row_bytes + 8 * g) = e4m3x8(v);
-            else
-                *reinterpret_cast<uint32_t*>(codes + cell * row_bytes + 4 * g) = e2m1x8(v[0], v[1], v[2], v[3], v[4], v[5], v[6], v[7]);
-            if ((g & 3) == 0) {
-                uint8_t* s = scales + cell * c.scale_row;
-                s[g >> 2] = (uint8_t)S;
-                if ((g >> 2) == c.blocks - 1)
-                    for (int b = c.blocks; b < c.scale_row; ++b) s[b] = 0;
+                for (int i = 0; i < 8; ++i) {
+                    v[i] *= inv;
+                    x[i] *= inv;
+                }
+                if constexpr (FORMAT == kCacheFp8) {
+                    const uint2 a = e4m3x8(v), b = e4m3x8(x);
+                    *reinterpret_cast<uint4*>(to) = make_uint4(a.x, a.y, b.x, b.y);
+                } else {
+                    *reinterpret_cast<uint2*>(to) = make_uint2(e2m1x8(v[0], v[1], v[2], v[3], v[4], v[5], v[6], v[7]),
+                                                               e2m1x8(x[0], x[1], x[2], x[3], x[4], x[5], x[6], x[7]));
+                }
+                if ((g & 1) == 0) {
+                    uint8_t* s = scales + (uint64_t)(uint32_t)cell * c.scale_row;
+                    s[0] = (uint8_t)S;
+                    if ((g >> 1) == c.blocks - 1)
+                        for (int b = c.blocks; b < c.scale_row; ++b) s[b - c.blocks + 1] = 0;
+                }
             }
         }
     }
 }
 
+// sixteen values to a row of T: `width` 32 or 16 bytes at a time (all of them, or the first eight), or the first `left` one by one
 template <typename T>
-__device__ __forceinline__ void cache_store8(T* at, int left, bool vec, const float (&v)[8]) {
-    if (vec) {
-        if constexpr (sizeof(T) == 4) {
-            reinterpret_cast<float4*>(at)[0] = make_float4(v[0], v[1], v[2], v[3]);
-            reinterpret_cast<float4*>(at)[1] = make_float4(v[4], v[5], v[6], v[7]);
-        } else {
-            uint32_t w[4];
+__device__ __forceinline__ void cache_store16(T* at, int left, int width, const float (&v)[16]) {
+    if (width) {
+        constexpr int kWords = sizeof(T) == 4 ? 16 : 8;
+        uint32_t w[kWords];
 #pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                if constexpr (__is_same(T, __half)) {
-                    const __half2 h = __floats2half2_rn(v[2 * i], v[2 * i + 1]);
-                    w[i] = *reinterpret_cast<const uint32_t*>(&h);
-                } else {
-                    const __nv_bfloat162 h = __floats2bfloat162_rn(v[2 * i], v[2 * i + 1]);
-                    w[i] = *reinterpret_cast<const uint32_t*>(&h);
-                }
+        for (int i = 0; i < 8; ++i) {
+            if constexpr (sizeof(T) == 4) {
+                w[2 * i] = __float_as_uint(v[2 * i]);
+                w[2 * i + 1] = __float_as_uint(v[2 * i + 1]);
+            } else if constexpr (__is_same(T, __half)) {
+                w[i] = pack_f16(v[2 * i], v[2 * i + 1]);
+            } else {
+                w[i] = pack_bf16(v[2 * i], v[2 * i + 1]);
             }
-            st_stream_16(at, make_uint4(w[0], w[1], w[2], w[3]));
+        }
+        uint32_t* to = reinterpret_cast<uint32_t*>(at);
+        if (width == 32) {
+#pragma unroll
+            for (int i = 0; i < kWords; i += 8) store_32_bytes(to + i, w[i], w[i + 1], w[i + 2], w[i + 3], w[i + 4], w[i + 5], w[i + 6], w[i + 7]);
+        } else {
+#pragma unroll
+            for (int i = 0; i < kWords; i += 4)
+                if (i < kWords / 2 || left > 8) st_stream_16(to + i, make_uint4(w[i], w[i + 1], w[i + 2], w[i + 3]));
         }
     } else {
 #pragma unroll
-        for (int i = 0; i < 8; ++i)
+        for (int i = 0; i < 16; ++i)
             if (i < left) at[i] = rotary_round<T>(v[i]);
     }
 }
 
-constexpr int kReadAhead = 4;            // units of a thread in flight
-
-// CF16: a 16-bit cache holds fp16 (else bf16).  T: type of the rows.
+// CF16: a 16-bit cache holds fp16 (else bf16).  T: type of the rows.  width: bytes of a store to them (32, 16 or, for any alignment, 0).
+// blockDim and blockIdx as above.
 template <typename T, int FORMAT, bool CF16>
-__global__ void __launch_bounds__(kCacheThreads) cache_read_kernel(const __grid_constant__ CacheRef c, const __grid_constant__ CacheRows p, const int vec) {
-    __shared__ CachePlace places[kCacheRowsMax];
+__global__ void __launch_bounds__(kCacheThreads) cache_read_kernel(const __grid_constant__ CacheRef c, const __grid_constant__ CacheRows p, const int width) {
+    constexpr int kAhead = FORMAT == kCache16 ? 2 : 4;                   // rows of a thread in flight
+    constexpr int kWords = FORMAT == kCache16 ? 8 : (FORMAT == kCacheFp8 ? 4 : 2);
+    __shared__ int64_t cells[kCacheRowsMax];
     pdl_launch_dependents();
     pdl_wait_prior_grid();
     const int64_t row0 = (int64_t)blockIdx.x * p.rows_per_cta;
     const int rows = (int)(p.rows - row0 < p.rows_per_cta ? p.rows - row0 : p.rows_per_cta);
-    find_places(c, p, row0, rows, places);
+    find_cells(c, p, row0, rows, cells, threadIdx.y * blockDim.x + threadIdx.x, blockDim.x * blockDim.y);
     const bool values = blockIdx.y != 0;
-    T* dst = static_cast<T*>(values ? p.v : p.k);
     const int64_t row_stride = values ? p.v_row : p.k_row, head_stride = values ? p.v_head : p.k_head;
-    const uint8_t* codes = values ? c.v : c.k;
-    const uint8_t* scales = values ? c.v_scales : c.k_scales;
-    const int groups = (c.head_dim + 7) / 8, total = rows * p.units, row_bytes = c.row_bytes();
-    for (int u0 = threadIdx.x; u0 < total; u0 += kReadAhead * kCacheThreads) {
-        uint4 w[kReadAhead];
-        uint32_t S[kReadAhead];
-        int left[kReadAhead];                                            // channels to write; 0: no unit
-        T* at[kReadAhead];
+    T* dst = static_cast<T*>(values ? p.v : p.k) + row0 * row_stride;
+    const int groups = (c.head_dim + 15) / 16, step = blockDim.y;
+    const uint32_t row_bytes = (uint32_t)c.row_bytes();
+    for (int u = threadIdx.x; u < p.units; u += blockDim.x) {
+        const int head = (int)p.by_groups.div((uint32_t)u), g = u - head * groups, left = c.head_dim - 16 * g;
+        T* to = dst + head * head_stride + 16 * g;
+        const uint64_t head_cells = (uint64_t)head * c.page_size;
+        const uint8_t* codes = (values ? c.v : c.k) + head_cells * row_bytes + g * 4 * kWords;
+        const uint8_t* scales = (values ? c.v_scales : c.k_scales) + head_cells * c.scale_row + (g >> 1);
+        for (int r0 = threadIdx.y; r0 < rows; r0 += kAhead * step) {
+            uint32_t w[kAhead][kWords], S[kAhead];
+            int64_t cell[kAhead];
 #pragma unroll
-        for (int k = 0; k < kReadAhead; ++k) {
-            const int u = u0 + k * kCacheThreads;
-            left[k] = 0;
-            w[k] = make_uint4(0, 0, 0, 0);
-            S[k] = 0;
-            if (u >= total) continue;
-            const int r = (int)p.by_units.div((uint32_t)u), rest = u - r * p.units;
-            const int head = (int)p.by_groups.div((uint32_t)rest), g = rest - head * groups;
-            const CachePlace place = places[r];
-            if (place.page == -2) continue;
-            left[k] = c.head_dim - 8 * g;
-            at[k] = dst + (row0 + r) * row_stride + head * head_stride + 8 * g;
-            if (place.page < 0) continue;
-            const int64_t cell = ((int64_t)place.page * c.heads + head) * c.page_size + place.slot;
-            if constexpr (FORMAT == kCache16) {
-                w[k] = ld_stream_16(codes + cell * row_bytes + 16 * g);
-            } else {
-                if constexpr (FORMAT == kCacheFp8) {
-                    const uint2 q = __ldg(reinterpret_cast<const uint2*>(codes + cell * row_bytes + 8 * g));
-                    w[k].x = q.x;
-                    w[k].y = q.y;
+            for (int k = 0; k < kAhead; ++k) {
+                cell[k] = r0 + k * step < rows ? cells[r0 + k * step] : -2;
+                S[k] = 0;
+#pragma unroll
+                for (int i = 0; i < kWords; ++i) w[k][i] = 0;
+                if (cell[k] < 0) continue;
+                const uint8_t* at = codes + (uint64_t)(uint32_t)cell[k] * row_bytes;
+                if constexpr (FORMAT == kCacheFp4) {
+                    const uint2 q = __ldg(reinterpret_cast<const uint2*>(at));
+                    w[k][0] = q.x; w[k][1] = q.y;
                 } else {
-                    w[k].x = __ldg(reinterpret_cast<const uint32_t*>(codes + cell * row_bytes + 4 * g));
-                }
-                S[k] = __ldg(scales + cell * c.scale_row + (g >> 2));
-            }
-        }
 #pragma unroll
-        for (int k = 0; k < kReadAhead; ++k) {
-            if (left[k] <= 0) continue;
-            float v[8];
-            if constexpr (FORMAT == kCache16) {
-                widen8_any<CF16>(w[k], v);
-            } else {
-                const float scale = scale_from_e8m0(S[k]);
-#pragma unroll
-                for (int i = 0; i < 4; ++i) {
-                    float2 f;
-                    if constexpr (FORMAT == kCacheFp8) f = e4m3x2_to_float2((i < 2 ? w[k].x : w[k].y) >> (16 * (i & 1)));
-                    else f = e2m1x2_to_float2((w[k].x >> (8 * i)) & 0xFFu);
-                    v[2 * i] = f.x * scale;
-                    v[2 * i + 1] = f.y * scale;
+                    for (int i = 0; i < kWords / 4; ++i) {
+                        const uint4 q = __ldg(reinterpret_cast<const uint4*>(at) + i);
+                        w[k][4 * i] = q.x; w[k][4 * i + 1] = q.y; w[k][4 * i + 2] = q.z; w[k][4 * i + 3] = q.w;
+                    }
                 }
+                if constexpr (FORMAT != kCache16) S[k] = __ldg(scales + (uint64_t)(uint32_t)cell[k] * c.scale_row);
             }
-            cache_store8<T>(at[k], left[k], vec != 0, v);
+#pragma unroll
+            for (int k = 0; k < kAhead; ++k) {
+                if (cell[k] == -2) continue;
+                T* at = to + (r0 + k * step) * row_stride;
+                float v[16];
+                if constexpr (FORMAT == kCache16) {
+                    float a[8], b[8];
+                    widen8_any<CF16>(make_uint4(w[k][0], w[k][1], w[k][2], w[k][3]), a);
+                    widen8_any<CF16>(make_uint4(w[k][4], w[k][5], w[k][6], w[k][7]), b);
+#pragma unroll
+                    for (int i = 0; i < 8; ++i) {
+                        v[i] = a[i];
+                        v[8 + i] = b[i];
+                    }
+                } else {
+                    const float scale = scale_from_e8m0(S[k]);
+#pragma unroll
+                    for (int i = 0; i < kWords; ++i) {
+                        uint32_t h[4];
+                        if constexpr (FORMAT == kCacheFp8) e4m3x4_to_f16(w[k][i], h[0], h[1]);
+                        else e2m1x8_to_f16(w[k][i], h);
+                        constexpr int kPairs = FORMAT == kCacheFp8 ? 2 : 4;
+#pragma unroll
+                        for (int q = 0; q < kPairs; ++q) {
+                            const float2 f = __half22float2(*reinterpret_cast<const __half2*>(&h[q]));
+                            v[2 * (kPairs * i + q)] = f.x * scale;
+                            v[2 * (kPairs * i + q) + 1] = f.y * scale;
+                        }
+                    }
+                }
+                cache_store16<T>(at, left, width, v);
+            }
         }
     }
 }

@@ -12,21 +12,22 @@
 // Operand order.  Any order of channels serves K Q^T, and any order of positions P^T as long as both products use the same, so that a
 // lane takes what lies together: of K, with j = lane % 4, whole 16-byte chunks of the rows of positions lane / 4 and lane / 4 + 8; of V,
 // with g = lane / 4, D/8 consecutive channels of four positions.  P^T is S^T with rows and columns of 8 x 8 blocks exchanged (movmatrix).
-// Chunks are stored permuted within a row so that both kinds of access take all banks.
+// Rows of codes are stored with pairs of chunks exchanged, rows of 16-bit values 16 bytes further apart, so that both kinds of access take
+// all banks (an asynchronous copy that puts the halves of 32 bytes apart takes several times as long).
 //
 // Scales.  A code times 2^(S - 127) would leave fp16, so K is taken relative to the largest scale byte of its position (a factor of the
 // score, fp32) and V relative to the largest of its position, which goes into P: p 2^(S_t - R + 14), R the largest S_t so far (a
-// running maximum that rescales the accumulator as m does).  Code times 2^(S - S_t) has at most 4 significant bits, exact in fp16 down to
-// 2^-24: what falls below is 2^-25 of a code's unit.  Queries are fp16 times a power of two per row, exact for both 16-bit types up to
-// values 2^-29 of the row's largest.  P is rounded to fp16 (11 bits; a weight below 2^-28 of the largest keeps fewer, which is 2^-39 of the
-// largest value at most), with bf16 values to two bf16 terms (16 bits).
+// running maximum that rescales the accumulator as m does).  Code times 2^(S - S_t + kLift) has at most 4 significant bits and is exact in
+// fp16; a block whose scale is 2^-28 (E2M1) or 2^-21 (E4M3) of its position's largest, or less, counts as zero.  The queries of a CTA are
+// fp16 times one power of two, exact for both 16-bit types down to values 2^-29 of the largest.  P is rounded to fp16 (11 bits; a weight
+// below 2^-28 of the largest keeps fewer, which is 2^-39 of the largest value at most), with bf16 values to two bf16 terms (16 bits).
 //
-// Work.  Tiles (4 steps) of all (sequence, head) items are laid end to end and every CTA takes an equal run of them: ragged batches
-// balance, one long sequence fills the GPU.  An item that ends within its CTA is written; the parts of others go to the scratch
-// space (at most two per CTA) and a second kernel joins them in order.  Lengths are read on the device.
+// Work.  Tiles (4 steps) of all (sequence, head) items are laid end to end, each item led by kLead tiles' worth of nothing for what
+// beginning and ending it costs, and every CTA takes an equal run: ragged batches balance, one long sequence fills the GPU.  An
+// item that lies within one CTA is written; the parts of others go to the scratch space (at most two per CTA) and a second
+// kernel joins them in order.  Lengths are read on the device.
 #pragma once
 #include "kq_cache.cuh"
-#include "kq_mma16.cuh"
 
 namespace kq {
 
@@ -38,7 +39,7 @@ struct AttentionProblem {
     CacheRef c;
     int sequences, q_heads, group, chunks;       // group: query heads of a cache head, taken in `chunks` runs
     const void* q;
-    int q_f16;
+    int q_f16, q_vec;                    // q_vec: 8-byte loads of four channels
     int64_t q_row, q_head;
     void* out;
     int out_type;
@@ -51,9 +52,14 @@ struct AttentionProblem {
     float scale_log2e;
     float* lse;
     float* partial;                      // [2 per CTA][NQ][D], then [2 per CTA][2][NQ]: maximum, sum.  null: items are taken whole
+    int2* parts;                         // of each item: first CTA and number of CTAs that took it; {., 1}: written
     int ctas;                            // of the attention kernel
-    int min_tiles;                       // smallest run of a CTA
+    int min_run;                         // smallest run of a CTA
 };
+
+// What an item costs besides its tiles, in tiles: queries, first copies, joining the warps.  24 sequences of 341 to 8192 positions: 63 us with 0,
+// 50 with 1, 49 with 2.
+constexpr int kLead = 1;
 
 // Positions of a sequence that its token sees, and their tiles (at least one, so that an empty row is written).
 struct VisibleRange { int begin, end; };
@@ -68,19 +74,6 @@ __device__ __forceinline__ int tiles_of(const VisibleRange& v) {
     const int n = v.end - v.begin;
     return n <= TN ? 1 : (n - 1) / TN + 1;
 }
-// Tiles of an item of sequences 0 .. upto - 1, by one warp; upto < 0: of all.
-template <int TN>
-__device__ __forceinline__ int64_t tiles_before(const AttentionProblem& p, int upto, int lane) {
-    int64_t sum = 0;
-    for (int s = lane; s < upto; s += 32) sum += tiles_of<TN>(visible_range(p, s));
-#pragma unroll
-    for (int o = 16; o > 0; o >>= 1) sum += __shfl_xor_sync(0xFFFFFFFFu, sum, o);
-    return sum;
-}
-__device__ __forceinline__ int64_t run_length(const AttentionProblem& p, int64_t total) {
-    const int64_t even = (total + p.ctas - 1) / p.ctas;
-    return even < p.min_tiles ? p.min_tiles : even;
-}
 
 __device__ __forceinline__ float exp2_fast(float x) {
     float y;
@@ -88,13 +81,13 @@ __device__ __forceinline__ float exp2_fast(float x) {
     return y;
 }
 __device__ __forceinline__ uint32_t shared_u32(const void* p) { return (uint32_t)__cvta_generic_to_shared(p); }
-// N bytes (4, 8 or 16), zeros where `exists` does not hold
+// 16 bytes of which the first `size` are copied and the others zero; 4 or 8 bytes, zeros where `exists` does not hold
+__device__ __forceinline__ void copy_async_16(uint32_t dst, const uint8_t* src, uint32_t size) {
+    asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst), "l"(src), "r"(size) : "memory");
+}
 template <int N>
-__device__ __forceinline__ void copy_async(uint32_t dst, const void* src, bool exists) {
-    if constexpr (N == 16)
-        asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst), "l"(src), "r"(exists ? 16 : 0) : "memory");
-    else
-        asm volatile("cp.async.ca.shared.global [%0], [%1], %3, %2;" ::"r"(dst), "l"(src), "r"(exists ? N : 0), "n"(N) : "memory");
+__device__ __forceinline__ void copy_async_small(uint32_t dst, const uint8_t* src, bool exists) {
+    asm volatile("cp.async.ca.shared.global [%0], [%1], %3, %2;" ::"r"(dst), "l"(src), "r"(exists ? N : 0), "n"(N) : "memory");
 }
 
 template <int FMT, int D, int NQ>
@@ -103,13 +96,15 @@ struct AttnShape {
     static constexpr int kBits = FMT == kAttnFp4 ? 4 : (FMT == kAttnFp8 ? 8 : 16);
     static constexpr int kStep = kCodes ? 32 : 16;               // positions of a step
     static constexpr int kTile = kStep * kAttnWarps;
-    static constexpr int kRow = D * kBits / 8;                   // bytes of a row in shared memory
-    static constexpr int kChunks = kRow / 16;
+    static constexpr int kChunks = D * kBits / 128;              // of 16 bytes in a row
+    static constexpr int kRow = 16 * kChunks + (kCodes ? 0 : 16);    // from row to row in shared memory
     static constexpr int kScaleRow = kCodes ? (D > 128 ? 8 : 4) : 0;
     static constexpr int kScaleOff = 2 * kStep * kRow;
     static constexpr int kMaskOff = kScaleOff + 2 * kStep * kScaleRow;
     static constexpr int kStageBytes = kMaskOff + 16;
-    static constexpr int kStages = D > 128 && !kCodes ? 2 : 3;
+    // Two stages: a third in the place of a CTA is slower (24 sequences, MXFP8: 57 us with two CTAs of three stages, 50 with three of two).
+    static constexpr int kStages = 2;
+    static constexpr int kLift = FMT == kAttnFp4 ? 13 : 6;       // largest code 2^kLift stays below 2^16
     static constexpr int kMulBytes = kCodes ? 2 * (D / 32) * kStep * 2 : 0;      // fp16 multipliers [K, V][block][position]
     static constexpr int kRing = kStages * kStageBytes;
     static constexpr int kWarpBytes = kRing + kMulBytes;
@@ -126,7 +121,7 @@ struct AttnShape {
 
     // where chunk c of a step's row r lies
     static __device__ __forceinline__ int chunk_at(int r, int c) {
-        if constexpr (!kCodes) return c ^ (r & 7);
+        if constexpr (!kCodes) return c;
         else if constexpr (kChunks >= 8) return c ^ (2 * (r & 3));
         else if constexpr (kChunks == 4) return c ^ (r & 2);
         else return c;
@@ -161,29 +156,41 @@ __global__ void __launch_bounds__(kAttnThreads, (AttnShape<FMT, D, NQ>::kPerSm))
     extern __shared__ __align__(16) uint8_t attn_smem[];
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, g = lane >> 2, j = lane & 3;
     uint8_t* ring = attn_smem + warp * L::kWarpBytes;
-    __half* mul = reinterpret_cast<__half*>(ring + L::kRing);
+    uint16_t* mul = reinterpret_cast<uint16_t*>(ring + L::kRing);
+    const int row_lane = L::row_of(lane & (L::kStep - 1));
     float* join = reinterpret_cast<float*>(attn_smem);
     float* stats = reinterpret_cast<float*>(attn_smem + L::kStatsOff);
     const int real_chunks = p.c.row_bytes() / 16, blocks = p.c.blocks;
     const bool padded = real_chunks < L::kChunks;
+    // what a lane copies: chunk lane % kChunks of every row
+    const bool lane_copies = lane % L::kChunks < real_chunks;
+    const uint32_t ring_at = shared_u32(ring), copy_row = lane / L::kChunks * L::kRow;
+    const uint8_t *k_lane = p.c.k + 16 * (lane % L::kChunks), *v_lane = p.c.v + 16 * (lane % L::kChunks);
+    const uint32_t row_bytes = (uint32_t)p.c.row_bytes(), pages = (uint32_t)p.c.pages, heads = (uint32_t)p.c.heads, page_size = (uint32_t)p.c.page_size;
+    constexpr uint32_t kFull = L::kStep == 32 ? 0xFFFFFFFFu : (1u << L::kStep) - 1u;
     const uint32_t byte_mask0 = blocks >= 4 ? 0xFFFFFFFFu : (1u << (8 * blocks)) - 1u;
     const uint32_t byte_mask1 = blocks >= 8 ? 0xFFFFFFFFu : (blocks <= 4 ? 0u : (1u << (8 * (blocks - 4))) - 1u);
     pdl_launch_dependents();
     pdl_wait_prior_grid();
 
-    // ---- this CTA's run of tiles ----
+    // ---- this CTA's run ----
     const int per_seq = p.c.heads * p.chunks;
     int64_t at = 0, stop = 0, quota = 0;
-    int seq = 0, item = 0, tile = 0;
+    int seq = 0, item = 0, unit = 0;                                     // unit: of the item, kLead and then its tiles
     if (p.partial) {
-        const int64_t total = tiles_before<L::kTile>(p, p.sequences, lane) * per_seq;
-        quota = run_length(p, total);
+        int64_t sum = 0;
+        for (int s = lane; s < p.sequences; s += 32) sum += tiles_of<L::kTile>(visible_range(p, s)) + kLead;
+#pragma unroll
+        for (int o = 16; o > 0; o >>= 1) sum += __shfl_xor_sync(0xFFFFFFFFu, sum, o);
+        const int64_t total = sum * per_seq;
+        quota = (total + p.ctas - 1) / p.ctas;
+        if (quota < p.min_run) quota = p.min_run;
         at = blockIdx.x * quota;
         stop = at + quota < total ? at + quota : total;
         if (at >= stop) return;
-        int64_t before = 0;                                              // tiles per head of the sequences before
+        int64_t before = 0;                                              // units per head of the sequences before
         for (int s0 = 0;; s0 += 32) {
-            const int n = s0 + lane < p.sequences ? tiles_of<L::kTile>(visible_range(p, s0 + lane)) : 0;
+            const int n = s0 + lane < p.sequences ? tiles_of<L::kTile>(visible_range(p, s0 + lane)) + kLead : 0;
             int64_t upto = n;
 #pragma unroll
             for (int o = 1; o < 32; o <<= 1) {
@@ -194,10 +201,10 @@ __global__ void __launch_bounds__(kAttnThreads, (AttnShape<FMT, D, NQ>::kPerSm))
             if (past) {
                 const int first = __ffs(past) - 1;
                 seq = s0 + first;
-                const int tiles = __shfl_sync(0xFFFFFFFFu, n, first);
-                const int64_t rest = at - (before + __shfl_sync(0xFFFFFFFFu, upto, first) - tiles) * per_seq;
-                item = (int)(rest / tiles);
-                tile = (int)(rest - (int64_t)item * tiles);
+                const int units = __shfl_sync(0xFFFFFFFFu, n, first);
+                const int64_t rest = at - (before + __shfl_sync(0xFFFFFFFFu, upto, first) - units) * per_seq;
+                item = (int)(rest / units);
+                unit = (int)(rest - (int64_t)item * units);
                 break;
             }
             before += __shfl_sync(0xFFFFFFFFu, upto, 31);
@@ -213,19 +220,44 @@ __global__ void __launch_bounds__(kAttnThreads, (AttnShape<FMT, D, NQ>::kPerSm))
             seq = (int)(at / per_seq);
             item = (int)(at - (int64_t)seq * per_seq);
         }
+        int s_seq, s_item;                                               // what is done here (seq and item move on)
         const VisibleRange range = visible_range(p, seq);
         const int tiles = tiles_of<L::kTile>(range);
-        int count = tiles - tile;
-        if (p.partial && count > stop - at) count = (int)(stop - at);
+        // tiles tile .. tile + count - 1 of the item
+        int tile = 0, count = tiles;
+        if (p.partial) {
+            const int64_t left = stop - at;
+            const int units = left < tiles + kLead - unit ? (int)left : tiles + kLead - unit, last = unit + units - kLead;
+            tile = unit > kLead ? unit - kLead : 0;
+            count = last > tile ? last - tile : 0;
+            const int64_t item_at = at - unit;
+            at += units;
+            const int item_now = item, seq_now = seq;
+            unit = 0;
+            if (++item == per_seq) {
+                item = 0;
+                ++seq;
+            }
+            if (count == 0) continue;                                    // (the item's lead alone)
+            if (tile == 0 && threadIdx.x == 0)
+                p.parts[(int64_t)seq_now * per_seq + item_now] =
+                    make_int2((int)blockIdx.x, (int)((item_at + kLead + tiles - 1) / quota) - (int)blockIdx.x + 1);
+            s_seq = seq_now;
+            s_item = item_now;
+        } else {
+            s_seq = seq;
+            s_item = item;
+            at += gridDim.x;
+        }
         const bool whole = tile == 0 && count == tiles;
         const int slot = 2 * (int)blockIdx.x + (tile == 0 ? 1 : 0);
-        const int head = item / p.chunks, chunk = item - head * p.chunks;
+        const int head = s_item / p.chunks, chunk = s_item - head * p.chunks;
         const int token0 = range.begin + tile * L::kTile;
         const int64_t token_end = (int64_t)token0 + (int64_t)count * L::kTile;
         const int end = token_end < range.end ? (int)token_end : range.end;
         const int steps = end > token0 ? (end - token0 + L::kStep - 1) / L::kStep : 0;
         const int my_steps = steps > warp ? (steps - warp + kAttnWarps - 1) / kAttnWarps : 0;
-        const int32_t* table = p.table + (int64_t)seq * p.table_stride;
+        const int32_t* table = p.table + (int64_t)s_seq * p.table_stride;
 
         if (padded || first_segment) {                                   // columns behind the rows' channels stay zero
             if (padded)
@@ -234,35 +266,43 @@ __global__ void __launch_bounds__(kAttnThreads, (AttnShape<FMT, D, NQ>::kPerSm))
             __syncwarp();
         }
 
-        // ---- queries: operand registers and the power of two of each row ----
+        // ---- queries: operand registers and their power of two ----
         uint32_t qf[kM][NT][2];
-        float q_scale[NT][2];
+        float q_scale = p.scale_log2e;
+        uint32_t amax = 0;                                               // of the magnitude bits
 #pragma unroll
         for (int nt = 0; nt < NT; ++nt) {
             const int row = chunk * NQ + nt * 8 + g;                     // query head within the group
             const bool exists = row < p.group;
-            const uint16_t* q = static_cast<const uint16_t*>(p.q) + (int64_t)seq * p.q_row + (int64_t)(head * p.group + (exists ? row : 0)) * p.q_head;
-            uint32_t amax = 0;                                           // of the magnitude bits
+            const uint16_t* q = static_cast<const uint16_t*>(p.q) + (int64_t)s_seq * p.q_row + (int64_t)(head * p.group + (exists ? row : 0)) * p.q_head;
 #pragma unroll
             for (int m = 0; m < kM; ++m) {
                 const int ch = L::k_channel(m, j);
-                uint32_t v[4];
+                uint32_t v[4] = {0, 0, 0, 0};
+                if (p.q_vec) {                                           // four channels at a time
+                    if (exists && ch < p.c.head_dim) {
+                        const uint2 w = __ldg(reinterpret_cast<const uint2*>(q + ch));
+                        v[0] = w.x & 0xFFFFu; v[1] = w.x >> 16; v[2] = w.y & 0xFFFFu; v[3] = w.y >> 16;
+                    }
+                } else {
 #pragma unroll
-                for (int i = 0; i < 4; ++i) {
-                    v[i] = exists && ch + i < p.c.head_dim ? q[ch + i] : 0u;
-                    amax = max(amax, v[i] & 0x7FFFu);
+                    for (int i = 0; i < 4; ++i)
+                        if (exists && ch + i < p.c.head_dim) v[i] = q[ch + i];
                 }
+#pragma unroll
+                for (int i = 0; i < 4; ++i) amax = max(amax, v[i] & 0x7FFFu);
                 qf[m][nt][0] = v[0] | (v[1] << 16);
                 qf[m][nt][1] = v[2] | (v[3] << 16);
             }
-            q_scale[nt][0] = q_scale[nt][1] = p.scale_log2e;
-            if constexpr (L::kCodes) {
-                amax = max(amax, __shfl_xor_sync(0xFFFFFFFFu, amax, 1));
-                amax = max(amax, __shfl_xor_sync(0xFFFFFFFFu, amax, 2));
-                const float top = p.q_f16 ? __half2float(__ushort_as_half((unsigned short)amax)) : __uint_as_float(amax << 16);
-                int e = (int)(__float_as_uint(top) >> 23) - 127;         // (0 and subnormal rows: -127)
-                e = e < -112 ? -112 : e;
-                const float up = exp2_int(14 - e);
+        }
+        if constexpr (L::kCodes) {
+            amax = __reduce_max_sync(0xFFFFFFFFu, amax);
+            const float top = p.q_f16 ? __half2float(__ushort_as_half((unsigned short)amax)) : __uint_as_float(amax << 16);
+            int e = (int)(__float_as_uint(top) >> 23) - 127;             // (0 and subnormal values: -127)
+            e = e < -100 ? -100 : e;
+            const float up = exp2_int(14 - e);
+#pragma unroll
+            for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
                 for (int m = 0; m < kM; ++m)
 #pragma unroll
@@ -278,10 +318,7 @@ __global__ void __launch_bounds__(kAttnThreads, (AttnShape<FMT, D, NQ>::kPerSm))
                         }
                         qf[m][nt][i] = pack_f16(lo * up, hi * up);
                     }
-                const float down = exp2_int(e - 14);
-#pragma unroll
-                for (int i = 0; i < 2; ++i) q_scale[nt][i] *= __shfl_sync(0xFFFFFFFFu, down, 4 * (2 * j + i));
-            }
+            q_scale *= exp2_int(e - 14 - L::kLift);
         }
 
         float o[kM][NT][4];
@@ -298,71 +335,69 @@ __global__ void __launch_bounds__(kAttnThreads, (AttnShape<FMT, D, NQ>::kPerSm))
         }
 
         // ---- copies of a step ----
-        // cell of position `lane` of step i of this warp; false: none
-        auto locate = [&](int i, uint32_t& cell) -> bool {
+        // table entry and slot of position `lane` of step i of this warp; the entry is looked at when the step is copied, one step later
+        int page_next = -1;
+        uint32_t slot_next = 0;
+        auto look_up = [&](int i) {
             const int t = token0 + (warp + i * kAttnWarps) * L::kStep + lane;
-            if (i >= my_steps || lane >= L::kStep || t >= end) return false;
+            page_next = -1;
+            if (i >= my_steps || lane >= L::kStep || t >= end) return;
             const uint32_t entry = p.c.by_page.div((uint32_t)t);
-            const int page = __ldg(table + entry);
-            if (page < 0 || page >= p.c.pages) return false;
-            cell = (uint32_t)(((uint32_t)page * (uint32_t)p.c.heads + (uint32_t)head) * (uint32_t)p.c.page_size + ((uint32_t)t - entry * (uint32_t)p.c.page_size));
-            return true;
+            slot_next = (uint32_t)t - entry * page_size;
+            page_next = __ldg(table + entry);
         };
-        uint32_t cell_next = 0;
-        bool live_next = locate(0, cell_next);
+        look_up(0);
+        int fill = 0;                                                    // stage of the next step to copy
         auto issue = [&](int i) {
             if (i < my_steps) {
-                const uint32_t cell = cell_next;
-                const uint32_t mask = __ballot_sync(0xFFFFFFFFu, live_next);
-                const bool live = live_next;
-                cell_next = 0;
-                live_next = locate(i + 1, cell_next);
-                uint8_t* stage = ring + (i % L::kStages) * L::kStageBytes;
-                const uint32_t base = shared_u32(stage);
-                const int64_t row_bytes = p.c.row_bytes();
+                const bool live = (uint32_t)page_next < pages;
+                const uint32_t cell = live ? ((uint32_t)page_next * heads + (uint32_t)head) * page_size + slot_next : 0u;
+                const uint32_t mask = __ballot_sync(0xFFFFFFFFu, live);
+                look_up(i + 1);
+                const uint32_t base = ring_at + fill * L::kStageBytes;
+                fill = fill + 1 == L::kStages ? 0 : fill + 1;
+                constexpr int kRows = 32 / L::kChunks, kPasses = L::kStep / kRows;   // rows of a pass
 #pragma unroll
-                for (int c0 = 0; c0 < L::kStep * L::kChunks; c0 += 32) {
-                    const int r = (c0 + lane) / L::kChunks, c = (c0 + lane) % L::kChunks;
-                    const uint32_t from = __shfl_sync(0xFFFFFFFFu, cell, r);
-                    const int64_t off = (int64_t)from * row_bytes + 16 * c;
-                    const bool exists = (mask >> r) & 1u;
-                    if (c < real_chunks) {
-                        const uint32_t dst = base + r * L::kRow + 16 * L::chunk_at(r, c);
-                        copy_async<16>(dst, exists ? p.c.k + off : p.c.k, exists);
-                        copy_async<16>(dst + L::kStep * L::kRow, exists ? p.c.v + off : p.c.v, exists);
+                for (int x = 0; x < kPasses; ++x) {
+                    const int r = x * kRows + lane / L::kChunks;
+                    const uint64_t from = __shfl_sync(0xFFFFFFFFu, cell, r);
+                    const uint32_t dst = base + copy_row + x * kRows * L::kRow + 16 * L::chunk_at(r, lane % L::kChunks);
+                    const uint32_t size = mask == kFull ? 16u : ((mask >> r) & 1u) << 4;
+                    if (lane_copies) {
+                        copy_async_16(dst, k_lane + from * row_bytes, size);
+                        copy_async_16(dst + L::kStep * L::kRow, v_lane + from * row_bytes, size);
                     }
                 }
                 if constexpr (L::kCodes) {
-                    const int64_t off = live ? (int64_t)cell * L::kScaleRow : 0;
-                    copy_async<L::kScaleRow>(base + L::kScaleOff + lane * L::kScaleRow, p.c.k_scales + off, live);
-                    copy_async<L::kScaleRow>(base + L::kScaleOff + (L::kStep + lane) * L::kScaleRow, p.c.v_scales + off, live);
+                    copy_async_small<L::kScaleRow>(base + L::kScaleOff + lane * L::kScaleRow, p.c.k_scales + (uint64_t)cell * L::kScaleRow, live);
+                    copy_async_small<L::kScaleRow>(base + L::kScaleOff + (L::kStep + lane) * L::kScaleRow, p.c.v_scales + (uint64_t)cell * L::kScaleRow, live);
                 }
-                if (lane == 0) *reinterpret_cast<uint32_t*>(stage + L::kMaskOff) = mask;
+                if (lane == 0) asm volatile("st.shared.u32 [%0], %1;" ::"r"(base + L::kMaskOff), "r"(mask) : "memory");
             }
             asm volatile("cp.async.commit_group;" ::: "memory");
         };
 
 #pragma unroll
         for (int i = 0; i < L::kStages - 1; ++i) issue(i);
+        int use = 0;
         for (int it = 0; it < my_steps; ++it) {
             asm volatile("cp.async.wait_group %0;" ::"n"(L::kStages - 2) : "memory");
             __syncwarp();
             issue(it + L::kStages - 1);                                  // (into the stage of the step before, which all lanes have left)
-            const uint8_t* stage = ring + (it % L::kStages) * L::kStageBytes;
+            const uint8_t* stage = ring + use * L::kStageBytes;
+            use = use + 1 == L::kStages ? 0 : use + 1;
             const uint8_t* kst = stage;
             const uint8_t* vst = stage + L::kStep * L::kRow;
             const uint32_t mask = *reinterpret_cast<const uint32_t*>(stage + L::kMaskOff);
 
             // ---- scales: lane = position of the products ----
-            float k_factor = 1.f, v_factor = 1.f;
+            float k_factor = q_scale, v_factor = 1.f;
             int v_new = v_run;
             if constexpr (L::kCodes) {
-                const int r = L::row_of(lane);
-                const bool live = (mask >> r) & 1u;
                 int top[2];
 #pragma unroll
                 for (int kv = 0; kv < 2; ++kv) {
-                    const uint8_t* s = stage + L::kScaleOff + (kv * L::kStep + r) * L::kScaleRow;
+                    const uint8_t* s = stage + L::kScaleOff + (kv * L::kStep + row_lane) * L::kScaleRow;
                     uint32_t w[L::kScaleRow / 4];
                     w[0] = *reinterpret_cast<const uint32_t*>(s) & byte_mask0;
                     if constexpr (L::kScaleRow == 8) w[1] = *reinterpret_cast<const uint32_t*>(s + 4) & byte_mask1;
@@ -373,11 +408,13 @@ __global__ void __launch_bounds__(kAttnThreads, (AttnShape<FMT, D, NQ>::kPerSm))
                         most = max(most, S[b]);
                     }
                     top[kv] = most;
+                    // fp16 bits of 2^(S - most + kLift), 0 below its normal range
 #pragma unroll
-                    for (int b = 0; b < D / 32; ++b) mul[(kv * (D / 32) + b) * L::kStep + lane] = __float2half_rn(exp2_int(S[b] - most));
+                    for (int b = 0; b < D / 32; ++b)
+                        mul[(kv * (D / 32) + b) * L::kStep + lane] = (uint16_t)(max(S[b] - most + 15 + L::kLift, 0) << 10);
                 }
-                k_factor = exp2_int(top[0] - 127);
-                v_new = max(v_run, (int)__reduce_max_sync(0xFFFFFFFFu, live ? top[1] : 0));
+                k_factor *= exp2_int(top[0] - 127);
+                v_new = max(v_run, (int)__reduce_max_sync(0xFFFFFFFFu, top[1]));     // (0 where there is no position)
                 v_factor = exp2_int(top[1] - v_new + 14);
                 __syncwarp();
             }
@@ -395,8 +432,7 @@ __global__ void __launch_bounds__(kAttnThreads, (AttnShape<FMT, D, NQ>::kPerSm))
                 const uint8_t* b = kst + r1 * L::kRow;
                 if constexpr (FMT == kAttnFp4 && L::kChunks == 2) {
                     const uint2 x = *reinterpret_cast<const uint2*>(a + 8 * j), y = *reinterpret_cast<const uint2*>(b + 8 * j);
-                    const __half2 ma = __half2half2(mul[(j >> 1) * L::kStep + 16 * mt + g]), mb = __half2half2(mul[(j >> 1) * L::kStep + 16 * mt + g + 8]);
-                    const uint32_t xs = *reinterpret_cast<const uint32_t*>(&ma), ys = *reinterpret_cast<const uint32_t*>(&mb);
+                    const uint32_t xs = mul[(j >> 1) * L::kStep + 16 * mt + g] * 0x10001u, ys = mul[(j >> 1) * L::kStep + 16 * mt + g + 8] * 0x10001u;
 #pragma unroll
                     for (int w = 0; w < 2; ++w) {
                         uint32_t hx[4], hy[4];
@@ -429,8 +465,7 @@ __global__ void __launch_bounds__(kAttnThreads, (AttnShape<FMT, D, NQ>::kPerSm))
                                 }
                         } else {
                             const int block = FMT == kAttnFp8 ? c >> 1 : c;
-                            const __half2 ma = __half2half2(mul[block * L::kStep + 16 * mt + g]), mb = __half2half2(mul[block * L::kStep + 16 * mt + g + 8]);
-                            const uint32_t xs = *reinterpret_cast<const uint32_t*>(&ma), ys = *reinterpret_cast<const uint32_t*>(&mb);
+                            const uint32_t xs = mul[block * L::kStep + 16 * mt + g] * 0x10001u, ys = mul[block * L::kStep + 16 * mt + g + 8] * 0x10001u;
 #pragma unroll
                             for (int w = 0; w < 4; ++w) {
                                 if constexpr (FMT == kAttnFp8) {
@@ -467,17 +502,17 @@ __global__ void __launch_bounds__(kAttnThreads, (AttnShape<FMT, D, NQ>::kPerSm))
 #pragma unroll
                 for (int h = 0; h < 2; ++h) {
                     const int k = 16 * mt + 8 * h + g;
-                    float kf = 1.f;
+                    float kf = q_scale;
                     vf[mt][h] = FMT == kAttnF16 ? 16384.f : 1.f;
                     if constexpr (L::kCodes) {
                         kf = __shfl_sync(0xFFFFFFFFu, k_factor, k);
                         vf[mt][h] = __shfl_sync(0xFFFFFFFFu, v_factor, k);
                     }
-                    const bool live = (mask >> L::row_of(k)) & 1u;
+                    const float shut = (mask >> L::row_of(k)) & 1u ? 0.f : kMinus;       // (keys without a place were read as zeros)
 #pragma unroll
                     for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
-                        for (int i = 0; i < 2; ++i) s[mt][nt][2 * h + i] = live ? s[mt][nt][2 * h + i] * q_scale[nt][i] * kf : kMinus;
+                        for (int i = 0; i < 2; ++i) s[mt][nt][2 * h + i] = fmaf(s[mt][nt][2 * h + i], kf, shut);
                 }
             bool grown = v_new != v_run;
             float m_new[NT][2];
@@ -554,7 +589,7 @@ __global__ void __launch_bounds__(kAttnThreads, (AttnShape<FMT, D, NQ>::kPerSm))
                     }
                 }
             } else {
-                constexpr int kBytesV = L::kRow / 8, kWords = kBytesV / 4;   // of a lane's channels at one position
+                constexpr int kBytesV = 2 * L::kChunks, kWords = kBytesV / 4;   // of a lane's channels at one position
                 const int block = g * (D / 8) / 32;
 #pragma unroll
                 for (int mt = 0; mt < kMt; ++mt) {
@@ -576,7 +611,7 @@ __global__ void __launch_bounds__(kAttnThreads, (AttnShape<FMT, D, NQ>::kPerSm))
                             }
                         }
                     }
-                    const __half* mv = mul + (D / 32 + block) * L::kStep + 16 * mt + 2 * j;
+                    const uint16_t* mv = mul + (D / 32 + block) * L::kStep + 16 * mt + 2 * j;
                     const uint32_t m01 = *reinterpret_cast<const uint32_t*>(mv), m23 = *reinterpret_cast<const uint32_t*>(mv + 8);
 #pragma unroll
                     for (int x = 0; x < kWords; ++x) {
@@ -628,7 +663,7 @@ __global__ void __launch_bounds__(kAttnThreads, (AttnShape<FMT, D, NQ>::kPerSm))
                 }
             }
         __syncthreads();                                                 // all warps have left their rings
-        const float unit = L::kCodes ? exp2_int(v_run - 127 - 14) : (FMT == kAttnF16 ? 1.f / 16384.f : 1.f);
+        const float unit = L::kCodes ? exp2_int(v_run - 127 - 14 - L::kLift) : (FMT == kAttnF16 ? 1.f / 16384.f : 1.f);
 #pragma unroll
         for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
@@ -666,12 +701,12 @@ __global__ void __launch_bounds__(kAttnThreads, (AttnShape<FMT, D, NQ>::kPerSm))
                 const int q_head = head * p.group + chunk * NQ + col;
                 const float v = l == 0.f ? 0.f : sum / l;
                 if (ch < p.c.head_dim) {
-                    const int64_t to = (int64_t)seq * p.out_row + (int64_t)q_head * p.out_head + ch;
+                    const int64_t to = (int64_t)s_seq * p.out_row + (int64_t)q_head * p.out_head + ch;
                     if (p.out_type == 0) static_cast<float*>(p.out)[to] = v;
                     else if (p.out_type == 2) static_cast<__half*>(p.out)[to] = __float2half_rn(v);
                     else static_cast<__nv_bfloat16*>(p.out)[to] = __float2bfloat16_rn(v);
                 }
-                if (p.lse && ch == 0) p.lse[(int64_t)seq * p.q_heads + q_head] = l == 0.f ? kMinus : (top + log2f(l)) * 0.6931471805599453f;
+                if (p.lse && ch == 0) p.lse[(int64_t)s_seq * p.q_heads + q_head] = l == 0.f ? kMinus : (top + log2f(l)) * 0.6931471805599453f;
             } else {
                 p.partial[((int64_t)slot * NQ + col) * D + ch] = sum;
                 if (ch == 0) {
@@ -682,80 +717,81 @@ __global__ void __launch_bounds__(kAttnThreads, (AttnShape<FMT, D, NQ>::kPerSm))
             }
         }
         __syncthreads();                                                 // the rings are free again
-
-        if (p.partial) {
-            at += count;
-            tile = 0;
-            if (++item == per_seq) {
-                item = 0;
-                ++seq;
-            }
-        } else {
-            at += gridDim.x;
-        }
     }
 }
 
-constexpr int kJoinThreads = 256;
+constexpr int kJoinThreads = 512;
 
 // Joins the parts of an item that several CTAs took: blockIdx.x = item, blockIdx.y = query of the chunk.  The threads are D/4 groups of
-// four channels times lanes that take every so many parts; the lanes' sums are added in order.
-template <int TN, int D, int NQ>
+// four channels times lanes that take every so many parts with a running maximum; the lanes' sums are added in order.
+template <int D, int NQ>
 __global__ void __launch_bounds__(kJoinThreads) cache_attention_join(const __grid_constant__ AttentionProblem p) {
     constexpr int kCols = D / 4, kLanes = kJoinThreads / kCols;
     __shared__ float4 sums[kJoinThreads];
-    __shared__ float weights[kLanes];
+    __shared__ float tops[kLanes], weights[kLanes];
     pdl_launch_dependents();
-    pdl_wait_prior_grid();
-    const int per_seq = p.c.heads * p.chunks, lane = threadIdx.x & 31;
+    const int per_seq = p.c.heads * p.chunks;
     const int seq = (int)blockIdx.x / per_seq, item = (int)blockIdx.x - seq * per_seq;
     const int head = item / p.chunks, col = blockIdx.y, row = (item - head * p.chunks) * NQ + col;
     if (row >= p.group) return;
-    const int64_t before = tiles_before<TN>(p, seq, lane);
-    const int tiles = tiles_of<TN>(visible_range(p, seq));
-    int64_t rest = 0;
-    for (int s = seq + lane; s < p.sequences; s += 32) rest += tiles_of<TN>(visible_range(p, s));
-#pragma unroll
-    for (int o = 16; o > 0; o >>= 1) rest += __shfl_xor_sync(0xFFFFFFFFu, rest, o);
-    const int64_t quota = run_length(p, (before + rest) * per_seq);
-    const int64_t a = before * per_seq + (int64_t)item * tiles;
-    const int c0 = (int)(a / quota), c1 = (int)((a + tiles - 1) / quota);
-    if (c0 == c1) return;                                                // written by its CTA
+    pdl_wait_prior_grid();
+    const int2 parts = p.parts[blockIdx.x];
+    if (parts.y <= 1) return;                                            // written by its CTA
     const float* st = p.partial + (int64_t)2 * p.ctas * NQ * D;
-    auto slot = [&](int c) { return 2 * c + (c == c0 ? 1 : 0); };
-    float top = -INFINITY;
-    for (int c = c0 + lane; c <= c1; c += 32) top = fmaxf(top, st[(int64_t)slot(c) * 2 * NQ + col]);
-#pragma unroll
-    for (int o = 16; o > 0; o >>= 1) top = fmaxf(top, __shfl_xor_sync(0xFFFFFFFFu, top, o));
-    const float ref = top == -INFINITY ? 0.f : top;
     const int x = threadIdx.x % kCols, y = threadIdx.x / kCols;
     float4 sum = make_float4(0.f, 0.f, 0.f, 0.f);
-    float l = 0.f;
-#pragma unroll 4
-    for (int c = c0 + y; c <= c1; c += kLanes) {
-        const float4 v = *reinterpret_cast<const float4*>(p.partial + ((int64_t)slot(c) * NQ + col) * D + 4 * x);
-        const float* s = st + (int64_t)slot(c) * 2 * NQ + col;
-        const float f = exp2_fast(s[0] - ref);
-        l += f * s[NQ];
-        sum.x += f * v.x; sum.y += f * v.y; sum.z += f * v.z; sum.w += f * v.w;
+    float l = 0.f, top = -INFINITY;
+    constexpr int kAhead = 4;
+    for (int c = y; c < parts.y; c += kAhead * kLanes) {
+        float4 v[kAhead];
+        float m[kAhead], w[kAhead];
+#pragma unroll
+        for (int i = 0; i < kAhead; ++i) {
+            const int k = c + i * kLanes;
+            const int64_t slot = 2 * (int64_t)(parts.x + (k < parts.y ? k : 0)) + (k == 0 || k >= parts.y ? 1 : 0);
+            v[i] = *reinterpret_cast<const float4*>(p.partial + (slot * NQ + col) * D + 4 * x);
+            m[i] = k < parts.y ? st[slot * 2 * NQ + col] : -INFINITY;
+            w[i] = st[slot * 2 * NQ + NQ + col];
+        }
+#pragma unroll
+        for (int i = 0; i < kAhead; ++i) {
+            if (c + i * kLanes >= parts.y) break;
+            const float up = fmaxf(top, m[i]), ref = up == -INFINITY ? 0.f : up;
+            const float f = exp2_fast(top - ref), e = exp2_fast(m[i] - ref);
+            top = up;
+            l = l * f + w[i] * e;
+            sum.x = sum.x * f + v[i].x * e;
+            sum.y = sum.y * f + v[i].y * e;
+            sum.z = sum.z * f + v[i].z * e;
+            sum.w = sum.w * f + v[i].w * e;
+        }
     }
     sums[threadIdx.x] = sum;
-    if (x == 0) weights[y] = l;
+    if (x == 0) {
+        tops[y] = top;
+        weights[y] = l;
+    }
     __syncthreads();
     if (y != 0) return;
-    l = weights[0];
-    for (int k = 1; k < kLanes; ++k) {
+    const int lanes = parts.y < kLanes ? parts.y : kLanes;
+    top = tops[0];
+    for (int k = 1; k < lanes; ++k) top = fmaxf(top, tops[k]);
+    const float ref = top == -INFINITY ? 0.f : top;
+    sum = make_float4(0.f, 0.f, 0.f, 0.f);
+    l = 0.f;
+    for (int k = 0; k < lanes; ++k) {
         const float4 v = sums[k * kCols + x];
-        sum.x += v.x; sum.y += v.y; sum.z += v.z; sum.w += v.w;
-        l += weights[k];
+        const float e = exp2_fast(tops[k] - ref);
+        sum.x += v.x * e; sum.y += v.y * e; sum.z += v.z * e; sum.w += v.w * e;
+        l += weights[k] * e;
     }
     const int q_head = head * p.group + row;
-    const float inv[4] = {sum.x, sum.y, sum.z, sum.w};
+    const float all[4] = {sum.x, sum.y, sum.z, sum.w};
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
         const int ch = 4 * x + i;
         if (ch >= p.c.head_dim) continue;
-        const float v = l == 0.f ? 0.f : inv[i] / l;
+        const float v = l == 0.f ? 0.f : all[i] / l;
         const int64_t to = (int64_t)seq * p.out_row + (int64_t)q_head * p.out_head + ch;
         if (p.out_type == 0) static_cast<float*>(p.out)[to] = v;
         else if (p.out_type == 2) static_cast<__half*>(p.out)[to] = __float2half_rn(v);

@@ -31,21 +31,28 @@ struct W4A16Problem {
 };
 
 constexpr int kW4Threads = 256;
-constexpr int kW4Units = 24;             // of x in shared memory at a time
+constexpr int kW4Stages = 3;             // units of a warp on the way or in use
+constexpr int kW4Lift = 13;              // 6 * 2^13 is the largest power-of-two multiple of a code in fp16
+constexpr int kW4StageBytes = 2048 + 128;                                // [q][lane] x 16 bytes of codes, [g] x 16 scale bytes
 template <int NT> struct W4Smem {
-    static constexpr int kXBytes = kW4Units * NT * 2048;                 // [unit][column tile][piece of 8 channels][lane] x 16 bytes
-    static constexpr int kPartBytes = 2 * 8 * NT * 128 * 4;              // [half of the warps][row of x][weight row], in x's place
-    static constexpr int kScaleOff = kXBytes > kPartBytes ? kXBytes : kPartBytes;
-    static constexpr int kBytes = kScaleOff + kW4Units * 8 * NT * 4;
+    static constexpr int kUnits = NT == 1 ? 24 : 14;                     // of x at a time (even: the halves of the warps take turns); two CTAs fit an SM
+    static constexpr int kXOff = (kW4Threads / 32) * kW4Stages * kW4StageBytes;
+    static constexpr int kXBytes = kUnits * NT * 2048;                 // [unit][row][128 channels]
+    static constexpr int kPartBytes = 2 * 8 * NT * 128 * 4;              // [half of the warps][row of x][weight row], from the start
+    static constexpr int kScaleOff = kXOff + kXBytes;
+    static constexpr int kBytes = kScaleOff + kUnits * 8 * NT * 4;
+    static_assert(kPartBytes <= kXOff, "partial sums take the place of the stages");
 };
 
-__device__ __forceinline__ uint4 w4_load(const uint8_t* p, bool exists) { return exists ? ld_stream_16(p) : make_uint4(0, 0, 0, 0); }
+// Place (16 bytes) of the k-th eight channels of block j within the 256 bytes of 128 channels of row m: neighbouring operands fill all banks.
+__device__ __forceinline__ int w4_place(int m, int k, int j) { return (4 * k + j) ^ ((m & 1) << 2); }
 
 // grid: x = tiles of 128 weight rows times splits (a cluster), y = runs of 8 NT rows of x
 template <bool GLU, int NT, bool XF16>
 __global__ void __launch_bounds__(kW4Threads, 2) linear_w4a16_kernel(const __grid_constant__ W4A16Problem p, const int splits) {
     using L = W4Smem<NT>;
     extern __shared__ __align__(16) uint8_t w4_smem[];
+    uint4* x_smem = reinterpret_cast<uint4*>(w4_smem + L::kXOff);
     float* x_scale = reinterpret_cast<float*>(w4_smem + L::kScaleOff);
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, g = lane >> 2, j = lane & 3;
     const int rank = splits > 1 ? (int)cluster_ctarank() : 0;
@@ -60,15 +67,27 @@ __global__ void __launch_bounds__(kW4Threads, 2) linear_w4a16_kernel(const __gri
     pdl_launch_dependents();
     pdl_wait_prior_grid();
 
-    uint4 w[2][4], sc[2];
-    auto fetch = [&](int u, uint4 (&wr)[4], uint4& s) {
-        const bool exists = u < u1 && 4 * u + j < blocks;
+    // A lane copies the codes that it will use itself, and lane 4 g the scales of its quad.
+    uint8_t* ring = w4_smem + (threadIdx.x >> 5) * (kW4Stages * kW4StageBytes);
+    const uint32_t ring_at = smem_u32(ring);
+    int fill = 0;
+    auto fetch = [&](int u) {
+        if (u < u1) {
+            const uint32_t to = ring_at + fill * kW4StageBytes;
+            const uint8_t* from = codes + (int64_t)u * 64;
+            const bool exists = 4 * u + j < blocks;
 #pragma unroll
-        for (int q = 0; q < 4; ++q) wr[q] = w4_load(codes + (int64_t)(32 * q) * pitch + (int64_t)u * 64, exists && base_row + 32 * q < p.lin.R);
-        s = w4_load(scales + (int64_t)u * 512, u < u1);
+            for (int q = 0; q < 4; ++q) {
+                const bool row = exists && base_row + 32 * q < p.lin.R;
+                asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;"
+                             ::"r"(to + q * 512 + lane * 16), "l"(row ? from + (int64_t)(32 * q) * pitch : p.codes), "r"(row ? 16 : 0) : "memory");
+            }
+            if (j == 0) asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(to + 2048 + g * 16), "l"(scales + (int64_t)u * 512) : "memory");
+            fill = fill + 1 == kW4Stages ? 0 : fill + 1;
+        }
+        asm volatile("cp.async.commit_group;" ::: "memory");
     };
-    fetch(u0 + half, w[0], sc[0]);
-    fetch(u0 + half + 2, w[1], sc[1]);
+    int use = 0;
 
     float acc[2][NT][4];
 #pragma unroll
@@ -78,109 +97,130 @@ __global__ void __launch_bounds__(kW4Threads, 2) linear_w4a16_kernel(const __gri
 #pragma unroll
             for (int i = 0; i < 4; ++i) acc[t][nt][i] = 0.f;
 
-    for (int p0 = u0; p0 < u1; p0 += kW4Units) {
-        const int p1 = p0 + kW4Units < u1 ? p0 + kW4Units : u1;
+    NarrowColumn<GLU> col;
+    const LinearItem item = {0, 0, tile, 0, p.lin.M};
+    col.open(p.lin, item, (int)threadIdx.x);                             // (the bias is on its way meanwhile)
+    if (p.lin.epi.residual && col.live)
+        for (int c = col.first + rank * NarrowColumn<GLU>::kStep; c < rows; c += NarrowColumn<GLU>::kStep * splits)
+            asm volatile("prefetch.global.L2 [%0];" ::"l"(static_cast<const uint8_t*>(p.lin.epi.residual) +
+                         ((int64_t)(m0 + c) * p.lin.epi.ld_residual + col.n) * (p.lin.epi.residual_type == kTypeF32 ? 4 : 2)));
+
+    // A group of 16 lanes keeps one row of x and takes its 128 channels of every `turns`-th unit, a lane eight channels.
+    const int piece = threadIdx.x & 15, group = threadIdx.x >> 4, turns = (kW4Threads / 16) / rows;
+    const int m = group % rows, first = group < turns * rows ? group / rows : L::kUnits;
+    const uint16_t* x_at = static_cast<const uint16_t*>(p.x) + (int64_t)(m0 + m) * p.ld_x + 8 * piece;
+    uint4* const x_row = x_smem + m * 16;
+    for (int p0 = u0; p0 < u1; p0 += L::kUnits) {
+        const int p1 = p0 + L::kUnits < u1 ? p0 + L::kUnits : u1;
         if (p0 != u0) __syncthreads();
-        // x of these units: 16 lanes per row and unit, eight channels each
-        for (int i = threadIdx.x; i < (p1 - p0) * 8 * NT * 16; i += kW4Threads) {
-            const int piece = i & 15, m = (i >> 4) % (8 * NT), ul = (i >> 4) / (8 * NT);
-            const int ch = (p0 + ul) * 128 + 8 * piece;
-            uint32_t r[4] = {0, 0, 0, 0};
-            if (m < rows && ch < p.K) {
-                const uint16_t* at = static_cast<const uint16_t*>(p.x) + (int64_t)(m0 + m) * p.ld_x + ch;
-                if (p.x_vec) {
-                    const uint4 v = __ldg(reinterpret_cast<const uint4*>(at));
-                    r[0] = v.x; r[1] = v.y; r[2] = v.z; r[3] = v.w;
-                } else {
+        // x of these units, as it is and in its order (asynchronous copies that put neighbouring 16 bytes apart take four times as long).
+        // Columns of the products without a row of x hold what is there: they reach no output.
+#pragma unroll 4
+        for (int u = first; u < p1 - p0; u += turns) {
+            const int ch = (p0 + u) * 128;
+            const bool exists = ch + 8 * piece < p.K;
+            if (p.x_vec) {
+                asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;"
+                             ::"r"(smem_u32(x_row + u * 8 * NT * 16 + piece)), "l"(exists ? x_at + ch : static_cast<const uint16_t*>(p.x)), "r"(exists ? 16 : 0) : "memory");
+            } else {
+                uint32_t r[4] = {0, 0, 0, 0};
+                if (exists)
 #pragma unroll
-                    for (int k = 0; k < 4; ++k) r[k] = (uint32_t)at[2 * k] | ((uint32_t)at[2 * k + 1] << 16);
-                }
+                    for (int i = 0; i < 4; ++i) r[i] = (uint32_t)x_at[ch + 2 * i] | ((uint32_t)x_at[ch + 2 * i + 1] << 16);
+                x_row[u * 8 * NT * 16 + piece] = make_uint4(r[0], r[1], r[2], r[3]);
             }
-            float v[8];
-            widen8_any<XF16>(make_uint4(r[0], r[1], r[2], r[3]), v);
-            float amax = absmax8(v);
-            const uint32_t group = 0xFFFFu << (lane & 16);
+        }
+        asm volatile("cp.async.commit_group;" ::: "memory");
+        if (p0 == u0) {
 #pragma unroll
-            for (int o = 1; o < 16; o <<= 1) amax = fmaxf(amax, __shfl_xor_sync(group, amax, o));
-            int e = (int)(__float_as_uint(amax) >> 23) - 127;
+            for (int i = 0; i < kW4Stages - 1; ++i) fetch(u0 + half + 2 * i);
+            asm volatile("cp.async.wait_group %0;" ::"n"(kW4Stages - 1) : "memory");
+        } else {
+            asm volatile("cp.async.wait_group 0;" ::: "memory");
+        }
+        // what a lane copied becomes fp16 times the power of two of its 128 channels and goes to its place among them
+        const uint32_t lanes = 0xFFFFu << (lane & 16);
+#pragma unroll 2
+        for (int u = first; u < p1 - p0; u += turns) {
+            uint4* row = x_row + u * 8 * NT * 16;
+            float v[8];
+            widen8_any<XF16>(row[piece], v);
+            int e = (int)(__reduce_max_sync(lanes, __float_as_uint(absmax8(v))) >> 23) - 127;          // (and all have read)
             e = e < -112 ? -112 : e;
             const float up = exp2_int(14 - e);
-            uint32_t h[4];
-#pragma unroll
-            for (int k = 0; k < 4; ++k) {
-                const __half2 two = __floats2half2_rn(v[2 * k] * up, v[2 * k + 1] * up);
-                h[k] = *reinterpret_cast<const uint32_t*>(&two);
-            }
-            const int to = ((ul * NT + (m >> 3)) * 4 + (piece & 3)) * 32 + (m & 7) * 4 + (piece >> 2);
-            reinterpret_cast<uint4*>(w4_smem)[to] = make_uint4(h[0], h[1], h[2], h[3]);
-            if (piece == 0) x_scale[ul * 8 * NT + m] = exp2_int(e - 14);
+            __syncwarp(lanes);
+            row[w4_place(m, piece & 3, piece >> 2)] = make_uint4(pack_f16(v[0] * up, v[1] * up), pack_f16(v[2] * up, v[3] * up),
+                                                                 pack_f16(v[4] * up, v[5] * up), pack_f16(v[6] * up, v[7] * up));
+            if (piece == 0) x_scale[u * 8 * NT + m] = exp2_int(e - 14);
         }
         __syncthreads();
-        // (units of this warp in the pass: p0 + half, p0 + half + 2, ...; kW4Units is even, so the order goes on over passes)
-        for (int u = p0 + half; u < p1; u += 4) {
+        for (int u = p0 + half; u < p1; u += 2) {                        // (the number of units is even: the order goes on over the passes)
+            asm volatile("cp.async.wait_group %0;" ::"n"(kW4Stages - 2) : "memory");
+            __syncwarp();
+            fetch(u + 2 * (kW4Stages - 1));                              // into the stage that all lanes have left
+            const uint8_t* stage = ring + use * kW4StageBytes;
+            use = use + 1 == kW4Stages ? 0 : use + 1;
+            uint4 w[4];
 #pragma unroll
-            for (int b = 0; b < 2; ++b) {
-                const int uu = u + 2 * b;
-                if (uu >= p1) break;
-                const int left = blocks - 4 * uu;                        // blocks of this unit
-                const uint32_t mask = left >= 4 ? 0xFFFFFFFFu : (1u << (8 * left)) - 1u;
-                const uint32_t sw[4] = {sc[b].x & mask, sc[b].y & mask, sc[b].z & mask, sc[b].w & mask};
-                uint32_t mul[4];
-                float factor[4];
+            for (int q = 0; q < 4; ++q) w[q] = *reinterpret_cast<const uint4*>(stage + q * 512 + lane * 16);
+            const uint4 sc = *reinterpret_cast<const uint4*>(stage + 2048 + g * 16);
+            const int left = blocks - 4 * u;                             // blocks of this unit
+            const uint32_t mask = left >= 4 ? 0xFFFFFFFFu : (1u << (8 * left)) - 1u;
+            const uint32_t sw[4] = {sc.x & mask, sc.y & mask, sc.z & mask, sc.w & mask};
+            uint32_t mul[4];
+            float factor[4];
 #pragma unroll
-                for (int q = 0; q < 4; ++q) {
-                    const int s0 = (int)(sw[q] & 0xFFu), s1 = (int)((sw[q] >> 8) & 0xFFu), s2 = (int)((sw[q] >> 16) & 0xFFu), s3 = (int)(sw[q] >> 24);
-                    const int top = max(max(s0, s1), max(s2, s3));
-                    const int own = (int)((sw[q] >> (8 * j)) & 0xFFu);
-                    const __half2 two = __half2half2(__float2half_rn(exp2_int(own - top)));
-                    mul[q] = *reinterpret_cast<const uint32_t*>(&two);
-                    factor[q] = exp2_int(top - 127);
+            for (int q = 0; q < 4; ++q) {
+                const int s0 = (int)(sw[q] & 0xFFu), s1 = (int)((sw[q] >> 8) & 0xFFu), s2 = (int)((sw[q] >> 16) & 0xFFu), s3 = (int)(sw[q] >> 24);
+                const int top = max(max(s0, s1), max(s2, s3));
+                const int own = (int)((sw[q] >> (8 * j)) & 0xFFu);
+                mul[q] = (uint32_t)max(own - top + 15 + kW4Lift, 0) * 0x04000400u;       // two fp16 2^(own - top + kW4Lift), 0 below the normal range
+                factor[q] = exp2_int(top - 127 - kW4Lift);
+            }
+            float part[2][NT][4];
+#pragma unroll
+            for (int t = 0; t < 2; ++t)
+#pragma unroll
+                for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) part[t][nt][i] = 0.f;
+            const uint4* xs = x_smem + ((u - p0) * 8 * NT + g) * 16;
+#pragma unroll
+            for (int k = 0; k < 4; ++k) {
+                uint32_t xw[NT][4];
+#pragma unroll
+                for (int nt = 0; nt < NT; ++nt) {
+                    const uint4 v = xs[nt * 128 + w4_place(g, k, j)];
+                    xw[nt][0] = v.x; xw[nt][1] = v.y; xw[nt][2] = v.z; xw[nt][3] = v.w;
                 }
-                float part[2][NT][4];
+#pragma unroll
+                for (int t = 0; t < 2; ++t) {
+                    uint32_t lo[4], hi[4];
+                    const uint4 &wl = w[2 * t], &wh = w[2 * t + 1];
+                    e2m1x8_to_f16(k == 0 ? wl.x : k == 1 ? wl.y : k == 2 ? wl.z : wl.w, lo);
+                    e2m1x8_to_f16(k == 0 ? wh.x : k == 1 ? wh.y : k == 2 ? wh.z : wh.w, hi);
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) { lo[i] = mul_f16x2(lo[i], mul[2 * t]); hi[i] = mul_f16x2(hi[i], mul[2 * t + 1]); }
+#pragma unroll
+                    for (int h = 0; h < 2; ++h)
+#pragma unroll
+                        for (int nt = 0; nt < NT; ++nt)
+                            mma_16816_f16(part[t][nt], lo[2 * h], hi[2 * h], lo[2 * h + 1], hi[2 * h + 1], xw[nt][2 * h], xw[nt][2 * h + 1]);
+                }
+            }
+#pragma unroll
+            for (int nt = 0; nt < NT; ++nt) {
+                const float2 xf = *reinterpret_cast<const float2*>(x_scale + (u - p0) * 8 * NT + nt * 8 + 2 * j);
 #pragma unroll
                 for (int t = 0; t < 2; ++t)
 #pragma unroll
-                    for (int nt = 0; nt < NT; ++nt)
-#pragma unroll
-                        for (int i = 0; i < 4; ++i) part[t][nt][i] = 0.f;
-                const uint4* xs = reinterpret_cast<const uint4*>(w4_smem) + (uu - p0) * NT * 128 + lane;
-#pragma unroll
-                for (int k = 0; k < 4; ++k) {
-                    uint32_t xw[NT][4];
-#pragma unroll
-                    for (int nt = 0; nt < NT; ++nt) {
-                        const uint4 v = xs[nt * 128 + k * 32];
-                        xw[nt][0] = v.x; xw[nt][1] = v.y; xw[nt][2] = v.z; xw[nt][3] = v.w;
-                    }
-#pragma unroll
-                    for (int t = 0; t < 2; ++t) {
-                        uint32_t lo[4], hi[4];
-                        const uint4 &wl = w[b][2 * t], &wh = w[b][2 * t + 1];
-                        e2m1x8_to_f16(k == 0 ? wl.x : k == 1 ? wl.y : k == 2 ? wl.z : wl.w, lo);
-                        e2m1x8_to_f16(k == 0 ? wh.x : k == 1 ? wh.y : k == 2 ? wh.z : wh.w, hi);
-#pragma unroll
-                        for (int i = 0; i < 4; ++i) { lo[i] = mul_f16x2(lo[i], mul[2 * t]); hi[i] = mul_f16x2(hi[i], mul[2 * t + 1]); }
-#pragma unroll
-                        for (int h = 0; h < 2; ++h)
-#pragma unroll
-                            for (int nt = 0; nt < NT; ++nt)
-                                mma_16816_f16(part[t][nt], lo[2 * h], hi[2 * h], lo[2 * h + 1], hi[2 * h + 1], xw[nt][2 * h], xw[nt][2 * h + 1]);
-                    }
-                }
-                fetch(uu + 4, w[b], sc[b]);
-#pragma unroll
-                for (int nt = 0; nt < NT; ++nt) {
-                    const float2 xf = *reinterpret_cast<const float2*>(x_scale + (uu - p0) * 8 * NT + nt * 8 + 2 * j);
-#pragma unroll
-                    for (int t = 0; t < 2; ++t)
-#pragma unroll
-                        for (int i = 0; i < 4; ++i)
-                            acc[t][nt][i] = fmaf(part[t][nt][i] * factor[2 * t + (i >> 1)], (i & 1) ? xf.y : xf.x, acc[t][nt][i]);
-                }
+                    for (int i = 0; i < 4; ++i)
+                        acc[t][nt][i] = fmaf(part[t][nt][i] * factor[2 * t + (i >> 1)], (i & 1) ? xf.y : xf.x, acc[t][nt][i]);
             }
         }
     }
 
+    asm volatile("cp.async.wait_group 0;" ::: "memory");
     __syncthreads();
     float* sums = reinterpret_cast<float*>(w4_smem);
 #pragma unroll
@@ -192,32 +232,52 @@ __global__ void __launch_bounds__(kW4Threads, 2) linear_w4a16_kernel(const __gri
                 sums[(half * 8 * NT + nt * 8 + 2 * j + (i & 1)) * 128 + 32 * (2 * t + (i >> 1)) + 8 * (warp & 3) + g] = acc[t][nt][i];
     if (splits > 1) cluster_sync_all(); else __syncthreads();
 
-    NarrowColumn<GLU> col;
-    const LinearItem item = {0, 0, tile, 0, p.lin.M};
-    col.open(p.lin, item, (int)threadIdx.x);
+    // Two rows of a column at a time; the partial sums of four CTAs are on the way together and are added in order.  Peers may go on
+    // with this CTA's shared memory gone once they have read it, so all meet again after the reads, not after the stores.
     const int stride = NarrowColumn<GLU>::kStep * splits;
+    bool met = splits == 1;
     for (int c = col.first + rank * NarrowColumn<GLU>::kStep; c < rows; c += 2 * stride) {
         float v[2] = {0.f, 0.f}, u[2] = {0.f, 0.f};
-        for (int q = 0; q < splits; ++q)
+        for (int q0 = 0; q0 < splits; q0 += 4) {
+            float x[4][2][2], y[4][2][2];
 #pragma unroll
-            for (int h = 0; h < 2; ++h)
+            for (int q = 0; q < 4; ++q)
 #pragma unroll
-                for (int k = 0; k < 2; ++k) {
-                    const int m = c + k * stride;
-                    if (m >= rows) continue;
-                    const float* at = sums + (h * 8 * NT + m) * 128 + col.r;
-                    if (splits > 1) {
-                        const uint32_t far = mapa_shared(smem_u32(at), (uint32_t)q);
-                        v[k] += ld_cluster_f32(far);
-                        if (GLU) u[k] += ld_cluster_f32(far + 128u);
-                    } else {
-                        v[k] += at[0];
-                        if (GLU) u[k] += at[32];
+                for (int h = 0; h < 2; ++h)
+#pragma unroll
+                    for (int k = 0; k < 2; ++k) {
+                        x[q][h][k] = y[q][h][k] = 0.f;
+                        if (q0 + q >= splits || c + k * stride >= rows) continue;
+                        const float* at = sums + (h * 8 * NT + c + k * stride) * 128 + col.r;
+                        if (splits > 1) {
+                            const uint32_t far = mapa_shared(smem_u32(at), (uint32_t)(q0 + q));
+                            x[q][h][k] = ld_cluster_f32(far);
+                            if (GLU) y[q][h][k] = ld_cluster_f32(far + 128u);
+                        } else {
+                            x[q][h][k] = at[0];
+                            if (GLU) y[q][h][k] = at[32];
+                        }
                     }
-                }
+#pragma unroll
+            for (int q = 0; q < 4; ++q)
+#pragma unroll
+                for (int h = 0; h < 2; ++h)
+#pragma unroll
+                    for (int k = 0; k < 2; ++k) {
+                        v[k] += x[q][h][k];
+                        if (GLU) u[k] += y[q][h][k];
+                    }
+        }
+        if (c + 2 * stride >= rows && !met) {
+            met = true;
+            asm volatile("barrier.cluster.arrive.release;" ::: "memory");
+        }
         col.template write<2>(p.lin.epi, m0 + c, stride, (rows - c + stride - 1) / stride, nullptr, v, u);
     }
-    if (splits > 1) cluster_sync_all();                                  // nobody's sums go away while a peer reads them
+    if (splits > 1) {
+        if (!met) asm volatile("barrier.cluster.arrive.release;" ::: "memory");
+        asm volatile("barrier.cluster.wait.acquire;" ::: "memory");
+    }
 }
 
 }  // namespace kq

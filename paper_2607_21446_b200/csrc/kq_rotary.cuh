@@ -23,8 +23,9 @@ struct FastDiv {                         // n / d for n < 2^31
 struct RotaryTensor {
     const void* x;
     void* out;
-    int heads;
-    int64_t xb, xt, xh, ob, ot, oh;      // strides: batch, token, head
+    int64_t xb, ob;                      // batch strides
+    int heads, xt, xh, ot, oh;           // token and head strides, below 2^31
+    FastDiv by_heads;
 };
 struct RotaryProblem {
     int64_t rows;                        // batches * tokens
@@ -35,9 +36,8 @@ struct RotaryProblem {
     const void* positions;
     int64_t pos_batch, pos_token;
     RotaryTensor t[2];
-    int heads;                           // of both
-    int tokens_per_cta, heads_per_cta;   // heads_per_cta < heads: blockIdx.y takes runs of heads
-    FastDiv by_heads;                    // heads_per_cta
+    int tensors;
+    int tokens_per_cta, head_parts;      // blockIdx.y takes every head_parts-th run of rows
 };
 
 template <typename T> __device__ __forceinline__ float rotary_widen(T v);
@@ -51,6 +51,24 @@ template <> __device__ __forceinline__ __nv_bfloat16 rotary_round<__nv_bfloat16>
 
 // N elements of one access
 template <typename T, int N> struct alignas(sizeof(T) * N) RotaryPack { T v[N]; };
+
+// (cos, sin) of N pairs from p0 on; two at a time where the place allows
+template <int N>
+__device__ __forceinline__ void load_turns(float2 (&turn)[N], const float2* cs, int p0, int pairs) {
+    if (N % 2 == 0 && pairs % 2 == 0) {                                  // (rows of the table stay 16-byte aligned)
+#pragma unroll
+        for (int i = 0; i < N; i += 2) {
+            if (p0 + i >= pairs) break;
+            const float4 c = *reinterpret_cast<const float4*>(cs + p0 + i);
+            turn[i] = make_float2(c.x, c.y);
+            if (i + 1 < N) turn[i + 1] = make_float2(c.z, c.w);
+        }
+    } else {
+#pragma unroll
+        for (int i = 0; i < N; ++i)
+            if (p0 + i < pairs) turn[i] = cs[p0 + i];
+    }
+}
 
 // E: elements of an access (their bytes aligned; 1: any alignment of the type).  A unit is one access (interleaved; two elements, each
 // its own access, with E = 1) or the two accesses of E pairs (half).  Behind the pairs a unit copies E elements.
@@ -83,11 +101,13 @@ struct RotaryUnit {
     __device__ __forceinline__ void turn_and_store(T* row, int w, int pairs, int dim, const float2* cs) {
         if constexpr (!HALF) {
             const int p0 = w * kPairs;
+            float2 turn[kPairs];
+            load_turns<kPairs>(turn, cs, p0, pairs);
 #pragma unroll
             for (int i = 0; i < kPairs; ++i)
                 if (p0 + i < pairs) {
                     const float x = rotary_widen(a[2 * i]), y = rotary_widen(a[2 * i + 1]);
-                    const float2 c = cs[p0 + i];
+                    const float2 c = turn[i];
                     a[2 * i] = rotary_round<T>(fmaf(x, c.x, -(y * c.y)));
                     a[2 * i + 1] = rotary_round<T>(fmaf(x, c.y, y * c.x));
                 }
@@ -103,10 +123,12 @@ struct RotaryUnit {
         } else {
             RotaryPack<T, E> p, q;
             if (w * E < pairs) {
+                float2 turn[E];
+                load_turns<E>(turn, cs, w * E, pairs);
 #pragma unroll
                 for (int i = 0; i < E; ++i) {
                     const float x = rotary_widen(a[i]), y = rotary_widen(b[i]);
-                    const float2 c = cs[w * E + i];
+                    const float2 c = turn[i];
                     p.v[i] = rotary_round<T>(fmaf(x, c.x, -(y * c.y)));
                     q.v[i] = rotary_round<T>(fmaf(x, c.y, y * c.x));
                 }
@@ -122,52 +144,48 @@ struct RotaryUnit {
 };
 
 constexpr int kRotaryThreads = 512;      // at most
-constexpr int kRotaryAhead = 4;          // rows of a thread in flight
 
 // blockDim: x = units of a head, y = rows (token, head) at a time.  Dynamic shared memory: float2 [tokens_per_cta][pairs].
 template <typename T, int E, bool HALF>
 __global__ void __launch_bounds__(kRotaryThreads) rotary_kernel(const __grid_constant__ RotaryProblem p) {
-    extern __shared__ float2 rotary_cs[];
+    extern __shared__ __align__(16) float2 rotary_cs[];
     pdl_launch_dependents();
     pdl_wait_prior_grid();
     const int64_t token0 = (int64_t)blockIdx.x * p.tokens_per_cta;
     const int tokens = (int)(p.rows - token0 < p.tokens_per_cta ? p.rows - token0 : p.tokens_per_cta);
-    const int head0 = (int)blockIdx.y * p.heads_per_cta;
-    const int rows = tokens * p.heads_per_cta;
-    const int w = threadIdx.x, step = blockDim.y;
+    const int w = threadIdx.x, first = threadIdx.y + blockIdx.y * blockDim.y, step = blockDim.y * p.head_parts;
+    int64_t batch0 = 0, t0 = token0;                                      // batch and token of the CTA's first row
+    if (p.tokens != p.rows) {
+        batch0 = token0 / p.tokens;
+        t0 = token0 - batch0 * p.tokens;
+    }
 
-    RotaryUnit<T, E, HALF> unit[kRotaryAhead];
-    T* out[kRotaryAhead];
-    int local[kRotaryAhead];                                              // token of the row within the CTA; < 0: no row
-    auto fetch = [&](int r0) {
+    constexpr int kAhead = sizeof(RotaryUnit<T, E, HALF>) > 16 ? 2 : 4;   // rows of a thread in flight
+    RotaryUnit<T, E, HALF> unit[kAhead];
+    // element of row r (token lt of the CTA) behind its first token's first head
+    auto place = [&](const RotaryTensor& s, int lt, int head, int64_t batch, int token, int head_stride) {
+        int64_t at = (int64_t)lt * token + (int64_t)head * head_stride;
+        if (p.tokens != p.rows && t0 + lt >= p.tokens) at += (t0 + lt) / p.tokens * (batch - p.tokens * token);   // into later batches
+        return at;
+    };
+    auto fetch = [&](const RotaryTensor& s, int r0, int rows) {
+        const T* x = static_cast<const T*>(s.x) + batch0 * s.xb + t0 * s.xt;
 #pragma unroll
-        for (int u = 0; u < kRotaryAhead; ++u) {
+        for (int u = 0; u < kAhead; ++u) {
             const int r = r0 + u * step;
-            local[u] = -1;
-            if (r >= rows) continue;
-            const int lt = (int)p.by_heads.div((uint32_t)r);
-            int head = head0 + r - lt * p.heads_per_cta;
-            if (head >= p.heads) continue;
-            local[u] = lt;
-            int64_t t = token0 + lt, b = 0;
-            if (p.tokens != p.rows) {
-                b = t / p.tokens;
-                t -= b * p.tokens;
+            if (r < rows) {
+                const int lt = (int)s.by_heads.div((uint32_t)r);
+                unit[u].load(x + place(s, lt, r - lt * s.heads, s.xb, s.xt, s.xh), w, p.pairs, p.head_dim);
             }
-            const bool second = head >= p.t[0].heads;
-            if (second) head -= p.t[0].heads;
-            const RotaryTensor& s = p.t[second ? 1 : 0];
-            unit[u].load(static_cast<const T*>(s.x) + b * s.xb + t * s.xt + head * s.xh, w, p.pairs, p.head_dim);
-            out[u] = static_cast<T*>(s.out) + b * s.ob + t * s.ot + head * s.oh;
         }
     };
-    fetch(threadIdx.y);
+    fetch(p.t[0], first, tokens * p.t[0].heads);
     for (int i = threadIdx.y * blockDim.x + threadIdx.x; i < tokens * p.pairs; i += blockDim.x * blockDim.y) {
         const int lt = i / p.pairs, pair = i - lt * p.pairs;
-        int64_t t = token0 + lt, b = 0;
-        if (p.tokens != p.rows) {
-            b = t / p.tokens;
-            t -= b * p.tokens;
+        int64_t t = t0 + lt, b = batch0;
+        if (p.tokens != p.rows && t >= p.tokens) {
+            b += t / p.tokens;
+            t %= p.tokens;
         }
         const int axis = (pair >= p.axis_end[0]) + (pair >= p.axis_end[1]) + (pair >= p.axis_end[2]);
         const int64_t at = b * p.pos_batch + t * p.pos_token + axis;
@@ -182,11 +200,21 @@ __global__ void __launch_bounds__(kRotaryThreads) rotary_kernel(const __grid_con
         rotary_cs[i] = make_float2(cos_t, p.inverse ? -sin_t : sin_t);
     }
     __syncthreads();
-    for (int r0 = threadIdx.y; r0 < rows; r0 += kRotaryAhead * step) {
-        if (r0 != threadIdx.y) fetch(r0);
+    for (int k = 0; k < p.tensors; ++k) {
+        const RotaryTensor& s = p.t[k];
+        const int rows = tokens * s.heads;
+        T* out = static_cast<T*>(s.out) + batch0 * s.ob + t0 * s.ot;
+        for (int r0 = first; r0 < rows; r0 += kAhead * step) {
+            if (k || r0 != first) fetch(s, r0, rows);
 #pragma unroll
-        for (int u = 0; u < kRotaryAhead; ++u)
-            if (local[u] >= 0) unit[u].turn_and_store(out[u], w, p.pairs, p.head_dim, rotary_cs + local[u] * p.pairs);
+            for (int u = 0; u < kAhead; ++u) {
+                const int r = r0 + u * step;
+                if (r < rows) {
+                    const int lt = (int)s.by_heads.div((uint32_t)r);
+                    unit[u].turn_and_store(out + place(s, lt, r - lt * s.heads, s.ob, s.ot, s.oh), w, p.pairs, p.head_dim, rotary_cs + lt * p.pairs);
+                }
+            }
+        }
     }
 }
 

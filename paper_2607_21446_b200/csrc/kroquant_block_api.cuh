@@ -171,21 +171,51 @@ kq_status_t run_linear(const uint8_t* a_codes, const uint8_t* a_scales, const ui
 
 // ---- rows in 16 bits ----------------------------------------------------------------------------------
 
+// How many clusters of 1 .. 8 CTAs the device runs at once (fewer than CTAs / size: a cluster stays within a GPC).
+template <typename Kernel>
+int clusters_at_once(Kernel* kernel, int threads, int smem, int size) {
+    static std::atomic<int> known[64][9];
+    const int dev = DeviceOnce::dev();
+    if (dev < 0) return 0;
+    int n = known[dev][size].load(std::memory_order_relaxed);
+    if (n == 0) {
+        cudaLaunchConfig_t cfg;
+        cudaLaunchAttribute attr[2];
+        launch_config(&cfg, attr, dim3((unsigned)size), dim3((unsigned)threads), (size_t)smem, size, nullptr);
+        cfg.attrs = attr + 1;                                        // the cluster alone
+        cfg.numAttrs = 1;
+        attr[1].id = cudaLaunchAttributeClusterDimension;
+        attr[1].val.clusterDim.x = (unsigned)size;
+        attr[1].val.clusterDim.y = attr[1].val.clusterDim.z = 1;
+        if (cudaOccupancyMaxActiveClusters(&n, kernel, &cfg) != cudaSuccess || n < 1) {
+            (void)cudaGetLastError();
+            return 0;
+        }
+        known[dev][size].store(n, std::memory_order_relaxed);
+    }
+    return n;
+}
 template <bool GLU, int NT, bool XF16>
-kq_status_t launch_w4a16(const kq::W4A16Problem& p, int tiles, int splits, cudaStream_t st) {
+kq_status_t launch_w4a16(const kq::W4A16Problem& p, int tiles, cudaStream_t st) {
     constexpr int kBytes = kq::W4Smem<NT>::kBytes;
+    auto* kernel = kq::linear_w4a16_kernel<GLU, NT, XF16>;
     static DeviceOnce attr_done;
     if (attr_done.needed()) {
-        if (cudaFuncSetAttribute(kq::linear_w4a16_kernel<GLU, NT, XF16>, cudaFuncAttributeMaxDynamicSharedMemorySize, kBytes) != cudaSuccess) {
+        if (cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kBytes) != cudaSuccess) {
             (void)cudaGetLastError();
             return KQ_ERR_CUDA;
         }
         attr_done.done();
     }
+    // K goes over as many CTAs of a cluster as run at once, four units each at least.  12288 -> 4608 with 16 rows, 1 to 8 CTAs: 68, 37, 29,
+    // 33, 29, 26, 22.5, 43 us (36 clusters of eight do not fit at once); 5 rows of 4096 -> 2 x 5632: 18.5, 18.5, 14.4, 18 us.
+    const int runs = (p.lin.M + 8 * NT - 1) / (8 * NT);
+    int splits = 1;
+    while (splits < 8 && p.units >= 4 * (splits + 1) && (int64_t)tiles * runs <= clusters_at_once(kernel, kq::kW4Threads, kBytes, splits + 1)) ++splits;
     cudaLaunchConfig_t cfg;
     cudaLaunchAttribute attr[2];
-    launch_config(&cfg, attr, dim3((unsigned)(tiles * splits), (unsigned)((p.lin.M + 8 * NT - 1) / (8 * NT))), dim3(kq::kW4Threads), kBytes, splits, st);
-    return launch(cfg, kq::linear_w4a16_kernel<GLU, NT, XF16>, p, splits);
+    launch_config(&cfg, attr, dim3((unsigned)(tiles * splits), (unsigned)runs), dim3(kq::kW4Threads), kBytes, splits, st);
+    return launch(cfg, kernel, p, splits);
 }
 constexpr int kW4MaxRows = 64;
 
@@ -435,15 +465,11 @@ kq_status_t kroquant_linear_w4a16(const void* x, kq_xdtype_t x_dtype, int64_t ld
     p.codes = b_codes;
     p.scales = b_scales;
     const int tiles = (int)((R + 127) / 128);
-    // as many CTAs of a cluster along K as two CTAs per SM have room for, two units each at least
-    const int runs = M <= 8 ? 1 : (int)((M + 15) / 16);
-    int splits = 1;
-    while (splits < 8 && (int64_t)tiles * runs * (splits + 1) <= 2 * sms && p.units >= 2 * (splits + 1)) ++splits;
     cudaStream_t st = reinterpret_cast<cudaStream_t>(stream);
     auto go = [&](auto glu, auto nt) {
         constexpr bool GLU = decltype(glu)::value;
         constexpr int NT = decltype(nt)::value;
-        return x_dtype == KQ_X_FP16 ? launch_w4a16<GLU, NT, true>(p, tiles, splits, st) : launch_w4a16<GLU, NT, false>(p, tiles, splits, st);
+        return x_dtype == KQ_X_FP16 ? launch_w4a16<GLU, NT, true>(p, tiles, st) : launch_w4a16<GLU, NT, false>(p, tiles, st);
     };
     using One = std::integral_constant<int, 1>;
     using Two = std::integral_constant<int, 2>;

@@ -33,27 +33,29 @@ kq_status_t launch_rotary(kq::RotaryProblem& p, int sms, cudaStream_t st) {
     const int units = HALF ? (E == 1 ? p.head_dim - p.pairs : (p.head_dim - p.pairs) / E) : (E == 1 ? (p.head_dim + 1) / 2 : p.head_dim / E);
     int rows = 256 / units;                                          // at a time
     if (rows < 1) rows = 1;
-    // A CTA's threads have four rows each: fewer tokens where that leaves SMs without work, and where few tokens have many heads the
-    // heads go over several CTAs, each of which forms the token's sines again (1 token of 40 heads).
-    int64_t per_cta = ((int64_t)rows * kq::kRotaryAhead + p.heads - 1) / p.heads;
-    const int64_t even = (p.rows + 2 * sms - 1) / (2 * sms);
-    if (per_cta > even) per_cta = even;
-    if (per_cta * p.pairs > 4096) per_cta = 4096 / p.pairs;          // 32 KB
-    if (per_cta < 1) per_cta = 1;
+    // Tokens of a CTA: the fewest that give every thread about four rows and leave few of them idle in the last ones (4608 tokens of 36 +
+    // 36 heads: two tokens), but not so many that SMs go without work.  One token of many heads goes over several CTAs, each of which
+    // forms the token's sines again.
+    int64_t per_cta = 1;
+    for (int64_t n = 1; n <= 64 && n * p.pairs <= 4096 && (n == 1 || p.rows >= n * 4 * sms); ++n) {
+        int64_t taken = 0, room = 0;
+        for (int i = 0; i < p.tensors; ++i) {
+            taken += n * p.t[i].heads;
+            room += (n * p.t[i].heads + rows - 1) / rows * rows;
+        }
+        per_cta = n;
+        if (room >= 4 * rows && taken * 8 >= room * 7) break;
+    }
     p.tokens_per_cta = (int)per_cta;
     const int64_t tiles = (p.rows + per_cta - 1) / per_cta;
-    p.heads_per_cta = p.heads;
-    if (tiles < sms && rows < p.heads) {
-        int64_t parts = (2 * sms + tiles - 1) / tiles;
-        const int64_t most = (p.heads + rows - 1) / rows;
-        if (parts > most) parts = most;
-        p.heads_per_cta = (int)((p.heads + parts - 1) / parts);
-    }
-    if (rows > p.heads_per_cta * (int)per_cta) rows = p.heads_per_cta * (int)per_cta;
-    p.by_heads = fast_div((uint32_t)p.heads_per_cta);
+    int most = p.t[0].heads;
+    if (p.tensors > 1 && p.t[1].heads > most) most = p.t[1].heads;
+    if (rows > most * (int)per_cta) rows = most * (int)per_cta;
+    const int64_t spare = (2 * sms + tiles - 1) / tiles, runs = (most * per_cta + rows - 1) / rows;
+    p.head_parts = (int)(spare < runs ? spare : runs);
     cudaLaunchConfig_t cfg;
     cudaLaunchAttribute attr[2];
-    launch_config(&cfg, attr, dim3((unsigned)tiles, (unsigned)((p.heads + p.heads_per_cta - 1) / p.heads_per_cta)), dim3((unsigned)units, (unsigned)rows),
+    launch_config(&cfg, attr, dim3((unsigned)tiles, (unsigned)p.head_parts), dim3((unsigned)units, (unsigned)rows),
                   (size_t)per_cta * p.pairs * sizeof(float2), 1, st);
     return launch(cfg, kq::rotary_kernel<T, E, HALF>, p);
 }
@@ -127,24 +129,30 @@ kq_status_t run_cache(const kq_cache_t* cache, const kq_cache_rows_t* rows, void
     p.rows = r.rows; p.sequences = r.sequences; p.table = r.table; p.table_stride = r.table_stride; p.table_width = r.table_width;
     p.offsets = r.offsets; p.starts = r.starts;
     p.k = r.k; p.v = r.v; p.k_row = r.k_row_stride; p.k_head = r.k_head_stride; p.v_row = r.v_row_stride; p.v_head = r.v_head_stride;
-    const int groups = write ? 4 * ref.blocks : (c.head_dim + 7) / 8;
-    if ((int64_t)c.heads * groups > (1 << 24)) return KQ_ERR_SHAPE;  // (a row's units times 64 rows are counted in 32 bits)
+    const int groups = write ? 2 * ref.blocks : (c.head_dim + 15) / 16;
+    if ((int64_t)c.heads * groups > (1 << 30)) return KQ_ERR_SHAPE;
     p.units = c.heads * groups;
-    p.by_units = fast_div((uint32_t)p.units);
     p.by_groups = fast_div((uint32_t)groups);
-    // four units for each thread of a CTA, fewer rows where that leaves SMs idle
-    int64_t per_cta = (4 * kq::kCacheThreads + p.units - 1) / p.units;
-    const int64_t even = (r.rows + 2 * sms - 1) / (2 * sms);
+    // eight rows for each thread of a CTA (four units in flight, twice), fewer where that leaves SMs idle
+    const int across = p.units < kq::kCacheThreads ? p.units : kq::kCacheThreads;
+    int at_once = kq::kCacheThreads / across;
+    int64_t per_cta = 8 * at_once;
+    const int64_t even = (r.rows + 4 * sms - 1) / (4 * sms);
     if (per_cta > even) per_cta = even;
     if (per_cta > kq::kCacheRowsMax) per_cta = kq::kCacheRowsMax;
-    if (per_cta < 1) per_cta = 1;
+    if (at_once > per_cta) at_once = (int)per_cta;
+    if (at_once * across < 32) at_once = (31 + across) / across;     // (a whole warp searches the offsets)
     p.rows_per_cta = (int)per_cta;
-    const bool vec = c.head_dim % 8 == 0 && rows_aligned(r.k, r.k_row_stride, r.dtype, 16) && rows_aligned(r.k, r.k_head_stride, r.dtype, 16) &&
-                     rows_aligned(r.v, r.v_row_stride, r.dtype, 16) && rows_aligned(r.v, r.v_head_stride, r.dtype, 16);
+    auto allows = [&](int bytes) {
+        return rows_aligned(r.k, r.k_row_stride, r.dtype, bytes) && rows_aligned(r.k, r.k_head_stride, r.dtype, bytes) &&
+               rows_aligned(r.v, r.v_row_stride, r.dtype, bytes) && rows_aligned(r.v, r.v_head_stride, r.dtype, bytes);
+    };
+    const bool vec = c.head_dim % 8 == 0 && allows(16);
+    const int width = !vec ? 0 : (c.head_dim % 16 == 0 && allows(32) ? 32 : 16);
     cudaStream_t st = reinterpret_cast<cudaStream_t>(stream);
     cudaLaunchConfig_t cfg;
     cudaLaunchAttribute attr[2];
-    launch_config(&cfg, attr, dim3((unsigned)((r.rows + per_cta - 1) / per_cta), 2), dim3(kq::kCacheThreads), 0, 1, st);
+    launch_config(&cfg, attr, dim3((unsigned)((r.rows + per_cta - 1) / per_cta), 2), dim3((unsigned)across, (unsigned)at_once), 0, 1, st);
     if (write) {
         auto go = [&](auto type, auto format) {
             using T = decltype(type);
@@ -160,10 +168,10 @@ kq_status_t run_cache(const kq_cache_t* cache, const kq_cache_rows_t* rows, void
     }
     auto by_format = [&](auto type) {
         using T = decltype(type);
-        if (c.format == KQ_CACHE_MXFP4) return launch(cfg, kq::cache_read_kernel<T, kq::kCacheFp4, false>, ref, p, (int)vec);
-        if (c.format == KQ_CACHE_MXFP8) return launch(cfg, kq::cache_read_kernel<T, kq::kCacheFp8, false>, ref, p, (int)vec);
-        if (c.dtype == KQ_OUT_FP16) return launch(cfg, kq::cache_read_kernel<T, kq::kCache16, true>, ref, p, (int)vec);
-        return launch(cfg, kq::cache_read_kernel<T, kq::kCache16, false>, ref, p, (int)vec);
+        if (c.format == KQ_CACHE_MXFP4) return launch(cfg, kq::cache_read_kernel<T, kq::kCacheFp4, false>, ref, p, width);
+        if (c.format == KQ_CACHE_MXFP8) return launch(cfg, kq::cache_read_kernel<T, kq::kCacheFp8, false>, ref, p, width);
+        if (c.dtype == KQ_OUT_FP16) return launch(cfg, kq::cache_read_kernel<T, kq::kCache16, true>, ref, p, width);
+        return launch(cfg, kq::cache_read_kernel<T, kq::kCache16, false>, ref, p, width);
     };
     if (r.dtype == KQ_OUT_FP16) return by_format(__half{});
     if (r.dtype == KQ_OUT_BF16) return by_format(__nv_bfloat16{});
@@ -179,9 +187,10 @@ struct AttentionPlan {
     int tile;                            // positions of a tile
     int per_sm;
     int64_t items, most_tiles;           // most_tiles: of an item
-    int ctas, min_tiles;
+    int ctas, min_run;
     bool whole;                          // no item is split
-    int64_t scratch_floats() const { return whole ? 0 : (int64_t)2 * ctas * (columns * channels + 2 * columns); }
+    int64_t partial_floats() const { return (int64_t)2 * ctas * (columns * channels + 2 * columns); }
+    int64_t scratch_bytes() const { return whole ? 0 : partial_floats() * (int64_t)sizeof(float) + items * (int64_t)sizeof(int2); }
 };
 
 template <typename F>
@@ -226,10 +235,10 @@ AttentionPlan plan_attention(const kq_cache_t& c, const kq_attention_args_t& a, 
     int64_t most = (int64_t)a.table_width * c.page_size;
     if (a.window > 0 && most > a.window) most = a.window;
     p.most_tiles = most <= p.tile ? 1 : (most - 1) / p.tile + 1;
-    p.min_tiles = 2;
+    p.min_run = 3;
     p.whole = p.most_tiles <= 4;
     int64_t ctas = (int64_t)sms * p.per_sm;
-    const int64_t useful = p.whole ? p.items : (p.items * p.most_tiles + p.min_tiles - 1) / p.min_tiles;
+    const int64_t useful = p.whole ? p.items : (p.items * (p.most_tiles + kq::kLead) + p.min_run - 1) / p.min_run;
     p.ctas = (int)(ctas < useful ? ctas : useful);
     return p;
 }
@@ -263,9 +272,12 @@ kq_status_t kroquant_rotary(const kq_rotary_args_t* args, void* stream) {
     if (2 * p.pairs > a.head_dim || p.pairs < 1) return KQ_ERR_SHAPE;
     const int tensors = a.x[1] || a.out[1] ? 2 : 1;
     int bytes = 16;
+    const int64_t far = (int64_t)1 << 31;
     for (int i = 0; i < tensors; ++i) {
         if (a.heads[i] < 1 || a.heads[i] > (1 << 20)) return KQ_ERR_SHAPE;
-        p.heads += a.heads[i];
+        const int64_t strides[] = {a.x_token_stride[i], a.x_head_stride[i], a.out_token_stride[i], a.out_head_stride[i]};
+        for (int64_t stride : strides)
+            if (stride >= far || stride <= -far) return KQ_ERR_SHAPE;
     }
     const int64_t rows = a.batches * a.tokens;
     if (rows == 0) return KQ_OK;
@@ -275,8 +287,8 @@ kq_status_t kroquant_rotary(const kq_rotary_args_t* args, void* stream) {
     for (int i = 0; i < tensors; ++i) {
         if (!a.x[i] || !a.out[i]) return KQ_ERR_NULL;
         if (!element_aligned(a.x[i], a.dtype) || !element_aligned(a.out[i], a.dtype)) return KQ_ERR_ALIGN;
-        p.t[i] = {a.x[i], a.out[i], a.heads[i], a.x_batch_stride[i], a.x_token_stride[i], a.x_head_stride[i],
-                  a.out_batch_stride[i], a.out_token_stride[i], a.out_head_stride[i]};
+        p.t[i] = {a.x[i], a.out[i], a.x_batch_stride[i], a.out_batch_stride[i], a.heads[i], (int)a.x_token_stride[i], (int)a.x_head_stride[i],
+                  (int)a.out_token_stride[i], (int)a.out_head_stride[i], fast_div((uint32_t)a.heads[i])};
         const int64_t strides[] = {a.x_batch_stride[i], a.x_token_stride[i], a.x_head_stride[i], a.out_batch_stride[i], a.out_token_stride[i], a.out_head_stride[i]};
         const int64_t used[] = {a.batches, a.tokens, a.heads[i], a.batches, a.tokens, a.heads[i]};
         for (int width = 16; width >= 8; width /= 2) {
@@ -288,7 +300,7 @@ kq_status_t kroquant_rotary(const kq_rotary_args_t* args, void* stream) {
     }
     const int sms = sm_count();
     if (sms <= 0) return KQ_ERR_CUDA;
-    p.rows = rows; p.tokens = a.tokens; p.head_dim = a.head_dim; p.inverse = a.inverse; p.positions_f32 = a.positions_f32;
+    p.tensors = tensors; p.rows = rows; p.tokens = a.tokens; p.head_dim = a.head_dim; p.inverse = a.inverse; p.positions_f32 = a.positions_f32;
     p.frequencies = a.frequencies; p.positions = a.positions; p.pos_batch = a.position_batch_stride; p.pos_token = a.position_token_stride;
     cudaStream_t st = reinterpret_cast<cudaStream_t>(stream);
     const bool half = a.layout == KQ_ROTARY_HALF;
@@ -302,7 +314,7 @@ kq_status_t kroquant_cache_read(const kq_cache_t* cache, const kq_cache_rows_t* 
 
 int64_t kroquant_cache_attention_scratch_bytes(const kq_cache_t* cache, const kq_attention_args_t* args) {
     if (!cache || !args || check_attention(*cache, *args) != KQ_OK || args->sequences == 0) return 0;
-    return plan_attention(*cache, *args, sm_count()).scratch_floats() * (int64_t)sizeof(float);
+    return plan_attention(*cache, *args, sm_count()).scratch_bytes();
 }
 
 kq_status_t kroquant_cache_attention(const kq_cache_t* cache, const kq_attention_args_t* args, void* scratch, int64_t scratch_bytes, void* stream) {
@@ -321,19 +333,22 @@ kq_status_t kroquant_cache_attention(const kq_cache_t* cache, const kq_attention
     if (!plan.whole) {
         if (!scratch) return KQ_ERR_NULL;
         if (!aligned16(scratch)) return KQ_ERR_ALIGN;
-        if (scratch_bytes < plan.scratch_floats() * (int64_t)sizeof(float)) return KQ_ERR_SHAPE;
+        if (scratch_bytes < plan.scratch_bytes()) return KQ_ERR_SHAPE;
     }
     kq::AttentionProblem p = {};
     p.c = cache_ref(c);
     p.sequences = a.sequences; p.q_heads = a.q_heads; p.group = a.q_heads / c.heads; p.chunks = (p.group + plan.columns - 1) / plan.columns;
-    p.q = a.q; p.q_f16 = a.q_dtype == KQ_OUT_FP16; p.q_row = a.q_row_stride; p.q_head = a.q_head_stride;
+    p.q = a.q; p.q_f16 = a.q_dtype == KQ_OUT_FP16;
+    p.q_vec = reinterpret_cast<uintptr_t>(a.q) % 8 == 0 && a.q_row_stride % 4 == 0 && a.q_head_stride % 4 == 0 && c.head_dim % 4 == 0;
+    p.q_row = a.q_row_stride; p.q_head = a.q_head_stride;
     p.out = a.out; p.out_type = a.out_dtype; p.out_row = a.out_row_stride; p.out_head = a.out_head_stride;
     p.table = a.table; p.table_stride = a.table_stride; p.table_width = a.table_width; p.lengths = a.lengths; p.window = a.window;
     p.scale_log2e = a.scale * 1.4426950408889634f;
     p.lse = a.lse;
     p.partial = plan.whole ? nullptr : static_cast<float*>(scratch);
+    p.parts = plan.whole ? nullptr : reinterpret_cast<int2*>(p.partial + plan.partial_floats());
     p.ctas = plan.ctas;
-    p.min_tiles = plan.min_tiles;
+    p.min_run = plan.min_run;
     cudaStream_t st = reinterpret_cast<cudaStream_t>(stream);
     return with_shape(c.format, c.dtype, plan.channels, plan.columns, [&](auto shape, auto fmt, auto d, auto nq) {
         using L = decltype(shape);
@@ -347,7 +362,7 @@ kq_status_t kroquant_cache_attention(const kq_cache_t* cache, const kq_attention
         r = launch(cfg, kq::cache_attention_kernel<FMT, D, NQ>, p);
         if (r != KQ_OK || plan.whole) return r;
         launch_config(&cfg, attr, dim3((unsigned)plan.items, (unsigned)(p.group < NQ ? p.group : NQ)), dim3(kq::kJoinThreads), 0, 1, st);
-        return launch(cfg, kq::cache_attention_join<L::kTile, D, NQ>, p);
+        return launch(cfg, kq::cache_attention_join<D, NQ>, p);
     });
 }
 

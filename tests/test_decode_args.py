@@ -140,3 +140,12 @@ def test_elements_apart_and_spans():
 def test_frequencies():
     f = kb.rotary_frequencies((4, 6), theta=100.0, device="cpu")
     assert f.dtype is torch.float64 and torch.allclose(f, torch.tensor([1, 0.1, 1, 100 ** (-1 / 3), 100 ** (-2 / 3)], dtype=torch.float64), rtol=1e-15)
+
+
+def test_packed_structs_have_the_layout_of_the_c_ones():
+    import struct
+    for pack, cls in ((kb._PACK_ROTARY, kb._RotaryArgs), (kb._PACK_ROWS, kb._CacheRows), (kb._PACK_ATTENTION, kb._AttentionArgs)):
+        values = [i + 1 for i in range(len(cls._fields_))]
+        a = cls.from_buffer_copy(pack(*values))
+        assert [getattr(a, f[0]) for f in cls._fields_] == values
+    assert struct.calcsize("@P") == 8
