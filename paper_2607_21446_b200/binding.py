@@ -9,6 +9,7 @@ from __future__ import annotations
 
 import contextlib
 import ctypes as C
+import functools
 import os
 import struct
 import threading
@@ -971,7 +972,6 @@ def kroquant_norm_residual_grad(dn: Optional[torch.Tensor], h: torch.Tensor, *, 
 
 # ---- one step over new tokens: positions, the cache of keys and values, attention --------------------------------------
 ROTARY_LAYOUTS = {"interleaved": 0, "half": 1}
-_NO_AXES = (0, 0, 0, 0)
 CACHE_FORMATS = {"16bit": 0, "mxfp8": 1, "mxfp4": 2}
 
 
@@ -1013,6 +1013,15 @@ _PACK_ROWS = struct.Struct("@qiPqiPPiPPqqqq").pack
 _PACK_ATTENTION = struct.Struct("@4iPPqqqqPqiPifP").pack
 
 
+@functools.lru_cache(maxsize=256)
+def _axes_of(axes, pairs: int, d: int):
+    """Number of axes and their channels, filled up to four (a plan by sizes alone)."""
+    axes = (2 * pairs,) if axes is None else axes
+    if not 1 <= len(axes) <= 4 or any(a < 0 or a % 2 for a in axes) or sum(axes) != 2 * pairs or not 0 < 2 * pairs <= d:
+        raise ValueError("axes: one to four even numbers of channels, together twice the frequencies and at most d")
+    return len(axes), axes + (0, 0, 0)[: 4 - len(axes)]
+
+
 def rotary_frequencies(axes, theta: float = 10000.0, device="cuda") -> torch.Tensor:
     """float64 [sum(axes) / 2]: theta ** (-2 i / a) for the a / 2 pairs of every axis of a channels."""
     return torch.cat([theta ** (-torch.arange(0, a, 2, dtype=torch.float64) / a) for a in axes]).to(device)
@@ -1052,33 +1061,30 @@ def kroquant_rotary(q: torch.Tensor, k: Optional[torch.Tensor], positions: torch
     positions[t, i] * frequencies[p], formed in 64 bits; channels behind the axes are copied.  layout: "interleaved" pairs
     (2p, 2p + 1) or "half" (p, p + pairs).  inverse turns back: the backward pass, with the gradients in place of q and k.
     out: tensor, or pair of tensors with k, to write to; each may be its input."""
-    dims = q.dim()
-    if dims not in (3, 4):
-        raise ValueError("q must be [tokens, heads, d] or [batch, tokens, heads, d]")
-    _heads_last(q, "q", dims)
-    shape, dtype, dev = q.shape, q.dtype, q.get_device()
+    shape, qt, dtype, dev = q.shape, q.stride(), q.dtype, _device()
+    dims = len(shape)
+    if dims not in (3, 4) or dtype not in _DTYPES or q.get_device() != dev or (qt[-1] != 1 and shape[-1] > 1):
+        raise ValueError("q must be a CUDA float32, bfloat16 or float16 tensor [tokens, heads, d] or [batch, tokens, heads, d] on the current device "
+                         "with contiguous channels")
     d, tokens, batches = shape[-1], shape[-3], shape[0] if dims == 4 else 1
     if k is not None:
-        _heads_last(k, "k", dims)
-        if k.dtype is not dtype or k.shape[-1] != d or k.shape[:-2] != shape[:-2]:
-            raise ValueError("k must have q's dtype and shape but for the number of heads")
+        ks, kt = k.shape, k.stride()
+        if len(ks) != dims or k.dtype is not dtype or k.get_device() != dev or ks[-1] != d or ks[-3] != tokens or (dims == 4 and ks[0] != batches) or \
+                (kt[-1] != 1 and d > 1):
+            raise ValueError("k must have q's dtype, device and shape but for the number of heads, and contiguous channels")
+    pairs = frequencies.numel()
     if frequencies.dtype is not torch.float64 or frequencies.dim() != 1 or frequencies.get_device() != dev or not frequencies.is_contiguous():
         raise ValueError("frequencies must be a contiguous CUDA float64 tensor [pairs]")
-    pairs = frequencies.shape[0]
-    axes = (2 * pairs,) if axes is None else tuple(axes)
-    n = len(axes)
-    if not 1 <= n <= 4 or any(a < 0 or a % 2 for a in axes) or sum(axes) != 2 * pairs or not 0 < 2 * pairs <= d:
-        raise ValueError("axes: one to four even numbers of channels, together twice the frequencies and at most d")
+    n, wide = _axes_of(None if axes is None else tuple(axes), pairs, d)
     way = ROTARY_LAYOUTS.get(layout)
     if way is None:
         raise ValueError(f"layout must be one of {sorted(ROTARY_LAYOUTS)}")
-    if positions.dtype not in (torch.int32, torch.float32) or positions.get_device() != dev:
-        raise ValueError("positions must be a CUDA int32 or float32 tensor")
     place, ps = positions.shape, positions.stride()
     if n == 1 and len(place) == 1:
         place, ps = (place[0], 1), (ps[0], 1)
-    if place != (tokens, n) and (dims != 4 or place != (batches, tokens, n)) or (n > 1 and ps[-1] != 1):
-        raise ValueError("positions must be [tokens, axes], or [batch, tokens, axes], with contiguous axes")
+    if (positions.dtype is not torch.int32 and positions.dtype is not torch.float32) or positions.get_device() != dev or \
+            (place != (tokens, n) and (dims != 4 or place != (batches, tokens, n))) or (n > 1 and ps[-1] != 1):
+        raise ValueError("positions must be a CUDA int32 or float32 tensor [tokens, axes], or [batch, tokens, axes], with contiguous axes")
     outs = (None, None) if out is None else (out, None) if k is None else tuple(out)
     made = []
     for x, o in ((q, outs[0]), (k, outs[1])):
@@ -1095,22 +1101,17 @@ def kroquant_rotary(q: torch.Tensor, k: Optional[torch.Tensor], positions: torch
                 raise ValueError("out may be its input, but must not overlap it in another way")
         made.append(o)
 
-    if dims == 3:
-        (xt, xh, _), (ot, oh, _) = q.stride(), made[0].stride()
-        xb = ob = 0
+    ot, no_k = made[0].stride(), k is None
+    if no_k:
+        kt = pt = (0, 0, 0, 0)
     else:
-        (xb, xt, xh, _), (ob, ot, oh, _) = q.stride(), made[0].stride()
-    if k is None:
-        k_at = ko_at = kv = kb = kt = kh = pb = pt = ph = 0
-    else:
-        k_at, ko_at, kv, kb, pb = k.data_ptr(), made[1].data_ptr(), k.shape[-2], 0, 0
-        if dims == 3:
-            (kt, kh, _), (pt, ph, _) = k.stride(), made[1].stride()
-        else:
-            (kb, kt, kh, _), (pb, pt, ph, _) = k.stride(), made[1].stride()
-    a = _PACK_ROTARY(_DTYPES[dtype], batches, tokens, d, way, 1 if inverse else 0, n, *axes, *_NO_AXES[n:], frequencies.data_ptr(),
+        pt = made[1].stride()
+    batched = dims == 4
+    a = _PACK_ROTARY(_DTYPES[dtype], batches, tokens, d, way, 1 if inverse else 0, n, *wide, frequencies.data_ptr(),
                      positions.data_ptr(), 1 if positions.dtype is torch.float32 else 0, ps[0] if len(ps) == 3 else 0, ps[-2],
-                     q.data_ptr(), k_at, made[0].data_ptr(), ko_at, shape[-2], kv, xb, kb, xt, kt, xh, kh, ob, pb, ot, pt, oh, ph)
+                     q.data_ptr(), 0 if no_k else k.data_ptr(), made[0].data_ptr(), 0 if no_k else made[1].data_ptr(), shape[-2], 0 if no_k else ks[-2],
+                     qt[0] if batched else 0, kt[0] if batched else 0, qt[-3], kt[-3], qt[-2], kt[-2],
+                     ot[0] if batched else 0, pt[0] if batched else 0, ot[-3], pt[-3], ot[-2], pt[-2])
     rc = load_library().kroquant_rotary(a, _stream(stream))
     if rc:
         raise KroQuantError(rc, "kroquant_rotary")

@@ -9,7 +9,7 @@
 // Both directions are bound by memory (2 bytes of 16-bit values and 0.53, 1.03 or 2 bytes of cache per element) or, for a few rows,
 // by latency.  A thread keeps a place within a row, 16 channels of one head, and walks the rows of its CTA, so that what it computes
 // per 16 channels is two addresses and the code; the two threads of a block of 32 channels exchange its largest magnitude by one
-// shuffle.  The cell of a row (a search of offsets by one warp, 32 entries at a time, and one table entry) is found once per CTA and row.
+// shuffle.  The cell of a row (a search of offsets and one table entry) is found once per CTA and row.
 #pragma once
 #include "kq_mma16.cuh"
 #include "kq_rotary.cuh"
@@ -52,38 +52,25 @@ struct CacheRows {
     FastDiv by_groups;
 };
 
-// The last sequence whose offset is <= row, by one warp: 32 entries at a time.
-__device__ __forceinline__ int find_sequence(const int32_t* offsets, int sequences, int64_t row, int lane) {
-    int lo = 0, count = sequences;                                       // offsets[lo] <= row < offsets[lo + count] where row has one
-    while (count > 1) {
-        const int step = (count + 31) / 32;
-        const int at = lane * step;
-        const bool below = at < count && (lane == 0 || __ldg(offsets + lo + at) <= row);
-        const uint32_t mask = __ballot_sync(0xFFFFFFFFu, below);
-        const int last = 31 - __clz(mask);                                // (with offsets out of order: some entry, in range all the same)
-        lo += last * step;
-        count = count - last * step < step ? count - last * step : step;
-    }
-    return lo;
-}
-// cells[i]: of row row0 + i for head 0; -1: no place, -2: a row of no sequence.  All threads of the CTA.
+// cells[i]: of row row0 + i for head 0; -1: no place, -2: a row of no sequence.  All threads of the CTA, one per row.
 __device__ __forceinline__ void find_cells(const CacheRef& c, const CacheRows& p, int64_t row0, int rows, int64_t* cells, int thread, int threads) {
-    const int lane = thread & 31, whole = threads >> 5;                   // (a last warp that is not whole leaves the search to the others)
-    if (!p.offsets) {
-        for (int i = thread; i < rows; i += threads) {
-            const int64_t s = row0 + i;
-            cells[i] = cache_cell(c, p.table + s * p.table_stride, p.table_width, p.starts ? (int64_t)__ldg(p.starts + s) : 0);
-        }
-    } else if (thread >> 5 < whole) {
-        for (int i = thread >> 5; i < rows; i += whole) {
-            const int64_t row = row0 + i;
-            const int s = find_sequence(p.offsets, p.sequences, row, lane);
-            if (lane == 0) {
-                const int64_t first = __ldg(p.offsets + s), position = (p.starts ? (int64_t)__ldg(p.starts + s) : 0) + (row - first);
-                const bool exists = row >= first && row < __ldg(p.offsets + s + 1);
-                cells[i] = exists ? cache_cell(c, p.table + (int64_t)s * p.table_stride, p.table_width, position) : -2;
+    for (int i = thread; i < rows; i += threads) {
+        const int64_t row = row0 + i;
+        int s = (int)row;
+        int64_t first = row;
+        bool exists = true;
+        if (p.offsets) {
+            int lo = 0, hi = p.sequences;                                // the last sequence whose offset is <= row (offsets out of order: some sequence)
+            while (hi - lo > 1) {
+                const int mid = (lo + hi) >> 1;
+                if (__ldg(p.offsets + mid) <= row) lo = mid; else hi = mid;
             }
+            s = lo;
+            first = __ldg(p.offsets + s);
+            exists = row >= first && row < __ldg(p.offsets + s + 1);
         }
+        const int64_t position = (p.starts ? (int64_t)__ldg(p.starts + s) : 0) + (row - first);
+        cells[i] = exists ? cache_cell(c, p.table + (int64_t)s * p.table_stride, p.table_width, position) : -2;
     }
     __syncthreads();
 }
@@ -100,12 +87,20 @@ __device__ __forceinline__ uint2 e4m3x8(const float (&v)[8]) {
     }
     return make_uint2(h[0] | (h[1] << 16), h[2] | (h[3] << 16));
 }
+__device__ __forceinline__ float2 scale_pair(float2 f, float scale) {
+    unsigned long long v, s;
+    asm("mov.b64 %0, {%1, %2};" : "=l"(v) : "f"(f.x), "f"(f.y));
+    asm("mov.b64 %0, {%1, %1};" : "=l"(s) : "f"(scale));
+    asm("mul.rn.f32x2 %0, %0, %1;" : "+l"(v) : "l"(s));
+    asm("mov.b64 {%0, %1}, %2;" : "=f"(f.x), "=f"(f.y) : "l"(v));
+    return f;
+}
 __device__ __forceinline__ void store_32_bytes(void* p, uint32_t a, uint32_t b, uint32_t c, uint32_t d, uint32_t e, uint32_t f, uint32_t g, uint32_t h) {
     asm volatile("st.global.v8.b32 [%0], {%1,%2,%3,%4,%5,%6,%7,%8};"
                  ::"l"(p), "r"(a), "r"(b), "r"(c), "r"(d), "r"(e), "r"(f), "r"(g), "r"(h) : "memory");
 }
 
-constexpr int kCacheThreads = 256;       // at most, and at least 32
+constexpr int kCacheThreads = 256;       // at most
 constexpr int kCacheRowsMax = 64;        // rows of a CTA
 
 // blockDim: x = units of a row (or 256 of them), y = rows at a time.  blockIdx.y: keys, values.  T: type of the rows.  VEC: rows allow
@@ -287,9 +282,9 @@ __global__ void __launch_bounds__(kCacheThreads) cache_read_kernel(const __grid_
                         constexpr int kPairs = FORMAT == kCacheFp8 ? 2 : 4;
 #pragma unroll
                         for (int q = 0; q < kPairs; ++q) {
-                            const float2 f = __half22float2(*reinterpret_cast<const __half2*>(&h[q]));
-                            v[2 * (kPairs * i + q)] = f.x * scale;
-                            v[2 * (kPairs * i + q) + 1] = f.y * scale;
+                            const float2 f = scale_pair(__half22float2(*reinterpret_cast<const __half2*>(&h[q])), scale);
+                            v[2 * (kPairs * i + q)] = f.x;
+                            v[2 * (kPairs * i + q) + 1] = f.y;
                         }
                     }
                 }

@@ -178,19 +178,21 @@ __global__ void __launch_bounds__(kAttnThreads, (AttnShape<FMT, D, NQ>::kPerSm))
     int64_t at = 0, stop = 0, quota = 0;
     int seq = 0, item = 0, unit = 0;                                     // unit: of the item, kLead and then its tiles
     if (p.partial) {
-        int64_t sum = 0;
-        for (int s = lane; s < p.sequences; s += 32) sum += tiles_of<L::kTile>(visible_range(p, s)) + kLead;
+        // units of the sequences 0 .. 31, a lane each: most calls need no others
+        const int n0 = lane < p.sequences ? tiles_of<L::kTile>(visible_range(p, lane)) + kLead : 0;
+        int64_t sum = n0;
+        for (int s = lane + 32; s < p.sequences; s += 32) sum += tiles_of<L::kTile>(visible_range(p, s)) + kLead;
 #pragma unroll
         for (int o = 16; o > 0; o >>= 1) sum += __shfl_xor_sync(0xFFFFFFFFu, sum, o);
-        const int64_t total = sum * per_seq;
-        quota = (total + p.ctas - 1) / p.ctas;
+        const int64_t total = sum * per_seq, rounded = total + p.ctas - 1;
+        quota = rounded < 0x7FFFFFFF ? (uint32_t)rounded / (uint32_t)p.ctas : rounded / p.ctas;      // (32 bits divide in a third of the time)
         if (quota < p.min_run) quota = p.min_run;
         at = blockIdx.x * quota;
         stop = at + quota < total ? at + quota : total;
         if (at >= stop) return;
         int64_t before = 0;                                              // units per head of the sequences before
         for (int s0 = 0;; s0 += 32) {
-            const int n = s0 + lane < p.sequences ? tiles_of<L::kTile>(visible_range(p, s0 + lane)) + kLead : 0;
+            const int n = s0 == 0 ? n0 : s0 + lane < p.sequences ? tiles_of<L::kTile>(visible_range(p, s0 + lane)) + kLead : 0;
             int64_t upto = n;
 #pragma unroll
             for (int o = 1; o < 32; o <<= 1) {
@@ -203,7 +205,7 @@ __global__ void __launch_bounds__(kAttnThreads, (AttnShape<FMT, D, NQ>::kPerSm))
                 seq = s0 + first;
                 const int units = __shfl_sync(0xFFFFFFFFu, n, first);
                 const int64_t rest = at - (before + __shfl_sync(0xFFFFFFFFu, upto, first) - units) * per_seq;
-                item = (int)(rest / units);
+                item = (int)(rest < 0x7FFFFFFF ? (uint32_t)rest / (uint32_t)units : rest / units);
                 unit = (int)(rest - (int64_t)item * units);
                 break;
             }
@@ -239,9 +241,10 @@ __global__ void __launch_bounds__(kAttnThreads, (AttnShape<FMT, D, NQ>::kPerSm))
                 ++seq;
             }
             if (count == 0) continue;                                    // (the item's lead alone)
+            const bool whole_run = count == tiles;
             if (tile == 0 && threadIdx.x == 0)
                 p.parts[(int64_t)seq_now * per_seq + item_now] =
-                    make_int2((int)blockIdx.x, (int)((item_at + kLead + tiles - 1) / quota) - (int)blockIdx.x + 1);
+                    make_int2((int)blockIdx.x, whole_run ? 1 : (int)((item_at + kLead + tiles - 1) / quota) - (int)blockIdx.x + 1);
             s_seq = seq_now;
             s_item = item_now;
         } else {
@@ -264,74 +267,6 @@ __global__ void __launch_bounds__(kAttnThreads, (AttnShape<FMT, D, NQ>::kPerSm))
                 for (int i = lane; i < L::kRing / 16; i += 32) reinterpret_cast<uint4*>(ring)[i] = make_uint4(0, 0, 0, 0);
             first_segment = false;
             __syncwarp();
-        }
-
-        // ---- queries: operand registers and their power of two ----
-        uint32_t qf[kM][NT][2];
-        float q_scale = p.scale_log2e;
-        uint32_t amax = 0;                                               // of the magnitude bits
-#pragma unroll
-        for (int nt = 0; nt < NT; ++nt) {
-            const int row = chunk * NQ + nt * 8 + g;                     // query head within the group
-            const bool exists = row < p.group;
-            const uint16_t* q = static_cast<const uint16_t*>(p.q) + (int64_t)s_seq * p.q_row + (int64_t)(head * p.group + (exists ? row : 0)) * p.q_head;
-#pragma unroll
-            for (int m = 0; m < kM; ++m) {
-                const int ch = L::k_channel(m, j);
-                uint32_t v[4] = {0, 0, 0, 0};
-                if (p.q_vec) {                                           // four channels at a time
-                    if (exists && ch < p.c.head_dim) {
-                        const uint2 w = __ldg(reinterpret_cast<const uint2*>(q + ch));
-                        v[0] = w.x & 0xFFFFu; v[1] = w.x >> 16; v[2] = w.y & 0xFFFFu; v[3] = w.y >> 16;
-                    }
-                } else {
-#pragma unroll
-                    for (int i = 0; i < 4; ++i)
-                        if (exists && ch + i < p.c.head_dim) v[i] = q[ch + i];
-                }
-#pragma unroll
-                for (int i = 0; i < 4; ++i) amax = max(amax, v[i] & 0x7FFFu);
-                qf[m][nt][0] = v[0] | (v[1] << 16);
-                qf[m][nt][1] = v[2] | (v[3] << 16);
-            }
-        }
-        if constexpr (L::kCodes) {
-            amax = __reduce_max_sync(0xFFFFFFFFu, amax);
-            const float top = p.q_f16 ? __half2float(__ushort_as_half((unsigned short)amax)) : __uint_as_float(amax << 16);
-            int e = (int)(__float_as_uint(top) >> 23) - 127;             // (0 and subnormal values: -127)
-            e = e < -100 ? -100 : e;
-            const float up = exp2_int(14 - e);
-#pragma unroll
-            for (int nt = 0; nt < NT; ++nt)
-#pragma unroll
-                for (int m = 0; m < kM; ++m)
-#pragma unroll
-                    for (int i = 0; i < 2; ++i) {
-                        const uint32_t w = qf[m][nt][i];
-                        float lo, hi;
-                        if (p.q_f16) {
-                            lo = __half2float(__ushort_as_half((unsigned short)(w & 0xFFFFu)));
-                            hi = __half2float(__ushort_as_half((unsigned short)(w >> 16)));
-                        } else {
-                            lo = bf16lo_to_f32(w);
-                            hi = bf16hi_to_f32(w);
-                        }
-                        qf[m][nt][i] = pack_f16(lo * up, hi * up);
-                    }
-            q_scale *= exp2_int(e - 14 - L::kLift);
-        }
-
-        float o[kM][NT][4];
-        float m_run[NT][2], l_run[NT][2];
-        int v_run = 0;                                                   // R of the comment above
-#pragma unroll
-        for (int nt = 0; nt < NT; ++nt) {
-#pragma unroll
-            for (int m = 0; m < kM; ++m)
-#pragma unroll
-                for (int i = 0; i < 4; ++i) o[m][nt][i] = 0.f;
-            m_run[nt][0] = m_run[nt][1] = kMinus;
-            l_run[nt][0] = l_run[nt][1] = 0.f;
         }
 
         // ---- copies of a step ----
@@ -377,8 +312,76 @@ __global__ void __launch_bounds__(kAttnThreads, (AttnShape<FMT, D, NQ>::kPerSm))
             asm volatile("cp.async.commit_group;" ::: "memory");
         };
 
+        // ---- queries: operand registers and their power of two ----
+        uint32_t qf[kM][NT][2];
+        float q_scale = p.scale_log2e;
+        uint32_t amax = 0;                                               // of the magnitude bits
+#pragma unroll
+        for (int nt = 0; nt < NT; ++nt) {
+            const int row = chunk * NQ + nt * 8 + g;                     // query head within the group
+            const bool exists = row < p.group;
+            const uint16_t* q = static_cast<const uint16_t*>(p.q) + (int64_t)s_seq * p.q_row + (int64_t)(head * p.group + (exists ? row : 0)) * p.q_head;
+#pragma unroll
+            for (int m = 0; m < kM; ++m) {
+                const int ch = L::k_channel(m, j);
+                uint32_t v[4] = {0, 0, 0, 0};
+                if (p.q_vec) {                                           // four channels at a time
+                    if (exists && ch < p.c.head_dim) {
+                        const uint2 w = __ldg(reinterpret_cast<const uint2*>(q + ch));
+                        v[0] = w.x & 0xFFFFu; v[1] = w.x >> 16; v[2] = w.y & 0xFFFFu; v[3] = w.y >> 16;
+                    }
+                } else {
+#pragma unroll
+                    for (int i = 0; i < 4; ++i)
+                        if (exists && ch + i < p.c.head_dim) v[i] = q[ch + i];
+                }
+#pragma unroll
+                for (int i = 0; i < 4; ++i) amax = max(amax, v[i] & 0x7FFFu);
+                qf[m][nt][0] = v[0] | (v[1] << 16);
+                qf[m][nt][1] = v[2] | (v[3] << 16);
+            }
+        }
+        float o[kM][NT][4];
+        float m_run[NT][2], l_run[NT][2];
+        int v_run = 0;                                                   // R of the comment above
+#pragma unroll
+        for (int nt = 0; nt < NT; ++nt) {
+#pragma unroll
+            for (int m = 0; m < kM; ++m)
+#pragma unroll
+                for (int i = 0; i < 4; ++i) o[m][nt][i] = 0.f;
+            m_run[nt][0] = m_run[nt][1] = kMinus;
+            l_run[nt][0] = l_run[nt][1] = 0.f;
+        }
+
 #pragma unroll
         for (int i = 0; i < L::kStages - 1; ++i) issue(i);
+        if constexpr (L::kCodes) {
+            amax = __reduce_max_sync(0xFFFFFFFFu, amax);
+            const float top = p.q_f16 ? __half2float(__ushort_as_half((unsigned short)amax)) : __uint_as_float(amax << 16);
+            int e = (int)(__float_as_uint(top) >> 23) - 127;             // (0 and subnormal values: -127)
+            e = e < -100 ? -100 : e;
+            const float up = exp2_int(14 - e);
+#pragma unroll
+            for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+                for (int m = 0; m < kM; ++m)
+#pragma unroll
+                    for (int i = 0; i < 2; ++i) {
+                        const uint32_t w = qf[m][nt][i];
+                        float lo, hi;
+                        if (p.q_f16) {
+                            lo = __half2float(__ushort_as_half((unsigned short)(w & 0xFFFFu)));
+                            hi = __half2float(__ushort_as_half((unsigned short)(w >> 16)));
+                        } else {
+                            lo = bf16lo_to_f32(w);
+                            hi = bf16hi_to_f32(w);
+                        }
+                        qf[m][nt][i] = pack_f16(lo * up, hi * up);
+                    }
+            q_scale *= exp2_int(e - 14 - L::kLift);
+        }
+
         int use = 0;
         for (int it = 0; it < my_steps; ++it) {
             asm volatile("cp.async.wait_group %0;" ::"n"(L::kStages - 2) : "memory");

@@ -31,32 +31,27 @@ kq_status_t allow_shared(DeviceOnce& once, Kernel* kernel, int bytes) {
 template <typename T, int E, bool HALF>
 kq_status_t launch_rotary(kq::RotaryProblem& p, int sms, cudaStream_t st) {
     const int units = HALF ? (E == 1 ? p.head_dim - p.pairs : (p.head_dim - p.pairs) / E) : (E == 1 ? (p.head_dim + 1) / 2 : p.head_dim / E);
-    int rows = 256 / units;                                          // at a time
+    int rows = 192 / units;                                          // at a time
     if (rows < 1) rows = 1;
-    // Tokens of a CTA: the fewest that give every thread about four rows and leave few of them idle in the last ones (4608 tokens of 36 +
-    // 36 heads: two tokens), but not so many that SMs go without work.  One token of many heads goes over several CTAs, each of which
-    // forms the token's sines again.
-    int64_t per_cta = 1;
-    for (int64_t n = 1; n <= 64 && n * p.pairs <= 4096 && (n == 1 || p.rows >= n * 4 * sms); ++n) {
-        int64_t taken = 0, room = 0;
-        for (int i = 0; i < p.tensors; ++i) {
-            taken += n * p.t[i].heads;
-            room += (n * p.t[i].heads + rows - 1) / rows * rows;
-        }
-        per_cta = n;
-        if (room >= 4 * rows && taken * 8 >= room * 7) break;
-    }
+    int heads = p.t[0].heads + (p.tensors > 1 ? p.t[1].heads : 0);
+    // Tokens of a CTA: all CTAs run at once (five on an SM), since a second wave that is not full costs as much as the first.  One token of
+    // many heads goes over several CTAs, each of which forms the token's sines again.
+    int64_t per_cta = (p.rows + 5 * sms - 1) / (5 * sms);
+    if (per_cta * p.pairs > 2048) per_cta = 2048 / p.pairs;          // 16 KB
+    if (per_cta < 1) per_cta = 1;
     p.tokens_per_cta = (int)per_cta;
-    const int64_t tiles = (p.rows + per_cta - 1) / per_cta;
-    int most = p.t[0].heads;
-    if (p.tensors > 1 && p.t[1].heads > most) most = p.t[1].heads;
-    if (rows > most * (int)per_cta) rows = most * (int)per_cta;
-    const int64_t spare = (2 * sms + tiles - 1) / tiles, runs = (most * per_cta + rows - 1) / rows;
+    const int64_t tiles = (p.rows + per_cta - 1) / per_cta, taken = heads * per_cta;
+    const int64_t spare = tiles < sms ? (2 * sms + tiles - 1) / tiles : 1, runs = (taken + rows - 1) / rows;
     p.head_parts = (int)(spare < runs ? spare : runs);
+    if (rows > taken) rows = (int)taken;
+    const int smem = (units * rows * kq::rotary_slot_bytes<T, E, HALF>() + 15) / 16 * 16 + (int)per_cta * p.pairs * (int)sizeof(float2);
+    static DeviceOnce attr_done;
+    const kq_status_t rc = allow_shared(attr_done, kq::rotary_kernel<T, E, HALF>, 100 * 1024);
+    if (rc != KQ_OK) return rc;
     cudaLaunchConfig_t cfg;
     cudaLaunchAttribute attr[2];
     launch_config(&cfg, attr, dim3((unsigned)tiles, (unsigned)p.head_parts), dim3((unsigned)units, (unsigned)rows),
-                  (size_t)per_cta * p.pairs * sizeof(float2), 1, st);
+                  (size_t)smem, 1, st);
     return launch(cfg, kq::rotary_kernel<T, E, HALF>, p);
 }
 template <typename T>
@@ -141,7 +136,6 @@ kq_status_t run_cache(const kq_cache_t* cache, const kq_cache_rows_t* rows, void
     if (per_cta > even) per_cta = even;
     if (per_cta > kq::kCacheRowsMax) per_cta = kq::kCacheRowsMax;
     if (at_once > per_cta) at_once = (int)per_cta;
-    if (at_once * across < 32) at_once = (31 + across) / across;     // (a whole warp searches the offsets)
     p.rows_per_cta = (int)per_cta;
     auto allows = [&](int bytes) {
         return rows_aligned(r.k, r.k_row_stride, r.dtype, bytes) && rows_aligned(r.k, r.k_head_stride, r.dtype, bytes) &&
@@ -236,7 +230,7 @@ AttentionPlan plan_attention(const kq_cache_t& c, const kq_attention_args_t& a, 
     if (a.window > 0 && most > a.window) most = a.window;
     p.most_tiles = most <= p.tile ? 1 : (most - 1) / p.tile + 1;
     p.min_run = 3;
-    p.whole = p.most_tiles <= 4;
+    p.whole = p.most_tiles <= 8;
     int64_t ctas = (int64_t)sms * p.per_sm;
     const int64_t useful = p.whole ? p.items : (p.items * (p.most_tiles + kq::kLead) + p.min_run - 1) / p.min_run;
     p.ctas = (int)(ctas < useful ? ctas : useful);
