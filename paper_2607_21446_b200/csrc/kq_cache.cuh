@@ -101,7 +101,7 @@ __device__ __forceinline__ void store_32_bytes(void* p, uint32_t a, uint32_t b, 
 }
 
 constexpr int kCacheThreads = 256;       // at most
-constexpr int kCacheRowsMax = 64;        // rows of a CTA
+constexpr int kCacheRowsMax = 256;       // rows of a CTA
 
 // blockDim: x = units of a row (or 256 of them), y = rows at a time.  blockIdx.y: keys, values.  T: type of the rows.  VEC: rows allow
 // 16-byte accesses and head_dim is a multiple of 8.

@@ -16,11 +16,11 @@
 // all banks (an asynchronous copy that puts the halves of 32 bytes apart takes several times as long).
 //
 // Scales.  A code times 2^(S - 127) would leave fp16, so K is taken relative to the largest scale byte of its position (a factor of the
-// score, fp32) and V relative to the largest of its position, which goes into P: p 2^(S_t - R + 14), R the largest S_t so far (a
+// score, fp32) and V relative to the largest of its position, which goes into P: p 2^(S_t - R + 9), R the largest S_t so far (a
 // running maximum that rescales the accumulator as m does).  Code times 2^(S - S_t + kLift) has at most 4 significant bits and is exact in
 // fp16; a block whose scale is 2^-28 (E2M1) or 2^-21 (E4M3) of its position's largest, or less, counts as zero.  The queries of a CTA are
 // fp16 times one power of two, exact for both 16-bit types down to values 2^-29 of the largest.  P is rounded to fp16 (11 bits; a weight
-// below 2^-28 of the largest keeps fewer, which is 2^-39 of the largest value at most), with bf16 values to two bf16 terms (16 bits).
+// below 2^-23 of the largest keeps fewer, which is 2^-34 of the largest value at most), with bf16 values to two bf16 terms (16 bits).
 //
 // Work.  Tiles (4 steps) of all (sequence, head) items are laid end to end, each item led by kLead tiles' worth of nothing for what
 // beginning and ending it costs, and every CTA takes an equal run: ragged batches balance, one long sequence fills the GPU.  An
@@ -30,6 +30,11 @@
 #include "kq_cache.cuh"
 
 namespace kq {
+
+// The running maximum follows the scores only when one exceeds it by more than kSlack (in powers of two), so that the accumulator is seldom
+// rescaled: weights are then up to 2^kSlack, times 2^kPLift below fp16's largest.
+constexpr float kSlack = 6;
+constexpr int kPLift = 9;
 
 enum { kAttnBf16 = 0, kAttnF16 = 1, kAttnFp8 = 2, kAttnFp4 = 3 };
 constexpr int kAttnWarps = 4;
@@ -114,7 +119,7 @@ struct AttnShape {
     static constexpr int kBytes = kStatsOff + kAttnWarps * NQ * 2 * 4;
     // CTAs of an SM: what registers (operands and accumulators of a lane, some 60 besides) and shared memory allow
     static constexpr int kRegs = D * NQ / 32 + D * NQ / 64;
-    static constexpr int kByRegs = kRegs <= 48 ? 4 : (kRegs <= 96 ? 3 : 2);
+        static constexpr int kByRegs = kRegs <= 48 ? 4 : (kRegs <= 96 ? 3 : 2);
     static constexpr int kBySmem = 227 * 1024 / (kBytes + 1024);
     static constexpr int kPerSm = kByRegs < kBySmem ? kByRegs : kBySmem;
     static_assert(kPerSm >= 1 && kStageBytes % 16 == 0 && kWarpBytes % 16 == 0, "shared memory");
@@ -315,7 +320,6 @@ __global__ void __launch_bounds__(kAttnThreads, (AttnShape<FMT, D, NQ>::kPerSm))
         // ---- queries: operand registers and their power of two ----
         uint32_t qf[kM][NT][2];
         float q_scale = p.scale_log2e;
-        uint32_t amax = 0;                                               // of the magnitude bits
 #pragma unroll
         for (int nt = 0; nt < NT; ++nt) {
             const int row = chunk * NQ + nt * 8 + g;                     // query head within the group
@@ -324,23 +328,22 @@ __global__ void __launch_bounds__(kAttnThreads, (AttnShape<FMT, D, NQ>::kPerSm))
 #pragma unroll
             for (int m = 0; m < kM; ++m) {
                 const int ch = L::k_channel(m, j);
-                uint32_t v[4] = {0, 0, 0, 0};
-                if (p.q_vec) {                                           // four channels at a time
-                    if (exists && ch < p.c.head_dim) {
-                        const uint2 w = __ldg(reinterpret_cast<const uint2*>(q + ch));
-                        v[0] = w.x & 0xFFFFu; v[1] = w.x >> 16; v[2] = w.y & 0xFFFFu; v[3] = w.y >> 16;
-                    }
+                if (p.q_vec) {                                           // four channels at a time; nothing waits for them yet
+                    uint2 w = make_uint2(0, 0);
+                    if (exists && ch < p.c.head_dim) w = __ldg(reinterpret_cast<const uint2*>(q + ch));
+                    qf[m][nt][0] = w.x;
+                    qf[m][nt][1] = w.y;
                 } else {
+                    uint32_t v[4] = {0, 0, 0, 0};
 #pragma unroll
                     for (int i = 0; i < 4; ++i)
                         if (exists && ch + i < p.c.head_dim) v[i] = q[ch + i];
+                    qf[m][nt][0] = v[0] | (v[1] << 16);
+                    qf[m][nt][1] = v[2] | (v[3] << 16);
                 }
-#pragma unroll
-                for (int i = 0; i < 4; ++i) amax = max(amax, v[i] & 0x7FFFu);
-                qf[m][nt][0] = v[0] | (v[1] << 16);
-                qf[m][nt][1] = v[2] | (v[3] << 16);
             }
         }
+
         float o[kM][NT][4];
         float m_run[NT][2], l_run[NT][2];
         int v_run = 0;                                                   // R of the comment above
@@ -357,6 +360,13 @@ __global__ void __launch_bounds__(kAttnThreads, (AttnShape<FMT, D, NQ>::kPerSm))
 #pragma unroll
         for (int i = 0; i < L::kStages - 1; ++i) issue(i);
         if constexpr (L::kCodes) {
+            uint32_t amax = 0;                                           // of the magnitude bits
+#pragma unroll
+            for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+                for (int m = 0; m < kM; ++m)
+#pragma unroll
+                    for (int i = 0; i < 2; ++i) amax = max(amax, max(qf[m][nt][i] & 0x7FFFu, (qf[m][nt][i] >> 16) & 0x7FFFu));
             amax = __reduce_max_sync(0xFFFFFFFFu, amax);
             const float top = p.q_f16 ? __half2float(__ushort_as_half((unsigned short)amax)) : __uint_as_float(amax << 16);
             int e = (int)(__float_as_uint(top) >> 23) - 127;             // (0 and subnormal values: -127)
@@ -416,9 +426,9 @@ __global__ void __launch_bounds__(kAttnThreads, (AttnShape<FMT, D, NQ>::kPerSm))
                     for (int b = 0; b < D / 32; ++b)
                         mul[(kv * (D / 32) + b) * L::kStep + lane] = (uint16_t)(max(S[b] - most + 15 + L::kLift, 0) << 10);
                 }
-                k_factor *= exp2_int(top[0] - 127);
+                k_factor *= __uint_as_float((uint32_t)top[0] << 23);     // 2^(S - 127)
                 v_new = max(v_run, (int)__reduce_max_sync(0xFFFFFFFFu, top[1]));     // (0 where there is no position)
-                v_factor = exp2_int(top[1] - v_new + 14);
+                v_factor = __uint_as_float((uint32_t)max(top[1] - v_new + 127 + kPLift, 0) << 23);
                 __syncwarp();
             }
 
@@ -506,7 +516,7 @@ __global__ void __launch_bounds__(kAttnThreads, (AttnShape<FMT, D, NQ>::kPerSm))
                 for (int h = 0; h < 2; ++h) {
                     const int k = 16 * mt + 8 * h + g;
                     float kf = q_scale;
-                    vf[mt][h] = FMT == kAttnF16 ? 16384.f : 1.f;
+                    vf[mt][h] = FMT == kAttnF16 ? (float)(1 << kPLift) : 1.f;
                     if constexpr (L::kCodes) {
                         kf = __shfl_sync(0xFFFFFFFFu, k_factor, k);
                         vf[mt][h] = __shfl_sync(0xFFFFFFFFu, v_factor, k);
@@ -530,9 +540,9 @@ __global__ void __launch_bounds__(kAttnThreads, (AttnShape<FMT, D, NQ>::kPerSm))
                     m = fmaxf(m, __shfl_xor_sync(0xFFFFFFFFu, m, 8));
                     m = fmaxf(m, __shfl_xor_sync(0xFFFFFFFFu, m, 16));
                     m_new[nt][i] = m;
-                    grown |= m != m_run[nt][i];
+                    grown |= m > m_run[nt][i] + kSlack;
                 }
-            if (__any_sync(0xFFFFFFFFu, grown)) {
+            if (__any_sync(0xFFFFFFFFu, grown)) {                        // (seldom, thanks to the slack)
                 const float v_down = exp2_int(v_run - v_new);
 #pragma unroll
                 for (int nt = 0; nt < NT; ++nt)
@@ -666,7 +676,7 @@ __global__ void __launch_bounds__(kAttnThreads, (AttnShape<FMT, D, NQ>::kPerSm))
                 }
             }
         __syncthreads();                                                 // all warps have left their rings
-        const float unit = L::kCodes ? exp2_int(v_run - 127 - 14 - L::kLift) : (FMT == kAttnF16 ? 1.f / 16384.f : 1.f);
+        const float unit = L::kCodes ? exp2_int(v_run - 127 - kPLift - L::kLift) : (FMT == kAttnF16 ? 1.f / (1 << kPLift) : 1.f);
 #pragma unroll
         for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
@@ -723,15 +733,16 @@ __global__ void __launch_bounds__(kAttnThreads, (AttnShape<FMT, D, NQ>::kPerSm))
     }
 }
 
-constexpr int kJoinThreads = 512;
+constexpr int kJoinThreads = 1024;       // at most; 256 where there are many items, most of which have a few parts
 
 // Joins the parts of an item that several CTAs took: blockIdx.x = item, blockIdx.y = query of the chunk.  The threads are D/4 groups of
 // four channels times lanes that take every so many parts with a running maximum; the lanes' sums are added in order.
 template <int D, int NQ>
 __global__ void __launch_bounds__(kJoinThreads) cache_attention_join(const __grid_constant__ AttentionProblem p) {
-    constexpr int kCols = D / 4, kLanes = kJoinThreads / kCols;
+    constexpr int kCols = D / 4;
     __shared__ float4 sums[kJoinThreads];
-    __shared__ float tops[kLanes], weights[kLanes];
+    __shared__ float tops[kJoinThreads / kCols], weights[kJoinThreads / kCols];
+    const int every = (int)blockDim.x / kCols;
     pdl_launch_dependents();
     const int per_seq = p.c.heads * p.chunks;
     const int seq = (int)blockIdx.x / per_seq, item = (int)blockIdx.x - seq * per_seq;
@@ -744,13 +755,13 @@ __global__ void __launch_bounds__(kJoinThreads) cache_attention_join(const __gri
     const int x = threadIdx.x % kCols, y = threadIdx.x / kCols;
     float4 sum = make_float4(0.f, 0.f, 0.f, 0.f);
     float l = 0.f, top = -INFINITY;
-    constexpr int kAhead = 4;
-    for (int c = y; c < parts.y; c += kAhead * kLanes) {
+    constexpr int kAhead = 8;
+    for (int c = y; c < parts.y; c += kAhead * every) {
         float4 v[kAhead];
         float m[kAhead], w[kAhead];
 #pragma unroll
         for (int i = 0; i < kAhead; ++i) {
-            const int k = c + i * kLanes;
+            const int k = c + i * every;
             const int64_t slot = 2 * (int64_t)(parts.x + (k < parts.y ? k : 0)) + (k == 0 || k >= parts.y ? 1 : 0);
             v[i] = *reinterpret_cast<const float4*>(p.partial + (slot * NQ + col) * D + 4 * x);
             m[i] = k < parts.y ? st[slot * 2 * NQ + col] : -INFINITY;
@@ -758,7 +769,7 @@ __global__ void __launch_bounds__(kJoinThreads) cache_attention_join(const __gri
         }
 #pragma unroll
         for (int i = 0; i < kAhead; ++i) {
-            if (c + i * kLanes >= parts.y) break;
+            if (c + i * every >= parts.y) break;
             const float up = fmaxf(top, m[i]), ref = up == -INFINITY ? 0.f : up;
             const float f = exp2_fast(top - ref), e = exp2_fast(m[i] - ref);
             top = up;
@@ -776,7 +787,7 @@ __global__ void __launch_bounds__(kJoinThreads) cache_attention_join(const __gri
     }
     __syncthreads();
     if (y != 0) return;
-    const int lanes = parts.y < kLanes ? parts.y : kLanes;
+    const int lanes = parts.y < every ? parts.y : every;
     top = tops[0];
     for (int k = 1; k < lanes; ++k) top = fmaxf(top, tops[k]);
     const float ref = top == -INFINITY ? 0.f : top;

@@ -128,12 +128,11 @@ kq_status_t run_cache(const kq_cache_t* cache, const kq_cache_rows_t* rows, void
     if ((int64_t)c.heads * groups > (1 << 30)) return KQ_ERR_SHAPE;
     p.units = c.heads * groups;
     p.by_groups = fast_div((uint32_t)groups);
-    // eight rows for each thread of a CTA (four units in flight, twice), fewer where that leaves SMs idle
+    // Rows of a CTA: as many as let all CTAs run at once (four of them on an SM: the rows' cells, which the others wait for, are then found
+    // once), up to the room for their cells.
     const int across = p.units < kq::kCacheThreads ? p.units : kq::kCacheThreads;
     int at_once = kq::kCacheThreads / across;
-    int64_t per_cta = 8 * at_once;
-    const int64_t even = (r.rows + 4 * sms - 1) / (4 * sms);
-    if (per_cta > even) per_cta = even;
+    int64_t per_cta = (2 * r.rows + 4 * sms - 1) / (4 * sms);        // (keys and values: two grids of CTAs)
     if (per_cta > kq::kCacheRowsMax) per_cta = kq::kCacheRowsMax;
     if (at_once > per_cta) at_once = (int)per_cta;
     p.rows_per_cta = (int)per_cta;
@@ -355,7 +354,8 @@ kq_status_t kroquant_cache_attention(const kq_cache_t* cache, const kq_attention
         launch_config(&cfg, attr, dim3((unsigned)plan.ctas), dim3(kq::kAttnThreads), (size_t)L::kBytes, 1, st);
         r = launch(cfg, kq::cache_attention_kernel<FMT, D, NQ>, p);
         if (r != KQ_OK || plan.whole) return r;
-        launch_config(&cfg, attr, dim3((unsigned)plan.items, (unsigned)(p.group < NQ ? p.group : NQ)), dim3(kq::kJoinThreads), 0, 1, st);
+        const unsigned queries = (unsigned)(p.group < NQ ? p.group : NQ);
+        launch_config(&cfg, attr, dim3((unsigned)plan.items, queries), dim3(plan.items * queries <= 2 * sms ? kq::kJoinThreads : 256), 0, 1, st);
         return launch(cfg, kq::cache_attention_join<D, NQ>, p);
     });
 }

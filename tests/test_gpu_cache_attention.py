@@ -6,9 +6,10 @@ products lose at most (C / 16 + 8) 2^-23 of scale * sum |q k| (16 products a ste
     |out - exact| <= (2^-11 + 2^-21 + 2 delta) sum_t w_t |v_t| + half a step of out's type,
 and the sum over positions adds (T / 16 + 8) 2^-23 in the worst case.
 
-Weights enter as fp16(w 2^14 2^(S - R)), w relative to the largest weight, S and R scale bytes (1 for 16-bit values), with fp16's smallest step 2^-24: one
-rounds by up to 2^-25, that is 2^-39 of the largest weight, times a code of at most 6 (448) units of R, where the largest value has at least 4
-(256): 1.75 max |v|.  Where the positions that count hold zeros in a channel this is all there is: 2^-39 * 1.75 T max |v| more (not with bf16 values)."""
+Weights enter as fp16(w 2^9 2^(S - R)), w relative to a reference that is the largest weight or up to 2^6 below it, S and R scale bytes (1 for 16-bit
+values), with fp16's smallest step 2^-24: one rounds by up to 2^-25, that is 2^-34 of the reference, times a code of at most 6 (448) units of R, where
+the largest value has at least 4 (256): 1.75 max |v|; the sum they are divided by is at least 1, the reference's own weight.  Where the
+positions that count hold zeros in a channel this is all there is: 2^-34 * 1.75 T max |v| more (not with bf16 values)."""
 import math
 
 import pytest
@@ -76,7 +77,7 @@ def check(out, q, cache, table, lengths, scale, window=0, lse=None):
         want = (w @ v).reshape(q_heads, d)
         size = (w @ v.abs()).reshape(q_heads, d)
         delta = (d / 16 + 8) * 2.0 ** -23 * abs(scale) * (qs.abs() @ k.abs().mT).amax(-1).reshape(q_heads, 1)
-        least = 0 if half_w < 2.0 ** -11 else 2.0 ** -39 * 1.75 * (length - first) * v.abs().amax((1, 2)).repeat_interleave(group)[:, None]
+        least = 0 if half_w < 2.0 ** -11 else 2.0 ** -34 * 1.75 * (length - first) * v.abs().amax((1, 2)).repeat_interleave(group)[:, None]
         tol = least + (half_w + 2.0 ** -21 + 2 * delta + ((length - first) / 16 + 8) * 2.0 ** -23) * size
         tol = tol + torch.finfo(out.dtype).eps / 2 * (want.abs() + tol) + torch.finfo(out.dtype).smallest_normal
         over = (out[i].double() - want).abs() - tol
