@@ -1086,6 +1086,8 @@ def kroquant_rotary(q: torch.Tensor, k: Optional[torch.Tensor], positions: torch
             (place != (tokens, n) and (dims != 4 or place != (batches, tokens, n))) or (n > 1 and ps[-1] != 1):
         raise ValueError("positions must be a CUDA int32 or float32 tensor [tokens, axes], or [batch, tokens, axes], with contiguous axes")
     outs = (None, None) if out is None else (out, None) if k is None else tuple(out)
+    if len(outs) != 2 or (out is not None and not isinstance(outs[0], torch.Tensor)):
+        raise ValueError("out must be a tensor, or a pair of tensors where k is given")
     made = []
     for x, o in ((q, outs[0]), (k, outs[1])):
         if x is None:
@@ -1153,12 +1155,15 @@ class KVCache:
         for t in (k, v) if code == 0 else (k, v, k_scales, v_scales):
             if not t.is_contiguous() or t.get_device() != k.get_device():
                 raise ValueError("the cache's buffers must be contiguous tensors on one device")
-        self.k, self.v, self.k_scales, self.v_scales = k, v, k_scales, v_scales
+        self._buffers = (k, v, k_scales, v_scales)
         self.format, self.dtype, self.head_dim, self.device = format, dtype, head_dim, k.device
         self.pages, self.heads, self.page_size = k.shape[0], k.shape[1], k.shape[2]
         self._device, self._c = k.get_device(), _Cache(code, _DTYPES[dtype], k.shape[0], k.shape[2], k.shape[1], head_dim, k.data_ptr(), v.data_ptr(),
                                                        None if code == 0 else k_scales.data_ptr(), None if code == 0 else v_scales.data_ptr())
         self._at = C.addressof(self._c)
+
+    # (the C struct points into these: a cache keeps the buffers it was made with)
+    k, v, k_scales, v_scales = (property(lambda self, i=i: self._buffers[i]) for i in range(4))
 
     @classmethod
     def empty(cls, pages: int, page_size: int, heads: int, head_dim: int, format: str = "mxfp4", dtype=torch.bfloat16, device="cuda") -> "KVCache":
@@ -1267,6 +1272,8 @@ def kroquant_cache_attention(q: torch.Tensor, cache: KVCache, table: torch.Tenso
         _heads_last(out, "out", 3)
         if out.shape != q.shape or out_dtype not in (None, out.dtype) or not _apart(out):
             raise ValueError("out must have q's shape and elements of its own")
+        if out.data_ptr() == q.data_ptr() and q.numel():
+            raise ValueError("out must not be q")
     lib, logs, scratch = load_library(), None, None
     if lse:
         with _allocating(stream):

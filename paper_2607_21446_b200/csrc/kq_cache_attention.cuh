@@ -20,7 +20,8 @@
 // running maximum that rescales the accumulator as m does).  Code times 2^(S - S_t + kLift) has at most 4 significant bits and is exact in
 // fp16; a block whose scale is 2^-28 (E2M1) or 2^-21 (E4M3) of its position's largest, or less, counts as zero.  The queries of a CTA are
 // fp16 times one power of two, exact for both 16-bit types down to values 2^-29 of the largest.  P is rounded to fp16 (11 bits; a weight
-// below 2^-23 of the largest keeps fewer, which is 2^-34 of the largest value at most), with bf16 values to two bf16 terms (16 bits).
+// below 2^-23 of the largest keeps fewer, which is 2^-34 of the largest value at most), with 16-bit values, where memory leaves the time, to
+// two terms of their type (16 and 22 bits).
 //
 // Work.  Tiles (4 steps) of all (sequence, head) items are laid end to end, each item led by kLead tiles' worth of nothing for what
 // beginning and ending it costs, and every CTA takes an equal run: ragged batches balance, one long sequence fills the GPU.  An
@@ -561,7 +562,7 @@ __global__ void __launch_bounds__(kAttnThreads, (AttnShape<FMT, D, NQ>::kPerSm))
                 v_run = v_new;
             }
             // weights, as operand B of O^T += V^T P^T
-            uint32_t pb[kMt][NT][2], pl[FMT == kAttnBf16 ? kMt : 1][NT][2];
+            uint32_t pb[kMt][NT][2], pl[L::kCodes ? 1 : kMt][NT][2];
 #pragma unroll
             for (int nt = 0; nt < NT; ++nt) {
                 const float m0 = m_run[nt][0] == kMinus ? 0.f : m_run[nt][0], m1 = m_run[nt][1] == kMinus ? 0.f : m_run[nt][1];
@@ -577,7 +578,13 @@ __global__ void __launch_bounds__(kAttnThreads, (AttnShape<FMT, D, NQ>::kPerSm))
                             pb[mt][nt][h] = transpose_8x8(hi);
                             pl[mt][nt][h] = transpose_8x8(pack_bf16(p0 - bf16lo_to_f32(hi), p1 - bf16hi_to_f32(hi)));
                         } else {
-                            pb[mt][nt][h] = transpose_8x8(pack_f16(p0 * vf[mt][h], p1 * vf[mt][h]));
+                            const float w0 = p0 * vf[mt][h], w1 = p1 * vf[mt][h];
+                            const uint32_t hi = pack_f16(w0, w1);
+                            pb[mt][nt][h] = transpose_8x8(hi);
+                            if constexpr (FMT == kAttnF16) {
+                                const float2 back = __half22float2(*reinterpret_cast<const __half2*>(&hi));
+                                pl[mt][nt][h] = transpose_8x8(pack_f16(w0 - back.x, w1 - back.y));
+                            }
                         }
                     }
             }
@@ -598,6 +605,7 @@ __global__ void __launch_bounds__(kAttnThreads, (AttnShape<FMT, D, NQ>::kPerSm))
                             mma_16816_bf16(o[m][nt], a0, a1, a2, a3, pl[0][nt][0], pl[0][nt][1]);
                         } else {
                             mma_16816_f16(o[m][nt], a0, a1, a2, a3, pb[0][nt][0], pb[0][nt][1]);
+                            mma_16816_f16(o[m][nt], a0, a1, a2, a3, pl[0][nt][0], pl[0][nt][1]);
                         }
                     }
                 }

@@ -38,6 +38,7 @@ kq_status_t launch_rotary(kq::RotaryProblem& p, int sms, cudaStream_t st) {
     // many heads goes over several CTAs, each of which forms the token's sines again.
     int64_t per_cta = (p.rows + 5 * sms - 1) / (5 * sms);
     if (per_cta * p.pairs > 2048) per_cta = 2048 / p.pairs;          // 16 KB
+    if (per_cta * heads > (1 << 24)) per_cta = (1 << 24) / heads;    // (rows are counted in 32 bits)
     if (per_cta < 1) per_cta = 1;
     p.tokens_per_cta = (int)per_cta;
     const int64_t tiles = (p.rows + per_cta - 1) / per_cta, taken = heads * per_cta;

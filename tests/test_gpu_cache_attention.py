@@ -263,6 +263,17 @@ def test_streams_and_graphs_share_nothing():
         assert torch.equal(o, w)
 
 
+def test_a_page_for_every_sequence_and_a_sequence_twice():
+    """Sequences may read the same pages: rows of a batch that share a prefix, or all of it."""
+    cache, table, n = make([3000], 2, 64, 16, "mxfp4", torch.bfloat16, 60)
+    q = torch.randn(1, 8, 64, device="cuda", generator=gen(60)).bfloat16()
+    one = kb.kroquant_cache_attention(q, cache, table, n, out_dtype=torch.float32)
+    many = kb.kroquant_cache_attention(q.expand(40, 8, 64), cache, table.expand(40, table.shape[1]), n.repeat(40), out_dtype=torch.float32)
+    for i in range(40):
+        check(many[i : i + 1], q, cache, table, n, 0.125)
+    check(one, q, cache, table, n, 0.125)
+
+
 def test_scratch_is_as_large_as_it_says():
     import ctypes as C
     cache, table, n = make([9000], 2, 64, 16, "mxfp4", torch.bfloat16, 40)
@@ -290,6 +301,6 @@ def test_refusals():
     for args, kw in (((q[:1], c, table, n), {}), ((q[:, :3], c, table, n), {}), ((q[:, :, :32], c, table, n), {}), ((q.float(), c, table, n), {}), ((q, b, table, n), {}),
                      ((q.cpu(), c, table, n), {}), ((q, c, table.cpu(), n), {}), ((q, c, table, n.long()), {}), ((q, c, table, n[:1]), {}), ((q, c, table, n.cpu()), {}),
                      ((q, c, table, n), dict(window=-1)), ((q, c, table, n), dict(out=q[:1])), ((q, c, table, n), dict(out_dtype=torch.int8)),
-                     ((q, c, table, n), dict(out=q[:, :1].expand(2, 4, 64))), ((q.transpose(1, 2), c, table, n), {})):
+                     ((q, c, table, n), dict(out=q[:, :1].expand(2, 4, 64))), ((q, c, table, n), dict(out=q)), ((q.transpose(1, 2), c, table, n), {})):
         with pytest.raises(ValueError):
             kb.kroquant_cache_attention(*args, **kw)

@@ -125,6 +125,19 @@ def test_batches(shared):
         check(a[i], q[i], p, f, axes, "interleaved"), check(b[i], k[i], p, f, axes, "interleaved")
 
 
+@pytest.mark.parametrize("B,T,H,d", [(700, 3, 2, 64), (1500, 1, 1, 64), (300, 7, 1, 71)])
+def test_batches_of_few_tokens(B, T, H, d):
+    """A CTA's tokens run over several batches."""
+    g, axes = gen(B), (22, 20)
+    x = torch.randn(T, B, H, d, device="cuda", generator=g).half().transpose(0, 1)
+    for pos in (torch.randint(0, 999, (T, 2), device="cuda", generator=g, dtype=torch.int32), torch.randint(0, 999, (B, T, 2), device="cuda", generator=g, dtype=torch.int32)):
+        f = kb.rotary_frequencies(axes)
+        y, z = kb.kroquant_rotary(x, x.flip(2), pos, f, axes=axes, layout="half")
+        every = pos.expand(B, T, 2).reshape(-1, 2)
+        check(y.reshape(-1, H, d), x.reshape(-1, H, d), every, f, axes, "half")
+        check(z.reshape(-1, H, d), x.flip(2).reshape(-1, H, d), every, f, axes, "half")
+
+
 @pytest.mark.parametrize("layout", ["interleaved", "half"])
 def test_gradient_against_differences(layout):
     """sum(g * y(x)) is linear in x: its difference along h is sum(x_grad * h) up to 32-bit rounding of both sides."""
@@ -178,7 +191,7 @@ def test_refusals():
     for bad in (dict(q=q[0]), dict(q=q.double()), dict(q=q.transpose(1, 2)), dict(q=q.cpu()), dict(k=q.half()), dict(k=q[:3]), dict(k=q[..., :32]),
                 dict(frequencies=f.float()), dict(frequencies=f.cpu()), dict(frequencies=f.repeat(2)), dict(positions=pos.long()), dict(positions=pos[:3]),
                 dict(positions=pos.cpu()), dict(axes=(32, 30)), dict(axes=(33, 31)), dict(axes=(16, 16, 16, 8, 8)), dict(layout="other"),
-                dict(axes=(32, 32)), dict(out=q[:, :1].expand(4, 2, 64)), dict(out=q.half()), dict(out=q[:3])):
+                dict(axes=(32, 32)), dict(out=(q, q)), dict(k=q, out=q[:1]), dict(out=q[:, :1].expand(4, 2, 64)), dict(out=q.half()), dict(out=q[:3])):
         with pytest.raises(ValueError):
             kb.kroquant_rotary(**{**ok, **bad})
     big = torch.zeros(5, 2, 64, device="cuda")
