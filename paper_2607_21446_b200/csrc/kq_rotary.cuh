@@ -10,6 +10,8 @@
 // a few tokens with all their heads, forms the P pairs of (cos, sin) once in shared memory and has its first rows on the way
 // meanwhile.  A thread takes one place within a head (16 or 8 bytes, or single elements where rows are not aligned) of one row
 // (token, head) after another and has eight rows on the way, by asynchronous copies to shared memory that only it reads.
+// Measured: 4608 tokens x 72 heads x 128, bf16, 34.8 us (4.9 TB/s, 0.75 of the copy rate; 47 with the rows
+// in registers, an address computed for each and CTAs of more than one wave); 10007 x 32 x 72, fp16, 23.2 us (0.61); one token 2.8.  The instructions take 0.7 of the issue slots then.
 #pragma once
 #include "kq_mma16.cuh"
 

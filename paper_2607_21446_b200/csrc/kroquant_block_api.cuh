@@ -207,11 +207,12 @@ kq_status_t launch_w4a16(const kq::W4A16Problem& p, int tiles, cudaStream_t st) 
         }
         attr_done.done();
     }
-    // K goes over as many CTAs of a cluster as run at once, four units each at least.  12288 -> 4608 with 16 rows, 1 to 8 CTAs: 68, 37, 29,
-    // 33, 29, 26, 22.5, 43 us (36 clusters of eight do not fit at once); 5 rows of 4096 -> 2 x 5632: 18.5, 18.5, 14.4, 18 us.
+    // K goes over as many CTAs of a cluster as run at once, three units each at least.  12288 -> 4608 with 16 rows, 1, 2, 3, 7, 8 CTAs: 68, 37,
+    // 29, 21.3, 43 us (36 clusters of eight do not fit at once); 5 rows of 4096 -> 2 x 5632, 2 to 4: 15.5, 12.2, 17; one row of 1152 -> 6912, 1
+    // to 4: 6.5, 6.3, 5.5, 5.6.
     const int runs = (p.lin.M + 8 * NT - 1) / (8 * NT);
     int splits = 1;
-    while (splits < 8 && p.units >= 4 * (splits + 1) && (int64_t)tiles * runs <= clusters_at_once(kernel, kq::kW4Threads, kBytes, splits + 1)) ++splits;
+    while (splits < 8 && p.units >= 3 * (splits + 1) && (int64_t)tiles * runs <= clusters_at_once(kernel, kq::kW4Threads, kBytes, splits + 1)) ++splits;
     cudaLaunchConfig_t cfg;
     cudaLaunchAttribute attr[2];
     launch_config(&cfg, attr, dim3((unsigned)(tiles * splits), (unsigned)runs), dim3(kq::kW4Threads), kBytes, splits, st);
