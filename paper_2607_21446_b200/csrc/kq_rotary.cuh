@@ -10,8 +10,9 @@
 // a few tokens with all their heads, forms the P pairs of (cos, sin) once in shared memory and has its first rows on the way
 // meanwhile.  A thread takes one place within a head (16 or 8 bytes, or single elements where rows are not aligned) of one row
 // (token, head) after another and has eight rows on the way, by asynchronous copies to shared memory that only it reads.
-// Measured: 4608 tokens x 72 heads x 128, bf16, 34.8 us (4.9 TB/s, 0.75 of the copy rate; 47 with the rows
-// in registers, an address computed for each and CTAs of more than one wave); 10007 x 32 x 72, fp16, 23.2 us (0.61); one token 2.8.  The instructions take 0.7 of the issue slots then.
+// Measured: 4608 tokens x 72 heads x 128, bf16, 31.2 us (5.5 TB/s, 0.83 of the copy rate; 34.8 where the copies of k began behind the last row of q and
+// out's addresses were formed from more terms, 47 with the rows in registers and CTAs of more than one wave); 10007 x 32 x 72, fp16, accesses
+// of 8 bytes, 21.6 us (0.65); one token 2.8.  Instructions take two thirds of the issue slots; a loop of 8 rows a turn was slower (its code).
 #pragma once
 #include "kq_mma16.cuh"
 
@@ -51,21 +52,19 @@ template <> __device__ __forceinline__ float rotary_round<float>(float v) { retu
 template <> __device__ __forceinline__ __half rotary_round<__half>(float v) { return __float2half_rn(v); }
 template <> __device__ __forceinline__ __nv_bfloat16 rotary_round<__nv_bfloat16>(float v) { return __float2bfloat16_rn(v); }
 
-// (cos, sin) of N pairs from p0 on; two at a time where the place allows
+// (cos, sin) of N pairs; two at a time (rows of the table and the places of units of more than one pair are 16-byte aligned)
 template <int N>
-__device__ __forceinline__ void load_turns(float2 (&turn)[N], const float2* cs, int p0, int pairs) {
-    if (N % 2 == 0 && pairs % 2 == 0) {                                  // (rows of the table stay 16-byte aligned)
+__device__ __forceinline__ void load_turns(float2 (&turn)[N], const float2* cs) {
+    if constexpr (N % 2 == 0) {
 #pragma unroll
         for (int i = 0; i < N; i += 2) {
-            if (p0 + i >= pairs) break;
-            const float4 c = *reinterpret_cast<const float4*>(cs + p0 + i);
+            const float4 c = *reinterpret_cast<const float4*>(cs + i);
             turn[i] = make_float2(c.x, c.y);
-            if (i + 1 < N) turn[i + 1] = make_float2(c.z, c.w);
+            turn[i + 1] = make_float2(c.z, c.w);
         }
     } else {
 #pragma unroll
-        for (int i = 0; i < N; ++i)
-            if (p0 + i < pairs) turn[i] = cs[p0 + i];
+        for (int i = 0; i < N; ++i) turn[i] = cs[i];
     }
 }
 
@@ -108,69 +107,79 @@ __device__ __forceinline__ void rotary_store(void* at, const uint32_t (&w)[WORDS
 template <typename T, int E, bool HALF>
 struct RotaryUnit {
     static constexpr int kWords = E * (int)sizeof(T) / 4;
-    uint32_t a[kWords], b[HALF ? kWords : 1];
     static constexpr int kBytes = 4 * kWords;                            // of an access
-    // w: place in the head.  Copies the unit to `slot` in shared memory, its second access `second` bytes behind it.
-    static __device__ __forceinline__ void copy(uint32_t slot, uint32_t second, const T* row, int w, int pairs) {
-        const int at = !HALF || w * E < pairs ? w * E : w * E + pairs;   // (half: behind the first members come the second ones)
-        rotary_copy<kBytes>(slot, row + at);
+    static constexpr int kPairs = HALF ? E : E / 2;
+    uint32_t a[kWords], b[HALF ? kWords : 1];
+    // Unit w: its first element in the head (half: behind the first members come the second ones) and how many of its pairs turn.
+    static __device__ __forceinline__ int place(int w, int pairs) { return !HALF || w * E < pairs ? w * E : w * E + pairs; }
+    static __device__ __forceinline__ int turning(int w, int pairs) {
+        const int left = pairs - w * kPairs;
+        return left < 0 ? 0 : left < kPairs ? left : kPairs;
+    }
+    // at: the unit's first element of a row.  To `slot` in shared memory, the second access `second` bytes behind it.
+    static __device__ __forceinline__ void copy(uint32_t slot, uint32_t second, const uint8_t* at, int turning, int pairs) {
+        rotary_copy<kBytes>(slot, at);
         if constexpr (HALF)
-            if (w * E < pairs) rotary_copy<kBytes>(slot + second, row + at + pairs);
+            if (turning) rotary_copy<kBytes>(slot + second, at + pairs * (int)sizeof(T));
     }
-    __device__ __forceinline__ void take(const uint8_t* slot, int second) {
-        rotary_load(a, slot);
-        if constexpr (HALF) rotary_load(b, slot + second);
+    __device__ __forceinline__ void take(const uint8_t* at, int second) {
+        rotary_load(a, at);
+        if constexpr (HALF) rotary_load(b, at + second);
     }
-    __device__ __forceinline__ void turn_and_store(T* row, int w, int pairs, int, const float2* cs) {
+    __device__ __forceinline__ void load(const uint8_t* at, int turning, int pairs) {
+        rotary_load(a, at);
+        if constexpr (HALF)
+            if (turning) rotary_load(b, at + pairs * (int)sizeof(T));
+    }
+    // cs: of the unit's first pair
+    __device__ __forceinline__ void turn(int turning, const float2* cs) {
         if constexpr (!HALF) {
-            constexpr int kPairs = E / 2;
-            const int p0 = w * kPairs;
-            float2 turn[kPairs];
-            load_turns<kPairs>(turn, cs, p0, pairs);
-            auto pair = [&](int i) {
+            auto pair = [&](int i, const float2& c) {
                 if constexpr (sizeof(T) == 2) {
                     float2 v = rotary_widen2<T>(a[i]);
-                    rotary_turn(v.x, v.y, turn[i]);
+                    rotary_turn(v.x, v.y, c);
                     a[i] = rotary_round2<T>(v.x, v.y);
                 } else {
                     float x = __uint_as_float(a[2 * i]), y = __uint_as_float(a[2 * i + 1]);
-                    rotary_turn(x, y, turn[i]);
+                    rotary_turn(x, y, c);
                     a[2 * i] = __float_as_uint(x);
                     a[2 * i + 1] = __float_as_uint(y);
                 }
             };
-            if (p0 + kPairs <= pairs) {
+            if (turning == kPairs) {
+                float2 c[kPairs];
+                load_turns<kPairs>(c, cs);
 #pragma unroll
-                for (int i = 0; i < kPairs; ++i) pair(i);
-            } else {
+                for (int i = 0; i < kPairs; ++i) pair(i, c[i]);
+            } else if (turning) {
 #pragma unroll
                 for (int i = 0; i < kPairs; ++i)
-                    if (p0 + i < pairs) pair(i);
+                    if (i < turning) pair(i, cs[i]);
             }
-            rotary_store(row + w * E, a);
-        } else if (w * E < pairs) {
-            float2 turn[E];
-            load_turns<E>(turn, cs, w * E, pairs);
+        } else if (turning) {                                            // (all of them)
+            float2 c[E];
+            load_turns<E>(c, cs);
 #pragma unroll
             for (int i = 0; i < kWords; ++i) {
                 if constexpr (sizeof(T) == 2) {
                     float2 x = rotary_widen2<T>(a[i]), y = rotary_widen2<T>(b[i]);
-                    rotary_turn(x.x, y.x, turn[2 * i]);
-                    rotary_turn(x.y, y.y, turn[2 * i + 1]);
+                    rotary_turn(x.x, y.x, c[2 * i]);
+                    rotary_turn(x.y, y.y, c[2 * i + 1]);
                     a[i] = rotary_round2<T>(x.x, x.y);
                     b[i] = rotary_round2<T>(y.x, y.y);
                 } else {
                     float x = __uint_as_float(a[i]), y = __uint_as_float(b[i]);
-                    rotary_turn(x, y, turn[i]);
+                    rotary_turn(x, y, c[i]);
                     a[i] = __float_as_uint(x);
                     b[i] = __float_as_uint(y);
                 }
             }
-            rotary_store(row + w * E, a);
-            rotary_store(row + w * E + pairs, b);
-        } else {
-            rotary_store(row + w * E + pairs, a);
         }
+    }
+    __device__ __forceinline__ void store(uint8_t* at, int turning, int pairs) const {
+        rotary_store(at, a);
+        if constexpr (HALF)
+            if (turning) rotary_store(at + pairs * (int)sizeof(T), b);
     }
 };
 template <typename T, bool HALF>
@@ -203,19 +212,58 @@ struct RotaryUnit<T, 1, HALF> {
 };
 
 constexpr int kRotaryThreads = 512;      // at most
+__host__ __device__ constexpr int rotary_pitch(int pairs) { return (pairs + 1) & ~1; }      // of the table of sines
 // Rows of a thread on the way: copies to shared memory of its own (aligned rows), or registers.
 template <typename T, int E, bool HALF>
 __host__ __device__ constexpr int rotary_ahead() { return E == 1 || (HALF && E * sizeof(T) == 16) ? 4 : 8; }
 template <typename T, int E, bool HALF>
 __host__ __device__ constexpr int rotary_slot_bytes() { return E == 1 ? 0 : E * (int)sizeof(T) * (HALF ? 2 : 1) * rotary_ahead<T, E, HALF>(); }   // of a thread
 
+// A thread's way through the rows (token, head) of the tensors, one after the other, on one side (x or out).  From a row to the
+// next its address moves on by the same step, and by another one more where the head passes the last: none is formed anew.
+struct RotaryWalk {
+    uint8_t* at;
+    int64_t step, wrap;                  // bytes
+    int head, dh, heads, left, tensor;   // left: rows of this tensor, with the present one
+    template <bool OUT, typename T>
+    __device__ __forceinline__ void open(const RotaryProblem& p, int n, int tokens, int first, int rows_step, int64_t batch0, int64_t t0, int place) {
+        for (left = 0; n < p.tensors; ++n) {
+            const RotaryTensor& s = p.t[n];
+            if (first >= tokens * s.heads) continue;
+            const int dt = (int)s.by_heads.div((uint32_t)rows_step), lt = (int)s.by_heads.div((uint32_t)first);
+            const int64_t token = (OUT ? s.ot : s.xt) * (int64_t)sizeof(T), each = (OUT ? s.oh : s.xh) * (int64_t)sizeof(T);
+            heads = s.heads;
+            dh = rows_step - dt * heads;
+            head = first - lt * heads;
+            step = dt * token + dh * each;
+            wrap = token - heads * each;
+            at = (OUT ? static_cast<uint8_t*>(s.out) : static_cast<uint8_t*>(const_cast<void*>(s.x))) + batch0 * (OUT ? s.ob : s.xb) * (int64_t)sizeof(T) +
+                 (t0 + lt) * token + head * each + place * (int)sizeof(T);
+            left = (tokens * heads - 1 - first) / rows_step + 1;
+            tensor = n;
+            break;
+        }
+    }
+    __device__ __forceinline__ bool next() {                             // into the next token
+        at += step;
+        head += dh;
+        if (head < heads) return false;
+        head -= heads;
+        at += wrap;
+        return true;
+    }
+};
+
 // blockDim: x = units of a head, y = rows (token, head) at a time.  Dynamic shared memory: the slots of the copies, then
-// float2 [tokens_per_cta][pairs].
+// float2 [tokens_per_cta][pairs, an even number].
 template <typename T, int E, bool HALF>
-__global__ void __launch_bounds__(kRotaryThreads) rotary_kernel(const __grid_constant__ RotaryProblem p) {
+__global__ void __launch_bounds__(kRotaryThreads, 2) rotary_kernel(const __grid_constant__ RotaryProblem p) {
     extern __shared__ __align__(16) uint8_t rotary_smem[];
+    using Unit = RotaryUnit<T, E, HALF>;
+    constexpr int kAhead = rotary_ahead<T, E, HALF>();
     const int thread = threadIdx.y * blockDim.x + threadIdx.x, threads = blockDim.x * blockDim.y;
     float2* rotary_cs = reinterpret_cast<float2*>(rotary_smem + (threads * rotary_slot_bytes<T, E, HALF>() + 15) / 16 * 16);
+    const int pitch = rotary_pitch(p.pairs);
     pdl_launch_dependents();
     pdl_wait_prior_grid();
     const int64_t token0 = (int64_t)blockIdx.x * p.tokens_per_cta;
@@ -226,64 +274,38 @@ __global__ void __launch_bounds__(kRotaryThreads) rotary_kernel(const __grid_con
         batch0 = token0 / p.tokens;
         t0 = token0 - batch0 * p.tokens;
     }
-
-    constexpr int kAhead = rotary_ahead<T, E, HALF>();
     const bool crosses = p.tokens != p.rows && t0 + tokens > p.tokens;   // into later batches
-    // element of a token (counted within the CTA) and head
-    auto place = [&](int lt, int head, int64_t batch, int token, int head_stride) {
-        int64_t at = batch0 * batch + t0 * token + ((int64_t)lt * token + (int64_t)head * head_stride);
-        if (crosses && t0 + lt >= p.tokens) at += (t0 + lt) / p.tokens * (batch - p.tokens * token);
-        return at;
-    };
-    auto source = [&](const RotaryTensor& s, int r) -> const T* {
-        const int lt = (int)s.by_heads.div((uint32_t)r);
-        return static_cast<const T*>(s.x) + place(lt, r - lt * s.heads, s.xb, s.xt, s.xh);
-    };
-    auto finish = [&](const RotaryTensor& s, RotaryUnit<T, E, HALF>& unit, int r) {
-        const int lt = (int)s.by_heads.div((uint32_t)r);
-        unit.turn_and_store(static_cast<T*>(s.out) + place(lt, r - lt * s.heads, s.ob, s.ot, s.oh), w, p.pairs, p.head_dim, rotary_cs + lt * p.pairs);
-    };
 
-    // Aligned rows: a pipeline of copies.  From one row of a thread to its next, x and out move on by the same step, and by another
-    // one more where the head passes the last: no row's address is formed anew.
+    // Aligned rows: a pipeline of copies, each into a slot that only its thread reads, from tensor to tensor without a break.
     constexpr int kUnitBytes = E * (int)sizeof(T);
-    const uint32_t slot0 = (uint32_t)__cvta_generic_to_shared(rotary_smem) + thread * kUnitBytes, second = threads * kUnitBytes;
-    const uint32_t slot_step = second * (HALF ? 2 : 1);
-    const T* from = nullptr;                                              // the next row to copy: its address, head and number
-    int from_head = 0, from_row = 0, fill = 0;
-    auto copy_next = [&](const RotaryTensor& s, int rows, int dt, int dh) {
+    const uint32_t second = threads * kUnitBytes, slot_step = second * (HALF ? 2 : 1);
+    const uint8_t* const slots = rotary_smem + thread * kUnitBytes;
+    const uint32_t slots_at = (uint32_t)__cvta_generic_to_shared(slots);
+    int turning = 0, place = 0;
+    if constexpr (E > 1) {
+        turning = Unit::turning(w, p.pairs);
+        place = Unit::place(w, p.pairs);
+    }
+    RotaryWalk in = {}, out = {};
+    auto copy_next = [&](uint32_t slot) {
         if constexpr (E > 1) {
-            if (from_row < rows) {
-                RotaryUnit<T, E, HALF>::copy(slot0 + fill * slot_step, second, crosses ? source(s, from_row) : from, w, p.pairs);
-                from_row += step;
-                from_head += dh;
-                from += (int64_t)dt * s.xt + (int64_t)dh * s.xh;
-                if (from_head >= s.heads) {
-                    from_head -= s.heads;
-                    from += s.xt - (int64_t)s.heads * s.xh;
-                }
+            if (in.left > 0) {
+                Unit::copy(slots_at + slot, second, in.at, turning, p.pairs);
+                in.next();
+                if (--in.left == 0) in.open<false, T>(p, in.tensor + 1, tokens, first, step, batch0, t0, place);
             }
-            fill = fill + 1 == kAhead ? 0 : fill + 1;
             asm volatile("cp.async.commit_group;" ::: "memory");
         }
     };
-    auto begin = [&](const RotaryTensor& s, int rows, int dt, int dh) {
-        if constexpr (E > 1) {
-            from_row = first;
-            if (first < rows) {
-                from_head = first - (int)s.by_heads.div((uint32_t)first) * s.heads;
-                from = source(s, first);
-            }
+    if (E > 1 && !crosses) {
+        in.open<false, T>(p, 0, tokens, first, step, batch0, t0, place);
 #pragma unroll
-            for (int u = 0; u < kAhead - 1; ++u) copy_next(s, rows, dt, dh);
-        }
-    };
-    const int dt0 = (int)p.t[0].by_heads.div((uint32_t)step), dh0 = step - dt0 * p.t[0].heads;
-    begin(p.t[0], tokens * p.t[0].heads, dt0, dh0);
+        for (int u = 0; u < kAhead - 1; ++u) copy_next(u * slot_step);
+    }
     for (int i = thread; i < tokens * p.pairs; i += threads) {
         const int lt = i / p.pairs, pair = i - lt * p.pairs;
         int64_t t = t0 + lt, b = batch0;
-        if (p.tokens != p.rows && t >= p.tokens) {
+        if (crosses && t >= p.tokens) {
             b += t / p.tokens;
             t %= p.tokens;
         }
@@ -297,55 +319,78 @@ __global__ void __launch_bounds__(kRotaryThreads) rotary_kernel(const __grid_con
         float s, c;
         sincospif(2.f * head, &s, &c);
         const float cos_t = fmaf(-s, tail, c), sin_t = fmaf(c, tail, s);
-        rotary_cs[i] = make_float2(cos_t, p.inverse ? -sin_t : sin_t);
+        rotary_cs[lt * pitch + pair] = make_float2(cos_t, p.inverse ? -sin_t : sin_t);
     }
     __syncthreads();
-    auto run = [&](const RotaryTensor& s, int dt, int dh) {
-        const int rows = tokens * s.heads;
-        if constexpr (E > 1) {
-            if (first >= rows) return;
-            RotaryUnit<T, E, HALF> unit;
-            const int lt = (int)s.by_heads.div((uint32_t)first);
-            int head = first - lt * s.heads;
-            const float2* cs = rotary_cs + lt * p.pairs;
-            T* to = static_cast<T*>(s.out) + place(lt, head, s.ob, s.ot, s.oh);
-            const int64_t ahead = (int64_t)dt * s.ot + (int64_t)dh * s.oh, wrap = s.ot - (int64_t)s.heads * s.oh;
-            for (int r = first; r < rows; r += step) {
+    if constexpr (E > 1) {
+        if (!crosses) {
+            out.open<true, T>(p, 0, tokens, first, step, batch0, t0, place);
+            if (out.left == 0) return;
+            const float2* const mine = rotary_cs + w * Unit::kPairs;
+            const float2* cs;
+            int cs_step;
+            auto turns_of = [&] {                                        // where out begins a tensor
+                const RotaryTensor& s = p.t[out.tensor];
+                cs = mine + (int)s.by_heads.div((uint32_t)first) * pitch;
+                cs_step = (int)s.by_heads.div((uint32_t)step) * pitch;
+            };
+            turns_of();
+            for (uint32_t slot = 0, before = (kAhead - 1) * slot_step;;) {
                 asm volatile("cp.async.wait_group %0;" ::"n"(kAhead - 2) : "memory");
-                const int slot = fill + 1 == kAhead ? 0 : fill + 1;      // (the one behind the slot to fill next, which is the row before's)
-                copy_next(s, rows, dt, dh);
-                unit.take(rotary_smem + thread * kUnitBytes + slot * slot_step, (int)second);
-                if (crosses) {
-                    finish(s, unit, r);
-                    continue;
-                }
-                unit.turn_and_store(to, w, p.pairs, p.head_dim, cs);
-                to += ahead;
-                cs += dt * p.pairs;
-                head += dh;
-                if (head >= s.heads) {
-                    head -= s.heads;
-                    to += wrap;
-                    cs += p.pairs;
+                copy_next(before);                                       // (the slot of the row before)
+                Unit unit;
+                unit.take(slots + slot, (int)second);
+                before = slot;
+                slot += slot_step;
+                if (slot == kAhead * slot_step) slot = 0;
+                unit.turn(turning, cs);
+                unit.store(out.at, turning, p.pairs);
+                cs += cs_step;
+                if (out.next()) cs += pitch;
+                if (--out.left == 0) {
+                    out.open<true, T>(p, out.tensor + 1, tokens, first, step, batch0, t0, place);
+                    if (out.left == 0) return;
+                    turns_of();
                 }
             }
+        }
+    }
+    // Rows of any alignment, and the CTAs whose tokens lie in several batches: each row's address by itself.
+    for (int n = 0; n < p.tensors; ++n) {
+        const RotaryTensor& s = p.t[n];
+        const int rows = tokens * s.heads;
+        auto element = [&](int r, int64_t batch, int token, int head, int& lt) {
+            lt = (int)s.by_heads.div((uint32_t)r);
+            int64_t b = batch0, t = t0 + lt;
+            if (crosses && t >= p.tokens) {
+                b += t / p.tokens;
+                t %= p.tokens;
+            }
+            return b * batch + t * token + (int64_t)(r - lt * s.heads) * head;
+        };
+        int lt;
+        if constexpr (E > 1) {
+            for (int r = first; r < rows; r += step) {
+                const int64_t from = element(r, s.xb, s.xt, s.xh, lt) + place, to = element(r, s.ob, s.ot, s.oh, lt) + place;
+                Unit unit;
+                unit.load(static_cast<const uint8_t*>(s.x) + from * (int)sizeof(T), turning, p.pairs);
+                unit.turn(turning, rotary_cs + lt * pitch + w * Unit::kPairs);
+                unit.store(static_cast<uint8_t*>(s.out) + to * (int)sizeof(T), turning, p.pairs);
+            }
         } else {
-            RotaryUnit<T, E, HALF> unit[kAhead];
+            Unit unit[kAhead];
             for (int r0 = first; r0 < rows; r0 += kAhead * step) {
 #pragma unroll
                 for (int u = 0; u < kAhead; ++u)
-                    if (r0 + u * step < rows) unit[u].load(source(s, r0 + u * step), w, p.pairs, p.head_dim);
+                    if (r0 + u * step < rows) unit[u].load(static_cast<const T*>(s.x) + element(r0 + u * step, s.xb, s.xt, s.xh, lt), w, p.pairs, p.head_dim);
 #pragma unroll
                 for (int u = 0; u < kAhead; ++u)
-                    if (r0 + u * step < rows) finish(s, unit[u], r0 + u * step);
+                    if (r0 + u * step < rows) {
+                        T* to = static_cast<T*>(s.out) + element(r0 + u * step, s.ob, s.ot, s.oh, lt);
+                        unit[u].turn_and_store(to, w, p.pairs, p.head_dim, rotary_cs + lt * pitch);
+                    }
             }
         }
-    };
-    run(p.t[0], dt0, dh0);
-    if (p.tensors > 1) {
-        const int dt = (int)p.t[1].by_heads.div((uint32_t)step), dh = step - dt * p.t[1].heads;
-        begin(p.t[1], tokens * p.t[1].heads, dt, dh);
-        run(p.t[1], dt, dh);
     }
 }
 

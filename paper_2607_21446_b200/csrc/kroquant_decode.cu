@@ -45,7 +45,7 @@ kq_status_t launch_rotary(kq::RotaryProblem& p, int sms, cudaStream_t st) {
     const int64_t spare = tiles < sms ? (2 * sms + tiles - 1) / tiles : 1, runs = (taken + rows - 1) / rows;
     p.head_parts = (int)(spare < runs ? spare : runs);
     if (rows > taken) rows = (int)taken;
-    const int smem = (units * rows * kq::rotary_slot_bytes<T, E, HALF>() + 15) / 16 * 16 + (int)per_cta * p.pairs * (int)sizeof(float2);
+    const int smem = (units * rows * kq::rotary_slot_bytes<T, E, HALF>() + 15) / 16 * 16 + (int)per_cta * kq::rotary_pitch(p.pairs) * (int)sizeof(float2);
     static DeviceOnce attr_done;
     const kq_status_t rc = allow_shared(attr_done, kq::rotary_kernel<T, E, HALF>, 100 * 1024);
     if (rc != KQ_OK) return rc;

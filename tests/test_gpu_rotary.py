@@ -198,3 +198,22 @@ def test_refusals():
     with pytest.raises(ValueError):                                      # shifted over its input
         kb.kroquant_rotary(big[:4], None, pos, f, out=big[1:])
     kb.kroquant_rotary(big[:2], None, pos[:2], f, out=big[2:4])
+
+
+def test_outputs_keep_to_themselves():
+    """out of q on k (or the other way round, or one out for both) would be read after it is written: refused.  Slices of one
+    buffer lie between one another and share nothing."""
+    g = torch.Generator(device="cuda")
+    g.manual_seed(31)
+    packed = torch.randn(37, 12, 64, device="cuda", generator=g).bfloat16()
+    q, k = packed[:, :8], packed[:, 8:]
+    pos, f = torch.arange(37, device="cuda", dtype=torch.int32), kb.rotary_frequencies((64,))
+    want = kb.kroquant_rotary(q, k, pos, f)
+    same = torch.zeros_like(q)
+    for out in ((k.new_zeros(37, 8, 64), q[:, :4]), (same, same[:, :4])):
+        with pytest.raises(ValueError):
+            kb.kroquant_rotary(q, k, pos, f, out=out)
+    with pytest.raises(ValueError):
+        kb.kroquant_rotary(q[:, :4], k, pos, f, out=(k, torch.zeros_like(k)))
+    got = kb.kroquant_rotary(q, k, pos, f, out=(q, k))
+    assert torch.equal(got[0], want[0]) and torch.equal(packed[:, 8:], want[1])
