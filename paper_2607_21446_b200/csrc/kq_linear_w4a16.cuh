@@ -6,7 +6,7 @@
 // 16 rows of the product, rows of x as its 8 columns, so that codes go from memory through the converter into the operand and are never
 // stored again (an operand for tcgen05 has to lie in shared memory, in 16 bits: four times the bytes of the codes written and read).
 //
-// A CTA has 128 weight rows, one tile of the scale layout.  Warp w takes rows 32 q + 8 (w % 4) + g, q = 0..3, g = lane / 4, so that the 16
+// Eight warps take 128 weight rows, one tile of the scale layout (a CTA has one such tile, or two and x for both).  Warp w takes rows 32 q + 8 (w % 4) + g, q = 0..3, g = lane / 4, so that the 16
 // scale bytes a lane loads are those of its four rows and no scale is fetched twice; lane j = lane % 4 of a quad takes block j of 128
 // channels, 16 bytes of codes of each row.  The channels' order within the products is the lanes', which x follows in shared memory.
 // The two halves of the warps take every other 128 channels, and the CTAs of a cluster runs of them; the partial sums
@@ -17,9 +17,9 @@
 // largest of the row's four scale bytes: at most 2 significant bits, exact; a block whose scale is 2^-28 of S0's, or less, counts as zero.
 // 2^(S0 - 127 - 13) and x's power multiply the fp32 sum of 128 channels.
 //
-// Measured (us, and the time of the bytes at the copy rate): one row 1152 -> 6912 5.5 (0.7), 5 rows 4096 -> 2 x 5632 gated 12.2 (3.8), 16 rows 12288 -> 4608
-// 21.3 (4.7).  Of the last, 5 us go by until x is converted, 6 with 7 units for each warp (four fifths of the issue slots of an SM with two CTAs, while
-// a third of the SMs have one), 5 waiting for the cluster's last CTA and 4 with its sums and the epilogue.
+// Measured (us, and the time of the bytes at the copy rate): one row 1152 -> 6912 5.5 (0.7), 5 rows 4096 -> 2 x 5632 gated 12.1 (3.8), 16 rows 12288 -> 4608
+// 19.3 (4.7).  Of the last, some 5 us go by until x is converted (mostly latencies), 6 with 6 or 7 units for each warp, the rest waiting for the cluster's
+// last CTA, its sums and the epilogue.
 #pragma once
 #include "kq_linear.cuh"
 #include "kq_mma16.cuh"
@@ -35,15 +35,15 @@ struct W4A16Problem {
     const uint8_t *codes, *scales;
 };
 
-constexpr int kW4Threads = 256;
+constexpr int kW4Threads = 256;          // of a tile
 constexpr int kW4Stages = 3;             // units of a warp on the way or in use
 constexpr int kW4Lift = 13;              // 6 * 2^13 is the largest power-of-two multiple of a code in fp16
 constexpr int kW4StageBytes = 2048 + 128;                                // [q][lane] x 16 bytes of codes, [g] x 16 scale bytes
-template <int NT> struct W4Smem {
-    static constexpr int kUnits = NT == 1 ? 24 : 14;                     // of x at a time (even: the halves of the warps take turns); two CTAs fit an SM
-    static constexpr int kXOff = (kW4Threads / 32) * kW4Stages * kW4StageBytes;
+template <int NT, int TILES> struct W4Smem {                            // (an SM has room for two tiles, in two CTAs or one)
+    static constexpr int kUnits = (NT == 1 ? 24 : 14) * TILES;           // of x at a time (even: the halves of the warps take turns)
+    static constexpr int kXOff = TILES * (kW4Threads / 32) * kW4Stages * kW4StageBytes;
     static constexpr int kXBytes = kUnits * NT * 2048;                   // [unit][row][128 channels]
-    static constexpr int kPartBytes = 2 * 8 * NT * 128 * 4;              // [half of the warps][row of x][weight row], from the start
+    static constexpr int kPartBytes = TILES * 2 * 8 * NT * 128 * 4;      // [tile][half of the warps][row of x][weight row], from the start
     static constexpr int kScaleOff = kXOff + kXBytes;
     static constexpr int kBytes = kScaleOff + kUnits * 8 * NT * 4;
     static_assert(kPartBytes <= kXOff, "partial sums take the place of the stages");
@@ -52,22 +52,25 @@ template <int NT> struct W4Smem {
 // Place (16 bytes) of the k-th eight channels of block j within the 256 bytes of 128 channels of row m: neighbouring operands fill all banks.
 __device__ __forceinline__ int w4_place(int m, int k, int j) { return (4 * k + j) ^ ((m & 1) << 2); }
 
-// grid: x = tiles of 128 weight rows times splits (a cluster), y = runs of 8 NT rows of x
-template <bool GLU, int NT, bool XF16>
-__global__ void __launch_bounds__(kW4Threads, 2) linear_w4a16_kernel(const __grid_constant__ W4A16Problem p, const int splits) {
-    using L = W4Smem<NT>;
+// grid: x = TILES tiles of 128 weight rows times splits (a cluster), y = runs of 8 NT rows of x
+template <bool GLU, int NT, bool XF16, int TILES>
+__global__ void __launch_bounds__(kW4Threads * TILES, 2 / TILES) linear_w4a16_kernel(const __grid_constant__ W4A16Problem p, const int splits) {
+    using L = W4Smem<NT, TILES>;
+    constexpr int kThreads = kW4Threads * TILES;
     extern __shared__ __align__(16) uint8_t w4_smem[];
     uint4* x_smem = reinterpret_cast<uint4*>(w4_smem + L::kXOff);
     float* x_scale = reinterpret_cast<float*>(w4_smem + L::kScaleOff);
-    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, g = lane >> 2, j = lane & 3;
+    const int own_tile = TILES > 1 ? threadIdx.x / kW4Threads : 0, thread = threadIdx.x - own_tile * kW4Threads;
+    const int warp = thread >> 5, lane = threadIdx.x & 31, g = lane >> 2, j = lane & 3;
     const int rank = splits > 1 ? (int)cluster_ctarank() : 0;
-    const int tile = (int)blockIdx.x / splits, m0 = (int)blockIdx.y * 8 * NT;
+    const int tile = (int)blockIdx.x / splits * TILES + own_tile, m0 = (int)blockIdx.y * 8 * NT;
     const int rows = p.lin.M - m0 < 8 * NT ? p.lin.M - m0 : 8 * NT;
     const int u0 = (int)((int64_t)p.units * rank / splits), u1 = (int)((int64_t)p.units * (rank + 1) / splits);
     const int half = warp >> 2, base_row = tile * 128 + 8 * (warp & 3) + g;
     const int blocks = p.K / 32;
     const int64_t pitch = p.K / 2;
-    const uint8_t* scales = p.scales + ((int64_t)tile * p.units * 512) + (8 * (warp & 3) + g) * 16;
+    const bool exists = TILES == 1 || tile * 128 < p.lin.R;             // (a last tile alone: its neighbour's warps get zeros)
+    const uint8_t* scales = p.scales + ((int64_t)(exists ? tile : 0) * p.units * 512) + (8 * (warp & 3) + g) * 16;
     const uint8_t* codes = p.codes + (int64_t)base_row * pitch + 16 * j;
     pdl_launch_dependents();
     pdl_wait_prior_grid();
@@ -80,10 +83,10 @@ __global__ void __launch_bounds__(kW4Threads, 2) linear_w4a16_kernel(const __gri
         if (u < u1) {
             const uint32_t to = ring_at + fill * kW4StageBytes;
             const uint8_t* from = codes + (int64_t)u * 64;
-            const bool exists = 4 * u + j < blocks;
+            const bool inside = 4 * u + j < blocks;
 #pragma unroll
             for (int q = 0; q < 4; ++q) {
-                const bool row = exists && base_row + 32 * q < p.lin.R;
+                const bool row = inside && base_row + 32 * q < p.lin.R;
                 asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;"
                              ::"r"(to + q * 512 + lane * 16), "l"(row ? from + (int64_t)(32 * q) * pitch : p.codes), "r"(row ? 16 : 0) : "memory");
             }
@@ -104,14 +107,14 @@ __global__ void __launch_bounds__(kW4Threads, 2) linear_w4a16_kernel(const __gri
 
     NarrowColumn<GLU> col;
     const LinearItem item = {0, 0, tile, 0, p.lin.M};
-    col.open(p.lin, item, (int)threadIdx.x);                             // (the bias is on its way meanwhile)
+    col.open(p.lin, item, thread);                             // (the bias is on its way meanwhile)
     if (p.lin.epi.residual && col.live)
         for (int c = col.first + rank * NarrowColumn<GLU>::kStep; c < rows; c += NarrowColumn<GLU>::kStep * splits)
             asm volatile("prefetch.global.L2 [%0];" ::"l"(static_cast<const uint8_t*>(p.lin.epi.residual) +
                          ((int64_t)(m0 + c) * p.lin.epi.ld_residual + col.n) * (p.lin.epi.residual_type == kTypeF32 ? 4 : 2)));
 
     // A group of 16 lanes keeps one row of x and takes its 128 channels of every `turns`-th unit, a lane eight channels.
-    const int piece = threadIdx.x & 15, group = threadIdx.x >> 4, turns = (kW4Threads / 16) / rows;
+    const int piece = threadIdx.x & 15, group = threadIdx.x >> 4, turns = (kThreads / 16) / rows;
     const int m = group % rows, first = group < turns * rows ? group / rows : L::kUnits;
     const uint16_t* x_at = static_cast<const uint16_t*>(p.x) + (int64_t)(m0 + m) * p.ld_x + 8 * piece;
     uint4* const x_row = x_smem + m * 16;
@@ -227,7 +230,7 @@ __global__ void __launch_bounds__(kW4Threads, 2) linear_w4a16_kernel(const __gri
 
     asm volatile("cp.async.wait_group 0;" ::: "memory");
     __syncthreads();
-    float* sums = reinterpret_cast<float*>(w4_smem);
+    float* sums = reinterpret_cast<float*>(w4_smem) + own_tile * (2 * 8 * NT * 128);
 #pragma unroll
     for (int t = 0; t < 2; ++t)
 #pragma unroll

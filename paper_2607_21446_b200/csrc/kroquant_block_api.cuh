@@ -172,8 +172,8 @@ kq_status_t run_linear(const uint8_t* a_codes, const uint8_t* a_scales, const ui
 // ---- rows in 16 bits ----------------------------------------------------------------------------------
 
 // How many clusters of 1 .. 8 CTAs the device runs at once (fewer than CTAs / size: a cluster stays within a GPC).
-template <typename Kernel>
-int clusters_at_once(Kernel* kernel, int threads, int smem, int size) {
+template <auto kernel>                                               // (what is known is known of one kernel)
+int clusters_at_once(int threads, int smem, int size) {
     static std::atomic<int> known[64][9];
     const int dev = DeviceOnce::dev();
     if (dev < 0) return 0;
@@ -195,28 +195,52 @@ int clusters_at_once(Kernel* kernel, int threads, int smem, int size) {
     }
     return n;
 }
-template <bool GLU, int NT, bool XF16>
-kq_status_t launch_w4a16(const kq::W4A16Problem& p, int tiles, cudaStream_t st) {
-    constexpr int kBytes = kq::W4Smem<NT>::kBytes;
-    auto* kernel = kq::linear_w4a16_kernel<GLU, NT, XF16>;
-    static DeviceOnce attr_done;
-    if (attr_done.needed()) {
-        if (cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kBytes) != cudaSuccess) {
-            (void)cudaGetLastError();
-            return KQ_ERR_CUDA;
+template <bool GLU, int NT, bool XF16, int TILES>
+struct W4A16Launch {
+    static constexpr int kBytes = kq::W4Smem<NT, TILES>::kBytes, kThreads = kq::kW4Threads * TILES;
+    static constexpr auto* kernel = kq::linear_w4a16_kernel<GLU, NT, XF16, TILES>;
+    int tiles, runs, splits;
+    // K goes over as many CTAs of a cluster as run at once, three units each at least.  CTAs of one tile, 12288 -> 4608 with 16 rows, 1, 2, 3, 7, 8 of
+    // them: 68, 37, 29, 21.3, 43 us (36 clusters of eight do not fit at once); 5 rows of 4096 -> 2 x 5632, 2 to 4: 15.5, 12.2, 17; one row of
+    // 1152 -> 6912, 1 to 4: 6.5, 6.3, 5.5, 5.6.  Sizes other than 2, 4 and 8 leave gaps among those that still run: they keep a fortieth free: 55 clusters of
+    // 56 that fit, one row 4096 -> 7000, 13.2 us (4 CTAs: 9.0).
+    kq_status_t plan(const kq::W4A16Problem& p) {
+        static DeviceOnce attr_done;
+        if (attr_done.needed()) {
+            if (cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kBytes) != cudaSuccess) {
+                (void)cudaGetLastError();
+                return KQ_ERR_CUDA;
+            }
+            attr_done.done();
         }
-        attr_done.done();
+        tiles = (p.lin.R + 128 * TILES - 1) / (128 * TILES);
+        runs = (p.lin.M + 8 * NT - 1) / (8 * NT);
+        splits = 1;
+        for (int n = 2; n <= 8 && p.units >= 3 * n; ++n) {
+            const int64_t fit = clusters_at_once<kernel>(kThreads, kBytes, n), need = (int64_t)tiles * runs;
+            if (need <= ((n & (n - 1)) == 0 ? fit : fit * 39 / 40)) splits = n;
+        }
+        return KQ_OK;
     }
-    // K goes over as many CTAs of a cluster as run at once, three units each at least.  12288 -> 4608 with 16 rows, 1, 2, 3, 7, 8 CTAs: 68, 37,
-    // 29, 21.3, 43 us (36 clusters of eight do not fit at once); 5 rows of 4096 -> 2 x 5632, 2 to 4: 15.5, 12.2, 17; one row of 1152 -> 6912, 1
-    // to 4: 6.5, 6.3, 5.5, 5.6.
-    const int runs = (p.lin.M + 8 * NT - 1) / (8 * NT);
-    int splits = 1;
-    while (splits < 8 && p.units >= 3 * (splits + 1) && (int64_t)tiles * runs <= clusters_at_once(kernel, kq::kW4Threads, kBytes, splits + 1)) ++splits;
-    cudaLaunchConfig_t cfg;
-    cudaLaunchAttribute attr[2];
-    launch_config(&cfg, attr, dim3((unsigned)(tiles * splits), (unsigned)runs), dim3(kq::kW4Threads), kBytes, splits, st);
-    return launch(cfg, kernel, p, splits);
+    kq_status_t run(const kq::W4A16Problem& p, cudaStream_t st) const {
+        cudaLaunchConfig_t cfg;
+        cudaLaunchAttribute attr[2];
+        launch_config(&cfg, attr, dim3((unsigned)(tiles * splits), (unsigned)runs), dim3(kThreads), kBytes, splits, st);
+        return launch(cfg, kernel, p, splits);
+    }
+};
+template <bool GLU, int NT, bool XF16>
+kq_status_t launch_w4a16(const kq::W4A16Problem& p, int sms, cudaStream_t st) {
+    W4A16Launch<GLU, NT, XF16, 1> one;
+    W4A16Launch<GLU, NT, XF16, 2> two;
+    kq_status_t rc = one.plan(p);
+    if (rc == KQ_OK) rc = two.plan(p);
+    if (rc != KQ_OK) return rc;
+    // Two tiles of weight rows in a CTA convert x once for both and leave every SM one CTA, but halve what there is to spread.  us with two | one: 16 rows
+    // 4608 -> 12288 21.2 | 24.5, 12288 -> 4608 19.3 | 21.3, 9216 -> 2304 13.7 | 14.6, 4608 -> 1152 10.1 | 9.4, 2048 -> 9000 11.5 | 9.5, 4096 -> 2 x 5632
+    // (2 and 3 CTAs) 18.7 | 16.2; 5 rows 4608 -> 4608 8.8 | 10.1; one row 12288 -> 4608 14.3 | 13.5; 33 rows 4608 -> 18432, more than run at once, 65 | 58.
+    const int64_t tile_runs = (int64_t)one.tiles * one.runs;
+    return p.lin.M > 4 && p.units >= 32 && tile_runs >= 16 && tile_runs <= 2 * sms && 4 * two.splits >= 3 * one.splits ? two.run(p, st) : one.run(p, st);
 }
 constexpr int kW4MaxRows = 64;
 
@@ -465,12 +489,11 @@ kq_status_t kroquant_linear_w4a16(const void* x, kq_xdtype_t x_dtype, int64_t ld
     p.units = (K + 127) / 128;
     p.codes = b_codes;
     p.scales = b_scales;
-    const int tiles = (int)((R + 127) / 128);
     cudaStream_t st = reinterpret_cast<cudaStream_t>(stream);
     auto go = [&](auto glu, auto nt) {
         constexpr bool GLU = decltype(glu)::value;
         constexpr int NT = decltype(nt)::value;
-        return x_dtype == KQ_X_FP16 ? launch_w4a16<GLU, NT, true>(p, tiles, st) : launch_w4a16<GLU, NT, false>(p, tiles, st);
+        return x_dtype == KQ_X_FP16 ? launch_w4a16<GLU, NT, true>(p, sms, st) : launch_w4a16<GLU, NT, false>(p, sms, st);
     };
     using One = std::integral_constant<int, 1>;
     using Two = std::integral_constant<int, 2>;

@@ -100,6 +100,26 @@ def test_epilogue(activation, glu, M, N, K):
     check(kb.kroquant_linear_w4a16(x, q, s, features=N, **{**full, "residual": out, "out": out}), *expected(x, w, N, **full))
 
 
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float16])
+@pytest.mark.parametrize("M,N,K,glu", [(1, 2150, 4096, False), (4, 2113, 4128, False), (8, 2049, 8192, True), (16, 1050, 4160, True), (20, 1150, 6144, False),
+                                       (64, 600, 4608, False), (33, 2305, 12320, False)])
+def test_long_rows_and_many_tiles(dtype, M, N, K, glu):
+    """Odd and even numbers of tiles of 128 weight rows, where K is long and the tiles are many, but all run at once."""
+    g = gen(M + N + 1)
+    R = 64 * ((N + 31) // 32) if glu else N
+    q, s, w = weight(R, K, g)
+    x = torch.randn(M, K, device="cuda", generator=g).to(dtype)
+    residual = torch.randn(M, N, device="cuda", generator=g).to(dtype)
+    kw = dict(bias=torch.randn(R, device="cuda", generator=g), glu=glu, activation="silu" if glu else "none", residual=residual)
+    want, tol = expected(x, w, N, **kw)
+    check(kb.kroquant_linear_w4a16(x, q, s, features=N, out_dtype=torch.float32, **kw), want, tol)
+    guard = torch.full((M + 2, N), 7.0, device="cuda", dtype=dtype)
+    out = kb.kroquant_linear_w4a16(x, q, s, features=N, out=guard[1:-1], **kw)
+    check(out, want, tol)
+    assert bool((guard[0] == 7).all()) and bool((guard[-1] == 7).all())
+    assert torch.equal(out, kb.kroquant_linear_w4a16(x, q, s, features=N, out_dtype=dtype, **kw))
+
+
 @pytest.mark.parametrize("offset,pitch", [(0, 296), (1, 289), (8, 304), (4, 292)])
 def test_rows_with_a_pitch(offset, pitch):
     g = gen(pitch)
