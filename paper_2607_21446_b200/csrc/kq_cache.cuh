@@ -35,7 +35,7 @@ struct CacheRef {
 __device__ __forceinline__ int64_t cache_cell(const CacheRef& c, const int32_t* table_row, int table_width, int64_t position) {
     if (position < 0 || position >= (int64_t)table_width * c.page_size) return -1;
     const uint32_t entry = position < 0x7FFFFFFF ? c.by_page.div((uint32_t)position) : (uint32_t)(position / c.page_size);
-    const int page = __ldg(table_row + entry);
+    const int page = table_row[entry];
     if (page < 0 || page >= c.pages) return -1;
     return (int64_t)page * c.heads * c.page_size + (position - (int64_t)entry * c.page_size);
 }
@@ -65,13 +65,13 @@ __device__ __forceinline__ void find_cells(const CacheRef& c, const CacheRows& p
             int lo = 0, hi = p.sequences;                                // the last sequence whose offset is <= row (offsets out of order: some sequence)
             while (hi - lo > 1) {
                 const int mid = (lo + hi) >> 1;
-                if (__ldg(p.offsets + mid) <= row) lo = mid; else hi = mid;
+                if (p.offsets[mid] <= row) lo = mid; else hi = mid;
             }
             s = lo;
-            first = __ldg(p.offsets + s);
-            exists = row >= first && row < __ldg(p.offsets + s + 1);
+            first = p.offsets[s];
+            exists = row >= first && row < p.offsets[s + 1];
         }
-        const int64_t position = (p.starts ? (int64_t)__ldg(p.starts + s) : 0) + (row - first);
+        const int64_t position = (p.starts ? (int64_t)p.starts[s] : 0) + (row - first);
         cells[i] = exists ? cache_cell(c, p.table + (int64_t)s * p.table_stride, p.table_width, position) : -2;
     }
     __syncthreads();
@@ -249,16 +249,16 @@ __global__ void __launch_bounds__(kCacheThreads) cache_read_kernel(const __grid_
                 if (cell[k] < 0) continue;
                 const uint8_t* at = codes + (uint64_t)(uint32_t)cell[k] * row_bytes;
                 if constexpr (FORMAT == kCacheFp4) {
-                    const uint2 q = __ldg(reinterpret_cast<const uint2*>(at));
+                    const uint2 q = *reinterpret_cast<const uint2*>(at);
                     w[k][0] = q.x; w[k][1] = q.y;
                 } else {
 #pragma unroll
                     for (int i = 0; i < kWords / 4; ++i) {
-                        const uint4 q = __ldg(reinterpret_cast<const uint4*>(at) + i);
+                        const uint4 q = reinterpret_cast<const uint4*>(at)[i];
                         w[k][4 * i] = q.x; w[k][4 * i + 1] = q.y; w[k][4 * i + 2] = q.z; w[k][4 * i + 3] = q.w;
                     }
                 }
-                if constexpr (FORMAT != kCache16) S[k] = __ldg(scales + (uint64_t)(uint32_t)cell[k] * c.scale_row);
+                if constexpr (FORMAT != kCache16) S[k] = scales[(uint64_t)(uint32_t)cell[k] * c.scale_row];
             }
 #pragma unroll
             for (int k = 0; k < kAhead; ++k) {

@@ -74,7 +74,7 @@ constexpr int kLead = 1;
 struct VisibleRange { int begin, end; };
 __device__ __forceinline__ VisibleRange visible_range(const AttentionProblem& p, int s) {
     const int64_t room = (int64_t)p.table_width * p.c.page_size;
-    int n = __ldg(p.lengths + s);
+    int n = p.lengths[s];
     n = n < 0 ? 0 : (n > room ? (int)room : n);
     return {p.window > 0 && n > p.window ? n - p.window : 0, n};
 }
@@ -123,7 +123,7 @@ struct AttnShape {
     static constexpr int kBytes = kStatsOff + kAttnWarps * NQ * 2 * 4;
     // CTAs of an SM: what registers (operands and accumulators of a lane, some 60 besides) and shared memory allow
     static constexpr int kRegs = D * NQ / 32 + D * NQ / 64;
-        static constexpr int kByRegs = kRegs <= 48 ? 4 : (kRegs <= 96 ? 3 : 2);
+    static constexpr int kByRegs = kRegs <= 48 ? 4 : (kRegs <= 96 ? 3 : 2);
     static constexpr int kBySmem = 227 * 1024 / (kBytes + 1024);
     static constexpr int kPerSm = kByRegs < kBySmem ? kByRegs : kBySmem;
     static_assert(kPerSm >= 1 && kStageBytes % 16 == 0 && kWarpBytes % 16 == 0, "shared memory");
@@ -288,7 +288,7 @@ __global__ void __launch_bounds__(kAttnThreads, (AttnShape<FMT, D, NQ>::kPerSm))
             if (i >= my_steps || lane >= L::kStep || t >= end) return;
             const uint32_t entry = p.c.by_page.div((uint32_t)t);
             slot_next = (uint32_t)t - entry * page_size;
-            page_next = __ldg(table + entry);
+            page_next = table[entry];
         };
         look_up(0);
         int fill = 0;                                                    // stage of the next step to copy
@@ -334,7 +334,7 @@ __global__ void __launch_bounds__(kAttnThreads, (AttnShape<FMT, D, NQ>::kPerSm))
                 const int ch = L::k_channel(m, j);
                 if (p.q_vec) {                                           // four channels at a time; nothing waits for them yet
                     uint2 w = make_uint2(0, 0);
-                    if (exists && ch < p.c.head_dim) w = __ldg(reinterpret_cast<const uint2*>(q + ch));
+                    if (exists && ch < p.c.head_dim) w = *reinterpret_cast<const uint2*>(q + ch);
                     qf[m][nt][0] = w.x;
                     qf[m][nt][1] = w.y;
                 } else {

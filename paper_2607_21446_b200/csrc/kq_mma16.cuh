@@ -1,5 +1,7 @@
 // Products of 16 x 8 tiles whose operands are made in registers, sm_100a: the instruction, the converters from E2M1 and E4M3 codes to
 // fp16 pairs, and powers of two.
+// (The kernels of a step read with plain loads what the kernel before may have written: it still runs when they begin, and a load that
+// assumes constant memory may be moved in front of the wait for it.)
 #pragma once
 #include "kq_common.cuh"
 

@@ -311,9 +311,9 @@ __global__ void __launch_bounds__(kRotaryThreads, 2) rotary_kernel(const __grid_
         }
         const int axis = (pair >= p.axis_end[0]) + (pair >= p.axis_end[1]) + (pair >= p.axis_end[2]);
         const int64_t at = b * p.pos_batch + t * p.pos_token + axis;
-        const double position = p.positions_f32 ? (double)__ldg(static_cast<const float*>(p.positions) + at)
-                                                : (double)__ldg(static_cast<const int*>(p.positions) + at);
-        const double turns = position * (__ldg(p.frequencies + pair) * 0.15915494309189533577);
+        const double position = p.positions_f32 ? (double)static_cast<const float*>(p.positions)[at]
+                                                : (double)static_cast<const int*>(p.positions)[at];
+        const double turns = position * (p.frequencies[pair] * 0.15915494309189533577);
         const double rest = turns - rint(turns);
         const float head = (float)rest, tail = 6.2831853071795865f * (float)(rest - (double)head);
         float s, c;
