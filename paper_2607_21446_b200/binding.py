@@ -1046,7 +1046,8 @@ def _span(t: torch.Tensor):
 
 
 def _heads_last(t: torch.Tensor, what: str, dims: int, dtypes=_DTYPES) -> None:
-    if t.dim() != dims or t.dtype not in dtypes or t.get_device() != _device() or (t.stride(-1) != 1 and t.shape[-1] > 1):
+    stride = t.stride()
+    if len(stride) != dims or t.dtype not in dtypes or t.get_device() != _device() or (stride[-1] != 1 and t.shape[-1] > 1):
         raise ValueError(f"{what} must be a {dims}-D CUDA tensor of {', '.join(str(d)[6:] for d in dtypes)} on the current device with contiguous channels")
 
 
@@ -1189,12 +1190,13 @@ def _int_vector(t: torch.Tensor, size: int, dev: int, what: str) -> int:
 
 def _table(cache: KVCache, table: torch.Tensor):
     """(sequences, pointer, stride, width) of a table of pages, on the cache's device, which must be the current one."""
-    if cache._device != _device():
+    dev, shape, stride = cache._device, table.shape, table.stride()
+    if dev != _device():
         raise ValueError("the cache is not on the current CUDA device")
-    if table.dtype is not torch.int32 or table.dim() != 2 or table.get_device() != cache._device or \
-            (table.shape[1] > 1 and table.stride(1) != 1) or (table.shape[0] > 1 and table.stride(0) < 0):
+    if table.dtype is not torch.int32 or len(shape) != 2 or table.get_device() != dev or (shape[1] > 1 and stride[1] != 1) or \
+            (shape[0] > 1 and stride[0] < 0):
         raise ValueError("table must be an int32 tensor [sequences, pages of a sequence] on the cache's device with contiguous rows")
-    return table.shape[0], table.data_ptr(), table.stride(0), table.shape[1]
+    return shape[0], table.data_ptr(), stride[0], shape[1]
 
 
 def _cache_rows(call: str, cache: KVCache, k, v, rows, where, offsets, starts, stream) -> None:
@@ -1218,12 +1220,13 @@ def kroquant_cache_write(cache: KVCache, k: torch.Tensor, v: torch.Tensor, table
     where = _table(cache, table)
     _heads_last(k, "k", 3, X_DTYPES)
     _heads_last(v, "v", 3, X_DTYPES)
-    shape = (k.shape[0], cache.heads, cache.head_dim)
-    if k.shape != shape or v.shape != shape or v.dtype is not k.dtype or (cache.format == "16bit" and k.dtype is not cache.dtype):
+    shape, dtype = k.shape, k.dtype
+    rows = shape[0]
+    if shape != (rows, cache.heads, cache.head_dim) or v.shape != shape or v.dtype is not dtype or (cache.format == "16bit" and dtype is not cache.dtype):
         raise ValueError("k and v must be [rows, heads, head_dim] of the cache, of one dtype (a 16bit cache: its own)")
-    if offsets is None and shape[0] != where[0]:
+    if offsets is None and rows != where[0]:
         raise ValueError("without offsets there is one row per sequence")
-    _cache_rows("kroquant_cache_write", cache, k, v, shape[0], where, offsets, starts, stream)
+    _cache_rows("kroquant_cache_write", cache, k, v, rows, where, offsets, starts, stream)
 
 
 def kroquant_cache_read(cache: KVCache, table: torch.Tensor, rows: int, *, offsets: Optional[torch.Tensor] = None,
@@ -1237,9 +1240,13 @@ def kroquant_cache_read(cache: KVCache, table: torch.Tensor, rows: int, *, offse
         dtype = cache.dtype if dtype is None else dtype
         if dtype not in _DTYPES:
             raise ValueError("dtype must be float32, bfloat16 or float16")
-        with _allocating(stream):
-            k = torch.empty_strided(shape, (shape[1] * shape[2], shape[2], 1), dtype=dtype, device=cache.device)       # (2.4 us by its shape alone)
+        strides = (shape[1] * shape[2], shape[2], 1)
+        if stream is None:
+            k = torch.empty_strided(shape, strides, dtype=dtype, device=cache.device)                # (2.4 us by its shape alone)
             v = torch.empty_like(k)
+        else:
+            with _allocating(stream):
+                k, v = (torch.empty_strided(shape, strides, dtype=dtype, device=cache.device) for _ in range(2))
     else:
         k, v = out
         for t in (k, v):
