@@ -1051,6 +1051,25 @@ def _heads_last(t: torch.Tensor, what: str, dims: int, dtypes=_DTYPES) -> None:
         raise ValueError(f"{what} must be a {dims}-D CUDA tensor of {', '.join(str(d)[6:] for d in dtypes)} on the current device with contiguous channels")
 
 
+def _turned_into(q: torch.Tensor, k: Optional[torch.Tensor], out, dims: int):
+    """The outputs a caller gave :func:`kroquant_rotary`: each its input, or apart from all that the call reads and writes."""
+    outs = (out, None) if k is None else tuple(out)
+    if len(outs) != 2 or not isinstance(outs[0], torch.Tensor) or (k is not None and not isinstance(outs[1], torch.Tensor)):
+        raise ValueError("out must be a tensor, or a pair of tensors where k is given")
+    for x, o in ((q, outs[0]), (k, outs[1])):
+        if x is None:
+            continue
+        _heads_last(o, "out", dims)
+        if o.shape != x.shape or o.dtype is not q.dtype or not _apart(o):
+            raise ValueError("out must have its input's shape and dtype, and elements of their own")
+        (a0, a1), (b0, b1) = _span(o), _span(x)
+        if a0 < b1 and b0 < a1 and (a0 != b0 or o.stride() != x.stride()):
+            raise ValueError("out may be its input, but must not overlap it in another way")
+    if k is not None and k.numel() and q.numel() and (outs[0].data_ptr() in (k.data_ptr(), outs[1].data_ptr()) or outs[1].data_ptr() == q.data_ptr()):
+        raise ValueError("out of q must be neither k nor out of k, and out of k not q")
+    return outs
+
+
 def kroquant_rotary(q: torch.Tensor, k: Optional[torch.Tensor], positions: torch.Tensor, frequencies: torch.Tensor, *, axes=None,
                     layout: str = "interleaved", inverse: bool = False, out=None, stream=None):
     """Rotary positions: -> q turned, or (q, k) turned where k is given.
@@ -1086,42 +1105,27 @@ def kroquant_rotary(q: torch.Tensor, k: Optional[torch.Tensor], positions: torch
     if (positions.dtype is not torch.int32 and positions.dtype is not torch.float32) or positions.get_device() != dev or \
             (place != (tokens, n) and (dims != 4 or place != (batches, tokens, n))) or (n > 1 and ps[-1] != 1):
         raise ValueError("positions must be a CUDA int32 or float32 tensor [tokens, axes], or [batch, tokens, axes], with contiguous axes")
-    outs = (None, None) if out is None else (out, None) if k is None else tuple(out)
-    if len(outs) != 2 or (out is not None and not isinstance(outs[0], torch.Tensor)):
-        raise ValueError("out must be a tensor, or a pair of tensors where k is given")
-    made = []
-    for x, o in ((q, outs[0]), (k, outs[1])):
-        if x is None:
-            continue
-        if o is None:
-            o = _empty_rows(x, dtype, stream)
-        else:
-            _heads_last(o, "out", dims)
-            if o.shape != x.shape or o.dtype is not dtype or not _apart(o):
-                raise ValueError("out must have its input's shape and dtype, and elements of their own")
-            (a0, a1), (b0, b1) = _span(o), _span(x)
-            if a0 < b1 and b0 < a1 and (a0 != b0 or o.stride() != x.stride()):
-                raise ValueError("out may be its input, but must not overlap it in another way")
-        made.append(o)
-
-    ot, no_k = made[0].stride(), k is None
-    if out is not None and not no_k and k.numel() and q.numel() and (
-            made[0].data_ptr() in (k.data_ptr(), made[1].data_ptr()) or made[1].data_ptr() == q.data_ptr()):
-        raise ValueError("out of q must be neither k nor out of k, and out of k not q")
+    no_k = k is None
+    if out is None:
+        qo = torch.empty_like(q) if stream is None and q.is_contiguous() else _empty_rows(q, dtype, stream)
+        ko = None if no_k else torch.empty_like(k) if stream is None and k.is_contiguous() else _empty_rows(k, dtype, stream)
+    else:
+        qo, ko = _turned_into(q, k, out, dims)
+    ot = qo.stride()
     if no_k:
         kt = pt = (0, 0, 0, 0)
     else:
-        pt = made[1].stride()
+        pt = ko.stride()
     batched = dims == 4
     a = _PACK_ROTARY(_DTYPES[dtype], batches, tokens, d, way, 1 if inverse else 0, n, *wide, frequencies.data_ptr(),
                      positions.data_ptr(), 1 if positions.dtype is torch.float32 else 0, ps[0] if len(ps) == 3 else 0, ps[-2],
-                     q.data_ptr(), 0 if no_k else k.data_ptr(), made[0].data_ptr(), 0 if no_k else made[1].data_ptr(), shape[-2], 0 if no_k else ks[-2],
+                     q.data_ptr(), 0 if no_k else k.data_ptr(), qo.data_ptr(), 0 if no_k else ko.data_ptr(), shape[-2], 0 if no_k else ks[-2],
                      qt[0] if batched else 0, kt[0] if batched else 0, qt[-3], kt[-3], qt[-2], kt[-2],
                      ot[0] if batched else 0, pt[0] if batched else 0, ot[-3], pt[-3], ot[-2], pt[-2])
     rc = load_library().kroquant_rotary(a, _stream(stream))
     if rc:
         raise KroQuantError(rc, "kroquant_rotary")
-    return made[0] if k is None else (made[0], made[1])
+    return qo if no_k else (qo, ko)
 
 
 class KVCache:

@@ -215,11 +215,12 @@ struct W4A16Launch {
         }
         tiles = (p.lin.R + 128 * TILES - 1) / (128 * TILES);
         runs = (p.lin.M + 8 * NT - 1) / (8 * NT);
-        splits = 1;
-        for (int n = 2; n <= 8 && p.units >= 3 * n; ++n) {
-            const int64_t fit = clusters_at_once<kernel>(kThreads, kBytes, n), need = (int64_t)tiles * runs;
-            if (need <= ((n & (n - 1)) == 0 ? fit : fit * 39 / 40)) splits = n;
+        const int64_t need = (int64_t)tiles * runs;
+        for (splits = p.units < 24 ? p.units / 3 : 8; splits > 1; --splits) {
+            const int64_t fit = clusters_at_once<kernel>(kThreads, kBytes, splits);
+            if (need <= ((splits & (splits - 1)) == 0 ? fit : fit * 39 / 40)) break;
         }
+        if (splits < 1) splits = 1;
         return KQ_OK;
     }
     kq_status_t run(const kq::W4A16Problem& p, cudaStream_t st) const {
@@ -234,13 +235,15 @@ kq_status_t launch_w4a16(const kq::W4A16Problem& p, int sms, cudaStream_t st) {
     W4A16Launch<GLU, NT, XF16, 1> one;
     W4A16Launch<GLU, NT, XF16, 2> two;
     kq_status_t rc = one.plan(p);
-    if (rc == KQ_OK) rc = two.plan(p);
     if (rc != KQ_OK) return rc;
     // Two tiles of weight rows in a CTA convert x once for both and leave every SM one CTA, but halve what there is to spread.  us with two | one: 16 rows
     // 4608 -> 12288 21.2 | 24.5, 12288 -> 4608 19.3 | 21.3, 9216 -> 2304 13.7 | 14.6, 4608 -> 1152 10.1 | 9.4, 2048 -> 9000 11.5 | 9.5, 4096 -> 2 x 5632
     // (2 and 3 CTAs) 18.7 | 16.2; 5 rows 4608 -> 4608 8.8 | 10.1; one row 12288 -> 4608 14.3 | 13.5; 33 rows 4608 -> 18432, more than run at once, 65 | 58.
     const int64_t tile_runs = (int64_t)one.tiles * one.runs;
-    return p.lin.M > 4 && p.units >= 32 && tile_runs >= 16 && tile_runs <= 2 * sms && 4 * two.splits >= 3 * one.splits ? two.run(p, st) : one.run(p, st);
+    if (p.lin.M <= 4 || p.units < 32 || tile_runs < 16 || tile_runs > 2 * sms) return one.run(p, st);
+    rc = two.plan(p);
+    if (rc != KQ_OK) return rc;
+    return 4 * two.splits >= 3 * one.splits ? two.run(p, st) : one.run(p, st);
 }
 constexpr int kW4MaxRows = 64;
 
