@@ -22,7 +22,8 @@
 // score, fp32) and V relative to the largest of its position, which goes into P: p 2^(S_t - R + 9), R the largest S_t so far (a
 // running maximum that rescales the accumulator as m does).  Code times 2^(S - S_t + kLift) has at most 4 significant bits and is exact in
 // fp16; a block whose scale is 2^-28 (E2M1) or 2^-21 (E4M3) of its position's largest, or less, counts as zero.  The queries of a CTA are
-// fp16 times one power of two, exact for both 16-bit types down to values 2^-29 of the largest.  P is rounded to fp16 (11 bits; a weight
+// fp16 times one power of two, or one each where their sizes differ much, so that none costs another its digits: exact for both 16-bit types
+// down to values 2^-21 of the query's largest.  P is rounded to fp16 (11 bits; a weight
 // below 2^-23 of the largest keeps fewer, which is 2^-34 of the largest value at most), with 16-bit values, where memory leaves the time, to
 // two terms of their type (16 and 22 bits).
 //
@@ -39,6 +40,10 @@ namespace kq {
 // rescaled: weights are then up to 2^kSlack, times 2^kPLift below fp16's largest.
 constexpr float kSlack = 6;
 constexpr int kPLift = 9;
+
+// Queries of a CTA share one power of two unless the largest values of two of them are further apart than 2^kQueryRange.  (A power for each in every
+// call: one sequence of 131071 in MXFP4 46 us, with it 45.)
+constexpr int kQueryRange = 8;
 
 enum { kAttnBf16 = 0, kAttnF16 = 1, kAttnFp8 = 2, kAttnFp4 = 3 };
 constexpr int kAttnWarps = 4;
@@ -324,6 +329,8 @@ __global__ void __launch_bounds__(kAttnThreads, (AttnShape<FMT, D, NQ>::kPerSm))
         // ---- queries: operand registers and their power of two ----
         uint32_t qf[kM][NT][2];
         float q_scale = p.scale_log2e;
+        bool apart = false;                                              // the queries have a power of two each
+        float* const powers = stats + warp * NQ;                         // then: those (the place of the warp's maxima)
 #pragma unroll
         for (int nt = 0; nt < NT; ++nt) {
             const int row = chunk * NQ + nt * 8 + g;                     // query head within the group
@@ -364,20 +371,29 @@ __global__ void __launch_bounds__(kAttnThreads, (AttnShape<FMT, D, NQ>::kPerSm))
 #pragma unroll
         for (int i = 0; i < L::kStages - 1; ++i) issue(i);
         if constexpr (L::kCodes) {
-            uint32_t amax = 0;                                           // of the magnitude bits
+            int e[NT], most = -100;                                      // exponent of the largest value of query 8 nt + g (0 and subnormal ones: -100), of all
 #pragma unroll
-            for (int nt = 0; nt < NT; ++nt)
+            for (int nt = 0; nt < NT; ++nt) {
+                uint32_t amax = 0;                                       // of the magnitude bits
 #pragma unroll
                 for (int m = 0; m < kM; ++m)
 #pragma unroll
                     for (int i = 0; i < 2; ++i) amax = max(amax, max(qf[m][nt][i] & 0x7FFFu, (qf[m][nt][i] >> 16) & 0x7FFFu));
-            amax = __reduce_max_sync(0xFFFFFFFFu, amax);
-            const float top = p.q_f16 ? __half2float(__ushort_as_half((unsigned short)amax)) : __uint_as_float(amax << 16);
-            int e = (int)(__float_as_uint(top) >> 23) - 127;             // (0 and subnormal values: -127)
-            e = e < -100 ? -100 : e;
-            const float up = exp2_int(14 - e);
+                amax = max(amax, __shfl_xor_sync(0xFFFFFFFFu, amax, 1));
+                amax = max(amax, __shfl_xor_sync(0xFFFFFFFFu, amax, 2));
+                const float top = p.q_f16 ? __half2float(__ushort_as_half((unsigned short)amax)) : __uint_as_float(amax << 16);
+                e[nt] = max((int)(__float_as_uint(top) >> 23) - 127, -100);              // (infinity and NaN: 128)
+                most = max(most, e[nt]);
+            }
+            most = __reduce_max_sync(0xFFFFFFFFu, most);
 #pragma unroll
-            for (int nt = 0; nt < NT; ++nt)
+            for (int nt = 0; nt < NT; ++nt) apart |= most - e[nt] > kQueryRange;
+            apart = __any_sync(0xFFFFFFFFu, apart);
+#pragma unroll
+            for (int nt = 0; nt < NT; ++nt) {
+                if (!apart) e[nt] = most;
+                else if (j == 0) powers[nt * 8 + g] = exp2_int(e[nt]);
+                const float up = exp2_int(14 - e[nt]);
 #pragma unroll
                 for (int m = 0; m < kM; ++m)
 #pragma unroll
@@ -393,7 +409,9 @@ __global__ void __launch_bounds__(kAttnThreads, (AttnShape<FMT, D, NQ>::kPerSm))
                         }
                         qf[m][nt][i] = pack_f16(lo * up, hi * up);
                     }
-            q_scale *= exp2_int(e - 14 - L::kLift);
+            }
+            q_scale *= exp2_int((apart ? 0 : most) - 14 - L::kLift);
+            __syncwarp();
         }
 
         int use = 0;
@@ -514,23 +532,40 @@ __global__ void __launch_bounds__(kAttnThreads, (AttnShape<FMT, D, NQ>::kPerSm))
 
             // ---- scores, running maximum and sum ----
             float vf[kMt][2];
+            auto scores = [&](auto own) {                                // own: with the queries' own powers
+                float power[NT][2];
+                if constexpr (decltype(own)::value) {
 #pragma unroll
-            for (int mt = 0; mt < kMt; ++mt)
-#pragma unroll
-                for (int h = 0; h < 2; ++h) {
-                    const int k = 16 * mt + 8 * h + g;
-                    float kf = q_scale;
-                    vf[mt][h] = FMT == kAttnF16 ? (float)(1 << kPLift) : 1.f;
-                    if constexpr (L::kCodes) {
-                        kf = __shfl_sync(0xFFFFFFFFu, k_factor, k);
-                        vf[mt][h] = __shfl_sync(0xFFFFFFFFu, v_factor, k);
+                    for (int nt = 0; nt < NT; ++nt) {
+                        const float2 two = *reinterpret_cast<const float2*>(powers + nt * 8 + 2 * j);
+                        power[nt][0] = two.x;
+                        power[nt][1] = two.y;
                     }
-                    const float shut = (mask >> L::row_of(k)) & 1u ? 0.f : kMinus;       // (keys without a place were read as zeros)
-#pragma unroll
-                    for (int nt = 0; nt < NT; ++nt)
-#pragma unroll
-                        for (int i = 0; i < 2; ++i) s[mt][nt][2 * h + i] = fmaf(s[mt][nt][2 * h + i], kf, shut);
                 }
+#pragma unroll
+                for (int mt = 0; mt < kMt; ++mt)
+#pragma unroll
+                    for (int h = 0; h < 2; ++h) {
+                        const int k = 16 * mt + 8 * h + g;
+                        float kf = q_scale;
+                        vf[mt][h] = FMT == kAttnF16 ? (float)(1 << kPLift) : 1.f;
+                        if constexpr (L::kCodes) {
+                            kf = __shfl_sync(0xFFFFFFFFu, k_factor, k);
+                            vf[mt][h] = __shfl_sync(0xFFFFFFFFu, v_factor, k);
+                        }
+                        const float shut = (mask >> L::row_of(k)) & 1u ? 0.f : kMinus;   // (keys without a place were read as zeros)
+#pragma unroll
+                        for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+                            for (int i = 0; i < 2; ++i) {
+                                float f = kf;
+                                if constexpr (decltype(own)::value) f *= power[nt][i];
+                                s[mt][nt][2 * h + i] = fmaf(s[mt][nt][2 * h + i], f, shut);
+                            }
+                    }
+            };
+            if (L::kCodes && apart) scores(std::true_type{});
+            else scores(std::false_type{});
             bool grown = v_new != v_run;
             float m_new[NT][2];
 #pragma unroll
