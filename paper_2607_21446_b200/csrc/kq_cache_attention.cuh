@@ -415,6 +415,7 @@ __global__ void __launch_bounds__(kAttnThreads, (AttnShape<FMT, D, NQ>::kPerSm))
         }
 
         int use = 0;
+        uint32_t seen = 0;                                               // whether any position has had a place
         for (int it = 0; it < my_steps; ++it) {
             asm volatile("cp.async.wait_group %0;" ::"n"(L::kStages - 2) : "memory");
             __syncwarp();
@@ -424,6 +425,7 @@ __global__ void __launch_bounds__(kAttnThreads, (AttnShape<FMT, D, NQ>::kPerSm))
             const uint8_t* kst = stage;
             const uint8_t* vst = stage + L::kStep * L::kRow;
             const uint32_t mask = *reinterpret_cast<const uint32_t*>(stage + L::kMaskOff);
+            seen |= mask;
 
             // ---- scales: lane = position of the products ----
             float k_factor = q_scale, v_factor = 1.f;
@@ -716,6 +718,7 @@ __global__ void __launch_bounds__(kAttnThreads, (AttnShape<FMT, D, NQ>::kPerSm))
                 l += __shfl_xor_sync(0xFFFFFFFFu, l, 4);
                 l += __shfl_xor_sync(0xFFFFFFFFu, l, 8);
                 l += __shfl_xor_sync(0xFFFFFFFFu, l, 16);
+                if (seen == 0) l = 0.f;                                  // (a query that is not finite has met no position)
                 if (g == 0) {
                     stats[warp * NQ + nt * 8 + 2 * j + i] = m_run[nt][i];
                     stats[(kAttnWarps + warp) * NQ + nt * 8 + 2 * j + i] = l;

@@ -62,3 +62,19 @@ def test_heads_of_every_size(form, dtype, group, loud):
         zero = torch.where(keep[..., None], q, torch.zeros_like(q))
         instead, its_lse = kb.kroquant_cache_attention(zero, cache, table, n, out_dtype=torch.float32, lse=True, scale=scale)
         check(torch.where(keep[..., None], out, instead), zero, cache, table, n, scale, lse=torch.where(keep, lse, its_lse))
+
+
+@pytest.mark.parametrize("form,dtype", FORMATS)
+@pytest.mark.parametrize("value", [float("nan"), float("inf")])
+def test_a_row_without_any_position_is_zero_whatever_its_query(form, dtype, value):
+    cache, table, _ = make([100, 100, 100], 2, 64, 16, form, dtype, 6)
+    table[0] = -1
+    q = torch.randn(3, 4, 64, device="cuda", generator=gen(6)).to(dtype)
+    q[0], q[1] = value, value
+    n = torch.tensor([100, 0, 100], dtype=torch.int32, device="cuda")
+    wide = torch.cat([table, torch.full((3, 3000), -1, dtype=torch.int32, device="cuda")], 1)
+    longer = torch.tensor([40000, 0, 100], dtype=torch.int32, device="cuda")
+    for t, lengths in ((table, n), (wide, n), (wide, longer)):
+        out, lse = kb.kroquant_cache_attention(q, cache, t, lengths, lse=True)
+        assert bool((out[:2] == 0).all()) and bool((lse[:2] == -math.inf).all())
+        check(out[2:], q[2:], cache, t[2:], lengths[2:], 0.125, lse=lse[2:])
