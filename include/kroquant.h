@@ -541,7 +541,8 @@ kq_status_t kroquant_cache_attention(const kq_cache_t *cache, const kq_attention
 /* kroquant_linear_mxfp4 with the rows of A left in 16 bits (x: DEVICE [M] rows of ld_x elements, bf16 or fp16, any alignment) instead of
  * quantized: the weight is the same (codes and tiled scales, 16-byte aligned), and so are the epilogue and out.  For few rows, where
  * reading the weight is the cost and 4-bit activations would save nothing: 1 <= M <= 64.  Products of the weight's values with x
- * (x to 11 significant bits within 128 channels, which holds both types), fp32 sums, one rounding.  One launch. */
+ * (x to 11 significant bits within 128 channels, which holds both types), fp32 sums, one rounding.  One launch.  out may be the residual
+ * (same pitch) and must not overlap x: rows of out are written while others are still to be formed from x. */
 kq_status_t kroquant_linear_w4a16(const void *x, kq_xdtype_t x_dtype, int64_t ld_x, const uint8_t *b_codes, const uint8_t *b_scales,
                                   int64_t M, int N, int K, const kq_epilogue_t *epilogue, void *out, kq_dtype_t out_dtype,
                                   int64_t ld_out, void *stream);

@@ -10,6 +10,7 @@ from __future__ import annotations
 import contextlib
 import ctypes as C
 import functools
+import math
 import os
 import struct
 import threading
@@ -674,6 +675,27 @@ def _rows2d(t: torch.Tensor, shape, what: str) -> int:
                      "contiguous rows that do not overlap")
 
 
+def _span(t: torch.Tensor):
+    """First byte of t and the one behind its last."""
+    base = t.data_ptr()
+    return base, base + t.element_size() * (1 + sum((n - 1) * s for n, s in zip(t.shape, t.stride()))) if t.numel() else base
+
+
+def _meet(a: torch.Tensor, b: torch.Tensor) -> bool:
+    """Whether two tensors may have a byte in common.  They have none where their spans lie apart, or where they are different parts of the same
+    packed rows: with steps from row to row that are all multiples of P, each stays within its own bytes modulo P."""
+    (a0, a1), (b0, b1) = _span(a), _span(b)
+    if a1 <= b0 or b1 <= a0 or a0 == a1 or b0 == b1:
+        return False
+    sides = [[(s * t.element_size(), n) for n, s in zip(t.shape, t.stride()) if n > 1 and s] for t in (a, b)]
+    for least in {step for side in sides for step, _ in side}:
+        period = math.gcd(*(step for side in sides for step, _ in side if step >= least))
+        wide = [t.element_size() + sum((n - 1) * step for step, n in side if step < least) for t, side in zip((a, b), sides)]
+        if wide[0] <= (b0 - a0) % period <= period - wide[1]:
+            return False
+    return True
+
+
 def _linear(a_codes, a_scales, b_codes, b_scales, offsets, features, bias, activation, glu, gate, rows_per_gate, row_scale,
             residual, residual_scale, out, out_dtype, stream, ld_x=None):
     dev = _device()
@@ -732,6 +754,8 @@ def _linear(a_codes, a_scales, b_codes, b_scales, offsets, features, bias, activ
         ld_out = N
     else:
         ld_out = _rows2d(out, (M, N), "out")
+        if not quantized and _meet(out, a_codes):
+            raise ValueError("out must not overlap x, which other parts of the call still read")
     if grouped:
         if offsets.dtype is not torch.int32 or offsets.shape != (experts + 1,) or offsets.get_device() != dev or not offsets.is_contiguous():
             raise ValueError("offsets must be a contiguous CUDA int32 tensor [experts + 1]")
@@ -794,7 +818,7 @@ def kroquant_linear_w4a16(x: torch.Tensor, b_codes: torch.Tensor, b_scales: torc
                           stream=None) -> torch.Tensor:
     """:func:`kroquant_linear_mxfp4` with rows that stay in 16 bits: x [M, K] bfloat16 or float16 (a row pitch is allowed),
     1 <= M <= 64, the weight and the keyword arguments as there.  For a few rows (a decode step, a conditioning vector)
-    it reads what the quantized form reads and keeps the activations' digits."""
+    it reads what the quantized form reads and keeps the activations' digits.  out may be the residual, but must not overlap x."""
     if x.dtype not in X_DTYPES:
         raise ValueError("x must be bfloat16 or float16")
     if x.dim() != 2:
@@ -1037,12 +1061,6 @@ def _apart(t: torch.Tensor) -> bool:
             return False
         reach = stride * (size - 1) + reach
     return True
-
-
-def _span(t: torch.Tensor):
-    """First byte of t and the one behind its last."""
-    base = t.data_ptr()
-    return base, base + t.element_size() * (1 + sum((n - 1) * s for n, s in zip(t.shape, t.stride()))) if t.numel() else base
 
 
 def _heads_last(t: torch.Tensor, what: str, dims: int, dtypes=_DTYPES) -> None:

@@ -1,0 +1,78 @@
+"""CPU-only: outputs of a decode step's calls that share memory with what the call reads, or with one another, are refused before any launch."""
+import random
+
+import pytest
+import torch
+
+from paper_2607_21446_b200 import binding as kb
+
+
+def addresses(t):
+    """Byte addresses of a CPU tensor's elements."""
+    at = torch.zeros(t.shape, dtype=torch.int64)
+    for i, (n, s) in enumerate(zip(t.shape, t.stride())):
+        at += (torch.arange(n) * s * t.element_size()).view([-1 if k == i else 1 for k in range(t.dim())])
+    return {t.data_ptr() + int(a) + b for a in at.flatten() for b in range(t.element_size())}
+
+
+def test_meet_never_overlooks_a_shared_byte():
+    rng = random.Random(1)
+    room = torch.zeros(4096, dtype=torch.uint8)
+    apart = 0
+    for _ in range(3000):
+        views = []
+        for _ in range(2):
+            t = room.view(rng.choice([torch.uint8, torch.bfloat16, torch.float32]))
+            shape = [rng.randint(1, 4) for _ in range(rng.randint(1, 4))]
+            stride = [rng.choice([0, 1, 2, 3, 4, 8, 12, 16, 24, 32, 48, 64]) for _ in shape]
+            reach = sum((n - 1) * s for n, s in zip(shape, stride))
+            views.append(t.as_strided(shape, stride, rng.randint(0, min(40, t.numel() - reach - 1))))
+        met = bool(addresses(views[0]) & addresses(views[1]))
+        assert kb._meet(*views) == kb._meet(*views[::-1])
+        if not kb._meet(*views):
+            apart += 1
+            assert not met
+    assert apart > 500
+
+
+def test_parts_of_packed_rows_do_not_meet():
+    packed = torch.zeros(5, 11, 8, dtype=torch.bfloat16)
+    q, k, v = packed.split((6, 2, 3), 1)
+    pairs = [(q, k), (q, v), (k, v), (q[..., :4], q[..., 4:]), (packed[::2], packed[1::2]), (packed[:0], packed), (q[:2], q[2:])]
+    batched = torch.zeros(3, 5, 11, 8)
+    pairs += [(batched[:, :, :6], batched[:, :, 6:]), (batched[:, :2], batched[:, 2:]), (batched[..., :3], batched[..., 3:])]
+    heads_first = batched.transpose(1, 2)
+    pairs += [(heads_first[:, :6], heads_first[:, 6:]), (batched.expand(3, 5, 11, 8)[:1], batched[1:])]
+    for a, b in pairs:
+        assert not kb._meet(a, b) and not kb._meet(b, a)
+    for a, b in ((q, q), (q, packed), (packed[:, 0:8], packed[:, 4:11]), (packed[:3], packed[2:]), (q, packed[:, 5:7]), (packed.view(5, 88), k)):
+        assert kb._meet(a, b) and kb._meet(b, a)
+
+
+@pytest.fixture
+def here(monkeypatch):
+    """CPU tensors pass for tensors on the current device: what the checks do not refuse reaches the library, which finds no device."""
+    monkeypatch.setattr(kb, "_device", lambda: -1)
+
+
+def refused(call, *args, **kw):
+    with pytest.raises(ValueError):
+        call(*args, **kw)
+
+
+def passes(call, *args, **kw):
+    if not torch.cuda.is_available():                                    # (on a device the call would run on these addresses)
+        with pytest.raises(kb.KroQuantError):
+            call(*args, **kw)
+
+
+def test_few_row_product_refuses_out_on_x(here):
+    M, N = 3, 64
+    x = torch.zeros(M, N, dtype=torch.bfloat16)
+    w, s = torch.zeros(N, N // 2, dtype=torch.uint8), torch.zeros(kb.tiled_scale_bytes(N, N), dtype=torch.uint8)
+    room = torch.zeros(M, 2 * N, dtype=torch.bfloat16)
+    for a, out in ((x, x), (room[:, :N], room[:, N // 2 : N // 2 + N]), (room[:, 1 : N + 1], room[:, :N]), (x, x.view(torch.float16))):
+        refused(kb.kroquant_linear_w4a16, a, w, s, out=out, stream=0)
+        refused(kb.kroquant_linear_w4a16, a, w, s, out=out, residual=out, stream=0)
+    passes(kb.kroquant_linear_w4a16, room[:, :N], w, s, out=room[:, N:], stream=0)
+    passes(kb.kroquant_linear_w4a16, x, w, s, out=room[:, N:], residual=room[:, N:], stream=0)
