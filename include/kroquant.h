@@ -490,7 +490,8 @@ typedef struct kq_cache {
  * [offsets[0], offsets[sequences]) are neither written nor read.  No value of offsets, starts or table leads outside the buffers;
  * pages that two sequences share may be read, but must not be written by both.
  * k, v: DEVICE, row i of head h at i * row stride + h * head stride (elements), contiguous channels, any alignment of the type.
- * write takes bf16 or fp16 (16BIT: the cache's dtype) and finite values; read gives any of the three types. */
+ * write takes bf16 or fp16 (16BIT: the cache's dtype) and finite values; read gives any of the three types, into k and v that overlap neither
+ * one another nor the cache. */
 typedef struct kq_cache_rows {
     int64_t rows;
     int sequences;

@@ -1255,7 +1255,8 @@ def kroquant_cache_read(cache: KVCache, table: torch.Tensor, rows: int, *, offse
                         starts: Optional[torch.Tensor] = None, dtype=None, out=None, stream=None):
     """The inverse of :func:`kroquant_cache_write`: -> (k, v) [rows, heads, head_dim] in `dtype` (default: the cache's; float32 is allowed), the
     values that the cache holds at the places of the rows.  Rows without a place are zeros; rows outside the sequences
-    (before offsets[0], from offsets[-1] on) are left as they are.  out: a pair of tensors to write to."""
+    (before offsets[0], from offsets[-1] on) are left as they are.  out: a pair of tensors to write to, which overlap neither one another
+    nor the cache."""
     where = _table(cache, table)
     shape = (rows, cache.heads, cache.head_dim)
     if out is None:
@@ -1275,6 +1276,8 @@ def kroquant_cache_read(cache: KVCache, table: torch.Tensor, rows: int, *, offse
             _heads_last(t, "out", 3)
             if t.shape != shape or t.dtype is not k.dtype or dtype not in (None, t.dtype) or not _apart(t):
                 raise ValueError("out must be two tensors [rows, heads, head_dim] of one dtype with elements of their own")
+        if _meet(k, v) or any(t is not None and (_meet(k, t) or _meet(v, t)) for t in cache._buffers):
+            raise ValueError("the two tensors of out must overlap neither one another nor the cache")
     if offsets is None and rows != where[0]:
         raise ValueError("without offsets there is one row per sequence")
     _cache_rows("kroquant_cache_read", cache, k, v, rows, where, offsets, starts, stream)

@@ -76,3 +76,21 @@ def test_few_row_product_refuses_out_on_x(here):
         refused(kb.kroquant_linear_w4a16, a, w, s, out=out, residual=out, stream=0)
     passes(kb.kroquant_linear_w4a16, room[:, :N], w, s, out=room[:, N:], stream=0)
     passes(kb.kroquant_linear_w4a16, x, w, s, out=room[:, N:], residual=room[:, N:], stream=0)
+
+
+def cache_of(form, dtype=torch.bfloat16):
+    return kb.KVCache.empty(4, 8, 2, 64, form, dtype, device="cpu"), torch.zeros(3, 2, dtype=torch.int32)
+
+
+@pytest.mark.parametrize("form", ["16bit", "mxfp8"])
+def test_cache_read_refuses_outputs_on_one_another_or_on_the_cache(here, form):
+    cache, table = cache_of(form)
+    room = torch.zeros(3, 6, 64, dtype=torch.bfloat16)
+    k, v = room[:, :2], room[:, 2:4]
+    for out in ((k, k), (k, room[:, 1:3]), (room[:, :4:2], room[:, 2:4]), (k, k.view(torch.float16).view(torch.bfloat16))):
+        refused(kb.kroquant_cache_read, cache, table, 3, out=out, stream=0)
+    inside = cache.k.view(torch.bfloat16).view(-1)[: 3 * 2 * 64].view(3, 2, 64)
+    for out in ((inside, v), (k, inside)):
+        refused(kb.kroquant_cache_read, cache, table, 3, out=out, stream=0)
+    passes(kb.kroquant_cache_read, cache, table, 3, out=(k, v), stream=0)
+    passes(kb.kroquant_cache_read, cache, table, 3, out=(room[:, ::2][:, :2], room[:, 1::2][:, :2]), stream=0)
