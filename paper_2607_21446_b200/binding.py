@@ -677,23 +677,38 @@ def _rows2d(t: torch.Tensor, shape, what: str) -> int:
 
 def _span(t: torch.Tensor):
     """First byte of t and the one behind its last."""
-    base = t.data_ptr()
-    return base, base + t.element_size() * (1 + sum((n - 1) * s for n, s in zip(t.shape, t.stride()))) if t.numel() else base
+    base, count = t.data_ptr(), t.numel()
+    if count and not t.is_contiguous():
+        count = 1
+        for n, s in zip(t.shape, t.stride()):
+            count += (n - 1) * s
+    return base, base + count * t.element_size()
 
 
 def _meet(a: torch.Tensor, b: torch.Tensor) -> bool:
-    """Whether two tensors may have a byte in common.  They have none where their spans lie apart, or where they are different parts of the same
-    packed rows: with steps from row to row that are all multiples of P, each stays within its own bytes modulo P."""
-    (a0, a1), (b0, b1) = _span(a), _span(b)
-    if a1 <= b0 or b1 <= a0 or a0 == a1 or b0 == b1:
+    """Whether two tensors may have a byte in common."""
+    return _spans_meet(a, _span(a), b, _span(b))
+
+
+def _spans_meet(a: torch.Tensor, a_span, b: torch.Tensor, b_span) -> bool:
+    """The same with the spans known."""
+    if a_span[1] <= b_span[0] or b_span[1] <= a_span[0] or a_span[0] == a_span[1] or b_span[0] == b_span[1]:
         return False
-    sides = [[(s * t.element_size(), n) for n, s in zip(t.shape, t.stride()) if n > 1 and s] for t in (a, b)]
-    for least in {step for side in sides for step, _ in side}:
-        period = math.gcd(*(step for side in sides for step, _ in side if step >= least))
-        wide = [t.element_size() + sum((n - 1) * step for step, n in side if step < least) for t, side in zip((a, b), sides)]
-        if wide[0] <= (b0 - a0) % period <= period - wide[1]:
-            return False
-    return True
+    return not _parts_of_rows(b_span[0] - a_span[0], a.element_size(), a.shape, a.stride(), b.element_size(), b.shape, b.stride())
+
+
+@functools.lru_cache(maxsize=256)
+def _parts_of_rows(ahead: int, a_size: int, a_shape, a_stride, b_size: int, b_shape, b_stride) -> bool:
+    """Whether tensors whose spans overlap, the second `ahead` bytes behind the first, are different parts of the same packed rows: with steps from
+    row to row that are all multiples of P, each stays within its own bytes modulo P."""
+    a_steps = [(s * a_size, n) for n, s in zip(a_shape, a_stride) if n > 1 and s]
+    b_steps = [(s * b_size, n) for n, s in zip(b_shape, b_stride) if n > 1 and s]
+    for least in {step for step, _ in a_steps + b_steps}:
+        period = math.gcd(*(step for step, _ in a_steps + b_steps if step >= least))
+        a_wide, b_wide = (size + sum((n - 1) * step for step, n in steps if step < least) for size, steps in ((a_size, a_steps), (b_size, b_steps)))
+        if a_wide <= ahead % period <= period - b_wide:
+            return True
+    return False
 
 
 def _linear(a_codes, a_scales, b_codes, b_scales, offsets, features, bias, activation, glu, gate, rows_per_gate, row_scale,
@@ -1055,12 +1070,17 @@ def _apart(t: torch.Tensor) -> bool:
     """Whether the elements of t lie at different addresses."""
     if t.is_contiguous():
         return True
-    reach = 1
-    for size, stride in sorted(((n, s) for n, s in zip(t.shape, t.stride()) if n > 1), key=lambda p: p[1]):
-        if stride < reach:
-            return False
-        reach = stride * (size - 1) + reach
-    return True
+    dims = list(zip(t.stride(), t.shape))
+    for order in (dims[::-1], None):                                     # most often the last dimension is the innermost
+        reach = 1
+        for stride, size in order or sorted(dims):
+            if size > 1:
+                if stride < reach:
+                    break
+                reach += stride * (size - 1)
+        else:
+            return True
+    return False
 
 
 def _heads_last(t: torch.Tensor, what: str, dims: int, dtypes=_DTYPES) -> None:
@@ -1069,22 +1089,37 @@ def _heads_last(t: torch.Tensor, what: str, dims: int, dtypes=_DTYPES) -> None:
         raise ValueError(f"{what} must be a {dims}-D CUDA tensor of {', '.join(str(d)[6:] for d in dtypes)} on the current device with contiguous channels")
 
 
-def _turned_into(q: torch.Tensor, k: Optional[torch.Tensor], out, dims: int):
-    """The outputs a caller gave :func:`kroquant_rotary`: each its input, or apart from all that the call reads and writes."""
+def _same_rows(a: torch.Tensor, b: torch.Tensor) -> bool:
+    """Whether two tensors of one shape and dtype are the same elements in the same order."""
+    return a is b or a.data_ptr() == b.data_ptr() and all(s == t for n, s, t in zip(a.shape, a.stride(), b.stride()) if n > 1)
+
+
+def _turned_into(q: torch.Tensor, k: Optional[torch.Tensor], out, dims: int, others):
+    """The outputs a caller gave :func:`kroquant_rotary`: each its input, or apart from all that the call reads and writes (others: besides q and k)."""
     outs = (out, None) if k is None else tuple(out)
     if len(outs) != 2 or not isinstance(outs[0], torch.Tensor) or (k is not None and not isinstance(outs[1], torch.Tensor)):
         raise ValueError("out must be a tensor, or a pair of tensors where k is given")
-    for x, o in ((q, outs[0]), (k, outs[1])):
-        if x is None:
-            continue
-        _heads_last(o, "out", dims)
-        if o.shape != x.shape or o.dtype is not q.dtype or not _apart(o):
-            raise ValueError("out must have its input's shape and dtype, and elements of their own")
-        (a0, a1), (b0, b1) = _span(o), _span(x)
-        if a0 < b1 and b0 < a1 and (a0 != b0 or o.stride() != x.stride()):
-            raise ValueError("out may be its input, but must not overlap it in another way")
-    if k is not None and k.numel() and q.numel() and (outs[0].data_ptr() in (k.data_ptr(), outs[1].data_ptr()) or outs[1].data_ptr() == q.data_ptr()):
-        raise ValueError("out of q must be neither k nor out of k, and out of k not q")
+    ins = (q,) if k is None else (q, k)
+    spans = [_span(x) for x in ins]
+    rest = [(t, _span(t)) for t in others]
+    seen = []                                                            # outputs, and the inputs that are none
+    for x, o, span in zip(ins, outs, spans):
+        if o is not x:
+            _heads_last(o, "out", dims)
+            if o.shape != x.shape or o.dtype is not q.dtype:
+                raise ValueError("out must have its input's shape and dtype")
+        if not _apart(o):
+            raise ValueError("out must have elements of their own")
+        if not _same_rows(o, x):
+            place = _span(o)
+            if _spans_meet(o, place, x, span):
+                raise ValueError("out may be its input, but must not overlap it in another way")
+            rest.append((x, span))
+            span = place
+        seen.append((o, span))
+    # each output against the other one and against what is only read (its own input among that: once more)
+    if len(seen) == 2 and _spans_meet(*seen[0], *seen[1]) or any(_spans_meet(*o, *t) for o in seen for t in rest):
+        raise ValueError("out of q must overlap neither k nor out of k, out of k not q, and none the positions or frequencies")
     return outs
 
 
@@ -1128,7 +1163,7 @@ def kroquant_rotary(q: torch.Tensor, k: Optional[torch.Tensor], positions: torch
         qo = torch.empty_like(q) if stream is None and q.is_contiguous() else _empty_rows(q, dtype, stream)
         ko = None if no_k else torch.empty_like(k) if stream is None and k.is_contiguous() else _empty_rows(k, dtype, stream)
     else:
-        qo, ko = _turned_into(q, k, out, dims)
+        qo, ko = _turned_into(q, k, out, dims, (positions, frequencies))
     ot = qo.stride()
     if no_k:
         kt = pt = (0, 0, 0, 0)

@@ -94,3 +94,26 @@ def test_cache_read_refuses_outputs_on_one_another_or_on_the_cache(here, form):
         refused(kb.kroquant_cache_read, cache, table, 3, out=out, stream=0)
     passes(kb.kroquant_cache_read, cache, table, 3, out=(k, v), stream=0)
     passes(kb.kroquant_cache_read, cache, table, 3, out=(room[:, ::2][:, :2], room[:, 1::2][:, :2]), stream=0)
+
+
+def test_rotary_refuses_outputs_on_what_it_reads_or_writes(here):
+    where, f = torch.zeros(5, dtype=torch.int32), torch.ones(4, dtype=torch.float64)
+    packed = torch.zeros(5, 11, 8, dtype=torch.bfloat16)
+    q, k = packed[:, :6], packed[:, 6:8]
+    room = torch.zeros(5, 16, 8, dtype=torch.bfloat16)
+    rot = lambda q, k, out, **kw: kb.kroquant_rotary(q, k, where, f, out=out, stream=0, **kw)  # noqa: E731
+    for out in ((packed[:, 1:7], k), (room[:, :6], packed[:, 5:7]), (room[:, :6], room[:, 5:7]), (packed[:, 2:8], room[:, :2]), (q, packed[:, 5:7]),
+                (room[:, :6], q[:, :2]), (room[:, :6], room[:, :2])):
+        refused(rot, q, k, out)
+    for t in (where, f):
+        inside = torch.as_strided(t.view(torch.bfloat16), (1, 1, 8), (8, 8, 1))
+        refused(kb.kroquant_rotary, room[:1, :1], None, where[:1], f, out=inside, stream=0)
+    refused(rot, q, None, packed[:, 1:7])
+    batched = packed.view(1, 5, 11, 8).expand(2, 5, 11, 8)
+    refused(rot, batched[:, :, :6], None, batched[:, :, :6])             # the same elements twice
+    for out in ((q, k), (q, room[:, :2]), (room[:, :6], k), (room[:, :6], room[:, 6:8]), (room[:, ::2][:, :6], room[:, 1::2][:, :2])):
+        passes(rot, q, k, out)
+    two = torch.zeros(2, 5, 11, 8)
+    passes(rot, two[:, :, :6], two[:, :, 6:8], (two[:, :, :6], two[:, :, 6:8]))
+    one = torch.zeros(1, 6, 8).as_strided((1, 6, 8), (999, 8, 1))
+    passes(kb.kroquant_rotary, one, None, where[:1], f, out=one.as_strided((1, 6, 8), (48, 8, 1)), stream=0)
