@@ -513,7 +513,7 @@ kq_status_t kroquant_cache_read(const kq_cache_t *cache, const kq_cache_rows_t *
  * over the positions max(0, lengths[s] - window) <= t < lengths[s] (window 0: all) that have a place in the cache.  A row without
  * any gives zeros (and lse -inf).  lse (optional): float [sequences][q_heads], the natural logarithm of the sum of exponentials.
  * q and out: strides in elements, contiguous channels, any alignment; q bf16 or fp16 (16BIT: the cache's dtype), out any type, apart from
- * q.
+ * q and the cache.
  * q_heads a multiple of the cache's heads; lengths: DEVICE int32, read on the device, clamped to [0, table_width * page_size], which is
  * at most 2^30.
  * Products are formed on the tensor cores from the cache's own values (q as it is; the weights w to 11 bits or more), sums and

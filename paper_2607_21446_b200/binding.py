@@ -10,7 +10,6 @@ from __future__ import annotations
 import contextlib
 import ctypes as C
 import functools
-import math
 import os
 import struct
 import threading
@@ -699,16 +698,22 @@ def _spans_meet(a: torch.Tensor, a_span, b: torch.Tensor, b_span) -> bool:
 
 @functools.lru_cache(maxsize=256)
 def _parts_of_rows(ahead: int, a_size: int, a_shape, a_stride, b_size: int, b_shape, b_stride) -> bool:
-    """Whether tensors whose spans overlap, the second `ahead` bytes behind the first, are different parts of the same packed rows: with steps from
-    row to row that are all multiples of P, each stays within its own bytes modulo P."""
-    a_steps = [(s * a_size, n) for n, s in zip(a_shape, a_stride) if n > 1 and s]
-    b_steps = [(s * b_size, n) for n, s in zip(b_shape, b_stride) if n > 1 and s]
-    for least in {step for step, _ in a_steps + b_steps}:
-        period = math.gcd(*(step for step, _ in a_steps + b_steps if step >= least))
-        a_wide, b_wide = (size + sum((n - 1) * step for step, n in steps if step < least) for size, steps in ((a_size, a_steps), (b_size, b_steps)))
-        if a_wide <= ahead % period <= period - b_wide:
+    """Whether tensors whose spans overlap, the second `ahead` bytes behind the first, have no byte in common all the same, as different parts of the
+    same packed rows: a byte of both would need offsets within the rows that differ by a multiple of the rows' step, and so on within the row."""
+    def apart(ahead, a_steps, b_steps):
+        a_wide, b_wide = (size + sum((n - 1) * step for step, n in steps) for size, steps in ((a_size, a_steps), (b_size, b_steps)))
+        if ahead >= a_wide or -ahead >= b_wide:
             return True
-    return False
+        if not a_steps and not b_steps:
+            return False
+        step = max(a_steps + b_steps)[0]
+        a_in, b_in = ([p for p in steps if p[0] != step] for steps in (a_steps, b_steps))
+        a_wide, b_wide = (size + sum((n - 1) * s for s, n in steps) for size, steps in ((a_size, a_in), (b_size, b_in)))
+        ahead %= step
+        first, last = -((a_wide - 1 - ahead) // step), (ahead + b_wide - 1) // step                    # multiples of the step that offsets may differ by
+        return last - first < 4 and all(apart(ahead - m * step, a_in, b_in) for m in range(first, last + 1))
+
+    return apart(ahead, [(s * a_size, n) for n, s in zip(a_shape, a_stride) if n > 1 and s], [(s * b_size, n) for n, s in zip(b_shape, b_stride) if n > 1 and s])
 
 
 def _linear(a_codes, a_scales, b_codes, b_scales, offsets, features, bias, activation, glu, gate, rows_per_gate, row_scale,
@@ -1326,7 +1331,7 @@ def kroquant_cache_attention(q: torch.Tensor, cache: KVCache, table: torch.Tenso
     logarithms of the sums of exponentials.  q [sequences, q_heads, head_dim] bfloat16 or float16 (a 16bit cache: its dtype),
     q_heads a multiple of the cache's heads: query head h reads cache head h // (q_heads / heads).  scale: default
     head_dim ** -0.5.  lengths int32 [sequences] counts the new token, written before; it is read on the device.  A sequence
-    without positions (length 0, no pages) gives zeros and -inf.  out_dtype: default q's."""
+    without positions (length 0, no pages) gives zeros and -inf.  out_dtype: default q's.  out overlaps neither q nor the cache."""
     where = _table(cache, table)
     _heads_last(q, "q", 3, X_DTYPES)
     n, heads, d = q.shape
@@ -1343,8 +1348,9 @@ def kroquant_cache_attention(q: torch.Tensor, cache: KVCache, table: torch.Tenso
         _heads_last(out, "out", 3)
         if out.shape != q.shape or out_dtype not in (None, out.dtype) or not _apart(out):
             raise ValueError("out must have q's shape and elements of its own")
-        if out.data_ptr() == q.data_ptr() and q.numel():
-            raise ValueError("out must not be q")
+        place = _span(out)
+        if _spans_meet(out, place, q, _span(q)) or any(t is not None and _spans_meet(out, place, t, _span(t)) for t in cache._buffers):
+            raise ValueError("out must overlap neither q nor the cache")
     lib, logs, scratch = load_library(), None, None
     if lse:
         with _allocating(stream):

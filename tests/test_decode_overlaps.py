@@ -41,6 +41,7 @@ def test_parts_of_packed_rows_do_not_meet():
     pairs = [(q, k), (q, v), (k, v), (q[..., :4], q[..., 4:]), (packed[::2], packed[1::2]), (packed[:0], packed), (q[:2], q[2:])]
     batched = torch.zeros(3, 5, 11, 8)
     pairs += [(batched[:, :, :6], batched[:, :, 6:]), (batched[:, :2], batched[:, 2:]), (batched[..., :3], batched[..., 3:])]
+    pairs += [(packed[:, :10:2], packed[:, 1:11:2]), (packed[:, ::3, :5], packed[:, 1::3]), (batched[:, :, 4:9:2, 1:], batched[:, :, 1::2])]
     heads_first = batched.transpose(1, 2)
     pairs += [(heads_first[:, :6], heads_first[:, 6:]), (batched.expand(3, 5, 11, 8)[:1], batched[1:])]
     for a, b in pairs:
@@ -117,3 +118,16 @@ def test_rotary_refuses_outputs_on_what_it_reads_or_writes(here):
     passes(rot, two[:, :, :6], two[:, :, 6:8], (two[:, :, :6], two[:, :, 6:8]))
     one = torch.zeros(1, 6, 8).as_strided((1, 6, 8), (999, 8, 1))
     passes(kb.kroquant_rotary, one, None, where[:1], f, out=one.as_strided((1, 6, 8), (48, 8, 1)), stream=0)
+
+
+@pytest.mark.parametrize("form", ["16bit", "mxfp4"])
+def test_attention_refuses_out_on_q_or_on_the_cache(here, form):
+    cache, table = cache_of(form)
+    n = torch.ones(3, dtype=torch.int32)
+    room = torch.zeros(3, 9, 64, dtype=torch.bfloat16)
+    q = room[:, :4]
+    inside = cache.v.view(torch.bfloat16).view(-1)[: 3 * 4 * 64].view(3, 4, 64)
+    for out in (q, room[:, 1:5], room[:, 3:7], room[:, :8:2], inside, q.view(torch.float16)):
+        refused(kb.kroquant_cache_attention, q, cache, table, n, out=out, stream=0)
+    passes(kb.kroquant_cache_attention, q, cache, table, n, out=room[:, 4:8], stream=0)
+    passes(kb.kroquant_cache_attention, room[:, :8:2], cache, table, n, out=room[:, 1:8:2], stream=0)
