@@ -488,7 +488,8 @@ typedef struct kq_cache {
  * NULL: row i belongs to sequence i (rows == sequences).  starts: DEVICE int32 [sequences], or NULL: 0.  A position that is negative or
  * beyond the table, and a table entry outside [0, pages), is no place: write leaves such a row out, read gives zeros.  Rows outside
  * [offsets[0], offsets[sequences]) are neither written nor read.  No value of offsets, starts or table leads outside the buffers;
- * pages that two sequences share may be read, but must not be written by both.
+ * pages that two sequences share, or that one has twice, may be read, but no place in them may be written twice by one call, and a cache whose
+ * buffers overlap may only be read.  Rows that a call writes do not lie in the places it writes them to.
  * k, v: DEVICE, row i of head h at i * row stride + h * head stride (elements), contiguous channels, any alignment of the type.
  * write takes bf16 or fp16 (16BIT: the cache's dtype) and finite values; read gives any of the three types, into k and v that overlap neither
  * one another nor the cache. */

@@ -1191,7 +1191,8 @@ class KVCache:
     as they are ("16bit") or in MXFP8 or MXFP4.  The buffers are torch tensors: k, v [pages, heads, page_size, row] (16-bit values of
     `dtype`, or uint8 codes) and for the codes k_scales, v_scales uint8 [pages, heads, page_size, scale row]; a row has
     32 * ceil(head_dim / 32) channels, those behind head_dim zero.  dtype is what :func:`kroquant_cache_read` gives unless asked
-    for another.  Which pages belong to which sequence is the caller's table."""
+    for another.  Which pages belong to which sequence is the caller's table.  Buffers that overlap (keys that are the values, too) can be
+    read but not written."""
 
     def __init__(self, k: torch.Tensor, v: torch.Tensor, k_scales: Optional[torch.Tensor] = None, v_scales: Optional[torch.Tensor] = None, *,
                  head_dim: int, format: str = "mxfp4", dtype=None):
@@ -1222,6 +1223,8 @@ class KVCache:
             if not t.is_contiguous() or t.get_device() != k.get_device():
                 raise ValueError("the cache's buffers must be contiguous tensors on one device")
         self._buffers = (k, v, k_scales, v_scales)
+        own = [t for t in self._buffers if t is not None]
+        self._shared = any(_meet(a, b) for i, a in enumerate(own) for b in own[:i])      # may be read, but not written
         self.format, self.dtype, self.head_dim, self.device = format, dtype, head_dim, k.device
         self.pages, self.heads, self.page_size = k.shape[0], k.shape[1], k.shape[2]
         self._device, self._c = k.get_device(), _Cache(code, _DTYPES[dtype], k.shape[0], k.shape[2], k.shape[1], head_dim, k.data_ptr(), v.data_ptr(),
@@ -1284,6 +1287,8 @@ def kroquant_cache_write(cache: KVCache, k: torch.Tensor, v: torch.Tensor, table
     _heads_last(v, "v", 3, X_DTYPES)
     shape, dtype = k.shape, k.dtype
     rows = shape[0]
+    if cache._shared:
+        raise ValueError("the cache's buffers overlap: it can only be read")
     if shape != (rows, cache.heads, cache.head_dim) or v.shape != shape or v.dtype is not dtype or (cache.format == "16bit" and dtype is not cache.dtype):
         raise ValueError("k and v must be [rows, heads, head_dim] of the cache, of one dtype (a 16bit cache: its own)")
     if offsets is None and rows != where[0]:

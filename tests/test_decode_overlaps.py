@@ -131,3 +131,15 @@ def test_attention_refuses_out_on_q_or_on_the_cache(here, form):
         refused(kb.kroquant_cache_attention, q, cache, table, n, out=out, stream=0)
     passes(kb.kroquant_cache_attention, q, cache, table, n, out=room[:, 4:8], stream=0)
     passes(kb.kroquant_cache_attention, room[:, :8:2], cache, table, n, out=room[:, 1:8:2], stream=0)
+
+
+def test_cache_whose_buffers_overlap_is_not_written(here):
+    table, one = torch.zeros(3, 2, dtype=torch.int32), torch.zeros(3, 2, 64, dtype=torch.bfloat16)
+    c = kb.KVCache.empty(4, 8, 2, 64, "mxfp8", device="cpu")
+    b = kb.KVCache.empty(4, 8, 2, 64, "16bit", device="cpu")
+    for shared in (kb.KVCache(b.k, b.k, head_dim=64, format="16bit"), kb.KVCache(c.k, c.k, c.k_scales, c.v_scales, head_dim=64, format="mxfp8"),
+                   kb.KVCache(c.k, c.v, c.k_scales, c.k_scales, head_dim=64, format="mxfp8")):
+        refused(kb.kroquant_cache_write, shared, one, one, table, stream=0)
+        passes(kb.kroquant_cache_read, shared, table, 3, out=(one, one.clone()), stream=0)
+    halves = torch.zeros(8, 2, 8, 64, dtype=torch.bfloat16)
+    passes(kb.kroquant_cache_write, kb.KVCache(halves[:4], halves[4:], head_dim=64, format="16bit"), one, one, table, stream=0)
