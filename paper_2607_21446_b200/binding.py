@@ -181,8 +181,6 @@ def _allocating(stream):
 
 def _empty_rows(like: torch.Tensor, dtype, stream) -> torch.Tensor:
     """A tensor of like's shape with rows one after the other (empty_like costs 1 us of a call, new_empty with a shape 2)."""
-    if stream is None and like.dtype is dtype and like.is_contiguous():
-        return torch.empty_like(like)
     if stream is None:
         return torch.empty_like(like, dtype=dtype, memory_format=torch.contiguous_format)
     with _allocating(stream):
@@ -1165,8 +1163,7 @@ def kroquant_rotary(q: torch.Tensor, k: Optional[torch.Tensor], positions: torch
         raise ValueError("positions must be a CUDA int32 or float32 tensor [tokens, axes], or [batch, tokens, axes], with contiguous axes")
     no_k = k is None
     if out is None:
-        qo = torch.empty_like(q) if stream is None and q.is_contiguous() else _empty_rows(q, dtype, stream)
-        ko = None if no_k else torch.empty_like(k) if stream is None and k.is_contiguous() else _empty_rows(k, dtype, stream)
+        qo, ko = _empty_rows(q, dtype, stream), None if no_k else _empty_rows(k, dtype, stream)
     else:
         qo, ko = _turned_into(q, k, out, dims, (positions, frequencies))
     ot = qo.stride()
