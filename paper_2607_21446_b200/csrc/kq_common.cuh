@@ -97,10 +97,11 @@ __device__ __forceinline__ int64_t tiled_scale_index(int64_t t, int j, int cb) {
     return ((t >> 7) * cb + (j >> 2)) * 512 + (t & 31) * 16 + ((t >> 5) & 3) * 4 + (j & 3);
 }
 
-// streaming (read-once / write-once) global accesses
+// streaming (read-once / write-once) global accesses.  (Not .nc: the data may be written while this kernel already runs, by the kernel before it,
+// which it waits for.)
 __device__ __forceinline__ uint4 ld_stream_16(const void* p) {
     uint4 v;
-    asm volatile("ld.global.nc.L1::no_allocate.v4.u32 {%0,%1,%2,%3}, [%4];"
+    asm volatile("ld.global.L1::no_allocate.v4.u32 {%0,%1,%2,%3}, [%4];"
                  : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "l"(p));
     return v;
 }

@@ -1,0 +1,20 @@
+"""CPU-only, by the sources: the kernels of a block and of a step are launched so that they may begin while the kernel before them in the stream still
+writes what they will read.  They wait for it (griddepcontrol.wait), and what they read then must be read by loads that cannot be moved in front of
+the wait and that see what was written while the kernel already ran: no __ldg and no ld.global.nc."""
+import os
+import re
+
+import pytest
+
+CSRC = os.path.join(os.path.dirname(os.path.dirname(os.path.abspath(__file__))), "paper_2607_21446_b200", "csrc")
+
+
+def code(name):
+    """The file without comments."""
+    with open(os.path.join(CSRC, name)) as f:
+        return re.sub(r"//[^\n]*", "", f.read())
+
+
+@pytest.mark.parametrize("name", ["kq_common.cuh", "kq_mma16.cuh", "kq_rotary.cuh", "kq_cache.cuh", "kq_cache_attention.cuh", "kq_linear_w4a16.cuh"])
+def test_kernels_of_a_step_read_with_plain_loads(name):
+    assert "__ldg" not in code(name) and ".nc" not in code(name)

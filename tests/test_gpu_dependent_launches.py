@@ -1,0 +1,56 @@
+"""What a kernel writes is what the next one in the stream reads, although that one may begin early: chains of calls captured into one graph, over
+inputs that change from link to link, against the same calls one at a time.  Equal bits."""
+import pytest
+import torch
+
+from paper_2607_21446_b200 import binding as kb
+
+pytestmark = pytest.mark.gpu
+
+
+def gen(seed):
+    g = torch.Generator(device="cuda")
+    g.manual_seed(seed)
+    return g
+
+
+def same_in_one_graph(links, call):
+    """call(i) -> tensors; each link once with a wait in front and behind, then all of them in one graph, three times."""
+    want = []
+    for i in range(links):
+        torch.cuda.synchronize()
+        want.append([t.clone() for t in call(i)])
+        torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        got = [call(i) for i in range(links)]
+    for _ in range(3):
+        for link in got:
+            for t in link:
+                t.view(torch.uint8).fill_(0x7F)
+        graph.replay()
+        torch.cuda.synchronize()
+        for a, b in zip(got, want):
+            assert all(torch.equal(s.view(torch.uint8), t.view(torch.uint8)) for s, t in zip(a, b))
+    assert kb.kroquant_last_device_error() == 0
+
+
+@pytest.mark.parametrize("form", ["16bit", "mxfp8", "mxfp4"])
+@pytest.mark.parametrize("d,layout", [(128, "half"), (72, "half"), (64, "interleaved")])
+def test_rotary_in_place_then_write_then_read(form, d, layout):
+    rows, heads, size = 700, 6, 16
+    x = torch.randn(8, rows, 3 * heads, d, device="cuda", generator=gen(d)).bfloat16()
+    cache = kb.KVCache.empty(rows // size + 1, size, heads, d, form)
+    table = torch.arange(rows // size + 1, dtype=torch.int32, device="cuda")[None]
+    offsets = torch.tensor([0, rows], dtype=torch.int32, device="cuda")
+    where, f = torch.arange(rows, dtype=torch.int32, device="cuda"), kb.rotary_frequencies([d])
+    packed = torch.empty_like(x[0])
+
+    def link(i):
+        packed.copy_(x[i])
+        q, k, v = packed.split(heads, 1)
+        kb.kroquant_rotary(q, k, where, f, layout=layout, out=(q, k))
+        kb.kroquant_cache_write(cache, k, v, table, offsets=offsets)
+        return kb.kroquant_cache_read(cache, table, rows, offsets=offsets)
+
+    same_in_one_graph(8, link)
