@@ -221,7 +221,7 @@ gemm_mxfp4_umma(const __grid_constant__ CUtensorMap tmap_a, const __grid_constan
 #pragma unroll
                         for (int q = 0; q < 4; ++q) {
                             float t[8];
-                            widen8(__ldg(ap + q), t);
+                            widen8(ap[q], t);
 #pragma unroll
                             for (int e = 0; e < 8; ++e) v[8 * q + e] += t[e];
                         }

@@ -188,7 +188,7 @@ __device__ __forceinline__ int rows_taken(const int32_t* offsets, int M, int exp
     int end = 0;
 #pragma unroll 1
     for (int e = 0; e < expert; ++e) {
-        int lo = __ldg(offsets + e), hi = __ldg(offsets + e + 1);
+        int lo = offsets[e], hi = offsets[e + 1];
         clamp_rows(M, lo, hi);
         if (hi > lo && hi > end) end = hi;
     }
@@ -202,7 +202,7 @@ __device__ __forceinline__ void build_item_table(const LinearProblem& p, int* cu
         const int e = e0 + lane;
         int items = 0, decreases = 0;
         if (e < p.experts) {
-            int lo = __ldg(p.offsets + e), hi = __ldg(p.offsets + e + 1);
+            int lo = p.offsets[e], hi = p.offsets[e + 1];
             decreases = hi < lo;
             clamp_rows(p.M, lo, hi);
             if (hi > lo) items = ((hi - 1) / ROWS - lo / ROWS + 1) * p.tiles_n;
@@ -223,7 +223,7 @@ __device__ __forceinline__ void build_item_table(const LinearProblem& p, int* cu
             int end = 0;
             base = 0;
             for (int e = 0; e < p.experts; ++e) {
-                int lo = __ldg(p.offsets + e), hi = __ldg(p.offsets + e + 1);
+                int lo = p.offsets[e], hi = p.offsets[e + 1];
                 clamp_rows(p.M, lo, hi);
                 cum[e] = base;
                 if (hi <= lo || hi <= end) continue;
@@ -256,8 +256,8 @@ __device__ __forceinline__ ItemAhead item_ahead(const LinearProblem& p, const in
             if (cum[mid] <= t) lo = mid; else hi = mid;
         }
         a.expert = lo;
-        a.lo = __ldg(p.offsets + lo);
-        a.hi = __ldg(p.offsets + lo + 1);
+        a.lo = p.offsets[lo];
+        a.hi = p.offsets[lo + 1];
     }
     return a;
 }
@@ -701,7 +701,7 @@ linear_mxfp4_pair(const __grid_constant__ CUtensorMap tmap_a, const __grid_const
                 const int row = c.row0 + lane < c.hi ? (c.row0 + lane > c.lo ? c.row0 + lane : c.lo) : c.hi - 1;
                 c.which = p.epi.gate.ptr ? row / p.epi.rows_per_gate : 0;
                 c.uniform = __all_sync(0xFFFFFFFFu, c.which == __shfl_sync(0xFFFFFFFFu, c.which, 0));
-                c.scale = p.epi.row_scale ? __ldg(p.epi.row_scale + row) : 1.f;
+                c.scale = p.epi.row_scale ? p.epi.row_scale[row] : 1.f;
                 __syncwarp();                                                       // the vectors of the item before have been read
                 if (copied) fetch_residual(p.epi, mem, bar_res, c.row0 + lane, c.lo, c.hi, col, lane);
                 fetch_vectors<GLU>(p.epi, reinterpret_cast<float*>(mem + kLinVecOff), w.expert, wrow, p.R, col, c.which, p.epi.gate.ptr && c.uniform, lane);
@@ -856,7 +856,7 @@ struct NarrowColumn {
             const bool ok = j < count;
             res[j] = p.residual && ok ? load_typed(p.residual, p.residual_type, (int64_t)row * p.ld_residual + n) : 0.f;
             gate[j] = p.gate.ptr && ok ? vec_entry(p.gate, row / p.rows_per_gate, n, 1.f) : 1.f;
-            scale[j] = !p.row_scale || !ok ? 1.f : (row_scale ? row_scale[j * stride] : __ldg(p.row_scale + row));
+            scale[j] = !p.row_scale || !ok ? 1.f : (row_scale ? row_scale[j * stride] : p.row_scale[row]);
         }
 #pragma unroll
         for (int j = 0; j < J; ++j) v[j] += bias;
@@ -1049,7 +1049,7 @@ linear_mxfp4_narrow(const __grid_constant__ CUtensorMap tmap_w, const __grid_con
             // loads wait behind the operand stages in flight (2 us): the row scales come while the item is multiplied
             if (p.epi.row_scale && threadIdx.x < 64 + 128) {
                 const int row = w.tile_m * 128 + (int)threadIdx.x - 64;
-                scales[threadIdx.x - 64] = row < p.M ? __ldg(p.epi.row_scale + row) : 0.f;
+                scales[threadIdx.x - 64] = row < p.M ? p.epi.row_scale[row] : 0.f;
             }
             // A wait that gives up must not keep this warp from the barriers below: the decision to stop is taken by all
             // epilogue warps together, from a word that is only written before the first of them.

@@ -18,3 +18,13 @@ def code(name):
 @pytest.mark.parametrize("name", ["kq_common.cuh", "kq_mma16.cuh", "kq_rotary.cuh", "kq_cache.cuh", "kq_cache_attention.cuh", "kq_linear_w4a16.cuh"])
 def test_kernels_of_a_step_read_with_plain_loads(name):
     assert "__ldg" not in code(name) and ".nc" not in code(name)
+
+
+@pytest.mark.parametrize("name", ["kq_linear.cuh"])
+def test_kernels_of_a_block_read_with_plain_loads(name):
+    assert "__ldg" not in code(name) and ".nc" not in code(name)
+
+
+@pytest.mark.parametrize("name", ["kq_gemm_fp4.cuh", "kq_gemm_fp4_pair.cuh"])
+def test_products_read_the_branch_they_add_with_plain_loads(name):
+    assert not re.search(r"__ldg\(ap", code(name))

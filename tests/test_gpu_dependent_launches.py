@@ -54,3 +54,28 @@ def test_rotary_in_place_then_write_then_read(form, d, layout):
         return kb.kroquant_cache_read(cache, table, rows, offsets=offsets)
 
     same_in_one_graph(8, link)
+
+
+def weight(rows, K, g):
+    w = (torch.randn(rows, K, device="cuda", generator=g) * K ** -0.5).bfloat16()
+    return kb.kroquant_mxfp4_quantize(w, scale_layout="tiled")
+
+
+@pytest.mark.parametrize("M", [8, 300])
+def test_row_scales_from_the_product_before(M):
+    """A product of few rows with one column as router weights of the next product."""
+    g = gen(M)
+    K, N = 1152, 640
+    x = torch.randn(8, M, K, device="cuda", generator=g).bfloat16()
+    router, w = weight(1, K, g), weight(N, K, g)
+    scales = torch.empty(M, 1, device="cuda")
+
+    def link(i):
+        a = kb.kroquant_mxfp4_quantize(x[i], scale_layout="tiled") if M > 64 else None
+        for r in range(0, M, 64):
+            kb.kroquant_linear_w4a16(x[i, r : r + 64], *router, out=scales[r : r + 64])
+        if M > 64:
+            return (kb.kroquant_linear_mxfp4(*a, *w, row_scale=scales.view(-1)),)
+        return (kb.kroquant_linear_w4a16(x[i], *w, row_scale=scales.view(-1)),)
+
+    same_in_one_graph(8, link)
