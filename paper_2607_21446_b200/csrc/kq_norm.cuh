@@ -140,6 +140,27 @@ __device__ __forceinline__ int owned(int d, int c, int step) {
     const int left = c < d ? (d - c + step - 1) / step : 0;
     return left < 8 ? left : 8;
 }
+// Loads of what the kernel before may have written: they see it (no .nc) and stay behind the wait for it, since `q` comes from behind it (behind_wait),
+// but are as free as __ldg otherwise: no store of the kernels that use them reaches the vectors.
+__device__ __forceinline__ const void* behind_wait(const void* q) {
+    asm volatile("" : "+l"(q));
+    return q;
+}
+__device__ __forceinline__ uint4 ld_vector_16(const void* q) {
+    uint4 v;
+    asm("ld.global.v4.u32 {%0,%1,%2,%3}, [%4];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "l"(q));
+    return v;
+}
+__device__ __forceinline__ float ld_vector_4(const void* q) {
+    float v;
+    asm("ld.global.f32 %0, [%1];" : "=f"(v) : "l"(q));
+    return v;
+}
+__device__ __forceinline__ uint32_t ld_vector_2(const void* q) {
+    uint16_t v;
+    asm("ld.global.u16 %0, [%1];" : "=h"(v) : "l"(q));
+    return v;
+}
 // eight entries of a parameter vector at channel c (absent: `none`)
 __device__ __forceinline__ void load_param(const NormVec& p, int64_t batch, int c, int count, bool vec, int step, float none, float (&v)[8]) {
     if (!p.ptr) {
@@ -149,24 +170,26 @@ __device__ __forceinline__ void load_param(const NormVec& p, int64_t batch, int 
     }
     const int64_t at = batch * p.stride + c;
     if (p.type == kTypeF32) {
-        const float* q = static_cast<const float*>(p.ptr) + at;
+        const float* q = static_cast<const float*>(behind_wait(p.ptr)) + at;
         if (vec) {
-            const float4 a = __ldg(reinterpret_cast<const float4*>(q)), b = __ldg(reinterpret_cast<const float4*>(q) + 1);
-            v[0] = a.x; v[1] = a.y; v[2] = a.z; v[3] = a.w; v[4] = b.x; v[5] = b.y; v[6] = b.z; v[7] = b.w;
+            const uint4 a = ld_vector_16(q), b = ld_vector_16(q + 4);
+            const uint32_t w[8] = {a.x, a.y, a.z, a.w, b.x, b.y, b.z, b.w};
+#pragma unroll
+            for (int i = 0; i < 8; ++i) v[i] = __uint_as_float(w[i]);
         } else {
 #pragma unroll
-            for (int i = 0; i < 8; ++i) v[i] = i < count ? __ldg(q + i * step) : 0.f;
+            for (int i = 0; i < 8; ++i) v[i] = i < count ? ld_vector_4(q + i * step) : 0.f;
         }
     } else {
-        const uint16_t* q = static_cast<const uint16_t*>(p.ptr) + at;
+        const uint16_t* q = static_cast<const uint16_t*>(behind_wait(p.ptr)) + at;
         uint4 u;
         if (vec) {
-            u = __ldg(reinterpret_cast<const uint4*>(q));
+            u = ld_vector_16(q);
         } else {
             uint32_t w[4];
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
-                const uint32_t lo = 2 * i < count ? __ldg(q + 2 * i * step) : 0u, hi = 2 * i + 1 < count ? __ldg(q + (2 * i + 1) * step) : 0u;
+                const uint32_t lo = 2 * i < count ? ld_vector_2(q + 2 * i * step) : 0u, hi = 2 * i + 1 < count ? ld_vector_2(q + (2 * i + 1) * step) : 0u;
                 w[i] = lo | (hi << 16);
             }
             u = make_uint4(w[0], w[1], w[2], w[3]);

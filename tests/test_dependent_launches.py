@@ -20,7 +20,7 @@ def test_kernels_of_a_step_read_with_plain_loads(name):
     assert "__ldg" not in code(name) and ".nc" not in code(name)
 
 
-@pytest.mark.parametrize("name", ["kq_linear.cuh"])
+@pytest.mark.parametrize("name", ["kq_linear.cuh", "kq_norm.cuh"])
 def test_kernels_of_a_block_read_with_plain_loads(name):
     assert "__ldg" not in code(name) and ".nc" not in code(name)
 

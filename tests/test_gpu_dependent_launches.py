@@ -79,3 +79,24 @@ def test_row_scales_from_the_product_before(M):
         return (kb.kroquant_linear_w4a16(x[i], *w, row_scale=scales.view(-1)),)
 
     same_in_one_graph(8, link)
+
+
+@pytest.mark.parametrize("rows,d,dtype", [(64, 1152, torch.float32), (3000, 1152, torch.bfloat16), (700, 5600, torch.float32), (90, 203, torch.float16)])
+def test_norm_vectors_from_the_product_before(rows, d, dtype):
+    """The modulation layer's product of one row gives gate, scale and shift of the norm behind it; then the norm's backward pass."""
+    g = gen(d)
+    K, D = 256, (d + 7) // 8 * 8
+    w = weight(3 * D, K, g)
+    t = torch.randn(8, 1, K, device="cuda", generator=g).bfloat16()
+    x, y, dn = (torch.randn(rows, d, device="cuda", generator=g).bfloat16() for _ in range(3))
+    six = torch.empty(1, 3 * D, dtype=dtype, device="cuda")
+
+    def link(i):
+        kb.kroquant_linear_w4a16(t[i], *w, out=six)
+        gate, scale, shift = (six[:, j * D : j * D + d] for j in range(3))
+        h, n = kb.kroquant_norm_residual(x, y, gate=gate, scale=scale, shift=shift, norm="layer")
+        kb.kroquant_linear_w4a16(t[i], *w, out=six)
+        back = kb.kroquant_norm_residual_grad(dn, h, y=y, gate=gate, scale=scale, shift=shift, norm="layer")
+        return h, n, back["dx"], back["dy"], back["dscale"]
+
+    same_in_one_graph(8, link)
