@@ -117,4 +117,29 @@ __device__ __forceinline__ void st_stream_4(void* p, uint32_t v) {
 __device__ __forceinline__ void pdl_launch_dependents() { asm volatile("griddepcontrol.launch_dependents;" ::: "memory"); }
 __device__ __forceinline__ void pdl_wait_prior_grid() { asm volatile("griddepcontrol.wait;" ::: "memory"); }
 
+// Loads of what the kernel before may have written: they see it (no .nc) and stay behind the wait for it, since `q` comes from behind it (behind_wait),
+// but are as free as __ldg otherwise: no store of the kernels that use them reaches the vectors.
+__device__ __forceinline__ const void* behind_wait(const void* q) {
+    asm volatile("" : "+l"(q));
+    return q;
+}
+__device__ __forceinline__ uint4 ld_vector_16(const void* q) {
+    uint4 v;
+    asm("ld.global.v4.u32 {%0,%1,%2,%3}, [%4];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "l"(q));
+    return v;
+}
+__device__ __forceinline__ float4 as_float4(const uint4& v) {
+    return make_float4(__uint_as_float(v.x), __uint_as_float(v.y), __uint_as_float(v.z), __uint_as_float(v.w));
+}
+__device__ __forceinline__ float ld_vector_4(const void* q) {
+    float v;
+    asm("ld.global.f32 %0, [%1];" : "=f"(v) : "l"(q));
+    return v;
+}
+__device__ __forceinline__ uint32_t ld_vector_2(const void* q) {
+    uint16_t v;
+    asm("ld.global.u16 %0, [%1];" : "=h"(v) : "l"(q));
+    return v;
+}
+
 }  // namespace kq

@@ -140,27 +140,6 @@ __device__ __forceinline__ int owned(int d, int c, int step) {
     const int left = c < d ? (d - c + step - 1) / step : 0;
     return left < 8 ? left : 8;
 }
-// Loads of what the kernel before may have written: they see it (no .nc) and stay behind the wait for it, since `q` comes from behind it (behind_wait),
-// but are as free as __ldg otherwise: no store of the kernels that use them reaches the vectors.
-__device__ __forceinline__ const void* behind_wait(const void* q) {
-    asm volatile("" : "+l"(q));
-    return q;
-}
-__device__ __forceinline__ uint4 ld_vector_16(const void* q) {
-    uint4 v;
-    asm("ld.global.v4.u32 {%0,%1,%2,%3}, [%4];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "l"(q));
-    return v;
-}
-__device__ __forceinline__ float ld_vector_4(const void* q) {
-    float v;
-    asm("ld.global.f32 %0, [%1];" : "=f"(v) : "l"(q));
-    return v;
-}
-__device__ __forceinline__ uint32_t ld_vector_2(const void* q) {
-    uint16_t v;
-    asm("ld.global.u16 %0, [%1];" : "=h"(v) : "l"(q));
-    return v;
-}
 // eight entries of a parameter vector at channel c (absent: `none`)
 __device__ __forceinline__ void load_param(const NormVec& p, int64_t batch, int c, int count, bool vec, int step, float none, float (&v)[8]) {
     if (!p.ptr) {

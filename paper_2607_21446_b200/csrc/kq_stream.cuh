@@ -108,8 +108,8 @@ quantize_stream(const uint4* __restrict__ X, int64_t n_quads, int blocks_per_row
             if (pos >= quads_per_row) pos -= quads_per_row;
             if (MODE == MODE_SCALE) {
                 if (live) {
-                    const float4* sp = reinterpret_cast<const float4*>(chan_scale + j * kBlock + quad * 8);
-                    const float4 s0 = __ldg(sp), s1 = __ldg(sp + 1);
+                    const float4* sp = static_cast<const float4*>(behind_wait(chan_scale + j * kBlock + quad * 8));
+                    const float4 s0 = as_float4(ld_vector_16(sp)), s1 = as_float4(ld_vector_16(sp + 1));
                     y[0] *= s0.x; y[1] *= s0.y; y[2] *= s0.z; y[3] *= s0.w;
                     y[4] *= s1.x; y[5] *= s1.y; y[6] *= s1.z; y[7] *= s1.w;
                 }
@@ -165,9 +165,9 @@ scale_quantize_rows(const uint4* __restrict__ X, int64_t tokens, int quads_per_r
     const int64_t r0 = t / quads_per_row;
     const int quad = threadIdx.x & 3;
     const uint32_t qmask = 0xFu << (threadIdx.x & 28);
-    const float4* sp = reinterpret_cast<const float4*>(chan_scale + (int64_t)p * 8);
-    const float4 s0 = __ldg(sp), s1 = __ldg(sp + 1);      // the scale vector is immutable input
     asm volatile("griddepcontrol.wait;" ::: "memory");
+    const float4* sp = static_cast<const float4*>(behind_wait(chan_scale + (int64_t)p * 8));        // (the vector may come from the kernel before)
+    const float4 s0 = as_float4(ld_vector_16(sp)), s1 = as_float4(ld_vector_16(sp + 1));
     if (r0 >= R) return;                                  // leftover threads of the last partial row group
     for (int64_t r = r0; r < tokens; r += R * kStreamUnroll) {
         uint4 raw[kStreamUnroll];

@@ -28,3 +28,10 @@ def test_kernels_of_a_block_read_with_plain_loads(name):
 @pytest.mark.parametrize("name", ["kq_gemm_fp4.cuh", "kq_gemm_fp4_pair.cuh"])
 def test_products_read_the_branch_they_add_with_plain_loads(name):
     assert not re.search(r"__ldg\(ap", code(name))
+
+
+def test_scale_quantizers_read_their_vector_behind_the_wait():
+    body = code("kq_stream.cuh")
+    assert not re.search(r"__ldg\(sp", body)
+    rows = body[body.index("scale_quantize_rows(") :]
+    assert rows.index("griddepcontrol.wait") < rows.index("chan_scale", rows.index("{"))

@@ -100,3 +100,20 @@ def test_norm_vectors_from_the_product_before(rows, d, dtype):
         return h, n, back["dx"], back["dy"], back["dscale"]
 
     same_in_one_graph(8, link)
+
+
+@pytest.mark.parametrize("tokens,d", [(300, 1152), (2, 4608), (1, 40960)])
+@pytest.mark.parametrize("staged", [True, False])
+def test_scale_vector_from_the_product_before(tokens, d, staged):
+    g = gen(d)
+    w = weight(d, 256, g)
+    t = torch.randn(8, 1, 256, device="cuda", generator=g).bfloat16()
+    x = torch.randn(tokens, d, device="cuda", generator=g).bfloat16()
+    s = torch.empty(1, d, device="cuda")
+    tuning = None if staged else kb.Tuning(compare_staged=0)
+
+    def link(i):
+        kb.kroquant_linear_w4a16(t[i], *w, out=s)
+        return kb.kroquant_scale_quantize(x, s.view(-1), tuning=tuning)
+
+    same_in_one_graph(8, link)
