@@ -371,7 +371,7 @@ __global__ void __launch_bounds__(kAttnThreads, (AttnShape<FMT, D, NQ>::kPerSm))
 #pragma unroll
         for (int i = 0; i < L::kStages - 1; ++i) issue(i);
         if constexpr (L::kCodes) {
-            int e[NT], most = -100;                                      // exponent of the largest value of query 8 nt + g (0 and subnormal ones: -100), of all
+            int e[NT], most = -100, least = 128;                         // exponent of the largest value of query 8 nt + g (-100 at least), of all queries'
 #pragma unroll
             for (int nt = 0; nt < NT; ++nt) {
                 uint32_t amax = 0;                                       // of the magnitude bits
@@ -384,11 +384,10 @@ __global__ void __launch_bounds__(kAttnThreads, (AttnShape<FMT, D, NQ>::kPerSm))
                 const float top = p.q_f16 ? __half2float(__ushort_as_half((unsigned short)amax)) : __uint_as_float(amax << 16);
                 e[nt] = max((int)(__float_as_uint(top) >> 23) - 127, -100);              // (infinity and NaN: 128)
                 most = max(most, e[nt]);
+                if (amax) least = min(least, e[nt]);                     // (queries that are zero, or that there are none of, go with any power)
             }
             most = __reduce_max_sync(0xFFFFFFFFu, most);
-#pragma unroll
-            for (int nt = 0; nt < NT; ++nt) apart |= most - e[nt] > kQueryRange;
-            apart = __any_sync(0xFFFFFFFFu, apart);
+            apart = most - __reduce_min_sync(0xFFFFFFFFu, least) > kQueryRange;
 #pragma unroll
             for (int nt = 0; nt < NT; ++nt) {
                 if (!apart) e[nt] = most;
