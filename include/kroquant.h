@@ -517,8 +517,12 @@ kq_status_t kroquant_cache_read(const kq_cache_t *cache, const kq_cache_rows_t *
  * q and the cache.
  * q_heads a multiple of the cache's heads; lengths: DEVICE int32, read on the device, clamped to [0, table_width * page_size], which is
  * at most 2^30.
- * Products are formed on the tensor cores from the cache's own values (q as it is; the weights w to 11 bits or more), sums and
- * softmax statistics are 32-bit.  The work is split over the length and joined in a fixed order: same bits every time.
+ * Products are formed on the tensor cores from the cache's own values, sums and softmax statistics are 32-bit.  What counts with fewer digits:
+ *   weights: 11 bits with MXFP8 and MXFP4, 16 and 22 with bf16 and fp16 (two terms); each w_t v_t also to 2^-34 of the largest |v| that the row
+ *     sees at best (not bf16), so that positions whose values are 2^12 below that lose the digits of weights from 2^-11 on;
+ *   MXFP8 and MXFP4: a block of 32 channels whose scale is 2^-21 (MXFP8) or 2^-28 (MXFP4) of the largest at its position, or less, counts as zero
+ *     (kroquant_cache_read returns it); values of q below 2^-21 of the largest of their query head.  Heads do not touch one another.
+ * A head whose scores leave float's range gives NaN.  The work is split over the length and joined in a fixed order: same bits every time.
  * scratch: DEVICE, 16-byte aligned, kroquant_cache_attention_scratch_bytes(...) bytes (0: may be NULL), contents irrelevant; two
  * calls that may overlap need one each. */
 typedef struct kq_attention_args {

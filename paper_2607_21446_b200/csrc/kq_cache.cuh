@@ -10,8 +10,9 @@
 // by latency.  A thread keeps a place within a row, 16 channels of one head, and walks the rows of its CTA, so that what it computes
 // per 16 channels is two addresses and the code; the two threads of a block of 32 channels exchange its largest magnitude by one
 // shuffle.  The cell of a row (a search of offsets and one table entry) is found once per CTA and row.
-// Measured: 2823 new rows into and 32823 rows out of an MXFP4 cache of 8 heads x 128 39.6 us, of which the read takes 30: 134 MB of writes at
-// 4.4 TB/s, the rate at which this device is filled.
+// Measured: 2823 new rows into and 32823 rows out of an MXFP4 cache of 8 heads x 128 39.8 us, of which the read takes 30: 134 MB of writes at
+// 4.4 TB/s, the rate at which this device is filled.  The write waits for offsets, starts, table and a barrier one after another before it asks for
+// its first row: 9 us from memory (2.2 of bytes), 5.5 with rows in L2 (MXFP8 5.6, 16 bits 8.4).
 #pragma once
 #include "kq_mma16.cuh"
 #include "kq_rotary.cuh"

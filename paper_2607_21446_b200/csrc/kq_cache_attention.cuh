@@ -2,15 +2,17 @@
 //     out[s][h] = sum_t w_t v_t / sum_t w_t,    w_t = exp(scale q[s][h] . k_t - m),   m the largest score so far
 // One pass over the positions with a running maximum and sum: when m grows, the sum and the accumulated values are scaled down.
 //
-// The cache is read once, by 4 warps of a CTA that each take every fourth step of 16 (16-bit) or 32 positions, with rings of their own
+// The cache is read once (for each 16 query heads of a cache head, where it has more), by 4 warps of a CTA that each take every fourth step of 16 (16-bit) or 32 positions, with rings of their own
 // in shared memory (cp.async; no barrier between the warps until the end of a segment).  A warp multiplies with mma.sync, positions
 // as the 16 rows of the product and the query heads of one cache head as its 8 (or twice 8) columns:
 //     S^T [position][query] = K Q^T,     O^T [channel][query] += V^T P^T.
-// So nothing is padded to 128 rows, and codes go from shared memory through the converter into the operand registers, never back: an
-// operand for tcgen05 would have to be written to shared memory again.
-// Measured (us, and the time of the bytes at the copy rate): one sequence of 300 in 16 bits 7.1 (0.2), 24 of 341 to 8192 in MXFP8 43 (30), one of
-// 131071 in MXFP4 44 (22), 5 with a window of 4096 in 16 bits, 20 heads of 112, 42 (28; 32 with the channels that fill the rows up).  The formats of codes
-// are bound by instructions (some 750 per 32 positions of a head; converter, extraction of its byte and scale are half of them), 16 bits by memory.
+// So nothing is padded to 128 rows, and codes go from shared memory through the converter into the operand registers, never back.  For V^T P^T
+// tcgen05 would want V written to shared memory again in 16 bits, as its scale blocks do not run along the positions; keys in E4M3 could be a
+// block-scaled operand as they lie (not built).
+// Measured (us, and the time of the bytes at the copy rate): one sequence of 300 in 16 bits 7.1 (0.2; 10.0 under a table with room for 8192, whose
+// items may be split), 24 of 341 to 8192 in MXFP8 43.5 (30), one of 131071 in MXFP4 44 (22), 5 with a window of 4096 in 16 bits, 20 heads of 112, 41 (28;
+// 32 with the channels that fill the rows up); 8 of 8192 in MXFP8 with 8, 12 and 16 query heads a cache head 35, 46, 46 (21).  The formats of codes are
+// bound by instructions (some 750 per 32 positions of a head; converter, extraction of its byte and scale are nearly half of them), 16 bits by memory.
 //
 // Operand order.  Any order of channels serves K Q^T, and any order of positions P^T as long as both products use the same, so that a
 // lane takes what lies together: of K, with j = lane % 4, whole 16-byte chunks of the rows of positions lane / 4 and lane / 4 + 8; of V,
@@ -23,9 +25,10 @@
 // running maximum that rescales the accumulator as m does).  Code times 2^(S - S_t + kLift) has at most 4 significant bits and is exact in
 // fp16; a block whose scale is 2^-28 (E2M1) or 2^-21 (E4M3) of its position's largest, or less, counts as zero.  The queries of a CTA are
 // fp16 times one power of two, or one each where their sizes differ much, so that none costs another its digits: exact for both 16-bit types
-// down to values 2^-21 of the query's largest.  P is rounded to fp16 (11 bits; a weight
-// below 2^-23 of the largest keeps fewer, which is 2^-34 of the largest value at most), with 16-bit values, where memory leaves the time, to
-// two terms of their type (16 and 22 bits).
+// down to values 2^-21 of the query's largest.  P is rounded to fp16: 11 bits, down to 2^-23 of the largest weight where a position's S_t is R, 2^(R - S_t)
+// above that where it is less; what is lost below is 2^-34 of the largest value at most.  With 16-bit values, where memory leaves the time, P is
+// two terms of their type (16 and 22 bits).  Two terms with codes as well: 3 to 8 % slower (131071 in MXFP4 44 -> 47), the error against 64 bits
+// 1.7e-4 -> 3e-7 in float32, and no other in 16 bits (1.7e-3 in bf16 either way, by out's own rounding).
 //
 // Work.  Tiles (4 steps) of all (sequence, head) items are laid end to end, each item led by kLead tiles' worth of nothing for what
 // beginning and ending it costs, and every CTA takes an equal run: ragged batches balance, one long sequence fills the GPU.  An

@@ -17,9 +17,10 @@
 // largest of the row's four scale bytes: at most 2 significant bits, exact; a block whose scale is 2^-28 of S0's, or less, counts as zero.
 // 2^(S0 - 127 - 13) and x's power multiply the fp32 sum of 128 channels.
 //
-// Measured (us, and the time of the bytes at the copy rate): one row 1152 -> 6912 5.5 (0.7), 5 rows 4096 -> 2 x 5632 gated 12.1 (3.8), 16 rows 12288 -> 4608
-// 19.3 (4.7).  Of the last, some 5 us go by until x is converted (mostly latencies), 6 with 6 or 7 units for each warp, the rest waiting for the cluster's
-// last CTA, its sums and the epilogue.
+// Measured (us, and the time of the bytes at the copy rate): one row 1152 -> 6912 5.5 (0.7), 5 rows 4096 -> 2 x 5632 gated 12.2 (3.8), 16 rows 12288 -> 4608
+// 19.3, with a residual 20.1 (4.7).  The last runs as 18 clusters of six CTAs of two tiles, 8 units of 128 channels for each warp: some 7 us are theirs, the
+// others go by until x is converted (mostly latencies) and waiting for the cluster's last CTA, its sums and the epilogue.  Runs of more than 16 rows
+// read and decode the weight once for each 16: 33 and 64 rows 4608 -> 12288 37 and 69 (4.8), 16 rows 21.
 #pragma once
 #include "kq_linear.cuh"
 #include "kq_mma16.cuh"

@@ -18,7 +18,7 @@
 
 namespace kq {
 
-struct FastDiv {                         // n / d for n < 2^31
+struct FastDiv {                         // n / d for n < 2^31, by Granlund and Montgomery's multiplication (1994)
     uint32_t d, mul, shift;
     __device__ __forceinline__ uint32_t div(uint32_t n) const { return (__umulhi(n, mul) + n) >> shift; }
 };

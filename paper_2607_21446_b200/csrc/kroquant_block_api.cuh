@@ -202,7 +202,7 @@ struct W4A16Launch {
     int tiles, runs, splits;
     // K goes over as many CTAs of a cluster as run at once, three units each at least.  CTAs of one tile, 12288 -> 4608 with 16 rows, 1, 2, 3, 7, 8 of
     // them: 68, 37, 29, 21.3, 43 us (36 clusters of eight do not fit at once); 5 rows of 4096 -> 2 x 5632, 2 to 4: 15.5, 12.2, 17; one row of
-    // 1152 -> 6912, 1 to 4: 6.5, 6.3, 5.5, 5.6.  Sizes other than 2, 4 and 8 leave gaps among those that still run: they keep a fortieth free: 55 clusters of
+    // 1152 -> 6912, 1 to 4: 6.5, 6.3, 5.5, 5.6.  Sizes other than 2, 4 and 8 leave gaps among those that still run: they keep a fortieth free (by one shape): 55 clusters of
     // 56 that fit, one row 4096 -> 7000, 13.2 us (4 CTAs: 9.0).
     kq_status_t plan(const kq::W4A16Problem& p) {
         static DeviceOnce attr_done;
