@@ -492,7 +492,7 @@ typedef struct kq_cache {
  * buffers overlap may only be read.  Rows that a call writes do not lie in the places it writes them to.
  * k, v: DEVICE, row i of head h at i * row stride + h * head stride (elements), contiguous channels, any alignment of the type.
  * write takes bf16 or fp16 (16BIT: the cache's dtype) and finite values; read gives any of the three types, into k and v that overlap neither
- * one another nor the cache. */
+ * one another nor the places it reads. */
 typedef struct kq_cache_rows {
     int64_t rows;
     int sequences;

@@ -1278,7 +1278,8 @@ def kroquant_cache_write(cache: KVCache, k: torch.Tensor, v: torch.Tensor, table
     cache: its dtype), any strides with contiguous channels.  table int32 [sequences, n]: the pages of each sequence in order.
     offsets int32 [sequences + 1]: rows offsets[s] .. offsets[s + 1] - 1 belong to sequence s (None: one row per sequence); starts
     int32 [sequences]: the position of each sequence's first row (None: 0).  All three are read on the device; a row whose
-    position lies before 0 or beyond the table, or whose table entry is no page (-1, say), is left out."""
+    position lies before 0 or beyond the table, or whose table entry is no page (-1, say), is left out.  No place may be written twice by
+    one call (a page that two sequences have, or one has twice)."""
     where = _table(cache, table)
     _heads_last(k, "k", 3, X_DTYPES)
     _heads_last(v, "v", 3, X_DTYPES)
@@ -1297,8 +1298,8 @@ def kroquant_cache_read(cache: KVCache, table: torch.Tensor, rows: int, *, offse
                         starts: Optional[torch.Tensor] = None, dtype=None, out=None, stream=None):
     """The inverse of :func:`kroquant_cache_write`: -> (k, v) [rows, heads, head_dim] in `dtype` (default: the cache's; float32 is allowed), the
     values that the cache holds at the places of the rows.  Rows without a place are zeros; rows outside the sequences
-    (before offsets[0], from offsets[-1] on) are left as they are.  out: a pair of tensors to write to, which overlap neither one another
-    nor the cache."""
+    (before offsets[0], from offsets[-1] on) are left as they are.  out: a pair of tensors to write to, which do not overlap (pages of a 16bit
+    cache among them, where the call reads others: a copy of pages)."""
     where = _table(cache, table)
     shape = (rows, cache.heads, cache.head_dim)
     if out is None:
@@ -1318,8 +1319,8 @@ def kroquant_cache_read(cache: KVCache, table: torch.Tensor, rows: int, *, offse
             _heads_last(t, "out", 3)
             if t.shape != shape or t.dtype is not k.dtype or dtype not in (None, t.dtype) or not _apart(t):
                 raise ValueError("out must be two tensors [rows, heads, head_dim] of one dtype with elements of their own")
-        if _meet(k, v) or any(t is not None and (_meet(k, t) or _meet(v, t)) for t in cache._buffers):
-            raise ValueError("the two tensors of out must overlap neither one another nor the cache")
+        if _meet(k, v):
+            raise ValueError("the two tensors of out must not overlap")
     if offsets is None and rows != where[0]:
         raise ValueError("without offsets there is one row per sequence")
     _cache_rows("kroquant_cache_read", cache, k, v, rows, where, offsets, starts, stream)

@@ -84,15 +84,15 @@ def cache_of(form, dtype=torch.bfloat16):
 
 
 @pytest.mark.parametrize("form", ["16bit", "mxfp8"])
-def test_cache_read_refuses_outputs_on_one_another_or_on_the_cache(here, form):
+def test_cache_read_refuses_outputs_on_one_another(here, form):
     cache, table = cache_of(form)
     room = torch.zeros(3, 6, 64, dtype=torch.bfloat16)
     k, v = room[:, :2], room[:, 2:4]
     for out in ((k, k), (k, room[:, 1:3]), (room[:, :4:2], room[:, 2:4]), (k, k.view(torch.float16).view(torch.bfloat16))):
         refused(kb.kroquant_cache_read, cache, table, 3, out=out, stream=0)
-    inside = cache.k.view(torch.bfloat16).view(-1)[: 3 * 2 * 64].view(3, 2, 64)
-    for out in ((inside, v), (k, inside)):
-        refused(kb.kroquant_cache_read, cache, table, 3, out=out, stream=0)
+    if form == "16bit":                                                  # pages read into other pages
+        offsets = torch.tensor([0, 8], dtype=torch.int32)
+        passes(kb.kroquant_cache_read, cache, table[:1], 8, out=(cache.k[3].transpose(0, 1), cache.v[3].transpose(0, 1)), offsets=offsets, stream=0)
     passes(kb.kroquant_cache_read, cache, table, 3, out=(k, v), stream=0)
     passes(kb.kroquant_cache_read, cache, table, 3, out=(room[:, ::2][:, :2], room[:, 1::2][:, :2]), stream=0)
 
